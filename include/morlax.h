@@ -259,6 +259,38 @@ int64_t morlax_hypervolume_workspace_bytes(int32_t n, int32_t K);
 int morlax_pareto_hypervolume(const float* J, const float* ref, int32_t n, int32_t K, uint8_t* front,
                               double* hv, void* ws, int64_t ws_bytes, void* stream);
 
+/* ---- Policies for any mix of preferences, with memory ------------------------------------------------------
+ * Entry points without a context: a struct of dimensions and strides, passed by pointer, takes its place.  What the conventions at
+ * the top say of ownership, streams, workspaces and errors holds here too.  Tensors whose strides are arguments (x, y, z, dt and
+ * their gradients) need the alignment of one element only; kernels use 16-byte accesses where pointers and strides allow them.  All
+ * other pointers are 16-byte aligned.  dtype: 0 fp32, 1 bf16.  Sums and states are fp32.  A call with no rows (T, N or rows zero)
+ * launches nothing that reads them: gradients of parameters are then zero.
+ *
+ * A shared projection with a low-rank adapter per preference (Sec. III-B's W_l(p) = W0_l + A_l(p) B_l(p), with no W_l(p) formed):
+ * row m of x goes through the adapter that index[m] names, rows in any order and any number to an adapter.  An index outside
+ * [0, n_adapters) is a row without one.
+ *   y[m] = W0 x[m] + bias + A[p] (B[p] x[m]),  p = index[m]
+ *   x [rows, d_in] (row stride ld_x elements), w0 [d_out, d_in], bias [d_out] fp32 or NULL, A [n_adapters, d_out, rank],
+ *   B [n_adapters, rank, d_in], index [rows] int32, y [rows, d_out] (row stride ld_y); x, w0, A, B, y of the given type.
+ * B[p] x[m] is kept in fp32.  The result of a row depends on its own x and its own adapter alone.
+ * Limits: 1 <= rank <= 32, 1 <= d_in, d_out <= 65536, 1 <= n_adapters <= 2^20. */
+typedef struct {
+    int32_t rows, d_in, d_out, rank, n_adapters;
+    int32_t dtype;
+    int64_t ld_x, ld_y;
+} morlax_adapter_dims;
+
+/* bytes of scratch of morlax_adapter_fwd (backward 0) and morlax_adapter_bwd (1); -1 for dimensions that are not served */
+int64_t morlax_adapter_workspace_bytes(const morlax_adapter_dims* dims, int32_t backward);
+int morlax_adapter_fwd(const morlax_adapter_dims* dims, const void* x, const void* w0, const float* bias, const void* A,
+                       const void* B, const int32_t* index, void* y, void* ws, int64_t ws_bytes, void* stream);
+/* Reverse mode: dy [rows, d_out] (stride ld_y) -> dx [rows, d_in] (stride ld_x, dtype), dw0 [d_out, d_in], dbias [d_out],
+ * dA [n_adapters, d_out, rank], dB [n_adapters, rank, d_in] (fp32, overwritten, zero for an adapter without rows).  Any of
+ * the outputs may be NULL: what only it needs is left out.  Sums in a fixed order: results repeat bit for bit. */
+int morlax_adapter_bwd(const morlax_adapter_dims* dims, const void* x, const void* w0, const void* A, const void* B,
+                       const int32_t* index, const void* dy, void* dx, float* dw0, float* dbias, float* dA, float* dB, void* ws,
+                       int64_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -25,6 +25,15 @@ class Rows(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("t0", "t_cnt", "j0", "j_cnt")]
 
 
+class AdapterDims(C.Structure):
+    """morlax_adapter_dims: `adapters` is n_adapters; row strides in elements, those of contiguous rows where they are not given."""
+    _fields_ = [(n, C.c_int32) for n in ("rows", "d_in", "d_out", "rank", "n_adapters", "dtype")] + \
+               [(n, C.c_int64) for n in ("ld_x", "ld_y")]
+
+    def __init__(self, rows, d_in, d_out, rank, adapters, dtype, ld_x=None, ld_y=None):
+        super().__init__(rows, d_in, d_out, rank, adapters, dtype, d_in if ld_x is None else ld_x, d_out if ld_y is None else ld_y)
+
+
 class MorlaxError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__(f"morlax error {code}: {msg}")
@@ -41,7 +50,7 @@ EXPORTS = ("morlax_create", "morlax_destroy", "morlax_last_error", "morlax_hpara
            "morlax_sample_preferences", "morlax_scalarize_normalized", "morlax_ppo_loss_grad",
            "morlax_ppo_loss_grad_static", "morlax_eval_returns",
            "morlax_hypervolume_workspace_bytes", "morlax_pareto_hypervolume", "morlax_profile_begin",
-           "morlax_profile_end")
+           "morlax_profile_end", "morlax_adapter_workspace_bytes", "morlax_adapter_fwd", "morlax_adapter_bwd")
 
 GEMM_KINDS = ("fwd_first", "fwd_hidden", "dx_hidden", "dw_hidden", "dw_first", "fwd_fused")
 
@@ -94,6 +103,13 @@ def load():
     lib.morlax_hypervolume_workspace_bytes.restype = i64
     lib.morlax_pareto_hypervolume.argtypes = [vp, vp, i32, i32, vp, vp, vp, i64, vp]
     lib.morlax_pareto_hypervolume.restype = C.c_int
+    dp = C.POINTER(AdapterDims)
+    lib.morlax_adapter_workspace_bytes.argtypes = [dp, i32]
+    lib.morlax_adapter_workspace_bytes.restype = i64
+    lib.morlax_adapter_fwd.argtypes = [dp] + [vp] * 8 + [i64, vp]
+    lib.morlax_adapter_bwd.argtypes = [dp] + [vp] * 12 + [i64, vp]
+    for name in ("morlax_adapter_fwd", "morlax_adapter_bwd"):
+        getattr(lib, name).restype = C.c_int
     lib.morlax_profile_begin.argtypes = [vp]
     lib.morlax_profile_begin.restype = C.c_int
     lib.morlax_profile_end.argtypes = [vp, C.POINTER(C.c_double), C.POINTER(i64), C.POINTER(C.c_double)]
@@ -301,3 +317,33 @@ def pareto_hypervolume(J, ref, n, K, front, hv, ws, stream=None):
                                        _nbytes(ws), stream if stream is not None else _stream())
     if rc != OK:
         raise MorlaxError(rc, lib.morlax_last_error().decode())
+
+
+def _call(fn, *args):
+    rc = fn(*args)
+    if rc != OK:
+        raise MorlaxError(rc, _lib.morlax_last_error().decode())
+
+
+def _size(n):
+    """What a workspace query answers; dimensions that are not served raise."""
+    if n < 0:
+        raise MorlaxError(ERR_SHAPE, _lib.morlax_last_error().decode())
+    return int(n)
+
+
+def adapter_workspace_bytes(dims, backward=False):
+    """Bytes of device scratch that adapter_fwd (adapter_bwd) needs for these dimensions."""
+    return _size(load().morlax_adapter_workspace_bytes(C.byref(dims), int(bool(backward))))
+
+
+def adapter_fwd(dims, x, w0, bias, A, B, index, y, ws, stream=None):
+    """morlax_adapter_fwd: y[m] = W0 x[m] + bias + A[p] (B[p] x[m]) with p = index[m]."""
+    _call(load().morlax_adapter_fwd, C.byref(dims), _ptr(x), _ptr(w0), _ptr(bias), _ptr(A), _ptr(B), _ptr(index), _ptr(y), _ptr(ws),
+          _nbytes(ws), stream if stream is not None else _stream())
+
+
+def adapter_bwd(dims, x, w0, A, B, index, dy, dx, dw0, dbias, dA, dB, ws, stream=None):
+    """morlax_adapter_bwd: gradients of adapter_fwd; outputs that are None are left out."""
+    _call(load().morlax_adapter_bwd, C.byref(dims), _ptr(x), _ptr(w0), _ptr(A), _ptr(B), _ptr(index), _ptr(dy), _ptr(dx), _ptr(dw0),
+          _ptr(dbias), _ptr(dA), _ptr(dB), _ptr(ws), _nbytes(ws), stream if stream is not None else _stream())

@@ -1,0 +1,717 @@
+// A shared projection with a low-rank adapter per preference, every row naming its own (the factors of Sec. III-B's
+// W_l(p) = W0_l + A_l(p) B_l(p), applied without ever forming W_l(p)):
+//
+//   forward    u_m = B_p x_m,   y_m = W0 x_m + bias + A_p u_m                     p = index[m]
+//   backward   v_m = A_p^T dy_m,  dx_m = W0^T dy_m + B_p^T v_m
+//              dW0 = sum_m dy_m x_m^T,  dbias = sum_m dy_m,
+//              dA_p = sum_{m of p} dy_m u_m^T,  dB_p = sum_{m of p} v_m x_m^T
+//
+// An index outside [0, n_adapters) is a row without an adapter.  u and v are fp32.  Rows may come in any order: the products
+// with W0 take rows as they lie and add the adapters' part block by block of 32 rows, once for every adapter that a block
+// holds; the gradients of the factors walk the rows sorted by adapter (k_ad_plan), pieces of at most AD_PIECE rows each, and
+// what a piece leaves is added in order, so results repeat bit for bit.
+#include "mlp_device.h"
+
+typedef short short4_t __attribute__((ext_vector_type(4)));
+
+#define AD_PIECE 256    // sorted rows of a factor-gradient workgroup
+#define AD_MAX_RANK 32
+
+struct AdArgs {
+    const void *x, *w0, *A, *B, *dy;
+    const float* bias;
+    const int32_t* index;
+    void *y, *dx;
+    float *dw0, *dbias, *dA, *dB;
+    int64_t ld_x, ld_y;
+    int M, I, O, r, P;
+    // scratch
+    float *u, *v;        // [M][rp]
+    int32_t *seg, *perm; // [P + 2], [M]
+    float *pw, *pA, *pB, *pb;  // partial sums: [split][O][I], [piece][O][r], [piece][r][I], [piece][O]
+    int rp, split, kchunk, pieces;
+};
+
+// sixteen consecutive values of a matrix row, of which the first `avail` exist (the others are zero): vector loads where VEC
+// says that the row's address allows them
+template <typename T>
+__device__ inline void load16(const T* p, int avail, bool vec, uint4 (&v)[sizeof(T)]) {
+    constexpr int VE = 16 / (int)sizeof(T);
+#pragma unroll
+    for (int q = 0; q < (int)sizeof(T); ++q) {
+        v[q] = make_uint4(0, 0, 0, 0);
+        if (vec && avail >= (q + 1) * VE) {
+            v[q] = *reinterpret_cast<const uint4*>(p + q * VE);
+        } else if (avail > q * VE) {
+            T e[VE];
+#pragma unroll
+            for (int i = 0; i < VE; ++i) e[i] = q * VE + i < avail ? p[q * VE + i] : (T)0.f;
+            v[q] = *reinterpret_cast<uint4*>(e);
+        }
+    }
+}
+// the bf16 parts of them: one (the values) or three (split3), 32 bytes each
+template <bool BOUNDED = false>
+__device__ inline void parts16(const uint4 (&v)[2], uint4 (&lo)[1], uint4 (&hi)[1]) { lo[0] = v[0]; hi[0] = v[1]; }
+template <bool BOUNDED = false>
+__device__ inline void parts16(const uint4 (&v)[4], uint4 (&lo)[3], uint4 (&hi)[3]) {
+    uint2 p[4][3];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) split3<BOUNDED>(v[q], p[q]);
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+        lo[q] = make_uint4(p[0][q].x, p[0][q].y, p[1][q].x, p[1][q].y);
+        hi[q] = make_uint4(p[2][q].x, p[2][q].y, p[3][q].x, p[3][q].y);
+    }
+}
+
+// One operand of a tiled product: `rows` x `kdim`, element (row, k) at base[row * ld + k] (KC, contraction contiguous) or
+// base[k * ld + row] (KS).  A stage is 128 rows x 32 k, in LDS as bf16 planes: KC [row][32 k], 80 bytes a row (the sixteen rows of
+// a fragment read start in different groups of four banks); KS [k][128 rows], 320 bytes a k, read transposed.
+enum { KC = 0, KS = 1 };
+template <typename T, int KIND>
+struct AdOperand {
+    static constexpr int NP = sizeof(T) == 4 ? 3 : 1;
+    static constexpr int PLANE = 10240;
+    const T* base;
+    int64_t ld;
+    int rows, kdim;
+    bool vec;
+    uint4 reg[sizeof(T)];
+
+    __device__ inline void init(const void* b, int64_t l, int r, int k) {
+        base = reinterpret_cast<const T*>(b);
+        ld = l; rows = r; kdim = k;
+        vec = ((reinterpret_cast<uintptr_t>(b) | (uintptr_t)(l * (int64_t)sizeof(T))) & 15) == 0;
+    }
+    __device__ inline float elem(int row, int k) const {
+        if (row >= rows || k >= kdim) return 0.f;
+        return to_f(base[KIND == KC ? (int64_t)row * ld + k : (int64_t)k * ld + row]);
+    }
+    __device__ inline void fetch(int t0, int k0) {
+        const int tid = threadIdx.x;
+        if (KIND == KC) {
+            const int row = t0 + tid / 2, k = k0 + 16 * (tid % 2);
+            load16(base + (int64_t)row * ld + k, row < rows ? kdim - k : 0, vec, reg);
+        } else {
+            const int k = k0 + tid / 8, row = t0 + 16 * (tid % 8);
+            load16(base + (int64_t)k * ld + row, k < kdim ? rows - row : 0, vec, reg);
+        }
+    }
+    __device__ inline void put(unsigned char* lds) const {
+        const int tid = threadIdx.x;
+        uint4 lo[NP], hi[NP];
+        parts16(reg, lo, hi);
+        unsigned char* d = lds + (KIND == KC ? (tid / 2) * 80 + (tid % 2) * 32 : (tid / 8) * 320 + (tid % 8) * 32);
+#pragma unroll
+        for (int q = 0; q < NP; ++q) {
+            *reinterpret_cast<uint4*>(d + q * PLANE) = lo[q];
+            *reinterpret_cast<uint4*>(d + q * PLANE + 16) = hi[q];
+        }
+    }
+    // the lane's operand of the 32-row block at `row`, contraction indices 16 ks + 8 lg + [0, 8)
+    __device__ static inline void frag(const unsigned char* lds, int row, int ks, uint4 (&f)[NP]) {
+        const int lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5;
+#pragma unroll
+        for (int q = 0; q < NP; ++q) {
+            if (KIND == KC) {
+                f[q] = *reinterpret_cast<const uint4*>(lds + q * PLANE + (row + lr) * 80 + ks * 32 + lg * 16);
+            } else {
+                typedef __attribute__((address_space(3))) short4_t lds_s4;
+                const int a = lane & 15, q0 = (lane >> 4) & 1, e = a >> 2, c = a & 3;
+                const unsigned char* s = lds + q * PLANE + (16 * ks + 8 * lg + e) * 320 + (row + 16 * q0 + 4 * c) * 2;
+                const uint2 u0 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)s));
+                const uint2 u1 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(s + 4 * 320)));
+                f[q] = make_uint4(u0.x, u0.y, u1.x, u1.y);
+            }
+        }
+    }
+};
+
+// acc += a b^T for operands of one part, or of three each (six products, the five small ones into `low`)
+__device__ inline void mma_parts(const uint4 (&a)[1], const uint4 (&b)[1], float16_t& acc, float16_t&) { Mma32<bf16_t>::run(a[0], b[0], acc); }
+__device__ inline void mma_parts(const uint4 (&a)[3], const uint4 (&b)[3], float16_t& acc, float16_t& low) {
+#pragma unroll
+    for (int t = 0; t < 6; ++t) split_mma(t, a, b, acc, low);
+}
+__device__ inline float16_t zero16() {
+    float16_t z;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) z[e] = 0.f;
+    return z;
+}
+
+// Factor (n, j) of adapter p for output column n: forward A_p [O][r], backward B_p [r][I].
+template <typename T, bool BWD>
+struct AdFactor {
+    const T* base;
+    int N, r;
+    __device__ inline const T* at(int p, int n, int j) const {
+        return base + (int64_t)p * N * r + (BWD ? (int64_t)j * N + n : (int64_t)n * r + j);
+    }
+    __device__ inline T get(int p, int n, int j) const { return n < N && j < r ? *at(p, n, j) : (T)0.f; }
+    // eight j of column n
+    __device__ inline uint4 frag(int p, int n, int j0, bool vec) const {
+        if (!BWD && vec && n < N && j0 + 8 <= r) return *reinterpret_cast<const uint4*>(at(p, n, j0));
+        T e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = get(p, n, j0 + i);
+        return *reinterpret_cast<uint4*>(e);
+    }
+};
+
+// The adapters' part of a 32 x (32 NB) block of outputs, a lane holding row m (accumulator: columns n0 + 8 (e / 4) + 4 lg + e % 4):
+// one product of the block per adapter among its rows.  Where they are several, a product goes only to its own rows' lanes: an
+// undefined factor of one adapter stays out of the others' rows.  bf16: u as two bf16 parts (what is left out is 2^-17 of it; rounding
+// it to one would double the error of y); fp32 on the fp32 instructions.
+template <typename T, bool BWD, int NB>
+__device__ inline void ad_expand(const AdFactor<T, BWD>& F, const float* u, int rp, const int32_t* index, int P, int M, int m0, int n0,
+                                 float16_t* acc) {
+    const int lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5, m = m0 + lr;
+    int p = m < M ? index[m] : -1;
+    if (p < 0 || p >= P) p = -1;
+    uint64_t todo = __ballot(p >= 0) & 0xffffffffull;
+    if (!todo) return;
+    const bool vec = (F.r & 7) == 0;
+    const float* um = u + (int64_t)(m < M ? m : M - 1) * rp;
+    uint4 hi[2] = {}, lo[2] = {};
+    if (sizeof(T) == 2)
+        for (int s = 0; s < rp / 16; ++s) {
+            const float4 a = *reinterpret_cast<const float4*>(um + 16 * s + 8 * lg), b = *reinterpret_cast<const float4*>(um + 16 * s + 8 * lg + 4);
+            float t[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}, l[8];
+            hi[s] = pack_chunk<bf16_t>(t);
+            const uint32_t w[4] = {hi[s].x, hi[s].y, hi[s].z, hi[s].w};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {  // (an infinite value has no second part)
+                const float d = t[i] - __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+                l[i] = __builtin_fabsf(d) < __builtin_inff() ? d : 0.f;
+            }
+            lo[s] = pack_chunk<bf16_t>(l);
+        }
+    while (todo) {
+        const int q = __shfl(p, __ffsll((unsigned long long)todo) - 1);
+        const uint64_t mine = __ballot(p == q) & 0xffffffffull;
+        todo &= ~mine;
+        const bool all = mine == 0xffffffffull;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            float16_t t = all ? acc[b] : zero16();
+            const int n = n0 + 32 * b + lr;
+            if (sizeof(T) == 2) {
+                for (int s = 0; s < rp / 16; ++s) {
+                    const uint4 f = F.frag(q, n, 16 * s + 8 * lg, vec);
+                    Mma32<bf16_t>::run(f, lo[s], t);
+                    Mma32<bf16_t>::run(f, hi[s], t);
+                }
+            } else {
+                for (int j = 0; j < F.r; j += 2)
+                    t = __builtin_amdgcn_mfma_f32_32x32x2f32(to_f(F.get(q, n, j + lg)), um[j + lg], t, 0, 0, 0);
+            }
+            if (all) acc[b] = t;
+            else
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[b][e] += p == q ? t[e] : 0.f;
+        }
+    }
+}
+
+// A wave's 32 x 64 outputs (row m0 + lr of lane lr) through a patch of LDS into whole row segments of C.
+template <typename T>
+__device__ inline void ad_store(const float16_t* acc, unsigned char* patch, T* C, int64_t ldc, int M, int N, int m0, int n0, bool vec) {
+    constexpr int VE = 16 / (int)sizeof(T), PITCH = 64 * (int)sizeof(T) + 16, CH = 64 / VE;
+    const int lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            unsigned char* d = patch + lr * PITCH + (32 * b + 8 * g + 4 * lg) * (int)sizeof(T);
+            if (sizeof(T) == 2)
+                *reinterpret_cast<uint2*>(d) = make_uint2(pack2(acc[b][4 * g], acc[b][4 * g + 1]), pack2(acc[b][4 * g + 2], acc[b][4 * g + 3]));
+            else
+                *reinterpret_cast<float4*>(d) = make_float4(acc[b][4 * g], acc[b][4 * g + 1], acc[b][4 * g + 2], acc[b][4 * g + 3]);
+        }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < 32 * CH / 64; ++i) {
+        const int pos = 64 * i + lane, row = pos / CH, n = n0 + (pos % CH) * VE;
+        const uint4 v = *reinterpret_cast<const uint4*>(patch + row * PITCH + (pos % CH) * 16);
+        if (m0 + row < M && n < N) {
+            T* d = C + (int64_t)(m0 + row) * ldc + n;
+            if (vec && n + VE <= N) {
+                *reinterpret_cast<uint4*>(d) = v;
+            } else {
+                T e[VE];
+                *reinterpret_cast<uint4*>(e) = v;
+#pragma unroll
+                for (int k = 0; k < VE; ++k)
+                    if (n + k < N) d[k] = e[k];
+            }
+        }
+    }
+    __builtin_amdgcn_wave_barrier();
+}
+
+// The three products with or of W0, on 128 x 128 tiles of four waves of 64 x 64: any size, stride and alignment.
+enum { AD_FWD = 0, AD_DX = 1, AD_DW = 2 };
+template <int ROLE> struct AdRole;
+template <> struct AdRole<AD_FWD> { static constexpr int KA = KC, KB = KC; };
+template <> struct AdRole<AD_DX> { static constexpr int KA = KC, KB = KS; };
+template <> struct AdRole<AD_DW> { static constexpr int KA = KS, KB = KS; };
+
+template <typename T, int ROLE>
+__global__ __launch_bounds__(256, 2) void k_ad_gemm(AdArgs g) {
+    constexpr int KA = AdRole<ROLE>::KA, KB = AdRole<ROLE>::KB;
+    typedef AdOperand<T, KA> OpA;
+    typedef AdOperand<T, KB> OpB;
+    constexpr int NP = OpA::NP;
+    __shared__ __align__(16) unsigned char lds[(2 * NP * OpA::PLANE > 4 * 32 * 272) ? 2 * NP * OpA::PLANE : 4 * 32 * 272];
+    const int wave = threadIdx.x >> 6, lr = threadIdx.x & 31;
+    const int wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
+    const int rows_a = ROLE == AD_DW ? g.O : g.M, rows_b = ROLE == AD_FWD ? g.O : g.I;
+    const int tiles_n = (rows_b + 127) / 128;
+    const int tile = blockIdx.x;
+    const int tm = (tile / tiles_n) * 128, tn = (tile % tiles_n) * 128;
+    OpA a;
+    OpB b;
+    int kdim;
+    if (ROLE == AD_FWD) {
+        kdim = g.I;
+        a.init(g.x, g.ld_x, g.M, kdim);
+        b.init(g.w0, g.I, g.O, kdim);
+    } else if (ROLE == AD_DX) {
+        kdim = g.O;
+        a.init(g.dy, g.ld_y, g.M, kdim);
+        b.init(g.w0, g.I, g.I, kdim);
+    } else {
+        const int k0 = blockIdx.y * g.kchunk;
+        kdim = g.M - k0 < g.kchunk ? g.M - k0 : g.kchunk;
+        if (kdim < 0) kdim = 0;
+        a.init(reinterpret_cast<const T*>(g.dy) + (int64_t)k0 * g.ld_y, g.ld_y, g.O, kdim);
+        b.init(reinterpret_cast<const T*>(g.x) + (int64_t)k0 * g.ld_x, g.ld_x, g.I, kdim);
+    }
+    unsigned char* lb = lds + NP * OpA::PLANE;
+    float16_t acc[2][2], low[2][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[i][j] = low[i][j] = zero16();
+    if (kdim > 0) {
+        a.fetch(tm, 0);
+        b.fetch(tn, 0);
+    }
+    for (int k = 0; k < kdim; k += 32) {
+        a.put(lds);
+        b.put(lb);
+        __syncthreads();
+        if (k + 32 < kdim) {
+            a.fetch(tm, k + 32);
+            b.fetch(tn, k + 32);
+        }
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            uint4 fa[2][NP], fb[2][NP];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) OpA::frag(lds, wm + 32 * i, ks, fa[i]);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) OpB::frag(lb, wn + 32 * j, ks, fb[j]);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) mma_parts(fb[j], fa[i], acc[i][j], low[i][j]);
+        }
+        __syncthreads();
+    }
+    if (NP == 3) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[i][j][e] += low[i][j][e];
+                if (any_undefined(acc[i][j])) {  // those sums again on the fp32 instructions, from memory; the others stay as they are
+                    const int lg = (threadIdx.x >> 5) & 1;
+                    float16_t t = zero16();
+#pragma unroll 1
+                    for (int k = 0; k < kdim; k += 2)
+                        t = __builtin_amdgcn_mfma_f32_32x32x2f32(b.elem(tn + wn + 32 * j + lr, k + lg), a.elem(tm + wm + 32 * i + lr, k + lg), t, 0, 0, 0);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (!(__builtin_fabsf(acc[i][j][e]) < __builtin_inff())) acc[i][j][e] = t[e];
+                }
+            }
+    }
+    unsigned char* patch = lds + wave * (32 * 272);
+    const int lg = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int m0 = tm + wm + 32 * i, n0 = tn + wn;
+        if (ROLE == AD_FWD) {
+            if (g.bias)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int n = n0 + 32 * j + 8 * (e / 4) + 4 * lg + e % 4;
+                        acc[i][j][e] += n < g.O ? g.bias[n] : 0.f;
+                    }
+            const AdFactor<T, false> F = {reinterpret_cast<const T*>(g.A), g.O, g.r};
+            ad_expand<T, false, 2>(F, g.u, g.rp, g.index, g.P, g.M, m0, n0, acc[i]);
+            ad_store<T>(acc[i], patch, reinterpret_cast<T*>(g.y), g.ld_y, g.M, g.O, m0, n0,
+                        ((reinterpret_cast<uintptr_t>(g.y) | (uintptr_t)(g.ld_y * (int64_t)sizeof(T))) & 15) == 0);
+        } else if (ROLE == AD_DX) {
+            const AdFactor<T, true> F = {reinterpret_cast<const T*>(g.B), g.I, g.r};
+            ad_expand<T, true, 2>(F, g.v, g.rp, g.index, g.P, g.M, m0, n0, acc[i]);
+            ad_store<T>(acc[i], patch, reinterpret_cast<T*>(g.dx), g.ld_x, g.M, g.I, m0, n0,
+                        ((reinterpret_cast<uintptr_t>(g.dx) | (uintptr_t)(g.ld_x * (int64_t)sizeof(T))) & 15) == 0);
+        } else {
+            float* C = g.split > 1 ? g.pw + (int64_t)blockIdx.y * g.O * g.I : g.dw0;
+            ad_store<float>(acc[i], patch, C, g.I, g.O, g.I, m0, n0, (g.I & 3) == 0);
+        }
+    }
+}
+
+// u (or v): the rows' products with their adapters' short factor.  A workgroup takes 32 rows, its four waves a quarter of the
+// contraction each; one pass over the rows per adapter among them.  bf16 on 32x32x16, fp32 on 32x32x2 (the factor's 32 rows are at most
+// `rank` real ones; the pass is bound by its reads).
+template <typename T, bool BWD>
+__global__ __launch_bounds__(256) void k_ad_shrink(AdArgs g) {
+    __shared__ float part[4][32][33];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5;
+    const int m0 = blockIdx.x * 32, m = m0 + lr;
+    const int K = BWD ? g.O : g.I;
+    const int64_t ld = BWD ? g.ld_y : g.ld_x;
+    const T* base = reinterpret_cast<const T*>(BWD ? g.dy : g.x);
+    const bool vec = ((reinterpret_cast<uintptr_t>(base) | (uintptr_t)(ld * (int64_t)sizeof(T))) & 15) == 0;
+    const T* row = base + (int64_t)(m < g.M ? m : g.M - 1) * ld;
+    const T* fac = reinterpret_cast<const T*>(BWD ? g.A : g.B);
+    float* out = BWD ? g.v : g.u;
+    int p = m < g.M ? g.index[m] : -1;
+    if (p < 0 || p >= g.P) p = -1;
+    uint64_t todo = __ballot(p >= 0) & 0xffffffffull;
+    const int kw = ((K + 63) / 64) * 16;  // contraction indices of a wave
+    const int k0 = wave * kw, k1 = k0 + kw < K ? k0 + kw : K;
+    while (todo) {
+        const int q = __shfl(p, __ffsll((unsigned long long)todo) - 1);
+        const uint64_t mine = __ballot(p == q) & 0xffffffffull;
+        todo &= ~mine;
+        // factor (j, k): backward A_q [O][r], forward B_q [r][I]
+        const T* f = fac + (int64_t)q * K * g.r + (BWD ? (int64_t)lr : (int64_t)(lr < g.r ? lr : 0) * K);
+        const int64_t fs = BWD ? g.r : 1;
+        const bool fv = !BWD && (K * (int)sizeof(T)) % 16 == 0;
+        float16_t acc = zero16();
+        for (int k = k0; k < k1; k += 16) {
+            const int kk = k + 8 * lg;
+            T xe[8], fe[8];
+            if (vec && kk + 8 <= K) {
+#pragma unroll
+                for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(xe)[i] = reinterpret_cast<const uint4*>(row + kk)[i];
+            } else
+#pragma unroll
+                for (int i = 0; i < 8; ++i) xe[i] = kk + i < K ? row[kk + i] : (T)0.f;
+            if (fv && kk + 8 <= K) {
+#pragma unroll
+                for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(fe)[i] = reinterpret_cast<const uint4*>(f + kk)[i];
+            } else
+#pragma unroll
+                for (int i = 0; i < 8; ++i) fe[i] = kk + i < K && lr < g.r ? f[(kk + i) * fs] : (T)0.f;
+            if constexpr (sizeof(T) == 2) {
+                Mma32<bf16_t>::run(*reinterpret_cast<uint4*>(fe), *reinterpret_cast<uint4*>(xe), acc);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(fe[i], xe[i], acc, 0, 0, 0);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) part[wave][8 * (e / 4) + 4 * lg + e % 4][lr] = acc[e];
+        __syncthreads();
+        for (int i = threadIdx.x; i < 32 * g.rp; i += 256) {
+            const int ml = i / g.rp, j = i % g.rp;
+            if (mine >> ml & 1)
+                out[(int64_t)(m0 + ml) * g.rp + j] = j < g.r ? part[0][j][ml] + part[1][j][ml] + part[2][j][ml] + part[3][j][ml] : 0.f;
+        }
+        __syncthreads();
+    }
+    const uint64_t none = __ballot(p < 0) & 0xffffffffull;  // rows without an adapter
+    for (int i = threadIdx.x; i < 32 * g.rp; i += 256) {
+        const int ml = i / g.rp;
+        if ((none >> ml & 1) && m0 + ml < g.M) out[(int64_t)(m0 + ml) * g.rp + i % g.rp] = 0.f;
+    }
+}
+
+// Rows sorted by adapter, order kept among a preference's own: workgroup q walks the index twice, to count the rows that come
+// before its own, and to place them.  q = P: the rows without one.
+__global__ __launch_bounds__(1024) void k_ad_plan(AdArgs g) {
+    __shared__ int s_cnt[16], s_base;
+    const int q = blockIdx.x, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    int before = 0;
+    for (int m = tid; m < g.M; m += 1024) {
+        const int p = g.index[m];
+        before += p >= 0 && p < q;  // (q <= P, so only valid ones)
+    }
+    for (int o = 32; o; o >>= 1) before += __shfl_xor(before, o);
+    if (lane == 0) s_cnt[wave] = before;
+    __syncthreads();
+    if (tid == 0) {
+        int s = 0;
+        for (int w = 0; w < 16; ++w) s += s_cnt[w];
+        s_base = s;
+        g.seg[q] = s;
+        if (q == g.P) g.seg[g.P + 1] = g.M;
+    }
+    __syncthreads();
+    int at = s_base;
+    for (int m0 = 0; m0 < g.M; m0 += 1024) {
+        const int m = m0 + tid;
+        int p = m < g.M ? g.index[m] : 0;
+        if (p < 0 || p >= g.P) p = g.P;
+        if (m >= g.M) p = -1;
+        const uint64_t hit = __ballot(p == q);
+        if (lane == 0) s_cnt[wave] = __popcll(hit);
+        __syncthreads();
+        int ahead = 0, total = 0;
+        for (int w = 0; w < 16; ++w) {
+            ahead += w < wave ? s_cnt[w] : 0;
+            total += s_cnt[w];
+        }
+        if (p == q) g.perm[at + ahead + __popcll(hit & ((1ull << lane) - 1))] = m;
+        at += total;
+        __syncthreads();
+    }
+}
+
+// The gradients of the factors and of the bias, one piece of sorted rows and 128 columns of dy (role 0: dA, dbias) or x (role 1:
+// dB) a workgroup: out[c][j] = sum_m src[m][c] w[m][j] with w = u or v in three bf16 parts; a column of ones beside u's gives dbias.
+// Piece c of the sorted rows: segment p and block b = c - p of AD_PIECE rows, p the last one with seg[p] / AD_PIECE + p <= c.
+template <typename T, int JB>
+__global__ __launch_bounds__(256) void k_ad_factor_grad(AdArgs g, int col_blocks_y) {
+    constexpr int NP = sizeof(T) == 4 ? 3 : 1;
+    constexpr int SP = 32 * 320;                 // a plane of 32 rows x 128 columns
+    constexpr int WP = (JB * 32) * 2 + 16;       // bytes of a row of w
+    __shared__ __align__(16) unsigned char src[NP * SP], wts[3 * 32 * WP];
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, lr = lane & 31, lg = lane >> 5;
+    const int c = blockIdx.x;
+    int lo = 0, hi = g.P;  // last segment p in [0, P] with seg[p] / AD_PIECE + p <= c
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (g.seg[mid] / AD_PIECE + mid <= c) lo = mid;
+        else hi = mid - 1;
+    }
+    const int p = lo, b = c - p;
+    const int s0 = g.seg[p] > b * AD_PIECE ? g.seg[p] : b * AD_PIECE;
+    const int s1 = g.seg[p + 1] < (b + 1) * AD_PIECE ? g.seg[p + 1] : (b + 1) * AD_PIECE;
+    if (b < 0 || s0 >= s1) return;
+    const bool whole = s0 == g.seg[p] && s1 == g.seg[p + 1];
+    const bool is_y = (int)blockIdx.y < col_blocks_y;
+    const int C = is_y ? g.O : g.I;
+    const int c0 = (is_y ? blockIdx.y : blockIdx.y - col_blocks_y) * 128;
+    if (p == g.P && !is_y) return;
+    const T* base = reinterpret_cast<const T*>(is_y ? g.dy : g.x);
+    const int64_t ld = is_y ? g.ld_y : g.ld_x;
+    const float* w = is_y ? g.u : g.v;
+    const bool vec = ((reinterpret_cast<uintptr_t>(base) | (uintptr_t)(ld * (int64_t)sizeof(T))) & 15) == 0;
+    float16_t acc[JB];
+#pragma unroll
+    for (int j = 0; j < JB; ++j) acc[j] = zero16();
+    for (int s = s0; s < s1; s += 32) {
+        {   // 32 rows x 128 columns of src: eight threads a row, sixteen columns each
+            const int row = tid / 8, cc = c0 + 16 * (tid % 8);
+            const int m = s + row < s1 ? g.perm[s + row] : -1;
+            uint4 reg[sizeof(T)], l[NP], h[NP];
+            load16(base + (int64_t)(m < 0 ? 0 : m) * ld + cc, m < 0 ? 0 : C - cc, vec, reg);
+            parts16<true>(reg, l, h);
+#pragma unroll
+            for (int q = 0; q < NP; ++q) {
+                *reinterpret_cast<uint4*>(src + q * SP + row * 320 + (tid % 8) * 32) = l[q];
+                *reinterpret_cast<uint4*>(src + q * SP + row * 320 + (tid % 8) * 32 + 16) = h[q];
+            }
+            // JB * 32 weights of a row: eight threads, 4 JB each
+#pragma unroll
+            for (int jj = 0; jj < JB; ++jj) {
+                const int j = 32 * jj + 4 * (tid % 8);
+                float t[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    t[i] = m < 0 ? 0.f : j + i < g.r ? (p < g.P ? w[(int64_t)m * g.rp + j + i] : 0.f) : j + i == g.r ? 1.f : 0.f;
+                uint2 parts[3];
+                split3<true>(make_uint4(__float_as_uint(t[0]), __float_as_uint(t[1]), __float_as_uint(t[2]), __float_as_uint(t[3])), parts);
+#pragma unroll
+                for (int q = 0; q < 3; ++q) *reinterpret_cast<uint2*>(wts + q * 32 * WP + row * WP + j * 2) = parts[q];
+            }
+        }
+        __syncthreads();
+        typedef __attribute__((address_space(3))) short4_t lds_s4;
+        const int a = lane & 15, q0 = (lane >> 4) & 1, e = a >> 2, cw = a & 3;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            const int k = 16 * ks + 8 * lg + e;
+            uint4 fs[NP];
+#pragma unroll
+            for (int q = 0; q < NP; ++q) {
+                const unsigned char* at = src + q * SP + k * 320 + (32 * wave + 16 * q0 + 4 * cw) * 2;
+                const uint2 u0 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)at));
+                const uint2 u1 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(at + 4 * 320)));
+                fs[q] = make_uint4(u0.x, u0.y, u1.x, u1.y);
+            }
+#pragma unroll
+            for (int j = 0; j < JB; ++j) {
+                uint4 fw[3];
+#pragma unroll
+                for (int q = 0; q < 3; ++q) {
+                    const unsigned char* at = wts + q * 32 * WP + k * WP + (32 * j + 16 * q0 + 4 * cw) * 2;
+                    const uint2 u0 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)at));
+                    const uint2 u1 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(at + 4 * WP)));
+                    fw[q] = make_uint4(u0.x, u0.y, u1.x, u1.y);
+                }
+                // lane: column of src; accumulator: j
+#pragma unroll
+                for (int q = 2; q >= 0; --q)
+#pragma unroll
+                    for (int r = NP - 1; r >= 0; --r)
+                        if (q + r <= 2) Mma32<bf16_t>::run(fw[q], fs[r], acc[j]);
+            }
+        }
+        __syncthreads();
+    }
+    const int col = c0 + 32 * wave + lr;
+    if (col >= C) return;
+    float* out = is_y ? g.dA : g.dB;
+    if (out && !whole) out = is_y ? g.pA : g.pB;
+    const int64_t pi = whole ? p : c;
+#pragma unroll
+    for (int j = 0; j < JB; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int jj = 32 * j + 8 * (e / 4) + 4 * lg + e % 4;
+            if (jj < g.r) {
+                if (out && p < g.P) out[is_y ? (pi * g.O + col) * g.r + jj : (pi * g.r + jj) * g.I + col] = acc[j][e];
+            } else if (jj == g.r && is_y && g.dbias) {
+                g.pb[(int64_t)c * g.O + col] = acc[j][e];
+            }
+        }
+}
+
+// What is left in pieces, added in order: split dW0; factor gradients of preferences with several pieces (none: zero); dbias.
+__global__ __launch_bounds__(256) void k_ad_final(AdArgs g, int64_t n_w, int64_t n_f, int blocks_w, int blocks_f) {
+    if ((int)blockIdx.x < blocks_w) {
+        const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+        if (i >= n_w) return;
+        float s = 0.f;
+        for (int q = 0; q < g.split; ++q) s += g.pw[q * n_w + i];
+        g.dw0[i] = s;
+    } else if ((int)blockIdx.x < blocks_w + blocks_f) {
+        const int64_t i = (int64_t)(blockIdx.x - blocks_w) * 256 + threadIdx.x;  // of [P][r (O + I)]
+        if (i >= n_f) return;
+        const int64_t per = (int64_t)g.r * (g.O + g.I);
+        const int p = (int)(i / per);
+        int64_t k = i % per;
+        const int s0 = g.seg[p], s1 = g.seg[p + 1];
+        const int c0 = s0 / AD_PIECE + p, c1 = s1 > s0 ? (s1 - 1) / AD_PIECE + p : c0 - 1;
+        if (c1 == c0) return;
+        const bool in_a = k < (int64_t)g.r * g.O;
+        if (!in_a) k -= (int64_t)g.r * g.O;
+        const int64_t n = (int64_t)g.r * (in_a ? g.O : g.I);
+        float* out = in_a ? g.dA : g.dB;
+        const float* part = in_a ? g.pA : g.pB;
+        if (!out) return;
+        float s = 0.f;
+        for (int c = c0; c <= c1; ++c) s += part[c * n + k];
+        out[p * n + k] = s;
+    } else {
+        const int o = (blockIdx.x - blocks_w - blocks_f) * 256 + threadIdx.x;
+        if (o >= g.O) return;
+        float s = 0.f;
+        for (int p = 0; p <= g.P; ++p) {
+            const int s0 = g.seg[p], s1 = g.seg[p + 1];
+            if (s1 > s0)
+                for (int c = s0 / AD_PIECE + p; c <= (s1 - 1) / AD_PIECE + p; ++c) s += g.pb[(int64_t)c * g.O + o];
+        }
+        g.dbias[o] = s;
+    }
+}
+
+static int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// sizes of the scratch regions for these dimensions; carve(nullptr) gives the total
+static int64_t ad_carve(AdArgs& g, bool bwd, void* ws) {
+    char* at = reinterpret_cast<char*>(ws);
+    int64_t off = 0;
+    auto take = [&](int64_t bytes) {
+        void* q = ws ? at + off : nullptr;
+        off += align_up(bytes, 256);
+        return q;
+    };
+    g.rp = g.r <= 16 ? 16 : 32;
+    g.u = (float*)take((int64_t)g.M * g.rp * 4);
+    if (bwd) {
+        g.v = (float*)take((int64_t)g.M * g.rp * 4);
+        g.seg = (int32_t*)take(((int64_t)g.P + 2) * 4);
+        g.perm = (int32_t*)take((int64_t)g.M * 4);
+        const int64_t tiles = cdiv(g.O, 128) * cdiv(g.I, 128);
+        int64_t split = cdiv(512, tiles);  // two workgroups a CU
+        const int64_t most = cdiv(g.M, 256);
+        if (split > most) split = most;
+        if (split < 1) split = 1;
+        g.kchunk = (int)align_up(cdiv(g.M > 0 ? g.M : 1, split), 32);
+        g.split = (int)cdiv(g.M > 0 ? g.M : 1, g.kchunk);
+        g.pw = (float*)take(g.split > 1 ? (int64_t)g.split * g.O * g.I * 4 : 0);
+        g.pieces = (int)(g.M / AD_PIECE + 1 + g.P);  // ids run to (M - 1) / AD_PIECE + P
+        g.pA = (float*)take((int64_t)g.pieces * g.O * g.r * 4);
+        g.pB = (float*)take((int64_t)g.pieces * g.I * g.r * 4);
+        g.pb = (float*)take((int64_t)g.pieces * g.O * 4);
+    }
+    return off > 0 ? off : 256;
+}
+static AdArgs ad_args(const morlax_adapter_dims& d) {
+    AdArgs g = {};
+    g.M = d.rows; g.I = d.d_in; g.O = d.d_out; g.r = d.rank; g.P = d.n_adapters;
+    g.ld_x = d.ld_x; g.ld_y = d.ld_y;
+    return g;
+}
+int64_t adapter_ws_bytes(const morlax_adapter_dims& d, bool bwd) {
+    AdArgs g = ad_args(d);
+    return ad_carve(g, bwd, nullptr);
+}
+
+template <typename T>
+static void fwd(const AdArgs& g, hipStream_t s) {
+    k_ad_shrink<T, false><<<cdiv(g.M, 32), 256, 0, s>>>(g);
+    k_ad_gemm<T, AD_FWD><<<cdiv(g.M, 128) * cdiv(g.O, 128), 256, 0, s>>>(g);
+}
+void launch_adapter_fwd(const morlax_adapter_dims& d, const void* x, const void* w0, const float* bias, const void* A, const void* B,
+                        const int32_t* index, void* y, void* ws, hipStream_t s) {
+    AdArgs g = ad_args(d);
+    if (g.M == 0) return;
+    ad_carve(g, false, ws);
+    g.x = x; g.w0 = w0; g.bias = bias; g.A = A; g.B = B; g.index = index; g.y = y;
+    if (d.dtype) fwd<bf16_t>(g, s);
+    else fwd<float>(g, s);
+}
+
+template <typename T>
+static void bwd(const AdArgs& g, hipStream_t s) {
+    const bool factors = g.dA || g.dB || g.dbias;
+    if (g.M > 0) {
+        if (g.dA) k_ad_shrink<T, false><<<cdiv(g.M, 32), 256, 0, s>>>(g);
+        if (g.dx || g.dB) k_ad_shrink<T, true><<<cdiv(g.M, 32), 256, 0, s>>>(g);
+        if (g.dx) k_ad_gemm<T, AD_DX><<<cdiv(g.M, 128) * cdiv(g.I, 128), 256, 0, s>>>(g);
+    }
+    if (g.dw0) k_ad_gemm<T, AD_DW><<<dim3(cdiv(g.O, 128) * cdiv(g.I, 128), g.split), 256, 0, s>>>(g);
+    if (factors) {
+        k_ad_plan<<<g.P + 1, 1024, 0, s>>>(g);
+        const int by = g.dA || g.dbias ? (int)cdiv(g.O, 128) : 0, bx = g.dB ? (int)cdiv(g.I, 128) : 0;
+        if (g.r < 32) k_ad_factor_grad<T, 1><<<dim3(g.pieces, by + bx), 256, 0, s>>>(g, by);
+        else k_ad_factor_grad<T, 2><<<dim3(g.pieces, by + bx), 256, 0, s>>>(g, by);
+    }
+    const int64_t n_w = g.dw0 && g.split > 1 ? (int64_t)g.O * g.I : 0, n_f = g.dA || g.dB ? (int64_t)g.P * g.r * (g.O + g.I) : 0;
+    const int64_t bw = cdiv(n_w, 256), bf = cdiv(n_f, 256), bb = g.dbias ? cdiv(g.O, 256) : 0;
+    if (bw + bf + bb > 0) k_ad_final<<<bw + bf + bb, 256, 0, s>>>(g, n_w, n_f, (int)bw, (int)bf);
+}
+void launch_adapter_bwd(const morlax_adapter_dims& d, const void* x, const void* w0, const void* A, const void* B, const int32_t* index,
+                        const void* dy, void* dx, float* dw0, float* dbias, float* dA, float* dB, void* ws, hipStream_t s) {
+    AdArgs g = ad_args(d);
+    ad_carve(g, true, ws);
+    g.x = x; g.w0 = w0; g.A = A; g.B = B; g.index = index; g.dy = dy;
+    g.dx = dx; g.dw0 = dw0; g.dbias = dbias; g.dA = dA; g.dB = dB;
+    if (d.dtype) bwd<bf16_t>(g, s);
+    else bwd<float>(g, s);
+}

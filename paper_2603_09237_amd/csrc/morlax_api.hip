@@ -486,3 +486,72 @@ extern "C" int morlax_ppo_loss_grad_static(morlax_ctx* ctx, const morlax_rows* r
                          norm_adv, dmu, dlogsig, dv, stats, ws, (hipStream_t)stream);
     return finish(who);
 }
+
+// ---- policies for any mix of preferences, with memory ----------------------------------------------------------
+// a strided tensor: present and aligned to its elements
+static int strided(const void* p, int dtype, const char* name, const char* who) {
+    if (!p) return fail(MORLAX_ERR_NULL, "%s: %s is NULL", who, name);
+    if ((reinterpret_cast<uintptr_t>(p) & (dtype ? 1u : 3u)) != 0)
+        return fail(MORLAX_ERR_SHAPE, "%s: %s is not aligned to its elements", who, name);
+    return MORLAX_OK;
+}
+#define STRIDED(ptr, dtype, who)                                        \
+    do {                                                                \
+        const int rc_ = strided(ptr, dtype, #ptr, who);                 \
+        if (rc_ != MORLAX_OK) return rc_;                               \
+    } while (0)
+
+static int check_adapter(const morlax_adapter_dims* d, const char* who) {
+    if (!d) return fail(MORLAX_ERR_NULL, "%s: dims is NULL", who);
+    if (d->rows < 0 || d->d_in < 1 || d->d_out < 1 || d->rank < 1 || d->n_adapters < 1)
+        return fail(MORLAX_ERR_SHAPE, "%s: rows must be >= 0, d_in, d_out, rank and n_adapters >= 1", who);
+    if (d->dtype != 0 && d->dtype != 1) return fail(MORLAX_ERR_UNSUPPORTED, "%s: dtype must be 0 (fp32) or 1 (bf16)", who);
+    if (d->rank > MORLAX_MAX_RANK) return fail(MORLAX_ERR_UNSUPPORTED, "%s: rank must be <= %d", who, MORLAX_MAX_RANK);
+    if (d->d_in > 65536 || d->d_out > 65536 || d->n_adapters > 1 << 20)
+        return fail(MORLAX_ERR_UNSUPPORTED, "%s: d_in and d_out must be <= 65536, n_adapters <= 2^20", who);
+    if (d->ld_x < d->d_in || d->ld_y < d->d_out)
+        return fail(MORLAX_ERR_SHAPE, "%s: a row stride is shorter than its row", who);
+    // a launch carries its output tiles, or the elements of the factors' gradients in blocks of 256, in gridDim.x
+    const int64_t wide = d->d_in > d->d_out ? d->d_in : d->d_out;
+    if (((int64_t)d->rows / 128 + 1) * (wide / 128 + 1) >= (int64_t)1 << 31 ||
+        (int64_t)d->n_adapters * d->rank * ((int64_t)d->d_in + d->d_out) >= (int64_t)1 << 38)
+        return fail(MORLAX_ERR_UNSUPPORTED, "%s: more output tiles than a launch has workgroups", who);
+    return MORLAX_OK;
+}
+
+extern "C" int64_t morlax_adapter_workspace_bytes(const morlax_adapter_dims* d, int32_t backward) {
+    if (check_adapter(d, "morlax_adapter_workspace_bytes") != MORLAX_OK) return -1;
+    return adapter_ws_bytes(*d, backward != 0);
+}
+
+extern "C" int morlax_adapter_fwd(const morlax_adapter_dims* dims, const void* x, const void* w0, const float* bias, const void* A,
+                                  const void* B, const int32_t* index, void* y, void* ws, int64_t ws_bytes, void* stream) {
+    const char* who = "morlax_adapter_fwd";
+    const int rc = check_adapter(dims, who);
+    if (rc != MORLAX_OK) return rc;
+    REQ(w0, who); REQ(A, who); REQ(B, who); OPT(bias, who);
+    if (dims->rows == 0) return MORLAX_OK;
+    STRIDED(x, dims->dtype, who); STRIDED(y, dims->dtype, who);
+    REQ(index, who);
+    WS(ws, ws_bytes, adapter_ws_bytes(*dims, false), who);
+    launch_adapter_fwd(*dims, x, w0, bias, A, B, index, y, ws, (hipStream_t)stream);
+    return finish(who);
+}
+
+extern "C" int morlax_adapter_bwd(const morlax_adapter_dims* dims, const void* x, const void* w0, const void* A, const void* B,
+                                  const int32_t* index, const void* dy, void* dx, float* dw0, float* dbias, float* dA, float* dB,
+                                  void* ws, int64_t ws_bytes, void* stream) {
+    const char* who = "morlax_adapter_bwd";
+    const int rc = check_adapter(dims, who);
+    if (rc != MORLAX_OK) return rc;
+    REQ(w0, who); REQ(A, who); REQ(B, who);
+    OPT(dw0, who); OPT(dbias, who); OPT(dA, who); OPT(dB, who);
+    if (dims->rows > 0) {  // (without rows there may be no tensors of them)
+        STRIDED(x, dims->dtype, who); STRIDED(dy, dims->dtype, who);
+        if (dx) STRIDED(dx, dims->dtype, who);
+        REQ(index, who);
+    }
+    WS(ws, ws_bytes, adapter_ws_bytes(*dims, true), who);
+    launch_adapter_bwd(*dims, x, w0, A, B, index, dy, dx, dw0, dbias, dA, dB, ws, (hipStream_t)stream);
+    return finish(who);
+}

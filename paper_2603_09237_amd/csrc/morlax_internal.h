@@ -113,4 +113,10 @@ uint64_t hv_tuples(int n, int K);
 void launch_pareto_hypervolume(const float* J, const float* ref, int n, int K, uint8_t* front, double* hv, void* ws,
                                hipStream_t s);
 
+int64_t adapter_ws_bytes(const morlax_adapter_dims& d, bool bwd);
+void launch_adapter_fwd(const morlax_adapter_dims& d, const void* x, const void* w0, const float* bias, const void* A, const void* B,
+                        const int32_t* index, void* y, void* ws, hipStream_t s);
+void launch_adapter_bwd(const morlax_adapter_dims& d, const void* x, const void* w0, const void* A, const void* B, const int32_t* index,
+                        const void* dy, void* dx, float* dw0, float* dbias, float* dA, float* dB, void* ws, hipStream_t s);
+
 static inline int64_t align_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }

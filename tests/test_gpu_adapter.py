@@ -1,0 +1,214 @@
+"""The shared projection with an adapter per preference against its definition in 64 bits: every preference's own matrix W0 + A_p B_p
+on the rows that name it."""
+import numpy as np
+import pytest
+
+from paper_2603_09237_amd import binding
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = 0, 1
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def problem(M, I, O, r, P, dtype, mix="mixed", seed=0, pad=0):
+    """Inputs on the device (rows of x and dy `pad` elements apart beyond their width) and the same values in 64 bits."""
+    torch = _torch()
+    g = torch.Generator().manual_seed(seed)
+    td = torch.bfloat16 if dtype == BF16 else torch.float32
+
+    def normal(*shape, scale=1.0, t=td):
+        return (torch.randn(*shape, generator=g) * scale).to(t)
+
+    d = dict(x=normal(M, I + pad)[:, :I], w0=normal(O, I, scale=I ** -0.5), A=normal(P, O, r, scale=0.4 * r ** -0.5),
+             B=normal(P, r, I, scale=0.4 * I ** -0.5), bias=normal(O, t=torch.float32), dy=normal(M, O + pad)[:, :O])
+    if mix == "mixed":       # some rows without an adapter, some named beyond the last
+        index = torch.randint(-2, P + 1, (M,), generator=g)
+    elif mix == "grouped":
+        index = torch.arange(M) * P // max(M, 1)
+    elif mix == "one":       # all rows one adapter's: every other one's gradient is zero
+        index = torch.full((M,), P // 2)
+    else:
+        index = torch.full((M,), -1)
+    d["index"] = index.to(torch.int32)
+    ref = {k: v.double().numpy() for k, v in d.items() if k != "index"}
+    ref["index"] = d["index"].numpy()
+    dev = {}
+    for k, v in d.items():
+        if k in ("x", "dy") and pad:
+            whole = torch.zeros(M, v.shape[1] + pad, dtype=v.dtype, device="cuda")
+            dev[k] = whole[:, :v.shape[1]]
+            dev[k].copy_(v)
+        else:
+            dev[k] = v.contiguous().cuda()
+    dims = binding.AdapterDims(M, I, O, r, P, dtype, I + pad, O + pad)
+    return dims, dev, ref
+
+
+def definition(ref, P):
+    """y, dx and the gradients, and beside each the same sums of magnitudes, against which rounding is measured."""
+    x, w0, A, B, dy = (ref[k] for k in ("x", "w0", "A", "B", "dy"))
+    out = {}
+    for tag, f in (("", lambda v: v), ("abs", np.abs)):
+        X, W, AA, BB, D = f(x), f(w0), f(A), f(B), f(dy)
+        y, dx = X @ W.T + f(ref["bias"]), D @ W
+        dA, dB = np.zeros_like(A), np.zeros_like(B)
+        for p in range(P):
+            m = ref["index"] == p
+            u, v = X[m] @ BB[p].T, D[m] @ AA[p]
+            y[m] += u @ AA[p].T
+            dx[m] += v @ BB[p]
+            dA[p], dB[p] = D[m].T @ u, v.T @ X[m]
+        out.update({"y" + tag: y, "dx" + tag: dx, "dw0" + tag: D.T @ X, "dbias" + tag: D.sum(0), "dA" + tag: dA, "dB" + tag: dB})
+    return out
+
+
+def check(got, want, size, terms, rounded, what):
+    """Each of the two or three chained sums of at most `terms` products is off by at most (terms + 8) 2^-24 of its sum of magnitudes in
+    the worst order; products of split operands and sums in blocks are better.  An output rounded to bf16: 2^-8 of itself more (half a
+    unit in the last place is 2^-9), and 2^-16 of the magnitudes for u in two bf16 parts."""
+    got = got.double().cpu().numpy()
+    tol = 3 * (terms + 8) * 2.0 ** -24 * size + (2.0 ** -8 * np.abs(want) + 2.0 ** -16 * size if rounded else 0) + 1e-30
+    bad = ~(np.abs(got - want) <= tol)
+    assert not bad.any(), (what, int(bad.sum()), bad.size, float(np.abs(got - want)[bad].max()))
+
+
+def run_fwd(dims, d, bias=True):
+    torch = _torch()
+    y = torch.full((dims.rows, dims.ld_y), 7.0, dtype=d["w0"].dtype, device="cuda")
+    ws = torch.empty(binding.adapter_workspace_bytes(dims), dtype=torch.uint8, device="cuda").fill_(255)
+    binding.adapter_fwd(dims, d["x"], d["w0"], d["bias"] if bias else None, d["A"], d["B"], d["index"], y, ws)
+    assert (y[:, dims.d_out:] == 7.0).all()   # nothing beyond a row's end
+    return y[:, :dims.d_out]
+
+
+def run_bwd(dims, d, only=None):
+    torch = _torch()
+    M, I, O, r, P = dims.rows, dims.d_in, dims.d_out, dims.rank, dims.n_adapters
+    o = dict(dx=torch.full((M, dims.ld_x), 7.0, dtype=d["w0"].dtype, device="cuda"), dw0=torch.full((O, I), 7.0, device="cuda"),
+             dbias=torch.full((O,), 7.0, device="cuda"), dA=torch.full((P, O, r), 7.0, device="cuda"), dB=torch.full((P, r, I), 7.0, device="cuda"))
+    o = {k: v if only is None or k in only else None for k, v in o.items()}
+    ws = torch.empty(binding.adapter_workspace_bytes(dims, True), dtype=torch.uint8, device="cuda").fill_(255)
+    binding.adapter_bwd(dims, d["x"], d["w0"], d["A"], d["B"], d["index"], d["dy"], o["dx"], o["dw0"], o["dbias"], o["dA"], o["dB"], ws)
+    if o["dx"] is not None:
+        assert (o["dx"][:, I:] == 7.0).all()
+        o["dx"] = o["dx"][:, :I]
+    return o
+
+
+# rows, d_in, d_out, rank, adapters, order, elements between rows
+SHAPES = [(1, 8, 8, 1, 1, "one", 0), (1, 64, 96, 16, 5, "mixed", 0), (3, 27, 50, 5, 6, "mixed", 1), (33, 64, 130, 8, 4, "grouped", 0),
+          (64, 256, 320, 16, 64, "mixed", 8), (129, 40, 264, 32, 3, "mixed", 0), (257, 31, 33, 17, 300, "mixed", 3), (600, 136, 200, 31, 2, "one", 0),
+          (1030, 512, 72, 4, 16, "grouped", 0), (515, 72, 512, 16, 7, "none", 0), (2100, 264, 392, 9, 130, "mixed", 0)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("M,I,O,r,P,mix,pad", SHAPES)
+def test_forward(M, I, O, r, P, mix, pad, dtype):
+    dims, d, ref = problem(M, I, O, r, P, dtype, mix, seed=M + I, pad=pad)
+    want = definition(ref, P)
+    check(run_fwd(dims, d), want["y"], want["yabs"], max(I, r), dtype == BF16, "y")
+    check(run_fwd(dims, d, bias=False), want["y"] - ref["bias"], want["yabs"], max(I, r), dtype == BF16, "y without bias")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("M,I,O,r,P,mix,pad", SHAPES)
+def test_backward(M, I, O, r, P, mix, pad, dtype):
+    dims, d, ref = problem(M, I, O, r, P, dtype, mix, seed=M + O, pad=pad)
+    want = definition(ref, P)
+    got = run_bwd(dims, d)
+    again = run_bwd(dims, d)
+    for k in ("dx", "dw0", "dbias", "dA", "dB"):
+        check(got[k], want[k], want[k + "abs"], max(O if k in ("dx", "dB") else 0, I if k == "dA" else 0, M), dtype == BF16 and k == "dx", k)
+        assert _torch().equal(got[k], again[k]), k   # bit for bit
+
+
+@pytest.mark.parametrize("only", [("dx",), ("dA",), ("dB",), ("dbias",), ("dw0", "dA")])
+def test_backward_outputs_left_out(only):
+    dims, d, ref = problem(150, 40, 48, 6, 9, BF16, seed=3)
+    whole, part = run_bwd(dims, d), run_bwd(dims, d, only)
+    for k in whole:
+        assert (part[k] is None) == (k not in only)
+        if k in only:
+            assert _torch().equal(whole[k], part[k]), k
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_no_rows(dtype):
+    dims, d, _ = problem(0, 24, 32, 4, 3, dtype, "none")
+    got = run_bwd(dims, d)
+    for k in ("dw0", "dbias", "dA", "dB"):
+        assert (got[k] == 0).all(), k
+    assert run_fwd(dims, d).shape == (0, 32)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_an_undefined_adapter_stays_in_its_rows(dtype):
+    """Rows of other adapters, in the same blocks of rows, do not see one whose factors are infinite or undefined."""
+    torch = _torch()
+    dims, d, ref = problem(96, 48, 80, 8, 5, dtype, seed=5)
+    clean = run_fwd(dims, d).clone()
+    clean_dx = run_bwd(dims, d, ("dx",))["dx"].clone()
+    d["A"][2, :, 3] = float("nan")
+    d["B"][2, 1] = float("inf")
+    other = torch.from_numpy(ref["index"] != 2).cuda()
+    for got, was in ((run_fwd(dims, d), clean), (run_bwd(dims, d, ("dx",))["dx"], clean_dx)):
+        assert torch.equal(got[other], was[other])
+        assert not torch.isfinite(got[~other]).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_an_undefined_row_stays_a_row(dtype):
+    torch = _torch()
+    dims, d, ref = problem(96, 48, 80, 8, 5, dtype, seed=6)
+    clean = run_fwd(dims, d).clone()
+    d["x"][17] = float("nan")
+    d["x"][40, 5] = float("inf")
+    got = run_fwd(dims, d)
+    keep = torch.ones(96, dtype=torch.bool, device="cuda")
+    keep[[17, 40]] = False
+    assert torch.equal(got[keep], clean[keep])
+    assert torch.isnan(got[17]).all() and not torch.isfinite(got[40]).any()
+
+
+@pytest.mark.parametrize("dtype", [F32])
+def test_gradients_against_differences(dtype):
+    """The definition's gradients, which the other tests hold the kernels to, against central differences of the definition."""
+    dims, d, ref = problem(7, 5, 6, 2, 3, dtype, seed=8)
+    P = 3
+    want = definition(ref, P)
+
+    def loss(r):
+        return float((definition(r, P)["y"] * r["dy"]).sum())
+
+    for name, grad in (("x", "dx"), ("w0", "dw0"), ("A", "dA"), ("B", "dB"), ("bias", "dbias")):
+        flat = ref[name].reshape(-1)
+        for i in range(0, flat.size, max(1, flat.size // 7)):
+            h, keep = 1e-6, flat[i]
+            vals = []
+            for s in (h, -h):
+                r = dict(ref)
+                r[name] = ref[name].copy()
+                r[name].reshape(-1)[i] = keep + s
+                vals.append(loss(r))
+            assert abs((vals[0] - vals[1]) / (2 * h) - want[grad].reshape(-1)[i]) < 1e-6, (name, i)
+
+
+def test_other_stream():
+    """The call runs on the stream that is current, behind what was put there."""
+    torch = _torch()
+    dims, d, ref = problem(300, 64, 64, 8, 4, BF16, seed=9)
+    want = run_fwd(dims, d).clone()
+    x = d["x"].clone()
+    d["x"].zero_()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        d["x"].copy_(x)
+        got = run_fwd(dims, d)
+    s.synchronize()
+    assert torch.equal(got, want)
