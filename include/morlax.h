@@ -291,6 +291,67 @@ int morlax_adapter_bwd(const morlax_adapter_dims* dims, const void* x, const voi
                        const int32_t* index, const void* dy, void* dx, float* dw0, float* dbias, float* dA, float* dB, void* ws,
                        int64_t ws_bytes, void* stream);
 
+/* Memory over time.  Environments' episodes begin where first [T, N] u8 is non-zero (NULL: nowhere): as in the GAE scan a select,
+ * nothing before an episode's first step reaches it or anything behind it, in values or gradients, be it infinite or undefined.  (That
+ * step t begins an episode is `done` of step t - 1.)  State tensors carry the memory from one call to the next; NULL on the way in is
+ * an empty memory, NULL on the way out is not wanted.
+ *
+ * Short causal convolution, one filter a channel: y[t, n, c] = act(b[c] + sum_k w[c, k] x[t - (width - 1) + k, n, c]) over the steps
+ * of t's own episode.  x, y [T, N, channels] of the given type, step (t, n) at t * x_t + n * x_n (y_t, y_n) elements; w [channels, width],
+ * b [channels] (or NULL) fp32; state_in, state_out [N, width - 1, channels] of the given type: the last inputs, oldest first.
+ * y must not be x, state_out not state_in.  act: 0 none, 1 SiLU.  Limits: T, N, channels >= 1, 1 <= width <= 4. */
+typedef struct {
+    int32_t T, N, channels, width;
+    int32_t act, dtype;
+    int64_t x_t, x_n, y_t, y_n;
+} morlax_conv_dims;
+
+int64_t morlax_conv_workspace_bytes(const morlax_conv_dims* dims); /* of the backward; -1 for dimensions that are not served */
+int morlax_conv_fwd(const morlax_conv_dims* dims, const void* x, const float* w, const float* b, const uint8_t* first,
+                    const void* state_in, void* y, void* state_out, void* stream);
+/* Reverse mode: dy (strides of y), dstate_out [N, width - 1, channels] or NULL (zero) -> dx (strides of x), dw [channels, width]
+ * and db [channels] fp32 (or NULL), dstate_in (or NULL).  Sums in a fixed order. */
+int morlax_conv_bwd(const morlax_conv_dims* dims, const void* x, const float* w, const float* b, const uint8_t* first,
+                    const void* state_in, const void* dy, const void* dstate_out, void* dx, float* dw, float* db, void* dstate_in,
+                    void* ws, int64_t ws_bytes, void* stream);
+
+/* Selective state space scan.  Per environment, head and step, with dt = softplus(dt_raw + dt_bias[head]) and
+ * a = -exp(a_log[head]):
+ *   h_t = exp(dt a) h_{t-1} + dt x_t B_t^T  (h_{t-1} = 0 where an episode begins),   y_t = (h_t C_t + d_skip[head] x_t) silu(z_t)
+ * x, z, y rows [heads * head_dim], b and c rows [groups * state] (heads / groups consecutive heads share them), dt rows [heads]; x, b and
+ * c have the strides x_t, x_n (they may be slices of the convolution's rows); z NULL: no gate.  a_log, d_skip (or NULL: 0), dt_bias (or
+ * NULL: 0) [heads] fp32; state_in, state_out [N, heads, head_dim, state] fp32, which may be the same buffer.  Sums and states are
+ * fp32 whatever the type, y is rounded once.  An infinite or undefined input makes what depends on it infinite or undefined (not
+ * always the one that step-by-step arithmetic would give).  saved: morlax_scan_saved_bytes() bytes that the backward needs, or NULL.
+ * Limits: T, N, heads, groups, state, head_dim >= 1, groups | heads, head_dim <= 64, state <= 64. */
+typedef struct {
+    int32_t T, N, heads, head_dim, groups, state;
+    int32_t dtype;
+    int64_t x_t, x_n, z_t, z_n, dt_t, dt_n, y_t, y_n;
+} morlax_scan_dims;
+
+int64_t morlax_scan_saved_bytes(const morlax_scan_dims* dims);
+int64_t morlax_scan_workspace_bytes(const morlax_scan_dims* dims, int32_t backward);
+int morlax_scan_fwd(const morlax_scan_dims* dims, const void* x, const void* b, const void* c, const void* dt, const void* z,
+                    const float* a_log, const float* d_skip, const float* dt_bias, const uint8_t* first, const float* state_in,
+                    void* y, float* state_out, void* saved, void* ws, int64_t ws_bytes, void* stream);
+/* Reverse mode; `saved` comes from the matching morlax_scan_fwd (same dims and inputs).  dy (strides of y), dstate_out [N, heads,
+ * head_dim, state] fp32 or NULL (zero) -> dx, db, dc (strides of x), ddt (of dt), dz (of z; NULL exactly where z is), and fp32:
+ * da_log, dd_skip, ddt_bias [heads], dstate_in [N, heads, head_dim, state] (each or NULL).  Sums in a fixed order. */
+int morlax_scan_bwd(const morlax_scan_dims* dims, const void* x, const void* b, const void* c, const void* dt, const void* z,
+                    const float* a_log, const float* d_skip, const float* dt_bias, const uint8_t* first, const void* saved,
+                    const void* dy, const float* dstate_out, void* dx, void* db, void* dc, void* ddt, void* dz, float* da_log,
+                    float* dd_skip, float* ddt_bias, float* dstate_in, void* ws, int64_t ws_bytes, void* stream);
+
+/* One time step of both (dims->T = 1; the *_t strides are not used): the convolution with SiLU over the rows xbc [N, heads *
+ * head_dim + 2 groups * state] (x, then B, then C), stride x_n, and the scan on its outputs, which stay in fp32 between the two.
+ * width, conv_w, conv_b, conv_in, conv_out as in morlax_conv_fwd on those channels, the others as in morlax_scan_fwd; first [N].
+ * conv_out must not be conv_in; state_out may be state_in. */
+int morlax_memory_step(const morlax_scan_dims* dims, int32_t width, const void* xbc, const void* dt, const void* z,
+                       const float* conv_w, const float* conv_b, const float* a_log, const float* d_skip, const float* dt_bias,
+                       const uint8_t* first, const void* conv_in, const float* state_in, void* y, void* conv_out, float* state_out,
+                       void* stream);
+
 #ifdef __cplusplus
 }
 #endif

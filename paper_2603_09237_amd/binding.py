@@ -34,6 +34,29 @@ class AdapterDims(C.Structure):
         super().__init__(rows, d_in, d_out, rank, adapters, dtype, d_in if ld_x is None else ld_x, d_out if ld_y is None else ld_y)
 
 
+class ConvDims(C.Structure):
+    """morlax_conv_dims: strides in elements, those of a contiguous [T, N, channels] where they are not given."""
+    _fields_ = [(n, C.c_int32) for n in ("T", "N", "channels", "width", "act", "dtype")] + \
+               [(n, C.c_int64) for n in ("x_t", "x_n", "y_t", "y_n")]
+
+    def __init__(self, T, N, channels, width, act, dtype, x_t=None, x_n=None, y_t=None, y_n=None):
+        full = [N * channels, channels] * 2
+        super().__init__(T, N, channels, width, act, dtype, *[f if v is None else v for v, f in zip((x_t, x_n, y_t, y_n), full)])
+
+
+class ScanDims(C.Structure):
+    """morlax_scan_dims: strides in elements; where they are not given, those of contiguous rows, x, B and C one after the other."""
+    _fields_ = [(n, C.c_int32) for n in ("T", "N", "heads", "head_dim", "groups", "state", "dtype")] + \
+               [(n, C.c_int64) for n in ("x_t", "x_n", "z_t", "z_n", "dt_t", "dt_n", "y_t", "y_n")]
+
+    def __init__(self, T, N, heads, head_dim, groups, state, dtype, x_t=None, x_n=None, z_t=None, z_n=None, dt_t=None, dt_n=None,
+                 y_t=None, y_n=None):
+        D = heads * head_dim
+        full = [k for w in (D + 2 * groups * state, D, heads, D) for k in (N * w, w)]
+        super().__init__(T, N, heads, head_dim, groups, state, dtype,
+                         *[f if v is None else v for v, f in zip((x_t, x_n, z_t, z_n, dt_t, dt_n, y_t, y_n), full)])
+
+
 class MorlaxError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__(f"morlax error {code}: {msg}")
@@ -50,7 +73,9 @@ EXPORTS = ("morlax_create", "morlax_destroy", "morlax_last_error", "morlax_hpara
            "morlax_sample_preferences", "morlax_scalarize_normalized", "morlax_ppo_loss_grad",
            "morlax_ppo_loss_grad_static", "morlax_eval_returns",
            "morlax_hypervolume_workspace_bytes", "morlax_pareto_hypervolume", "morlax_profile_begin",
-           "morlax_profile_end", "morlax_adapter_workspace_bytes", "morlax_adapter_fwd", "morlax_adapter_bwd")
+           "morlax_profile_end", "morlax_adapter_workspace_bytes", "morlax_adapter_fwd", "morlax_adapter_bwd",
+           "morlax_conv_workspace_bytes", "morlax_conv_fwd", "morlax_conv_bwd", "morlax_scan_saved_bytes",
+           "morlax_scan_workspace_bytes", "morlax_scan_fwd", "morlax_scan_bwd", "morlax_memory_step")
 
 GEMM_KINDS = ("fwd_first", "fwd_hidden", "dx_hidden", "dw_hidden", "dw_first", "fwd_fused")
 
@@ -108,6 +133,19 @@ def load():
     lib.morlax_adapter_workspace_bytes.restype = i64
     lib.morlax_adapter_fwd.argtypes = [dp] + [vp] * 8 + [i64, vp]
     lib.morlax_adapter_bwd.argtypes = [dp] + [vp] * 12 + [i64, vp]
+    cp, sp = C.POINTER(ConvDims), C.POINTER(ScanDims)
+    lib.morlax_conv_workspace_bytes.argtypes = [cp]
+    lib.morlax_scan_saved_bytes.argtypes = [sp]
+    lib.morlax_scan_workspace_bytes.argtypes = [sp, i32]
+    for name in ("morlax_conv_workspace_bytes", "morlax_scan_saved_bytes", "morlax_scan_workspace_bytes"):
+        getattr(lib, name).restype = i64
+    lib.morlax_conv_fwd.argtypes = [cp] + [vp] * 8
+    lib.morlax_conv_bwd.argtypes = [cp] + [vp] * 12 + [i64, vp]
+    lib.morlax_scan_fwd.argtypes = [sp] + [vp] * 14 + [i64, vp]
+    lib.morlax_scan_bwd.argtypes = [sp] + [vp] * 22 + [i64, vp]
+    lib.morlax_memory_step.argtypes = [sp, i32] + [vp] * 15
+    for name in ("morlax_conv_fwd", "morlax_conv_bwd", "morlax_scan_fwd", "morlax_scan_bwd", "morlax_memory_step"):
+        getattr(lib, name).restype = C.c_int
     for name in ("morlax_adapter_fwd", "morlax_adapter_bwd"):
         getattr(lib, name).restype = C.c_int
     lib.morlax_profile_begin.argtypes = [vp]
@@ -347,3 +385,53 @@ def adapter_bwd(dims, x, w0, A, B, index, dy, dx, dw0, dbias, dA, dB, ws, stream
     """morlax_adapter_bwd: gradients of adapter_fwd; outputs that are None are left out."""
     _call(load().morlax_adapter_bwd, C.byref(dims), _ptr(x), _ptr(w0), _ptr(A), _ptr(B), _ptr(index), _ptr(dy), _ptr(dx), _ptr(dw0),
           _ptr(dbias), _ptr(dA), _ptr(dB), _ptr(ws), _nbytes(ws), stream if stream is not None else _stream())
+
+
+def conv_workspace_bytes(dims):
+    """Bytes of device scratch that conv_bwd needs."""
+    return _size(load().morlax_conv_workspace_bytes(C.byref(dims)))
+
+
+def conv_fwd(dims, x, w, b, first, state_in, y, state_out, stream=None):
+    """morlax_conv_fwd: the short causal convolution over the steps of each episode."""
+    _call(load().morlax_conv_fwd, C.byref(dims), _ptr(x), _ptr(w), _ptr(b), _ptr(first), _ptr(state_in), _ptr(y), _ptr(state_out),
+          stream if stream is not None else _stream())
+
+
+def conv_bwd(dims, x, w, b, first, state_in, dy, dstate_out, dx, dw, db, dstate_in, ws, stream=None):
+    """morlax_conv_bwd: gradients of conv_fwd."""
+    _call(load().morlax_conv_bwd, C.byref(dims), _ptr(x), _ptr(w), _ptr(b), _ptr(first), _ptr(state_in), _ptr(dy), _ptr(dstate_out),
+          _ptr(dx), _ptr(dw), _ptr(db), _ptr(dstate_in), _ptr(ws), _nbytes(ws), stream if stream is not None else _stream())
+
+
+def scan_saved_bytes(dims):
+    """Bytes of the `saved` buffer that scan_fwd fills for scan_bwd."""
+    return _size(load().morlax_scan_saved_bytes(C.byref(dims)))
+
+
+def scan_workspace_bytes(dims, backward=False):
+    """Bytes of device scratch that scan_fwd (scan_bwd) needs."""
+    return _size(load().morlax_scan_workspace_bytes(C.byref(dims), int(bool(backward))))
+
+
+def scan_fwd(dims, x, b, c, dt, z, a_log, d_skip, dt_bias, first, state_in, y, state_out, saved, ws, stream=None):
+    """morlax_scan_fwd: the selective state space scan of all environments and heads."""
+    _call(load().morlax_scan_fwd, C.byref(dims), _ptr(x), _ptr(b), _ptr(c), _ptr(dt), _ptr(z), _ptr(a_log), _ptr(d_skip), _ptr(dt_bias),
+          _ptr(first), _ptr(state_in), _ptr(y), _ptr(state_out), _ptr(saved), _ptr(ws), _nbytes(ws),
+          stream if stream is not None else _stream())
+
+
+def scan_bwd(dims, x, b, c, dt, z, a_log, d_skip, dt_bias, first, saved, dy, dstate_out, dx, db, dc, ddt, dz, da_log, dd_skip, ddt_bias,
+             dstate_in, ws, stream=None):
+    """morlax_scan_bwd: gradients of scan_fwd from what it saved."""
+    _call(load().morlax_scan_bwd, C.byref(dims), _ptr(x), _ptr(b), _ptr(c), _ptr(dt), _ptr(z), _ptr(a_log), _ptr(d_skip), _ptr(dt_bias),
+          _ptr(first), _ptr(saved), _ptr(dy), _ptr(dstate_out), _ptr(dx), _ptr(db), _ptr(dc), _ptr(ddt), _ptr(dz), _ptr(da_log),
+          _ptr(dd_skip), _ptr(ddt_bias), _ptr(dstate_in), _ptr(ws), _nbytes(ws), stream if stream is not None else _stream())
+
+
+def memory_step(dims, width, xbc, dt, z, conv_w, conv_b, a_log, d_skip, dt_bias, first, conv_in, state_in, y, conv_out, state_out,
+                stream=None):
+    """morlax_memory_step: one time step of the convolution and the scan in one launch."""
+    _call(load().morlax_memory_step, C.byref(dims), int(width), _ptr(xbc), _ptr(dt), _ptr(z), _ptr(conv_w), _ptr(conv_b), _ptr(a_log),
+          _ptr(d_skip), _ptr(dt_bias), _ptr(first), _ptr(conv_in), _ptr(state_in), _ptr(y), _ptr(conv_out), _ptr(state_out),
+          stream if stream is not None else _stream())

@@ -1,0 +1,1367 @@
+// Memory over time for the policies: a short causal convolution and a selective state space scan, on time-major tensors [T, N, .]
+// of N environments whose episodes begin where `first` says so (as the GAE scan's episode ends, a select: nothing before an
+// episode's first step reaches it).
+//
+//   convolution  y[t, c] = act(b[c] + sum_k w[c, k] x[t - (width - 1) + k, c])        taps of the same episode
+//   scan         h_t = e_t h_{t-1} + dt_t x_t B_t^T,  y_t = (h_t C_t + D x_t) silu(z_t),  dt = softplus(dt_raw + dt_bias), e = exp(dt a),
+//                a = -exp(a_log), per environment and head; h [head_dim, state] fp32; e_t h_{t-1} is zero where an episode begins
+//
+// The scan runs on the matrix instructions, 32 steps at a time: with l_t the sum of dt a since the chunk's (or the episode's) start,
+//   y_t = exp(l_t) C_t h_in + sum_{s <= t} exp(l_t - l_s) dt_s (C_t . B_s) x_s,   h_out = exp(l_31) h_in + sum_s exp(l_31 - l_s) dt_s B_s x_s^T.
+// Every operand that is computed here (states, decays times scores) is fp32 and enters a product as bf16 parts (split3): the results are
+// fp32 ones, rounded once where they are stored as bf16.
+#include "mlp_device.h"
+
+typedef short short4_t __attribute__((ext_vector_type(4)));
+
+#define MEM_Q 32  // time steps of a chunk
+
+static int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+__device__ inline float silu_f(float v) { return v * __builtin_amdgcn_rcpf(1.f + __expf(-v)); }
+__device__ inline float sigmoid_f(float v) { return __builtin_amdgcn_rcpf(1.f + __expf(-v)); }
+
+// V consecutive values as floats: one access of V * sizeof(T) bytes, or (V == 1) of one element
+template <typename T, int V>
+__device__ inline void load_v(const T* p, float (&v)[V]) {
+    typedef T vec_t __attribute__((ext_vector_type(V)));
+    if constexpr (V == 1) {
+        v[0] = to_f(*p);
+    } else {
+        const vec_t u = *reinterpret_cast<const vec_t*>(p);
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = (float)u[i];
+    }
+}
+template <typename T, int V>
+__device__ inline void store_v(T* p, const float (&v)[V]) {
+    typedef T vec_t __attribute__((ext_vector_type(V)));
+    if constexpr (V == 1) {
+        *p = cvt<T>(v[0]);
+    } else {
+        vec_t u;
+#pragma unroll
+        for (int i = 0; i < V; ++i) u[i] = (T)v[i];
+        *reinterpret_cast<vec_t*>(p) = u;
+    }
+}
+
+// ---- convolution ----------------------------------------------------------------------------------------------------
+#define CONV_W 4  // taps that a thread keeps: a shorter convolution's leading ones are absent
+
+struct ConvArgs {
+    const void *x, *dy;
+    const float *w, *b;
+    const uint8_t* first;
+    const void *state_in, *dstate_out;
+    void *y, *state_out, *dx, *dstate_in;
+    float *dw, *db, *part;
+    int64_t x_t, x_n, y_t, y_n;
+    int T, N, C, width, act, run, runs, nblocks;
+};
+
+// A thread takes V channels of one environment and a run of time steps, the last inputs in registers.
+template <typename T, int V>
+__global__ __launch_bounds__(256) void k_conv_fwd(ConvArgs g) {
+    const int cols = (g.C + V - 1) / V;
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int n = (int)(id / cols), c = (int)(id % cols) * V;
+    if (n >= g.N) return;
+    const int t0 = blockIdx.y * g.run, t1 = t0 + g.run < g.T ? t0 + g.run : g.T, before = g.width - 1;
+    const T* x = reinterpret_cast<const T*>(g.x) + (int64_t)n * g.x_n + c;
+    T* y = reinterpret_cast<T*>(g.y) + (int64_t)n * g.y_n + c;
+    float w[CONV_W][V], b[V], win[CONV_W][V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        b[i] = g.b ? g.b[c + i] : 0.f;
+#pragma unroll
+        for (int k = 0; k < CONV_W; ++k) {
+            w[k][i] = k >= CONV_W - g.width ? g.w[(int64_t)(c + i) * g.width + k - (CONV_W - g.width)] : 0.f;
+            win[k][i] = 0.f;
+        }
+    }
+    for (int t = t0 - before; t < t1; ++t) {
+        float v[V];
+        if (t >= 0) load_v<T, V>(x + (int64_t)t * g.x_t, v);
+        else if (g.state_in) load_v<T, V>(reinterpret_cast<const T*>(g.state_in) + ((int64_t)n * before + t + before) * g.C + c, v);
+        else
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = 0.f;
+        const bool begin = t >= 0 && g.first && g.first[(int64_t)t * g.N + n];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+#pragma unroll
+            for (int k = 0; k + 1 < CONV_W; ++k) win[k][i] = begin ? 0.f : win[k + 1][i];
+            win[CONV_W - 1][i] = v[i];
+        }
+        if (t < t0) continue;
+        float o[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            float s = b[i];
+#pragma unroll
+            for (int k = 0; k < CONV_W; ++k)
+                if (k >= CONV_W - g.width) s += w[k][i] * win[k][i];
+            o[i] = g.act ? silu_f(s) : s;
+        }
+        store_v<T, V>(y + (int64_t)t * g.y_t, o);
+    }
+    if (t1 == g.T && g.state_out)
+#pragma unroll
+        for (int k = 1; k < CONV_W; ++k)
+            if (k > CONV_W - g.width)
+                store_v<T, V>(reinterpret_cast<T*>(g.state_out) + ((int64_t)n * before + k - (CONV_W - g.width) - 1) * g.C + c, win[k]);
+}
+
+// A thread's V channels of one environment after the other (n, n + stride, ..) and a run of time steps; it walks width - 1 steps
+// beyond its run, whose gradients reach back into it.  dw and db: registers over its environments, then over the
+// environments of its workgroup, then k_conv_final over the workgroups.
+template <typename T, int V>
+__global__ __launch_bounds__(256) void k_conv_bwd(ConvArgs g, int cols, int rows) {
+    extern __shared__ float red[];  // [rows][cols V (CONV_W + 1)]
+    const int col = threadIdx.x % cols, row = threadIdx.x / cols;
+    const int c = (blockIdx.x * cols + col) * V;
+    const bool live = row < rows && c < g.C;
+    const int t0 = blockIdx.z * g.run, t1 = t0 + g.run < g.T ? t0 + g.run : g.T, before = g.width - 1;
+    float dw[CONV_W + 1][V];
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+#pragma unroll
+        for (int k = 0; k <= CONV_W; ++k) dw[k][i] = 0.f;
+    if (live) {
+        float w[CONV_W][V], b[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            b[i] = g.b ? g.b[c + i] : 0.f;
+#pragma unroll
+            for (int k = 0; k < CONV_W; ++k) w[k][i] = k >= CONV_W - g.width ? g.w[(int64_t)(c + i) * g.width + k - (CONV_W - g.width)] : 0.f;
+        }
+        for (int n = blockIdx.y * rows + row; n < g.N; n += gridDim.y * rows) {
+            const T* x = reinterpret_cast<const T*>(g.x) + (int64_t)n * g.x_n + c;
+            const T* dy = reinterpret_cast<const T*>(g.dy) + (int64_t)n * g.y_n + c;
+            T* dx = reinterpret_cast<T*>(g.dx) + (int64_t)n * g.x_n + c;
+            float win[CONV_W][V], pend[CONV_W][V];  // pend[k]: gradient so far of step t - (CONV_W - 1) + k
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+#pragma unroll
+                for (int k = 0; k < CONV_W; ++k) win[k][i] = pend[k][i] = 0.f;
+            int e = -(1 << 30);  // the step at which the episode of t began
+            // gradient of input s is complete: what the state behind the last step passes back is added
+            auto done = [&](int s, const float(&v)[V]) {
+                float o[V], d[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) o[i] = v[i];
+                if (g.dstate_out && s >= g.T - before && s >= e) {
+                    load_v<T, V>(reinterpret_cast<const T*>(g.dstate_out) + ((int64_t)n * before + s - (g.T - before)) * g.C + c, d);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) o[i] += d[i];
+                }
+                if (s >= t0 && s < t1) store_v<T, V>(dx + (int64_t)s * g.x_t, o);
+                else if (s < 0 && s >= -before && t0 == 0 && g.dstate_in)
+                    store_v<T, V>(reinterpret_cast<T*>(g.dstate_in) + ((int64_t)n * before + s + before) * g.C + c, o);
+            };
+            const int end = t1 + before < g.T ? t1 + before : g.T;
+            for (int t = t0 - before; t < end; ++t) {
+                float v[V];
+                if (t >= 0) load_v<T, V>(x + (int64_t)t * g.x_t, v);
+                else if (g.state_in) load_v<T, V>(reinterpret_cast<const T*>(g.state_in) + ((int64_t)n * before + t + before) * g.C + c, v);
+                else
+#pragma unroll
+                    for (int i = 0; i < V; ++i) v[i] = 0.f;
+                if (t >= 0 && g.first && g.first[(int64_t)t * g.N + n]) e = t;
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+#pragma unroll
+                    for (int k = 0; k + 1 < CONV_W; ++k) win[k][i] = t == e ? 0.f : win[k + 1][i];
+                    win[CONV_W - 1][i] = v[i];
+                }
+                if (t >= t0) {
+                    float d[V];
+                    load_v<T, V>(dy + (int64_t)t * g.y_t, d);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        if (g.act) {
+                            float s = b[i];
+#pragma unroll
+                            for (int k = 0; k < CONV_W; ++k)
+                                if (k >= CONV_W - g.width) s += w[k][i] * win[k][i];
+                            const float sg = sigmoid_f(s);
+                            d[i] *= sg * (1.f + s * (1.f - sg));
+                        }
+                        if (t < t1) {
+#pragma unroll
+                            for (int k = 0; k < CONV_W; ++k)
+                                if (k >= CONV_W - g.width) dw[k][i] += d[i] * win[k][i];
+                            dw[CONV_W][i] += d[i];
+                        }
+#pragma unroll
+                        for (int k = 0; k < CONV_W; ++k)
+                            if (k >= CONV_W - g.width && t - (CONV_W - 1) + k >= e) pend[k][i] += w[k][i] * d[i];
+                    }
+                }
+                done(t - (CONV_W - 1), pend[0]);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+#pragma unroll
+                    for (int k = 0; k + 1 < CONV_W; ++k) pend[k][i] = pend[k + 1][i];
+                    pend[CONV_W - 1][i] = 0.f;
+                }
+            }
+#pragma unroll
+            for (int k = 0; k + 1 < CONV_W; ++k) done(end - (CONV_W - 1) + k, pend[k]);  // (end is T, or these lie beyond the run)
+        }
+    }
+    const int per = cols * V * (CONV_W + 1);
+    if (row < rows)
+#pragma unroll
+        for (int k = 0; k <= CONV_W; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) red[row * per + k * cols * V + col * V + i] = dw[k][i];
+    __syncthreads();
+    const int blk = blockIdx.z * gridDim.y + blockIdx.y;
+    for (int i = threadIdx.x; i < per; i += 256) {
+        const int k = i / (cols * V), cc = blockIdx.x * cols * V + i % (cols * V);
+        if (cc >= g.C) continue;
+        float s = 0.f;
+        for (int r = 0; r < rows; ++r) s += red[r * per + i];
+        g.part[((int64_t)blk * (CONV_W + 1) + k) * g.C + cc] = s;
+    }
+}
+// the workgroups' sums in order
+__global__ __launch_bounds__(256) void k_conv_final(ConvArgs g) {
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i >= (CONV_W + 1) * g.C) return;
+    const int k = i / g.C, c = i % g.C;
+    float s = 0.f;
+    for (int q = 0; q < g.nblocks; ++q) s += g.part[((int64_t)q * (CONV_W + 1) + k) * g.C + c];
+    if (k == CONV_W) {
+        if (g.db) g.db[c] = s;
+    } else if (k >= CONV_W - g.width && g.dw) {
+        g.dw[(int64_t)c * g.width + k - (CONV_W - g.width)] = s;
+    }
+}
+
+// ---- scan: one wave a head of an environment ----------------------------------------------------------------------------
+struct ScanArgs {
+    const void *x, *b, *c, *dt, *z, *dy;
+    const float *a_log, *d_skip, *dt_bias;
+    const uint8_t* first;
+    const float *state_in, *dstate_out;
+    void *y, *dx, *db, *dc, *ddt, *dz;
+    float *state_out, *dstate_in, *da_log, *dd_skip, *ddt_bias;
+    float *saved;        // per (n, h): chunks + 1 states as the registers hold them
+    float *pb, *pc;      // [head block][T][N][G][S] sums of dB, dC where a group's heads need several workgroups
+    float *ph;           // [3][H][N] sums of da, dD, ddt_bias
+    int64_t x_t, x_n, z_t, z_n, dt_t, dt_n, y_t, y_n;
+    int T, N, H, P, G, S, chunks, head_blocks;
+};
+
+template <typename T> struct Planes { static constexpr int N = sizeof(T) == 4 ? 3 : 1; };
+
+// eight consecutive values of a row of which `avail` exist, as bf16 parts
+template <typename T>
+__device__ inline void load8_raw(const T* p, int avail, bool vec, float (&v)[8]) {
+    if (vec && avail >= 8) {
+        load_v<T, 8>(p, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < avail ? to_f(p[i]) : 0.f;
+    }
+}
+template <int NP>
+__device__ inline void parts8(const float (&v)[8], uint4 (&p)[NP]) {
+    if constexpr (NP == 1) {
+        p[0] = pack_chunk<bf16_t>(v);
+    } else {
+        split3(v, p);
+    }
+}
+// a += sum of products of parts i, j with i + j <= 2, smallest first
+template <int NA, int NB>
+__device__ inline void mma_p(const uint4 (&a)[NA], const uint4 (&b)[NB], float16_t& c) {
+#pragma unroll
+    for (int s = (NA + NB - 2 < 2 ? NA + NB - 2 : 2); s >= 0; --s)
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+            if (s - i >= 0 && s - i < NB) Mma32<bf16_t>::run(a[i], b[s - i], c);
+}
+__device__ inline void zero(float16_t& c) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) c[e] = 0.f;
+}
+
+// A tile of 32 time steps x 32 B columns in LDS, NP planes of bf16.  Contraction order of all products here: the sixteen indices of step
+// kk are, for lane group lg, 16 kk + 4 lg + [0, 4) and 16 kk + 8 + 4 lg + [0, 4) -- the rows that a lane of an accumulator holds, so that
+// accumulators become operands without moving between lanes.
+template <int B, int NP>
+struct Tile {
+    static constexpr int PITCH = 64 * B + 16, PLANE = 32 * PITCH, BYTES = NP * PLANE;
+    unsigned char* at;
+    // operand: row lr, contraction over the columns
+    __device__ inline void rows(int kk, uint4 (&f)[NP]) const {
+        const int lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5;
+#pragma unroll
+        for (int q = 0; q < NP; ++q) {
+            const unsigned char* s = at + q * PLANE + lr * PITCH + kk * 32 + lg * 8;
+            const uint2 u = *reinterpret_cast<const uint2*>(s), v = *reinterpret_cast<const uint2*>(s + 16);
+            f[q] = make_uint4(u.x, u.y, v.x, v.y);
+        }
+    }
+    // operand: column 32 blk + lr, contraction over the time steps
+    __device__ inline void cols(int blk, int kk, uint4 (&f)[NP]) const {
+        typedef __attribute__((address_space(3))) short4_t lds_s4;
+        const int lane = threadIdx.x & 63, lg = lane >> 5, a = lane & 15, q0 = (lane >> 4) & 1, e = a >> 2, c = a & 3;
+#pragma unroll
+        for (int q = 0; q < NP; ++q) {
+            const unsigned char* s = at + q * PLANE + (16 * kk + 4 * lg + e) * PITCH + (32 * blk + 16 * q0 + 4 * c) * 2;
+            const uint2 u = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)s));
+            const uint2 v = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(s + 8 * PITCH)));
+            f[q] = make_uint4(u.x, u.y, v.x, v.y);
+        }
+    }
+    __device__ inline void put(int row, int c8, const uint4 (&p)[NP]) const {
+#pragma unroll
+        for (int q = 0; q < NP; ++q) *reinterpret_cast<uint4*>(at + q * PLANE + row * PITCH + c8 * 16) = p[q];
+    }
+    // four consecutive values of a row (whole again: the parts of a value add up to it)
+    __device__ inline void get4(int row, int col, float (&v)[4]) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = 0.f;
+#pragma unroll
+        for (int q = NP - 1; q >= 0; --q) {
+            const uint2 u = *reinterpret_cast<const uint2*>(at + q * PLANE + row * PITCH + col * 2);
+            v[0] += __uint_as_float(u.x << 16); v[1] += __uint_as_float(u.x & 0xffff0000u);
+            v[2] += __uint_as_float(u.y << 16); v[3] += __uint_as_float(u.y & 0xffff0000u);
+        }
+    }
+    __device__ inline float get(int row, int col) const {
+        float v = 0.f;
+#pragma unroll
+        for (int q = NP - 1; q >= 0; --q)
+            v += __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(at + q * PLANE + row * PITCH + col * 2) << 16);
+        return v;
+    }
+};
+
+// the rows t0 .. t0 + cnt - 1 of a tensor into a tile (others zero); returns whether a value of this lane is undefined or infinite
+template <typename T, int B, int NP>
+__device__ inline bool stage(const Tile<B, NP>& tile, const T* base, int64_t st, int t0, int cnt, int width, bool vec) {
+    constexpr int CH = 4 * B;
+    const int lane = threadIdx.x & 63;
+    float bad = 0.f;
+#pragma unroll
+    for (int i = 0; i < CH / 2; ++i) {
+        const int row = i * (64 / CH) + lane / CH, c8 = lane % CH;
+        float v[8];
+        load8_raw(base + (int64_t)(t0 + (row < cnt ? row : 0)) * st + 8 * c8, row < cnt ? width - 8 * c8 : 0, vec, v);
+        uint4 p[NP];
+        parts8<NP>(v, p);
+        tile.put(row, c8, p);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) bad += v[k] * 0.f;
+    }
+    return !(bad == 0.f);
+}
+
+// Time steps of a chunk: lane lr (both halves alike) holds step t0 + lr.
+struct Steps {
+    float dt, raw, hi, lo;  // dt; dt_raw + dt_bias; log2 of the decay since the chunk's or the episode's start, in two parts
+    int e;                  // chunk step at which the episode of this step began, or -1: before the chunk
+    bool begins;
+};
+// small per-chunk arrays in LDS, for lanes that need them by accumulator row
+struct StepLds { float hi[32], lo[32], dt[32], w[32]; int e[32]; };
+
+template <typename T>
+__device__ inline Steps steps(const ScanArgs& g, int n, int h, int t0, int cnt, double a2, float bias, StepLds* sl) {
+    const int lane = threadIdx.x & 63, lr = lane & 31;
+    Steps s;
+    s.raw = s.dt = 0.f;
+    s.begins = false;
+    if (lr < cnt) {
+        s.raw = to_f(reinterpret_cast<const T*>(g.dt)[(int64_t)(t0 + lr) * g.dt_t + (int64_t)n * g.dt_n + h]) + bias;
+        s.dt = s.raw > 20.f ? s.raw : log1pf(expf(s.raw));
+        s.begins = g.first && g.first[(int64_t)(t0 + lr) * g.N + n];
+    }
+    const uint32_t begun = (uint32_t)__ballot(s.begins) & (uint32_t)((2ull << lr) - 1);
+    s.e = begun ? 31 - __clz(begun) : -1;
+    // in 64 bits: a difference of two sums keeps its precision whatever they have grown to
+    double l = s.begins ? 0.0 : (double)s.dt * a2;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const double up = __shfl_up(l, o, 32);
+        if (lr - o >= (s.e < 0 ? 0 : s.e)) l += up;
+    }
+    s.hi = (float)l;
+    s.lo = (float)(l - (double)s.hi);
+    if (!(__builtin_fabsf(s.lo) < __builtin_inff())) s.lo = 0.f;
+    if (lane < 32) {
+        sl->hi[lr] = s.hi;
+        sl->lo[lr] = s.lo;
+        sl->dt[lr] = s.dt;
+        sl->e[lr] = s.e;
+    }
+    return s;
+}
+__device__ inline float decay(float hi1, float lo1, float hi0, float lo0) { return __builtin_amdgcn_exp2f((hi1 - hi0) + (lo1 - lo0)); }
+__device__ inline int acc_row(int e, int lg) { return 8 * (e / 4) + 4 * lg + e % 4; }
+
+// a state [state][head_dim] of a head as accumulators: rows n, column p = lr
+template <int PB, int SB>
+struct State {
+    float16_t v[SB][PB];
+    __device__ inline void clear() {
+#pragma unroll
+        for (int s = 0; s < SB; ++s)
+#pragma unroll
+            for (int p = 0; p < PB; ++p) zero(v[s][p]);
+    }
+    // from / to [head_dim][state] in memory
+    __device__ inline void load(const float* m, int P, int S) {
+        const int lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5;
+#pragma unroll
+        for (int s = 0; s < SB; ++s)
+#pragma unroll
+            for (int p = 0; p < PB; ++p)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int nn = 32 * s + acc_row(e, lg), pp = 32 * p + lr;
+                    v[s][p][e] = nn < S && pp < P ? m[(int64_t)pp * S + nn] : 0.f;
+                }
+    }
+    __device__ inline void store(float* m, int P, int S) const {
+        const int lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5;
+#pragma unroll
+        for (int s = 0; s < SB; ++s)
+#pragma unroll
+            for (int p = 0; p < PB; ++p)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int nn = 32 * s + acc_row(e, lg), pp = 32 * p + lr;
+                    if (nn < S && pp < P) m[(int64_t)pp * S + nn] = v[s][p][e];
+                }
+    }
+    // from / to the registers' own order: whole kilobytes an access
+    __device__ inline void dump(float* m) const {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int i = 0; i < SB * PB * 4; ++i)
+            reinterpret_cast<float4*>(m)[i * 64 + lane] = make_float4(v[i / 4 / PB][i / 4 % PB][i % 4 * 4], v[i / 4 / PB][i / 4 % PB][i % 4 * 4 + 1],
+                                                                      v[i / 4 / PB][i / 4 % PB][i % 4 * 4 + 2], v[i / 4 / PB][i / 4 % PB][i % 4 * 4 + 3]);
+    }
+    __device__ inline void undump(const float* m) {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int i = 0; i < SB * PB * 4; ++i) {
+            const float4 f = reinterpret_cast<const float4*>(m)[i * 64 + lane];
+            v[i / 4 / PB][i / 4 % PB][i % 4 * 4] = f.x;
+            v[i / 4 / PB][i / 4 % PB][i % 4 * 4 + 1] = f.y;
+            v[i / 4 / PB][i / 4 % PB][i % 4 * 4 + 2] = f.z;
+            v[i / 4 / PB][i / 4 % PB][i % 4 * 4 + 3] = f.w;
+        }
+    }
+};
+// eight accumulator values (the second or first half of a block) as an operand's parts
+__device__ inline void acc_parts(const float16_t& a, int half, uint4 (&p)[3]) {
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = a[8 * half + i];
+    split3(v, p);
+}
+// the values of an operand's parts times eight factors, as parts again
+template <int NP>
+__device__ inline void scaled_parts(const uint4 (&f)[NP], const float (&w)[8], uint4 (&p)[3]) {
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = 0.f;
+#pragma unroll
+    for (int q = NP - 1; q >= 0; --q) {
+        const uint32_t u[4] = {f[q].x, f[q].y, f[q].z, f[q].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[2 * i] += __uint_as_float(u[i] << 16);
+            v[2 * i + 1] += __uint_as_float(u[i] & 0xffff0000u);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = w[i] != 0.f ? v[i] * w[i] : 0.f;  // (a step that does not count, whatever it holds)
+    split3(v, p);
+}
+__device__ inline void eight(const float* a, int kk, float (&v)[8]) {  // values of the contraction indices of step kk
+    const int lg = (threadIdx.x >> 5) & 1;
+    const float4 u = *reinterpret_cast<const float4*>(a + 16 * kk + 4 * lg), w = *reinterpret_cast<const float4*>(a + 16 * kk + 8 + 4 * lg);
+    v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w; v[4] = w.x; v[5] = w.y; v[6] = w.z; v[7] = w.w;
+}
+
+template <typename T, int PB, int SB>
+struct ScanFwdLds {
+    static constexpr int NP = Planes<T>::N;
+    static constexpr int NW = sizeof(T) == 4 ? 2 : 4;  // waves of a workgroup
+    static constexpr int X = Tile<PB, NP>::BYTES, N = Tile<SB, NP>::BYTES;
+    static constexpr int WAVE = X + 2 * N + (int)sizeof(StepLds);
+};
+
+template <typename T, int PB, int SB>
+__global__ __launch_bounds__((ScanFwdLds<T, PB, SB>::NW * 64)) void k_scan_fwd(ScanArgs g) {
+    typedef ScanFwdLds<T, PB, SB> L;
+    constexpr int NP = L::NP;
+    extern __shared__ __align__(16) unsigned char lds[];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5;
+    const int64_t id = (int64_t)blockIdx.x * L::NW + wave;
+    if (id >= (int64_t)g.N * g.H) return;
+    const int n = (int)(id / g.H), h = (int)(id % g.H), grp = h / (g.H / g.G);
+    unsigned char* own = lds + wave * L::WAVE;
+    const Tile<PB, NP> X = {own};
+    const Tile<SB, NP> B = {own + L::X}, C = {own + L::X + L::N};
+    StepLds* sl = reinterpret_cast<StepLds*>(own + L::X + 2 * L::N);
+    const T* x = reinterpret_cast<const T*>(g.x) + (int64_t)n * g.x_n + (int64_t)h * g.P;
+    const T* b = reinterpret_cast<const T*>(g.b) + (int64_t)n * g.x_n + (int64_t)grp * g.S;
+    const T* c = reinterpret_cast<const T*>(g.c) + (int64_t)n * g.x_n + (int64_t)grp * g.S;
+    auto fits = [&](const void* p, int64_t st) { return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(st * (int64_t)sizeof(T))) & 15) == 0; };
+    const bool vx = fits(x, g.x_t), vb = fits(b, g.x_t), vc = fits(c, g.x_t);
+    const double a2 = -(double)expf(g.a_log[h]) * 1.4426950408889634;
+    const float dskip = g.d_skip ? g.d_skip[h] : 0.f, bias = g.dt_bias ? g.dt_bias[h] : 0.f;
+    State<PB, SB> st;
+    if (g.state_in) st.load(g.state_in + id * g.P * g.S, g.P, g.S);
+    else st.clear();
+    const int64_t per = (int64_t)SB * PB * 1024;
+    float* saved = g.saved ? g.saved + id * (g.chunks + 1) * per : nullptr;
+    int slow = 0;  // steps to take one by one: a chunk with an undefined or infinite input, which would reach others through products with zero
+    for (int t = 0; t < g.T;) {
+        int cnt = g.T - t < MEM_Q ? g.T - t : MEM_Q;
+        if (slow) cnt = 1;
+        const bool bad = stage(X, x, g.x_t, t, cnt, g.P, vx);
+        if (__any(bad) && cnt > 1) {
+            slow = cnt;
+            continue;
+        }
+        stage(B, b, g.x_t, t, cnt, g.S, vb);
+        stage(C, c, g.x_t, t, cnt, g.S, vc);
+        const Steps s = steps<T>(g, n, h, t, cnt, a2, bias, sl);
+        // the last step's sums: decay to the chunk's end
+        const float hiq = __shfl(s.hi, 31), loq = __shfl(s.lo, 31);
+        const int eq = __shfl(s.e, 31);
+        const float w = lr >= eq ? s.dt * decay(hiq, loq, s.hi, s.lo) : 0.f;
+        if (lane < 32) sl->w[lr] = w;
+        __builtin_amdgcn_wave_barrier();
+        if (saved && t % MEM_Q == 0) st.dump(saved + (t / MEM_Q) * per);
+        // scores [s | t] and what the state gives, [p | t]
+        float16_t m, y[PB];
+        zero(m);
+#pragma unroll
+        for (int p = 0; p < PB; ++p) zero(y[p]);
+#pragma unroll
+        for (int kk = 0; kk < 2 * SB; ++kk) {
+            uint4 fb[NP], fc[NP], fh[3];
+            C.rows(kk, fc);
+            B.rows(kk, fb);
+            mma_p(fb, fc, m);
+#pragma unroll
+            for (int p = 0; p < PB; ++p) {
+                acc_parts(st.v[kk / 2][p], kk % 2, fh);
+                mma_p(fh, fc, y[p]);
+            }
+        }
+        const float in = s.e < 0 ? __builtin_amdgcn_exp2f(s.hi + s.lo) : 0.f;
+#pragma unroll
+        for (int p = 0; p < PB; ++p)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) y[p][e] = s.e < 0 ? y[p][e] * in : 0.f;
+#pragma unroll
+        for (int k4 = 0; k4 < 4; ++k4) {
+            const int r0 = 8 * k4 + 4 * lg;
+            const float4 hi = *reinterpret_cast<const float4*>(sl->hi + r0), lo = *reinterpret_cast<const float4*>(sl->lo + r0),
+                         dt = *reinterpret_cast<const float4*>(sl->dt + r0);
+            const float a[4] = {hi.x, hi.y, hi.z, hi.w}, bb[4] = {lo.x, lo.y, lo.z, lo.w}, d[4] = {dt.x, dt.y, dt.z, dt.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const bool on = r0 + i <= lr && r0 + i >= s.e;
+                m[4 * k4 + i] = on ? m[4 * k4 + i] * (d[i] * decay(s.hi, s.lo, a[i], bb[i])) : 0.f;
+            }
+        }
+        // state to the chunk's end: what is left of the old one
+        const float left = eq < 0 ? __builtin_amdgcn_exp2f(hiq + loq) : 0.f;
+#pragma unroll
+        for (int i = 0; i < SB; ++i)
+#pragma unroll
+            for (int p = 0; p < PB; ++p)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) st.v[i][p][e] = eq < 0 ? st.v[i][p][e] * left : 0.f;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            uint4 fm[3], fx[PB][NP];
+            acc_parts(m, kk, fm);
+#pragma unroll
+            for (int p = 0; p < PB; ++p) {
+                X.cols(p, kk, fx[p]);
+                mma_p(fx[p], fm, y[p]);
+            }
+            float wk[8];
+            eight(sl->w, kk, wk);
+#pragma unroll
+            for (int i = 0; i < SB; ++i) {
+                uint4 fb[NP], fw[3];
+                B.cols(i, kk, fb);
+                scaled_parts(fb, wk, fw);
+#pragma unroll
+                for (int p = 0; p < PB; ++p) mma_p(fw, fx[p], st.v[i][p]);
+            }
+        }
+        if (lr < cnt) {
+            T* yo = reinterpret_cast<T*>(g.y) + (int64_t)(t + lr) * g.y_t + (int64_t)n * g.y_n + (int64_t)h * g.P;
+            const T* zo = g.z ? reinterpret_cast<const T*>(g.z) + (int64_t)(t + lr) * g.z_t + (int64_t)n * g.z_n + (int64_t)h * g.P : nullptr;
+#pragma unroll
+            for (int p = 0; p < PB; ++p)
+#pragma unroll
+                for (int k4 = 0; k4 < 4; ++k4) {
+                    const int p0 = 32 * p + 8 * k4 + 4 * lg;
+                    float xv[4];
+                    X.get4(lr, p0, xv);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (p0 + i < g.P) {
+                            float o = y[p][4 * k4 + i] + dskip * xv[i];
+                            if (zo) o *= silu_f(to_f(zo[p0 + i]));
+                            yo[p0 + i] = cvt<T>(o);
+                        }
+                }
+        }
+        __builtin_amdgcn_wave_barrier();
+        t += cnt;
+        if (slow) --slow;
+    }
+    if (saved) st.dump(saved + (int64_t)g.chunks * per);
+    if (g.state_out) st.store(g.state_out + id * g.P * g.S, g.P, g.S);
+}
+
+// ---- backward of the scan: the chunks in reverse, a workgroup of NW waves taking heads of one group, whose dB and dC it adds up ----
+// With dh the gradient of the state behind a chunk, R[t, s] = dy_t . x_s, E[t, s] the decay between steps, u_s that to the chunk's end and q_t that
+// from its start (zero across an episode's begin):
+//   dC_t = sum_s E R dt_s B_s + q_t h_in dy_t,           dB_s = dt_s dB'_s,  dB'_s = sum_t E R C_t + u_s dh x_s,
+//   dx_s = dt_s (sum_t E (C_t . B_s) dy_t + u_s dh^T B_s) + D dy_s,   dh_in = exp(l_31) dh + sum_t q_t C_t dy_t^T,
+// and for the decays' exponents, whose gradient at step i is the sum over the pairs (t, s) that it lies between,
+//   d(dt_i a) = sum_{t >= i} (C_t . dC_t - dt_t B_t . dB'_t) + <h_out, dh>      over i's episode; zero where it begins.
+template <typename T, int PB, int SB>
+struct ScanBwdLds {
+    static constexpr int NP = Planes<T>::N;
+    static constexpr int NW = sizeof(T) == 4 ? 2 : 4;
+    static constexpr int X = Tile<PB, NP>::BYTES, N = Tile<SB, NP>::BYTES, DY = Tile<PB, 3>::BYTES;
+    static constexpr int RED = 32 * (32 * SB + 4) * 4;  // one of dB, dC of a wave, for the sum over the waves
+    static constexpr int WAVE = X + 2 * N + DY + RED + (int)sizeof(StepLds);
+};
+
+template <typename T, int PB, int SB>
+__global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(ScanArgs g) {
+    typedef ScanBwdLds<T, PB, SB> L;
+    constexpr int NP = L::NP, NW = L::NW, RP = 32 * SB + 4;
+    extern __shared__ __align__(16) unsigned char lds[];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5;
+    const int rep = g.H / g.G;
+    int blk = blockIdx.x;
+    const int hb = blk % g.head_blocks;
+    blk /= g.head_blocks;
+    const int grp = blk % g.G, n = blk / g.G;
+    const bool live = hb * NW + wave < rep;   // (a wave without a head runs along on another's inputs and leaves nothing)
+    const int h = grp * rep + (live ? hb * NW + wave : rep - 1);
+    const int64_t id = (int64_t)n * g.H + h;
+    unsigned char* own = lds + wave * L::WAVE;
+    const Tile<PB, NP> X = {own};
+    const Tile<SB, NP> B = {own + L::X}, C = {own + L::X + L::N};
+    const Tile<PB, 3> D = {own + L::X + 2 * L::N};
+    float* red = reinterpret_cast<float*>(own + L::X + 2 * L::N + L::DY);
+    StepLds* sl = reinterpret_cast<StepLds*>(own + L::X + 2 * L::N + L::DY + L::RED);
+    const T* x = reinterpret_cast<const T*>(g.x) + (int64_t)n * g.x_n + (int64_t)h * g.P;
+    const T* b = reinterpret_cast<const T*>(g.b) + (int64_t)n * g.x_n + (int64_t)grp * g.S;
+    const T* c = reinterpret_cast<const T*>(g.c) + (int64_t)n * g.x_n + (int64_t)grp * g.S;
+    const T* dy = reinterpret_cast<const T*>(g.dy) + (int64_t)n * g.y_n + (int64_t)h * g.P;
+    const T* z = g.z ? reinterpret_cast<const T*>(g.z) + (int64_t)n * g.z_n + (int64_t)h * g.P : nullptr;
+    auto fits = [&](const void* p, int64_t st) { return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(st * (int64_t)sizeof(T))) & 15) == 0; };
+    const bool vx = fits(x, g.x_t), vb = fits(b, g.x_t), vc = fits(c, g.x_t), vdy = fits(dy, g.y_t), vz = z && fits(z, g.z_t);
+    const float av = -expf(g.a_log[h]);
+    const double a2 = (double)av * 1.4426950408889634;
+    const float dskip = g.d_skip ? g.d_skip[h] : 0.f, bias = g.dt_bias ? g.dt_bias[h] : 0.f;
+    const int64_t per = (int64_t)SB * PB * 1024;
+    const float* saved = g.saved + id * (g.chunks + 1) * per;
+    // dh twice: rows n, column p, and rows p, column n -- the operand that a product needs has its contraction in the registers
+    State<PB, SB> dh1;
+    float16_t dh2[PB][SB];
+    if (g.dstate_out) {
+        dh1.load(g.dstate_out + id * g.P * g.S, g.P, g.S);
+        const float* m = g.dstate_out + id * g.P * g.S;
+#pragma unroll
+        for (int p = 0; p < PB; ++p)
+#pragma unroll
+            for (int i = 0; i < SB; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int pp = 32 * p + acc_row(e, lg), nn = 32 * i + lr;
+                    dh2[p][i][e] = nn < g.S && pp < g.P ? m[(int64_t)pp * g.S + nn] : 0.f;
+                }
+    } else {
+        dh1.clear();
+#pragma unroll
+        for (int p = 0; p < PB; ++p)
+#pragma unroll
+            for (int i = 0; i < SB; ++i) zero(dh2[p][i]);
+    }
+    float sum_a = 0.f, sum_d = 0.f, sum_b = 0.f;  // per lane: of its steps
+    float inner;                                  // <state behind the chunk, dh>
+    {
+        State<PB, SB> last;
+        last.undump(saved + (int64_t)g.chunks * per);
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < SB; ++i)
+#pragma unroll
+            for (int p = 0; p < PB; ++p)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s += last.v[i][p][e] * dh1.v[i][p][e];
+        for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
+        inner = s;
+    }
+    int slow = 0;
+    for (int t_end = g.T; t_end > 0;) {
+        const int base = (t_end - 1) / MEM_Q * MEM_Q;
+        int t = base, cnt = t_end - base;
+        if (slow) {
+            t = t_end - 1;
+            cnt = 1;
+        }
+        bool bad = stage(X, x, g.x_t, t, cnt, g.P, vx);
+        bad |= stage(B, b, g.x_t, t, cnt, g.S, vb);
+        bad |= stage(C, c, g.x_t, t, cnt, g.S, vc);
+        {   // dy silu(z), three parts
+            constexpr int CH = 4 * PB;
+            float nan = 0.f;
+#pragma unroll
+            for (int i = 0; i < CH / 2; ++i) {
+                const int row = i * (64 / CH) + lane / CH, c8 = lane % CH, r = row < cnt ? row : 0, av8 = row < cnt ? g.P - 8 * c8 : 0;
+                float v[8], zv[8];
+                load8_raw(dy + (int64_t)(t + r) * g.y_t + 8 * c8, av8, vdy, v);
+                if (z) {
+                    load8_raw(z + (int64_t)(t + r) * g.z_t + 8 * c8, av8, vz, zv);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) v[k] *= silu_f(zv[k]);
+                }
+                uint4 p[3];
+                split3(v, p);
+                D.put(row, c8, p);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) nan += v[k] * 0.f;
+            }
+            bad |= !(nan == 0.f);
+        }
+        if (__syncthreads_or(bad) && cnt > 1) {  // all waves step by step together
+            slow = cnt;
+            continue;
+        }
+        // the state before step t
+        State<PB, SB> hin;
+        hin.undump(saved + (int64_t)(base / MEM_Q) * per);
+        for (int q = base; q < t; ++q) {  // step by step: forward again from the chunk's start
+            const float raw = to_f(reinterpret_cast<const T*>(g.dt)[(int64_t)q * g.dt_t + (int64_t)n * g.dt_n + h]) + bias;
+            const float dt = raw > 20.f ? raw : log1pf(expf(raw)), e = __builtin_amdgcn_exp2f((float)((double)dt * a2));
+            const bool begins = g.first && g.first[(int64_t)q * g.N + n];
+#pragma unroll
+            for (int p = 0; p < PB; ++p) {
+                const float xv = 32 * p + lr < g.P ? to_f(x[(int64_t)q * g.x_t + 32 * p + lr]) * dt : 0.f;
+#pragma unroll
+                for (int i = 0; i < SB; ++i)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        const int nn = 32 * i + acc_row(k, lg);
+                        const float bv = nn < g.S ? to_f(b[(int64_t)q * g.x_t + nn]) : 0.f;
+                        hin.v[i][p][k] = (begins ? 0.f : e * hin.v[i][p][k]) + xv * bv;
+                    }
+            }
+        }
+        const Steps s = steps<T>(g, n, h, t, cnt, a2, bias, sl);
+        const float hiq = __shfl(s.hi, 31), loq = __shfl(s.lo, 31);
+        const int eq = __shfl(s.e, 31);
+        const float us = lr >= eq ? decay(hiq, loq, s.hi, s.lo) : 0.f;                     // to the chunk's end
+        const float qs = s.e < 0 ? __builtin_amdgcn_exp2f(s.hi + s.lo) : 0.f;              // from its start
+        if (lane < 32) sl->w[lr] = qs;
+        __builtin_amdgcn_wave_barrier();
+        // scores and dy . x in both layouts: [s | t] (lane: the later step) and [t | s] (lane: the earlier one)
+        float16_t g1, g2, r1, r2;
+        zero(g1); zero(g2); zero(r1); zero(r2);
+#pragma unroll
+        for (int kk = 0; kk < 2 * SB; ++kk) {
+            uint4 fb[NP], fc[NP];
+            C.rows(kk, fc);
+            B.rows(kk, fb);
+            mma_p(fb, fc, g1);
+            mma_p(fc, fb, g2);
+        }
+#pragma unroll
+        for (int kk = 0; kk < 2 * PB; ++kk) {
+            uint4 fx[NP], fd[3];
+            X.rows(kk, fx);
+            D.rows(kk, fd);
+            mma_p(fx, fd, r1);
+            mma_p(fd, fx, r2);
+        }
+        // m1: scores that give y [s | t]; v1: E R dt_s [s | t]; g2: E scores [t | s]; r2: E R [t | s]
+        float16_t m1;
+        float diag = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int r = acc_row(e, lg);
+            const float rhi = sl->hi[r], rlo = sl->lo[r], rdt = sl->dt[r];
+            const int re = sl->e[r];
+            if (r == lr) diag = r1[e];
+            const bool on1 = r <= lr && r >= s.e, on2 = r >= lr && lr >= re;
+            const float d1 = decay(s.hi, s.lo, rhi, rlo) * rdt, d2 = decay(rhi, rlo, s.hi, s.lo);
+            m1[e] = on1 ? g1[e] * d1 : 0.f;
+            r1[e] = on1 ? r1[e] * d1 : 0.f;
+            g2[e] = on2 ? g2[e] * d2 : 0.f;
+            r2[e] = on2 ? r2[e] * d2 : 0.f;
+        }
+        diag += __shfl_xor(diag, 32);
+        if (lr < cnt && lg == 0) sum_d += diag;
+        // dz needs y again
+        if (z && g.dz) {
+            float16_t y[PB];
+#pragma unroll
+            for (int p = 0; p < PB; ++p) zero(y[p]);
+#pragma unroll
+            for (int kk = 0; kk < 2 * SB; ++kk) {
+                uint4 fc[NP], fh[3];
+                C.rows(kk, fc);
+#pragma unroll
+                for (int p = 0; p < PB; ++p) {
+                    acc_parts(hin.v[kk / 2][p], kk % 2, fh);
+                    mma_p(fh, fc, y[p]);
+                }
+            }
+#pragma unroll
+            for (int p = 0; p < PB; ++p)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) y[p][e] = s.e < 0 ? y[p][e] * qs : 0.f;
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk) {
+                uint4 fm[3], fx[NP];
+                acc_parts(m1, kk, fm);
+#pragma unroll
+                for (int p = 0; p < PB; ++p) {
+                    X.cols(p, kk, fx);
+                    mma_p(fx, fm, y[p]);
+                }
+            }
+            if (lr < cnt && live) {
+                const T* dyo = dy + (int64_t)(t + lr) * g.y_t;
+                const T* zo = z + (int64_t)(t + lr) * g.z_t;
+                T* dzo = reinterpret_cast<T*>(g.dz) + (int64_t)(t + lr) * g.z_t + (int64_t)n * g.z_n + (int64_t)h * g.P;
+#pragma unroll
+                for (int p = 0; p < PB; ++p)
+#pragma unroll
+                    for (int k4 = 0; k4 < 4; ++k4) {
+                        const int p0 = 32 * p + 8 * k4 + 4 * lg;
+                        float xv[4];
+                        X.get4(lr, p0, xv);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (p0 + i < g.P) {
+                                const float zv = to_f(zo[p0 + i]), sg = sigmoid_f(zv);
+                                dzo[p0 + i] = cvt<T>(to_f(dyo[p0 + i]) * (y[p][4 * k4 + i] + dskip * xv[i]) * sg * (1.f + zv * (1.f - sg)));
+                            }
+                    }
+            }
+        }
+        // dx [p | s]
+        {
+            float16_t o[PB];
+#pragma unroll
+            for (int p = 0; p < PB; ++p) zero(o[p]);
+#pragma unroll
+            for (int kk = 0; kk < 2 * SB; ++kk) {
+                uint4 fb[NP], fh[3];
+                B.rows(kk, fb);
+#pragma unroll
+                for (int p = 0; p < PB; ++p) {
+                    acc_parts(dh1.v[kk / 2][p], kk % 2, fh);
+                    mma_p(fh, fb, o[p]);
+                }
+            }
+#pragma unroll
+            for (int p = 0; p < PB; ++p)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[p][e] = lr >= eq ? o[p][e] * us : 0.f;
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk) {
+                uint4 fm[3], fd[3];
+                acc_parts(g2, kk, fm);
+#pragma unroll
+                for (int p = 0; p < PB; ++p) {
+                    D.cols(p, kk, fd);
+                    mma_p(fd, fm, o[p]);
+                }
+            }
+            if (lr < cnt && live) {
+                T* dxo = reinterpret_cast<T*>(g.dx) + (int64_t)(t + lr) * g.x_t + (int64_t)n * g.x_n + (int64_t)h * g.P;
+#pragma unroll
+                for (int p = 0; p < PB; ++p)
+#pragma unroll
+                    for (int k4 = 0; k4 < 4; ++k4) {
+                        const int p0 = 32 * p + 8 * k4 + 4 * lg;
+                        float dv[4];
+                        D.get4(lr, p0, dv);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (p0 + i < g.P) dxo[p0 + i] = cvt<T>(s.dt * o[p][4 * k4 + i] + dskip * dv[i]);
+                    }
+            }
+        }
+        // dC [n | t], dB' [n | s]
+        float row_tot = 0.f, col_tot = 0.f;
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            float16_t o[SB];
+#pragma unroll
+            for (int i = 0; i < SB; ++i) zero(o[i]);
+            // contraction over p: h_in dy_t, dh x_s
+            if (which) {
+#pragma unroll
+                for (int kk = 0; kk < 2 * PB; ++kk) {
+                    uint4 fx[NP], fh[3];
+                    X.rows(kk, fx);
+#pragma unroll
+                    for (int i = 0; i < SB; ++i) {
+                        acc_parts(dh2[kk / 2][i], kk % 2, fh);
+                        mma_p(fh, fx, o[i]);
+                    }
+                }
+            } else {  // h_in has p in its lanes: its blocks are turned in LDS
+#pragma unroll
+                for (int p = 0; p < PB; ++p) {
+                    uint4 fd[2][3];
+                    D.rows(2 * p, fd[0]);
+                    D.rows(2 * p + 1, fd[1]);
+#pragma unroll
+                    for (int i = 0; i < SB; ++i) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) red[acc_row(e, lg) * 36 + lr] = hin.v[i][p][e];
+                        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                        for (int kk = 0; kk < 2; ++kk) {
+                            float v[8];
+                            uint4 fh[3];
+                            eight(red + lr * 36, kk, v);
+                            split3(v, fh);
+                            mma_p(fh, fd[kk], o[i]);
+                        }
+                        __builtin_amdgcn_wave_barrier();
+                    }
+                }
+            }
+            const float lane_scale = which ? us : qs;
+            const bool lane_on = which ? lr >= eq : s.e < 0;
+#pragma unroll
+            for (int i = 0; i < SB; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[i][e] = lane_on ? o[i][e] * lane_scale : 0.f;
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk) {
+                uint4 fv[3], f[NP];
+                acc_parts(which ? r2 : r1, kk, fv);
+#pragma unroll
+                for (int i = 0; i < SB; ++i) {
+                    if (which) C.cols(i, kk, f);
+                    else B.cols(i, kk, f);
+                    mma_p(f, fv, o[i]);
+                }
+            }
+            float tot = 0.f;
+#pragma unroll
+            for (int i = 0; i < SB; ++i)
+#pragma unroll
+                for (int k4 = 0; k4 < 4; ++k4) {
+                    const int n0 = 32 * i + 8 * k4 + 4 * lg;
+                    float v[4];
+                    if (which) B.get4(lr, n0, v);
+                    else C.get4(lr, n0, v);
+                    float4 r;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) tot += v[k] * o[i][4 * k4 + k];
+                    const float sc = live ? (which ? s.dt : 1.f) : 0.f;
+                    r.x = o[i][4 * k4] * sc; r.y = o[i][4 * k4 + 1] * sc; r.z = o[i][4 * k4 + 2] * sc; r.w = o[i][4 * k4 + 3] * sc;
+                    *reinterpret_cast<float4*>(red + lr * RP + n0) = r;
+                }
+            tot += __shfl_xor(tot, 32);
+            if (which) col_tot = tot;
+            else row_tot = tot;
+            __syncthreads();
+            for (int i = threadIdx.x; i < cnt * 32 * SB; i += NW * 64) {
+                const int tt = i / (32 * SB), nn = i % (32 * SB);
+                if (nn >= g.S) continue;
+                float v = 0.f;
+#pragma unroll
+                for (int q = 0; q < NW; ++q)
+                    if (hb * NW + q < rep) v += reinterpret_cast<const float*>(lds + q * L::WAVE + L::X + 2 * L::N + L::DY)[tt * RP + nn];
+                if (g.head_blocks == 1) {
+                    T* o2 = reinterpret_cast<T*>(which ? g.db : g.dc) + (int64_t)(t + tt) * g.x_t + (int64_t)n * g.x_n + (int64_t)grp * g.S + nn;
+                    *o2 = cvt<T>(v);
+                } else {
+                    (which ? g.pb : g.pc)[((((int64_t)hb * g.T + t + tt) * g.N + n) * g.G + grp) * g.S + nn] = v;
+                }
+            }
+            __syncthreads();
+        }
+        // gradients of the steps
+        {
+            float q = row_tot - s.dt * col_tot;
+            if (lr >= cnt) q = 0.f;
+            // sum over the later steps of the episode: step t' belongs to it while its e is not beyond this step
+            float acc = q;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const float dn = __shfl_down(acc, o, 32);
+                const int eo = __shfl_down(s.e, o, 32);
+                if (lr + o < 32 && eo <= lr) acc += dn;
+            }
+            if (lr >= eq) acc += inner;
+            if (s.begins) acc = 0.f;
+            const float ddt = col_tot + av * acc;
+            const float draw = s.raw > 20.f ? ddt : ddt * sigmoid_f(s.raw);
+            if (lr < cnt && lg == 0) {
+                sum_a += s.dt * acc;
+                sum_b += draw;
+                if (live) reinterpret_cast<T*>(g.ddt)[(int64_t)(t + lr) * g.dt_t + (int64_t)n * g.dt_n + h] = cvt<T>(draw);
+            }
+        }
+        // dh before the chunk
+        const float left = eq < 0 ? __builtin_amdgcn_exp2f(hiq + loq) : 0.f;
+#pragma unroll
+        for (int i = 0; i < SB; ++i)
+#pragma unroll
+            for (int p = 0; p < PB; ++p)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    dh1.v[i][p][e] = eq < 0 ? dh1.v[i][p][e] * left : 0.f;
+                    dh2[p][i][e] = eq < 0 ? dh2[p][i][e] * left : 0.f;
+                }
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            float qk[8];
+            eight(sl->w, kk, qk);
+            uint4 fd[PB][3];
+#pragma unroll
+            for (int p = 0; p < PB; ++p) D.cols(p, kk, fd[p]);
+#pragma unroll
+            for (int i = 0; i < SB; ++i) {
+                uint4 f[NP], fq[3];
+                C.cols(i, kk, f);
+                scaled_parts(f, qk, fq);
+#pragma unroll
+                for (int p = 0; p < PB; ++p) {
+                    mma_p(fq, fd[p], dh1.v[i][p]);
+                    mma_p(fd[p], fq, dh2[p][i]);
+                }
+            }
+        }
+        float si = 0.f;
+#pragma unroll
+        for (int i = 0; i < SB; ++i)
+#pragma unroll
+            for (int p = 0; p < PB; ++p)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) si += hin.v[i][p][e] * dh1.v[i][p][e];
+        for (int o = 32; o; o >>= 1) si += __shfl_xor(si, o);
+        inner = si;
+        __syncthreads();
+        t_end -= cnt;
+        if (slow) --slow;
+    }
+    if (!live) return;
+    if (g.dstate_in) dh1.store(g.dstate_in + id * g.P * g.S, g.P, g.S);
+    for (int o = 32; o; o >>= 1) {
+        sum_a += __shfl_xor(sum_a, o);
+        sum_d += __shfl_xor(sum_d, o);
+        sum_b += __shfl_xor(sum_b, o);
+    }
+    if (lane == 0) {
+        g.ph[(int64_t)h * g.N + n] = sum_a * av;
+        g.ph[((int64_t)g.H + h) * g.N + n] = sum_d;
+        g.ph[((int64_t)2 * g.H + h) * g.N + n] = sum_b;
+    }
+}
+
+// the sums over a group's head blocks, in order
+template <typename T>
+__global__ __launch_bounds__(256) void k_scan_bc(ScanArgs g) {
+    const int64_t per = (int64_t)g.T * g.N * g.G * g.S;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < per; i += (int64_t)gridDim.x * 256) {
+        const int s = (int)(i % g.S);
+        int64_t k = i / g.S;
+        const int grp = (int)(k % g.G);
+        k /= g.G;
+        const int n = (int)(k % g.N);
+        const int64_t t = k / g.N, to = t * g.x_t + (int64_t)n * g.x_n + (int64_t)grp * g.S + s;
+        float b = 0.f, c = 0.f;
+        for (int q = 0; q < g.head_blocks; ++q) {
+            b += g.pb[q * per + i];
+            c += g.pc[q * per + i];
+        }
+        reinterpret_cast<T*>(g.db)[to] = cvt<T>(b);
+        reinterpret_cast<T*>(g.dc)[to] = cvt<T>(c);
+    }
+}
+// gradients of a_log, D and dt_bias: a head's sums over the environments
+__global__ __launch_bounds__(256) void k_scan_heads(ScanArgs g) {
+    __shared__ float part[4];
+    const int h = blockIdx.x % g.H, which = blockIdx.x / g.H;
+    float* out = which == 0 ? g.da_log : which == 1 ? g.dd_skip : g.ddt_bias;
+    if (!out) return;
+    float s = 0.f;
+    for (int n = threadIdx.x; n < g.N; n += 256) s += g.ph[((int64_t)which * g.H + h) * g.N + n];
+    for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) out[h] = part[0] + part[1] + part[2] + part[3];
+}
+
+// ---- a single time step: convolution, state and output of a head in one launch ------------------------------------------
+struct StepArgs {
+    ScanArgs s;
+    const void *xbc, *conv_in;
+    const float *conv_w, *conv_b;
+    void* conv_out;
+    int width;
+};
+// A wave a head of an environment.  The convolution's outputs stay in fp32 in LDS; a row of the state (state values of one channel)
+// is shared by LPR lanes of four values each, or of single ones where rows are not whole 16-byte pieces.
+template <typename T>
+__global__ __launch_bounds__(256) void k_memory_step(StepArgs a, int lpr, int vec) {
+    extern __shared__ float slds[];
+    const ScanArgs& g = a.s;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int64_t id = (int64_t)blockIdx.x * 4 + wave;
+    if (id >= (int64_t)g.N * g.H) return;
+    const int n = (int)(id / g.H), h = (int)(id % g.H), rep = g.H / g.G, grp = h / rep, D = g.H * g.P;
+    const int chans = D + 2 * g.G * g.S, before = a.width - 1;
+    float* xs = slds + wave * (g.P + 2 * g.S);
+    const bool begins = g.first && g.first[n];
+    const T* row = reinterpret_cast<const T*>(a.xbc) + (int64_t)n * g.x_n;
+    for (int i = lane; i < g.P + 2 * g.S; i += 64) {
+        const int c = i < g.P ? h * g.P + i : i < g.P + g.S ? D + grp * g.S + i - g.P : D + g.G * g.S + grp * g.S + i - g.P - g.S;
+        float v = a.conv_b ? a.conv_b[c] : 0.f;
+        const bool mine = i < g.P || h == grp * rep;  // one head of a group keeps its B and C
+        for (int k = 0; k < a.width; ++k) {
+            T in = (T)0.f;
+            if (k == before) in = row[c];
+            else if (a.conv_in && !begins) in = reinterpret_cast<const T*>(a.conv_in)[((int64_t)n * before + k) * chans + c];
+            if (k == before || !begins) v += a.conv_w[(int64_t)c * a.width + k] * to_f(in);
+            if (k > 0 && mine && a.conv_out) reinterpret_cast<T*>(a.conv_out)[((int64_t)n * before + k - 1) * chans + c] = in;
+        }
+        xs[i] = silu_f(v);
+    }
+    __builtin_amdgcn_wave_barrier();
+    const float raw = to_f(reinterpret_cast<const T*>(g.dt)[(int64_t)n * g.dt_n + h]) + (g.dt_bias ? g.dt_bias[h] : 0.f);
+    const float dt = raw > 20.f ? raw : log1pf(expf(raw));
+    const float e = expf(-dt * expf(g.a_log[h])), dskip = g.d_skip ? g.d_skip[h] : 0.f;
+    const float* hi = g.state_in ? g.state_in + id * g.P * g.S : nullptr;
+    float* ho = g.state_out + id * g.P * g.S;
+    const float *bs = xs + g.P, *cs = bs + g.S;
+    const int sub = lane % lpr, per = vec ? 4 : 1;
+    for (int p0 = 0; p0 < g.P; p0 += 64 / lpr) {
+        const int p = p0 + lane / lpr;
+        float y = 0.f;
+        if (p < g.P) {
+            const float xv = dt * xs[p];
+            for (int s = sub * per; s < g.S; s += lpr * per) {
+                if (vec) {
+                    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (hi && !begins) v = *reinterpret_cast<const float4*>(hi + (int64_t)p * g.S + s);
+                    v.x = e * v.x + xv * bs[s]; v.y = e * v.y + xv * bs[s + 1]; v.z = e * v.z + xv * bs[s + 2]; v.w = e * v.w + xv * bs[s + 3];
+                    *reinterpret_cast<float4*>(ho + (int64_t)p * g.S + s) = v;
+                    y += v.x * cs[s] + v.y * cs[s + 1] + v.z * cs[s + 2] + v.w * cs[s + 3];
+                } else {
+                    const float v = (hi && !begins ? e * hi[(int64_t)p * g.S + s] : 0.f) + xv * bs[s];
+                    ho[(int64_t)p * g.S + s] = v;
+                    y += v * cs[s];
+                }
+            }
+        }
+        for (int o = lpr / 2; o; o >>= 1) y += __shfl_xor(y, o);
+        if (p < g.P && sub == 0) {
+            y += dskip * xs[p];
+            if (g.z) y *= silu_f(to_f(reinterpret_cast<const T*>(g.z)[(int64_t)n * g.z_n + (int64_t)h * g.P + p]));
+            reinterpret_cast<T*>(g.y)[(int64_t)n * g.y_n + (int64_t)h * g.P + p] = cvt<T>(y);
+        }
+    }
+}
+
+// ---- host side ------------------------------------------------------------------------------------------------------
+static bool on16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+// whether rows of 16-byte pieces do for every tensor of a convolution
+static bool conv_vec(const morlax_conv_dims& d, const ConvArgs& g) {
+    const int64_t V = d.dtype ? 8 : 4;
+    return d.channels % V == 0 && d.x_t % V == 0 && d.x_n % V == 0 && d.y_t % V == 0 && d.y_n % V == 0 && on16(g.x) && on16(g.y) && on16(g.dy) &&
+           on16(g.dx);
+}
+static void conv_runs(ConvArgs& g, int64_t threads) {
+    // runs of time steps long enough that the steps before them, read again, do not count, where there are threads enough without
+    int run = g.T;
+    while (run > 16 && threads * cdiv(g.T, run) < 256 * 1024) run = (run + 1) / 2;
+    g.run = run;
+    g.runs = (int)cdiv(g.T, run);
+}
+static ConvArgs conv_args(const morlax_conv_dims& d) {
+    ConvArgs g = {};
+    g.T = d.T; g.N = d.N; g.C = d.channels; g.width = d.width; g.act = d.act;
+    g.x_t = d.x_t; g.x_n = d.x_n; g.y_t = d.y_t; g.y_n = d.y_n;
+    return g;
+}
+#define CONV_BLOCKS 1024  // workgroups that leave sums, at most
+int64_t conv_ws_bytes(const morlax_conv_dims& d) { return (int64_t)CONV_BLOCKS * (CONV_W + 1) * d.channels * 4; }
+template <typename T, int V>
+static void conv_fwd(ConvArgs& g, hipStream_t s) {
+    const int64_t threads = cdiv(g.C, V) * g.N;
+    conv_runs(g, threads);
+    k_conv_fwd<T, V><<<dim3(cdiv(threads, 256), g.runs), 256, 0, s>>>(g);
+}
+void launch_conv_fwd(const morlax_conv_dims& d, const void* x, const float* w, const float* b, const uint8_t* first, const void* state_in, void* y,
+                     void* state_out, hipStream_t s) {
+    ConvArgs g = conv_args(d);
+    g.x = x; g.w = w; g.b = b; g.first = first; g.state_in = state_in; g.y = y; g.state_out = state_out;
+    const bool vec = conv_vec(d, g);
+    if (d.dtype) {
+        if (vec) conv_fwd<bf16_t, 8>(g, s);
+        else conv_fwd<bf16_t, 1>(g, s);
+    } else {
+        if (vec) conv_fwd<float, 4>(g, s);
+        else conv_fwd<float, 1>(g, s);
+    }
+}
+template <typename T, int V>
+static void conv_bwd(ConvArgs& g, hipStream_t s) {
+    const int chunks = (int)cdiv(g.C, V);
+    const int cols = chunks < 64 ? chunks : 64, rows = 256 / cols;
+    conv_runs(g, (int64_t)chunks * g.N);
+    if (g.runs > CONV_BLOCKS) {
+        g.run = (int)cdiv(g.T, CONV_BLOCKS);
+        g.runs = (int)cdiv(g.T, g.run);
+    }
+    int64_t by = cdiv(g.N, rows);
+    const int64_t most = CONV_BLOCKS / g.runs;
+    if (by > most) by = most;
+    g.nblocks = (int)(by * g.runs);
+    k_conv_bwd<T, V><<<dim3(cdiv(chunks, cols), by, g.runs), 256, rows * cols * V * (CONV_W + 1) * 4, s>>>(g, cols, rows);
+    k_conv_final<<<cdiv((CONV_W + 1) * (int64_t)g.C, 256), 256, 0, s>>>(g);
+}
+void launch_conv_bwd(const morlax_conv_dims& d, const void* x, const float* w, const float* b, const uint8_t* first, const void* state_in,
+                     const void* dy, const void* dstate_out, void* dx, float* dw, float* db, void* dstate_in, void* ws, hipStream_t s) {
+    ConvArgs g = conv_args(d);
+    g.x = x; g.w = w; g.b = b; g.first = first; g.state_in = state_in; g.dy = dy; g.dstate_out = dstate_out;
+    g.dx = dx; g.dw = dw; g.db = db; g.dstate_in = dstate_in; g.part = (float*)ws;
+    const bool vec = conv_vec(d, g);
+    if (d.dtype) {
+        if (vec) conv_bwd<bf16_t, 8>(g, s);
+        else conv_bwd<bf16_t, 1>(g, s);
+    } else {
+        if (vec) conv_bwd<float, 4>(g, s);
+        else conv_bwd<float, 1>(g, s);
+    }
+}
+
+static ScanArgs scan_args(const morlax_scan_dims& d) {
+    ScanArgs g = {};
+    g.T = d.T; g.N = d.N; g.H = d.heads; g.P = d.head_dim; g.G = d.groups; g.S = d.state;
+    g.x_t = d.x_t; g.x_n = d.x_n; g.z_t = d.z_t; g.z_n = d.z_n; g.dt_t = d.dt_t; g.dt_n = d.dt_n; g.y_t = d.y_t; g.y_n = d.y_n;
+    g.chunks = (int)cdiv(d.T, MEM_Q);
+    g.head_blocks = (int)cdiv(d.heads / d.groups, d.dtype ? 4 : 2);
+    return g;
+}
+int64_t scan_saved_bytes(const morlax_scan_dims& d) {
+    const int64_t blocks = cdiv(d.head_dim, 32) * cdiv(d.state, 32);
+    return (int64_t)d.N * d.heads * (cdiv(d.T, MEM_Q) + 1) * blocks * 4096;
+}
+static int64_t scan_carve(ScanArgs& g, bool back, void* ws) {
+    char* at = reinterpret_cast<char*>(ws);
+    int64_t off = 0;
+    auto take = [&](int64_t bytes) {
+        float* q = ws ? (float*)(at + off) : nullptr;
+        off += align_up(bytes, 256);
+        return q;
+    };
+    if (back) {
+        g.ph = take((int64_t)3 * g.H * g.N * 4);
+        const int64_t n = g.head_blocks > 1 ? (int64_t)g.head_blocks * g.T * g.N * g.G * g.S * 4 : 0;
+        g.pb = take(n);
+        g.pc = take(n);
+    }
+    return off > 0 ? off : 256;
+}
+int64_t scan_ws_bytes(const morlax_scan_dims& d, bool back) {
+    ScanArgs g = scan_args(d);
+    return scan_carve(g, back, nullptr);
+}
+// allows a kernel its LDS; 0 on success
+static int allow_lds(const void* kernel, int bytes) {
+    if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess) return 0;
+    (void)hipGetLastError();
+    return -1;
+}
+template <typename T, int PB, int SB>
+static int scan_fwd(const ScanArgs& g, hipStream_t s) {
+    typedef ScanFwdLds<T, PB, SB> L;
+    constexpr int lds = L::NW * L::WAVE;
+    if (allow_lds(reinterpret_cast<const void*>(k_scan_fwd<T, PB, SB>), lds) != 0) return -1;
+    k_scan_fwd<T, PB, SB><<<cdiv((int64_t)g.N * g.H, L::NW), L::NW * 64, lds, s>>>(g);
+    return 0;
+}
+template <typename T, int PB, int SB>
+static int scan_bwd(const ScanArgs& g, hipStream_t s) {
+    typedef ScanBwdLds<T, PB, SB> L;
+    constexpr int lds = L::NW * L::WAVE;
+    if (allow_lds(reinterpret_cast<const void*>(k_scan_bwd<T, PB, SB>), lds) != 0) return -1;
+    k_scan_bwd<T, PB, SB><<<(int64_t)g.N * g.G * g.head_blocks, L::NW * 64, lds, s>>>(g);
+    if (g.head_blocks > 1) {
+        int64_t nb = cdiv((int64_t)g.T * g.N * g.G * g.S, 256);
+        k_scan_bc<T><<<nb < 8192 ? nb : 8192, 256, 0, s>>>(g);
+    }
+    k_scan_heads<<<3 * g.H, 256, 0, s>>>(g);
+    return 0;
+}
+template <typename T>
+static int scan_pick(const ScanArgs& g, bool back, hipStream_t s) {
+    const bool p2 = g.P > 32, s2 = g.S > 32;
+    if (back) return p2 ? (s2 ? scan_bwd<T, 2, 2>(g, s) : scan_bwd<T, 2, 1>(g, s)) : (s2 ? scan_bwd<T, 1, 2>(g, s) : scan_bwd<T, 1, 1>(g, s));
+    return p2 ? (s2 ? scan_fwd<T, 2, 2>(g, s) : scan_fwd<T, 2, 1>(g, s)) : (s2 ? scan_fwd<T, 1, 2>(g, s) : scan_fwd<T, 1, 1>(g, s));
+}
+int launch_scan_fwd(const morlax_scan_dims& d, const void* x, const void* b, const void* c, const void* dt, const void* z, const float* a_log,
+                    const float* d_skip, const float* dt_bias, const uint8_t* first, const float* state_in, void* y, float* state_out, void* saved,
+                    void* ws, hipStream_t s) {
+    ScanArgs g = scan_args(d);
+    scan_carve(g, false, ws);
+    g.x = x; g.b = b; g.c = c; g.dt = dt; g.z = z; g.a_log = a_log; g.d_skip = d_skip; g.dt_bias = dt_bias; g.first = first;
+    g.state_in = state_in; g.y = y; g.state_out = state_out; g.saved = (float*)saved;
+    return d.dtype ? scan_pick<bf16_t>(g, false, s) : scan_pick<float>(g, false, s);
+}
+int launch_scan_bwd(const morlax_scan_dims& d, const void* x, const void* b, const void* c, const void* dt, const void* z, const float* a_log,
+                    const float* d_skip, const float* dt_bias, const uint8_t* first, const void* saved, const void* dy, const float* dstate_out,
+                    void* dx, void* db, void* dc, void* ddt, void* dz, float* da_log, float* dd_skip, float* ddt_bias, float* dstate_in, void* ws,
+                    hipStream_t s) {
+    ScanArgs g = scan_args(d);
+    scan_carve(g, true, ws);
+    g.x = x; g.b = b; g.c = c; g.dt = dt; g.z = z; g.a_log = a_log; g.d_skip = d_skip; g.dt_bias = dt_bias; g.first = first;
+    g.saved = (float*)saved; g.dy = dy; g.dstate_out = dstate_out; g.dx = dx; g.db = db; g.dc = dc; g.ddt = ddt; g.dz = dz;
+    g.da_log = da_log; g.dd_skip = dd_skip; g.ddt_bias = ddt_bias; g.dstate_in = dstate_in;
+    return d.dtype ? scan_pick<bf16_t>(g, true, s) : scan_pick<float>(g, true, s);
+}
+void launch_memory_step(const morlax_scan_dims& d, int width, const void* xbc, const void* dt, const void* z, const float* conv_w, const float* conv_b,
+                        const float* a_log, const float* d_skip, const float* dt_bias, const uint8_t* first, const void* conv_in, const float* state_in,
+                        void* y, void* conv_out, float* state_out, hipStream_t s) {
+    StepArgs a = {};
+    a.s = scan_args(d);
+    ScanArgs& g = a.s;
+    a.xbc = xbc; a.conv_in = conv_in; a.conv_w = conv_w; a.conv_b = conv_b; a.conv_out = conv_out; a.width = width;
+    g.dt = dt; g.z = z; g.a_log = a_log; g.d_skip = d_skip; g.dt_bias = dt_bias; g.first = first; g.state_in = state_in; g.y = y; g.state_out = state_out;
+    const int vec = g.S % 4 == 0;
+    int lpr = 1;
+    while (lpr < 64 && lpr * (vec ? 4 : 1) < g.S) lpr *= 2;
+    const int lds = 4 * (g.P + 2 * g.S) * 4;
+    const int64_t blocks = cdiv((int64_t)g.N * g.H, 4);
+    if (d.dtype) k_memory_step<bf16_t><<<blocks, 256, lds, s>>>(a, lpr, vec);
+    else k_memory_step<float><<<blocks, 256, lds, s>>>(a, lpr, vec);
+}

@@ -555,3 +555,141 @@ extern "C" int morlax_adapter_bwd(const morlax_adapter_dims* dims, const void* x
     launch_adapter_bwd(*dims, x, w0, A, B, index, dy, dx, dw0, dbias, dA, dB, ws, (hipStream_t)stream);
     return finish(who);
 }
+
+static int check_conv(const morlax_conv_dims* d, const char* who) {
+    if (!d) return fail(MORLAX_ERR_NULL, "%s: dims is NULL", who);
+    if (d->T < 1 || d->N < 1 || d->channels < 1 || d->width < 1)
+        return fail(MORLAX_ERR_SHAPE, "%s: T, N, channels and width must be >= 1", who);
+    if (d->width > 4) return fail(MORLAX_ERR_UNSUPPORTED, "%s: width must be <= 4 (got %d)", who, d->width);
+    if (d->act != 0 && d->act != 1) return fail(MORLAX_ERR_UNSUPPORTED, "%s: act must be 0 (none) or 1 (SiLU)", who);
+    if (d->dtype != 0 && d->dtype != 1) return fail(MORLAX_ERR_UNSUPPORTED, "%s: dtype must be 0 (fp32) or 1 (bf16)", who);
+    if (d->channels > 1 << 20) return fail(MORLAX_ERR_UNSUPPORTED, "%s: channels must be <= 2^20", who);
+    if ((d->N > 1 && (d->x_n < d->channels || d->y_n < d->channels)) || (d->T > 1 && (d->x_t < d->channels || d->y_t < d->channels)))
+        return fail(MORLAX_ERR_SHAPE, "%s: a stride is shorter than a row", who);
+    if ((int64_t)d->N * d->channels >= (int64_t)1 << 38)
+        return fail(MORLAX_ERR_UNSUPPORTED, "%s: N * channels must stay below 2^38", who);
+    return MORLAX_OK;
+}
+extern "C" int64_t morlax_conv_workspace_bytes(const morlax_conv_dims* d) {
+    if (check_conv(d, "morlax_conv_workspace_bytes") != MORLAX_OK) return -1;
+    return conv_ws_bytes(*d);
+}
+extern "C" int morlax_conv_fwd(const morlax_conv_dims* dims, const void* x, const float* w, const float* b, const uint8_t* first,
+                               const void* state_in, void* y, void* state_out, void* stream) {
+    const char* who = "morlax_conv_fwd";
+    const int rc = check_conv(dims, who);
+    if (rc != MORLAX_OK) return rc;
+    STRIDED(x, dims->dtype, who); STRIDED(y, dims->dtype, who);
+    REQ(w, who); OPT(b, who); OPT(state_in, who); OPT(state_out, who);
+    if (x == y || (state_in && state_in == state_out))
+        return fail(MORLAX_ERR_SHAPE, "%s: an output is its input", who);
+    launch_conv_fwd(*dims, x, w, b, first, state_in, y, state_out, (hipStream_t)stream);
+    return finish(who);
+}
+extern "C" int morlax_conv_bwd(const morlax_conv_dims* dims, const void* x, const float* w, const float* b, const uint8_t* first,
+                               const void* state_in, const void* dy, const void* dstate_out, void* dx, float* dw, float* db,
+                               void* dstate_in, void* ws, int64_t ws_bytes, void* stream) {
+    const char* who = "morlax_conv_bwd";
+    const int rc = check_conv(dims, who);
+    if (rc != MORLAX_OK) return rc;
+    STRIDED(x, dims->dtype, who); STRIDED(dy, dims->dtype, who); STRIDED(dx, dims->dtype, who);
+    REQ(w, who); OPT(b, who); OPT(state_in, who); OPT(dstate_out, who); OPT(dw, who); OPT(db, who); OPT(dstate_in, who);
+    if (x == dx || dy == dx || (dstate_in && (dstate_in == dstate_out || dstate_in == state_in)))
+        return fail(MORLAX_ERR_SHAPE, "%s: an output is its input", who);
+    WS(ws, ws_bytes, conv_ws_bytes(*dims), who);
+    launch_conv_bwd(*dims, x, w, b, first, state_in, dy, dstate_out, dx, dw, db, dstate_in, ws, (hipStream_t)stream);
+    return finish(who);
+}
+
+static int check_scan(const morlax_scan_dims* d, const char* who) {
+    if (!d) return fail(MORLAX_ERR_NULL, "%s: dims is NULL", who);
+    if (d->T < 1 || d->N < 1 || d->heads < 1 || d->head_dim < 1 || d->groups < 1 || d->state < 1)
+        return fail(MORLAX_ERR_SHAPE, "%s: T, N, heads, head_dim, groups and state must be >= 1", who);
+    if (d->heads % d->groups != 0) return fail(MORLAX_ERR_SHAPE, "%s: groups = %d must divide heads = %d", who, d->groups, d->heads);
+    if (d->dtype != 0 && d->dtype != 1) return fail(MORLAX_ERR_UNSUPPORTED, "%s: dtype must be 0 (fp32) or 1 (bf16)", who);
+    if (d->head_dim > 64 || d->state > 64) return fail(MORLAX_ERR_UNSUPPORTED, "%s: head_dim and state must be <= 64", who);
+    if (d->heads > 65536 || (int64_t)d->N * d->heads >= (int64_t)1 << 31)
+        return fail(MORLAX_ERR_UNSUPPORTED, "%s: heads must be <= 65536 and N * heads below 2^31", who);
+    const int64_t D = (int64_t)d->heads * d->head_dim;
+    const int64_t gs = (int64_t)d->groups * d->state, wide = D > gs ? D : gs;
+    if (d->N > 1 && (d->x_n < wide || d->y_n < D || d->dt_n < d->heads))
+        return fail(MORLAX_ERR_SHAPE, "%s: a stride between environments is shorter than a row", who);
+    if (d->T > 1 && (d->x_t < wide || d->y_t < D || d->dt_t < d->heads))
+        return fail(MORLAX_ERR_SHAPE, "%s: a stride between time steps is shorter than a row", who);
+    return MORLAX_OK;
+}
+static int check_gate(const morlax_scan_dims* d, const void* z, const char* who) {
+    if (!z) return MORLAX_OK;
+    const int64_t D = (int64_t)d->heads * d->head_dim;
+    if ((d->N > 1 && d->z_n < D) || (d->T > 1 && d->z_t < D)) return fail(MORLAX_ERR_SHAPE, "%s: a stride of z is shorter than a row", who);
+    return strided(z, d->dtype, "z", who);
+}
+extern "C" int64_t morlax_scan_saved_bytes(const morlax_scan_dims* d) {
+    if (check_scan(d, "morlax_scan_saved_bytes") != MORLAX_OK) return -1;
+    return scan_saved_bytes(*d);
+}
+extern "C" int64_t morlax_scan_workspace_bytes(const morlax_scan_dims* d, int32_t backward) {
+    if (check_scan(d, "morlax_scan_workspace_bytes") != MORLAX_OK) return -1;
+    return scan_ws_bytes(*d, backward != 0);
+}
+extern "C" int morlax_scan_fwd(const morlax_scan_dims* dims, const void* x, const void* b, const void* c, const void* dt, const void* z,
+                               const float* a_log, const float* d_skip, const float* dt_bias, const uint8_t* first,
+                               const float* state_in, void* y, float* state_out, void* saved, void* ws, int64_t ws_bytes, void* stream) {
+    const char* who = "morlax_scan_fwd";
+    int rc = check_scan(dims, who);
+    if (rc != MORLAX_OK) return rc;
+    STRIDED(x, dims->dtype, who); STRIDED(b, dims->dtype, who); STRIDED(c, dims->dtype, who); STRIDED(dt, dims->dtype, who);
+    STRIDED(y, dims->dtype, who);
+    if ((rc = check_gate(dims, z, who)) != MORLAX_OK) return rc;
+    REQ(a_log, who); OPT(d_skip, who); OPT(dt_bias, who); OPT(state_in, who); OPT(state_out, who); OPT(saved, who);
+    if (y == x || y == z) return fail(MORLAX_ERR_SHAPE, "%s: an output is its input", who);
+    WS(ws, ws_bytes, scan_ws_bytes(*dims, false), who);
+    if (launch_scan_fwd(*dims, x, b, c, dt, z, a_log, d_skip, dt_bias, first, state_in, y, state_out, saved, ws, (hipStream_t)stream) != 0)
+        return fail(MORLAX_ERR_HIP, "%s: the kernel's LDS is not available on this device", who);
+    return finish(who);
+}
+extern "C" int morlax_scan_bwd(const morlax_scan_dims* dims, const void* x, const void* b, const void* c, const void* dt, const void* z,
+                               const float* a_log, const float* d_skip, const float* dt_bias, const uint8_t* first, const void* saved,
+                               const void* dy, const float* dstate_out, void* dx, void* db, void* dc, void* ddt, void* dz,
+                               float* da_log, float* dd_skip, float* ddt_bias, float* dstate_in, void* ws, int64_t ws_bytes,
+                               void* stream) {
+    const char* who = "morlax_scan_bwd";
+    int rc = check_scan(dims, who);
+    if (rc != MORLAX_OK) return rc;
+    STRIDED(x, dims->dtype, who); STRIDED(b, dims->dtype, who); STRIDED(c, dims->dtype, who); STRIDED(dt, dims->dtype, who);
+    STRIDED(dy, dims->dtype, who); STRIDED(dx, dims->dtype, who); STRIDED(db, dims->dtype, who); STRIDED(dc, dims->dtype, who);
+    STRIDED(ddt, dims->dtype, who);
+    if ((rc = check_gate(dims, z, who)) != MORLAX_OK) return rc;
+    if ((z == nullptr) != (dz == nullptr)) return fail(MORLAX_ERR_NULL, "%s: dz goes with z, both or neither", who);
+    if (dz) STRIDED(dz, dims->dtype, who);
+    REQ(a_log, who); REQ(saved, who); OPT(d_skip, who); OPT(dt_bias, who); OPT(dstate_out, who); OPT(da_log, who); OPT(dd_skip, who);
+    OPT(ddt_bias, who); OPT(dstate_in, who);
+    if (dx == x || dx == dy || db == b || dc == c || ddt == dt || (dz && (dz == z || dz == dy)))
+        return fail(MORLAX_ERR_SHAPE, "%s: an output is its input", who);
+    WS(ws, ws_bytes, scan_ws_bytes(*dims, true), who);
+    if (launch_scan_bwd(*dims, x, b, c, dt, z, a_log, d_skip, dt_bias, first, saved, dy, dstate_out, dx, db, dc, ddt, dz, da_log, dd_skip, ddt_bias,
+                        dstate_in, ws, (hipStream_t)stream) != 0)
+        return fail(MORLAX_ERR_HIP, "%s: the kernel's LDS is not available on this device", who);
+    return finish(who);
+}
+extern "C" int morlax_memory_step(const morlax_scan_dims* dims, int32_t width, const void* xbc, const void* dt, const void* z,
+                                  const float* conv_w, const float* conv_b, const float* a_log, const float* d_skip, const float* dt_bias,
+                                  const uint8_t* first, const void* conv_in, const float* state_in, void* y, void* conv_out,
+                                  float* state_out, void* stream) {
+    const char* who = "morlax_memory_step";
+    int rc = check_scan(dims, who);
+    if (rc != MORLAX_OK) return rc;
+    if (dims->T != 1) return fail(MORLAX_ERR_SHAPE, "%s: T must be 1 (got %d)", who, dims->T);
+    if (width < 1) return fail(MORLAX_ERR_SHAPE, "%s: width must be >= 1", who);
+    if (width > 4) return fail(MORLAX_ERR_UNSUPPORTED, "%s: width must be <= 4 (got %d)", who, width);
+    if (dims->N > 1 && dims->x_n < (int64_t)dims->heads * dims->head_dim + 2 * (int64_t)dims->groups * dims->state)
+        return fail(MORLAX_ERR_SHAPE, "%s: x_n is shorter than a row of x, B and C", who);
+    STRIDED(xbc, dims->dtype, who); STRIDED(dt, dims->dtype, who); STRIDED(y, dims->dtype, who);
+    if ((rc = check_gate(dims, z, who)) != MORLAX_OK) return rc;
+    REQ(conv_w, who); OPT(conv_b, who); REQ(a_log, who); OPT(d_skip, who); OPT(dt_bias, who); OPT(conv_in, who); OPT(state_in, who);
+    OPT(conv_out, who); REQ(state_out, who);
+    if (conv_in && conv_in == conv_out) return fail(MORLAX_ERR_SHAPE, "%s: conv_out is conv_in", who);
+    launch_memory_step(*dims, width, xbc, dt, z, conv_w, conv_b, a_log, d_skip, dt_bias, first, conv_in, state_in, y, conv_out, state_out,
+                       (hipStream_t)stream);
+    return finish(who);
+}

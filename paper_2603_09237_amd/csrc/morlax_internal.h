@@ -119,4 +119,23 @@ void launch_adapter_fwd(const morlax_adapter_dims& d, const void* x, const void*
 void launch_adapter_bwd(const morlax_adapter_dims& d, const void* x, const void* w0, const void* A, const void* B, const int32_t* index,
                         const void* dy, void* dx, float* dw0, float* dbias, float* dA, float* dB, void* ws, hipStream_t s);
 
+int64_t conv_ws_bytes(const morlax_conv_dims& d);
+void launch_conv_fwd(const morlax_conv_dims& d, const void* x, const float* w, const float* b, const uint8_t* first, const void* state_in, void* y,
+                     void* state_out, hipStream_t s);
+void launch_conv_bwd(const morlax_conv_dims& d, const void* x, const float* w, const float* b, const uint8_t* first, const void* state_in,
+                     const void* dy, const void* dstate_out, void* dx, float* dw, float* db, void* dstate_in, void* ws, hipStream_t s);
+int64_t scan_saved_bytes(const morlax_scan_dims& d);
+int64_t scan_ws_bytes(const morlax_scan_dims& d, bool back);
+// 0 on success
+int launch_scan_fwd(const morlax_scan_dims& d, const void* x, const void* b, const void* c, const void* dt, const void* z, const float* a_log,
+                    const float* d_skip, const float* dt_bias, const uint8_t* first, const float* state_in, void* y, float* state_out, void* saved,
+                    void* ws, hipStream_t s);
+int launch_scan_bwd(const morlax_scan_dims& d, const void* x, const void* b, const void* c, const void* dt, const void* z, const float* a_log,
+                    const float* d_skip, const float* dt_bias, const uint8_t* first, const void* saved, const void* dy, const float* dstate_out,
+                    void* dx, void* db, void* dc, void* ddt, void* dz, float* da_log, float* dd_skip, float* ddt_bias, float* dstate_in, void* ws,
+                    hipStream_t s);
+void launch_memory_step(const morlax_scan_dims& d, int width, const void* xbc, const void* dt, const void* z, const float* conv_w, const float* conv_b,
+                        const float* a_log, const float* d_skip, const float* dt_bias, const uint8_t* first, const void* conv_in, const float* state_in,
+                        void* y, void* conv_out, float* state_out, hipStream_t s);
+
 static inline int64_t align_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
