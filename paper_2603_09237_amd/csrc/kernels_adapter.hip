@@ -29,7 +29,14 @@ struct AdArgs {
     float *u, *v;        // [M][rp]
     int32_t *seg, *perm; // [P + 2], [M]
     float *pw, *pA, *pB, *pb;  // partial sums: [split][O][I], [piece][O][r], [piece][r][I], [piece][O]
+    const int32_t* order;  // perm where rows are taken sorted by adapter (u and v are then in that order), or NULL: as they lie
     int rp, split, kchunk, pieces;
+    __device__ inline int row(int s) const { return order ? order[s] : s; }
+    // adapter of the row at position s, or -1
+    __device__ inline int adapter(int s) const {
+        const int p = s < M ? index[row(s)] : -1;
+        return p >= 0 && p < P ? p : -1;
+    }
 };
 
 // sixteen consecutive values of a matrix row, of which the first `avail` exist (the others are zero): vector loads where VEC
@@ -77,22 +84,24 @@ struct AdOperand {
     int64_t ld;
     int rows, kdim;
     bool vec;
+    const int32_t* order;  // KC: rows through it, or NULL
     uint4 reg[sizeof(T)];
 
+    __device__ inline int64_t at(int row) const { return (order ? order[row] : row) * ld; }
     __device__ inline void init(const void* b, int64_t l, int r, int k) {
         base = reinterpret_cast<const T*>(b);
-        ld = l; rows = r; kdim = k;
+        ld = l; rows = r; kdim = k; order = nullptr;
         vec = ((reinterpret_cast<uintptr_t>(b) | (uintptr_t)(l * (int64_t)sizeof(T))) & 15) == 0;
     }
     __device__ inline float elem(int row, int k) const {
         if (row >= rows || k >= kdim) return 0.f;
-        return to_f(base[KIND == KC ? (int64_t)row * ld + k : (int64_t)k * ld + row]);
+        return to_f(base[KIND == KC ? at(row) + k : (int64_t)k * ld + row]);
     }
     __device__ inline void fetch(int t0, int k0) {
         const int tid = threadIdx.x;
         if (KIND == KC) {
             const int row = t0 + tid / 2, k = k0 + 16 * (tid % 2);
-            load16(base + (int64_t)row * ld + k, row < rows ? kdim - k : 0, vec, reg);
+            load16(base + (row < rows ? at(row) : 0) + k, row < rows ? kdim - k : 0, vec, reg);
         } else {
             const int k = k0 + tid / 8, row = t0 + 16 * (tid % 8);
             load16(base + (int64_t)k * ld + row, k < kdim ? rows - row : 0, vec, reg);
@@ -160,75 +169,114 @@ struct AdFactor {
     }
 };
 
-// The adapters' part of a 32 x (32 NB) block of outputs, a lane holding row m (accumulator: columns n0 + 8 (e / 4) + 4 lg + e % 4):
-// one product of the block per adapter among its rows.  Where they are several, a product goes only to its own rows' lanes: an
-// undefined factor of one adapter stays out of the others' rows.  bf16: u as two bf16 parts (what is left out is 2^-17 of it; rounding
-// it to one would double the error of y); fp32 on the fp32 instructions.
-template <typename T, bool BWD, int NB>
-__device__ inline void ad_expand(const AdFactor<T, BWD>& F, const float* u, int rp, const int32_t* index, int P, int M, int m0, int n0,
-                                 float16_t* acc) {
-    const int lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5, m = m0 + lr;
-    int p = m < M ? index[m] : -1;
-    if (p < 0 || p >= P) p = -1;
-    uint64_t todo = __ballot(p >= 0) & 0xffffffffull;
-    if (!todo) return;
-    const bool vec = (F.r & 7) == 0;
-    const float* um = u + (int64_t)(m < M ? m : M - 1) * rp;
-    uint4 hi[2] = {}, lo[2] = {};
-    if (sizeof(T) == 2)
-        for (int s = 0; s < rp / 16; ++s) {
-            const float4 a = *reinterpret_cast<const float4*>(um + 16 * s + 8 * lg), b = *reinterpret_cast<const float4*>(um + 16 * s + 8 * lg + 4);
-            float t[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}, l[8];
-            hi[s] = pack_chunk<bf16_t>(t);
-            const uint32_t w[4] = {hi[s].x, hi[s].y, hi[s].z, hi[s].w};
+// The adapters' part of a wave's 32 x 64 outputs, a lane holding row m0 + lr (accumulator: columns n0 + 8 (e / 4) + 4 lg + e % 4): one product
+// of the block per adapter among its rows, which goes to its own rows' lanes only -- so an undefined factor of one adapter stays out of
+// the others' rows, and a row's result does not depend on whose rows lie beside it.  The next adapter's factors are requested before
+// this one's product (one after the other, 64 rows with an adapter each waited 32 times for memory: 116 us a launch of 64 x 2048 x 2048).
+// bf16: u as two bf16 parts (what is left out is 2^-17 of it; rounding it to one would double the error of y); fp32 on the fp32
+// instructions.
+template <typename T, bool BWD, int RP>
+struct AdExpand {
+    static constexpr bool BF = sizeof(T) == 2;
+    static constexpr int K16 = RP / 16, KF = RP / 2;
+    AdFactor<T, BWD> F;
+    bool vec;
+    uint4 fb[BF ? 2 * K16 : 1];
+    float ff[BF ? 1 : 2 * KF];
+    __device__ inline void fetch(int p, int n0) {
+        const int lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {  // (an infinite value has no second part)
-                const float d = t[i] - __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
-                l[i] = __builtin_fabsf(d) < __builtin_inff() ? d : 0.f;
-            }
-            lo[s] = pack_chunk<bf16_t>(l);
-        }
-    while (todo) {
-        const int q = __shfl(p, __ffsll((unsigned long long)todo) - 1);
-        const uint64_t mine = __ballot(p == q) & 0xffffffffull;
-        todo &= ~mine;
-        const bool all = mine == 0xffffffffull;
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            float16_t t = all ? acc[b] : zero16();
+        for (int b = 0; b < 2; ++b) {
             const int n = n0 + 32 * b + lr;
-            if (sizeof(T) == 2) {
-                for (int s = 0; s < rp / 16; ++s) {
-                    const uint4 f = F.frag(q, n, 16 * s + 8 * lg, vec);
-                    Mma32<bf16_t>::run(f, lo[s], t);
-                    Mma32<bf16_t>::run(f, hi[s], t);
-                }
-            } else {
-                for (int j = 0; j < F.r; j += 2)
-                    t = __builtin_amdgcn_mfma_f32_32x32x2f32(to_f(F.get(q, n, j + lg)), um[j + lg], t, 0, 0, 0);
-            }
-            if (all) acc[b] = t;
-            else
+            if constexpr (BF) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) acc[b][e] += p == q ? t[e] : 0.f;
+                for (int s = 0; s < K16; ++s) fb[b * K16 + s] = F.frag(p, n, 16 * s + 8 * lg, vec);
+            } else {
+#pragma unroll
+                for (int s = 0; s < KF; ++s) ff[b * KF + s] = to_f(F.get(p, n, KF * lg + s));
+            }
         }
     }
-}
+    __device__ inline void run(const AdArgs& g, const float* u, int m0, int n0, float16_t (&acc)[2]) {
+        const int lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5, m = m0 + lr;
+        const int p = g.adapter(m);
+        uint64_t todo = __ballot(p >= 0) & 0xffffffffull;
+        if (!todo) return;
+        vec = (F.r & 7) == 0;
+        const float* um = u + (int64_t)(m < g.M ? m : g.M - 1) * RP;
+        uint4 hi[BF ? K16 : 1], lo[BF ? K16 : 1];
+        float uf[BF ? 1 : KF];
+        if constexpr (BF) {
+#pragma unroll
+            for (int s = 0; s < K16; ++s) {
+                const float4 a = *reinterpret_cast<const float4*>(um + 16 * s + 8 * lg), b = *reinterpret_cast<const float4*>(um + 16 * s + 8 * lg + 4);
+                float t[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}, l[8];
+                hi[s] = pack_chunk<bf16_t>(t);
+                const uint32_t w[4] = {hi[s].x, hi[s].y, hi[s].z, hi[s].w};
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {  // (an infinite value has no second part)
+                    const float d = t[i] - __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+                    l[i] = __builtin_fabsf(d) < __builtin_inff() ? d : 0.f;
+                }
+                lo[s] = pack_chunk<bf16_t>(l);
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < KF; s += 4) {
+                const float4 a = *reinterpret_cast<const float4*>(um + KF * lg + s);
+                uf[s] = a.x; uf[s + 1] = a.y; uf[s + 2] = a.z; uf[s + 3] = a.w;
+            }
+        }
+        auto next = [&]() {
+            const int q = __builtin_amdgcn_readlane(p, __ffsll((unsigned long long)todo) - 1);
+            todo &= ~__ballot(p == q);
+            return q;
+        };
+        int q = next();
+        fetch(q, n0);
+        for (;;) {
+            AdExpand now = *this;
+            const int mine = q;
+            const bool more = todo != 0;
+            if (more) {
+                q = next();
+                fetch(q, n0);
+            }
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                float16_t t = zero16();
+                if constexpr (BF) {
+#pragma unroll
+                    for (int s = 0; s < K16; ++s) Mma32<bf16_t>::run(now.fb[b * K16 + s], lo[s], t);
+#pragma unroll
+                    for (int s = 0; s < K16; ++s) Mma32<bf16_t>::run(now.fb[b * K16 + s], hi[s], t);
+                } else {
+#pragma unroll
+                    for (int s = 0; s < KF; ++s) t = __builtin_amdgcn_mfma_f32_32x32x2f32(now.ff[b * KF + s], uf[s], t, 0, 0, 0);
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[b][e] += p == mine ? t[e] : 0.f;
+            }
+            if (!more) break;
+        }
+    }
+};
 
-// A wave's 32 x 64 outputs (row m0 + lr of lane lr) through a patch of LDS into whole row segments of C.
-template <typename T>
-__device__ inline void ad_store(const float16_t* acc, unsigned char* patch, T* C, int64_t ldc, int M, int N, int m0, int n0, bool vec) {
+// A wave's 32 x 64 outputs (row m0 + lr of lane lr) through a patch of LDS into whole row segments of C, rows through g.order for DX.
+#define AD_PATCH (32 * 272)
+template <typename T, bool GATHER>
+__device__ inline void ad_store(const AdArgs& g, const float16_t (&acc)[2], unsigned char* patch, T* C, int64_t ldc, int M, int N, int m0, int n0, bool vec) {
     constexpr int VE = 16 / (int)sizeof(T), PITCH = 64 * (int)sizeof(T) + 16, CH = 64 / VE;
     const int lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5;
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            unsigned char* d = patch + lr * PITCH + (32 * b + 8 * g + 4 * lg) * (int)sizeof(T);
+        for (int g4 = 0; g4 < 4; ++g4) {
+            unsigned char* d = patch + lr * PITCH + (32 * b + 8 * g4 + 4 * lg) * (int)sizeof(T);
             if (sizeof(T) == 2)
-                *reinterpret_cast<uint2*>(d) = make_uint2(pack2(acc[b][4 * g], acc[b][4 * g + 1]), pack2(acc[b][4 * g + 2], acc[b][4 * g + 3]));
+                *reinterpret_cast<uint2*>(d) = make_uint2(pack2(acc[b][4 * g4], acc[b][4 * g4 + 1]), pack2(acc[b][4 * g4 + 2], acc[b][4 * g4 + 3]));
             else
-                *reinterpret_cast<float4*>(d) = make_float4(acc[b][4 * g], acc[b][4 * g + 1], acc[b][4 * g + 2], acc[b][4 * g + 3]);
+                *reinterpret_cast<float4*>(d) = make_float4(acc[b][4 * g4], acc[b][4 * g4 + 1], acc[b][4 * g4 + 2], acc[b][4 * g4 + 3]);
         }
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
@@ -236,7 +284,7 @@ __device__ inline void ad_store(const float16_t* acc, unsigned char* patch, T* C
         const int pos = 64 * i + lane, row = pos / CH, n = n0 + (pos % CH) * VE;
         const uint4 v = *reinterpret_cast<const uint4*>(patch + row * PITCH + (pos % CH) * 16);
         if (m0 + row < M && n < N) {
-            T* d = C + (int64_t)(m0 + row) * ldc + n;
+            T* d = C + (int64_t)(GATHER ? g.row(m0 + row) : m0 + row) * ldc + n;
             if (vec && n + VE <= N) {
                 *reinterpret_cast<uint4*>(d) = v;
             } else {
@@ -250,6 +298,12 @@ __device__ inline void ad_store(const float16_t* acc, unsigned char* patch, T* C
     }
     __builtin_amdgcn_wave_barrier();
 }
+static __device__ inline bool ad_vec(const void* p, int64_t ld, int size) {
+    return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * size)) & 15) == 0;
+}
+// what a wave does with its 32 x 64 sums
+template <typename T, int ROLE, int RP>
+__device__ inline void ad_finish(const AdArgs& g, float16_t (&acc)[2], unsigned char* patch, int m0, int n0);
 
 // The three products with or of W0, on 128 x 128 tiles of four waves of 64 x 64: any size, stride and alignment.
 enum { AD_FWD = 0, AD_DX = 1, AD_DW = 2 };
@@ -258,13 +312,40 @@ template <> struct AdRole<AD_FWD> { static constexpr int KA = KC, KB = KC; };
 template <> struct AdRole<AD_DX> { static constexpr int KA = KC, KB = KS; };
 template <> struct AdRole<AD_DW> { static constexpr int KA = KS, KB = KS; };
 
-template <typename T, int ROLE>
+template <typename T, int ROLE, int RP>
+__device__ inline void ad_finish(const AdArgs& g, float16_t (&acc)[2], unsigned char* patch, int m0, int n0) {
+    const int lg = (threadIdx.x >> 5) & 1;
+    if constexpr (ROLE == AD_FWD) {
+        if (g.bias)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int n = n0 + 32 * j + 8 * (e / 4) + 4 * lg + e % 4;
+                    acc[j][e] += n < g.O ? g.bias[n] : 0.f;
+                }
+        AdExpand<T, false, RP> x;
+        x.F = {reinterpret_cast<const T*>(g.A), g.O, g.r};
+        x.run(g, g.u, m0, n0, acc);
+        ad_store<T, false>(g, acc, patch, reinterpret_cast<T*>(g.y), g.ld_y, g.M, g.O, m0, n0, ad_vec(g.y, g.ld_y, sizeof(T)));
+    } else if constexpr (ROLE == AD_DX) {
+        AdExpand<T, true, RP> x;
+        x.F = {reinterpret_cast<const T*>(g.B), g.I, g.r};
+        x.run(g, g.v, m0, n0, acc);
+        ad_store<T, true>(g, acc, patch, reinterpret_cast<T*>(g.dx), g.ld_x, g.M, g.I, m0, n0, ad_vec(g.dx, g.ld_x, sizeof(T)));
+    } else {
+        float* C = g.split > 1 ? g.pw + (int64_t)blockIdx.y * g.O * g.I : g.dw0;
+        ad_store<float, false>(g, acc, patch, C, g.I, g.O, g.I, m0, n0, (g.I & 3) == 0);
+    }
+}
+
+template <typename T, int ROLE, int RP>
 __global__ __launch_bounds__(256, 2) void k_ad_gemm(AdArgs g) {
     constexpr int KA = AdRole<ROLE>::KA, KB = AdRole<ROLE>::KB;
     typedef AdOperand<T, KA> OpA;
     typedef AdOperand<T, KB> OpB;
     constexpr int NP = OpA::NP;
-    __shared__ __align__(16) unsigned char lds[(2 * NP * OpA::PLANE > 4 * 32 * 272) ? 2 * NP * OpA::PLANE : 4 * 32 * 272];
+    __shared__ __align__(16) unsigned char lds[(2 * NP * OpA::PLANE > 4 * AD_PATCH) ? 2 * NP * OpA::PLANE : 4 * AD_PATCH];
     const int wave = threadIdx.x >> 6, lr = threadIdx.x & 31;
     const int wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
     const int rows_a = ROLE == AD_DW ? g.O : g.M, rows_b = ROLE == AD_FWD ? g.O : g.I;
@@ -281,6 +362,7 @@ __global__ __launch_bounds__(256, 2) void k_ad_gemm(AdArgs g) {
     } else if (ROLE == AD_DX) {
         kdim = g.O;
         a.init(g.dy, g.ld_y, g.M, kdim);
+        a.order = g.order;
         b.init(g.w0, g.I, g.I, kdim);
     } else {
         const int k0 = blockIdx.y * g.kchunk;
@@ -340,86 +422,347 @@ __global__ __launch_bounds__(256, 2) void k_ad_gemm(AdArgs g) {
                 }
             }
     }
-    unsigned char* patch = lds + wave * (32 * 272);
-    const int lg = (threadIdx.x >> 5) & 1;
+    unsigned char* patch = lds + wave * AD_PATCH;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int m0 = tm + wm + 32 * i, n0 = tn + wn;
-        if (ROLE == AD_FWD) {
-            if (g.bias)
+    for (int i = 0; i < 2; ++i) ad_finish<T, ROLE, RP>(g, acc[i], patch, tm + wm + 32 * i, tn + wn);
+}
+
+// ---- bf16 operands whose rows are whole 16-byte pieces: direct-to-LDS loads, three stages of 32 contraction indices -------------------
+// Tiles of 64 MB x 128, four waves of 32 MB x 64.  A stage's pieces lie as the loads leave them, one KB an instruction; which piece a lane
+// fetches is free, and the bank swizzle is there: KC, piece (row, c) of four a row at position 4 row + (c ^ row's bits 2, 3); KS, piece
+// (k, c) of ROWS / 8 a contraction index at (ROWS / 8) k + (c ^ 4 (k mod 4)), read transposed.  A contraction that is no multiple of 32
+// begins with the rest of it, loaded through registers.
+template <int KIND, int ROWS>
+struct AdTile {
+    static constexpr int NI = ROWS / 16 / 4, CPR = ROWS / 8, BYTES = ROWS * 64;
+    const char* base;
+    uint32_t voff[NI];
+    int64_t kstep;
+    __device__ inline void init(const void* b, int64_t ld, int rows, int t0, const int32_t* order) {
+        base = reinterpret_cast<const char*>(b);
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int n = n0 + 32 * j + 8 * (e / 4) + 4 * lg + e % 4;
-                        acc[i][j][e] += n < g.O ? g.bias[n] : 0.f;
-                    }
-            const AdFactor<T, false> F = {reinterpret_cast<const T*>(g.A), g.O, g.r};
-            ad_expand<T, false, 2>(F, g.u, g.rp, g.index, g.P, g.M, m0, n0, acc[i]);
-            ad_store<T>(acc[i], patch, reinterpret_cast<T*>(g.y), g.ld_y, g.M, g.O, m0, n0,
-                        ((reinterpret_cast<uintptr_t>(g.y) | (uintptr_t)(g.ld_y * (int64_t)sizeof(T))) & 15) == 0);
-        } else if (ROLE == AD_DX) {
-            const AdFactor<T, true> F = {reinterpret_cast<const T*>(g.B), g.I, g.r};
-            ad_expand<T, true, 2>(F, g.v, g.rp, g.index, g.P, g.M, m0, n0, acc[i]);
-            ad_store<T>(acc[i], patch, reinterpret_cast<T*>(g.dx), g.ld_x, g.M, g.I, m0, n0,
-                        ((reinterpret_cast<uintptr_t>(g.dx) | (uintptr_t)(g.ld_x * (int64_t)sizeof(T))) & 15) == 0);
-        } else {
-            float* C = g.split > 1 ? g.pw + (int64_t)blockIdx.y * g.O * g.I : g.dw0;
-            ad_store<float>(acc[i], patch, C, g.I, g.O, g.I, m0, n0, (g.I & 3) == 0);
+        for (int i = 0; i < NI; ++i) {
+            const int j = NI * wave + i;
+            if (KIND == KC) {
+                const int row = 16 * j + lane / 4, c = (lane % 4) ^ ((row >> 2) & 3);
+                int r = t0 + row < rows ? t0 + row : rows - 1;
+                if (order) r = order[r];
+                voff[i] = (uint32_t)r * (uint32_t)(ld * 2) + 16 * c;
+            } else {
+                const int pos = 64 * j + lane, k = pos / CPR, c = (pos % CPR) ^ (4 * (k & 3));
+                const int r = t0 + 8 * c < rows - 8 ? t0 + 8 * c : rows - 8;
+                voff[i] = (uint32_t)k * (uint32_t)(ld * 2) + (uint32_t)r * 2;
+            }
         }
+        kstep = KIND == KC ? 64 : 64 * ld;
+    }
+    __device__ inline void issue(int64_t from, uint32_t tile) const {  // from: bytes along the contraction
+        const int wave = threadIdx.x >> 6;
+#pragma unroll
+        for (int i = 0; i < NI; ++i) dma16(base + from, voff[i], __builtin_amdgcn_readfirstlane(tile + (uint32_t)(NI * wave + i) * 1024u));
+    }
+    // the first `rest` (a multiple of 8 for KC) contraction indices, zeros behind them
+    __device__ inline void put_rest(int rest, unsigned char* tile) const {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            const int j = NI * wave + i;
+            const int k = KIND == KC ? 8 * ((lane % 4) ^ (((16 * j + lane / 4) >> 2) & 3)) : (64 * j + lane) / CPR;
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (k < rest) v = *reinterpret_cast<const uint4*>(base + voff[i]);
+            *reinterpret_cast<uint4*>(tile + j * 1024 + lane * 16) = v;
+        }
+    }
+    __device__ static inline uint4 frag(const unsigned char* tile, int row0, int ks) {
+        const int lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5;
+        if (KIND == KC) {
+            const int row = row0 + lr;
+            return *reinterpret_cast<const uint4*>(tile + row * 64 + (((2 * ks + lg) ^ ((row >> 2) & 3)) * 16));
+        } else {
+            typedef __attribute__((address_space(3))) short4_t lds_s4;
+            const int a = lane & 15, q0 = (lane >> 4) & 1, e = a >> 2, c = a & 3, col = row0 + 16 * q0 + 4 * c, k = 16 * ks + 8 * lg + e;
+            const unsigned char* s = tile + (k * CPR + ((col >> 3) ^ (4 * (k & 3)))) * 16 + ((col >> 2) & 1) * 8;
+            const uint2 u0 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)s));
+            const uint2 u1 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(s + 4 * CPR * 16)));
+            return make_uint4(u0.x, u0.y, u1.x, u1.y);
+        }
+    }
+};
+template <int MB> struct AdDma {
+    static constexpr int STAGE = (64 * MB + 128) * 64, LDS = 3 * STAGE > 4 * AD_PATCH ? 3 * STAGE : 4 * AD_PATCH, LOADS = MB + 2;
+};
+
+template <int ROLE, int MB, int RP>
+__global__ __launch_bounds__(256, MB == 2 ? 3 : 2) void k_ad_gemm_dma(AdArgs g) {
+    constexpr int KA = AdRole<ROLE>::KA, KB = AdRole<ROLE>::KB, TM = 64 * MB;
+    typedef AdTile<KA, TM> TA;
+    typedef AdTile<KB, 128> TB;
+    typedef AdDma<MB> S;
+    __shared__ __align__(16) unsigned char lds[S::LDS];
+    const int wave = threadIdx.x >> 6;
+    const int wm = (wave >> 1) * 32 * MB, wn = (wave & 1) * 64;
+    const int rows_a = ROLE == AD_DW ? g.O : g.M, rows_b = ROLE == AD_FWD ? g.O : g.I;
+    const int tiles_n = (rows_b + 127) / 128, tile = xcd_remap(blockIdx.x, gridDim.x);
+    const int tm = (tile / tiles_n) * TM, tn = (tile % tiles_n) * 128;
+    TA a;
+    TB b;
+    int kdim;
+    if (ROLE == AD_FWD) {
+        kdim = g.I;
+        a.init(g.x, g.ld_x, rows_a, tm, nullptr);
+        b.init(g.w0, g.I, rows_b, tn, nullptr);
+    } else if (ROLE == AD_DX) {
+        kdim = g.O;
+        a.init(g.dy, g.ld_y, rows_a, tm, g.order);
+        b.init(g.w0, g.I, rows_b, tn, nullptr);
+    } else {
+        const int k0 = blockIdx.y * g.kchunk;
+        kdim = g.M - k0 < g.kchunk ? g.M - k0 : g.kchunk;
+        a.init(reinterpret_cast<const bf16_t*>(g.dy) + (int64_t)k0 * g.ld_y, g.ld_y, rows_a, tm, nullptr);
+        b.init(reinterpret_cast<const bf16_t*>(g.x) + (int64_t)k0 * g.ld_x, g.ld_x, rows_b, tn, nullptr);
+    }
+    const uint32_t lbase = (uint32_t)(size_t)lds;
+    const int rest = kdim & 31, steps = (kdim + 31) / 32, shift = rest ? 1 : 0;
+    const int64_t skip_a = KA == KC ? 2 * rest : a.kstep / 32 * rest, skip_b = KB == KC ? 2 * rest : b.kstep / 32 * rest;
+    auto issue = [&](int s) {
+        const uint32_t to = lbase + (uint32_t)(s % 3) * S::STAGE;
+        a.issue(skip_a + (int64_t)(s - shift) * a.kstep, to);
+        b.issue(skip_b + (int64_t)(s - shift) * b.kstep, to + TA::BYTES);
+    };
+    if (rest) {
+        a.put_rest(rest, lds);
+        b.put_rest(rest, lds + TA::BYTES);
+    } else {
+        issue(0);
+    }
+    if (steps > 1) issue(1);
+    float16_t acc[MB][2];
+#pragma unroll
+    for (int i = 0; i < MB; ++i) acc[i][0] = acc[i][1] = zero16();
+    for (int s = 0; s < steps; ++s) {
+        if (s + 1 < steps) wait_vm<S::LOADS>();
+        else wait_vm<0>();
+        __syncthreads();  // stage s is complete, and stage s - 1 free
+        if (s + 2 < steps) issue(s + 2);
+        const unsigned char *ta = lds + (s % 3) * S::STAGE, *tb = ta + TA::BYTES;
+        uint4 fa[2][MB], fb[2][2];
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) fb[ks][j] = TB::frag(tb, wn + 32 * j, ks);
+#pragma unroll
+            for (int i = 0; i < MB; ++i) fa[ks][i] = TA::frag(ta, wm + 32 * i, ks);
+        }
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) Mma32<bf16_t>::run(fb[ks][j], fa[ks][i], acc[i][j]);
+    }
+    __syncthreads();
+    unsigned char* patch = lds + wave * AD_PATCH;
+#pragma unroll
+    for (int i = 0; i < MB; ++i) ad_finish<bf16_t, ROLE, RP>(g, acc[i], patch, tm + wm + 32 * i, tn + wn);
+}
+
+// ---- few rows: every workgroup sixteen columns of the output for 64 rows, its eight waves sharing the contraction --------------------
+// Bound by the latency of its few loads and the stream of W0, each row of which is read once; operands go straight into registers, 16
+// bytes a lane, and the waves' sums meet in LDS, where the adapters' part joins them in fp32: with so few rows each may have its own.
+template <typename T>
+__device__ inline uint4 ad_piece(const T* p, int64_t stride, int avail, bool vec) {  // 16 bytes of values `stride` apart
+    constexpr int VE = 16 / (int)sizeof(T);
+    if (vec && avail >= VE) return *reinterpret_cast<const uint4*>(p);
+    T e[VE];
+#pragma unroll
+    for (int i = 0; i < VE; ++i) e[i] = i < avail ? p[i * stride] : (T)0.f;
+    return *reinterpret_cast<uint4*>(e);
+}
+template <typename T, bool BWD>
+__global__ __launch_bounds__(512) void k_ad_few(AdArgs g) {
+    constexpr int VE = 16 / (int)sizeof(T), KS_ = 4 * VE;  // contraction indices of a step
+    __shared__ float red[8][64][17];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, l16 = lane & 15, kg = lane >> 4;
+    const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 64;
+    const int K = BWD ? g.O : g.I, N = BWD ? g.I : g.O;
+    const int64_t ld = BWD ? g.ld_y : g.ld_x;
+    const T *src = reinterpret_cast<const T*>(BWD ? g.dy : g.x), *w0 = reinterpret_cast<const T*>(g.w0);
+    const bool vx = ad_vec(src, ld, sizeof(T)), vw = !BWD && ad_vec(w0, g.I, sizeof(T));
+    const int n = n0 + l16 < N ? n0 + l16 : N - 1;
+    const T* wrow = w0 + (BWD ? (int64_t)n : (int64_t)n * g.I);
+    const int64_t ws = BWD ? g.I : 1;
+    const T* xrow[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int m = m0 + 16 * i + l16;
+        xrow[i] = src + (int64_t)g.row(m < g.M ? m : g.M - 1) * ld;
+    }
+    const int blocks = (g.M - m0 + 15) / 16 < 4 ? (g.M - m0 + 15) / 16 : 4;
+    float4_t acc[4] = {};
+#pragma unroll 4
+    for (int k = wave * KS_; k < K; k += 8 * KS_) {
+        const int kk = k + VE * kg;
+        const uint4 fw = ad_piece(wrow + kk * ws, ws, K - kk, vw);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < blocks) Mma16<T>::run(fw, ad_piece(xrow[i] + kk, 1, K - kk, vx), acc[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) red[wave][16 * i + l16][4 * kg + e] = acc[i][e];
+    __syncthreads();
+    const AdFactor<T, BWD> F = {reinterpret_cast<const T*>(BWD ? g.B : g.A), N, g.r};
+    const float* u = BWD ? g.v : g.u;
+    for (int o = threadIdx.x; o < 16 * 64; o += 512) {
+        const int m = m0 + o / 16, c = n0 + o % 16;
+        if (m >= g.M || c >= N) continue;
+        float s = 0.f;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) s += red[q][o / 16][o % 16];
+        if (!BWD && g.bias) s += g.bias[c];
+        const int p = g.adapter(m);
+        if (p >= 0) {
+            float t = 0.f;
+            const T* f = F.at(p, c, 0);
+            const int64_t fs = BWD ? N : 1;
+#pragma unroll 8
+            for (int j = 0; j < g.r; ++j) t += u[(int64_t)m * g.rp + j] * to_f(f[j * fs]);
+            s += t;
+        }
+        if (BWD) reinterpret_cast<T*>(g.dx)[(int64_t)g.row(m) * g.ld_x + c] = cvt<T>(s);
+        else reinterpret_cast<T*>(g.y)[(int64_t)m * g.ld_y + c] = cvt<T>(s);
     }
 }
 
-// u (or v): the rows' products with their adapters' short factor.  A workgroup takes 32 rows, its four waves a quarter of the
-// contraction each; one pass over the rows per adapter among them.  bf16 on 32x32x16, fp32 on 32x32x2 (the factor's 32 rows are at most
-// `rank` real ones; the pass is bound by its reads).
+// ---- u (or v): the rows' products with their adapters' short factor ------------------------------------------------------------------
+// Few rows: one a workgroup, whose threads share the contraction; the factor's values are used once.
+template <typename T, bool BWD, int RP>
+__global__ __launch_bounds__(256) void k_ad_shrink_row(AdArgs g) {
+    constexpr int VE = 16 / (int)sizeof(T);
+    __shared__ float part[4][RP];
+    const int m = blockIdx.x, p = g.adapter(m), wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int K = BWD ? g.O : g.I;
+    const T* row = reinterpret_cast<const T*>(BWD ? g.dy : g.x) + (int64_t)g.row(m) * (BWD ? g.ld_y : g.ld_x);
+    float acc[RP];
+#pragma unroll
+    for (int j = 0; j < RP; ++j) acc[j] = 0.f;
+    if (p >= 0) {
+        const T* f = reinterpret_cast<const T*>(BWD ? g.A : g.B) + (int64_t)p * K * g.r;
+        if (BWD) {  // A_p [O][r]: a thread's rows of it
+            const bool vec = (g.r * (int)sizeof(T)) % 16 == 0;
+            for (int k = threadIdx.x; k < K; k += 256) {
+                const float v = to_f(row[k]);
+#pragma unroll
+                for (int j = 0; j < RP; j += VE) {
+                    const uint4 q = ad_piece(f + (int64_t)k * g.r + j, 1, g.r - j, vec);
+                    const T* e = reinterpret_cast<const T*>(&q);
+#pragma unroll
+                    for (int i = 0; i < VE; ++i) acc[j + i] += v * to_f(e[i]);
+                }
+            }
+        } else {  // B_p [r][I]
+            const bool vx = ad_vec(row, 0, sizeof(T)), vf = (K * (int)sizeof(T)) % 16 == 0;
+            for (int k = threadIdx.x * VE; k < K; k += 256 * VE) {
+                const uint4 xq = ad_piece(row + k, 1, K - k, vx);
+                const T* xe = reinterpret_cast<const T*>(&xq);
+#pragma unroll
+                for (int j = 0; j < RP; ++j) {
+                    const uint4 q = ad_piece(f + (int64_t)j * K + k, 1, j < g.r ? K - k : 0, vf);
+                    const T* e = reinterpret_cast<const T*>(&q);
+#pragma unroll
+                    for (int i = 0; i < VE; ++i) acc[j] += to_f(xe[i]) * to_f(e[i]);
+                }
+            }
+        }
+    }
+    // sums over the wave: of RP values, a lane keeps fewer and fewer
+#pragma unroll
+    for (int h = RP / 2, o = 32; h >= 1; h /= 2, o /= 2)
+#pragma unroll
+        for (int j = 0; j < h; ++j) {
+            const bool up = lane & o;
+            const float give = up ? acc[j] : acc[j + h];
+            acc[j] = (up ? acc[j + h] : acc[j]) + __shfl_xor(give, o);
+        }
+    float s = acc[0];
+#pragma unroll
+    for (int o = 64 / RP / 2; o >= 1; o /= 2) s += __shfl_xor(s, o);
+    // (the lane's value: bits 5, 4, .. of the lane select the halves of j)
+    if (lane % (64 / RP) == 0) part[wave][lane / (64 / RP)] = s;
+    __syncthreads();
+    if (threadIdx.x < RP) {
+        const int j = threadIdx.x;
+        (BWD ? g.v : g.u)[(int64_t)m * RP + j] = j < g.r && p >= 0 ? part[0][j] + part[1][j] + part[2][j] + part[3][j] : 0.f;
+    }
+}
+
+// Many rows: 32 a workgroup, its four waves a quarter of the contraction each, one pass over the rows per adapter among them.  bf16 on
+// 32x32x16, fp32 on 32x32x2 (the factor's 32 rows are at most `rank` real ones; the pass is bound by its reads).  A lane takes 64 bytes of
+// its row at a time, so a line is read whole; the backward's factor, [O][r], is turned in LDS.
 template <typename T, bool BWD>
 __global__ __launch_bounds__(256) void k_ad_shrink(AdArgs g) {
+    constexpr int VE = 16 / (int)sizeof(T), KI = 8 * VE;  // contraction indices of an iteration: four pieces of either lane group
     __shared__ float part[4][32][33];
+    __shared__ __align__(16) T turn[BWD ? 4 : 1][BWD ? KI : 1][BWD ? 32 : 1];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5;
     const int m0 = blockIdx.x * 32, m = m0 + lr;
     const int K = BWD ? g.O : g.I;
     const int64_t ld = BWD ? g.ld_y : g.ld_x;
     const T* base = reinterpret_cast<const T*>(BWD ? g.dy : g.x);
-    const bool vec = ((reinterpret_cast<uintptr_t>(base) | (uintptr_t)(ld * (int64_t)sizeof(T))) & 15) == 0;
-    const T* row = base + (int64_t)(m < g.M ? m : g.M - 1) * ld;
+    const bool vec = ad_vec(base, ld, sizeof(T));
+    const T* row = base + (int64_t)g.row(m < g.M ? m : g.M - 1) * ld;
     const T* fac = reinterpret_cast<const T*>(BWD ? g.A : g.B);
     float* out = BWD ? g.v : g.u;
-    int p = m < g.M ? g.index[m] : -1;
-    if (p < 0 || p >= g.P) p = -1;
+    const int p = g.adapter(m);
     uint64_t todo = __ballot(p >= 0) & 0xffffffffull;
-    const int kw = ((K + 63) / 64) * 16;  // contraction indices of a wave
+    const int kw = ((K + 4 * KI - 1) / (4 * KI)) * KI;  // contraction indices of a wave
     const int k0 = wave * kw, k1 = k0 + kw < K ? k0 + kw : K;
     while (todo) {
-        const int q = __shfl(p, __ffsll((unsigned long long)todo) - 1);
+        const int q = __builtin_amdgcn_readlane(p, __ffsll((unsigned long long)todo) - 1);
         const uint64_t mine = __ballot(p == q) & 0xffffffffull;
         todo &= ~mine;
-        // factor (j, k): backward A_q [O][r], forward B_q [r][I]
-        const T* f = fac + (int64_t)q * K * g.r + (BWD ? (int64_t)lr : (int64_t)(lr < g.r ? lr : 0) * K);
-        const int64_t fs = BWD ? g.r : 1;
+        const T* f = fac + (int64_t)q * K * g.r;
         const bool fv = !BWD && (K * (int)sizeof(T)) % 16 == 0;
         float16_t acc = zero16();
-        for (int k = k0; k < k1; k += 16) {
-            const int kk = k + 8 * lg;
-            T xe[8], fe[8];
-            if (vec && kk + 8 <= K) {
-#pragma unroll
-                for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(xe)[i] = reinterpret_cast<const uint4*>(row + kk)[i];
-            } else
-#pragma unroll
-                for (int i = 0; i < 8; ++i) xe[i] = kk + i < K ? row[kk + i] : (T)0.f;
-            if (fv && kk + 8 <= K) {
-#pragma unroll
-                for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(fe)[i] = reinterpret_cast<const uint4*>(f + kk)[i];
-            } else
-#pragma unroll
-                for (int i = 0; i < 8; ++i) fe[i] = kk + i < K && lr < g.r ? f[(kk + i) * fs] : (T)0.f;
-            if constexpr (sizeof(T) == 2) {
-                Mma32<bf16_t>::run(*reinterpret_cast<uint4*>(fe), *reinterpret_cast<uint4*>(xe), acc);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(fe[i], xe[i], acc, 0, 0, 0);
+        for (int k = k0; k < k1; k += KI) {
+            if (BWD) {  // KI rows of the factor, r values each, one after the other in memory
+                const int n = (k1 - k < KI ? k1 - k : KI) * g.r;
+                const T* s = f + (int64_t)k * g.r;
+                const int rr = g.r;
+                if ((rr * (int)sizeof(T)) % 16 == 0) {
+                    for (int i = lane * VE; i < n; i += 64 * VE)
+                        *reinterpret_cast<uint4*>(&turn[wave][i / rr][i % rr]) = *reinterpret_cast<const uint4*>(s + i);
+                } else {
+                    for (int i = lane; i < n; i += 64) turn[wave][i / rr][i % rr] = s[i];
+                }
+                __builtin_amdgcn_wave_barrier();
             }
+            uint4 xq[4], fq[4];
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const int kk = k + 4 * VE * lg + VE * s;
+                xq[s] = ad_piece(row + kk, 1, K - kk, vec);
+                if (!BWD) {
+                    fq[s] = ad_piece(f + (int64_t)lr * K + kk, 1, lr < g.r ? K - kk : 0, fv);
+                } else {
+                    T e[VE];
+#pragma unroll
+                    for (int i = 0; i < VE; ++i) e[i] = kk + i < K && lr < g.r ? turn[wave][kk - k + i][lr] : (T)0.f;
+                    fq[s] = *reinterpret_cast<uint4*>(e);
+                }
+            }
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                if constexpr (sizeof(T) == 2) {
+                    Mma32<bf16_t>::run(fq[s], xq[s], acc);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(chunk_f32(fq[s], i), chunk_f32(xq[s], i), acc, 0, 0, 0);
+                }
+            }
+            if (BWD) __builtin_amdgcn_wave_barrier();
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) part[wave][8 * (e / 4) + 4 * lg + e % 4][lr] = acc[e];
@@ -439,43 +782,45 @@ __global__ __launch_bounds__(256) void k_ad_shrink(AdArgs g) {
 }
 
 // Rows sorted by adapter, order kept among a preference's own: workgroup q walks the index twice, to count the rows that come
-// before its own, and to place them.  q = P: the rows without one.
+// before its own, and to place them, a wave a contiguous sixteenth of the rows.  q = P: the rows without one.
 __global__ __launch_bounds__(1024) void k_ad_plan(AdArgs g) {
-    __shared__ int s_cnt[16], s_base;
-    const int q = blockIdx.x, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-    int before = 0;
-    for (int m = tid; m < g.M; m += 1024) {
-        const int p = g.index[m];
-        before += p >= 0 && p < q;  // (q <= P, so only valid ones)
+    __shared__ int s_less[16], s_mine[16];
+    const int q = blockIdx.x, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int len = (g.M + 1023) / 1024 * 64, lo = wave * len, hi = lo + len < g.M ? lo + len : g.M;
+    int less = 0, mine = 0;
+#pragma unroll 4
+    for (int m = lo + lane; m < hi; m += 64) {
+        const int p = g.index[m], s = p >= 0 && p < g.P ? p : g.P;
+        less += s < q;
+        mine += s == q;
     }
-    for (int o = 32; o; o >>= 1) before += __shfl_xor(before, o);
-    if (lane == 0) s_cnt[wave] = before;
+    for (int o = 32; o; o >>= 1) {
+        less += __shfl_xor(less, o);
+        mine += __shfl_xor(mine, o);
+    }
+    if (lane == 0) {
+        s_less[wave] = less;
+        s_mine[wave] = mine;
+    }
     __syncthreads();
-    if (tid == 0) {
-        int s = 0;
-        for (int w = 0; w < 16; ++w) s += s_cnt[w];
-        s_base = s;
-        g.seg[q] = s;
+    int start = 0, at = 0;
+    for (int w = 0; w < 16; ++w) {
+        start += s_less[w];
+        at += w < wave ? s_mine[w] : 0;
+    }
+    if (threadIdx.x == 0) {
+        g.seg[q] = start;
         if (q == g.P) g.seg[g.P + 1] = g.M;
     }
-    __syncthreads();
-    int at = s_base;
-    for (int m0 = 0; m0 < g.M; m0 += 1024) {
-        const int m = m0 + tid;
-        int p = m < g.M ? g.index[m] : 0;
-        if (p < 0 || p >= g.P) p = g.P;
-        if (m >= g.M) p = -1;
-        const uint64_t hit = __ballot(p == q);
-        if (lane == 0) s_cnt[wave] = __popcll(hit);
-        __syncthreads();
-        int ahead = 0, total = 0;
-        for (int w = 0; w < 16; ++w) {
-            ahead += w < wave ? s_cnt[w] : 0;
-            total += s_cnt[w];
-        }
-        if (p == q) g.perm[at + ahead + __popcll(hit & ((1ull << lane) - 1))] = m;
-        at += total;
-        __syncthreads();
+    if (mine == 0) return;
+    at += start;
+#pragma unroll 4
+    for (int m0 = lo; m0 < hi; m0 += 64) {
+        const int m = m0 + lane, p = m < hi ? g.index[m] : 0;
+        const bool hit = m < hi && (p >= 0 && p < g.P ? p : g.P) == q;
+        const uint64_t hits = __ballot(hit);
+        if (hit) g.perm[at + __popcll(hits & ((1ull << lane) - 1))] = m;
+        at += __popcll(hits);
     }
 }
 
@@ -499,12 +844,16 @@ __global__ __launch_bounds__(256) void k_ad_factor_grad(AdArgs g, int col_blocks
     const int p = lo, b = c - p;
     const int s0 = g.seg[p] > b * AD_PIECE ? g.seg[p] : b * AD_PIECE;
     const int s1 = g.seg[p + 1] < (b + 1) * AD_PIECE ? g.seg[p + 1] : (b + 1) * AD_PIECE;
-    if (b < 0 || s0 >= s1) return;
+    const bool empty = b < 0 || s0 >= s1;  // no such piece: nothing but its zeros in dbias
     const bool whole = s0 == g.seg[p] && s1 == g.seg[p + 1];
     const bool is_y = (int)blockIdx.y < col_blocks_y;
     const int C = is_y ? g.O : g.I;
     const int c0 = (is_y ? blockIdx.y : blockIdx.y - col_blocks_y) * 128;
-    if (p == g.P && !is_y) return;
+    if (!is_y && (empty || p == g.P)) return;
+    if (empty) {
+        if (g.dbias && threadIdx.x < 128 && c0 + (int)threadIdx.x < C) g.pb[(int64_t)c * g.O + c0 + threadIdx.x] = 0.f;
+        return;
+    }
     const T* base = reinterpret_cast<const T*>(is_y ? g.dy : g.x);
     const int64_t ld = is_y ? g.ld_y : g.ld_x;
     const float* w = is_y ? g.u : g.v;
@@ -531,7 +880,7 @@ __global__ __launch_bounds__(256) void k_ad_factor_grad(AdArgs g, int col_blocks
                 float t[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    t[i] = m < 0 ? 0.f : j + i < g.r ? (p < g.P ? w[(int64_t)m * g.rp + j + i] : 0.f) : j + i == g.r ? 1.f : 0.f;
+                    t[i] = m < 0 ? 0.f : j + i < g.r ? (p < g.P ? w[(int64_t)(s + row) * g.rp + j + i] : 0.f) : j + i == g.r ? 1.f : 0.f;
                 uint2 parts[3];
                 split3<true>(make_uint4(__float_as_uint(t[0]), __float_as_uint(t[1]), __float_as_uint(t[2]), __float_as_uint(t[3])), parts);
 #pragma unroll
@@ -617,15 +966,20 @@ __global__ __launch_bounds__(256) void k_ad_final(AdArgs g, int64_t n_w, int64_t
         for (int c = c0; c <= c1; ++c) s += part[c * n + k];
         out[p * n + k] = s;
     } else {
-        const int o = (blockIdx.x - blocks_w - blocks_f) * 256 + threadIdx.x;
-        if (o >= g.O) return;
+        // 32 columns of dbias, eight groups of threads a contiguous eighth of the pieces each
+        __shared__ float sums[8][32];
+        const int o = (blockIdx.x - blocks_w - blocks_f) * 32 + threadIdx.x % 32, q = threadIdx.x / 32;
+        const int each = (g.pieces + 7) / 8, c1 = (q + 1) * each < g.pieces ? (q + 1) * each : g.pieces;
         float s = 0.f;
-        for (int p = 0; p <= g.P; ++p) {
-            const int s0 = g.seg[p], s1 = g.seg[p + 1];
-            if (s1 > s0)
-                for (int c = s0 / AD_PIECE + p; c <= (s1 - 1) / AD_PIECE + p; ++c) s += g.pb[(int64_t)c * g.O + o];
+        if (o < g.O)
+#pragma unroll 8
+            for (int c = q * each; c < c1; ++c) s += g.pb[(int64_t)c * g.O + o];
+        sums[q][threadIdx.x % 32] = s;
+        __syncthreads();
+        if (q == 0 && o < g.O) {
+            for (int i = 1; i < 8; ++i) s += sums[i][threadIdx.x];
+            g.dbias[o] = s;
         }
-        g.dbias[o] = s;
     }
 }
 
@@ -672,10 +1026,57 @@ int64_t adapter_ws_bytes(const morlax_adapter_dims& d, bool bwd) {
     return ad_carve(g, bwd, nullptr);
 }
 
+static bool on16(const void* p, int64_t ld, int size) { return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * size)) & 15) == 0; }
+#define AD_FEW_ROWS 512  // rows up to which u and v take a workgroup a row
+
+template <typename T, bool BWD>
+static void shrink(const AdArgs& g, hipStream_t s) {
+    if (g.M <= AD_FEW_ROWS) {
+        if (g.rp == 16) k_ad_shrink_row<T, BWD, 16><<<g.M, 256, 0, s>>>(g);
+        else k_ad_shrink_row<T, BWD, 32><<<g.M, 256, 0, s>>>(g);
+    } else {
+        k_ad_shrink<T, BWD><<<cdiv(g.M, 32), 256, 0, s>>>(g);
+    }
+}
+// Which kernel multiplies with W0.  Few rows: 16 columns a workgroup where 128 x 128 tiles would leave most CUs without one.  Else tiles:
+// direct-to-LDS loads for bf16 rows of whole 16-byte pieces within 32-bit offsets (larger tiles where those still give every CU two
+// workgroups), the general kernel for the rest.
+template <typename T, int ROLE>
+static void product(const AdArgs& g, hipStream_t s) {
+    const int rows_a = ROLE == AD_DW ? g.O : g.M, rows_b = ROLE == AD_FWD ? g.O : g.I, K = ROLE == AD_FWD ? g.I : ROLE == AD_DX ? g.O : g.M;
+    const int64_t tiles = cdiv(rows_a, 128) * cdiv(rows_b, 128);
+    const int split = ROLE == AD_DW ? g.split : 1;
+    if constexpr (ROLE != AD_DW)
+        if (tiles <= 64 && cdiv(g.M, 64) <= 65535) {
+            k_ad_few<T, ROLE == AD_DX><<<dim3(cdiv(rows_b, 16), cdiv(g.M, 64)), 512, 0, s>>>(g);
+            return;
+        }
+    if constexpr (sizeof(T) == 2) {
+        const bool x_ok = on16(g.x, g.ld_x, 2) && (int64_t)g.M * g.ld_x * 2 < (int64_t)1 << 32;
+        const bool y_ok = on16(g.dy, g.ld_y, 2) && (int64_t)g.M * g.ld_y * 2 < (int64_t)1 << 32;
+        const bool w_ok = g.I % 8 == 0;  // (d_in, d_out <= 65536: W0 has at most 2^33 bytes)
+        const bool small_w = (int64_t)g.O * g.I * 2 < (int64_t)1 << 32;
+        const bool ok = ROLE == AD_FWD ? x_ok && w_ok && small_w : ROLE == AD_DX ? y_ok && w_ok && small_w && g.O % 8 == 0 : x_ok && y_ok && w_ok && g.O % 8 == 0;
+        if (ok && K >= 32) {
+            const int64_t big = cdiv(rows_a, 256) * cdiv(rows_b, 128);
+            if (big * split >= 512) {
+                if (g.rp == 16) k_ad_gemm_dma<ROLE, 4, 16><<<dim3(big, split), 256, 0, s>>>(g);
+                else k_ad_gemm_dma<ROLE, 4, 32><<<dim3(big, split), 256, 0, s>>>(g);
+            } else {
+                if (g.rp == 16) k_ad_gemm_dma<ROLE, 2, 16><<<dim3(tiles, split), 256, 0, s>>>(g);
+                else k_ad_gemm_dma<ROLE, 2, 32><<<dim3(tiles, split), 256, 0, s>>>(g);
+            }
+            return;
+        }
+    }
+    if (g.rp == 16) k_ad_gemm<T, ROLE, 16><<<dim3(tiles, split), 256, 0, s>>>(g);
+    else k_ad_gemm<T, ROLE, 32><<<dim3(tiles, split), 256, 0, s>>>(g);
+}
+
 template <typename T>
 static void fwd(const AdArgs& g, hipStream_t s) {
-    k_ad_shrink<T, false><<<cdiv(g.M, 32), 256, 0, s>>>(g);
-    k_ad_gemm<T, AD_FWD><<<cdiv(g.M, 128) * cdiv(g.O, 128), 256, 0, s>>>(g);
+    shrink<T, false>(g, s);
+    product<T, AD_FWD>(g, s);
 }
 void launch_adapter_fwd(const morlax_adapter_dims& d, const void* x, const void* w0, const float* bias, const void* A, const void* B,
                         const int32_t* index, void* y, void* ws, hipStream_t s) {
@@ -688,22 +1089,25 @@ void launch_adapter_fwd(const morlax_adapter_dims& d, const void* x, const void*
 }
 
 template <typename T>
-static void bwd(const AdArgs& g, hipStream_t s) {
+static void bwd(AdArgs& g, hipStream_t s) {
     const bool factors = g.dA || g.dB || g.dbias;
-    if (g.M > 0) {
-        if (g.dA) k_ad_shrink<T, false><<<cdiv(g.M, 32), 256, 0, s>>>(g);
-        if (g.dx || g.dB) k_ad_shrink<T, true><<<cdiv(g.M, 32), 256, 0, s>>>(g);
-        if (g.dx) k_ad_gemm<T, AD_DX><<<cdiv(g.M, 128) * cdiv(g.I, 128), 256, 0, s>>>(g);
-    }
-    if (g.dw0) k_ad_gemm<T, AD_DW><<<dim3(cdiv(g.O, 128) * cdiv(g.I, 128), g.split), 256, 0, s>>>(g);
-    if (factors) {
+    if (factors || g.dx) {
         k_ad_plan<<<g.P + 1, 1024, 0, s>>>(g);
+        g.order = g.perm;
+    }
+    if (g.M > 0) {
+        if (g.dA) shrink<T, false>(g, s);
+        if (g.dx || g.dB) shrink<T, true>(g, s);
+        if (g.dx) product<T, AD_DX>(g, s);
+    }
+    if (g.dw0) product<T, AD_DW>(g, s);
+    if (factors) {
         const int by = g.dA || g.dbias ? (int)cdiv(g.O, 128) : 0, bx = g.dB ? (int)cdiv(g.I, 128) : 0;
         if (g.r < 32) k_ad_factor_grad<T, 1><<<dim3(g.pieces, by + bx), 256, 0, s>>>(g, by);
         else k_ad_factor_grad<T, 2><<<dim3(g.pieces, by + bx), 256, 0, s>>>(g, by);
     }
     const int64_t n_w = g.dw0 && g.split > 1 ? (int64_t)g.O * g.I : 0, n_f = g.dA || g.dB ? (int64_t)g.P * g.r * (g.O + g.I) : 0;
-    const int64_t bw = cdiv(n_w, 256), bf = cdiv(n_f, 256), bb = g.dbias ? cdiv(g.O, 256) : 0;
+    const int64_t bw = cdiv(n_w, 256), bf = cdiv(n_f, 256), bb = g.dbias ? cdiv(g.O, 32) : 0;
     if (bw + bf + bb > 0) k_ad_final<<<bw + bf + bb, 256, 0, s>>>(g, n_w, n_f, (int)bw, (int)bf);
 }
 void launch_adapter_bwd(const morlax_adapter_dims& d, const void* x, const void* w0, const void* A, const void* B, const int32_t* index,
