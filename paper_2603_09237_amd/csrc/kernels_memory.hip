@@ -16,6 +16,20 @@ typedef short short4_t __attribute__((ext_vector_type(4)));
 
 #define MEM_Q 32  // time steps of a chunk
 
+// The end of a phase of a chunk's work: what one lane left in LDS is there for the others, and no instruction moves across (left to itself
+// the scheduler starts every phase's reads at once, and hundreds of registers spill).
+__device__ inline void phase() {
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+}
+// The lane, as a value that the compiler cannot know to be the same in the next chunk: or it computes the addresses of all of a chunk's
+// accesses once, ahead of the loop, and keeps some hundred of them in registers.
+__device__ inline int lane_now() {
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
+
 static int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 __device__ inline float silu_f(float v) { return v * __builtin_amdgcn_rcpf(1.f + __expf(-v)); }
@@ -251,21 +265,34 @@ struct ScanArgs {
     float *state_out, *dstate_in, *da_log, *dd_skip, *ddt_bias;
     float *saved;        // per (n, h): chunks + 1 states as the registers hold them
     float *pb, *pc;      // [head block][T][N][G][S] sums of dB, dC where a group's heads need several workgroups
-    float *ph;           // [3][H][N] sums of da, dD, ddt_bias
+    float *ph;           // [3][H][N][spans] sums of da, dD, ddt_bias
+    float *ends;         // [N H][spans] states that a span leaves or takes over, as the registers hold them
+    float *left;         // [N H][spans] what is left of a state over a span
     int64_t x_t, x_n, z_t, z_n, dt_t, dt_n, y_t, y_n;
     int T, N, H, P, G, S, chunks, head_blocks;
+    int span, spans;     // time steps that one wave takes, a multiple of MEM_Q, and their number
 };
 
 template <typename T> struct Planes { static constexpr int N = sizeof(T) == 4 ? 3 : 1; };
 
-// eight consecutive values of a row of which `avail` exist, as bf16 parts
+// Eight consecutive values of a row of `width` at column 8 c8, zero where the row ends or `on` is false.  No branch goes by the lane: rows that
+// are whole pieces of eight take one access (to the start of a row that exists, where there is none), others one a value.  (16-byte
+// accesses need the alignment of one element only.)
 template <typename T>
-__device__ inline void load8_raw(const T* p, int avail, bool vec, float (&v)[8]) {
-    if (vec && avail >= 8) {
-        load_v<T, 8>(p, v);
+__device__ inline void load8_raw(const T* row0, int64_t off, int c8, int width, bool on, float (&v)[8]) {
+    typedef T vec_t __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+    if (width % 8 == 0) {
+        const bool have = on && 8 * c8 < width;
+        const vec_t u = *reinterpret_cast<const vec_t*>(row0 + (have ? off + 8 * c8 : 0));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = have ? (float)u[i] : 0.f;
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < avail ? to_f(p[i]) : 0.f;
+        for (int i = 0; i < 8; ++i) {
+            const bool have = on && 8 * c8 + i < width;
+            const float e = to_f(row0[have ? off + 8 * c8 + i : 0]);
+            v[i] = have ? e : 0.f;
+        }
     }
 }
 template <int NP>
@@ -299,7 +326,7 @@ struct Tile {
     unsigned char* at;
     // operand: row lr, contraction over the columns
     __device__ inline void rows(int kk, uint4 (&f)[NP]) const {
-        const int lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5;
+        const int lane = lane_now(), lr = lane & 31, lg = lane >> 5;
 #pragma unroll
         for (int q = 0; q < NP; ++q) {
             const unsigned char* s = at + q * PLANE + lr * PITCH + kk * 32 + lg * 8;
@@ -345,17 +372,42 @@ struct Tile {
 
 // the rows t0 .. t0 + cnt - 1 of a tensor into a tile (others zero); returns whether a value of this lane is undefined or infinite
 template <typename T, int B, int NP>
-__device__ inline bool stage(const Tile<B, NP>& tile, const T* base, int64_t st, int t0, int cnt, int width, bool vec) {
+__device__ inline bool stage(const Tile<B, NP>& tile, const T* base, int64_t st, int t0, int cnt, int width) {
     constexpr int CH = 4 * B;
-    const int lane = threadIdx.x & 63;
+    const int lane = lane_now();
+    const T* row0 = base + (int64_t)t0 * st;
     float bad = 0.f;
 #pragma unroll
     for (int i = 0; i < CH / 2; ++i) {
         const int row = i * (64 / CH) + lane / CH, c8 = lane % CH;
         float v[8];
-        load8_raw(base + (int64_t)(t0 + (row < cnt ? row : 0)) * st + 8 * c8, row < cnt ? width - 8 * c8 : 0, vec, v);
+        load8_raw(row0, row * st, c8, width, row < cnt, v);
         uint4 p[NP];
         parts8<NP>(v, p);
+        tile.put(row, c8, p);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) bad += v[k] * 0.f;
+    }
+    return !(bad == 0.f);
+}
+// dy silu(z) (z NULL: dy) of a chunk, in three parts
+template <typename T, int PB>
+__device__ inline bool stage_dy(const Tile<PB, 3>& tile, const T* dy, int64_t st, const T* z, int64_t zt, int t0, int cnt, int width) {
+    constexpr int CH = 4 * PB;
+    const int lane = lane_now();
+    float bad = 0.f;
+#pragma unroll
+    for (int i = 0; i < CH / 2; ++i) {
+        const int row = i * (64 / CH) + lane / CH, c8 = lane % CH;
+        float v[8], zv[8];
+        load8_raw(dy + (int64_t)t0 * st, row * st, c8, width, row < cnt, v);
+        if (z) {
+            load8_raw(z + (int64_t)t0 * zt, row * zt, c8, width, row < cnt, zv);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] *= silu_f(zv[k]);
+        }
+        uint4 p[3];
+        split3(v, p);
         tile.put(row, c8, p);
 #pragma unroll
         for (int k = 0; k < 8; ++k) bad += v[k] * 0.f;
@@ -374,15 +426,15 @@ struct StepLds { float hi[32], lo[32], dt[32], w[32]; int e[32]; };
 
 template <typename T>
 __device__ inline Steps steps(const ScanArgs& g, int n, int h, int t0, int cnt, double a2, float bias, StepLds* sl) {
-    const int lane = threadIdx.x & 63, lr = lane & 31;
+    const int lane = lane_now(), lr = lane & 31;
     Steps s;
-    s.raw = s.dt = 0.f;
+    const int r = lr < cnt ? lr : 0;
+    const float raw = to_f(reinterpret_cast<const T*>(g.dt)[(int64_t)(t0 + r) * g.dt_t + (int64_t)n * g.dt_n + h]) + bias;
+    const float soft = log1pf(expf(raw));
+    s.raw = lr < cnt ? raw : 0.f;
+    s.dt = lr < cnt ? (raw > 20.f ? raw : soft) : 0.f;
     s.begins = false;
-    if (lr < cnt) {
-        s.raw = to_f(reinterpret_cast<const T*>(g.dt)[(int64_t)(t0 + lr) * g.dt_t + (int64_t)n * g.dt_n + h]) + bias;
-        s.dt = s.raw > 20.f ? s.raw : log1pf(expf(s.raw));
-        s.begins = g.first && g.first[(int64_t)(t0 + lr) * g.N + n];
-    }
+    if (g.first) s.begins = lr < cnt && g.first[(int64_t)(t0 + r) * g.N + n] != 0;
     const uint32_t begun = (uint32_t)__ballot(s.begins) & (uint32_t)((2ull << lr) - 1);
     s.e = begun ? 31 - __clz(begun) : -1;
     // in 64 bits: a difference of two sums keeps its precision whatever they have grown to
@@ -406,6 +458,7 @@ __device__ inline Steps steps(const ScanArgs& g, int n, int h, int t0, int cnt, 
 __device__ inline float decay(float hi1, float lo1, float hi0, float lo0) { return __builtin_amdgcn_exp2f((hi1 - hi0) + (lo1 - lo0)); }
 __device__ inline int acc_row(int e, int lg) { return 8 * (e / 4) + 4 * lg + e % 4; }
 
+template <int PB, int SB> constexpr int64_t per_state() { return (int64_t)SB * PB * 1024; }  // floats of one as the registers hold it
 // a state [state][head_dim] of a head as accumulators: rows n, column p = lr
 template <int PB, int SB>
 struct State {
@@ -416,30 +469,54 @@ struct State {
 #pragma unroll
             for (int p = 0; p < PB; ++p) zero(v[s][p]);
     }
-    // from / to [head_dim][state] in memory
-    __device__ inline void load(const float* m, int P, int S) {
+    // from / to [head_dim][state] in memory, whole lines an access: 32 rows at a time turned in `patch`, 32 rows of 32 SB + 4 floats
+    static constexpr int TP = 32 * SB + 4;
+    __device__ inline void load(const float* m, int P, int S, float* patch) {
         const int lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5;
+        const bool vec = S % 4 == 0 && (reinterpret_cast<uintptr_t>(m) & 15) == 0;
 #pragma unroll
-        for (int s = 0; s < SB; ++s)
+        for (int p = 0; p < PB; ++p) {
+            const int rows = P - 32 * p < 32 ? P - 32 * p : 32, n = rows > 0 ? rows * S : 0;
+            const float* from = m + (int64_t)32 * p * S;
+            if (vec)
+                for (int i = 4 * lane; i < n; i += 256) *reinterpret_cast<float4*>(patch + i / S * TP + i % S) = *reinterpret_cast<const float4*>(from + i);
+            else
+                for (int i = lane; i < n; i += 64) patch[i / S * TP + i % S] = from[i];
+            phase();
 #pragma unroll
-            for (int p = 0; p < PB; ++p)
+            for (int s = 0; s < SB; ++s)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int nn = 32 * s + acc_row(e, lg), pp = 32 * p + lr;
-                    v[s][p][e] = nn < S && pp < P ? m[(int64_t)pp * S + nn] : 0.f;
+                for (int k = 0; k < 4; ++k) {
+                    const int nn = 32 * s + 8 * k + 4 * lg;
+                    const float4 f = *reinterpret_cast<const float4*>(patch + lr * TP + nn);
+                    v[s][p][4 * k] = nn < S && lr < rows ? f.x : 0.f;
+                    v[s][p][4 * k + 1] = nn + 1 < S && lr < rows ? f.y : 0.f;
+                    v[s][p][4 * k + 2] = nn + 2 < S && lr < rows ? f.z : 0.f;
+                    v[s][p][4 * k + 3] = nn + 3 < S && lr < rows ? f.w : 0.f;
                 }
+            phase();
+        }
     }
-    __device__ inline void store(float* m, int P, int S) const {
+    __device__ inline void store(float* m, int P, int S, float* patch) const {
         const int lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5;
+        const bool vec = S % 4 == 0 && (reinterpret_cast<uintptr_t>(m) & 15) == 0;
 #pragma unroll
-        for (int s = 0; s < SB; ++s)
+        for (int p = 0; p < PB; ++p) {
+            const int rows = P - 32 * p < 32 ? P - 32 * p : 32, n = rows > 0 ? rows * S : 0;
+            float* to = m + (int64_t)32 * p * S;
 #pragma unroll
-            for (int p = 0; p < PB; ++p)
+            for (int s = 0; s < SB; ++s)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int nn = 32 * s + acc_row(e, lg), pp = 32 * p + lr;
-                    if (nn < S && pp < P) m[(int64_t)pp * S + nn] = v[s][p][e];
-                }
+                for (int k = 0; k < 4; ++k)
+                    *reinterpret_cast<float4*>(patch + lr * TP + 32 * s + 8 * k + 4 * lg) =
+                        make_float4(v[s][p][4 * k], v[s][p][4 * k + 1], v[s][p][4 * k + 2], v[s][p][4 * k + 3]);
+            phase();
+            if (vec)
+                for (int i = 4 * lane; i < n; i += 256) *reinterpret_cast<float4*>(to + i) = *reinterpret_cast<const float4*>(patch + i / S * TP + i % S);
+            else
+                for (int i = lane; i < n; i += 64) to[i] = patch[i / S * TP + i % S];
+            phase();
+        }
     }
     // from / to the registers' own order: whole kilobytes an access
     __device__ inline void dump(float* m) const {
@@ -493,6 +570,41 @@ __device__ inline void eight(const float* a, int kk, float (&v)[8]) {  // values
     v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w; v[4] = w.x; v[5] = w.y; v[6] = w.z; v[7] = w.w;
 }
 
+// results [column | time step] of a wave into `patch` as rows of 32 B + 4 floats
+template <int B>
+__device__ inline void to_rows(const float16_t (&o)[B], float* patch) {
+    const int lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5;
+#pragma unroll
+    for (int b = 0; b < B; ++b)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            *reinterpret_cast<float4*>(patch + lr * (32 * B + 4) + 32 * b + 8 * k + 4 * lg) =
+                make_float4(o[b][4 * k], o[b][4 * k + 1], o[b][4 * k + 2], o[b][4 * k + 3]);
+}
+// eight of a row's values to memory, as many as exist
+template <typename T>
+__device__ inline void store8_row(T* p, const float (&v)[8], int c8, int width, bool on) {
+    typedef T vec_t __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+    if (width % 8 == 0) {
+        vec_t u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[i] = (T)v[i];
+        if (on && 8 * c8 < width) *reinterpret_cast<vec_t*>(p + 8 * c8) = u;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (on && 8 * c8 + i < width) p[8 * c8 + i] = cvt<T>(v[i]);
+    }
+}
+__device__ inline void patch8(const float* row, int c8, float (&v)[8]) {
+    const float4 a = *reinterpret_cast<const float4*>(row + 8 * c8), b = *reinterpret_cast<const float4*>(row + 8 * c8 + 4);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+// The wave's index as a scalar: environment, head and every pointer that follows from it are then in scalar registers, and a branch on
+// them is a scalar one.  (With the index in the lanes, `if (z)` cost a mask of lanes, and the compiler, out of registers in the
+// backward, moved 26 of them into the accumulation file ahead of the place where the lanes come back: with no gate, none was on.)
+__device__ inline int wave_index() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
+
 template <typename T, int PB, int SB>
 struct ScanFwdLds {
     static constexpr int NP = Planes<T>::N;
@@ -501,86 +613,102 @@ struct ScanFwdLds {
     static constexpr int WAVE = X + 2 * N + (int)sizeof(StepLds);
 };
 
-template <typename T, int PB, int SB>
-__global__ __launch_bounds__((ScanFwdLds<T, PB, SB>::NW * 64)) void k_scan_fwd(ScanArgs g) {
+// LOCAL: only the state that a span of time leaves when nothing enters it, and what it leaves of a state that does.  (Where environments
+// and heads are too few to fill the machine, time is cut into spans: LOCAL for all of them at once, k_scan_join one after the other, then the
+// outputs of all of them at once.)
+template <typename T, int PB, int SB, bool LOCAL>
+__global__ __launch_bounds__((ScanFwdLds<T, PB, SB>::NW * 64), 2) void k_scan_fwd(ScanArgs g) {
     typedef ScanFwdLds<T, PB, SB> L;
     constexpr int NP = L::NP;
     extern __shared__ __align__(16) unsigned char lds[];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5;
-    const int64_t id = (int64_t)blockIdx.x * L::NW + wave;
-    if (id >= (int64_t)g.N * g.H) return;
+    const int wave = wave_index(), lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5;
+    const int64_t unit = (int64_t)blockIdx.x * L::NW + wave;
+    if (unit >= (int64_t)g.N * g.H * g.spans) return;
+    const int64_t id = unit / g.spans;
+    const int span = (int)(unit % g.spans), t_begin = span * g.span, t_end = t_begin + g.span < g.T ? t_begin + g.span : g.T;
     const int n = (int)(id / g.H), h = (int)(id % g.H), grp = h / (g.H / g.G);
     unsigned char* own = lds + wave * L::WAVE;
+    float* patch = reinterpret_cast<float*>(own);  // over the tiles, once they are done with
     const Tile<PB, NP> X = {own};
     const Tile<SB, NP> B = {own + L::X}, C = {own + L::X + L::N};
     StepLds* sl = reinterpret_cast<StepLds*>(own + L::X + 2 * L::N);
     const T* x = reinterpret_cast<const T*>(g.x) + (int64_t)n * g.x_n + (int64_t)h * g.P;
     const T* b = reinterpret_cast<const T*>(g.b) + (int64_t)n * g.x_n + (int64_t)grp * g.S;
     const T* c = reinterpret_cast<const T*>(g.c) + (int64_t)n * g.x_n + (int64_t)grp * g.S;
-    auto fits = [&](const void* p, int64_t st) { return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(st * (int64_t)sizeof(T))) & 15) == 0; };
-    const bool vx = fits(x, g.x_t), vb = fits(b, g.x_t), vc = fits(c, g.x_t);
+    const T* z = g.z ? reinterpret_cast<const T*>(g.z) + (int64_t)n * g.z_n + (int64_t)h * g.P : nullptr;
+    T* y_out = reinterpret_cast<T*>(g.y) + (int64_t)n * g.y_n + (int64_t)h * g.P;
     const double a2 = -(double)expf(g.a_log[h]) * 1.4426950408889634;
     const float dskip = g.d_skip ? g.d_skip[h] : 0.f, bias = g.dt_bias ? g.dt_bias[h] : 0.f;
-    State<PB, SB> st;
-    if (g.state_in) st.load(g.state_in + id * g.P * g.S, g.P, g.S);
-    else st.clear();
     const int64_t per = (int64_t)SB * PB * 1024;
-    float* saved = g.saved ? g.saved + id * (g.chunks + 1) * per : nullptr;
+    State<PB, SB> st;
+    if (LOCAL) st.clear();
+    else if (g.spans > 1) st.undump(g.ends + unit * per);
+    else if (g.state_in) st.load(g.state_in + id * g.P * g.S, g.P, g.S, patch);
+    else st.clear();
+    float* saved = !LOCAL && g.saved ? g.saved + id * (g.chunks + 1) * per : nullptr;
+    float all = 1.f;  // LOCAL: what is left of a state that enters the span
     int slow = 0;  // steps to take one by one: a chunk with an undefined or infinite input, which would reach others through products with zero
-    for (int t = 0; t < g.T;) {
-        int cnt = g.T - t < MEM_Q ? g.T - t : MEM_Q;
+    for (int t = t_begin; t < t_end;) {
+        int cnt = t_end - t < MEM_Q ? t_end - t : MEM_Q;
         if (slow) cnt = 1;
-        const bool bad = stage(X, x, g.x_t, t, cnt, g.P, vx);
+        const bool bad = stage(X, x, g.x_t, t, cnt, g.P);
         if (__any(bad) && cnt > 1) {
             slow = cnt;
             continue;
         }
-        stage(B, b, g.x_t, t, cnt, g.S, vb);
-        stage(C, c, g.x_t, t, cnt, g.S, vc);
+        phase();
+        stage(B, b, g.x_t, t, cnt, g.S);
+        phase();
+        if (!LOCAL) stage(C, c, g.x_t, t, cnt, g.S);
+        phase();
         const Steps s = steps<T>(g, n, h, t, cnt, a2, bias, sl);
         // the last step's sums: decay to the chunk's end
         const float hiq = __shfl(s.hi, 31), loq = __shfl(s.lo, 31);
         const int eq = __shfl(s.e, 31);
         const float w = lr >= eq ? s.dt * decay(hiq, loq, s.hi, s.lo) : 0.f;
         if (lane < 32) sl->w[lr] = w;
-        __builtin_amdgcn_wave_barrier();
+        phase();
         if (saved && t % MEM_Q == 0) st.dump(saved + (t / MEM_Q) * per);
         // scores [s | t] and what the state gives, [p | t]
         float16_t m, y[PB];
-        zero(m);
+        if (!LOCAL) {
+            zero(m);
 #pragma unroll
-        for (int p = 0; p < PB; ++p) zero(y[p]);
+            for (int p = 0; p < PB; ++p) zero(y[p]);
 #pragma unroll
-        for (int kk = 0; kk < 2 * SB; ++kk) {
-            uint4 fb[NP], fc[NP], fh[3];
-            C.rows(kk, fc);
-            B.rows(kk, fb);
-            mma_p(fb, fc, m);
+            for (int kk = 0; kk < 2 * SB; ++kk) {
+                uint4 fb[NP], fc[NP], fh[3];
+                C.rows(kk, fc);
+                B.rows(kk, fb);
+                mma_p(fb, fc, m);
 #pragma unroll
-            for (int p = 0; p < PB; ++p) {
-                acc_parts(st.v[kk / 2][p], kk % 2, fh);
-                mma_p(fh, fc, y[p]);
+                for (int p = 0; p < PB; ++p) {
+                    acc_parts(st.v[kk / 2][p], kk % 2, fh);
+                    mma_p(fh, fc, y[p]);
+                }
+            }
+            const float in = s.e < 0 ? __builtin_amdgcn_exp2f(s.hi + s.lo) : 0.f;
+#pragma unroll
+            for (int p = 0; p < PB; ++p)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) y[p][e] = s.e < 0 ? y[p][e] * in : 0.f;
+#pragma unroll
+            for (int k4 = 0; k4 < 4; ++k4) {
+                const int r0 = 8 * k4 + 4 * lg;
+                const float4 hi = *reinterpret_cast<const float4*>(sl->hi + r0), lo = *reinterpret_cast<const float4*>(sl->lo + r0),
+                             dt = *reinterpret_cast<const float4*>(sl->dt + r0);
+                const float a[4] = {hi.x, hi.y, hi.z, hi.w}, bb[4] = {lo.x, lo.y, lo.z, lo.w}, d[4] = {dt.x, dt.y, dt.z, dt.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const bool on = r0 + i <= lr && r0 + i >= s.e;
+                    m[4 * k4 + i] = on ? m[4 * k4 + i] * (d[i] * decay(s.hi, s.lo, a[i], bb[i])) : 0.f;
+                }
             }
         }
-        const float in = s.e < 0 ? __builtin_amdgcn_exp2f(s.hi + s.lo) : 0.f;
-#pragma unroll
-        for (int p = 0; p < PB; ++p)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) y[p][e] = s.e < 0 ? y[p][e] * in : 0.f;
-#pragma unroll
-        for (int k4 = 0; k4 < 4; ++k4) {
-            const int r0 = 8 * k4 + 4 * lg;
-            const float4 hi = *reinterpret_cast<const float4*>(sl->hi + r0), lo = *reinterpret_cast<const float4*>(sl->lo + r0),
-                         dt = *reinterpret_cast<const float4*>(sl->dt + r0);
-            const float a[4] = {hi.x, hi.y, hi.z, hi.w}, bb[4] = {lo.x, lo.y, lo.z, lo.w}, d[4] = {dt.x, dt.y, dt.z, dt.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const bool on = r0 + i <= lr && r0 + i >= s.e;
-                m[4 * k4 + i] = on ? m[4 * k4 + i] * (d[i] * decay(s.hi, s.lo, a[i], bb[i])) : 0.f;
-            }
-        }
+        phase();
         // state to the chunk's end: what is left of the old one
         const float left = eq < 0 ? __builtin_amdgcn_exp2f(hiq + loq) : 0.f;
+        if (LOCAL) all = eq < 0 ? all * left : 0.f;
 #pragma unroll
         for (int i = 0; i < SB; ++i)
 #pragma unroll
@@ -590,11 +718,11 @@ __global__ __launch_bounds__((ScanFwdLds<T, PB, SB>::NW * 64)) void k_scan_fwd(S
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
             uint4 fm[3], fx[PB][NP];
-            acc_parts(m, kk, fm);
+            if (!LOCAL) acc_parts(m, kk, fm);
 #pragma unroll
             for (int p = 0; p < PB; ++p) {
                 X.cols(p, kk, fx[p]);
-                mma_p(fx[p], fm, y[p]);
+                if (!LOCAL) mma_p(fx[p], fm, y[p]);
             }
             float wk[8];
             eight(sl->w, kk, wk);
@@ -607,31 +735,82 @@ __global__ __launch_bounds__((ScanFwdLds<T, PB, SB>::NW * 64)) void k_scan_fwd(S
                 for (int p = 0; p < PB; ++p) mma_p(fw, fx[p], st.v[i][p]);
             }
         }
-        if (lr < cnt) {
-            T* yo = reinterpret_cast<T*>(g.y) + (int64_t)(t + lr) * g.y_t + (int64_t)n * g.y_n + (int64_t)h * g.P;
-            const T* zo = g.z ? reinterpret_cast<const T*>(g.z) + (int64_t)(t + lr) * g.z_t + (int64_t)n * g.z_n + (int64_t)h * g.P : nullptr;
+        phase();
+        if (!LOCAL) {  // d x joins y; then rows, gated, eight values a lane
 #pragma unroll
             for (int p = 0; p < PB; ++p)
 #pragma unroll
                 for (int k4 = 0; k4 < 4; ++k4) {
-                    const int p0 = 32 * p + 8 * k4 + 4 * lg;
                     float xv[4];
-                    X.get4(lr, p0, xv);
+                    X.get4(lr, 32 * p + 8 * k4 + 4 * lg, xv);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (p0 + i < g.P) {
-                            float o = y[p][4 * k4 + i] + dskip * xv[i];
-                            if (zo) o *= silu_f(to_f(zo[p0 + i]));
-                            yo[p0 + i] = cvt<T>(o);
-                        }
+                    for (int i = 0; i < 4; ++i) y[p][4 * k4 + i] += dskip * xv[i];
                 }
+            phase();
+            to_rows(y, patch);
+            phase();
+            constexpr int CH = 4 * PB;
+            const int ln = lane_now();
+#pragma unroll
+            for (int i = 0; i < CH / 2; ++i) {
+                const int row = i * (64 / CH) + ln / CH, c8 = ln % CH;
+                float v[8];
+                patch8(patch + row * (32 * PB + 4), c8, v);
+                if (z) {
+                    float zv[8];
+                    load8_raw(z + (int64_t)t * g.z_t, row * g.z_t, c8, g.P, row < cnt, zv);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) v[k] *= silu_f(zv[k]);
+                }
+                store8_row(y_out + (int64_t)(t + row) * g.y_t, v, c8, g.P, row < cnt);
+            }
         }
-        __builtin_amdgcn_wave_barrier();
+        phase();
         t += cnt;
         if (slow) --slow;
     }
+    if (LOCAL) {
+        st.dump(g.ends + unit * per);
+        if (lane == 0) g.left[unit] = all;
+        return;
+    }
+    if (span + 1 < g.spans) return;
     if (saved) st.dump(saved + (int64_t)g.chunks * per);
-    if (g.state_out) st.store(g.state_out + id * g.P * g.S, g.P, g.S);
+    if (g.state_out && g.spans == 1) st.store(g.state_out + id * g.P * g.S, g.P, g.S, patch);
+}
+
+// The states between the spans of an environment's head, a thread four values of the register order: what span i leaves is replaced by what
+// enters it.  REVERSE: the gradients of states, from the last span to the first.
+template <int PB, int SB, bool REVERSE>
+__global__ __launch_bounds__(256) void k_scan_join(ScanArgs g) {
+    constexpr int per = SB * PB * 1024;
+    const int64_t id = blockIdx.x;
+    const int i = blockIdx.y * 256 + threadIdx.x, blk = i / 256, lane = i % 64;
+    // values 4 k .. 4 k + 3 of block (s, p), k = i / 64 % 4: states 32 s + 8 k + 4 lg + [0, 4) of channel 32 p + lr
+    const int nn = 32 * (blk / PB) + 8 * (i / 64 % 4) + 4 * (lane / 32), pp = 32 * (blk % PB) + lane % 32;
+    const float* from = REVERSE ? g.dstate_out : g.state_in;
+    float* to = REVERSE ? g.dstate_in : g.state_out;
+    const int64_t at = (id * g.P + pp) * g.S + nn;
+    float v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = from && pp < g.P && nn + k < g.S ? from[at + k] : 0.f;
+    float4* ends = reinterpret_cast<float4*>(g.ends + id * g.spans * per) + i;
+    const float* left = g.left + id * g.spans;
+#pragma unroll 4
+    for (int q = 0; q < g.spans; ++q) {
+        const int span = REVERSE ? g.spans - 1 - q : q;
+        const float4 gave = ends[(int64_t)span * (per / 4)];
+        const float l = left[span];
+        ends[(int64_t)span * (per / 4)] = make_float4(v[0], v[1], v[2], v[3]);
+        v[0] = (l != 0.f ? l * v[0] : 0.f) + gave.x;
+        v[1] = (l != 0.f ? l * v[1] : 0.f) + gave.y;
+        v[2] = (l != 0.f ? l * v[2] : 0.f) + gave.z;
+        v[3] = (l != 0.f ? l * v[3] : 0.f) + gave.w;
+    }
+    if (to && pp < g.P)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (nn + k < g.S) to[at + k] = v[k];
 }
 
 // ---- backward of the scan: the chunks in reverse, a workgroup of NW waves taking heads of one group, whose dB and dC it adds up ----
@@ -646,7 +825,7 @@ struct ScanBwdLds {
     static constexpr int NP = Planes<T>::N;
     static constexpr int NW = sizeof(T) == 4 ? 2 : 4;
     static constexpr int X = Tile<PB, NP>::BYTES, N = Tile<SB, NP>::BYTES, DY = Tile<PB, 3>::BYTES;
-    static constexpr int RED = 32 * (32 * SB + 4) * 4;  // one of dB, dC of a wave, for the sum over the waves
+    static constexpr int RED = 32 * (32 * (SB > PB ? SB : PB) + 4) * 4;  // one of dB, dC of a wave for the sum over the waves; dx, dz on their way to rows
     static constexpr int WAVE = X + 2 * N + DY + RED + (int)sizeof(StepLds);
 };
 
@@ -655,12 +834,15 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
     typedef ScanBwdLds<T, PB, SB> L;
     constexpr int NP = L::NP, NW = L::NW, RP = 32 * SB + 4;
     extern __shared__ __align__(16) unsigned char lds[];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5;
+    const int wave = wave_index(), lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5;
     const int rep = g.H / g.G;
-    int blk = blockIdx.x;
-    const int hb = blk % g.head_blocks;
+    int64_t blk = blockIdx.x;
+    const int hb = (int)(blk % g.head_blocks);
     blk /= g.head_blocks;
-    const int grp = blk % g.G, n = blk / g.G;
+    const int grp = (int)(blk % g.G);
+    blk /= g.G;
+    const int span = (int)(blk % g.spans), n = (int)(blk / g.spans);
+    const int t_begin = span * g.span, t_last = t_begin + g.span < g.T ? t_begin + g.span : g.T;
     const bool live = hb * NW + wave < rep;   // (a wave without a head runs along on another's inputs and leaves nothing)
     const int h = grp * rep + (live ? hb * NW + wave : rep - 1);
     const int64_t id = (int64_t)n * g.H + h;
@@ -675,8 +857,6 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
     const T* c = reinterpret_cast<const T*>(g.c) + (int64_t)n * g.x_n + (int64_t)grp * g.S;
     const T* dy = reinterpret_cast<const T*>(g.dy) + (int64_t)n * g.y_n + (int64_t)h * g.P;
     const T* z = g.z ? reinterpret_cast<const T*>(g.z) + (int64_t)n * g.z_n + (int64_t)h * g.P : nullptr;
-    auto fits = [&](const void* p, int64_t st) { return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(st * (int64_t)sizeof(T))) & 15) == 0; };
-    const bool vx = fits(x, g.x_t), vb = fits(b, g.x_t), vc = fits(c, g.x_t), vdy = fits(dy, g.y_t), vz = z && fits(z, g.z_t);
     const float av = -expf(g.a_log[h]);
     const double a2 = (double)av * 1.4426950408889634;
     const float dskip = g.d_skip ? g.d_skip[h] : 0.f, bias = g.dt_bias ? g.dt_bias[h] : 0.f;
@@ -685,30 +865,28 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
     // dh twice: rows n, column p, and rows p, column n -- the operand that a product needs has its contraction in the registers
     State<PB, SB> dh1;
     float16_t dh2[PB][SB];
-    if (g.dstate_out) {
-        dh1.load(g.dstate_out + id * g.P * g.S, g.P, g.S);
-        const float* m = g.dstate_out + id * g.P * g.S;
+    if (g.spans > 1) dh1.undump(g.ends + (id * g.spans + span) * per);
+    else if (g.dstate_out) dh1.load(g.dstate_out + id * g.P * g.S, g.P, g.S, red);
+    else dh1.clear();
 #pragma unroll
-        for (int p = 0; p < PB; ++p)
+    for (int p = 0; p < PB; ++p)
 #pragma unroll
-            for (int i = 0; i < SB; ++i)
+        for (int i = 0; i < SB; ++i) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int pp = 32 * p + acc_row(e, lg), nn = 32 * i + lr;
-                    dh2[p][i][e] = nn < g.S && pp < g.P ? m[(int64_t)pp * g.S + nn] : 0.f;
-                }
-    } else {
-        dh1.clear();
+            for (int e = 0; e < 16; ++e) red[acc_row(e, lg) * 36 + lr] = dh1.v[i][p][e];
+            phase();
 #pragma unroll
-        for (int p = 0; p < PB; ++p)
-#pragma unroll
-            for (int i = 0; i < SB; ++i) zero(dh2[p][i]);
-    }
+            for (int k = 0; k < 4; ++k) {
+                const float4 f = *reinterpret_cast<const float4*>(red + lr * 36 + 8 * k + 4 * lg);
+                dh2[p][i][4 * k] = f.x; dh2[p][i][4 * k + 1] = f.y; dh2[p][i][4 * k + 2] = f.z; dh2[p][i][4 * k + 3] = f.w;
+            }
+            phase();
+        }
     float sum_a = 0.f, sum_d = 0.f, sum_b = 0.f;  // per lane: of its steps
     float inner;                                  // <state behind the chunk, dh>
     {
         State<PB, SB> last;
-        last.undump(saved + (int64_t)g.chunks * per);
+        last.undump(saved + (int64_t)((t_last + MEM_Q - 1) / MEM_Q) * per);
         float s = 0.f;
 #pragma unroll
         for (int i = 0; i < SB; ++i)
@@ -720,37 +898,20 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
         inner = s;
     }
     int slow = 0;
-    for (int t_end = g.T; t_end > 0;) {
+    for (int t_end = t_last; t_end > t_begin;) {
         const int base = (t_end - 1) / MEM_Q * MEM_Q;
         int t = base, cnt = t_end - base;
         if (slow) {
             t = t_end - 1;
             cnt = 1;
         }
-        bool bad = stage(X, x, g.x_t, t, cnt, g.P, vx);
-        bad |= stage(B, b, g.x_t, t, cnt, g.S, vb);
-        bad |= stage(C, c, g.x_t, t, cnt, g.S, vc);
-        {   // dy silu(z), three parts
-            constexpr int CH = 4 * PB;
-            float nan = 0.f;
-#pragma unroll
-            for (int i = 0; i < CH / 2; ++i) {
-                const int row = i * (64 / CH) + lane / CH, c8 = lane % CH, r = row < cnt ? row : 0, av8 = row < cnt ? g.P - 8 * c8 : 0;
-                float v[8], zv[8];
-                load8_raw(dy + (int64_t)(t + r) * g.y_t + 8 * c8, av8, vdy, v);
-                if (z) {
-                    load8_raw(z + (int64_t)(t + r) * g.z_t + 8 * c8, av8, vz, zv);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) v[k] *= silu_f(zv[k]);
-                }
-                uint4 p[3];
-                split3(v, p);
-                D.put(row, c8, p);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) nan += v[k] * 0.f;
-            }
-            bad |= !(nan == 0.f);
-        }
+        bool bad = stage(X, x, g.x_t, t, cnt, g.P);
+        phase();
+        bad |= stage(B, b, g.x_t, t, cnt, g.S);
+        phase();
+        bad |= stage(C, c, g.x_t, t, cnt, g.S);
+        phase();
+        bad |= stage_dy(D, dy, g.y_t, z, g.z_t, t, cnt, g.P);
         if (__syncthreads_or(bad) && cnt > 1) {  // all waves step by step together
             slow = cnt;
             continue;
@@ -781,7 +942,8 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
         const float us = lr >= eq ? decay(hiq, loq, s.hi, s.lo) : 0.f;                     // to the chunk's end
         const float qs = s.e < 0 ? __builtin_amdgcn_exp2f(s.hi + s.lo) : 0.f;              // from its start
         if (lane < 32) sl->w[lr] = qs;
-        __builtin_amdgcn_wave_barrier();
+        phase();
+        phase();
         // scores and dy . x in both layouts: [s | t] (lane: the later step) and [t | s] (lane: the earlier one)
         float16_t g1, g2, r1, r2;
         zero(g1); zero(g2); zero(r1); zero(r2);
@@ -801,15 +963,14 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
             mma_p(fx, fd, r1);
             mma_p(fd, fx, r2);
         }
+        phase();
         // m1: scores that give y [s | t]; v1: E R dt_s [s | t]; g2: E scores [t | s]; r2: E R [t | s]
         float16_t m1;
-        float diag = 0.f;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             const int r = acc_row(e, lg);
             const float rhi = sl->hi[r], rlo = sl->lo[r], rdt = sl->dt[r];
             const int re = sl->e[r];
-            if (r == lr) diag = r1[e];
             const bool on1 = r <= lr && r >= s.e, on2 = r >= lr && lr >= re;
             const float d1 = decay(s.hi, s.lo, rhi, rlo) * rdt, d2 = decay(rhi, rlo, s.hi, s.lo);
             m1[e] = on1 ? g1[e] * d1 : 0.f;
@@ -817,8 +978,7 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
             g2[e] = on2 ? g2[e] * d2 : 0.f;
             r2[e] = on2 ? r2[e] * d2 : 0.f;
         }
-        diag += __shfl_xor(diag, 32);
-        if (lr < cnt && lg == 0) sum_d += diag;
+        phase();
         // dz needs y again
         if (z && g.dz) {
             float16_t y[PB];
@@ -848,26 +1008,37 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
                     mma_p(fx, fm, y[p]);
                 }
             }
-            if (lr < cnt && live) {
-                const T* dyo = dy + (int64_t)(t + lr) * g.y_t;
-                const T* zo = z + (int64_t)(t + lr) * g.z_t;
-                T* dzo = reinterpret_cast<T*>(g.dz) + (int64_t)(t + lr) * g.z_t + (int64_t)n * g.z_n + (int64_t)h * g.P;
 #pragma unroll
-                for (int p = 0; p < PB; ++p)
+            for (int p = 0; p < PB; ++p)
 #pragma unroll
-                    for (int k4 = 0; k4 < 4; ++k4) {
-                        const int p0 = 32 * p + 8 * k4 + 4 * lg;
-                        float xv[4];
-                        X.get4(lr, p0, xv);
+                for (int k4 = 0; k4 < 4; ++k4) {
+                    float xv[4];
+                    X.get4(lr, 32 * p + 8 * k4 + 4 * lg, xv);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (p0 + i < g.P) {
-                                const float zv = to_f(zo[p0 + i]), sg = sigmoid_f(zv);
-                                dzo[p0 + i] = cvt<T>(to_f(dyo[p0 + i]) * (y[p][4 * k4 + i] + dskip * xv[i]) * sg * (1.f + zv * (1.f - sg)));
-                            }
-                    }
+                    for (int i = 0; i < 4; ++i) y[p][4 * k4 + i] += dskip * xv[i];
+                }
+            to_rows(y, red);
+            phase();
+            T* dzo = reinterpret_cast<T*>(g.dz) + (int64_t)n * g.z_n + (int64_t)h * g.P;
+            constexpr int CH = 4 * PB;
+            const int ln = lane_now();
+#pragma unroll
+            for (int i = 0; i < CH / 2; ++i) {
+                const int row = i * (64 / CH) + ln / CH, c8 = ln % CH;
+                float v[8], dv[8], zv[8];
+                patch8(red + row * (32 * PB + 4), c8, v);
+                load8_raw(dy + (int64_t)t * g.y_t, row * g.y_t, c8, g.P, row < cnt, dv);
+                load8_raw(z + (int64_t)t * g.z_t, row * g.z_t, c8, g.P, row < cnt, zv);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float sg = sigmoid_f(zv[k]);
+                    v[k] *= dv[k] * sg * (1.f + zv[k] * (1.f - sg));
+                }
+                store8_row(dzo + (int64_t)(t + row) * g.z_t, v, c8, g.P, live && row < cnt);
             }
+            phase();
         }
+        phase();
         // dx [p | s]
         {
             float16_t o[PB];
@@ -897,20 +1068,35 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
                     mma_p(fd, fm, o[p]);
                 }
             }
-            if (lr < cnt && live) {
-                T* dxo = reinterpret_cast<T*>(g.dx) + (int64_t)(t + lr) * g.x_t + (int64_t)n * g.x_n + (int64_t)h * g.P;
+            phase();
+            float dd = 0.f;
 #pragma unroll
-                for (int p = 0; p < PB; ++p)
+            for (int p = 0; p < PB; ++p)
 #pragma unroll
-                    for (int k4 = 0; k4 < 4; ++k4) {
-                        const int p0 = 32 * p + 8 * k4 + 4 * lg;
-                        float dv[4];
-                        D.get4(lr, p0, dv);
+                for (int k4 = 0; k4 < 4; ++k4) {
+                    float dv[4], xv[4];
+                    D.get4(lr, 32 * p + 8 * k4 + 4 * lg, dv);
+                    X.get4(lr, 32 * p + 8 * k4 + 4 * lg, xv);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (p0 + i < g.P) dxo[p0 + i] = cvt<T>(s.dt * o[p][4 * k4 + i] + dskip * dv[i]);
+                    for (int i = 0; i < 4; ++i) {
+                        o[p][4 * k4 + i] = s.dt * o[p][4 * k4 + i] + dskip * dv[i];
+                        dd += dv[i] * xv[i];
                     }
+                }
+            if (lr < cnt) sum_d += dd;
+            to_rows(o, red);
+            phase();
+            T* dxo = reinterpret_cast<T*>(g.dx) + (int64_t)n * g.x_n + (int64_t)h * g.P;
+            constexpr int CH = 4 * PB;
+            const int ln = lane_now();
+#pragma unroll
+            for (int i = 0; i < CH / 2; ++i) {
+                const int row = i * (64 / CH) + ln / CH, c8 = ln % CH;
+                float v[8];
+                patch8(red + row * (32 * PB + 4), c8, v);
+                store8_row(dxo + (int64_t)(t + row) * g.x_t, v, c8, g.P, live && row < cnt);
             }
+            phase();
         }
         // dC [n | t], dB' [n | s]
         float row_tot = 0.f, col_tot = 0.f;
@@ -941,7 +1127,7 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
                     for (int i = 0; i < SB; ++i) {
 #pragma unroll
                         for (int e = 0; e < 16; ++e) red[acc_row(e, lg) * 36 + lr] = hin.v[i][p][e];
-                        __builtin_amdgcn_wave_barrier();
+                        phase();
 #pragma unroll
                         for (int kk = 0; kk < 2; ++kk) {
                             float v[8];
@@ -950,10 +1136,11 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
                             split3(v, fh);
                             mma_p(fh, fd[kk], o[i]);
                         }
-                        __builtin_amdgcn_wave_barrier();
+                        phase();
                     }
                 }
             }
+            phase();
             const float lane_scale = which ? us : qs;
             const bool lane_on = which ? lr >= eq : s.e < 0;
 #pragma unroll
@@ -971,6 +1158,7 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
                     mma_p(f, fv, o[i]);
                 }
             }
+            phase();
             float tot = 0.f;
 #pragma unroll
             for (int i = 0; i < SB; ++i)
@@ -1029,6 +1217,7 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
                 if (live) reinterpret_cast<T*>(g.ddt)[(int64_t)(t + lr) * g.dt_t + (int64_t)n * g.dt_n + h] = cvt<T>(draw);
             }
         }
+        phase();
         // dh before the chunk
         const float left = eq < 0 ? __builtin_amdgcn_exp2f(hiq + loq) : 0.f;
 #pragma unroll
@@ -1073,17 +1262,109 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
         if (slow) --slow;
     }
     if (!live) return;
-    if (g.dstate_in) dh1.store(g.dstate_in + id * g.P * g.S, g.P, g.S);
+    if (g.dstate_in && g.spans == 1) {
+        float* m = g.dstate_in + id * g.P * g.S;
+#pragma unroll
+        for (int p = 0; p < PB; ++p)
+#pragma unroll
+            for (int i = 0; i < SB; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int pp = 32 * p + acc_row(e, lg), nn = 32 * i + lr;
+                    if (nn < g.S && pp < g.P) m[(int64_t)pp * g.S + nn] = dh2[p][i][e];
+                }
+    }
     for (int o = 32; o; o >>= 1) {
         sum_a += __shfl_xor(sum_a, o);
         sum_d += __shfl_xor(sum_d, o);
         sum_b += __shfl_xor(sum_b, o);
     }
     if (lane == 0) {
-        g.ph[(int64_t)h * g.N + n] = sum_a * av;
-        g.ph[((int64_t)g.H + h) * g.N + n] = sum_d;
-        g.ph[((int64_t)2 * g.H + h) * g.N + n] = sum_b;
+        const int64_t parts = (int64_t)g.N * g.spans, at = (int64_t)n * g.spans + span;
+        g.ph[h * parts + at] = sum_a * av;
+        g.ph[((int64_t)g.H + h) * parts + at] = sum_d;
+        g.ph[((int64_t)2 * g.H + h) * parts + at] = sum_b;
     }
+}
+
+// What a span of time adds to the gradient of the state before it when none enters from behind, and what it leaves of one that does.
+template <typename T, int PB, int SB>
+struct ScanBwdLocalLds {
+    static constexpr int NP = Planes<T>::N;
+    static constexpr int N = Tile<SB, NP>::BYTES, DY = Tile<PB, 3>::BYTES;
+    static constexpr int WAVE = N + DY + (int)sizeof(StepLds);
+};
+template <typename T, int PB, int SB>
+__global__ __launch_bounds__(256) void k_scan_bwd_local(ScanArgs g) {
+    typedef ScanBwdLocalLds<T, PB, SB> L;
+    constexpr int NP = L::NP;
+    extern __shared__ __align__(16) unsigned char lds[];
+    const int wave = wave_index(), lane = threadIdx.x & 63, lr = lane & 31;
+    const int64_t unit = (int64_t)blockIdx.x * 4 + wave;
+    if (unit >= (int64_t)g.N * g.H * g.spans) return;
+    const int64_t id = unit / g.spans;
+    const int span = (int)(unit % g.spans), t_begin = span * g.span, t_last = t_begin + g.span < g.T ? t_begin + g.span : g.T;
+    const int n = (int)(id / g.H), h = (int)(id % g.H), grp = h / (g.H / g.G);
+    unsigned char* own = lds + wave * L::WAVE;
+    const Tile<SB, NP> C = {own};
+    const Tile<PB, 3> D = {own + L::N};
+    StepLds* sl = reinterpret_cast<StepLds*>(own + L::N + L::DY);
+    const T* c = reinterpret_cast<const T*>(g.c) + (int64_t)n * g.x_n + (int64_t)grp * g.S;
+    const T* dy = reinterpret_cast<const T*>(g.dy) + (int64_t)n * g.y_n + (int64_t)h * g.P;
+    const T* z = g.z ? reinterpret_cast<const T*>(g.z) + (int64_t)n * g.z_n + (int64_t)h * g.P : nullptr;
+    const double a2 = -(double)expf(g.a_log[h]) * 1.4426950408889634;
+    const float bias = g.dt_bias ? g.dt_bias[h] : 0.f;
+    State<PB, SB> dh;
+    dh.clear();
+    float all = 1.f;
+    int slow = 0;
+    for (int t_end = t_last; t_end > t_begin;) {
+        int t = (t_end - 1) / MEM_Q * MEM_Q, cnt = t_end - t;
+        if (slow) {
+            t = t_end - 1;
+            cnt = 1;
+        }
+        bool bad = stage(C, c, g.x_t, t, cnt, g.S);
+        bad |= stage_dy(D, dy, g.y_t, z, g.z_t, t, cnt, g.P);
+        if (__any(bad) && cnt > 1) {
+            slow = cnt;
+            continue;
+        }
+        const Steps s = steps<T>(g, n, h, t, cnt, a2, bias, sl);
+        const float hiq = __shfl(s.hi, 31), loq = __shfl(s.lo, 31);
+        const int eq = __shfl(s.e, 31);
+        if (lane < 32) sl->w[lr] = s.e < 0 ? __builtin_amdgcn_exp2f(s.hi + s.lo) : 0.f;
+        phase();
+        const float left = eq < 0 ? __builtin_amdgcn_exp2f(hiq + loq) : 0.f;
+        all = eq < 0 ? all * left : 0.f;
+#pragma unroll
+        for (int i = 0; i < SB; ++i)
+#pragma unroll
+            for (int p = 0; p < PB; ++p)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) dh.v[i][p][e] = eq < 0 ? dh.v[i][p][e] * left : 0.f;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            float qk[8];
+            eight(sl->w, kk, qk);
+            uint4 fd[PB][3];
+#pragma unroll
+            for (int p = 0; p < PB; ++p) D.cols(p, kk, fd[p]);
+#pragma unroll
+            for (int i = 0; i < SB; ++i) {
+                uint4 f[NP], fq[3];
+                C.cols(i, kk, f);
+                scaled_parts(f, qk, fq);
+#pragma unroll
+                for (int p = 0; p < PB; ++p) mma_p(fq, fd[p], dh.v[i][p]);
+            }
+        }
+        phase();
+        t_end -= cnt;
+        if (slow) --slow;
+    }
+    dh.dump(g.ends + unit * per_state<PB, SB>());
+    if (lane == 0) g.left[unit] = all;
 }
 
 // the sums over a group's head blocks, in order
@@ -1112,8 +1393,9 @@ __global__ __launch_bounds__(256) void k_scan_heads(ScanArgs g) {
     const int h = blockIdx.x % g.H, which = blockIdx.x / g.H;
     float* out = which == 0 ? g.da_log : which == 1 ? g.dd_skip : g.ddt_bias;
     if (!out) return;
+    const int64_t parts = (int64_t)g.N * g.spans;
     float s = 0.f;
-    for (int n = threadIdx.x; n < g.N; n += 256) s += g.ph[((int64_t)which * g.H + h) * g.N + n];
+    for (int64_t n = threadIdx.x; n < parts; n += 256) s += g.ph[((int64_t)which * g.H + h) * parts + n];
     for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
     __syncthreads();
@@ -1264,14 +1546,28 @@ void launch_conv_bwd(const morlax_conv_dims& d, const void* x, const float* w, c
     }
 }
 
+// Spans of time: one where environments and heads fill the machine's SIMDs, or the segment is short; else as many as give every SIMD a
+// wave, of two chunks at least (a span costs its inputs once more and a state to write and read).
+static void scan_spans(ScanArgs& g) {
+    const int64_t waves = (int64_t)g.N * g.H;
+    g.spans = 1;
+    g.span = g.chunks * MEM_Q;
+    if (waves > 512 || g.chunks < 8) return;
+    int64_t spans = cdiv(1024, waves);
+    if (spans > g.chunks / 2) spans = g.chunks / 2;
+    g.span = (int)(cdiv(g.chunks, spans) * MEM_Q);
+    g.spans = (int)cdiv(g.T, g.span);
+}
 static ScanArgs scan_args(const morlax_scan_dims& d) {
     ScanArgs g = {};
     g.T = d.T; g.N = d.N; g.H = d.heads; g.P = d.head_dim; g.G = d.groups; g.S = d.state;
     g.x_t = d.x_t; g.x_n = d.x_n; g.z_t = d.z_t; g.z_n = d.z_n; g.dt_t = d.dt_t; g.dt_n = d.dt_n; g.y_t = d.y_t; g.y_n = d.y_n;
     g.chunks = (int)cdiv(d.T, MEM_Q);
     g.head_blocks = (int)cdiv(d.heads / d.groups, d.dtype ? 4 : 2);
+    scan_spans(g);
     return g;
 }
+static int64_t scan_blocks(const ScanArgs& g) { return cdiv(g.P, 32) * cdiv(g.S, 32); }
 int64_t scan_saved_bytes(const morlax_scan_dims& d) {
     const int64_t blocks = cdiv(d.head_dim, 32) * cdiv(d.state, 32);
     return (int64_t)d.N * d.heads * (cdiv(d.T, MEM_Q) + 1) * blocks * 4096;
@@ -1284,8 +1580,12 @@ static int64_t scan_carve(ScanArgs& g, bool back, void* ws) {
         off += align_up(bytes, 256);
         return q;
     };
+    if (g.spans > 1) {
+        g.ends = take((int64_t)g.N * g.H * g.spans * scan_blocks(g) * 4096);
+        g.left = take((int64_t)g.N * g.H * g.spans * 4);
+    }
     if (back) {
-        g.ph = take((int64_t)3 * g.H * g.N * 4);
+        g.ph = take((int64_t)3 * g.H * g.N * g.spans * 4);
         const int64_t n = g.head_blocks > 1 ? (int64_t)g.head_blocks * g.T * g.N * g.G * g.S * 4 : 0;
         g.pb = take(n);
         g.pc = take(n);
@@ -1302,20 +1602,34 @@ static int allow_lds(const void* kernel, int bytes) {
     (void)hipGetLastError();
     return -1;
 }
-template <typename T, int PB, int SB>
-static int scan_fwd(const ScanArgs& g, hipStream_t s) {
+template <typename T, int PB, int SB, bool LOCAL>
+static int scan_fwd_pass(const ScanArgs& g, hipStream_t s) {
     typedef ScanFwdLds<T, PB, SB> L;
     constexpr int lds = L::NW * L::WAVE;
-    if (allow_lds(reinterpret_cast<const void*>(k_scan_fwd<T, PB, SB>), lds) != 0) return -1;
-    k_scan_fwd<T, PB, SB><<<cdiv((int64_t)g.N * g.H, L::NW), L::NW * 64, lds, s>>>(g);
+    if (allow_lds(reinterpret_cast<const void*>(k_scan_fwd<T, PB, SB, LOCAL>), lds) != 0) return -1;
+    k_scan_fwd<T, PB, SB, LOCAL><<<cdiv((int64_t)g.N * g.H * g.spans, L::NW), L::NW * 64, lds, s>>>(g);
     return 0;
+}
+template <typename T, int PB, int SB>
+static int scan_fwd(const ScanArgs& g, hipStream_t s) {
+    if (g.spans > 1) {
+        if (scan_fwd_pass<T, PB, SB, true>(g, s) != 0) return -1;
+        k_scan_join<PB, SB, false><<<dim3((int64_t)g.N * g.H, PB * SB), 256, 0, s>>>(g);
+    }
+    return scan_fwd_pass<T, PB, SB, false>(g, s);
 }
 template <typename T, int PB, int SB>
 static int scan_bwd(const ScanArgs& g, hipStream_t s) {
     typedef ScanBwdLds<T, PB, SB> L;
+    if (g.spans > 1) {
+        constexpr int lds = 4 * ScanBwdLocalLds<T, PB, SB>::WAVE;
+        if (allow_lds(reinterpret_cast<const void*>(k_scan_bwd_local<T, PB, SB>), lds) != 0) return -1;
+        k_scan_bwd_local<T, PB, SB><<<cdiv((int64_t)g.N * g.H * g.spans, 4), 256, lds, s>>>(g);
+        k_scan_join<PB, SB, true><<<dim3((int64_t)g.N * g.H, PB * SB), 256, 0, s>>>(g);
+    }
     constexpr int lds = L::NW * L::WAVE;
     if (allow_lds(reinterpret_cast<const void*>(k_scan_bwd<T, PB, SB>), lds) != 0) return -1;
-    k_scan_bwd<T, PB, SB><<<(int64_t)g.N * g.G * g.head_blocks, L::NW * 64, lds, s>>>(g);
+    k_scan_bwd<T, PB, SB><<<(int64_t)g.N * g.G * g.head_blocks * g.spans, L::NW * 64, lds, s>>>(g);
     if (g.head_blocks > 1) {
         int64_t nb = cdiv((int64_t)g.T * g.N * g.G * g.S, 256);
         k_scan_bc<T><<<nb < 8192 ? nb : 8192, 256, 0, s>>>(g);

@@ -218,7 +218,8 @@ def scan_truth(dims, h, grads=False, dstate=True):
 # T, N, heads, head_dim, groups, state, p_first, gate, pad, order
 SCAN = [(1, 1, 1, 1, 1, 1, 0.0, False, 0, "tn"), (1, 3, 4, 64, 1, 64, 0.5, True, 0, "tn"), (31, 2, 2, 32, 2, 16, 0.0, True, 0, "tn"),
         (32, 1, 5, 64, 1, 64, 0.1, False, 0, "nt"), (33, 2, 3, 8, 1, 40, 0.05, True, 1, "tn"), (100, 3, 4, 37, 2, 5, 0.03, True, 3, "nt"),
-        (129, 1, 1, 64, 1, 16, 0.0, False, 8, "tn"), (64, 5, 9, 24, 3, 64, 1.0, True, 0, "tn"), (70, 2, 6, 33, 1, 33, 0.2, False, 0, "tn")]
+        (129, 1, 1, 64, 1, 16, 0.0, False, 8, "tn"), (257, 1, 2, 64, 1, 64, 0.005, True, 0, "tn"), (610, 2, 3, 9, 1, 21, 0.0, False, 0, "nt"),
+        (333, 1, 8, 40, 2, 16, 0.3, True, 0, "tn"), (64, 5, 9, 24, 3, 64, 1.0, True, 0, "tn"), (70, 2, 6, 33, 1, 33, 0.2, False, 0, "tn")]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
@@ -304,11 +305,12 @@ def test_scan_carries_its_state(dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-def test_scan_keeps_episodes_apart(dtype):
+@pytest.mark.parametrize("T", [50, 400])   # one span of time, several
+def test_scan_keeps_episodes_apart(T, dtype):
     """Infinite and undefined inputs reach nothing of another episode, nothing of an earlier step, no other head or environment."""
     torch = _torch()
-    dims, h, d = scan_problem(50, 2, 3, 40, 1, 24, dtype, 0.0, True, seed=5)
-    first = torch.zeros(50, 2, dtype=torch.uint8)
+    dims, h, d = scan_problem(T, 2, 3, 40, 1, 24, dtype, 0.0, True, seed=5)
+    first = torch.zeros(T, 2, dtype=torch.uint8)
     first[20, 0] = first[45, 0] = 1
     h["first"], d["first"] = first, first.cuda()
     y0, out0, s0 = run_scan(dims, d, saved=True)
