@@ -181,6 +181,7 @@ struct AdExpand {
     static constexpr int K16 = RP / 16, KF = RP / 2;
     AdFactor<T, BWD> F;
     bool vec;
+    int kf;  // fp32: half the rank, rounded up; lane group lg takes values kf lg ..
     uint4 fb[BF ? 2 * K16 : 1];
     float ff[BF ? 1 : 2 * KF];
     __device__ inline void fetch(int p, int n0) {
@@ -193,7 +194,8 @@ struct AdExpand {
                 for (int s = 0; s < K16; ++s) fb[b * K16 + s] = F.frag(p, n, 16 * s + 8 * lg, vec);
             } else {
 #pragma unroll
-                for (int s = 0; s < KF; ++s) ff[b * KF + s] = to_f(F.get(p, n, KF * lg + s));
+                for (int s = 0; s < KF; ++s)
+                    if (s < kf) ff[b * KF + s] = to_f(F.get(p, n, kf * lg + s));
             }
         }
     }
@@ -203,6 +205,7 @@ struct AdExpand {
         uint64_t todo = __ballot(p >= 0) & 0xffffffffull;
         if (!todo) return;
         vec = (F.r & 7) == 0;
+        kf = (F.r + 1) / 2;
         const float* um = u + (int64_t)(m < g.M ? m : g.M - 1) * RP;
         uint4 hi[BF ? K16 : 1], lo[BF ? K16 : 1];
         float uf[BF ? 1 : KF];
@@ -222,10 +225,8 @@ struct AdExpand {
             }
         } else {
 #pragma unroll
-            for (int s = 0; s < KF; s += 4) {
-                const float4 a = *reinterpret_cast<const float4*>(um + KF * lg + s);
-                uf[s] = a.x; uf[s + 1] = a.y; uf[s + 2] = a.z; uf[s + 3] = a.w;
-            }
+            for (int s = 0; s < KF; ++s)
+                if (s < kf) uf[s] = um[kf * lg + s];
         }
         auto next = [&]() {
             const int q = __builtin_amdgcn_readlane(p, __ffsll((unsigned long long)todo) - 1);
@@ -252,7 +253,8 @@ struct AdExpand {
                     for (int s = 0; s < K16; ++s) Mma32<bf16_t>::run(now.fb[b * K16 + s], hi[s], t);
                 } else {
 #pragma unroll
-                    for (int s = 0; s < KF; ++s) t = __builtin_amdgcn_mfma_f32_32x32x2f32(now.ff[b * KF + s], uf[s], t, 0, 0, 0);
+                    for (int s = 0; s < KF; ++s)
+                        if (s < kf) t = __builtin_amdgcn_mfma_f32_32x32x2f32(now.ff[b * KF + s], uf[s], t, 0, 0, 0);
                 }
 #pragma unroll
                 for (int e = 0; e < 16; ++e) acc[b][e] += p == mine ? t[e] : 0.f;
@@ -567,82 +569,128 @@ __global__ __launch_bounds__(256, MB == 2 ? 3 : 2) void k_ad_gemm_dma(AdArgs g) 
     for (int i = 0; i < MB; ++i) ad_finish<bf16_t, ROLE, RP>(g, acc[i], patch, tm + wm + 32 * i, tn + wn);
 }
 
-// ---- few rows: every workgroup sixteen columns of the output for 64 rows, its eight waves sharing the contraction --------------------
+// ---- few rows: every workgroup sixteen columns of the output for 32 rows, its eight waves sharing the contraction --------------------
 // Bound by the latency of its few loads and the stream of W0, each row of which is read once; operands go straight into registers, 16
 // bytes a lane, and the waves' sums meet in LDS, where the adapters' part joins them in fp32: with so few rows each may have its own.
-template <typename T>
-__device__ inline uint4 ad_piece(const T* p, int64_t stride, int avail, bool vec) {  // 16 bytes of values `stride` apart
+// Sixteen bytes of a row of K values from k on, zero where it ends or `on` is false: one access where whole pieces make up the row (WHOLE;
+// with the alignment of one element only), else one a value; no branch goes by the lane.
+template <bool WHOLE, typename T>
+__device__ inline uint4 ad_piece(const T* row, int k, int K, bool on) {
     constexpr int VE = 16 / (int)sizeof(T);
-    if (vec && avail >= VE) return *reinterpret_cast<const uint4*>(p);
+    typedef T vec_t __attribute__((ext_vector_type(VE), aligned(sizeof(T))));
+    if constexpr (WHOLE) {
+        const bool have = on && k < K;
+        const uint4 u = __builtin_bit_cast(uint4, *reinterpret_cast<const vec_t*>(row + (have ? k : 0)));
+        return make_uint4(have ? u.x : 0, have ? u.y : 0, have ? u.z : 0, have ? u.w : 0);
+    }
     T e[VE];
 #pragma unroll
-    for (int i = 0; i < VE; ++i) e[i] = i < avail ? p[i * stride] : (T)0.f;
+    for (int i = 0; i < VE; ++i) {
+        const bool have = on && k + i < K;
+        const T v = row[have ? k + i : 0];
+        e[i] = have ? v : (T)0.f;
+    }
     return *reinterpret_cast<uint4*>(e);
 }
-template <typename T, bool BWD>
+template <typename T>
+__device__ inline uint4 ad_piece_of(bool whole, const T* row, int k, int K, bool on) {
+    return whole ? ad_piece<true>(row, k, K, on) : ad_piece<false>(row, k, K, on);
+}
+// the same of a column: values `stride` apart
+template <typename T>
+__device__ inline uint4 ad_column(const T* col, int64_t stride, int k, int K) {
+    constexpr int VE = 16 / (int)sizeof(T);
+    T e[VE];
+#pragma unroll
+    for (int i = 0; i < VE; ++i) {
+        const T v = col[(int64_t)(k + i < K ? k + i : 0) * stride];
+        e[i] = k + i < K ? v : (T)0.f;
+    }
+    return *reinterpret_cast<uint4*>(e);
+}
+// A workgroup has 16 columns x 32 rows, an output a thread; rows beyond the last one repeat it.
+template <typename T, bool BWD, int RP, bool WHOLE>
 __global__ __launch_bounds__(512) void k_ad_few(AdArgs g) {
-    constexpr int VE = 16 / (int)sizeof(T), KS_ = 4 * VE;  // contraction indices of a step
-    __shared__ float red[8][64][17];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, l16 = lane & 15, kg = lane >> 4;
-    const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 64;
+    constexpr int VE = 16 / (int)sizeof(T), STEP = 4 * VE, U = BWD ? 2 : 4;  // contraction indices of a step; steps requested together
+    __shared__ float red[8][32][17];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, l16 = lane & 15, kg = lane >> 4;
+    const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 32;
     const int K = BWD ? g.O : g.I, N = BWD ? g.I : g.O;
     const int64_t ld = BWD ? g.ld_y : g.ld_x;
     const T *src = reinterpret_cast<const T*>(BWD ? g.dy : g.x), *w0 = reinterpret_cast<const T*>(g.w0);
-    const bool vx = ad_vec(src, ld, sizeof(T)), vw = !BWD && ad_vec(w0, g.I, sizeof(T));
+    const int m = m0 + (int)threadIdx.x / 16, c = n0 + (int)threadIdx.x % 16, cc = c < N ? c : N - 1;
+    const int adapter = g.adapter(m);
     const int n = n0 + l16 < N ? n0 + l16 : N - 1;
     const T* wrow = w0 + (BWD ? (int64_t)n : (int64_t)n * g.I);
-    const int64_t ws = BWD ? g.I : 1;
-    const T* xrow[4];
+    const T* xrow[2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int m = m0 + 16 * i + l16;
-        xrow[i] = src + (int64_t)g.row(m < g.M ? m : g.M - 1) * ld;
+    for (int i = 0; i < 2; ++i) {
+        const int r = m0 + 16 * i + l16;
+        xrow[i] = src + (int64_t)g.row(r < g.M ? r : g.M - 1) * ld;
     }
-    const int blocks = (g.M - m0 + 15) / 16 < 4 ? (g.M - m0 + 15) / 16 : 4;
-    float4_t acc[4] = {};
-#pragma unroll 4
-    for (int k = wave * KS_; k < K; k += 8 * KS_) {
-        const int kk = k + VE * kg;
-        const uint4 fw = ad_piece(wrow + kk * ws, ws, K - kk, vw);
+    float4_t acc[2] = {};
+    auto steps = [&](auto count, int k) {
+        constexpr int C = decltype(count)::value;
+        uint4 fw[C], fx[C][2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < blocks) Mma16<T>::run(fw, ad_piece(xrow[i] + kk, 1, K - kk, vx), acc[i]);
-    }
+        for (int s = 0; s < C; ++s) {
+            const int kk = k + 8 * STEP * s + VE * kg;
+            fw[s] = BWD ? ad_column(wrow, g.I, kk, K) : ad_piece<WHOLE>(wrow, kk, K, true);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 2; ++i) fx[s][i] = ad_piece<WHOLE>(xrow[i], kk, K, true);
+        }
+#pragma unroll
+        for (int s = 0; s < C; ++s)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) Mma16<T>::run(fw[s], fx[s][i], acc[i]);
+    };
+    int k = wave * STEP;
+    for (; k + 8 * STEP * (U - 1) < K; k += 8 * STEP * U) steps(std::integral_constant<int, U>{}, k);
+    for (; k < K; k += 8 * STEP) steps(std::integral_constant<int, 1>{}, k);
+    // the adapter's part
+    const AdFactor<T, BWD> F = {reinterpret_cast<const T*>(BWD ? g.B : g.A), N, g.r};
+    const T* fp = F.at(adapter < 0 ? 0 : adapter, cc, 0);
+    uint4 f[RP / VE];
+#pragma unroll
+    for (int j = 0; j < RP / VE; ++j) f[j] = BWD ? ad_column(fp, N, j * VE, g.r) : ad_piece_of(g.r % VE == 0, fp, j * VE, g.r, true);
+    const float4* um = reinterpret_cast<const float4*>((BWD ? g.v : g.u) + (int64_t)(m < g.M ? m : g.M - 1) * RP);
+    float4 uv[RP / 4];
+#pragma unroll
+    for (int j = 0; j < RP / 4; ++j) uv[j] = um[j];
+    const float bias = !BWD && g.bias ? g.bias[cc] : 0.f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) red[wave][16 * i + l16][4 * kg + e] = acc[i][e];
     __syncthreads();
-    const AdFactor<T, BWD> F = {reinterpret_cast<const T*>(BWD ? g.B : g.A), N, g.r};
-    const float* u = BWD ? g.v : g.u;
-    for (int o = threadIdx.x; o < 16 * 64; o += 512) {
-        const int m = m0 + o / 16, c = n0 + o % 16;
-        if (m >= g.M || c >= N) continue;
-        float s = 0.f;
+    float s = 0.f, t = 0.f;
 #pragma unroll
-        for (int q = 0; q < 8; ++q) s += red[q][o / 16][o % 16];
-        if (!BWD && g.bias) s += g.bias[c];
-        const int p = g.adapter(m);
-        if (p >= 0) {
-            float t = 0.f;
-            const T* f = F.at(p, c, 0);
-            const int64_t fs = BWD ? N : 1;
-#pragma unroll 8
-            for (int j = 0; j < g.r; ++j) t += u[(int64_t)m * g.rp + j] * to_f(f[j * fs]);
-            s += t;
-        }
+    for (int q = 0; q < 8; ++q) s += red[q][threadIdx.x / 16][threadIdx.x % 16];
+    s += bias;
+#pragma unroll
+    for (int j = 0; j < RP; ++j) {
+        const float4 q = uv[j / 4];
+        const T* e = reinterpret_cast<const T*>(&f[j / VE]);
+        t += (j % 4 == 0 ? q.x : j % 4 == 1 ? q.y : j % 4 == 2 ? q.z : q.w) * to_f(e[j % VE]);
+    }
+    if (adapter >= 0) s += t;
+    if (m < g.M && c < N) {
         if (BWD) reinterpret_cast<T*>(g.dx)[(int64_t)g.row(m) * g.ld_x + c] = cvt<T>(s);
         else reinterpret_cast<T*>(g.y)[(int64_t)m * g.ld_y + c] = cvt<T>(s);
     }
 }
 
 // ---- u (or v): the rows' products with their adapters' short factor ------------------------------------------------------------------
-// Few rows: one a workgroup, whose threads share the contraction; the factor's values are used once.
-template <typename T, bool BWD, int RP>
+// Few rows, or small factors: WPR waves a row (four, or one where the contraction is short), which share the contraction; a factor's
+// values are used once.
+template <typename T, bool BWD, int RP, int WPR, bool WHOLE>
 __global__ __launch_bounds__(256) void k_ad_shrink_row(AdArgs g) {
     constexpr int VE = 16 / (int)sizeof(T);
     __shared__ float part[4][RP];
-    const int m = blockIdx.x, p = g.adapter(m), wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int m = WPR == 4 ? blockIdx.x : blockIdx.x * 4 + wave, tid = WPR == 4 ? threadIdx.x : lane;
+    if (WPR == 1 && m >= g.M) return;
+    const int p = __builtin_amdgcn_readfirstlane(g.adapter(m));
     const int K = BWD ? g.O : g.I;
     const T* row = reinterpret_cast<const T*>(BWD ? g.dy : g.x) + (int64_t)g.row(m) * (BWD ? g.ld_y : g.ld_x);
     float acc[RP];
@@ -651,33 +699,29 @@ __global__ __launch_bounds__(256) void k_ad_shrink_row(AdArgs g) {
     if (p >= 0) {
         const T* f = reinterpret_cast<const T*>(BWD ? g.A : g.B) + (int64_t)p * K * g.r;
         if (BWD) {  // A_p [O][r]: a thread's rows of it
-            const bool vec = (g.r * (int)sizeof(T)) % 16 == 0;
-            for (int k = threadIdx.x; k < K; k += 256) {
+            for (int k = tid; k < K; k += 64 * WPR) {
                 const float v = to_f(row[k]);
+                uint4 q[RP / VE];
 #pragma unroll
-                for (int j = 0; j < RP; j += VE) {
-                    const uint4 q = ad_piece(f + (int64_t)k * g.r + j, 1, g.r - j, vec);
-                    const T* e = reinterpret_cast<const T*>(&q);
+                for (int j = 0; j < RP / VE; ++j) q[j] = ad_piece<WHOLE>(f + (int64_t)k * g.r, j * VE, g.r, true);
 #pragma unroll
-                    for (int i = 0; i < VE; ++i) acc[j + i] += v * to_f(e[i]);
-                }
+                for (int j = 0; j < RP; ++j) acc[j] += j < g.r ? v * to_f(reinterpret_cast<const T*>(&q[j / VE])[j % VE]) : 0.f;
             }
         } else {  // B_p [r][I]
-            const bool vx = ad_vec(row, 0, sizeof(T)), vf = (K * (int)sizeof(T)) % 16 == 0;
-            for (int k = threadIdx.x * VE; k < K; k += 256 * VE) {
-                const uint4 xq = ad_piece(row + k, 1, K - k, vx);
-                const T* xe = reinterpret_cast<const T*>(&xq);
+            for (int k = tid * VE; k < K; k += 64 * WPR * VE) {
+                uint4 q[RP];
+                const uint4 xq = ad_piece<WHOLE>(row, k, K, true);
 #pragma unroll
-                for (int j = 0; j < RP; ++j) {
-                    const uint4 q = ad_piece(f + (int64_t)j * K + k, 1, j < g.r ? K - k : 0, vf);
-                    const T* e = reinterpret_cast<const T*>(&q);
+                for (int j = 0; j < RP; ++j) q[j] = ad_piece<WHOLE>(f + (int64_t)(j < g.r ? j : 0) * K, k, K, true);
 #pragma unroll
-                    for (int i = 0; i < VE; ++i) acc[j] += to_f(xe[i]) * to_f(e[i]);
-                }
+                for (int j = 0; j < RP; ++j)
+#pragma unroll
+                    for (int i = 0; i < VE; ++i)
+                        acc[j] += j < g.r ? to_f(reinterpret_cast<const T*>(&xq)[i]) * to_f(reinterpret_cast<const T*>(&q[j])[i]) : 0.f;
             }
         }
     }
-    // sums over the wave: of RP values, a lane keeps fewer and fewer
+    // sums over the wave: of RP values, a lane keeps fewer and fewer (bits 5, 4, .. of the lane select the halves of j)
 #pragma unroll
     for (int h = RP / 2, o = 32; h >= 1; h /= 2, o /= 2)
 #pragma unroll
@@ -689,12 +733,17 @@ __global__ __launch_bounds__(256) void k_ad_shrink_row(AdArgs g) {
     float s = acc[0];
 #pragma unroll
     for (int o = 64 / RP / 2; o >= 1; o /= 2) s += __shfl_xor(s, o);
-    // (the lane's value: bits 5, 4, .. of the lane select the halves of j)
-    if (lane % (64 / RP) == 0) part[wave][lane / (64 / RP)] = s;
+    float* out = (BWD ? g.v : g.u) + (int64_t)m * RP;
+    const int j = lane / (64 / RP);
+    if (WPR == 1) {
+        if (lane % (64 / RP) == 0) out[j] = j < g.r && p >= 0 ? s : 0.f;
+        return;
+    }
+    if (lane % (64 / RP) == 0) part[wave][j] = s;
     __syncthreads();
     if (threadIdx.x < RP) {
-        const int j = threadIdx.x;
-        (BWD ? g.v : g.u)[(int64_t)m * RP + j] = j < g.r && p >= 0 ? part[0][j] + part[1][j] + part[2][j] + part[3][j] : 0.f;
+        const int i = threadIdx.x;
+        out[i] = i < g.r && p >= 0 ? part[0][i] + part[1][i] + part[2][i] + part[3][i] : 0.f;
     }
 }
 
@@ -711,12 +760,12 @@ __global__ __launch_bounds__(256) void k_ad_shrink(AdArgs g) {
     const int K = BWD ? g.O : g.I;
     const int64_t ld = BWD ? g.ld_y : g.ld_x;
     const T* base = reinterpret_cast<const T*>(BWD ? g.dy : g.x);
-    const bool vec = ad_vec(base, ld, sizeof(T));
     const T* row = base + (int64_t)g.row(m < g.M ? m : g.M - 1) * ld;
     const T* fac = reinterpret_cast<const T*>(BWD ? g.A : g.B);
     float* out = BWD ? g.v : g.u;
     const int p = g.adapter(m);
     uint64_t todo = __ballot(p >= 0) & 0xffffffffull;
+    const bool whole = K % VE == 0;
     const int kw = ((K + 4 * KI - 1) / (4 * KI)) * KI;  // contraction indices of a wave
     const int k0 = wave * kw, k1 = k0 + kw < K ? k0 + kw : K;
     while (todo) {
@@ -724,7 +773,6 @@ __global__ __launch_bounds__(256) void k_ad_shrink(AdArgs g) {
         const uint64_t mine = __ballot(p == q) & 0xffffffffull;
         todo &= ~mine;
         const T* f = fac + (int64_t)q * K * g.r;
-        const bool fv = !BWD && (K * (int)sizeof(T)) % 16 == 0;
         float16_t acc = zero16();
         for (int k = k0; k < k1; k += KI) {
             if (BWD) {  // KI rows of the factor, r values each, one after the other in memory
@@ -743,9 +791,9 @@ __global__ __launch_bounds__(256) void k_ad_shrink(AdArgs g) {
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
                 const int kk = k + 4 * VE * lg + VE * s;
-                xq[s] = ad_piece(row + kk, 1, K - kk, vec);
+                xq[s] = ad_piece_of(whole, row, kk, K, true);
                 if (!BWD) {
-                    fq[s] = ad_piece(f + (int64_t)lr * K + kk, 1, lr < g.r ? K - kk : 0, fv);
+                    fq[s] = ad_piece_of(whole, f + (int64_t)(lr < g.r ? lr : 0) * K, kk, K, lr < g.r);
                 } else {
                     T e[VE];
 #pragma unroll
@@ -1002,7 +1050,7 @@ static int64_t ad_carve(AdArgs& g, bool bwd, void* ws) {
         g.perm = (int32_t*)take((int64_t)g.M * 4);
         const int64_t tiles = cdiv(g.O, 128) * cdiv(g.I, 128);
         int64_t split = cdiv(512, tiles);  // two workgroups a CU
-        const int64_t most = cdiv(g.M, 256);
+        const int64_t most = cdiv(g.M, 64);
         if (split > most) split = most;
         if (split < 1) split = 1;
         g.kchunk = (int)align_up(cdiv(g.M > 0 ? g.M : 1, split), 32);
@@ -1027,13 +1075,35 @@ int64_t adapter_ws_bytes(const morlax_adapter_dims& d, bool bwd) {
 }
 
 static bool on16(const void* p, int64_t ld, int size) { return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * size)) & 15) == 0; }
-#define AD_FEW_ROWS 512  // rows up to which u and v take a workgroup a row
+// u and v take a workgroup a row where the factors that the rows read, each its own copy, are at most so many bytes (of the L2)
+#define AD_ROW_BYTES (64 << 20)
 
+// run(padded rank, whole) with both as constants
+template <typename F>
+static void pick_rank(const AdArgs& g, bool whole, F run) {
+    typedef std::integral_constant<int, 16> R16;
+    typedef std::integral_constant<int, 32> R32;
+    if (g.rp == 16) {
+        if (whole) run(R16{}, std::true_type{});
+        else run(R16{}, std::false_type{});
+    } else {
+        if (whole) run(R32{}, std::true_type{});
+        else run(R32{}, std::false_type{});
+    }
+}
 template <typename T, bool BWD>
 static void shrink(const AdArgs& g, hipStream_t s) {
-    if (g.M <= AD_FEW_ROWS) {
-        if (g.rp == 16) k_ad_shrink_row<T, BWD, 16><<<g.M, 256, 0, s>>>(g);
-        else k_ad_shrink_row<T, BWD, 32><<<g.M, 256, 0, s>>>(g);
+    const int K = BWD ? g.O : g.I;
+    if ((int64_t)g.M * g.r * K * (int64_t)sizeof(T) <= AD_ROW_BYTES) {
+        const bool one = K <= (BWD ? 256 : 128 * 16 / (int)sizeof(T)) && g.M > 256;  // a wave a row: two rounds of its lanes or four, and waves enough
+        const bool whole = (BWD ? g.r : K) % (16 / (int)sizeof(T)) == 0;
+        auto run = [&](auto rp, auto w) {
+            constexpr int RP = decltype(rp)::value;
+            constexpr bool W = decltype(w)::value;
+            if (one) k_ad_shrink_row<T, BWD, RP, 1, W><<<cdiv(g.M, 4), 256, 0, s>>>(g);
+            else k_ad_shrink_row<T, BWD, RP, 4, W><<<g.M, 256, 0, s>>>(g);
+        };
+        pick_rank(g, whole, run);
     } else {
         k_ad_shrink<T, BWD><<<cdiv(g.M, 32), 256, 0, s>>>(g);
     }
@@ -1047,8 +1117,10 @@ static void product(const AdArgs& g, hipStream_t s) {
     const int64_t tiles = cdiv(rows_a, 128) * cdiv(rows_b, 128);
     const int split = ROLE == AD_DW ? g.split : 1;
     if constexpr (ROLE != AD_DW)
-        if (tiles <= 64 && cdiv(g.M, 64) <= 65535) {
-            k_ad_few<T, ROLE == AD_DX><<<dim3(cdiv(rows_b, 16), cdiv(g.M, 64)), 512, 0, s>>>(g);
+        if ((tiles <= 64 || K <= 64) && cdiv(g.M, 32) <= 65535) {
+            pick_rank(g, K % (16 / (int)sizeof(T)) == 0, [&](auto rp, auto w) {
+                k_ad_few<T, ROLE == AD_DX, decltype(rp)::value, decltype(w)::value><<<dim3(cdiv(rows_b, 16), cdiv(g.M, 32)), 512, 0, s>>>(g);
+            });
             return;
         }
     if constexpr (sizeof(T) == 2) {

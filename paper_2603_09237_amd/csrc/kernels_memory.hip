@@ -35,33 +35,33 @@ static int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 __device__ inline float silu_f(float v) { return v * __builtin_amdgcn_rcpf(1.f + __expf(-v)); }
 __device__ inline float sigmoid_f(float v) { return __builtin_amdgcn_rcpf(1.f + __expf(-v)); }
 
-// V consecutive values as floats: one access of V * sizeof(T) bytes, or (V == 1) of one element
+// V consecutive values as they are in memory: one access, with the alignment of one element
+template <typename T, int V> struct Run {
+    typedef T vec_t __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+    vec_t u;
+    __device__ inline void load(const T* p) { u = *reinterpret_cast<const vec_t*>(p); }
+    __device__ inline float get(int i) const { return (float)u[i]; }
+};
+template <typename T> struct Run<T, 1> {
+    T u;
+    __device__ inline void load(const T* p) { u = *p; }
+    __device__ inline float get(int) const { return to_f(u); }
+};
 template <typename T, int V>
-__device__ inline void load_v(const T* p, float (&v)[V]) {
-    typedef T vec_t __attribute__((ext_vector_type(V)));
-    if constexpr (V == 1) {
-        v[0] = to_f(*p);
-    } else {
-        const vec_t u = *reinterpret_cast<const vec_t*>(p);
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = (float)u[i];
-    }
-}
-template <typename T, int V>
-__device__ inline void store_v(T* p, const float (&v)[V]) {
-    typedef T vec_t __attribute__((ext_vector_type(V)));
+__device__ inline void store_run(T* p, const float (&v)[V]) {
     if constexpr (V == 1) {
         *p = cvt<T>(v[0]);
     } else {
-        vec_t u;
+        typename Run<T, V>::vec_t u;
 #pragma unroll
         for (int i = 0; i < V; ++i) u[i] = (T)v[i];
-        *reinterpret_cast<vec_t*>(p) = u;
+        *reinterpret_cast<typename Run<T, V>::vec_t*>(p) = u;
     }
 }
 
 // ---- convolution ----------------------------------------------------------------------------------------------------
 #define CONV_W 4  // taps that a thread keeps: a shorter convolution's leading ones are absent
+#define CONV_U 4  // time steps whose inputs a thread requests together
 
 struct ConvArgs {
     const void *x, *dy;
@@ -74,57 +74,103 @@ struct ConvArgs {
     int T, N, C, width, act, run, runs, nblocks;
 };
 
-// A thread takes V channels of one environment and a run of time steps, the last inputs in registers.
+// One thread's filters and the last inputs of its V channels (from channel c on) of one environment.
+template <typename T, int V>
+struct Taps {
+    float w[CONV_W][V], b[V], win[CONV_W][V];
+    __device__ inline void init(const ConvArgs& g, int c) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            b[i] = g.b ? g.b[c + i] : 0.f;
+#pragma unroll
+            for (int k = 0; k < CONV_W; ++k) w[k][i] = k >= CONV_W - g.width ? g.w[(int64_t)(c + i) * g.width + k - (CONV_W - g.width)] : 0.f;
+        }
+    }
+    __device__ inline void push(const Run<T, V>& x, bool begins) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+#pragma unroll
+            for (int k = 0; k + 1 < CONV_W; ++k) win[k][i] = begins ? 0.f : win[k + 1][i];
+            win[CONV_W - 1][i] = x.get(i);
+        }
+    }
+    // the inputs before step t0; returns the step among them at which an episode began last, or a very early one
+    __device__ inline int before(const ConvArgs& g, const T* x, int n, int c, int t0) {
+        const int before = g.width - 1;
+        int e = -(1 << 30);
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+#pragma unroll
+            for (int k = 0; k < CONV_W; ++k) win[k][i] = 0.f;
+        for (int t = t0 - before; t < t0; ++t) {
+            Run<T, V> v;
+            bool begins = false;
+            if (t >= 0) {
+                v.load(x + (int64_t)t * g.x_t);
+                begins = g.first && g.first[(int64_t)t * g.N + n];
+            } else if (g.state_in) {
+                v.load(reinterpret_cast<const T*>(g.state_in) + ((int64_t)n * before + t + before) * g.C + c);
+            } else {
+                v.u = (T)0.f;
+            }
+            if (begins) e = t;
+            push(v, begins);
+        }
+        return e;
+    }
+    __device__ inline float sum(const ConvArgs& g, int i) const {
+        float s = b[i];
+#pragma unroll
+        for (int k = 0; k < CONV_W; ++k)
+            if (k >= CONV_W - g.width) s += w[k][i] * win[k][i];
+        return s;
+    }
+};
+
+// A thread takes V channels of one environment and a run of time steps, the last inputs in registers, the next CONV_U requested together.
+// (The last V channels overlap with those before where V does not divide them: both threads write the same values.)  Bound by its
+// reads and writes: a run's first width - 1 inputs are read again.
 template <typename T, int V>
 __global__ __launch_bounds__(256) void k_conv_fwd(ConvArgs g) {
     const int cols = (g.C + V - 1) / V;
     const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int n = (int)(id / cols), c = (int)(id % cols) * V;
+    const int n = (int)(id / cols);
+    int c = (int)(id % cols) * V;
+    c = c + V <= g.C ? c : g.C - V;
     if (n >= g.N) return;
     const int t0 = blockIdx.y * g.run, t1 = t0 + g.run < g.T ? t0 + g.run : g.T, before = g.width - 1;
     const T* x = reinterpret_cast<const T*>(g.x) + (int64_t)n * g.x_n + c;
     T* y = reinterpret_cast<T*>(g.y) + (int64_t)n * g.y_n + c;
-    float w[CONV_W][V], b[V], win[CONV_W][V];
+    Taps<T, V> a;
+    a.init(g, c);
+    a.before(g, x, n, c, t0);
+    for (int t = t0; t < t1; t += CONV_U) {
+        Run<T, V> v[CONV_U];
+        uint32_t first[CONV_U];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        b[i] = g.b ? g.b[c + i] : 0.f;
-#pragma unroll
-        for (int k = 0; k < CONV_W; ++k) {
-            w[k][i] = k >= CONV_W - g.width ? g.w[(int64_t)(c + i) * g.width + k - (CONV_W - g.width)] : 0.f;
-            win[k][i] = 0.f;
+        for (int u = 0; u < CONV_U; ++u) {
+            const int tt = t + u < t1 ? t + u : t1 - 1;
+            v[u].load(x + (int64_t)tt * g.x_t);
+            first[u] = g.first ? g.first[(int64_t)tt * g.N + n] : 0;
         }
-    }
-    for (int t = t0 - before; t < t1; ++t) {
-        float v[V];
-        if (t >= 0) load_v<T, V>(x + (int64_t)t * g.x_t, v);
-        else if (g.state_in) load_v<T, V>(reinterpret_cast<const T*>(g.state_in) + ((int64_t)n * before + t + before) * g.C + c, v);
-        else
 #pragma unroll
-            for (int i = 0; i < V; ++i) v[i] = 0.f;
-        const bool begin = t >= 0 && g.first && g.first[(int64_t)t * g.N + n];
+        for (int u = 0; u < CONV_U; ++u) {
+            if (t + u >= t1) break;
+            a.push(v[u], first[u] != 0);
+            float o[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-#pragma unroll
-            for (int k = 0; k + 1 < CONV_W; ++k) win[k][i] = begin ? 0.f : win[k + 1][i];
-            win[CONV_W - 1][i] = v[i];
+            for (int i = 0; i < V; ++i) {
+                const float s = a.sum(g, i);
+                o[i] = g.act ? silu_f(s) : s;
+            }
+            store_run<T, V>(y + (int64_t)(t + u) * g.y_t, o);
         }
-        if (t < t0) continue;
-        float o[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            float s = b[i];
-#pragma unroll
-            for (int k = 0; k < CONV_W; ++k)
-                if (k >= CONV_W - g.width) s += w[k][i] * win[k][i];
-            o[i] = g.act ? silu_f(s) : s;
-        }
-        store_v<T, V>(y + (int64_t)t * g.y_t, o);
     }
     if (t1 == g.T && g.state_out)
 #pragma unroll
         for (int k = 1; k < CONV_W; ++k)
             if (k > CONV_W - g.width)
-                store_v<T, V>(reinterpret_cast<T*>(g.state_out) + ((int64_t)n * before + k - (CONV_W - g.width) - 1) * g.C + c, win[k]);
+                store_run<T, V>(reinterpret_cast<T*>(g.state_out) + ((int64_t)n * before + k - (CONV_W - g.width) - 1) * g.C + c, a.win[k]);
 }
 
 // A thread's V channels of one environment after the other (n, n + stride, ..) and a run of time steps; it walks width - 1 steps
@@ -132,10 +178,10 @@ __global__ __launch_bounds__(256) void k_conv_fwd(ConvArgs g) {
 // environments of its workgroup, then k_conv_final over the workgroups.
 template <typename T, int V>
 __global__ __launch_bounds__(256) void k_conv_bwd(ConvArgs g, int cols, int rows) {
-    extern __shared__ float red[];  // [rows][cols V (CONV_W + 1)]
-    const int col = threadIdx.x % cols, row = threadIdx.x / cols;
-    const int c = (blockIdx.x * cols + col) * V;
-    const bool live = row < rows && c < g.C;
+    extern __shared__ float red[];  // [rows][CONV_W + 1][cols][V]
+    const int col = threadIdx.x % cols, row = threadIdx.x / cols, chunk = blockIdx.x * cols + col;
+    const bool live = row < rows && chunk * V < g.C;
+    const int c = chunk * V + V <= g.C ? chunk * V : g.C - V;
     const int t0 = blockIdx.z * g.run, t1 = t0 + g.run < g.T ? t0 + g.run : g.T, before = g.width - 1;
     float dw[CONV_W + 1][V];
 #pragma unroll
@@ -143,82 +189,74 @@ __global__ __launch_bounds__(256) void k_conv_bwd(ConvArgs g, int cols, int rows
 #pragma unroll
         for (int k = 0; k <= CONV_W; ++k) dw[k][i] = 0.f;
     if (live) {
-        float w[CONV_W][V], b[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            b[i] = g.b ? g.b[c + i] : 0.f;
-#pragma unroll
-            for (int k = 0; k < CONV_W; ++k) w[k][i] = k >= CONV_W - g.width ? g.w[(int64_t)(c + i) * g.width + k - (CONV_W - g.width)] : 0.f;
-        }
+        Taps<T, V> a;
+        a.init(g, c);
         for (int n = blockIdx.y * rows + row; n < g.N; n += gridDim.y * rows) {
             const T* x = reinterpret_cast<const T*>(g.x) + (int64_t)n * g.x_n + c;
             const T* dy = reinterpret_cast<const T*>(g.dy) + (int64_t)n * g.y_n + c;
             T* dx = reinterpret_cast<T*>(g.dx) + (int64_t)n * g.x_n + c;
-            float win[CONV_W][V], pend[CONV_W][V];  // pend[k]: gradient so far of step t - (CONV_W - 1) + k
+            float pend[CONV_W][V];  // pend[k]: gradient so far of step t - (CONV_W - 1) + k
 #pragma unroll
             for (int i = 0; i < V; ++i)
 #pragma unroll
-                for (int k = 0; k < CONV_W; ++k) win[k][i] = pend[k][i] = 0.f;
-            int e = -(1 << 30);  // the step at which the episode of t began
+                for (int k = 0; k < CONV_W; ++k) pend[k][i] = 0.f;
+            int e = a.before(g, x, n, c, t0);  // the step at which the episode of t began
             // gradient of input s is complete: what the state behind the last step passes back is added
             auto done = [&](int s, const float(&v)[V]) {
-                float o[V], d[V];
+                float o[V];
 #pragma unroll
                 for (int i = 0; i < V; ++i) o[i] = v[i];
                 if (g.dstate_out && s >= g.T - before && s >= e) {
-                    load_v<T, V>(reinterpret_cast<const T*>(g.dstate_out) + ((int64_t)n * before + s - (g.T - before)) * g.C + c, d);
+                    Run<T, V> d;
+                    d.load(reinterpret_cast<const T*>(g.dstate_out) + ((int64_t)n * before + s - (g.T - before)) * g.C + c);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) o[i] += d[i];
+                    for (int i = 0; i < V; ++i) o[i] += d.get(i);
                 }
-                if (s >= t0 && s < t1) store_v<T, V>(dx + (int64_t)s * g.x_t, o);
+                if (s >= t0 && s < t1) store_run<T, V>(dx + (int64_t)s * g.x_t, o);
                 else if (s < 0 && s >= -before && t0 == 0 && g.dstate_in)
-                    store_v<T, V>(reinterpret_cast<T*>(g.dstate_in) + ((int64_t)n * before + s + before) * g.C + c, o);
+                    store_run<T, V>(reinterpret_cast<T*>(g.dstate_in) + ((int64_t)n * before + s + before) * g.C + c, o);
             };
             const int end = t1 + before < g.T ? t1 + before : g.T;
-            for (int t = t0 - before; t < end; ++t) {
-                float v[V];
-                if (t >= 0) load_v<T, V>(x + (int64_t)t * g.x_t, v);
-                else if (g.state_in) load_v<T, V>(reinterpret_cast<const T*>(g.state_in) + ((int64_t)n * before + t + before) * g.C + c, v);
-                else
+            for (int t4 = t0; t4 < end; t4 += CONV_U) {
+                Run<T, V> v[CONV_U], q[CONV_U];
+                uint32_t first[CONV_U];
 #pragma unroll
-                    for (int i = 0; i < V; ++i) v[i] = 0.f;
-                if (t >= 0 && g.first && g.first[(int64_t)t * g.N + n]) e = t;
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-#pragma unroll
-                    for (int k = 0; k + 1 < CONV_W; ++k) win[k][i] = t == e ? 0.f : win[k + 1][i];
-                    win[CONV_W - 1][i] = v[i];
+                for (int u = 0; u < CONV_U; ++u) {
+                    const int tt = t4 + u < end ? t4 + u : end - 1;
+                    v[u].load(x + (int64_t)tt * g.x_t);
+                    q[u].load(dy + (int64_t)tt * g.y_t);
+                    first[u] = g.first ? g.first[(int64_t)tt * g.N + n] : 0;
                 }
-                if (t >= t0) {
-                    float d[V];
-                    load_v<T, V>(dy + (int64_t)t * g.y_t, d);
+#pragma unroll
+                for (int u = 0; u < CONV_U; ++u) {
+                    const int t = t4 + u;
+                    if (t >= end) break;
+                    if (first[u]) e = t;
+                    a.push(v[u], first[u] != 0);
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
+                        float d = q[u].get(i);
                         if (g.act) {
-                            float s = b[i];
-#pragma unroll
-                            for (int k = 0; k < CONV_W; ++k)
-                                if (k >= CONV_W - g.width) s += w[k][i] * win[k][i];
-                            const float sg = sigmoid_f(s);
-                            d[i] *= sg * (1.f + s * (1.f - sg));
+                            const float s = a.sum(g, i), sg = sigmoid_f(s);
+                            d *= sg * (1.f + s * (1.f - sg));
                         }
                         if (t < t1) {
 #pragma unroll
                             for (int k = 0; k < CONV_W; ++k)
-                                if (k >= CONV_W - g.width) dw[k][i] += d[i] * win[k][i];
-                            dw[CONV_W][i] += d[i];
+                                if (k >= CONV_W - g.width) dw[k][i] += d * a.win[k][i];
+                            dw[CONV_W][i] += d;
                         }
 #pragma unroll
                         for (int k = 0; k < CONV_W; ++k)
-                            if (k >= CONV_W - g.width && t - (CONV_W - 1) + k >= e) pend[k][i] += w[k][i] * d[i];
+                            if (k >= CONV_W - g.width && t - (CONV_W - 1) + k >= e) pend[k][i] += a.w[k][i] * d;
                     }
-                }
-                done(t - (CONV_W - 1), pend[0]);
+                    done(t - (CONV_W - 1), pend[0]);
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
+                    for (int i = 0; i < V; ++i) {
 #pragma unroll
-                    for (int k = 0; k + 1 < CONV_W; ++k) pend[k][i] = pend[k + 1][i];
-                    pend[CONV_W - 1][i] = 0.f;
+                        for (int k = 0; k + 1 < CONV_W; ++k) pend[k][i] = pend[k + 1][i];
+                        pend[CONV_W - 1][i] = 0.f;
+                    }
                 }
             }
 #pragma unroll
@@ -230,24 +268,31 @@ __global__ __launch_bounds__(256) void k_conv_bwd(ConvArgs g, int cols, int rows
 #pragma unroll
         for (int k = 0; k <= CONV_W; ++k)
 #pragma unroll
-            for (int i = 0; i < V; ++i) red[row * per + k * cols * V + col * V + i] = dw[k][i];
+            for (int i = 0; i < V; ++i) red[row * per + (k * cols + col) * V + i] = dw[k][i];
     __syncthreads();
     const int blk = blockIdx.z * gridDim.y + blockIdx.y;
     for (int i = threadIdx.x; i < per; i += 256) {
-        const int k = i / (cols * V), cc = blockIdx.x * cols * V + i % (cols * V);
-        if (cc >= g.C) continue;
+        const int k = i / (cols * V), ch = blockIdx.x * cols + i % (cols * V) / V;
+        if (ch * V >= g.C) continue;
         float s = 0.f;
         for (int r = 0; r < rows; ++r) s += red[r * per + i];
-        g.part[((int64_t)blk * (CONV_W + 1) + k) * g.C + cc] = s;
+        g.part[((int64_t)blk * (CONV_W + 1) + k) * g.C + (ch * V + V <= g.C ? ch * V : g.C - V) + i % V] = s;
     }
 }
-// the workgroups' sums in order
+// the workgroups' sums: 32 of them a workgroup, eight groups of threads a contiguous eighth each, in order
 __global__ __launch_bounds__(256) void k_conv_final(ConvArgs g) {
-    const int i = blockIdx.x * 256 + threadIdx.x;
-    if (i >= (CONV_W + 1) * g.C) return;
-    const int k = i / g.C, c = i % g.C;
+    __shared__ float sums[8][32];
+    const int total = (CONV_W + 1) * g.C, i = blockIdx.x * 32 + threadIdx.x % 32, q = threadIdx.x / 32;
+    const int each = (g.nblocks + 7) / 8, b1 = (q + 1) * each < g.nblocks ? (q + 1) * each : g.nblocks;
     float s = 0.f;
-    for (int q = 0; q < g.nblocks; ++q) s += g.part[((int64_t)q * (CONV_W + 1) + k) * g.C + c];
+    if (i < total)
+#pragma unroll 8
+        for (int b = q * each; b < b1; ++b) s += g.part[(int64_t)b * total + i];
+    sums[q][threadIdx.x % 32] = s;
+    __syncthreads();
+    if (q != 0 || i >= total) return;
+    for (int j = 1; j < 8; ++j) s += sums[j][threadIdx.x];
+    const int k = i / g.C, c = i % g.C;
     if (k == CONV_W) {
         if (g.db) g.db[c] = s;
     } else if (k >= CONV_W - g.width && g.dw) {
@@ -1474,13 +1519,6 @@ __global__ __launch_bounds__(256) void k_memory_step(StepArgs a, int lpr, int ve
 }
 
 // ---- host side ------------------------------------------------------------------------------------------------------
-static bool on16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
-// whether rows of 16-byte pieces do for every tensor of a convolution
-static bool conv_vec(const morlax_conv_dims& d, const ConvArgs& g) {
-    const int64_t V = d.dtype ? 8 : 4;
-    return d.channels % V == 0 && d.x_t % V == 0 && d.x_n % V == 0 && d.y_t % V == 0 && d.y_n % V == 0 && on16(g.x) && on16(g.y) && on16(g.dy) &&
-           on16(g.dx);
-}
 static void conv_runs(ConvArgs& g, int64_t threads) {
     // runs of time steps long enough that the steps before them, read again, do not count, where there are threads enough without
     int run = g.T;
@@ -1494,7 +1532,7 @@ static ConvArgs conv_args(const morlax_conv_dims& d) {
     g.x_t = d.x_t; g.x_n = d.x_n; g.y_t = d.y_t; g.y_n = d.y_n;
     return g;
 }
-#define CONV_BLOCKS 1024  // workgroups that leave sums, at most
+#define CONV_BLOCKS 512  // workgroups that leave sums, at most
 int64_t conv_ws_bytes(const morlax_conv_dims& d) { return (int64_t)CONV_BLOCKS * (CONV_W + 1) * d.channels * 4; }
 template <typename T, int V>
 static void conv_fwd(ConvArgs& g, hipStream_t s) {
@@ -1506,19 +1544,18 @@ void launch_conv_fwd(const morlax_conv_dims& d, const void* x, const float* w, c
                      void* state_out, hipStream_t s) {
     ConvArgs g = conv_args(d);
     g.x = x; g.w = w; g.b = b; g.first = first; g.state_in = state_in; g.y = y; g.state_out = state_out;
-    const bool vec = conv_vec(d, g);
     if (d.dtype) {
-        if (vec) conv_fwd<bf16_t, 8>(g, s);
+        if (g.C >= 8) conv_fwd<bf16_t, 8>(g, s);
         else conv_fwd<bf16_t, 1>(g, s);
     } else {
-        if (vec) conv_fwd<float, 4>(g, s);
+        if (g.C >= 4) conv_fwd<float, 4>(g, s);
         else conv_fwd<float, 1>(g, s);
     }
 }
 template <typename T, int V>
 static void conv_bwd(ConvArgs& g, hipStream_t s) {
     const int chunks = (int)cdiv(g.C, V);
-    const int cols = chunks < 64 ? chunks : 64, rows = 256 / cols;
+    const int cols = (int)cdiv(chunks, cdiv(chunks, 64)), rows = 256 / cols;
     conv_runs(g, (int64_t)chunks * g.N);
     if (g.runs > CONV_BLOCKS) {
         g.run = (int)cdiv(g.T, CONV_BLOCKS);
@@ -1529,19 +1566,18 @@ static void conv_bwd(ConvArgs& g, hipStream_t s) {
     if (by > most) by = most;
     g.nblocks = (int)(by * g.runs);
     k_conv_bwd<T, V><<<dim3(cdiv(chunks, cols), by, g.runs), 256, rows * cols * V * (CONV_W + 1) * 4, s>>>(g, cols, rows);
-    k_conv_final<<<cdiv((CONV_W + 1) * (int64_t)g.C, 256), 256, 0, s>>>(g);
+    k_conv_final<<<cdiv((CONV_W + 1) * (int64_t)g.C, 32), 256, 0, s>>>(g);
 }
 void launch_conv_bwd(const morlax_conv_dims& d, const void* x, const float* w, const float* b, const uint8_t* first, const void* state_in,
                      const void* dy, const void* dstate_out, void* dx, float* dw, float* db, void* dstate_in, void* ws, hipStream_t s) {
     ConvArgs g = conv_args(d);
     g.x = x; g.w = w; g.b = b; g.first = first; g.state_in = state_in; g.dy = dy; g.dstate_out = dstate_out;
     g.dx = dx; g.dw = dw; g.db = db; g.dstate_in = dstate_in; g.part = (float*)ws;
-    const bool vec = conv_vec(d, g);
     if (d.dtype) {
-        if (vec) conv_bwd<bf16_t, 8>(g, s);
+        if (g.C >= 4) conv_bwd<bf16_t, 4>(g, s);
         else conv_bwd<bf16_t, 1>(g, s);
     } else {
-        if (vec) conv_bwd<float, 4>(g, s);
+        if (g.C >= 4) conv_bwd<float, 4>(g, s);
         else conv_bwd<float, 1>(g, s);
     }
 }
