@@ -320,33 +320,69 @@ struct ScanArgs {
 
 template <typename T> struct Planes { static constexpr int N = sizeof(T) == 4 ? 3 : 1; };
 
-// Eight consecutive values of a row of `width` at column 8 c8, zero where the row ends or `on` is false.  No branch goes by the lane: rows that
-// are whole pieces of eight take one access (to the start of a row that exists, where there is none), others one a value.  (16-byte
-// accesses need the alignment of one element only.)
+// Eight consecutive values of a row of `width` at column 8 c8 as they are in memory, zero where the row ends or `on` is false.  No branch
+// goes by the lane: rows that are whole pieces of eight take one access (to the start of a row that exists, where there is none), others
+// one a value.  (16-byte accesses need the alignment of one element only.)
 template <typename T>
-__device__ inline void load8_raw(const T* row0, int64_t off, int c8, int width, bool on, float (&v)[8]) {
-    typedef T vec_t __attribute__((ext_vector_type(8), aligned(sizeof(T))));
-    if (width % 8 == 0) {
-        const bool have = on && 8 * c8 < width;
-        const vec_t u = *reinterpret_cast<const vec_t*>(row0 + (have ? off + 8 * c8 : 0));
+struct Eight {
+    uint4 u[sizeof(T) / 2];
+    __device__ inline void load(const T* row0, int64_t off, int c8, int width, bool on) {
+        typedef T vec_t __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+        if (width % 8 == 0) {
+            const bool have = on && 8 * c8 < width;
+            const vec_t v = *reinterpret_cast<const vec_t*>(row0 + (have ? off + 8 * c8 : 0));
+            __builtin_memcpy(u, &v, sizeof(u));
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = have ? (float)u[i] : 0.f;
-    } else {
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) u[i] = make_uint4(have ? u[i].x : 0, have ? u[i].y : 0, have ? u[i].z : 0, have ? u[i].w : 0);
+        } else {
+            T e[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const bool have = on && 8 * c8 + i < width;
-            const float e = to_f(row0[have ? off + 8 * c8 + i : 0]);
-            v[i] = have ? e : 0.f;
+            for (int i = 0; i < 8; ++i) {
+                const bool have = on && 8 * c8 + i < width;
+                const T v = row0[have ? off + 8 * c8 + i : 0];
+                e[i] = have ? v : (T)0.f;
+            }
+            __builtin_memcpy(u, e, sizeof(u));
         }
     }
-}
-template <int NP>
-__device__ inline void parts8(const float (&v)[8], uint4 (&p)[NP]) {
-    if constexpr (NP == 1) {
-        p[0] = pack_chunk<bf16_t>(v);
-    } else {
-        split3(v, p);
+    __device__ inline void get(float (&v)[8]) const {
+        const uint32_t w[8] = {u[0].x, u[0].y, u[0].z, u[0].w, u[sizeof(T) / 2 - 1].x, u[sizeof(T) / 2 - 1].y, u[sizeof(T) / 2 - 1].z, u[sizeof(T) / 2 - 1].w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[i] = sizeof(T) == 4 ? __uint_as_float(w[i]) : __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
     }
+    // the larger of `top` and the magnitudes here, as bits: infinite and undefined values are the largest
+    __device__ inline uint32_t largest(uint32_t top) const {
+        const uint32_t w[8] = {u[0].x, u[0].y, u[0].z, u[0].w, u[sizeof(T) / 2 - 1].x, u[sizeof(T) / 2 - 1].y, u[sizeof(T) / 2 - 1].z, u[sizeof(T) / 2 - 1].w};
+        typedef unsigned short half_t __attribute__((ext_vector_type(2)));
+#pragma unroll
+        for (int i = 0; i < (sizeof(T) == 4 ? 8 : 4); ++i) {
+            if (sizeof(T) == 4) {
+                const uint32_t m = w[i] & 0x7fffffffu;
+                top = m > top ? m : top;
+            } else {
+                top = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(half_t, w[i] & 0x7fff7fffu), __builtin_bit_cast(half_t, top)));
+            }
+        }
+        return top;
+    }
+    __device__ static inline bool finite(uint32_t top) { return sizeof(T) == 4 ? top < 0x7f800000u : (top & 0xffffu) < 0x7f80u && top >> 16 < 0x7f80u; }
+};
+__device__ inline void parts8(const Eight<bf16_t>& e, uint4 (&p)[1]) { p[0] = e.u[0]; }
+__device__ inline void parts8(const Eight<float>& e, uint4 (&p)[3]) {
+    float v[8];
+    e.get(v);
+    split3(v, p);
+}
+// eight values as two or three parts: two leave out 2^-17 of them, where the result is rounded to bf16 anyway
+__device__ inline void split_parts(const float (&v)[8], uint4 (&p)[3]) { split3(v, p); }
+__device__ inline void split_parts(const float (&v)[8], uint4 (&p)[2]) {
+    float l[8];
+    p[0] = pack_chunk<bf16_t>(v);
+    const uint32_t w[4] = {p[0].x, p[0].y, p[0].z, p[0].w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) l[i] = v[i] - __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+    p[1] = pack_chunk<bf16_t>(l);
 }
 // a += sum of products of parts i, j with i + j <= 2, smallest first
 template <int NA, int NB>
@@ -415,45 +451,53 @@ struct Tile {
     }
 };
 
-// the rows t0 .. t0 + cnt - 1 of a tensor into a tile (others zero); returns whether a value of this lane is undefined or infinite
-template <typename T, int B, int NP>
-__device__ inline bool stage(const Tile<B, NP>& tile, const T* base, int64_t st, int t0, int cnt, int width) {
+// The rows t0 .. t0 + cnt - 1 of a tensor on their way to a tile (others zero), 2 B pieces of eight values a lane.  All of a chunk's tensors
+// are requested before the first is put down: one latency, not one each.
+template <typename T, int B>
+struct Fetch {
+    static constexpr int CH = 4 * B;
+    Eight<T> v[2 * B];
+    __device__ inline void request(const T* base, int64_t st, int t0, int cnt, int width) {
+        const int lane = lane_now();
+#pragma unroll
+        for (int i = 0; i < 2 * B; ++i) {
+            const int row = i * (64 / CH) + lane / CH;
+            v[i].load(base + (int64_t)t0 * st, row * st, lane % CH, width, row < cnt);
+        }
+    }
+    // into the tile; whether a value is undefined or infinite
+    template <int NP>
+    __device__ inline bool put(const Tile<B, NP>& tile) const {
+        const int lane = lane_now();
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 2 * B; ++i) {
+            uint4 p[NP];
+            parts8(v[i], p);
+            tile.put(i * (64 / CH) + lane / CH, lane % CH, p);
+            top = v[i].largest(top);
+        }
+        return !Eight<T>::finite(top);
+    }
+};
+// dy silu(z) (without a gate: dy) into a tile, in three parts
+template <typename T, int B>
+__device__ inline bool put_dy(const Tile<B, 3>& tile, const Fetch<T, B>& dy, const Fetch<T, B>& z, bool gate) {
     constexpr int CH = 4 * B;
     const int lane = lane_now();
-    const T* row0 = base + (int64_t)t0 * st;
     float bad = 0.f;
 #pragma unroll
-    for (int i = 0; i < CH / 2; ++i) {
-        const int row = i * (64 / CH) + lane / CH, c8 = lane % CH;
-        float v[8];
-        load8_raw(row0, row * st, c8, width, row < cnt, v);
-        uint4 p[NP];
-        parts8<NP>(v, p);
-        tile.put(row, c8, p);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) bad += v[k] * 0.f;
-    }
-    return !(bad == 0.f);
-}
-// dy silu(z) (z NULL: dy) of a chunk, in three parts
-template <typename T, int PB>
-__device__ inline bool stage_dy(const Tile<PB, 3>& tile, const T* dy, int64_t st, const T* z, int64_t zt, int t0, int cnt, int width) {
-    constexpr int CH = 4 * PB;
-    const int lane = lane_now();
-    float bad = 0.f;
-#pragma unroll
-    for (int i = 0; i < CH / 2; ++i) {
-        const int row = i * (64 / CH) + lane / CH, c8 = lane % CH;
+    for (int i = 0; i < 2 * B; ++i) {
         float v[8], zv[8];
-        load8_raw(dy + (int64_t)t0 * st, row * st, c8, width, row < cnt, v);
-        if (z) {
-            load8_raw(z + (int64_t)t0 * zt, row * zt, c8, width, row < cnt, zv);
+        dy.v[i].get(v);
+        if (gate) {
+            z.v[i].get(zv);
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] *= silu_f(zv[k]);
         }
         uint4 p[3];
         split3(v, p);
-        tile.put(row, c8, p);
+        tile.put(i * (64 / CH) + lane / CH, lane % CH, p);
 #pragma unroll
         for (int k = 0; k < 8; ++k) bad += v[k] * 0.f;
     }
@@ -584,11 +628,12 @@ struct State {
     }
 };
 // eight accumulator values (the second or first half of a block) as an operand's parts
-__device__ inline void acc_parts(const float16_t& a, int half, uint4 (&p)[3]) {
+template <int NP>
+__device__ inline void acc_parts(const float16_t& a, int half, uint4 (&p)[NP]) {
     float v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = a[8 * half + i];
-    split3(v, p);
+    split_parts(v, p);
 }
 // the values of an operand's parts times eight factors, as parts again
 template <int NP>
@@ -664,7 +709,7 @@ struct ScanFwdLds {
 template <typename T, int PB, int SB, bool LOCAL>
 __global__ __launch_bounds__((ScanFwdLds<T, PB, SB>::NW * 64), 2) void k_scan_fwd(ScanArgs g) {
     typedef ScanFwdLds<T, PB, SB> L;
-    constexpr int NP = L::NP;
+    constexpr int NP = L::NP, NY = sizeof(T) == 4 ? 3 : 2;  // parts of what only y sees
     extern __shared__ __align__(16) unsigned char lds[];
     const int wave = wave_index(), lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5;
     const int64_t unit = (int64_t)blockIdx.x * L::NW + wave;
@@ -696,15 +741,21 @@ __global__ __launch_bounds__((ScanFwdLds<T, PB, SB>::NW * 64), 2) void k_scan_fw
     for (int t = t_begin; t < t_end;) {
         int cnt = t_end - t < MEM_Q ? t_end - t : MEM_Q;
         if (slow) cnt = 1;
-        const bool bad = stage(X, x, g.x_t, t, cnt, g.P);
-        if (__any(bad) && cnt > 1) {
+        Fetch<T, PB> fx, fz;
+        Fetch<T, SB> fb, fc;
+        fx.request(x, g.x_t, t, cnt, g.P);
+        fb.request(b, g.x_t, t, cnt, g.S);
+        if (!LOCAL) {
+            fc.request(c, g.x_t, t, cnt, g.S);
+            if (z) fz.request(z, g.z_t, t, cnt, g.P);
+        }
+        phase();
+        if (__any(fx.put(X)) && cnt > 1) {
             slow = cnt;
             continue;
         }
-        phase();
-        stage(B, b, g.x_t, t, cnt, g.S);
-        phase();
-        if (!LOCAL) stage(C, c, g.x_t, t, cnt, g.S);
+        fb.put(B);
+        if (!LOCAL) fc.put(C);
         phase();
         const Steps s = steps<T>(g, n, h, t, cnt, a2, bias, sl);
         // the last step's sums: decay to the chunk's end
@@ -722,14 +773,14 @@ __global__ __launch_bounds__((ScanFwdLds<T, PB, SB>::NW * 64), 2) void k_scan_fw
             for (int p = 0; p < PB; ++p) zero(y[p]);
 #pragma unroll
             for (int kk = 0; kk < 2 * SB; ++kk) {
-                uint4 fb[NP], fc[NP], fh[3];
-                C.rows(kk, fc);
-                B.rows(kk, fb);
-                mma_p(fb, fc, m);
+                uint4 ob[NP], oc[NP], fh[NY];
+                C.rows(kk, oc);
+                B.rows(kk, ob);
+                mma_p(ob, oc, m);
 #pragma unroll
                 for (int p = 0; p < PB; ++p) {
                     acc_parts(st.v[kk / 2][p], kk % 2, fh);
-                    mma_p(fh, fc, y[p]);
+                    mma_p(fh, oc, y[p]);
                 }
             }
             const float in = s.e < 0 ? __builtin_amdgcn_exp2f(s.hi + s.lo) : 0.f;
@@ -762,22 +813,22 @@ __global__ __launch_bounds__((ScanFwdLds<T, PB, SB>::NW * 64), 2) void k_scan_fw
                 for (int e = 0; e < 16; ++e) st.v[i][p][e] = eq < 0 ? st.v[i][p][e] * left : 0.f;
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
-            uint4 fm[3], fx[PB][NP];
+            uint4 fm[NY], ox[PB][NP];
             if (!LOCAL) acc_parts(m, kk, fm);
 #pragma unroll
             for (int p = 0; p < PB; ++p) {
-                X.cols(p, kk, fx[p]);
-                if (!LOCAL) mma_p(fx[p], fm, y[p]);
+                X.cols(p, kk, ox[p]);
+                if (!LOCAL) mma_p(ox[p], fm, y[p]);
             }
             float wk[8];
             eight(sl->w, kk, wk);
 #pragma unroll
             for (int i = 0; i < SB; ++i) {
-                uint4 fb[NP], fw[3];
-                B.cols(i, kk, fb);
-                scaled_parts(fb, wk, fw);
+                uint4 ob[NP], fw[3];
+                B.cols(i, kk, ob);
+                scaled_parts(ob, wk, fw);
 #pragma unroll
-                for (int p = 0; p < PB; ++p) mma_p(fw, fx[p], st.v[i][p]);
+                for (int p = 0; p < PB; ++p) mma_p(fw, ox[p], st.v[i][p]);
             }
         }
         phase();
@@ -803,7 +854,7 @@ __global__ __launch_bounds__((ScanFwdLds<T, PB, SB>::NW * 64), 2) void k_scan_fw
                 patch8(patch + row * (32 * PB + 4), c8, v);
                 if (z) {
                     float zv[8];
-                    load8_raw(z + (int64_t)t * g.z_t, row * g.z_t, c8, g.P, row < cnt, zv);
+                    fz.v[i].get(zv);
 #pragma unroll
                     for (int k = 0; k < 8; ++k) v[k] *= silu_f(zv[k]);
                 }
@@ -877,7 +928,7 @@ struct ScanBwdLds {
 template <typename T, int PB, int SB>
 __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(ScanArgs g) {
     typedef ScanBwdLds<T, PB, SB> L;
-    constexpr int NP = L::NP, NW = L::NW, RP = 32 * SB + 4;
+    constexpr int NP = L::NP, NW = L::NW, RP = 32 * SB + 4, NY = sizeof(T) == 4 ? 3 : 2;  // NY: parts of what only dz and dx see
     extern __shared__ __align__(16) unsigned char lds[];
     const int wave = wave_index(), lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5;
     const int rep = g.H / g.G;
@@ -907,26 +958,10 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
     const float dskip = g.d_skip ? g.d_skip[h] : 0.f, bias = g.dt_bias ? g.dt_bias[h] : 0.f;
     const int64_t per = (int64_t)SB * PB * 1024;
     const float* saved = g.saved + id * (g.chunks + 1) * per;
-    // dh twice: rows n, column p, and rows p, column n -- the operand that a product needs has its contraction in the registers
     State<PB, SB> dh1;
-    float16_t dh2[PB][SB];
     if (g.spans > 1) dh1.undump(g.ends + (id * g.spans + span) * per);
     else if (g.dstate_out) dh1.load(g.dstate_out + id * g.P * g.S, g.P, g.S, red);
     else dh1.clear();
-#pragma unroll
-    for (int p = 0; p < PB; ++p)
-#pragma unroll
-        for (int i = 0; i < SB; ++i) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) red[acc_row(e, lg) * 36 + lr] = dh1.v[i][p][e];
-            phase();
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const float4 f = *reinterpret_cast<const float4*>(red + lr * 36 + 8 * k + 4 * lg);
-                dh2[p][i][4 * k] = f.x; dh2[p][i][4 * k + 1] = f.y; dh2[p][i][4 * k + 2] = f.z; dh2[p][i][4 * k + 3] = f.w;
-            }
-            phase();
-        }
     float sum_a = 0.f, sum_d = 0.f, sum_b = 0.f;  // per lane: of its steps
     float inner;                                  // <state behind the chunk, dh>
     {
@@ -950,20 +985,26 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
             t = t_end - 1;
             cnt = 1;
         }
-        bool bad = stage(X, x, g.x_t, t, cnt, g.P);
+        Fetch<T, PB> fx, fdy, fz;
+        Fetch<T, SB> fb, fc;
+        fx.request(x, g.x_t, t, cnt, g.P);
+        fb.request(b, g.x_t, t, cnt, g.S);
+        fc.request(c, g.x_t, t, cnt, g.S);
+        fdy.request(dy, g.y_t, t, cnt, g.P);
+        if (z) fz.request(z, g.z_t, t, cnt, g.P);
+        // the state before step t
+        State<PB, SB> hin;
+        hin.undump(saved + (int64_t)(base / MEM_Q) * per);
         phase();
-        bad |= stage(B, b, g.x_t, t, cnt, g.S);
+        bool bad = fx.put(X);
+        bad |= fb.put(B);
+        bad |= fc.put(C);
+        bad |= put_dy(D, fdy, fz, z != nullptr);
         phase();
-        bad |= stage(C, c, g.x_t, t, cnt, g.S);
-        phase();
-        bad |= stage_dy(D, dy, g.y_t, z, g.z_t, t, cnt, g.P);
         if (__syncthreads_or(bad) && cnt > 1) {  // all waves step by step together
             slow = cnt;
             continue;
         }
-        // the state before step t
-        State<PB, SB> hin;
-        hin.undump(saved + (int64_t)(base / MEM_Q) * per);
         for (int q = base; q < t; ++q) {  // step by step: forward again from the chunk's start
             const float raw = to_f(reinterpret_cast<const T*>(g.dt)[(int64_t)q * g.dt_t + (int64_t)n * g.dt_n + h]) + bias;
             const float dt = raw > 20.f ? raw : log1pf(expf(raw)), e = __builtin_amdgcn_exp2f((float)((double)dt * a2));
@@ -994,19 +1035,19 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
         zero(g1); zero(g2); zero(r1); zero(r2);
 #pragma unroll
         for (int kk = 0; kk < 2 * SB; ++kk) {
-            uint4 fb[NP], fc[NP];
-            C.rows(kk, fc);
-            B.rows(kk, fb);
-            mma_p(fb, fc, g1);
-            mma_p(fc, fb, g2);
+            uint4 ob[NP], oc[NP];
+            C.rows(kk, oc);
+            B.rows(kk, ob);
+            mma_p(ob, oc, g1);
+            mma_p(oc, ob, g2);
         }
 #pragma unroll
         for (int kk = 0; kk < 2 * PB; ++kk) {
-            uint4 fx[NP], fd[3];
-            X.rows(kk, fx);
+            uint4 ox[NP], fd[3];
+            X.rows(kk, ox);
             D.rows(kk, fd);
-            mma_p(fx, fd, r1);
-            mma_p(fd, fx, r2);
+            mma_p(ox, fd, r1);
+            mma_p(fd, ox, r2);
         }
         phase();
         // m1: scores that give y [s | t]; v1: E R dt_s [s | t]; g2: E scores [t | s]; r2: E R [t | s]
@@ -1031,12 +1072,12 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
             for (int p = 0; p < PB; ++p) zero(y[p]);
 #pragma unroll
             for (int kk = 0; kk < 2 * SB; ++kk) {
-                uint4 fc[NP], fh[3];
-                C.rows(kk, fc);
+                uint4 oc[NP], fh[NY];
+                C.rows(kk, oc);
 #pragma unroll
                 for (int p = 0; p < PB; ++p) {
                     acc_parts(hin.v[kk / 2][p], kk % 2, fh);
-                    mma_p(fh, fc, y[p]);
+                    mma_p(fh, oc, y[p]);
                 }
             }
 #pragma unroll
@@ -1045,12 +1086,12 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
                 for (int e = 0; e < 16; ++e) y[p][e] = s.e < 0 ? y[p][e] * qs : 0.f;
 #pragma unroll
             for (int kk = 0; kk < 2; ++kk) {
-                uint4 fm[3], fx[NP];
+                uint4 fm[NY], ox[NP];
                 acc_parts(m1, kk, fm);
 #pragma unroll
                 for (int p = 0; p < PB; ++p) {
-                    X.cols(p, kk, fx);
-                    mma_p(fx, fm, y[p]);
+                    X.cols(p, kk, ox);
+                    mma_p(ox, fm, y[p]);
                 }
             }
 #pragma unroll
@@ -1072,8 +1113,8 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
                 const int row = i * (64 / CH) + ln / CH, c8 = ln % CH;
                 float v[8], dv[8], zv[8];
                 patch8(red + row * (32 * PB + 4), c8, v);
-                load8_raw(dy + (int64_t)t * g.y_t, row * g.y_t, c8, g.P, row < cnt, dv);
-                load8_raw(z + (int64_t)t * g.z_t, row * g.z_t, c8, g.P, row < cnt, zv);
+                fdy.v[i].get(dv);
+                fz.v[i].get(zv);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                     const float sg = sigmoid_f(zv[k]);
@@ -1091,12 +1132,12 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
             for (int p = 0; p < PB; ++p) zero(o[p]);
 #pragma unroll
             for (int kk = 0; kk < 2 * SB; ++kk) {
-                uint4 fb[NP], fh[3];
-                B.rows(kk, fb);
+                uint4 ob[NP], fh[NY];
+                B.rows(kk, ob);
 #pragma unroll
                 for (int p = 0; p < PB; ++p) {
                     acc_parts(dh1.v[kk / 2][p], kk % 2, fh);
-                    mma_p(fh, fb, o[p]);
+                    mma_p(fh, ob, o[p]);
                 }
             }
 #pragma unroll
@@ -1105,7 +1146,7 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
                 for (int e = 0; e < 16; ++e) o[p][e] = lr >= eq ? o[p][e] * us : 0.f;
 #pragma unroll
             for (int kk = 0; kk < 2; ++kk) {
-                uint4 fm[3], fd[3];
+                uint4 fm[NY], fd[3];
                 acc_parts(g2, kk, fm);
 #pragma unroll
                 for (int p = 0; p < PB; ++p) {
@@ -1150,39 +1191,30 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
             float16_t o[SB];
 #pragma unroll
             for (int i = 0; i < SB; ++i) zero(o[i]);
-            // contraction over p: h_in dy_t, dh x_s
-            if (which) {
+            // contraction over p: h_in dy_t, dh x_s; both have p in their lanes, their blocks are turned in LDS
 #pragma unroll
-                for (int kk = 0; kk < 2 * PB; ++kk) {
-                    uint4 fx[NP], fh[3];
-                    X.rows(kk, fx);
+            for (int p = 0; p < PB; ++p) {
+                uint4 ox[2][NP], od[2][3];
 #pragma unroll
-                    for (int i = 0; i < SB; ++i) {
-                        acc_parts(dh2[kk / 2][i], kk % 2, fh);
-                        mma_p(fh, fx, o[i]);
-                    }
+                for (int kk = 0; kk < 2; ++kk) {
+                    if (which) X.rows(2 * p + kk, ox[kk]);
+                    else D.rows(2 * p + kk, od[kk]);
                 }
-            } else {  // h_in has p in its lanes: its blocks are turned in LDS
 #pragma unroll
-                for (int p = 0; p < PB; ++p) {
-                    uint4 fd[2][3];
-                    D.rows(2 * p, fd[0]);
-                    D.rows(2 * p + 1, fd[1]);
+                for (int i = 0; i < SB; ++i) {
 #pragma unroll
-                    for (int i = 0; i < SB; ++i) {
+                    for (int e = 0; e < 16; ++e) red[acc_row(e, lg) * 36 + lr] = which ? dh1.v[i][p][e] : hin.v[i][p][e];
+                    phase();
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) red[acc_row(e, lg) * 36 + lr] = hin.v[i][p][e];
-                        phase();
-#pragma unroll
-                        for (int kk = 0; kk < 2; ++kk) {
-                            float v[8];
-                            uint4 fh[3];
-                            eight(red + lr * 36, kk, v);
-                            split3(v, fh);
-                            mma_p(fh, fd[kk], o[i]);
-                        }
-                        phase();
+                    for (int kk = 0; kk < 2; ++kk) {
+                        float v[8];
+                        uint4 fh[3];
+                        eight(red + lr * 36, kk, v);
+                        split3(v, fh);
+                        if (which) mma_p(fh, ox[kk], o[i]);
+                        else mma_p(fh, od[kk], o[i]);
                     }
+                    phase();
                 }
             }
             phase();
@@ -1272,7 +1304,6 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     dh1.v[i][p][e] = eq < 0 ? dh1.v[i][p][e] * left : 0.f;
-                    dh2[p][i][e] = eq < 0 ? dh2[p][i][e] * left : 0.f;
                 }
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
@@ -1287,10 +1318,7 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
                 C.cols(i, kk, f);
                 scaled_parts(f, qk, fq);
 #pragma unroll
-                for (int p = 0; p < PB; ++p) {
-                    mma_p(fq, fd[p], dh1.v[i][p]);
-                    mma_p(fd[p], fq, dh2[p][i]);
-                }
+                for (int p = 0; p < PB; ++p) mma_p(fq, fd[p], dh1.v[i][p]);
             }
         }
         float si = 0.f;
@@ -1307,18 +1335,7 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
         if (slow) --slow;
     }
     if (!live) return;
-    if (g.dstate_in && g.spans == 1) {
-        float* m = g.dstate_in + id * g.P * g.S;
-#pragma unroll
-        for (int p = 0; p < PB; ++p)
-#pragma unroll
-            for (int i = 0; i < SB; ++i)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int pp = 32 * p + acc_row(e, lg), nn = 32 * i + lr;
-                    if (nn < g.S && pp < g.P) m[(int64_t)pp * g.S + nn] = dh2[p][i][e];
-                }
-    }
+    if (g.dstate_in && g.spans == 1) dh1.store(g.dstate_in + id * g.P * g.S, g.P, g.S, red);
     for (int o = 32; o; o >>= 1) {
         sum_a += __shfl_xor(sum_a, o);
         sum_d += __shfl_xor(sum_d, o);
@@ -1369,8 +1386,14 @@ __global__ __launch_bounds__(256) void k_scan_bwd_local(ScanArgs g) {
             t = t_end - 1;
             cnt = 1;
         }
-        bool bad = stage(C, c, g.x_t, t, cnt, g.S);
-        bad |= stage_dy(D, dy, g.y_t, z, g.z_t, t, cnt, g.P);
+        Fetch<T, SB> fc;
+        Fetch<T, PB> fdy, fz;
+        fc.request(c, g.x_t, t, cnt, g.S);
+        fdy.request(dy, g.y_t, t, cnt, g.P);
+        if (z) fz.request(z, g.z_t, t, cnt, g.P);
+        phase();
+        bool bad = fc.put(C);
+        bad |= put_dy(D, fdy, fz, z != nullptr);
         if (__any(bad) && cnt > 1) {
             slow = cnt;
             continue;
