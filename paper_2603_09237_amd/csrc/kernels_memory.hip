@@ -326,8 +326,12 @@ template <typename T> struct Planes { static constexpr int N = sizeof(T) == 4 ? 
 template <typename T>
 struct Eight {
     uint4 u[sizeof(T) / 2];
+    typedef T vec_t __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+    __device__ inline void load(const T* p) {
+        const vec_t v = *reinterpret_cast<const vec_t*>(p);
+        __builtin_memcpy(u, &v, sizeof(u));
+    }
     __device__ inline void load(const T* row0, int64_t off, int c8, int width, bool on) {
-        typedef T vec_t __attribute__((ext_vector_type(8), aligned(sizeof(T))));
         if (width % 8 == 0) {
             const bool have = on && 8 * c8 < width;
             const vec_t v = *reinterpret_cast<const vec_t*>(row0 + (have ? off + 8 * c8 : 0));
@@ -459,6 +463,13 @@ struct Fetch {
     Eight<T> v[2 * B];
     __device__ inline void request(const T* base, int64_t st, int t0, int cnt, int width) {
         const int lane = lane_now();
+        if (cnt == MEM_Q && width == 32 * B) {  // a whole tile: nothing to leave out
+            const T* p = base + (int64_t)t0 * st + (int64_t)(lane / CH) * st + lane % CH * 8;
+            const int64_t step = (64 / CH) * st;
+#pragma unroll
+            for (int i = 0; i < 2 * B; ++i) v[i].load(p + i * step);
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < 2 * B; ++i) {
             const int row = i * (64 / CH) + lane / CH;
@@ -510,6 +521,7 @@ struct Steps {
     int e;                  // chunk step at which the episode of this step began, or -1: before the chunk
     bool begins;
 };
+__device__ inline float last_of(float v) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 31)); }
 // small per-chunk arrays in LDS, for lanes that need them by accumulator row
 struct StepLds { float hi[32], lo[32], dt[32], w[32]; int e[32]; };
 
@@ -545,6 +557,10 @@ __device__ inline Steps steps(const ScanArgs& g, int n, int h, int t0, int cnt, 
     return s;
 }
 __device__ inline float decay(float hi1, float lo1, float hi0, float lo0) { return __builtin_amdgcn_exp2f((hi1 - hi0) + (lo1 - lo0)); }
+// v w, and zero where w is zero whatever v is: a step that does not count may hold anything.  (The instruction by the compiler's own name
+// for it: written as assembly, it reads matrix results before they are there, since nobody puts the waits between.)
+extern "C" __device__ float mul_zero_wins(float, float) __asm("llvm.amdgcn.fmul.legacy");
+__device__ inline float counted(float v, float w) { return mul_zero_wins(v, w); }
 __device__ inline int acc_row(int e, int lg) { return 8 * (e / 4) + 4 * lg + e % 4; }
 
 template <int PB, int SB> constexpr int64_t per_state() { return (int64_t)SB * PB * 1024; }  // floats of one as the registers hold it
@@ -567,7 +583,13 @@ struct State {
         for (int p = 0; p < PB; ++p) {
             const int rows = P - 32 * p < 32 ? P - 32 * p : 32, n = rows > 0 ? rows * S : 0;
             const float* from = m + (int64_t)32 * p * S;
-            if (vec)
+            if (vec && S == 32 * SB && rows == 32) {
+                float4 f[4 * SB];
+#pragma unroll
+                for (int i = 0; i < 4 * SB; ++i) f[i] = *reinterpret_cast<const float4*>(from + 256 * i + 4 * lane);
+#pragma unroll
+                for (int i = 0; i < 4 * SB; ++i) *reinterpret_cast<float4*>(patch + (256 * i + 4 * lane) / (32 * SB) * TP + 4 * lane % (32 * SB)) = f[i];
+            } else if (vec)
                 for (int i = 4 * lane; i < n; i += 256) *reinterpret_cast<float4*>(patch + i / S * TP + i % S) = *reinterpret_cast<const float4*>(from + i);
             else
                 for (int i = lane; i < n; i += 64) patch[i / S * TP + i % S] = from[i];
@@ -600,7 +622,12 @@ struct State {
                     *reinterpret_cast<float4*>(patch + lr * TP + 32 * s + 8 * k + 4 * lg) =
                         make_float4(v[s][p][4 * k], v[s][p][4 * k + 1], v[s][p][4 * k + 2], v[s][p][4 * k + 3]);
             phase();
-            if (vec)
+            if (vec && S == 32 * SB && rows == 32) {
+#pragma unroll
+                for (int i = 0; i < 4 * SB; ++i)
+                    *reinterpret_cast<float4*>(to + 256 * i + 4 * lane) =
+                        *reinterpret_cast<const float4*>(patch + (256 * i + 4 * lane) / (32 * SB) * TP + 4 * lane % (32 * SB));
+            } else if (vec)
                 for (int i = 4 * lane; i < n; i += 256) *reinterpret_cast<float4*>(to + i) = *reinterpret_cast<const float4*>(patch + i / S * TP + i % S);
             else
                 for (int i = lane; i < n; i += 64) to[i] = patch[i / S * TP + i % S];
@@ -651,7 +678,7 @@ __device__ inline void scaled_parts(const uint4 (&f)[NP], const float (&w)[8], u
         }
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = w[i] != 0.f ? v[i] * w[i] : 0.f;  // (a step that does not count, whatever it holds)
+    for (int i = 0; i < 8; ++i) v[i] = counted(v[i], w[i]);
     split3(v, p);
 }
 __device__ inline void eight(const float* a, int kk, float (&v)[8]) {  // values of the contraction indices of step kk
@@ -684,6 +711,34 @@ __device__ inline void store8_row(T* p, const float (&v)[8], int c8, int width, 
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if (on && 8 * c8 + i < width) p[8 * c8 + i] = cvt<T>(v[i]);
+    }
+}
+// piece i of a lane's rows of a chunk: store(row pointer) where the tile is whole, as few address steps as the loads take
+template <typename T, int B, typename F>
+__device__ inline void store_tile(T* base, int64_t st, int t0, int cnt, int width, bool live, F values) {
+    constexpr int CH = 4 * B;
+    typedef T vec_t __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+    const int lane = lane_now();
+    if (cnt == MEM_Q && width == 32 * B && live) {
+        T* p = base + (int64_t)t0 * st + (int64_t)(lane / CH) * st + lane % CH * 8;
+        const int64_t step = (64 / CH) * st;
+#pragma unroll
+        for (int i = 0; i < 2 * B; ++i) {
+            float v[8];
+            values(i, i * (64 / CH) + lane / CH, lane % CH, v);
+            vec_t u;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) u[k] = (T)v[k];
+            *reinterpret_cast<vec_t*>(p + i * step) = u;
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 2 * B; ++i) {
+        const int row = i * (64 / CH) + lane / CH;
+        float v[8];
+        values(i, row, lane % CH, v);
+        store8_row(base + (int64_t)(t0 + row) * st, v, lane % CH, width, live && row < cnt);
     }
 }
 __device__ inline void patch8(const float* row, int c8, float (&v)[8]) {
@@ -759,8 +814,8 @@ __global__ __launch_bounds__((ScanFwdLds<T, PB, SB>::NW * 64), 2) void k_scan_fw
         phase();
         const Steps s = steps<T>(g, n, h, t, cnt, a2, bias, sl);
         // the last step's sums: decay to the chunk's end
-        const float hiq = __shfl(s.hi, 31), loq = __shfl(s.lo, 31);
-        const int eq = __shfl(s.e, 31);
+        const float hiq = last_of(s.hi), loq = last_of(s.lo);
+        const int eq = __builtin_amdgcn_readlane(s.e, 31);
         const float w = lr >= eq ? s.dt * decay(hiq, loq, s.hi, s.lo) : 0.f;
         if (lane < 32) sl->w[lr] = w;
         phase();
@@ -787,7 +842,7 @@ __global__ __launch_bounds__((ScanFwdLds<T, PB, SB>::NW * 64), 2) void k_scan_fw
 #pragma unroll
             for (int p = 0; p < PB; ++p)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) y[p][e] = s.e < 0 ? y[p][e] * in : 0.f;
+                for (int e = 0; e < 16; ++e) y[p][e] = counted(y[p][e], in);
 #pragma unroll
             for (int k4 = 0; k4 < 4; ++k4) {
                 const int r0 = 8 * k4 + 4 * lg;
@@ -797,20 +852,20 @@ __global__ __launch_bounds__((ScanFwdLds<T, PB, SB>::NW * 64), 2) void k_scan_fw
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const bool on = r0 + i <= lr && r0 + i >= s.e;
-                    m[4 * k4 + i] = on ? m[4 * k4 + i] * (d[i] * decay(s.hi, s.lo, a[i], bb[i])) : 0.f;
+                    m[4 * k4 + i] = counted(m[4 * k4 + i], on ? d[i] * decay(s.hi, s.lo, a[i], bb[i]) : 0.f);
                 }
             }
         }
         phase();
         // state to the chunk's end: what is left of the old one
         const float left = eq < 0 ? __builtin_amdgcn_exp2f(hiq + loq) : 0.f;
-        if (LOCAL) all = eq < 0 ? all * left : 0.f;
+        if (LOCAL) all *= left;
 #pragma unroll
         for (int i = 0; i < SB; ++i)
 #pragma unroll
             for (int p = 0; p < PB; ++p)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) st.v[i][p][e] = eq < 0 ? st.v[i][p][e] * left : 0.f;
+                for (int e = 0; e < 16; ++e) st.v[i][p][e] = counted(st.v[i][p][e], left);
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
             uint4 fm[NY], ox[PB][NP];
@@ -845,12 +900,7 @@ __global__ __launch_bounds__((ScanFwdLds<T, PB, SB>::NW * 64), 2) void k_scan_fw
             phase();
             to_rows(y, patch);
             phase();
-            constexpr int CH = 4 * PB;
-            const int ln = lane_now();
-#pragma unroll
-            for (int i = 0; i < CH / 2; ++i) {
-                const int row = i * (64 / CH) + ln / CH, c8 = ln % CH;
-                float v[8];
+            store_tile<T, PB>(y_out, g.y_t, t, cnt, g.P, true, [&](int i, int row, int c8, float(&v)[8]) {
                 patch8(patch + row * (32 * PB + 4), c8, v);
                 if (z) {
                     float zv[8];
@@ -858,8 +908,7 @@ __global__ __launch_bounds__((ScanFwdLds<T, PB, SB>::NW * 64), 2) void k_scan_fw
 #pragma unroll
                     for (int k = 0; k < 8; ++k) v[k] *= silu_f(zv[k]);
                 }
-                store8_row(y_out + (int64_t)(t + row) * g.y_t, v, c8, g.P, row < cnt);
-            }
+            });
         }
         phase();
         t += cnt;
@@ -1023,8 +1072,8 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
             }
         }
         const Steps s = steps<T>(g, n, h, t, cnt, a2, bias, sl);
-        const float hiq = __shfl(s.hi, 31), loq = __shfl(s.lo, 31);
-        const int eq = __shfl(s.e, 31);
+        const float hiq = last_of(s.hi), loq = last_of(s.lo);
+        const int eq = __builtin_amdgcn_readlane(s.e, 31);
         const float us = lr >= eq ? decay(hiq, loq, s.hi, s.lo) : 0.f;                     // to the chunk's end
         const float qs = s.e < 0 ? __builtin_amdgcn_exp2f(s.hi + s.lo) : 0.f;              // from its start
         if (lane < 32) sl->w[lr] = qs;
@@ -1058,11 +1107,11 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
             const float rhi = sl->hi[r], rlo = sl->lo[r], rdt = sl->dt[r];
             const int re = sl->e[r];
             const bool on1 = r <= lr && r >= s.e, on2 = r >= lr && lr >= re;
-            const float d1 = decay(s.hi, s.lo, rhi, rlo) * rdt, d2 = decay(rhi, rlo, s.hi, s.lo);
-            m1[e] = on1 ? g1[e] * d1 : 0.f;
-            r1[e] = on1 ? r1[e] * d1 : 0.f;
-            g2[e] = on2 ? g2[e] * d2 : 0.f;
-            r2[e] = on2 ? r2[e] * d2 : 0.f;
+            const float d1 = on1 ? decay(s.hi, s.lo, rhi, rlo) * rdt : 0.f, d2 = on2 ? decay(rhi, rlo, s.hi, s.lo) : 0.f;
+            m1[e] = counted(g1[e], d1);
+            r1[e] = counted(r1[e], d1);
+            g2[e] = counted(g2[e], d2);
+            r2[e] = counted(r2[e], d2);
         }
         phase();
         // dz needs y again
@@ -1083,7 +1132,7 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
 #pragma unroll
             for (int p = 0; p < PB; ++p)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) y[p][e] = s.e < 0 ? y[p][e] * qs : 0.f;
+                for (int e = 0; e < 16; ++e) y[p][e] = counted(y[p][e], qs);
 #pragma unroll
             for (int kk = 0; kk < 2; ++kk) {
                 uint4 fm[NY], ox[NP];
@@ -1106,12 +1155,8 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
             to_rows(y, red);
             phase();
             T* dzo = reinterpret_cast<T*>(g.dz) + (int64_t)n * g.z_n + (int64_t)h * g.P;
-            constexpr int CH = 4 * PB;
-            const int ln = lane_now();
-#pragma unroll
-            for (int i = 0; i < CH / 2; ++i) {
-                const int row = i * (64 / CH) + ln / CH, c8 = ln % CH;
-                float v[8], dv[8], zv[8];
+            store_tile<T, PB>(dzo, g.z_t, t, cnt, g.P, live, [&](int i, int row, int c8, float(&v)[8]) {
+                float dv[8], zv[8];
                 patch8(red + row * (32 * PB + 4), c8, v);
                 fdy.v[i].get(dv);
                 fz.v[i].get(zv);
@@ -1120,8 +1165,7 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
                     const float sg = sigmoid_f(zv[k]);
                     v[k] *= dv[k] * sg * (1.f + zv[k] * (1.f - sg));
                 }
-                store8_row(dzo + (int64_t)(t + row) * g.z_t, v, c8, g.P, live && row < cnt);
-            }
+            });
             phase();
         }
         phase();
@@ -1143,7 +1187,7 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
 #pragma unroll
             for (int p = 0; p < PB; ++p)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) o[p][e] = lr >= eq ? o[p][e] * us : 0.f;
+                for (int e = 0; e < 16; ++e) o[p][e] = counted(o[p][e], us);
 #pragma unroll
             for (int kk = 0; kk < 2; ++kk) {
                 uint4 fm[NY], fd[3];
@@ -1173,15 +1217,7 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
             to_rows(o, red);
             phase();
             T* dxo = reinterpret_cast<T*>(g.dx) + (int64_t)n * g.x_n + (int64_t)h * g.P;
-            constexpr int CH = 4 * PB;
-            const int ln = lane_now();
-#pragma unroll
-            for (int i = 0; i < CH / 2; ++i) {
-                const int row = i * (64 / CH) + ln / CH, c8 = ln % CH;
-                float v[8];
-                patch8(red + row * (32 * PB + 4), c8, v);
-                store8_row(dxo + (int64_t)(t + row) * g.x_t, v, c8, g.P, live && row < cnt);
-            }
+            store_tile<T, PB>(dxo, g.x_t, t, cnt, g.P, live, [&](int, int row, int c8, float(&v)[8]) { patch8(red + row * (32 * PB + 4), c8, v); });
             phase();
         }
         // dC [n | t], dB' [n | s]
@@ -1219,11 +1255,10 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
             }
             phase();
             const float lane_scale = which ? us : qs;
-            const bool lane_on = which ? lr >= eq : s.e < 0;
 #pragma unroll
             for (int i = 0; i < SB; ++i)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) o[i][e] = lane_on ? o[i][e] * lane_scale : 0.f;
+                for (int e = 0; e < 16; ++e) o[i][e] = counted(o[i][e], lane_scale);
 #pragma unroll
             for (int kk = 0; kk < 2; ++kk) {
                 uint4 fv[3], f[NP];
@@ -1303,7 +1338,7 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
             for (int p = 0; p < PB; ++p)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    dh1.v[i][p][e] = eq < 0 ? dh1.v[i][p][e] * left : 0.f;
+                    dh1.v[i][p][e] = counted(dh1.v[i][p][e], left);
                 }
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
@@ -1399,18 +1434,18 @@ __global__ __launch_bounds__(256) void k_scan_bwd_local(ScanArgs g) {
             continue;
         }
         const Steps s = steps<T>(g, n, h, t, cnt, a2, bias, sl);
-        const float hiq = __shfl(s.hi, 31), loq = __shfl(s.lo, 31);
-        const int eq = __shfl(s.e, 31);
+        const float hiq = last_of(s.hi), loq = last_of(s.lo);
+        const int eq = __builtin_amdgcn_readlane(s.e, 31);
         if (lane < 32) sl->w[lr] = s.e < 0 ? __builtin_amdgcn_exp2f(s.hi + s.lo) : 0.f;
         phase();
         const float left = eq < 0 ? __builtin_amdgcn_exp2f(hiq + loq) : 0.f;
-        all = eq < 0 ? all * left : 0.f;
+        all *= left;
 #pragma unroll
         for (int i = 0; i < SB; ++i)
 #pragma unroll
             for (int p = 0; p < PB; ++p)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) dh.v[i][p][e] = eq < 0 ? dh.v[i][p][e] * left : 0.f;
+                for (int e = 0; e < 16; ++e) dh.v[i][p][e] = counted(dh.v[i][p][e], left);
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
             float qk[8];
