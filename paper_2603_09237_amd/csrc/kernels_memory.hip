@@ -61,7 +61,8 @@ __device__ inline void store_run(T* p, const float (&v)[V]) {
 
 // ---- convolution ----------------------------------------------------------------------------------------------------
 #define CONV_W 4  // taps that a thread keeps: a shorter convolution's leading ones are absent
-#define CONV_U 4  // time steps whose inputs a thread requests together
+#define CONV_U 8      // time steps whose inputs a thread requests together: forward
+#define CONV_U_BWD 4  // backward, which keeps more beside them (eight: 61 us instead of 45 for 32 x 1023 x 274 fp32)
 
 struct ConvArgs {
     const void *x, *dy;
@@ -82,8 +83,18 @@ struct Taps {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             b[i] = g.b ? g.b[c + i] : 0.f;
+            if (g.width == CONV_W) {  // (w is 16-byte aligned: so is a filter of four)
+                const float4_t f = *reinterpret_cast<const float4_t*>(g.w + (int64_t)(c + i) * CONV_W);
 #pragma unroll
-            for (int k = 0; k < CONV_W; ++k) w[k][i] = k >= CONV_W - g.width ? g.w[(int64_t)(c + i) * g.width + k - (CONV_W - g.width)] : 0.f;
+                for (int k = 0; k < CONV_W; ++k) w[k][i] = f[k];
+            } else {
+#pragma unroll
+                for (int k = 0; k < CONV_W; ++k) {
+                    const int q = k - (CONV_W - g.width);
+                    const float f = g.w[(int64_t)(c + i) * g.width + (q < 0 ? 0 : q)];
+                    w[k][i] = q < 0 ? 0.f : f;
+                }
+            }
         }
     }
     __device__ inline void push(const Run<T, V>& x, bool begins) {
@@ -102,19 +113,25 @@ struct Taps {
         for (int i = 0; i < V; ++i)
 #pragma unroll
             for (int k = 0; k < CONV_W; ++k) win[k][i] = 0.f;
-        for (int t = t0 - before; t < t0; ++t) {
-            Run<T, V> v;
-            bool begins = false;
-            if (t >= 0) {
-                v.load(x + (int64_t)t * g.x_t);
-                begins = g.first && g.first[(int64_t)t * g.N + n];
+        Run<T, V> v[CONV_W - 1];
+        bool begins[CONV_W - 1];
+#pragma unroll
+        for (int k = 0; k < CONV_W - 1; ++k) {  // input t0 - (CONV_W - 1) + k
+            const int s = t0 - (CONV_W - 1) + k;
+            begins[k] = false;
+            v[k].u = (T)0.f;
+            if (s < t0 - before) continue;
+            if (s >= 0) {
+                v[k].load(x + (int64_t)s * g.x_t);
+                begins[k] = g.first && g.first[(int64_t)s * g.N + n];
             } else if (g.state_in) {
-                v.load(reinterpret_cast<const T*>(g.state_in) + ((int64_t)n * before + t + before) * g.C + c);
-            } else {
-                v.u = (T)0.f;
+                v[k].load(reinterpret_cast<const T*>(g.state_in) + ((int64_t)n * before + s + before) * g.C + c);
             }
-            if (begins) e = t;
-            push(v, begins);
+        }
+#pragma unroll
+        for (int k = 0; k < CONV_W - 1; ++k) {
+            if (begins[k]) e = t0 - (CONV_W - 1) + k;
+            push(v[k], begins[k]);
         }
         return e;
     }
@@ -217,18 +234,18 @@ __global__ __launch_bounds__(256) void k_conv_bwd(ConvArgs g, int cols, int rows
                     store_run<T, V>(reinterpret_cast<T*>(g.dstate_in) + ((int64_t)n * before + s + before) * g.C + c, o);
             };
             const int end = t1 + before < g.T ? t1 + before : g.T;
-            for (int t4 = t0; t4 < end; t4 += CONV_U) {
-                Run<T, V> v[CONV_U], q[CONV_U];
-                uint32_t first[CONV_U];
+            for (int t4 = t0; t4 < end; t4 += CONV_U_BWD) {
+                Run<T, V> v[CONV_U_BWD], q[CONV_U_BWD];
+                uint32_t first[CONV_U_BWD];
 #pragma unroll
-                for (int u = 0; u < CONV_U; ++u) {
+                for (int u = 0; u < CONV_U_BWD; ++u) {
                     const int tt = t4 + u < end ? t4 + u : end - 1;
                     v[u].load(x + (int64_t)tt * g.x_t);
                     q[u].load(dy + (int64_t)tt * g.y_t);
                     first[u] = g.first ? g.first[(int64_t)tt * g.N + n] : 0;
                 }
 #pragma unroll
-                for (int u = 0; u < CONV_U; ++u) {
+                for (int u = 0; u < CONV_U_BWD; ++u) {
                     const int t = t4 + u;
                     if (t >= end) break;
                     if (first[u]) e = t;
@@ -584,11 +601,11 @@ struct State {
             const int rows = P - 32 * p < 32 ? P - 32 * p : 32, n = rows > 0 ? rows * S : 0;
             const float* from = m + (int64_t)32 * p * S;
             if (vec && S == 32 * SB && rows == 32) {
-                float4 f[4 * SB];
+                float4_t f[4 * SB];
 #pragma unroll
-                for (int i = 0; i < 4 * SB; ++i) f[i] = *reinterpret_cast<const float4*>(from + 256 * i + 4 * lane);
+                for (int i = 0; i < 4 * SB; ++i) f[i] = *reinterpret_cast<const float4_t*>(from + 256 * i + 4 * lane);
 #pragma unroll
-                for (int i = 0; i < 4 * SB; ++i) *reinterpret_cast<float4*>(patch + (256 * i + 4 * lane) / (32 * SB) * TP + 4 * lane % (32 * SB)) = f[i];
+                for (int i = 0; i < 4 * SB; ++i) *reinterpret_cast<float4_t*>(patch + (256 * i + 4 * lane) / (32 * SB) * TP + 4 * lane % (32 * SB)) = f[i];
             } else if (vec)
                 for (int i = 4 * lane; i < n; i += 256) *reinterpret_cast<float4*>(patch + i / S * TP + i % S) = *reinterpret_cast<const float4*>(from + i);
             else
@@ -1513,30 +1530,47 @@ struct StepArgs {
     void* conv_out;
     int width;
 };
-// A wave a head of an environment.  The convolution's outputs stay in fp32 in LDS; a row of the state (state values of one channel)
-// is shared by LPR lanes of four values each, or of single ones where rows are not whole 16-byte pieces.
+// A wave takes a head of an environment, or one of `parts` equal runs of its channels where there are few heads in all (each computes the
+// head's B and C for itself).  The convolution's outputs stay in fp32 in LDS; a row of the state (the state values of one channel) is shared
+// by lpr lanes of four values each, or of single ones where rows are not whole 16-byte pieces; STEP_U rows a lane are requested together.
+// Bound by the states, read and written once: 4096 environments x 8 heads of 64 x 64, 1.07 GB.
+#define STEP_U 4
 template <typename T>
-__global__ __launch_bounds__(256) void k_memory_step(StepArgs a, int lpr, int vec) {
+__global__ __launch_bounds__(256) void k_memory_step(StepArgs a, int lpr, int vec, int parts) {
     extern __shared__ float slds[];
     const ScanArgs& g = a.s;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int64_t id = (int64_t)blockIdx.x * 4 + wave;
-    if (id >= (int64_t)g.N * g.H) return;
+    const int wave = wave_index(), lane = threadIdx.x & 63;
+    const int64_t unit = (int64_t)blockIdx.x * 4 + wave;
+    if (unit >= (int64_t)g.N * g.H * parts) return;
+    const int64_t id = unit / parts;
+    const int each = (g.P + parts - 1) / parts, q0 = (int)(unit % parts) * each, q1 = q0 + each < g.P ? q0 + each : g.P;  // its channels
     const int n = (int)(id / g.H), h = (int)(id % g.H), rep = g.H / g.G, grp = h / rep, D = g.H * g.P;
-    const int chans = D + 2 * g.G * g.S, before = a.width - 1;
+    const int chans = D + 2 * g.G * g.S, before = a.width - 1, np = q1 > q0 ? q1 - q0 : 0;
     float* xs = slds + wave * (g.P + 2 * g.S);
     const bool begins = g.first && g.first[n];
     const T* row = reinterpret_cast<const T*>(a.xbc) + (int64_t)n * g.x_n;
-    for (int i = lane; i < g.P + 2 * g.S; i += 64) {
-        const int c = i < g.P ? h * g.P + i : i < g.P + g.S ? D + grp * g.S + i - g.P : D + g.G * g.S + grp * g.S + i - g.P - g.S;
+    const T* old = reinterpret_cast<const T*>(a.conv_in) + (int64_t)n * before * chans;
+    T* kept = reinterpret_cast<T*>(a.conv_out) + (int64_t)n * before * chans;
+    for (int i = lane; i < np + 2 * g.S; i += 64) {
+        const int c = i < np ? h * g.P + q0 + i : i < np + g.S ? D + grp * g.S + i - np : D + g.G * g.S + grp * g.S + i - np - g.S;
         float v = a.conv_b ? a.conv_b[c] : 0.f;
-        const bool mine = i < g.P || h == grp * rep;  // one head of a group keeps its B and C
-        for (int k = 0; k < a.width; ++k) {
-            T in = (T)0.f;
-            if (k == before) in = row[c];
-            else if (a.conv_in && !begins) in = reinterpret_cast<const T*>(a.conv_in)[((int64_t)n * before + k) * chans + c];
-            if (k == before || !begins) v += a.conv_w[(int64_t)c * a.width + k] * to_f(in);
-            if (k > 0 && mine && a.conv_out) reinterpret_cast<T*>(a.conv_out)[((int64_t)n * before + k - 1) * chans + c] = in;
+        const bool mine = i < np || (h == grp * rep && q0 == 0);  // one wave of a group keeps its B and C
+        T in[CONV_W];
+        float w[CONV_W];
+#pragma unroll
+        for (int k = 0; k < CONV_W; ++k) {
+            in[k] = (T)0.f;
+            w[k] = 0.f;
+            if (k < a.width) {
+                w[k] = a.conv_w[(int64_t)c * a.width + k];
+                if (k == before) in[k] = row[c];
+                else if (a.conv_in && !begins) in[k] = old[(int64_t)k * chans + c];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < CONV_W; ++k) {
+            if (k == before || (k < before && !begins)) v += w[k] * to_f(in[k]);
+            if (k > 0 && k < a.width && mine && a.conv_out) kept[(int64_t)(k - 1) * chans + c] = in[k];
         }
         xs[i] = silu_f(v);
     }
@@ -1544,34 +1578,61 @@ __global__ __launch_bounds__(256) void k_memory_step(StepArgs a, int lpr, int ve
     const float raw = to_f(reinterpret_cast<const T*>(g.dt)[(int64_t)n * g.dt_n + h]) + (g.dt_bias ? g.dt_bias[h] : 0.f);
     const float dt = raw > 20.f ? raw : log1pf(expf(raw));
     const float e = expf(-dt * expf(g.a_log[h])), dskip = g.d_skip ? g.d_skip[h] : 0.f;
-    const float* hi = g.state_in ? g.state_in + id * g.P * g.S : nullptr;
-    float* ho = g.state_out + id * g.P * g.S;
-    const float *bs = xs + g.P, *cs = bs + g.S;
-    const int sub = lane % lpr, per = vec ? 4 : 1;
-    for (int p0 = 0; p0 < g.P; p0 += 64 / lpr) {
-        const int p = p0 + lane / lpr;
-        float y = 0.f;
-        if (p < g.P) {
-            const float xv = dt * xs[p];
-            for (int s = sub * per; s < g.S; s += lpr * per) {
-                if (vec) {
-                    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (hi && !begins) v = *reinterpret_cast<const float4*>(hi + (int64_t)p * g.S + s);
-                    v.x = e * v.x + xv * bs[s]; v.y = e * v.y + xv * bs[s + 1]; v.z = e * v.z + xv * bs[s + 2]; v.w = e * v.w + xv * bs[s + 3];
-                    *reinterpret_cast<float4*>(ho + (int64_t)p * g.S + s) = v;
-                    y += v.x * cs[s] + v.y * cs[s + 1] + v.z * cs[s + 2] + v.w * cs[s + 3];
-                } else {
-                    const float v = (hi && !begins ? e * hi[(int64_t)p * g.S + s] : 0.f) + xv * bs[s];
-                    ho[(int64_t)p * g.S + s] = v;
-                    y += v * cs[s];
+    const bool have = g.state_in && !begins;
+    const float* hi = have ? g.state_in + (id * g.P + q0) * g.S : g.state_out;  // (never read where there is none)
+    float* ho = g.state_out + (id * g.P + q0) * g.S;
+    const float *bs = xs + np, *cs = bs + g.S;
+    const int sub = lane % lpr, rows = 64 / lpr;
+    const T* z = reinterpret_cast<const T*>(g.z) + (int64_t)n * g.z_n + (int64_t)h * g.P + q0;
+    T* yo = reinterpret_cast<T*>(g.y) + (int64_t)n * g.y_n + (int64_t)h * g.P + q0;
+    float4_t bv = {}, cv = {};
+    if (vec && 4 * sub < g.S) {
+        bv = *reinterpret_cast<const float4_t*>(bs + 4 * sub);
+        cv = *reinterpret_cast<const float4_t*>(cs + 4 * sub);
+    }
+    for (int p0 = 0; p0 < np; p0 += STEP_U * rows) {
+        float y[STEP_U];
+        if (vec) {
+            float4_t v[STEP_U];
+#pragma unroll
+            for (int u = 0; u < STEP_U; ++u) {
+                const int p = p0 + u * rows + lane / lpr;
+                v[u] = float4_t{};
+                if (have && p < np && 4 * sub < g.S) v[u] = *reinterpret_cast<const float4_t*>(hi + (int64_t)p * g.S + 4 * sub);
+            }
+#pragma unroll
+            for (int u = 0; u < STEP_U; ++u) {
+                const int p = p0 + u * rows + lane / lpr;
+                const float xv = dt * xs[p < np ? p : 0];
+                y[u] = 0.f;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    v[u][k] = e * v[u][k] + xv * bv[k];
+                    y[u] += v[u][k] * cv[k];
+                }
+                if (p < np && 4 * sub < g.S) *reinterpret_cast<float4_t*>(ho + (int64_t)p * g.S + 4 * sub) = v[u];
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < STEP_U; ++u) {
+                const int p = p0 + u * rows + lane / lpr;
+                y[u] = 0.f;
+                if (p < np && sub < g.S) {
+                    const float v = (have ? e * hi[(int64_t)p * g.S + sub] : 0.f) + dt * xs[p] * bs[sub];
+                    ho[(int64_t)p * g.S + sub] = v;
+                    y[u] = v * cs[sub];
                 }
             }
         }
-        for (int o = lpr / 2; o; o >>= 1) y += __shfl_xor(y, o);
-        if (p < g.P && sub == 0) {
-            y += dskip * xs[p];
-            if (g.z) y *= silu_f(to_f(reinterpret_cast<const T*>(g.z)[(int64_t)n * g.z_n + (int64_t)h * g.P + p]));
-            reinterpret_cast<T*>(g.y)[(int64_t)n * g.y_n + (int64_t)h * g.P + p] = cvt<T>(y);
+#pragma unroll
+        for (int u = 0; u < STEP_U; ++u) {
+            for (int o = lpr / 2; o; o >>= 1) y[u] += __shfl_xor(y[u], o);
+            const int p = p0 + u * rows + lane / lpr;
+            if (p < np && sub == 0) {
+                float v = y[u] + dskip * xs[p];
+                if (g.z) v *= silu_f(to_f(z[p]));
+                yo[p] = cvt<T>(v);
+            }
         }
     }
 }
@@ -1769,7 +1830,8 @@ void launch_memory_step(const morlax_scan_dims& d, int width, const void* xbc, c
     int lpr = 1;
     while (lpr < 64 && lpr * (vec ? 4 : 1) < g.S) lpr *= 2;
     const int lds = 4 * (g.P + 2 * g.S) * 4;
-    const int64_t blocks = cdiv((int64_t)g.N * g.H, 4);
-    if (d.dtype) k_memory_step<bf16_t><<<blocks, 256, lds, s>>>(a, lpr, vec);
-    else k_memory_step<float><<<blocks, 256, lds, s>>>(a, lpr, vec);
+    const int parts = (int64_t)g.N * g.H < 1024 && g.P >= 4 ? 4 : 1;  // a wave for every SIMD
+    const int64_t blocks = cdiv((int64_t)g.N * g.H * parts, 4);
+    if (d.dtype) k_memory_step<bf16_t><<<blocks, 256, lds, s>>>(a, lpr, vec, parts);
+    else k_memory_step<float><<<blocks, 256, lds, s>>>(a, lpr, vec, parts);
 }

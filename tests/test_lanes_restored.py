@@ -19,15 +19,20 @@ def places(listing):
 
     def look():
         at = {a: i for i, (a, _) in enumerate(code)}
-        reached = set()
+        reached, starts = set(), set()   # by a branch without lanes; by any branch
         for a, s in code:
-            m = re.match(r"s_cbranch_execz (\d+)", s)
+            m = re.match(r"s_c?branch\w* (\d+)", s)
             if m:
                 d = int(m.group(1))
-                reached.add(a + 4 + 4 * (d - 65536 if d >= 32768 else d))
+                to = a + 4 + 4 * (d - 65536 if d >= 32768 else d)
+                starts.add(to)
+                if s.startswith("s_cbranch_execz"):
+                    reached.add(to)
         for a in reached:
             hits = []
-            for _, s in code[at[a]:at[a] + 200] if a in at else []:
+            for b, s in code[at[a]:at[a] + 200] if a in at else []:
+                if b != a and b in starts:   # the next block: the lanes that run it have come from elsewhere too
+                    break
                 if re.match(r"s_or_b64 exec, exec,|s_mov_b64 exec|s_andn2_saveexec|s_or_saveexec", s):
                     if hits:
                         found.append((kernel, a, hits))
