@@ -30,7 +30,7 @@ struct AdArgs {
     int32_t *seg, *perm; // [P + 2], [M]
     float *pw, *pA, *pB, *pb;  // partial sums: [split][O][I], [piece][O][r], [piece][r][I], [piece][O]
     const int32_t* order;  // perm where rows are taken sorted by adapter (u and v are then in that order), or NULL: as they lie
-    int rp, split, kchunk, pieces;
+    int rp, split, kchunk, pieces, bf16;
     __device__ inline int row(int s) const { return order ? order[s] : s; }
     // adapter of the row at position s, or -1
     __device__ inline int adapter(int s) const {
@@ -747,6 +747,44 @@ __global__ __launch_bounds__(256) void k_ad_shrink_row(AdArgs g) {
     }
 }
 
+// acc += A^T x for the contraction indices [k0, k1) of a wave (k0 a multiple of 64), A [K][r] with r a multiple of 8: sixty-four rows of A at a
+// time through LDS, where they are turned, the next ones and the rows' values already on their way.  (One by one, with the factor's values
+// read from LDS singly: 41 us a launch for 32768 rows x 1160.)
+__device__ inline void shrink_turned(const bf16_t* f, const bf16_t* row, int K, int r, int k0, int k1, bf16_t* turn, float16_t& acc) {
+    const int lane = threadIdx.x & 63, lg = lane >> 5, a = lane & 15, q0 = (lane >> 4) & 1, e = a >> 2, c = a & 3, pieces = r / 8;
+    uint4 fq[4], xq[4];
+    auto fetch = [&](int k) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (q < pieces) fq[q] = ad_piece<true>(f, k * r + 8 * (lane + 64 * q), K * r, true);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) xq[s] = ad_piece<true>(row, k + 32 * lg + 8 * s, K, true);
+    };
+    if (k0 < k1) fetch(k0);
+    for (int k = k0; k < k1; k += 64) {
+        uint4 x[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (q < pieces) {
+                const int at = lane + 64 * q;
+                *reinterpret_cast<uint4*>(turn + at / pieces * 32 + at % pieces * 8) = fq[q];
+            }
+#pragma unroll
+        for (int s = 0; s < 4; ++s) x[s] = xq[s];
+        __builtin_amdgcn_wave_barrier();
+        if (k + 64 < k1) fetch(k + 64);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            typedef __attribute__((address_space(3))) short4_t lds_s4;
+            const bf16_t* p = turn + (32 * lg + 8 * s + e) * 32 + 16 * q0 + 4 * c;
+            const uint2 u0 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)p));
+            const uint2 u1 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(p + 4 * 32)));
+            Mma32<bf16_t>::run(make_uint4(u0.x, u0.y, u1.x, u1.y), x[s], acc);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
 // Many rows: 32 a workgroup, its four waves a quarter of the contraction each, one pass over the rows per adapter among them.  bf16 on
 // 32x32x16, fp32 on 32x32x2 (the factor's 32 rows are at most `rank` real ones; the pass is bound by its reads).  A lane takes 64 bytes of
 // its row at a time, so a line is read whole; the backward's factor, [O][r], is turned in LDS.
@@ -774,7 +812,12 @@ __global__ __launch_bounds__(256) void k_ad_shrink(AdArgs g) {
         todo &= ~mine;
         const T* f = fac + (int64_t)q * K * g.r;
         float16_t acc = zero16();
-        for (int k = k0; k < k1; k += KI) {
+        bool done = false;
+        if constexpr (BWD && sizeof(T) == 2) {
+            done = whole && (g.r & 7) == 0;
+            if (done) shrink_turned(f, row, K, g.r, k0, k1, &turn[wave][0][0], acc);
+        }
+        for (int k = k0; k < k1 && !done; k += KI) {
             if (BWD) {  // KI rows of the factor, r values each, one after the other in memory
                 const int n = (k1 - k < KI ? k1 - k : KI) * g.r;
                 const T* s = f + (int64_t)k * g.r;
@@ -1048,8 +1091,9 @@ static int64_t ad_carve(AdArgs& g, bool bwd, void* ws) {
         g.v = (float*)take((int64_t)g.M * g.rp * 4);
         g.seg = (int32_t*)take(((int64_t)g.P + 2) * 4);
         g.perm = (int32_t*)take((int64_t)g.M * 4);
-        const int64_t tiles = cdiv(g.O, 128) * cdiv(g.I, 128);
-        int64_t split = cdiv(512, tiles);  // two workgroups a CU
+        // dW0's contraction in ranges: bf16, one workgroup of the large tiles a CU (32768 x 512 x 1160, us: 12 ranges 65 and 13 for their sum, 25
+        // ranges 65 and 17, on small tiles 13 ranges 83 and 13); fp32, two of the small ones
+        int64_t split = g.bf16 ? 256 / (cdiv(g.O, 256) * cdiv(g.I, 128)) : cdiv(512, cdiv(g.O, 128) * cdiv(g.I, 128));
         const int64_t most = cdiv(g.M, 64);
         if (split > most) split = most;
         if (split < 1) split = 1;
@@ -1066,7 +1110,7 @@ static int64_t ad_carve(AdArgs& g, bool bwd, void* ws) {
 static AdArgs ad_args(const morlax_adapter_dims& d) {
     AdArgs g = {};
     g.M = d.rows; g.I = d.d_in; g.O = d.d_out; g.r = d.rank; g.P = d.n_adapters;
-    g.ld_x = d.ld_x; g.ld_y = d.ld_y;
+    g.ld_x = d.ld_x; g.ld_y = d.ld_y; g.bf16 = d.dtype;
     return g;
 }
 int64_t adapter_ws_bytes(const morlax_adapter_dims& d, bool bwd) {
@@ -1109,8 +1153,7 @@ static void shrink(const AdArgs& g, hipStream_t s) {
     }
 }
 // Which kernel multiplies with W0.  Few rows: 16 columns a workgroup where 128 x 128 tiles would leave most CUs without one.  Else tiles:
-// direct-to-LDS loads for bf16 rows of whole 16-byte pieces within 32-bit offsets (larger tiles where those still give every CU two
-// workgroups), the general kernel for the rest.
+// direct-to-LDS loads for bf16 rows of whole 16-byte pieces within 32-bit offsets, the general kernel for the rest.
 template <typename T, int ROLE>
 static void product(const AdArgs& g, hipStream_t s) {
     const int rows_a = ROLE == AD_DW ? g.O : g.M, rows_b = ROLE == AD_FWD ? g.O : g.I, K = ROLE == AD_FWD ? g.I : ROLE == AD_DX ? g.O : g.M;
@@ -1131,7 +1174,9 @@ static void product(const AdArgs& g, hipStream_t s) {
         const bool ok = ROLE == AD_FWD ? x_ok && w_ok && small_w : ROLE == AD_DX ? y_ok && w_ok && small_w && g.O % 8 == 0 : x_ok && y_ok && w_ok && g.O % 8 == 0;
         if (ok && K >= 32) {
             const int64_t big = cdiv(rows_a, 256) * cdiv(rows_b, 128);
-            if (big * split >= 512) {
+            // Large tiles do a product in 7/8 of the small ones' time and go two to a CU at a time, the small ones three; the CU with most tiles
+            // decides.  us: 16384 x 1160 x 512 (640 or 1280 tiles) 48 large, 40 small; dX of 32768 x 512 x 1160 (512 or 1024) 64 and 73
+            if (2 * 7 * cdiv(big * split, 256) <= 8 * cdiv(tiles * split, 256)) {
                 if (g.rp == 16) k_ad_gemm_dma<ROLE, 4, 16><<<dim3(big, split), 256, 0, s>>>(g);
                 else k_ad_gemm_dma<ROLE, 4, 32><<<dim3(big, split), 256, 0, s>>>(g);
             } else {
