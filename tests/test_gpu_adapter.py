@@ -103,7 +103,8 @@ def run_bwd(dims, d, only=None):
 # rows, d_in, d_out, rank, adapters, order, elements between rows
 SHAPES = [(1, 8, 8, 1, 1, "one", 0), (1, 64, 96, 16, 5, "mixed", 0), (3, 27, 50, 5, 6, "mixed", 1), (33, 64, 130, 8, 4, "grouped", 0),
           (64, 256, 320, 16, 64, "mixed", 8), (129, 40, 264, 32, 3, "mixed", 0), (257, 31, 33, 17, 300, "mixed", 3), (600, 136, 200, 31, 2, "one", 0),
-          (1030, 512, 72, 4, 16, "grouped", 0), (515, 72, 512, 16, 7, "none", 0), (2100, 264, 392, 9, 130, "mixed", 0)]
+          (1030, 512, 72, 4, 16, "grouped", 0), (515, 72, 512, 16, 7, "none", 0), (2100, 264, 392, 9, 130, "mixed", 0),
+          (4099, 27, 130, 5, 24, "mixed", 0), (16400, 264, 520, 16, 40, "grouped", 0), (16385, 200, 520, 12, 3, "mixed", 8), (9000, 520, 264, 24, 700, "mixed", 0)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
@@ -212,3 +213,25 @@ def test_other_stream():
         got = run_fwd(dims, d)
     s.synchronize()
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_rows_far_apart(dtype):
+    """Strides that take a tensor beyond 32-bit offsets."""
+    torch = _torch()
+    M, I, O, r, P, far = 2100, 72, 520, 4, 3, (1 << 20) + 8
+    near, d, ref = problem(M, I, O, r, P, dtype, seed=12)
+    want = definition(ref, P)
+    y = torch.empty(M, far, dtype=d["w0"].dtype, device="cuda")
+    x = torch.empty(M, far, dtype=d["w0"].dtype, device="cuda")
+    x[:, :I] = d["x"]
+    dims = binding.AdapterDims(M, I, O, r, P, dtype, far, far)
+    ws = torch.empty(binding.adapter_workspace_bytes(dims, True), dtype=torch.uint8, device="cuda")
+    binding.adapter_fwd(dims, x, d["w0"], d["bias"], d["A"], d["B"], d["index"], y, ws)
+    check(y[:, :O], want["y"], want["yabs"], max(I, r), dtype == BF16, "y")
+    y[:, :O] = d["dy"]
+    dw0, dA = torch.empty(O, I, device="cuda"), torch.empty(P, O, r, device="cuda")
+    dx = torch.empty(M, far, dtype=d["w0"].dtype, device="cuda")
+    binding.adapter_bwd(dims, x, d["w0"], d["A"], d["B"], d["index"], y, dx, dw0, None, dA, None, ws)
+    for got, k, terms in ((dx[:, :I], "dx", O), (dw0, "dw0", M), (dA, "dA", M)):
+        check(got, want[k], want[k + "abs"], terms, dtype == BF16 and k == "dx", k)

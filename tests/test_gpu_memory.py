@@ -401,3 +401,29 @@ def test_steps_follow_the_sequence():
         binding.memory_step(one, W, raw[t], d["dt"][t], d["z"][t], w, b, d["a_log"], d["d"], d["bias"], d["first"][t], conv[t % 2], state, ys[t],
                             conv[1 - t % 2], state)
     assert torch.allclose(ys, y, rtol=1e-4, atol=1e-4) and torch.allclose(state, out, rtol=1e-4, atol=1e-5)
+
+
+def test_time_steps_far_apart():
+    """Strides that take a segment beyond 32-bit offsets."""
+    torch = _torch()
+    T, N, H, P, G, S, far = 40, 2, 2, 32, 1, 16, (1 << 26) + 8
+    _, h, d = scan_problem(T, N, H, P, G, S, BF16, 0.1, True, seed=31)
+    D, C = H * P, H * P + 2 * G * S
+    y, last, _ = scan_truth(binding.ScanDims(T, N, H, P, G, S, BF16), h)
+    room = torch.empty(T * far, dtype=torch.bfloat16, device="cuda")
+    place = lambda n, at: room.as_strided((T, N, n), (far, n, 1), at)  # noqa: E731
+    tensors, at = {}, 0
+    for k, n in (("xbc", C), ("z", D), ("dt", H), ("y", D)):
+        tensors[k] = place(n, at)
+        at += N * n
+        if k != "y":
+            tensors[k].copy_(h[k])
+    dims = binding.ScanDims(T, N, H, P, G, S, BF16, far, C, far, D, far, H, far, D)
+    got, out, _ = run_scan(dims, dict(d, **tensors))
+    close(got, y, S + P + 32, True, "y")
+    close(out, last, S + P + 32, False, "state")
+    conv = binding.ConvDims(T, N, C, 4, 1, BF16, far, C, far, C)
+    w, other = torch.randn(C, 4), place(C, at)
+    want, _ = conv_definition(h["xbc"].double(), w.double(), None, h["first"], torch.zeros(N, 3, C).double(), 1)
+    binding.conv_fwd(conv, tensors["xbc"], w.cuda(), None, d["first"], None, other, None)
+    close(other, want, 8, True, "convolution")
