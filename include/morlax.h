@@ -263,8 +263,8 @@ int morlax_pareto_hypervolume(const float* J, const float* ref, int32_t n, int32
  * Entry points without a context: a struct of dimensions and strides, passed by pointer, takes its place.  What the conventions at
  * the top say of ownership, streams, workspaces and errors holds here too.  Tensors whose strides are arguments (x, y, z, dt and
  * their gradients) need the alignment of one element only; kernels use 16-byte accesses where pointers and strides allow them.  All
- * other pointers are 16-byte aligned.  dtype: 0 fp32, 1 bf16.  Sums and states are fp32.  A call with no rows (T, N or rows zero)
- * launches nothing that reads them: gradients of parameters are then zero.
+ * other pointers are 16-byte aligned.  dtype: 0 fp32, 1 bf16.  Sums and states are fp32.  An adapter call without rows
+ * reads none: gradients of parameters are then zero.
  *
  * A shared projection with a low-rank adapter per preference (Sec. III-B's W_l(p) = W0_l + A_l(p) B_l(p), with no W_l(p) formed):
  * row m of x goes through the adapter that index[m] names, rows in any order and any number to an adapter.  An index outside
@@ -273,7 +273,8 @@ int morlax_pareto_hypervolume(const float* J, const float* ref, int32_t n, int32
  *   x [rows, d_in] (row stride ld_x elements), w0 [d_out, d_in], bias [d_out] fp32 or NULL, A [n_adapters, d_out, rank],
  *   B [n_adapters, rank, d_in], index [rows] int32, y [rows, d_out] (row stride ld_y); x, w0, A, B, y of the given type.
  * B[p] x[m] is kept in fp32.  The result of a row depends on its own x and its own adapter alone.
- * Limits: 1 <= rank <= 32, 1 <= d_in, d_out <= 65536, 1 <= n_adapters <= 2^20. */
+ * Limits: 1 <= rank <= 32, 1 <= d_in, d_out <= 65536, 1 <= n_adapters <= 2^20, rows <= 2^28 and fewer than 2^24 tiles of 128 rows by
+ * 128 columns; backward, fewer than 255 * 2^24 elements in the factors' gradients. */
 typedef struct {
     int32_t rows, d_in, d_out, rank, n_adapters;
     int32_t dtype;
@@ -299,7 +300,8 @@ int morlax_adapter_bwd(const morlax_adapter_dims* dims, const void* x, const voi
  * Short causal convolution, one filter a channel: y[t, n, c] = act(b[c] + sum_k w[c, k] x[t - (width - 1) + k, n, c]) over the steps
  * of t's own episode.  x, y [T, N, channels] of the given type, step (t, n) at t * x_t + n * x_n (y_t, y_n) elements; w [channels, width],
  * b [channels] (or NULL) fp32; state_in, state_out [N, width - 1, channels] of the given type: the last inputs, oldest first.
- * y must not be x, state_out not state_in.  act: 0 none, 1 SiLU.  Limits: T, N, channels >= 1, 1 <= width <= 4. */
+ * y must not be x, state_out not state_in.  act: 0 none, 1 SiLU.  Limits: T, N >= 1, 1 <= channels <= 2^20,
+ * N * channels < 2^31, 1 <= width <= 4. */
 typedef struct {
     int32_t T, N, channels, width;
     int32_t act, dtype;
@@ -323,7 +325,8 @@ int morlax_conv_bwd(const morlax_conv_dims* dims, const void* x, const float* w,
  * NULL: 0) [heads] fp32; state_in, state_out [N, heads, head_dim, state] fp32, which may be the same buffer.  Sums and states are
  * fp32 whatever the type, y is rounded once.  An infinite or undefined input makes what depends on it infinite or undefined (not
  * always the one that step-by-step arithmetic would give).  saved: morlax_scan_saved_bytes() bytes that the backward needs, or NULL.
- * Limits: T, N, heads, groups, state, head_dim >= 1, groups | heads, head_dim <= 64, state <= 64. */
+ * Limits: T, N, heads, groups, state, head_dim >= 1, groups | heads, heads <= 65536, N * heads < 2^25,
+ * head_dim <= 64, state <= 64. */
 typedef struct {
     int32_t T, N, heads, head_dim, groups, state;
     int32_t dtype;

@@ -15,7 +15,6 @@
 typedef short short4_t __attribute__((ext_vector_type(4)));
 
 #define AD_PIECE 256    // sorted rows of a factor-gradient workgroup
-#define AD_MAX_RANK 32
 
 struct AdArgs {
     const void *x, *w0, *A, *B, *dy;
@@ -303,10 +302,6 @@ __device__ inline void ad_store(const AdArgs& g, const float16_t (&acc)[2], unsi
 static __device__ inline bool ad_vec(const void* p, int64_t ld, int size) {
     return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * size)) & 15) == 0;
 }
-// what a wave does with its 32 x 64 sums
-template <typename T, int ROLE, int RP>
-__device__ inline void ad_finish(const AdArgs& g, float16_t (&acc)[2], unsigned char* patch, int m0, int n0);
-
 // The three products with or of W0, on 128 x 128 tiles of four waves of 64 x 64: any size, stride and alignment.
 enum { AD_FWD = 0, AD_DX = 1, AD_DW = 2 };
 template <int ROLE> struct AdRole;
@@ -314,6 +309,7 @@ template <> struct AdRole<AD_FWD> { static constexpr int KA = KC, KB = KC; };
 template <> struct AdRole<AD_DX> { static constexpr int KA = KC, KB = KS; };
 template <> struct AdRole<AD_DW> { static constexpr int KA = KS, KB = KS; };
 
+// what a wave does with its 32 x 64 sums
 template <typename T, int ROLE, int RP>
 __device__ inline void ad_finish(const AdArgs& g, float16_t (&acc)[2], unsigned char* patch, int m0, int n0) {
     const int lg = (threadIdx.x >> 5) & 1;

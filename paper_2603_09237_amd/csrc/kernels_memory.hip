@@ -1641,7 +1641,8 @@ __global__ __launch_bounds__(256) void k_memory_step(StepArgs a, int lpr, int ve
 static void conv_runs(ConvArgs& g, int64_t threads) {
     // runs of time steps long enough that the steps before them, read again, do not count, where there are threads enough without
     int run = g.T;
-    while (run > 16 && threads * cdiv(g.T, run) < 256 * 1024) run = (run + 1) / 2;
+    // (and no more runs than a grid has along y)
+    while (run > 16 && threads * cdiv(g.T, run) < 256 * 1024 && g.T / 65535 < run / 4) run = (run + 1) / 2;
     g.run = run;
     g.runs = (int)cdiv(g.T, run);
 }

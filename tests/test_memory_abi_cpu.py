@@ -33,7 +33,8 @@ def adapter(**over):
 
 ADAPTER_BAD = [(dict(rows=-1), SHAPE), (dict(d_in=0), SHAPE), (dict(d_out=0), SHAPE), (dict(rank=0), SHAPE), (dict(adapters=0), SHAPE),
                (dict(dtype=2), UNSUPPORTED), (dict(rank=33), UNSUPPORTED), (dict(d_in=65537), UNSUPPORTED), (dict(adapters=(1 << 20) + 1), UNSUPPORTED),
-               (dict(ld_x=15), SHAPE), (dict(ld_y=23), SHAPE), (dict(rows=(1 << 31) - 1, d_out=65536), UNSUPPORTED)]
+               (dict(ld_x=15), SHAPE), (dict(ld_y=23), SHAPE), (dict(rows=1 << 24, d_out=65536), UNSUPPORTED),
+               (dict(rows=(1 << 28) + 1, d_out=1), UNSUPPORTED)]
 
 
 @pytest.mark.parametrize("over,code", ADAPTER_BAD)
@@ -77,6 +78,13 @@ def test_adapter_pointers_and_workspace():
     binding.adapter_fwd(adapter(rows=0), None, GOOD, None, GOOD, GOOD, None, None, (GOOD, 1 << 20), stream=0)
 
 
+def test_adapter_gradients_that_a_launch_cannot_hold():
+    d = adapter(adapters=1 << 20, rank=32, d_in=128, d_out=128)
+    assert binding.adapter_workspace_bytes(d) > 0
+    with pytest.raises(binding.MorlaxError):
+        binding.adapter_workspace_bytes(d, True)
+
+
 def conv(**over):
     d = dict(T=5, N=3, channels=16, width=4, act=1, dtype=1)
     d.update(over)
@@ -85,7 +93,8 @@ def conv(**over):
 
 @pytest.mark.parametrize("over,code", [(dict(T=0), SHAPE), (dict(N=0), SHAPE), (dict(channels=0), SHAPE), (dict(width=0), SHAPE),
                                        (dict(width=5), UNSUPPORTED), (dict(act=2), UNSUPPORTED), (dict(dtype=3), UNSUPPORTED), (dict(x_t=15), SHAPE),
-                                       (dict(y_n=8), SHAPE), (dict(channels=(1 << 20) + 1), UNSUPPORTED)])
+                                       (dict(y_n=8), SHAPE), (dict(channels=(1 << 20) + 1), UNSUPPORTED),
+                                       (dict(channels=1 << 20, N=1 << 11), UNSUPPORTED)])
 def test_convolution_dimensions(over, code):
     d = conv(**over)
     refused(code, lambda: binding.conv_fwd(d, GOOD, GOOD, GOOD, GOOD, GOOD, GOOD + 64, GOOD + 64, stream=0))
@@ -129,7 +138,7 @@ def scan(**over):
 
 SCAN_BAD = [(dict(T=0), SHAPE), (dict(N=0), SHAPE), (dict(heads=0, groups=1), SHAPE), (dict(head_dim=0), SHAPE), (dict(state=0), SHAPE), (dict(groups=3), SHAPE),
             (dict(dtype=2), UNSUPPORTED), (dict(head_dim=65), UNSUPPORTED), (dict(state=65), UNSUPPORTED), (dict(x_n=63), SHAPE), (dict(y_t=1), SHAPE),
-            (dict(dt_n=3), SHAPE)]
+            (dict(dt_n=3), SHAPE), (dict(heads=1 << 16, groups=1 << 16, head_dim=1, state=1, N=1 << 9), UNSUPPORTED)]
 
 
 @pytest.mark.parametrize("over,code", SCAN_BAD)
