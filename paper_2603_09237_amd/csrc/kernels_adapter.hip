@@ -649,7 +649,7 @@ __global__ __launch_bounds__(512) void k_ad_few(AdArgs g) {
     uint4 f[RP / VE];
 #pragma unroll
     for (int j = 0; j < RP / VE; ++j) f[j] = BWD ? ad_column(fp, N, j * VE, g.r) : ad_piece_of(g.r % VE == 0, fp, j * VE, g.r, true);
-    const float4* um = reinterpret_cast<const float4*>((BWD ? g.v : g.u) + (int64_t)(m < g.M ? m : g.M - 1) * RP);
+    const float4* um = reinterpret_cast<const float4*>((BWD ? g.v : g.u) + (int64_t)(m < g.M ? m : g.M - 1) * g.rp);
     float4 uv[RP / 4];
 #pragma unroll
     for (int j = 0; j < RP / 4; ++j) uv[j] = um[j];
@@ -694,21 +694,38 @@ __global__ __launch_bounds__(256) void k_ad_shrink_row(AdArgs g) {
     for (int j = 0; j < RP; ++j) acc[j] = 0.f;
     if (p >= 0) {
         const T* f = reinterpret_cast<const T*>(BWD ? g.A : g.B) + (int64_t)p * K * g.r;
-        if (BWD) {  // A_p [O][r]: a thread's rows of it
+        if (BWD) {  // A_p [O][r]: a thread's rows of it, two requested together
+            for (int k = tid; k < K; k += 2 * 64 * WPR) {
+                float v[2];
+                uint4 q[2][RP / VE];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int kk = k + 64 * WPR * u < K ? k + 64 * WPR * u : k;
+                    v[u] = to_f(row[kk]);
+#pragma unroll
+                    for (int j = 0; j < RP / VE; ++j) q[u][j] = ad_piece<WHOLE>(f + (int64_t)kk * g.r, j * VE, g.r, true);
+                }
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int j = 0; j < RP; ++j)
+                        acc[j] += j < g.r && k + 64 * WPR * u < K ? v[u] * to_f(reinterpret_cast<const T*>(&q[u][j / VE])[j % VE]) : 0.f;
+            }
+        } else if constexpr (!WHOLE) {  // B_p [r][I], rows that end inside a piece: a value a lane
             for (int k = tid; k < K; k += 64 * WPR) {
-                const float v = to_f(row[k]);
-                uint4 q[RP / VE];
+                T q[RP];
+                const T xv = row[k];
 #pragma unroll
-                for (int j = 0; j < RP / VE; ++j) q[j] = ad_piece<WHOLE>(f + (int64_t)k * g.r, j * VE, g.r, true);
+                for (int j = 0; j < RP; ++j) q[j] = f[(int64_t)(j < g.r ? j : 0) * K + k];
 #pragma unroll
-                for (int j = 0; j < RP; ++j) acc[j] += j < g.r ? v * to_f(reinterpret_cast<const T*>(&q[j / VE])[j % VE]) : 0.f;
+                for (int j = 0; j < RP; ++j) acc[j] += j < g.r ? to_f(xv) * to_f(q[j]) : 0.f;
             }
         } else {  // B_p [r][I]
             for (int k = tid * VE; k < K; k += 64 * WPR * VE) {
                 uint4 q[RP];
-                const uint4 xq = ad_piece<WHOLE>(row, k, K, true);
+                const uint4 xq = ad_piece<true>(row, k, K, true);
 #pragma unroll
-                for (int j = 0; j < RP; ++j) q[j] = ad_piece<WHOLE>(f + (int64_t)(j < g.r ? j : 0) * K, k, K, true);
+                for (int j = 0; j < RP; ++j) q[j] = ad_piece<true>(f + (int64_t)(j < g.r ? j : 0) * K, k, K, true);
 #pragma unroll
                 for (int j = 0; j < RP; ++j)
 #pragma unroll
@@ -729,8 +746,9 @@ __global__ __launch_bounds__(256) void k_ad_shrink_row(AdArgs g) {
     float s = acc[0];
 #pragma unroll
     for (int o = 64 / RP / 2; o >= 1; o /= 2) s += __shfl_xor(s, o);
-    float* out = (BWD ? g.v : g.u) + (int64_t)m * RP;
+    float* out = (BWD ? g.v : g.u) + (int64_t)m * g.rp;
     const int j = lane / (64 / RP);
+    if (RP == 8 && threadIdx.x % (64 * WPR) >= 8 && threadIdx.x % (64 * WPR) < 16) out[threadIdx.x % (64 * WPR)] = 0.f;  // (g.rp is 16)
     if (WPR == 1) {
         if (lane % (64 / RP) == 0) out[j] = j < g.r && p >= 0 ? s : 0.f;
         return;
@@ -1121,9 +1139,13 @@ static bool on16(const void* p, int64_t ld, int size) { return ((reinterpret_cas
 // run(padded rank, whole) with both as constants
 template <typename F>
 static void pick_rank(const AdArgs& g, bool whole, F run) {
+    typedef std::integral_constant<int, 8> R8;
     typedef std::integral_constant<int, 16> R16;
     typedef std::integral_constant<int, 32> R32;
-    if (g.rp == 16) {
+    if (g.r <= 8) {
+        if (whole) run(R8{}, std::true_type{});
+        else run(R8{}, std::false_type{});
+    } else if (g.rp == 16) {
         if (whole) run(R16{}, std::true_type{});
         else run(R16{}, std::false_type{});
     } else {
