@@ -761,39 +761,57 @@ __global__ __launch_bounds__(256) void k_ad_shrink_row(AdArgs g) {
     }
 }
 
-// acc += A^T x for the contraction indices [k0, k1) of a wave (k0 a multiple of 64), A [K][r] with r a multiple of 8: sixty-four rows of A at a
-// time through LDS, where they are turned, the next ones and the rows' values already on their way.  (One by one, with the factor's values
-// read from LDS singly: 41 us a launch for 32768 rows x 1160.)
-__device__ inline void shrink_turned(const bf16_t* f, const bf16_t* row, int K, int r, int k0, int k1, bf16_t* turn, float16_t& acc) {
-    const int lane = threadIdx.x & 63, lg = lane >> 5, a = lane & 15, q0 = (lane >> 4) & 1, e = a >> 2, c = a & 3, pieces = r / 8;
+// acc += F^T x for the contraction indices [k0, k1) of a wave (k0 a multiple of 64), 64 at a time, the next ones on their way.  A load takes
+// whole lines, eight lanes 128 bytes of a row (rows 8 i + lane / 8 for i = 0 .. 3), and the rows reach their lanes through LDS (`stage`, 32
+// rows x 64, piece c of a row at c ^ (row mod 8)).  Backward: A [K][r], r a multiple of 8, sixty-four rows of it turned in `turn`; forward:
+// B [r][K], a row a lane.
+template <bool BWD>
+__device__ inline void shrink_staged(const bf16_t* f, const bf16_t* const (&rows)[4], int K, int r, int k0, int k1, bf16_t* stage, bf16_t* turn,
+                                     float16_t& acc) {
+    const int lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5, a = lane & 15, q0 = (lane >> 4) & 1, e = a >> 2, c = a & 3, pieces = r / 8;
     uint4 fq[4], xq[4];
     auto fetch = [&](int k) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            if (q < pieces) fq[q] = ad_piece<true>(f, k * r + 8 * (lane + 64 * q), K * r, true);
+        for (int i = 0; i < 4; ++i) xq[i] = ad_piece<true>(rows[i], k + 8 * (lane & 7), K, true);
 #pragma unroll
-        for (int s = 0; s < 4; ++s) xq[s] = ad_piece<true>(row, k + 32 * lg + 8 * s, K, true);
+        for (int q = 0; q < 4; ++q) {
+            if constexpr (BWD) {
+                if (q < pieces) fq[q] = ad_piece<true>(f, k * r + 8 * (lane + 64 * q), K * r, true);
+            } else {
+                fq[q] = ad_piece<true>(f + (int64_t)(lr < r ? lr : 0) * K, k + 32 * lg + 8 * q, K, lr < r);
+            }
+        }
     };
     if (k0 < k1) fetch(k0);
     for (int k = k0; k < k1; k += 64) {
-        uint4 x[4];
+        uint4 fs[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            if (q < pieces) {
-                const int at = lane + 64 * q;
-                *reinterpret_cast<uint4*>(turn + at / pieces * 32 + at % pieces * 8) = fq[q];
+        for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<uint4*>(stage + (8 * i + lane / 8) * 64 + ((lane ^ lane / 8) & 7) * 8) = xq[i];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if constexpr (BWD) {
+                if (q < pieces) {
+                    const int at = lane + 64 * q;
+                    *reinterpret_cast<uint4*>(turn + at / pieces * 32 + at % pieces * 8) = fq[q];
+                }
+            } else {
+                fs[q] = fq[q];
             }
-#pragma unroll
-        for (int s = 0; s < 4; ++s) x[s] = xq[s];
+        }
         __builtin_amdgcn_wave_barrier();
         if (k + 64 < k1) fetch(k + 64);
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-            typedef __attribute__((address_space(3))) short4_t lds_s4;
-            const bf16_t* p = turn + (32 * lg + 8 * s + e) * 32 + 16 * q0 + 4 * c;
-            const uint2 u0 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)p));
-            const uint2 u1 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(p + 4 * 32)));
-            Mma32<bf16_t>::run(make_uint4(u0.x, u0.y, u1.x, u1.y), x[s], acc);
+            if constexpr (BWD) {
+                typedef __attribute__((address_space(3))) short4_t lds_s4;
+                const bf16_t* p = turn + (32 * lg + 8 * s + e) * 32 + 16 * q0 + 4 * c;
+                const uint2 u0 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)p));
+                const uint2 u1 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(p + 4 * 32)));
+                fs[s] = make_uint4(u0.x, u0.y, u1.x, u1.y);
+            }
+            const uint4 x = *reinterpret_cast<const uint4*>(stage + lr * 64 + (((4 * lg + s) ^ lr) & 7) * 8);
+            Mma32<bf16_t>::run(fs[s], x, acc);
         }
         __builtin_amdgcn_wave_barrier();
     }
@@ -805,14 +823,22 @@ __device__ inline void shrink_turned(const bf16_t* f, const bf16_t* row, int K, 
 template <typename T, bool BWD>
 __global__ __launch_bounds__(256) void k_ad_shrink(AdArgs g) {
     constexpr int VE = 16 / (int)sizeof(T), KI = 8 * VE;  // contraction indices of an iteration: four pieces of either lane group
-    __shared__ float part[4][32][33];
-    __shared__ __align__(16) T turn[BWD ? 4 : 1][BWD ? KI : 1][BWD ? 32 : 1];
+    // a wave's: the rows' pieces on their way (bf16), the factor turned (backward), then its sums
+    __shared__ __align__(16) unsigned char lds[4][BWD ? 8192 : 32 * 33 * 4];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5;
     const int m0 = blockIdx.x * 32, m = m0 + lr;
     const int K = BWD ? g.O : g.I;
     const int64_t ld = BWD ? g.ld_y : g.ld_x;
     const T* base = reinterpret_cast<const T*>(BWD ? g.dy : g.x);
     const T* row = base + (int64_t)g.row(m < g.M ? m : g.M - 1) * ld;
+    const T* rows[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int l = m0 + 8 * i + lane / 8;
+        rows[i] = base + (int64_t)g.row(l < g.M ? l : g.M - 1) * ld;
+    }
+    float(*part)[33] = reinterpret_cast<float(*)[33]>(lds[wave]);
+    T(*turn)[32] = reinterpret_cast<T(*)[32]>(lds[wave]);
     const T* fac = reinterpret_cast<const T*>(BWD ? g.A : g.B);
     float* out = BWD ? g.v : g.u;
     const int p = g.adapter(m);
@@ -827,9 +853,9 @@ __global__ __launch_bounds__(256) void k_ad_shrink(AdArgs g) {
         const T* f = fac + (int64_t)q * K * g.r;
         float16_t acc = zero16();
         bool done = false;
-        if constexpr (BWD && sizeof(T) == 2) {
-            done = whole && (g.r & 7) == 0;
-            if (done) shrink_turned(f, row, K, g.r, k0, k1, &turn[wave][0][0], acc);
+        if constexpr (sizeof(T) == 2) {
+            done = whole && (!BWD || (g.r & 7) == 0);
+            if (done) shrink_staged<BWD>(f, rows, K, g.r, k0, k1, reinterpret_cast<T*>(lds[wave] + (BWD ? 4096 : 0)), &turn[0][0], acc);
         }
         for (int k = k0; k < k1 && !done; k += KI) {
             if (BWD) {  // KI rows of the factor, r values each, one after the other in memory
@@ -838,9 +864,9 @@ __global__ __launch_bounds__(256) void k_ad_shrink(AdArgs g) {
                 const int rr = g.r;
                 if ((rr * (int)sizeof(T)) % 16 == 0) {
                     for (int i = lane * VE; i < n; i += 64 * VE)
-                        *reinterpret_cast<uint4*>(&turn[wave][i / rr][i % rr]) = *reinterpret_cast<const uint4*>(s + i);
+                        *reinterpret_cast<uint4*>(&turn[i / rr][i % rr]) = *reinterpret_cast<const uint4*>(s + i);
                 } else {
-                    for (int i = lane; i < n; i += 64) turn[wave][i / rr][i % rr] = s[i];
+                    for (int i = lane; i < n; i += 64) turn[i / rr][i % rr] = s[i];
                 }
                 __builtin_amdgcn_wave_barrier();
             }
@@ -854,7 +880,7 @@ __global__ __launch_bounds__(256) void k_ad_shrink(AdArgs g) {
                 } else {
                     T e[VE];
 #pragma unroll
-                    for (int i = 0; i < VE; ++i) e[i] = kk + i < K && lr < g.r ? turn[wave][kk - k + i][lr] : (T)0.f;
+                    for (int i = 0; i < VE; ++i) e[i] = kk + i < K && lr < g.r ? turn[kk - k + i][lr] : (T)0.f;
                     fq[s] = *reinterpret_cast<uint4*>(e);
                 }
             }
@@ -869,13 +895,20 @@ __global__ __launch_bounds__(256) void k_ad_shrink(AdArgs g) {
             }
             if (BWD) __builtin_amdgcn_wave_barrier();
         }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-        for (int e = 0; e < 16; ++e) part[wave][8 * (e / 4) + 4 * lg + e % 4][lr] = acc[e];
+        for (int e = 0; e < 16; ++e) part[8 * (e / 4) + 4 * lg + e % 4][lr] = acc[e];
         __syncthreads();
+        auto sum = [&](int j, int ml) {
+            float s = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) s += reinterpret_cast<const float(*)[33]>(lds[w])[j][ml];
+            return s;
+        };
         for (int i = threadIdx.x; i < 32 * g.rp; i += 256) {
             const int ml = i / g.rp, j = i % g.rp;
             if (mine >> ml & 1)
-                out[(int64_t)(m0 + ml) * g.rp + j] = j < g.r ? part[0][j][ml] + part[1][j][ml] + part[2][j][ml] + part[3][j][ml] : 0.f;
+                out[(int64_t)(m0 + ml) * g.rp + j] = j < g.r ? sum(j, ml) : 0.f;
         }
         __syncthreads();
     }
