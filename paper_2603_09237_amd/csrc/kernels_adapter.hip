@@ -999,33 +999,48 @@ __global__ __launch_bounds__(256) void k_ad_factor_grad(AdArgs g, int col_blocks
     float16_t acc[JB];
 #pragma unroll
     for (int j = 0; j < JB; ++j) acc[j] = zero16();
+    // 32 rows x 128 columns of src and their weights: eight threads a row, sixteen columns and 4 JB weights each.  Requested a step ahead, the
+    // rows' places two
+    const int row = tid / 8, cc = c0 + 16 * (tid % 8);
+    uint4 reg[sizeof(T)];
+    float wt[JB][4];
+    auto place = [&](int s) { return s + row < s1 ? g.perm[s + row] : -1; };
+    auto fetch = [&](int s, int m) {
+        load16(base + (int64_t)(m < 0 ? 0 : m) * ld + cc, m < 0 ? 0 : C - cc, vec, reg);
+#pragma unroll
+        for (int jj = 0; jj < JB; ++jj) {
+            const int j = 32 * jj + 4 * (tid % 8);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                wt[jj][i] = m < 0 ? 0.f : j + i < g.r ? (p < g.P ? w[(int64_t)(s + row) * g.rp + j + i] : 0.f) : j + i == g.r ? 1.f : 0.f;
+        }
+    };
+    int next = place(s0);
+    fetch(s0, next);
+    next = place(s0 + 32);
     for (int s = s0; s < s1; s += 32) {
-        {   // 32 rows x 128 columns of src: eight threads a row, sixteen columns each
-            const int row = tid / 8, cc = c0 + 16 * (tid % 8);
-            const int m = s + row < s1 ? g.perm[s + row] : -1;
-            uint4 reg[sizeof(T)], l[NP], h[NP];
-            load16(base + (int64_t)(m < 0 ? 0 : m) * ld + cc, m < 0 ? 0 : C - cc, vec, reg);
+        {
+            uint4 l[NP], h[NP];
             parts16<true>(reg, l, h);
 #pragma unroll
             for (int q = 0; q < NP; ++q) {
                 *reinterpret_cast<uint4*>(src + q * SP + row * 320 + (tid % 8) * 32) = l[q];
                 *reinterpret_cast<uint4*>(src + q * SP + row * 320 + (tid % 8) * 32 + 16) = h[q];
             }
-            // JB * 32 weights of a row: eight threads, 4 JB each
 #pragma unroll
             for (int jj = 0; jj < JB; ++jj) {
                 const int j = 32 * jj + 4 * (tid % 8);
-                float t[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    t[i] = m < 0 ? 0.f : j + i < g.r ? (p < g.P ? w[(int64_t)(s + row) * g.rp + j + i] : 0.f) : j + i == g.r ? 1.f : 0.f;
                 uint2 parts[3];
-                split3<true>(make_uint4(__float_as_uint(t[0]), __float_as_uint(t[1]), __float_as_uint(t[2]), __float_as_uint(t[3])), parts);
+                split3<true>(make_uint4(__float_as_uint(wt[jj][0]), __float_as_uint(wt[jj][1]), __float_as_uint(wt[jj][2]), __float_as_uint(wt[jj][3])), parts);
 #pragma unroll
                 for (int q = 0; q < 3; ++q) *reinterpret_cast<uint2*>(wts + q * 32 * WP + row * WP + j * 2) = parts[q];
             }
         }
         __syncthreads();
+        if (s + 32 < s1) {
+            fetch(s + 32, next);
+            next = place(s + 64);
+        }
         typedef __attribute__((address_space(3))) short4_t lds_s4;
         const int a = lane & 15, q0 = (lane >> 4) & 1, e = a >> 2, cw = a & 3;
 #pragma unroll
