@@ -157,10 +157,17 @@ struct AdFactor {
     __device__ inline const T* at(int p, int n, int j) const {
         return base + (int64_t)p * N * r + (BWD ? (int64_t)j * N + n : (int64_t)n * r + j);
     }
-    __device__ inline T get(int p, int n, int j) const { return n < N && j < r ? *at(p, n, j) : (T)0.f; }
-    // eight j of column n
+    // zero for j >= r; columns beyond the last one repeat it.  No branch goes by the lane: the loads of a block leave together
+    __device__ inline T get(int p, int n, int j) const {
+        const T v = *at(p, n < N ? n : N - 1, j < r ? j : 0);
+        return j < r ? v : (T)0.f;
+    }
+    // eight j of column n (vec: r is a multiple of 8)
     __device__ inline uint4 frag(int p, int n, int j0, bool vec) const {
-        if (!BWD && vec && n < N && j0 + 8 <= r) return *reinterpret_cast<const uint4*>(at(p, n, j0));
+        if (!BWD && vec) {
+            const uint4 u = *reinterpret_cast<const uint4*>(at(p, n < N ? n : N - 1, j0 < r ? j0 : 0));
+            return j0 < r ? u : make_uint4(0, 0, 0, 0);
+        }
         T e[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) e[i] = get(p, n, j0 + i);
@@ -198,9 +205,8 @@ struct AdExpand {
             }
         }
     }
-    __device__ inline void run(const AdArgs& g, const float* u, int m0, int n0, float16_t (&acc)[2]) {
+    __device__ inline void run(const AdArgs& g, const float* u, int p, int m0, int n0, float16_t (&acc)[2]) {  // p: the lane's row's adapter
         const int lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5, m = m0 + lr;
-        const int p = g.adapter(m);
         uint64_t todo = __ballot(p >= 0) & 0xffffffffull;
         if (!todo) return;
         vec = (F.r & 7) == 0;
@@ -311,28 +317,30 @@ template <> struct AdRole<AD_DW> { static constexpr int KA = KS, KB = KS; };
 
 // what a wave does with its 32 x 64 sums
 template <typename T, int ROLE, int RP>
-__device__ inline void ad_finish(const AdArgs& g, float16_t (&acc)[2], unsigned char* patch, int m0, int n0) {
+__device__ inline void ad_finish(const AdArgs& g, float16_t (&acc)[2], unsigned char* patch, int p, int range, int m0, int n0) {
     const int lg = (threadIdx.x >> 5) & 1;
     if constexpr (ROLE == AD_FWD) {
-        if (g.bias)
+        if (g.bias) {
+            asm volatile("" : "+v"(n0));  // (its values are read again for the next rows: held, they would cost the product its registers)
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const int n = n0 + 32 * j + 8 * (e / 4) + 4 * lg + e % 4;
-                    acc[j][e] += n < g.O ? g.bias[n] : 0.f;
+                    acc[j][e] += g.bias[n < g.O ? n : g.O - 1];
                 }
+        }
         AdExpand<T, false, RP> x;
         x.F = {reinterpret_cast<const T*>(g.A), g.O, g.r};
-        x.run(g, g.u, m0, n0, acc);
+        x.run(g, g.u, p, m0, n0, acc);
         ad_store<T, false>(g, acc, patch, reinterpret_cast<T*>(g.y), g.ld_y, g.M, g.O, m0, n0, ad_vec(g.y, g.ld_y, sizeof(T)));
     } else if constexpr (ROLE == AD_DX) {
         AdExpand<T, true, RP> x;
         x.F = {reinterpret_cast<const T*>(g.B), g.I, g.r};
-        x.run(g, g.v, m0, n0, acc);
+        x.run(g, g.v, p, m0, n0, acc);
         ad_store<T, true>(g, acc, patch, reinterpret_cast<T*>(g.dx), g.ld_x, g.M, g.I, m0, n0, ad_vec(g.dx, g.ld_x, sizeof(T)));
     } else {
-        float* C = g.split > 1 ? g.pw + (int64_t)blockIdx.y * g.O * g.I : g.dw0;
+        float* C = g.split > 1 ? g.pw + (int64_t)range * g.O * g.I : g.dw0;
         ad_store<float, false>(g, acc, patch, C, g.I, g.O, g.I, m0, n0, (g.I & 3) == 0);
     }
 }
@@ -422,7 +430,7 @@ __global__ __launch_bounds__(256, 2) void k_ad_gemm(AdArgs g) {
     }
     unsigned char* patch = lds + wave * AD_PATCH;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) ad_finish<T, ROLE, RP>(g, acc[i], patch, tm + wm + 32 * i, tn + wn);
+    for (int i = 0; i < 2; ++i) ad_finish<T, ROLE, RP>(g, acc[i], patch, ROLE == AD_DW ? 0 : g.adapter(tm + wm + 32 * i + lr), blockIdx.y, tm + wm + 32 * i, tn + wn);
 }
 
 // ---- bf16 operands whose rows are whole 16-byte pieces: direct-to-LDS loads, three stages of 32 contraction indices -------------------
@@ -455,10 +463,9 @@ struct AdTile {
         }
         kstep = KIND == KC ? 64 : 64 * ld;
     }
-    __device__ inline void issue(int64_t from, uint32_t tile) const {  // from: bytes along the contraction
+    __device__ inline void issue(int i, int64_t from, uint32_t tile) const {  // from: bytes along the contraction
         const int wave = threadIdx.x >> 6;
-#pragma unroll
-        for (int i = 0; i < NI; ++i) dma16(base + from, voff[i], __builtin_amdgcn_readfirstlane(tile + (uint32_t)(NI * wave + i) * 1024u));
+        dma16(base + from, voff[i], __builtin_amdgcn_readfirstlane(tile + (uint32_t)(NI * wave + i) * 1024u));
     }
     // the first `rest` (a multiple of 8 for KC) contraction indices, zeros behind them
     __device__ inline void put_rest(int rest, unsigned char* tile) const {
@@ -487,22 +494,24 @@ struct AdTile {
         }
     }
 };
-template <int MB> struct AdDma {
-    static constexpr int STAGE = (64 * MB + 128) * 64, LDS = 3 * STAGE > 4 * AD_PATCH ? 3 * STAGE : 4 * AD_PATCH, LOADS = MB + 2;
+template <int MB, int NB> struct AdDma {
+    static constexpr int STAGE = 64 * (MB + NB) * 64, LDS = 3 * STAGE > 4 * AD_PATCH ? 3 * STAGE : 4 * AD_PATCH, LOADS = MB + NB;
 };
 
-template <int ROLE, int MB, int RP>
-__global__ __launch_bounds__(256, MB == 2 ? 3 : 2) void k_ad_gemm_dma(AdArgs g) {
-    constexpr int KA = AdRole<ROLE>::KA, KB = AdRole<ROLE>::KB, TM = 64 * MB;
+template <int ROLE, int MB, int NB, int RP>
+__global__ __launch_bounds__(256, NB == 4 ? 1 : MB == 2 ? 3 : 2) void k_ad_gemm_dma(AdArgs g) {
+    constexpr int KA = AdRole<ROLE>::KA, KB = AdRole<ROLE>::KB, TM = 64 * MB, TN = 64 * NB;
     typedef AdTile<KA, TM> TA;
-    typedef AdTile<KB, 128> TB;
-    typedef AdDma<MB> S;
+    typedef AdTile<KB, TN> TB;
+    typedef AdDma<MB, NB> S;
     __shared__ __align__(16) unsigned char lds[S::LDS];
     const int wave = threadIdx.x >> 6;
-    const int wm = (wave >> 1) * 32 * MB, wn = (wave & 1) * 64;
+    const int wm = (wave >> 1) * 32 * MB, wn = (wave & 1) * 32 * NB;
     const int rows_a = ROLE == AD_DW ? g.O : g.M, rows_b = ROLE == AD_FWD ? g.O : g.I;
-    const int tiles_n = (rows_b + 127) / 128, tile = xcd_remap(blockIdx.x, gridDim.x);
-    const int tm = (tile / tiles_n) * TM, tn = (tile % tiles_n) * 128;
+    // consecutive workgroups of an XCD: the tiles of one range of the contraction, or of the same rows
+    const int tiles_n = (rows_b + TN - 1) / TN, id = xcd_remap(blockIdx.x, gridDim.x);
+    const int tiles = ROLE == AD_DW ? ((rows_a + TM - 1) / TM) * tiles_n : gridDim.x, tile = id % tiles, range = id / tiles;
+    const int tm = (tile / tiles_n) * TM, tn = (tile % tiles_n) * TN;
     TA a;
     TB b;
     int kdim;
@@ -515,54 +524,90 @@ __global__ __launch_bounds__(256, MB == 2 ? 3 : 2) void k_ad_gemm_dma(AdArgs g) 
         a.init(g.dy, g.ld_y, rows_a, tm, g.order);
         b.init(g.w0, g.I, rows_b, tn, nullptr);
     } else {
-        const int k0 = blockIdx.y * g.kchunk;
+        const int k0 = range * g.kchunk;
         kdim = g.M - k0 < g.kchunk ? g.M - k0 : g.kchunk;
         a.init(reinterpret_cast<const bf16_t*>(g.dy) + (int64_t)k0 * g.ld_y, g.ld_y, rows_a, tm, nullptr);
         b.init(reinterpret_cast<const bf16_t*>(g.x) + (int64_t)k0 * g.ld_x, g.ld_x, rows_b, tn, nullptr);
     }
+    int owner[MB];  // the adapters of the wave's rows
+#pragma unroll
+    for (int i = 0; i < MB; ++i) owner[i] = ROLE == AD_DW ? 0 : g.adapter(tm + wm + 32 * i + (threadIdx.x & 31));
     const uint32_t lbase = (uint32_t)(size_t)lds;
     const int rest = kdim & 31, steps = (kdim + 31) / 32, shift = rest ? 1 : 0;
     const int64_t skip_a = KA == KC ? 2 * rest : a.kstep / 32 * rest, skip_b = KB == KC ? 2 * rest : b.kstep / 32 * rest;
-    auto issue = [&](int s) {
+    auto issue_one = [&](int from, int s, int i) {
         const uint32_t to = lbase + (uint32_t)(s % 3) * S::STAGE;
-        a.issue(skip_a + (int64_t)(s - shift) * a.kstep, to);
-        b.issue(skip_b + (int64_t)(s - shift) * b.kstep, to + TA::BYTES);
+        const int64_t d = from - shift;
+        if (i < MB) a.issue(i, skip_a + d * a.kstep, to);
+        else b.issue(i - MB, skip_b + d * b.kstep, to + TA::BYTES);
+    };
+    auto issue = [&](int from, int s) {
+#pragma unroll
+        for (int i = 0; i < MB + NB; ++i) issue_one(from, s, i);
     };
     if (rest) {
         a.put_rest(rest, lds);
         b.put_rest(rest, lds + TA::BYTES);
     } else {
-        issue(0);
+        issue(0, 0);
     }
-    if (steps > 1) issue(1);
-    float16_t acc[MB][2];
+    // Behind the last stage it is requested again: the loop has no branch, and as many loads are on their way at every wait.  (A range of fewer
+    // than 32 indices has its rest alone.)
+    const bool full = ROLE != AD_DW || kdim >= 32;
+    if (full)
+        for (int s = 1; s < 3; ++s) issue(s < steps ? s : steps - 1, s);
+    float16_t acc[MB][NB];
 #pragma unroll
-    for (int i = 0; i < MB; ++i) acc[i][0] = acc[i][1] = zero16();
-    for (int s = 0; s < steps; ++s) {
-        if (s + 1 < steps) wait_vm<S::LOADS>();
-        else wait_vm<0>();
-        __syncthreads();  // stage s is complete, and stage s - 1 free
-        if (s + 2 < steps) issue(s + 2);
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) acc[i][j] = zero16();
+    uint4 fa[2][MB], fb[2][NB];
+    auto load_one = [&](int s, int ks, int f) {
         const unsigned char *ta = lds + (s % 3) * S::STAGE, *tb = ta + TA::BYTES;
-        uint4 fa[2][MB], fb[2][2];
+        if (f < NB) fb[ks][f] = TB::frag(tb, wn + 32 * f, ks);
+        else fa[ks][f - NB] = TA::frag(ta, wm + 32 * (f - NB), ks);
+    };
+    // the products of half a stage, `PIECES` pieces of other work between them, two or more behind each
+    auto products = [&](int ks, auto pieces, auto piece) {
+        constexpr int Q = MB * NB, PIECES = decltype(pieces)::value, EACH = (PIECES + Q - 1) / Q < 2 ? 2 : (PIECES + Q - 1) / Q;
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
+        for (int q = 0; q < Q; ++q) {
+            Mma32<bf16_t>::run(fb[ks][q % NB], fa[ks][q / NB], acc[q / NB][q % NB]);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) fb[ks][j] = TB::frag(tb, wn + 32 * j, ks);
-#pragma unroll
-            for (int i = 0; i < MB; ++i) fa[ks][i] = TA::frag(ta, wm + 32 * i, ks);
+            for (int e = 0; e < EACH; ++e)
+                if (q * EACH + e < PIECES) piece(q * EACH + e);
+            __builtin_amdgcn_sched_barrier(0);
         }
+    };
+    constexpr int F = MB + NB;
+    wait_vm<2 * S::LOADS>();
+    __syncthreads();
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks)
+    for (int f = 0; f < F; ++f) load_one(0, 0, f);
+    if (!full) {
 #pragma unroll
-            for (int i = 0; i < MB; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) Mma32<bf16_t>::run(fb[ks][j], fa[ks][i], acc[i][j]);
+        for (int f = 0; f < F; ++f) load_one(0, 1, f);
+        products(0, std::integral_constant<int, 0>{}, [](int) {});
+        products(1, std::integral_constant<int, 0>{}, [](int) {});
     }
+    for (int s = 0; full && s < steps; ++s) {
+        products(0, std::integral_constant<int, F>{}, [&](int f) { load_one(s, 1, f); });
+        wait_vm<S::LOADS>();
+        __syncthreads();  // stage s is in registers, stage s + 1 complete
+        const int from = s + 3 < steps ? s + 3 : steps - 1;
+        products(1, std::integral_constant<int, 2 * F>{}, [&](int f) {
+            if (f < F) load_one(s + 1, 0, f);
+            else issue_one(from, s + 3, f - F);
+        });
+    }
+    wait_vm<0>();
     __syncthreads();
     unsigned char* patch = lds + wave * AD_PATCH;
 #pragma unroll
-    for (int i = 0; i < MB; ++i) ad_finish<bf16_t, ROLE, RP>(g, acc[i], patch, tm + wm + 32 * i, tn + wn);
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; j += 2) ad_finish<bf16_t, ROLE, RP>(g, *reinterpret_cast<float16_t(*)[2]>(&acc[i][j]), patch, owner[i], range, tm + wm + 32 * i, tn + wn + 32 * j);
 }
 
 // ---- few rows: every workgroup sixteen columns of the output for 32 rows, its eight waves sharing the contraction --------------------
@@ -1243,11 +1288,11 @@ static void product(const AdArgs& g, hipStream_t s) {
             // Large tiles do a product in 7/8 of the small ones' time and go two to a CU at a time, the small ones three; the CU with most tiles
             // decides.  us: 16384 x 1160 x 512 (640 or 1280 tiles) 48 large, 40 small; dX of 32768 x 512 x 1160 (512 or 1024) 64 and 73
             if (2 * 7 * cdiv(big * split, 256) <= 8 * cdiv(tiles * split, 256)) {
-                if (g.rp == 16) k_ad_gemm_dma<ROLE, 4, 16><<<dim3(big, split), 256, 0, s>>>(g);
-                else k_ad_gemm_dma<ROLE, 4, 32><<<dim3(big, split), 256, 0, s>>>(g);
+                if (g.rp == 16) k_ad_gemm_dma<ROLE, 4, 2, 16><<<big * split, 256, 0, s>>>(g);
+                else k_ad_gemm_dma<ROLE, 4, 2, 32><<<big * split, 256, 0, s>>>(g);
             } else {
-                if (g.rp == 16) k_ad_gemm_dma<ROLE, 2, 16><<<dim3(tiles, split), 256, 0, s>>>(g);
-                else k_ad_gemm_dma<ROLE, 2, 32><<<dim3(tiles, split), 256, 0, s>>>(g);
+                if (g.rp == 16) k_ad_gemm_dma<ROLE, 2, 2, 16><<<tiles * split, 256, 0, s>>>(g);
+                else k_ad_gemm_dma<ROLE, 2, 2, 32><<<tiles * split, 256, 0, s>>>(g);
             }
             return;
         }
