@@ -965,18 +965,41 @@ __global__ __launch_bounds__(256) void k_ad_shrink(AdArgs g) {
 }
 
 // Rows sorted by adapter, order kept among a preference's own: workgroup q walks the index twice, to count the rows that come
-// before its own, and to place them, a wave a contiguous sixteenth of the rows.  q = P: the rows without one.
+// before its own, and to place them, a wave a contiguous sixteenth of the rows (and the last one those behind the last whole four).  q = P:
+// the rows without one.  Bound by latency: a lane takes four rows at a time and has four such pieces on their way.
 __global__ __launch_bounds__(1024) void k_ad_plan(AdArgs g) {
     __shared__ int s_less[16], s_mine[16];
-    const int q = blockIdx.x, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int len = (g.M + 1023) / 1024 * 64, lo = wave * len, hi = lo + len < g.M ? lo + len : g.M;
+    const int q = blockIdx.x, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int quads = g.M / 4, len = (quads + 1023) / 1024 * 64, lo = wave * len, hi = lo + len < quads ? lo + len : quads;
+    const int4* index = reinterpret_cast<const int4*>(g.index);
+    auto segment = [&](int p) { return p >= 0 && p < g.P ? p : g.P; };
+    // run(first row, its four's segments; -1: no row)
+    auto walk = [&](auto run) {
+        for (int i0 = lo; i0 < hi; i0 += 256) {
+            int4 v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[u] = index[i0 + 64 * u + lane < hi ? i0 + 64 * u + lane : hi - 1];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int i = i0 + 64 * u + lane;
+                const int p[4] = {i < hi ? segment(v[u].x) : -1, i < hi ? segment(v[u].y) : -1, i < hi ? segment(v[u].z) : -1, i < hi ? segment(v[u].w) : -1};
+                run(4 * i, p);
+            }
+        }
+        if (wave == 15 && (g.M & 3)) {
+            const int m = 4 * quads + lane;
+            const int p[4] = {m < g.M ? segment(g.index[m < g.M ? m : 0]) : -1, -1, -1, -1};
+            run(m, p);
+        }
+    };
     int less = 0, mine = 0;
-#pragma unroll 4
-    for (int m = lo + lane; m < hi; m += 64) {
-        const int p = g.index[m], s = p >= 0 && p < g.P ? p : g.P;
-        less += s < q;
-        mine += s == q;
-    }
+    walk([&](int, const int(&p)[4]) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            less += p[e] >= 0 && p[e] < q;
+            mine += p[e] == q;
+        }
+    });
     for (int o = 32; o; o >>= 1) {
         less += __shfl_xor(less, o);
         mine += __shfl_xor(mine, o);
@@ -997,14 +1020,19 @@ __global__ __launch_bounds__(1024) void k_ad_plan(AdArgs g) {
     }
     if (mine == 0) return;
     at += start;
-#pragma unroll 4
-    for (int m0 = lo; m0 < hi; m0 += 64) {
-        const int m = m0 + lane, p = m < hi ? g.index[m] : 0;
-        const bool hit = m < hi && (p >= 0 && p < g.P ? p : g.P) == q;
-        const uint64_t hits = __ballot(hit);
-        if (hit) g.perm[at + __popcll(hits & ((1ull << lane) - 1))] = m;
-        at += __popcll(hits);
-    }
+    walk([&](int m, const int(&p)[4]) {
+        const uint64_t below = (1ull << lane) - 1;
+        int to = at;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint64_t hits = __ballot(p[e] == q);
+            to += __popcll(hits & below);
+            at += __popcll(hits);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (p[e] == q) g.perm[to++] = m + e;
+    });
 }
 
 // The gradients of the factors and of the bias, one piece of sorted rows and 128 columns of dy (role 0: dA, dbias) or x (role 1:
@@ -1018,11 +1046,12 @@ __global__ __launch_bounds__(256) void k_ad_factor_grad(AdArgs g, int col_blocks
     __shared__ __align__(16) unsigned char src[NP * SP], wts[3 * 32 * WP];
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, lr = lane & 31, lg = lane >> 5;
     const int c = blockIdx.x;
-    int lo = 0, hi = g.P;  // last segment p in [0, P] with seg[p] / AD_PIECE + p <= c
+    int lo = 0, hi = g.P;  // last segment p in [0, P] with seg[p] / AD_PIECE + p <= c: 64 places looked at together
     while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (g.seg[mid] / AD_PIECE + mid <= c) lo = mid;
-        else hi = mid - 1;
+        const int step = (hi - lo + 64) / 64, at = lo + lane * step;
+        const bool under = at <= hi && g.seg[at <= hi ? at : hi] / AD_PIECE + at <= c;
+        lo += (__popcll(__ballot(under)) - 1) * step;
+        hi = lo + step - 1 < hi ? lo + step - 1 : hi;
     }
     const int p = lo, b = c - p;
     const int s0 = g.seg[p] > b * AD_PIECE ? g.seg[p] : b * AD_PIECE;
@@ -1140,11 +1169,24 @@ __global__ __launch_bounds__(256) void k_ad_factor_grad(AdArgs g, int col_blocks
 // What is left in pieces, added in order: split dW0; factor gradients of preferences with several pieces (none: zero); dbias.
 __global__ __launch_bounds__(256) void k_ad_final(AdArgs g, int64_t n_w, int64_t n_f, int blocks_w, int blocks_f) {
     if ((int)blockIdx.x < blocks_w) {
-        const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-        if (i >= n_w) return;
-        float s = 0.f;
-        for (int q = 0; q < g.split; ++q) s += g.pw[q * n_w + i];
-        g.dw0[i] = s;
+        const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+        if ((n_w & 3) == 0) {
+            if (i >= n_w) return;
+            float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+            for (int q = 0; q < g.split; ++q) {
+                const float4 v = *reinterpret_cast<const float4*>(g.pw + q * n_w + i);
+                s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+            }
+            *reinterpret_cast<float4*>(g.dw0 + i) = s;
+        } else {
+            for (int64_t e = i; e < i + 4 && e < n_w; ++e) {
+                float s = 0.f;
+#pragma unroll 8
+                for (int q = 0; q < g.split; ++q) s += g.pw[q * n_w + e];
+                g.dw0[e] = s;
+            }
+        }
     } else if ((int)blockIdx.x < blocks_w + blocks_f) {
         const int64_t i = (int64_t)(blockIdx.x - blocks_w) * 256 + threadIdx.x;  // of [P][r (O + I)]
         if (i >= n_f) return;
@@ -1170,7 +1212,7 @@ __global__ __launch_bounds__(256) void k_ad_final(AdArgs g, int64_t n_w, int64_t
         const int each = (g.pieces + 7) / 8, c1 = (q + 1) * each < g.pieces ? (q + 1) * each : g.pieces;
         float s = 0.f;
         if (o < g.O)
-#pragma unroll 8
+#pragma unroll 16
             for (int c = q * each; c < c1; ++c) s += g.pb[(int64_t)c * g.O + o];
         sums[q][threadIdx.x % 32] = s;
         __syncthreads();
@@ -1335,7 +1377,7 @@ static void bwd(AdArgs& g, hipStream_t s) {
         else k_ad_factor_grad<T, 2><<<dim3(g.pieces, by + bx), 256, 0, s>>>(g, by);
     }
     const int64_t n_w = g.dw0 && g.split > 1 ? (int64_t)g.O * g.I : 0, n_f = g.dA || g.dB ? (int64_t)g.P * g.r * (g.O + g.I) : 0;
-    const int64_t bw = cdiv(n_w, 256), bf = cdiv(n_f, 256), bb = g.dbias ? cdiv(g.O, 32) : 0;
+    const int64_t bw = cdiv(n_w, 1024), bf = cdiv(n_f, 256), bb = g.dbias ? cdiv(g.O, 32) : 0;
     if (bw + bf + bb > 0) k_ad_final<<<bw + bf + bb, 256, 0, s>>>(g, n_w, n_f, (int)bw, (int)bf);
 }
 void launch_adapter_bwd(const morlax_adapter_dims& d, const void* x, const void* w0, const void* A, const void* B, const int32_t* index,
