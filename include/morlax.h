@@ -274,7 +274,7 @@ int morlax_pareto_hypervolume(const float* J, const float* ref, int32_t n, int32
  *   B [n_adapters, rank, d_in], index [rows] int32, y [rows, d_out] (row stride ld_y); x, w0, A, B, y of the given type.
  * B[p] x[m] is kept in fp32.  The result of a row depends on its own x and its own adapter alone.
  * Limits: 1 <= rank <= 32, 1 <= d_in, d_out <= 65536, 1 <= n_adapters <= 2^20, rows <= 2^28 and fewer than 2^24 tiles of 128 rows by
- * 128 columns; backward, fewer than 255 * 2^24 elements in the factors' gradients. */
+ * 128 columns. */
 typedef struct {
     int32_t rows, d_in, d_out, rank, n_adapters;
     int32_t dtype;

@@ -1188,23 +1188,23 @@ __global__ __launch_bounds__(256) void k_ad_final(AdArgs g, int64_t n_w, int64_t
             }
         }
     } else if ((int)blockIdx.x < blocks_w + blocks_f) {
-        const int64_t i = (int64_t)(blockIdx.x - blocks_w) * 256 + threadIdx.x;  // of [P][r (O + I)]
-        if (i >= n_f) return;
-        const int64_t per = (int64_t)g.r * (g.O + g.I);
-        const int p = (int)(i / per);
-        int64_t k = i % per;
-        const int s0 = g.seg[p], s1 = g.seg[p + 1];
-        const int c0 = s0 / AD_PIECE + p, c1 = s1 > s0 ? (s1 - 1) / AD_PIECE + p : c0 - 1;
-        if (c1 == c0) return;
-        const bool in_a = k < (int64_t)g.r * g.O;
-        if (!in_a) k -= (int64_t)g.r * g.O;
-        const int64_t n = (int64_t)g.r * (in_a ? g.O : g.I);
-        float* out = in_a ? g.dA : g.dB;
-        const float* part = in_a ? g.pA : g.pB;
-        if (!out) return;
-        float s = 0.f;
-        for (int c = c0; c <= c1; ++c) s += part[c * n + k];
-        out[p * n + k] = s;
+        // of [P][r (O + I)]: most adapters have no rows in two pieces, and nothing is to be done for them
+        for (int64_t i = (int64_t)(blockIdx.x - blocks_w) * 256 + threadIdx.x; i < n_f; i += (int64_t)blocks_f * 256) {
+            const int64_t per = (int64_t)g.r * (g.O + g.I);
+            const int p = (int)(i / per);
+            int64_t k = i % per;
+            const int s0 = g.seg[p], s1 = g.seg[p + 1];
+            const int c0 = s0 / AD_PIECE + p, c1 = s1 > s0 ? (s1 - 1) / AD_PIECE + p : c0 - 1;
+            const bool in_a = k < (int64_t)g.r * g.O;
+            if (!in_a) k -= (int64_t)g.r * g.O;
+            const int64_t n = (int64_t)g.r * (in_a ? g.O : g.I);
+            float* out = in_a ? g.dA : g.dB;
+            const float* part = in_a ? g.pA : g.pB;
+            if (c1 == c0 || !out) continue;
+            float s = 0.f;
+            for (int c = c0; c <= c1; ++c) s += part[c * n + k];
+            out[p * n + k] = s;
+        }
     } else {
         // 32 columns of dbias, eight groups of threads a contiguous eighth of the pieces each
         __shared__ float sums[8][32];
@@ -1377,7 +1377,7 @@ static void bwd(AdArgs& g, hipStream_t s) {
         else k_ad_factor_grad<T, 2><<<dim3(g.pieces, by + bx), 256, 0, s>>>(g, by);
     }
     const int64_t n_w = g.dw0 && g.split > 1 ? (int64_t)g.O * g.I : 0, n_f = g.dA || g.dB ? (int64_t)g.P * g.r * (g.O + g.I) : 0;
-    const int64_t bw = cdiv(n_w, 1024), bf = cdiv(n_f, 256), bb = g.dbias ? cdiv(g.O, 32) : 0;
+    const int64_t bw = cdiv(n_w, 1024), bf = cdiv(n_f, 256) < 2048 ? cdiv(n_f, 256) : 2048, bb = g.dbias ? cdiv(g.O, 32) : 0;
     if (bw + bf + bb > 0) k_ad_final<<<bw + bf + bb, 256, 0, s>>>(g, n_w, n_f, (int)bw, (int)bf);
 }
 void launch_adapter_bwd(const morlax_adapter_dims& d, const void* x, const void* w0, const void* A, const void* B, const int32_t* index,

@@ -501,7 +501,7 @@ static int strided(const void* p, int dtype, const char* name, const char* who) 
         if (rc_ != MORLAX_OK) return rc_;                               \
     } while (0)
 
-static int check_adapter(const morlax_adapter_dims* d, bool backward, const char* who) {
+static int check_adapter(const morlax_adapter_dims* d, const char* who) {
     if (!d) return fail(MORLAX_ERR_NULL, "%s: dims is NULL", who);
     if (d->rows < 0 || d->d_in < 1 || d->d_out < 1 || d->rank < 1 || d->n_adapters < 1)
         return fail(MORLAX_ERR_SHAPE, "%s: rows must be >= 0, d_in, d_out, rank and n_adapters >= 1", who);
@@ -511,24 +511,22 @@ static int check_adapter(const morlax_adapter_dims* d, bool backward, const char
         return fail(MORLAX_ERR_UNSUPPORTED, "%s: d_in and d_out must be <= 65536, n_adapters <= 2^20", who);
     if (d->ld_x < d->d_in || d->ld_y < d->d_out)
         return fail(MORLAX_ERR_SHAPE, "%s: a row stride is shorter than its row", who);
-    // a launch holds fewer than 2^32 threads along x: 256 for an output tile, 8 for a row, one for an element of a factor's gradient
+    // a launch holds fewer than 2^32 threads along x: 256 for an output tile, 8 for a row
     const int64_t wide = d->d_in > d->d_out ? d->d_in : d->d_out;
     if (d->rows > 1 << 28 || ((int64_t)d->rows / 128 + 1) * (wide / 128 + 1) >= (int64_t)1 << 24)
         return fail(MORLAX_ERR_UNSUPPORTED, "%s: rows must be <= 2^28 and their 128 x 128 tiles fewer than 2^24", who);
-    if (backward && (int64_t)d->n_adapters * d->rank * ((int64_t)d->d_in + d->d_out) >= (int64_t)255 << 24)
-        return fail(MORLAX_ERR_UNSUPPORTED, "%s: the factors' gradients must have fewer than 255 * 2^24 elements", who);
     return MORLAX_OK;
 }
 
 extern "C" int64_t morlax_adapter_workspace_bytes(const morlax_adapter_dims* d, int32_t backward) {
-    if (check_adapter(d, backward != 0, "morlax_adapter_workspace_bytes") != MORLAX_OK) return -1;
+    if (check_adapter(d, "morlax_adapter_workspace_bytes") != MORLAX_OK) return -1;
     return adapter_ws_bytes(*d, backward != 0);
 }
 
 extern "C" int morlax_adapter_fwd(const morlax_adapter_dims* dims, const void* x, const void* w0, const float* bias, const void* A,
                                   const void* B, const int32_t* index, void* y, void* ws, int64_t ws_bytes, void* stream) {
     const char* who = "morlax_adapter_fwd";
-    const int rc = check_adapter(dims, false, who);
+    const int rc = check_adapter(dims, who);
     if (rc != MORLAX_OK) return rc;
     REQ(w0, who); REQ(A, who); REQ(B, who); OPT(bias, who);
     if (dims->rows == 0) return MORLAX_OK;
@@ -543,7 +541,7 @@ extern "C" int morlax_adapter_bwd(const morlax_adapter_dims* dims, const void* x
                                   const int32_t* index, const void* dy, void* dx, float* dw0, float* dbias, float* dA, float* dB,
                                   void* ws, int64_t ws_bytes, void* stream) {
     const char* who = "morlax_adapter_bwd";
-    const int rc = check_adapter(dims, true, who);
+    const int rc = check_adapter(dims, who);
     if (rc != MORLAX_OK) return rc;
     REQ(w0, who); REQ(A, who); REQ(B, who);
     OPT(dw0, who); OPT(dbias, who); OPT(dA, who); OPT(dB, who);

@@ -78,13 +78,6 @@ def test_adapter_pointers_and_workspace():
     binding.adapter_fwd(adapter(rows=0), None, GOOD, None, GOOD, GOOD, None, None, (GOOD, 1 << 20), stream=0)
 
 
-def test_adapter_gradients_that_a_launch_cannot_hold():
-    d = adapter(adapters=1 << 20, rank=32, d_in=128, d_out=128)
-    assert binding.adapter_workspace_bytes(d) > 0
-    with pytest.raises(binding.MorlaxError):
-        binding.adapter_workspace_bytes(d, True)
-
-
 def conv(**over):
     d = dict(T=5, N=3, channels=16, width=4, act=1, dtype=1)
     d.update(over)
