@@ -722,22 +722,16 @@ __global__ __launch_bounds__(512) void k_ad_few(AdArgs g) {
 }
 
 // ---- u (or v): the rows' products with their adapters' short factor ------------------------------------------------------------------
-// Few rows, or small factors: WPR waves a row (four, or one where the contraction is short), which share the contraction; a factor's
-// values are used once.
+// A thread's part of row position m's: WPR waves (four, or one) share the contraction, a factor's values are used once.
 template <typename T, bool BWD, int RP, int WPR, bool WHOLE>
-__global__ __launch_bounds__(256) void k_ad_shrink_row(AdArgs g) {
+__device__ inline void shrink_row(const AdArgs& g, int m, int p, int tid, float (&acc)[RP]) {
     constexpr int VE = 16 / (int)sizeof(T);
-    __shared__ float part[4][RP];
-    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int m = WPR == 4 ? blockIdx.x : blockIdx.x * 4 + wave, tid = WPR == 4 ? threadIdx.x : lane;
-    if (WPR == 1 && m >= g.M) return;
-    const int p = __builtin_amdgcn_readfirstlane(g.adapter(m));
     const int K = BWD ? g.O : g.I;
     const T* row = reinterpret_cast<const T*>(BWD ? g.dy : g.x) + (int64_t)g.row(m) * (BWD ? g.ld_y : g.ld_x);
-    float acc[RP];
 #pragma unroll
     for (int j = 0; j < RP; ++j) acc[j] = 0.f;
-    if (p >= 0) {
+    if (p < 0) return;
+    {
         const T* f = reinterpret_cast<const T*>(BWD ? g.A : g.B) + (int64_t)p * K * g.r;
         if (BWD) {  // A_p [O][r]: a thread's rows of it, two requested together
             for (int k = tid; k < K; k += 2 * 64 * WPR) {
@@ -779,7 +773,12 @@ __global__ __launch_bounds__(256) void k_ad_shrink_row(AdArgs g) {
             }
         }
     }
-    // sums over the wave: of RP values, a lane keeps fewer and fewer (bits 5, 4, .. of the lane select the halves of j)
+}
+// their sums over the wave: of RP values, a lane keeps fewer and fewer (bits 5, 4, .. of the lane select the halves of j); value
+// lane / (64 / RP) is returned
+template <int RP>
+__device__ inline float shrink_sum(float (&acc)[RP]) {
+    const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int h = RP / 2, o = 32; h >= 1; h /= 2, o /= 2)
 #pragma unroll
@@ -791,6 +790,19 @@ __global__ __launch_bounds__(256) void k_ad_shrink_row(AdArgs g) {
     float s = acc[0];
 #pragma unroll
     for (int o = 64 / RP / 2; o >= 1; o /= 2) s += __shfl_xor(s, o);
+    return s;
+}
+// Few rows, or small factors: WPR waves a row.
+template <typename T, bool BWD, int RP, int WPR, bool WHOLE>
+__global__ __launch_bounds__(256) void k_ad_shrink_row(AdArgs g) {
+    __shared__ float part[4][RP];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int m = WPR == 4 ? blockIdx.x : blockIdx.x * 4 + wave;
+    if (WPR == 1 && m >= g.M) return;
+    const int p = __builtin_amdgcn_readfirstlane(g.adapter(m));
+    float acc[RP];
+    shrink_row<T, BWD, RP, WPR, WHOLE>(g, m, p, WPR == 4 ? threadIdx.x : lane, acc);
+    const float s = shrink_sum<RP>(acc);
     float* out = (BWD ? g.v : g.u) + (int64_t)m * g.rp;
     const int j = lane / (64 / RP);
     if (RP == 8 && threadIdx.x % (64 * WPR) >= 8 && threadIdx.x % (64 * WPR) < 16) out[threadIdx.x % (64 * WPR)] = 0.f;  // (g.rp is 16)
@@ -862,15 +874,17 @@ __device__ inline void shrink_staged(const bf16_t* f, const bf16_t* const (&rows
     }
 }
 
+// adapters among 32 rows beyond which these are taken one by one
+#define AD_ONE_BY_ONE 4
 // Many rows: 32 a workgroup, its four waves a quarter of the contraction each, one pass over the rows per adapter among them.  bf16 on
 // 32x32x16, fp32 on 32x32x2 (the factor's 32 rows are at most `rank` real ones; the pass is bound by its reads).  A lane takes 64 bytes of
 // its row at a time, so a line is read whole; the backward's factor, [O][r], is turned in LDS.
-template <typename T, bool BWD>
-__global__ __launch_bounds__(256) void k_ad_shrink(AdArgs g) {
+template <typename T, bool BWD, int RP, bool WHOLE>
+__global__ __launch_bounds__(256, RP == 32 ? 2 : 4) void k_ad_shrink(AdArgs g) {
     constexpr int VE = 16 / (int)sizeof(T), KI = 8 * VE;  // contraction indices of an iteration: four pieces of either lane group
     // a wave's: the rows' pieces on their way (bf16), the factor turned (backward), then its sums
     __shared__ __align__(16) unsigned char lds[4][BWD ? 8192 : 32 * 33 * 4];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5;
     const int m0 = blockIdx.x * 32, m = m0 + lr;
     const int K = BWD ? g.O : g.I;
     const int64_t ld = BWD ? g.ld_y : g.ld_x;
@@ -888,6 +902,21 @@ __global__ __launch_bounds__(256) void k_ad_shrink(AdArgs g) {
     float* out = BWD ? g.v : g.u;
     const int p = g.adapter(m);
     uint64_t todo = __ballot(p >= 0) & 0xffffffffull;
+    int others = 0;  // adapters among the rows
+    for (uint64_t left = todo; left; ++others) left &= ~__ballot(p == __builtin_amdgcn_readlane(p, __ffsll((unsigned long long)left) - 1));
+    if (others > AD_ONE_BY_ONE) {
+        for (int i = 0; i < 8; ++i) {
+            const int mi = m0 + 8 * wave + i, pi = __builtin_amdgcn_readlane(p, 8 * wave + i);
+            if (mi >= g.M) break;
+            float acc[RP];
+            shrink_row<T, BWD, RP, 1, WHOLE>(g, mi, pi, lane, acc);
+            const float s = shrink_sum<RP>(acc);
+            const int j = lane / (64 / RP);
+            if (lane % (64 / RP) == 0) out[(int64_t)mi * g.rp + j] = j < g.r && pi >= 0 ? s : 0.f;
+            if (RP == 8 && lane >= 8 && lane < 16) out[(int64_t)mi * g.rp + lane] = 0.f;  // (g.rp is 16)
+        }
+        return;
+    }
     const bool whole = K % VE == 0;
     const int kw = ((K + 4 * KI - 1) / (4 * KI)) * KI;  // contraction indices of a wave
     const int k0 = wave * kw, k1 = k0 + kw < K ? k0 + kw : K;
@@ -1291,9 +1320,9 @@ static void pick_rank(const AdArgs& g, bool whole, F run) {
 template <typename T, bool BWD>
 static void shrink(const AdArgs& g, hipStream_t s) {
     const int K = BWD ? g.O : g.I;
+    const bool whole = (BWD ? g.r : K) % (16 / (int)sizeof(T)) == 0;
     if ((int64_t)g.M * g.r * K * (int64_t)sizeof(T) <= AD_ROW_BYTES) {
         const bool one = K <= (BWD ? 256 : 128 * 16 / (int)sizeof(T)) && g.M > 256;  // a wave a row: two rounds of its lanes or four, and waves enough
-        const bool whole = (BWD ? g.r : K) % (16 / (int)sizeof(T)) == 0;
         auto run = [&](auto rp, auto w) {
             constexpr int RP = decltype(rp)::value;
             constexpr bool W = decltype(w)::value;
@@ -1302,7 +1331,7 @@ static void shrink(const AdArgs& g, hipStream_t s) {
         };
         pick_rank(g, whole, run);
     } else {
-        k_ad_shrink<T, BWD><<<cdiv(g.M, 32), 256, 0, s>>>(g);
+        pick_rank(g, whole, [&](auto rp, auto w) { k_ad_shrink<T, BWD, decltype(rp)::value, decltype(w)::value><<<cdiv(g.M, 32), 256, 0, s>>>(g); });
     }
 }
 // Which kernel multiplies with W0.  Few rows: 16 columns a workgroup where 128 x 128 tiles would leave most CUs without one.  Else tiles:
@@ -1313,7 +1342,7 @@ static void product(const AdArgs& g, hipStream_t s) {
     const int64_t tiles = cdiv(rows_a, 128) * cdiv(rows_b, 128);
     const int split = ROLE == AD_DW ? g.split : 1;
     if constexpr (ROLE != AD_DW)
-        if ((tiles <= 64 || K <= 64) && cdiv(g.M, 32) <= 65535) {
+        if ((tiles <= (sizeof(T) == 4 && ROLE == AD_FWD ? 160 : 64) || (K <= 64 && (sizeof(T) == 4 || tiles <= 256))) && cdiv(g.M, 32) <= 65535) {
             pick_rank(g, K % (16 / (int)sizeof(T)) == 0, [&](auto rp, auto w) {
                 k_ad_few<T, ROLE == AD_DX, decltype(rp)::value, decltype(w)::value><<<dim3(cdiv(rows_b, 16), cdiv(g.M, 32)), 512, 0, s>>>(g);
             });

@@ -1703,12 +1703,13 @@ void launch_conv_bwd(const morlax_conv_dims& d, const void* x, const float* w, c
 }
 
 // Spans of time: one where environments and heads fill the machine's SIMDs, or the segment is short; else as many as give every SIMD a
-// wave, of two chunks at least (a span costs its inputs once more and a state to write and read).
+// wave, of two chunks at least (a span costs its inputs once more and a state to write and read).  us with and without, 64 x 64 bf16: 64
+// waves of 32 chunks 38 and 190, 256 of 8 39 and 53, 512 of 32 169 and 196; but 384 of 8 57 and 54, 512 of 8 62 and 55.
 static void scan_spans(ScanArgs& g) {
     const int64_t waves = (int64_t)g.N * g.H;
     g.spans = 1;
     g.span = g.chunks * MEM_Q;
-    if (waves > 512 || g.chunks < 8) return;
+    if (waves > 512 || g.chunks < (waves > 256 ? 32 : 8)) return;
     int64_t spans = cdiv(1024, waves);
     if (spans > g.chunks / 2) spans = g.chunks / 2;
     g.span = (int)(cdiv(g.chunks, spans) * MEM_Q);
@@ -1831,7 +1832,7 @@ void launch_memory_step(const morlax_scan_dims& d, int width, const void* xbc, c
     int lpr = 1;
     while (lpr < 64 && lpr * (vec ? 4 : 1) < g.S) lpr *= 2;
     const int lds = 4 * (g.P + 2 * g.S) * 4;
-    const int parts = (int64_t)g.N * g.H < 1024 && g.P >= 4 ? 4 : 1;  // a wave for every SIMD
+    const int parts = (int64_t)g.N * g.H <= 1536 && g.P >= 4 ? 4 : 1;  // a wave for every SIMD, or nearly
     const int64_t blocks = cdiv((int64_t)g.N * g.H * parts, 4);
     if (d.dtype) k_memory_step<bf16_t><<<blocks, 256, lds, s>>>(a, lpr, vec, parts);
     else k_memory_step<float><<<blocks, 256, lds, s>>>(a, lpr, vec, parts);
