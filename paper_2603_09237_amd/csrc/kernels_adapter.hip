@@ -308,7 +308,9 @@ __device__ inline void ad_store(const AdArgs& g, const float16_t (&acc)[2], unsi
 static __device__ inline bool ad_vec(const void* p, int64_t ld, int size) {
     return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * size)) & 15) == 0;
 }
-// The three products with or of W0, on 128 x 128 tiles of four waves of 64 x 64: any size, stride and alignment.
+// The three products with or of W0, on 128 x 128 tiles of four waves of 64 x 64: any size, stride and alignment.  fp32 as three bf16 parts
+// a value (split3: what the six products leave out is below 2^-24 of the largest term), two thirds of the fp32 instructions' cycles; the
+// split's arithmetic and the waits for registers on their way to LDS bound it (dW of 584 x 256 over 2051 rows: 15 us).
 enum { AD_FWD = 0, AD_DX = 1, AD_DW = 2 };
 template <int ROLE> struct AdRole;
 template <> struct AdRole<AD_FWD> { static constexpr int KA = KC, KB = KC; };
@@ -437,7 +439,11 @@ __global__ __launch_bounds__(256, 2) void k_ad_gemm(AdArgs g) {
 // Tiles of 64 MB x 128, four waves of 32 MB x 64.  A stage's pieces lie as the loads leave them, one KB an instruction; which piece a lane
 // fetches is free, and the bank swizzle is there: KC, piece (row, c) of four a row at position 4 row + (c ^ row's bits 2, 3); KS, piece
 // (k, c) of ROWS / 8 a contraction index at (ROWS / 8) k + (c ^ 4 (k mod 4)), read transposed.  A contraction that is no multiple of 32
-// begins with the rest of it, loaded through registers.
+// begins with the rest of it, loaded through registers.  Half a stage's products run while the other half's operands and the loads of the third
+// next stage are issued between them, with no branch in the loop.
+// 16384 x 512 x 1160, 20.3 GFLOP: 40 us, 0.5 PFLOP/s; dX and dW of 32768 x 512 x 1160, 39 GFLOP each: 62 and 61 us, 0.63 PFLOP/s.  Bound by the
+// loads: without the matrix instructions 37 of 40 and 55 of 62 us are left (rows of 64 bytes a request keep the L2 busy), without the loads 30
+// and 44; the last tiles' outputs, which nothing overlaps, take 10.  Tiles of 256 x 256 at a wave a SIMD took 67 and 57 (and 5 more to add up).
 template <int KIND, int ROWS>
 struct AdTile {
     static constexpr int NI = ROWS / 16 / 4, CPR = ROWS / 8, BYTES = ROWS * 64;
@@ -649,7 +655,8 @@ __device__ inline uint4 ad_column(const T* col, int64_t stride, int k, int K) {
     }
     return *reinterpret_cast<uint4*>(e);
 }
-// A workgroup has 16 columns x 32 rows, an output a thread; rows beyond the last one repeat it.
+// A workgroup has 16 columns x 32 rows, an output a thread; rows beyond the last one repeat it.  64 rows x 2048 x 2048 bf16 with an adapter each:
+// 9 us; 4099 x 27 x 523 fp32: 25 us, where a value of a row of 27 is a load of its own.
 template <typename T, bool BWD, int RP, bool WHOLE>
 __global__ __launch_bounds__(512) void k_ad_few(AdArgs g) {
     constexpr int VE = 16 / (int)sizeof(T), STEP = 4 * VE, U = BWD ? 2 : 4;  // contraction indices of a step; steps requested together
@@ -792,7 +799,8 @@ __device__ inline float shrink_sum(float (&acc)[RP]) {
     for (int o = 64 / RP / 2; o >= 1; o /= 2) s += __shfl_xor(s, o);
     return s;
 }
-// Few rows, or small factors: WPR waves a row.
+// Few rows, or small factors: WPR waves a row.  Latency: index, row and factor one after the other; 64 rows x 2048 bf16 8 us, 2051 x 584 fp32 of
+// rank 8 backward 8 us.
 template <typename T, bool BWD, int RP, int WPR, bool WHOLE>
 __global__ __launch_bounds__(256) void k_ad_shrink_row(AdArgs g) {
     __shared__ float part[4][RP];
@@ -874,11 +882,13 @@ __device__ inline void shrink_staged(const bf16_t* f, const bf16_t* const (&rows
     }
 }
 
-// adapters among 32 rows beyond which these are taken one by one
+// adapters among 32 rows beyond which these are taken one by one.  us of the forward, rows mixed: 2048 x 1160 x 1160 fp32 of 8 adapters 146
+// one by one, 292 adapter by adapter; 16384 x 512 x 1160 bf16 of 128 142 and 162; of 4 adapters 57 and 56 (above four are one by one)
 #define AD_ONE_BY_ONE 4
 // Many rows: 32 a workgroup, its four waves a quarter of the contraction each, one pass over the rows per adapter among them.  bf16 on
-// 32x32x16, fp32 on 32x32x2 (the factor's 32 rows are at most `rank` real ones; the pass is bound by its reads).  A lane takes 64 bytes of
-// its row at a time, so a line is read whole; the backward's factor, [O][r], is turned in LDS.
+// 32x32x16, fp32 on 32x32x2 (the factor's 32 rows are at most `rank` real ones; the pass is bound by its reads).  The backward's factor,
+// [O][r], is turned in LDS.  bf16, whole lines: 32768 x 512 13 us (2.6 TB/s), 32768 x 1160 backward 29 us (2.7 TB/s); a lane taking 64 bytes of
+// its own row at a time, as fp32 and rows of odd sizes do, needed 17 and 36.
 template <typename T, bool BWD, int RP, bool WHOLE>
 __global__ __launch_bounds__(256, RP == 32 ? 2 : 4) void k_ad_shrink(AdArgs g) {
     constexpr int VE = 16 / (int)sizeof(T), KI = 8 * VE;  // contraction indices of an iteration: four pieces of either lane group
@@ -995,7 +1005,8 @@ __global__ __launch_bounds__(256, RP == 32 ? 2 : 4) void k_ad_shrink(AdArgs g) {
 
 // Rows sorted by adapter, order kept among a preference's own: workgroup q walks the index twice, to count the rows that come
 // before its own, and to place them, a wave a contiguous sixteenth of the rows (and the last one those behind the last whole four).  q = P:
-// the rows without one.  Bound by latency: a lane takes four rows at a time and has four such pieces on their way.
+// the rows without one.  Bound by latency: a lane takes four rows at a time and has four such pieces on their way (32768 rows of 128: 8 us, one at
+// a time 13).
 __global__ __launch_bounds__(1024) void k_ad_plan(AdArgs g) {
     __shared__ int s_less[16], s_mine[16];
     const int q = blockIdx.x, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -1066,6 +1077,7 @@ __global__ __launch_bounds__(1024) void k_ad_plan(AdArgs g) {
 
 // The gradients of the factors and of the bias, one piece of sorted rows and 128 columns of dy (role 0: dA, dbias) or x (role 1:
 // dB) a workgroup: out[c][j] = sum_m src[m][c] w[m][j] with w = u or v in three bf16 parts; a column of ones beside u's gives dbias.
+// Bound by its reads, dy and x once more, and their way through LDS: 32768 x (1160 + 512) bf16, 110 MB, 37 us (2.9 TB/s).
 // Piece c of the sorted rows: segment p and block b = c - p of AD_PIECE rows, p the last one with seg[p] / AD_PIECE + p <= c.
 template <typename T, int JB>
 __global__ __launch_bounds__(256) void k_ad_factor_grad(AdArgs g, int col_blocks_y) {
@@ -1195,6 +1207,7 @@ __global__ __launch_bounds__(256) void k_ad_factor_grad(AdArgs g, int col_blocks
         }
 }
 
+// (32768 x 512 x 1160: 12 ranges of dW0, 28 MB, 12 us.)
 // What is left in pieces, added in order: split dW0; factor gradients of preferences with several pieces (none: zero); dbias.
 __global__ __launch_bounds__(256) void k_ad_final(AdArgs g, int64_t n_w, int64_t n_f, int blocks_w, int blocks_f) {
     if ((int)blockIdx.x < blocks_w) {
@@ -1334,7 +1347,9 @@ static void shrink(const AdArgs& g, hipStream_t s) {
         pick_rank(g, whole, [&](auto rp, auto w) { k_ad_shrink<T, BWD, decltype(rp)::value, decltype(w)::value><<<cdiv(g.M, 32), 256, 0, s>>>(g); });
     }
 }
-// Which kernel multiplies with W0.  Few rows: 16 columns a workgroup where 128 x 128 tiles would leave most CUs without one.  Else tiles:
+// Which kernel multiplies with W0.  Few rows: 16 columns a workgroup where 128 x 128 tiles would leave most CUs without one.  us, few rows' kernel
+// and tiles, 512 to 1160: bf16 64 rows 11 and 20, 256 14 and 21, 512 (40 tiles) 18 and 21, 2048 (160) 45 and 24; fp32 1024 41 and 72, 2048 (160)
+// 70 and 76; 64 to 512, where a tile has two steps: bf16 4099 rows (132) 23 and 37, 16384 (512) 89 and 55; fp32 4099 49 and 122.  Else tiles:
 // direct-to-LDS loads for bf16 rows of whole 16-byte pieces within 32-bit offsets, the general kernel for the rest.
 template <typename T, int ROLE>
 static void product(const AdArgs& g, hipStream_t s) {
