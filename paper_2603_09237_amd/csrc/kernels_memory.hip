@@ -325,7 +325,7 @@ struct ScanArgs {
     const float *state_in, *dstate_out;
     void *y, *dx, *db, *dc, *ddt, *dz;
     float *state_out, *dstate_in, *da_log, *dd_skip, *ddt_bias;
-    float *saved;        // per (n, h): chunks + 1 states as the registers hold them
+    float *saved;        // per (n, h): the state before each chunk, as the registers hold it
     float *pb, *pc;      // [head block][T][N][G][S] sums of dB, dC where a group's heads need several workgroups
     float *ph;           // [3][H][N][spans] sums of da, dD, ddt_bias
     float *ends;         // [N H][spans] states that a span leaves or takes over, as the registers hold them
@@ -405,14 +405,17 @@ __device__ inline void split_parts(const float (&v)[8], uint4 (&p)[2]) {
     for (int i = 0; i < 8; ++i) l[i] = v[i] - __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
     p[1] = pack_chunk<bf16_t>(l);
 }
-// a += sum of products of parts i, j with i + j <= 2, smallest first
-template <int NA, int NB>
+// a += sum of products of parts i, j with i + j <= 2, smallest first.  MIRROR: in the order that gives each element the bits that the product
+// with a and b exchanged gives it.
+template <bool MIRROR = false, int NA, int NB>
 __device__ inline void mma_p(const uint4 (&a)[NA], const uint4 (&b)[NB], float16_t& c) {
 #pragma unroll
     for (int s = (NA + NB - 2 < 2 ? NA + NB - 2 : 2); s >= 0; --s)
 #pragma unroll
-        for (int i = 0; i < NA; ++i)
-            if (s - i >= 0 && s - i < NB) Mma32<bf16_t>::run(a[i], b[s - i], c);
+        for (int k = 0; k <= s; ++k) {
+            const int i = MIRROR ? s - k : k;
+            if (i < NA && s - i < NB) Mma32<bf16_t>::run(a[i], b[s - i], c);
+        }
 }
 __device__ inline void zero(float16_t& c) {
 #pragma unroll
@@ -810,7 +813,7 @@ __global__ __launch_bounds__((ScanFwdLds<T, PB, SB>::NW * 64), 2) void k_scan_fw
     else if (g.spans > 1) st.undump(g.ends + unit * per);
     else if (g.state_in) st.load(g.state_in + id * g.P * g.S, g.P, g.S, patch);
     else st.clear();
-    float* saved = !LOCAL && g.saved ? g.saved + id * (g.chunks + 1) * per : nullptr;
+    float* saved = !LOCAL && g.saved ? g.saved + id * g.chunks * per : nullptr;
     float all = 1.f;  // LOCAL: what is left of a state that enters the span
     int slow = 0;  // steps to take one by one: a chunk with an undefined or infinite input, which would reach others through products with zero
     for (int t = t_begin; t < t_end;) {
@@ -940,7 +943,6 @@ __global__ __launch_bounds__((ScanFwdLds<T, PB, SB>::NW * 64), 2) void k_scan_fw
         return;
     }
     if (span + 1 < g.spans) return;
-    if (saved) st.dump(saved + (int64_t)g.chunks * per);
     if (g.state_out && g.spans == 1) st.store(g.state_out + id * g.P * g.S, g.P, g.S, patch);
 }
 
@@ -984,7 +986,10 @@ __global__ __launch_bounds__(256) void k_scan_join(ScanArgs g) {
 //   dC_t = sum_s E R dt_s B_s + q_t h_in dy_t,           dB_s = dt_s dB'_s,  dB'_s = sum_t E R C_t + u_s dh x_s,
 //   dx_s = dt_s (sum_t E (C_t . B_s) dy_t + u_s dh^T B_s) + D dy_s,   dh_in = exp(l_31) dh + sum_t q_t C_t dy_t^T,
 // and for the decays' exponents, whose gradient at step i is the sum over the pairs (t, s) that it lies between,
-//   d(dt_i a) = sum_{t >= i} (C_t . dC_t - dt_t B_t . dB'_t) + <h_out, dh>      over i's episode; zero where it begins.
+//   d(dt_i a) = sum_{s < i <= t} E (C_t . B_s) dt_s R[t, s] + sum_{t >= i} C_t . q_t h_in dy_t + sum_{s < i} dt_s B_s . u_s dh x_s + exp(l_31) <h_in, dh>,
+// the first sum as that over t >= i of what the pairs with earlier steps give less what those with later ones do: the pairs of two steps from i on
+// are in both.  (As sum_{t >= i} (C_t . dC_t - dt_t B_t . dB'_t) + <h_out, dh>, which costs no sums of its own, the pair of a step with itself and
+// what ends in h_out were taken once and taken off again: the error of a_log's gradient was ten times the plain form's in fp32.)
 // Half the environments of the forward's example: 322 us.  Bound by instructions and their waits: 58 million of the vector unit's (94 us of its
 // time) at one wave a SIMD, whose 498 registers and 37 KB of LDS leave no room for a second; 37 % of the cycles wait.
 template <typename T, int PB, int SB>
@@ -1028,26 +1033,12 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
     const double a2 = (double)av * 1.4426950408889634;
     const float dskip = g.d_skip ? g.d_skip[h] : 0.f, bias = g.dt_bias ? g.dt_bias[h] : 0.f;
     const int64_t per = (int64_t)SB * PB * 1024;
-    const float* saved = g.saved + id * (g.chunks + 1) * per;
+    const float* saved = g.saved + id * g.chunks * per;
     State<PB, SB> dh1;
     if (g.spans > 1) dh1.undump(g.ends + (id * g.spans + span) * per);
     else if (g.dstate_out) dh1.load(g.dstate_out + id * g.P * g.S, g.P, g.S, red);
     else dh1.clear();
     float sum_a = 0.f, sum_d = 0.f, sum_b = 0.f;  // per lane: of its steps
-    float inner;                                  // <state behind the chunk, dh>
-    {
-        State<PB, SB> last;
-        last.undump(saved + (int64_t)((t_last + MEM_Q - 1) / MEM_Q) * per);
-        float s = 0.f;
-#pragma unroll
-        for (int i = 0; i < SB; ++i)
-#pragma unroll
-            for (int p = 0; p < PB; ++p)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s += last.v[i][p][e] * dh1.v[i][p][e];
-        for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
-        inner = s;
-    }
     int slow = 0;
     for (int t_end = t_last; t_end > t_begin;) {
         const int base = (t_end - 1) / MEM_Q * MEM_Q;
@@ -1093,11 +1084,22 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
                     }
             }
         }
+        float through = 0.f;  // <h_in, dh>: the chunk's first state in its last
+#pragma unroll
+        for (int i = 0; i < SB; ++i)
+#pragma unroll
+            for (int p = 0; p < PB; ++p)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) through += hin.v[i][p][e] * dh1.v[i][p][e];
+        for (int o = 32; o; o >>= 1) through += __shfl_xor(through, o);
+        through = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(through)));
+        phase();
         const Steps s = steps<T>(g, n, h, t, cnt, a2, bias, sl);
         const float hiq = last_of(s.hi), loq = last_of(s.lo);
         const int eq = __builtin_amdgcn_readlane(s.e, 31);
         const float us = lr >= eq ? decay(hiq, loq, s.hi, s.lo) : 0.f;                     // to the chunk's end
         const float qs = s.e < 0 ? __builtin_amdgcn_exp2f(s.hi + s.lo) : 0.f;              // from its start
+        const float left = eq < 0 ? __builtin_amdgcn_exp2f(hiq + loq) : 0.f;                // over all of it
         if (lane < 32) sl->w[lr] = qs;
         phase();
         phase();
@@ -1110,7 +1112,7 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
             C.rows(kk, oc);
             B.rows(kk, ob);
             mma_p(ob, oc, g1);
-            mma_p(oc, ob, g2);
+            mma_p<true>(oc, ob, g2);
         }
 #pragma unroll
         for (int kk = 0; kk < 2 * PB; ++kk) {
@@ -1118,9 +1120,11 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
             X.rows(kk, ox);
             D.rows(kk, fd);
             mma_p(ox, fd, r1);
-            mma_p(fd, ox, r2);
+            mma_p<true>(fd, ox, r2);
         }
         phase();
+        // row_s, col_s: the sums over earlier steps of E scores R dt, over later ones of E scores R; self: the pair of a step with itself
+        float row_s = 0.f, col_s = 0.f, self = 0.f;
         // m1: scores that give y [s | t]; v1: E R dt_s [s | t]; g2: E scores [t | s]; r2: E R [t | s]
         float16_t m1;
 #pragma unroll
@@ -1131,8 +1135,12 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
             const bool on1 = r <= lr && r >= s.e, on2 = r >= lr && lr >= re;
             const float d1 = on1 ? decay(s.hi, s.lo, rhi, rlo) * rdt : 0.f, d2 = on2 ? decay(rhi, rlo, s.hi, s.lo) : 0.f;
             m1[e] = counted(g1[e], d1);
+            row_s += r != lr ? counted(r1[e], m1[e]) : 0.f;
             r1[e] = counted(r1[e], d1);
             g2[e] = counted(g2[e], d2);
+            const float pair = counted(r2[e], g2[e]);
+            col_s += r != lr ? pair : 0.f;
+            self += r != lr ? 0.f : pair;
             r2[e] = counted(r2[e], d2);
         }
         phase();
@@ -1243,7 +1251,7 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
             phase();
         }
         // dC [n | t], dB' [n | s]
-        float row_tot = 0.f, col_tot = 0.f;
+        float state_tot = 0.f, end_tot = 0.f;  // C_t . q_t h_in dy_t, B_s . u_s dh x_s
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
             float16_t o[SB];
@@ -1281,6 +1289,22 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
             for (int i = 0; i < SB; ++i)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) o[i][e] = counted(o[i][e], lane_scale);
+            {
+                float tot = 0.f;
+#pragma unroll
+                for (int i = 0; i < SB; ++i)
+#pragma unroll
+                    for (int k4 = 0; k4 < 4; ++k4) {
+                        float v[4];
+                        if (which) B.get4(lr, 32 * i + 8 * k4 + 4 * lg, v);
+                        else C.get4(lr, 32 * i + 8 * k4 + 4 * lg, v);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) tot += v[k] * o[i][4 * k4 + k];
+                    }
+                if (which) end_tot = tot;
+                else state_tot = tot;
+            }
+            phase();
 #pragma unroll
             for (int kk = 0; kk < 2; ++kk) {
                 uint4 fv[3], f[NP];
@@ -1293,25 +1317,16 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
                 }
             }
             phase();
-            float tot = 0.f;
 #pragma unroll
             for (int i = 0; i < SB; ++i)
 #pragma unroll
                 for (int k4 = 0; k4 < 4; ++k4) {
                     const int n0 = 32 * i + 8 * k4 + 4 * lg;
-                    float v[4];
-                    if (which) B.get4(lr, n0, v);
-                    else C.get4(lr, n0, v);
                     float4 r;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) tot += v[k] * o[i][4 * k4 + k];
                     const float sc = live ? (which ? s.dt : 1.f) : 0.f;
                     r.x = o[i][4 * k4] * sc; r.y = o[i][4 * k4 + 1] * sc; r.z = o[i][4 * k4 + 2] * sc; r.w = o[i][4 * k4 + 3] * sc;
                     *reinterpret_cast<float4*>(red + lr * RP + n0) = r;
                 }
-            tot += __shfl_xor(tot, 32);
-            if (which) col_tot = tot;
-            else row_tot = tot;
             __syncthreads();
             for (int i = threadIdx.x; i < cnt * 32 * SB; i += NW * 64) {
                 const int tt = i / (32 * SB), nn = i % (32 * SB);
@@ -1331,17 +1346,22 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
         }
         // gradients of the steps
         {
-            float q = row_tot - s.dt * col_tot;
-            if (lr >= cnt) q = 0.f;
-            // sum over the later steps of the episode: step t' belongs to it while its e is not beyond this step
-            float acc = q;
+            // later steps: pairs with two of them are in row_s and in col_s, with the same bits, or nearly
+            float acc = row_s - s.dt * col_s + state_tot, col_tot = self + col_s + end_tot;  // col_tot: B_s . dB'_s
+            acc += __shfl_xor(acc, 32);
+            col_tot += __shfl_xor(col_tot, 32);
+            end_tot += __shfl_xor(end_tot, 32);
+            float before = s.dt * end_tot;
+            if (lr >= cnt) acc = before = 0.f;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
-                const float dn = __shfl_down(acc, o, 32);
-                const int eo = __shfl_down(s.e, o, 32);
-                if (lr + o < 32 && eo <= lr) acc += dn;
+                const float dn = __shfl_down(acc, o, 32), up = __shfl_up(before, o, 32);
+                if (lr + o < 32) acc += dn;
+                if (lr >= o) before += up;
             }
-            if (lr >= eq) acc += inner;
+            before = __shfl_up(before, 1, 32);
+            if (lr > 0) acc += before;
+            acc += counted(through, left);
             if (s.begins) acc = 0.f;
             const float ddt = col_tot + av * acc;
             const float draw = s.raw > 20.f ? ddt : ddt * sigmoid_f(s.raw);
@@ -1353,7 +1373,6 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
         }
         phase();
         // dh before the chunk
-        const float left = eq < 0 ? __builtin_amdgcn_exp2f(hiq + loq) : 0.f;
 #pragma unroll
         for (int i = 0; i < SB; ++i)
 #pragma unroll
@@ -1378,15 +1397,6 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
                 for (int p = 0; p < PB; ++p) mma_p(fq, fd[p], dh1.v[i][p]);
             }
         }
-        float si = 0.f;
-#pragma unroll
-        for (int i = 0; i < SB; ++i)
-#pragma unroll
-            for (int p = 0; p < PB; ++p)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) si += hin.v[i][p][e] * dh1.v[i][p][e];
-        for (int o = 32; o; o >>= 1) si += __shfl_xor(si, o);
-        inner = si;
         __syncthreads();
         t_end -= cnt;
         if (slow) --slow;
@@ -1733,7 +1743,7 @@ static ScanArgs scan_args(const morlax_scan_dims& d) {
 static int64_t scan_blocks(const ScanArgs& g) { return cdiv(g.P, 32) * cdiv(g.S, 32); }
 int64_t scan_saved_bytes(const morlax_scan_dims& d) {
     const int64_t blocks = cdiv(d.head_dim, 32) * cdiv(d.state, 32);
-    return (int64_t)d.N * d.heads * (cdiv(d.T, MEM_Q) + 1) * blocks * 4096;
+    return (int64_t)d.N * d.heads * cdiv(d.T, MEM_Q) * blocks * 4096;
 }
 static int64_t scan_carve(ScanArgs& g, bool back, void* ws) {
     char* at = reinterpret_cast<char*>(ws);
