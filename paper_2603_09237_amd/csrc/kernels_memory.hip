@@ -778,7 +778,7 @@ struct ScanFwdLds {
     static constexpr int WAVE = X + 2 * N + (int)sizeof(StepLds);
 };
 
-// Bound by its reads and writes, half of them the states: 64 steps x 1024 environments x 8 heads of 64 x 64 bf16, 487 MB in 122 us, 4.0 TB/s.
+// Bound by its reads and writes, half of them the states: 64 steps x 1024 environments x 8 heads of 64 x 64 bf16, 487 MB in 120 us, 4.1 TB/s.
 // One wave a head keeps the state in registers over the whole segment.  Rounding: operands as bf16 parts (three in fp32 and where a state
 // follows; two, which leave out 2^-17, where only a bf16 y does), sums and states in fp32, y once.
 // LOCAL: only the state that a span of time leaves when nothing enters it, and what it leaves of a state that does.  (Where environments
@@ -988,10 +988,10 @@ __global__ __launch_bounds__(256) void k_scan_join(ScanArgs g) {
 // and for the decays' exponents, whose gradient at step i is the sum over the pairs (t, s) that it lies between,
 //   d(dt_i a) = sum_{s < i <= t} E (C_t . B_s) dt_s R[t, s] + sum_{t >= i} C_t . q_t h_in dy_t + sum_{s < i} dt_s B_s . u_s dh x_s + exp(l_31) <h_in, dh>,
 // the first sum as that over t >= i of what the pairs with earlier steps give less what those with later ones do: the pairs of two steps from i on
-// are in both.  (As sum_{t >= i} (C_t . dC_t - dt_t B_t . dB'_t) + <h_out, dh>, which costs no sums of its own, the pair of a step with itself and
-// what ends in h_out were taken once and taken off again: the error of a_log's gradient was ten times the plain form's in fp32.)
-// Half the environments of the forward's example: 322 us.  Bound by instructions and their waits: 58 million of the vector unit's (94 us of its
-// time) at one wave a SIMD, whose 498 registers and 37 KB of LDS leave no room for a second; 37 % of the cycles wait.
+// are in both.  (As sum_{t >= i} (C_t . dC_t - dt_t B_t . dB'_t) + <h_out, dh> the pair of a step with itself and what ends in h_out come in and
+// go out again: dt's gradient was 4.4e-7 off where it is 2.6e-7 now, and the last chunk's state had to be saved.)
+// Half the environments of the forward's example: 305 us.  Bound by instructions and their waits: 60 million of the vector unit's (98 us of its
+// time) at one wave a SIMD, whose 470 registers and 37 KB of LDS leave no room for a second; 34 % of the cycles wait.
 template <typename T, int PB, int SB>
 struct ScanBwdLds {
     static constexpr int NP = Planes<T>::N;
