@@ -104,7 +104,9 @@ def run_bwd(dims, d, only=None):
 SHAPES = [(1, 8, 8, 1, 1, "one", 0), (1, 64, 96, 16, 5, "mixed", 0), (3, 27, 50, 5, 6, "mixed", 1), (33, 64, 130, 8, 4, "grouped", 0),
           (64, 256, 320, 16, 64, "mixed", 8), (129, 40, 264, 32, 3, "mixed", 0), (257, 31, 33, 17, 300, "mixed", 3), (600, 136, 200, 31, 2, "one", 0),
           (1030, 512, 72, 4, 16, "grouped", 0), (515, 72, 512, 16, 7, "none", 0), (2100, 264, 392, 9, 130, "mixed", 0),
-          (4099, 27, 130, 5, 24, "mixed", 0), (16400, 264, 520, 16, 40, "grouped", 0), (16385, 200, 520, 12, 3, "mixed", 8), (9000, 520, 264, 24, 700, "mixed", 0)]
+          (4099, 27, 130, 5, 24, "mixed", 0), (16400, 264, 520, 16, 40, "grouped", 0), (16385, 200, 520, 12, 3, "mixed", 8), (9000, 520, 264, 24, 700, "mixed", 0),
+          (73, 264, 520, 4, 5, "mixed", 0), (15561, 264, 520, 7, 6, "grouped", 0), (4099, 520, 136, 8, 24, "mixed", 0), (8200, 530, 72, 5, 9, "mixed", 0),
+          (8300, 520, 136, 8, 24, "mixed", 0), (2500, 64, 2056, 6, 4, "mixed", 0)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
