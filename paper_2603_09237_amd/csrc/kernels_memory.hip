@@ -882,7 +882,7 @@ __global__ __launch_bounds__((ScanFwdLds<T, PB, SB>::NW * 64), 2) void k_scan_fw
         phase();
         // state to the chunk's end: what is left of the old one
         const float left = eq < 0 ? __builtin_amdgcn_exp2f(hiq + loq) : 0.f;
-        if (LOCAL) all *= left;
+        if (LOCAL) all = counted(all, left);  // (an episode's begin wins over an undefined step of another chunk)
 #pragma unroll
         for (int i = 0; i < SB; ++i)
 #pragma unroll
@@ -1471,7 +1471,7 @@ __global__ __launch_bounds__(256) void k_scan_bwd_local(ScanArgs g) {
         if (lane < 32) sl->w[lr] = s.e < 0 ? __builtin_amdgcn_exp2f(s.hi + s.lo) : 0.f;
         phase();
         const float left = eq < 0 ? __builtin_amdgcn_exp2f(hiq + loq) : 0.f;
-        all *= left;
+        all = counted(all, left);
 #pragma unroll
         for (int i = 0; i < SB; ++i)
 #pragma unroll

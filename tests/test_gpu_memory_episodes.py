@@ -1,0 +1,70 @@
+"""An undefined or infinite time step (dt) stays in its episode: what other episodes, heads and environments get is what they get without it,
+bit for bit, since no arithmetic of theirs takes part of it."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = 0, 1
+H, P, G, S = 3, 40, 1, 24
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def both(T, begins, where, value, dtype):
+    """(y, state, gradients) of a scan of two environments without and with dt[where, environment 0, head 1] = value."""
+    from test_gpu_memory import run_scan, run_scan_bwd, scan_problem
+    torch = _torch()
+    dims, h, d = scan_problem(T, 2, H, P, G, S, dtype, 0.0, True, seed=T + where)
+    d["first"] = torch.zeros(T, 2, dtype=torch.uint8, device="cuda")
+    for t in begins:
+        d["first"][t, 0] = 1
+    res = []
+    for v in (None, value):
+        if v is not None:
+            d["dt"][where, 0, 1] = v
+        y, out, saved = run_scan(dims, d, saved=True)
+        y, out = y.clone(), out.clone()
+        res.append((y, out, {k: g.clone() for k, g in run_scan_bwd(dims, d, saved).items()}))
+    return res
+
+
+def episode(T, begins, where):
+    """first step of the episode that `where` is in, and the first of the next one"""
+    edges = [0, *begins, T]
+    i = max(i for i, e in enumerate(edges) if e <= where)
+    return edges[i], edges[i + 1]
+
+
+def apart(T, begins, where, value, dtype):
+    torch = _torch()
+    (y0, out0, g0), (y, out, g) = both(T, begins, where, value, dtype)
+    e0, e1 = episode(T, begins, where)
+    heads = lambda v, n: v.reshape(*v.shape[:2], H, n)  # noqa: E731
+    ok = torch.ones(T, 2, H, dtype=torch.bool, device="cuda")
+    ok[where:e1, 0, 1] = False
+    assert torch.equal(heads(y, P)[ok], heads(y0, P)[ok])
+    assert not torch.isfinite(heads(y, P)[where, 0, 1]).all()
+    ends = torch.ones(2, H, dtype=torch.bool, device="cuda")
+    ends[0, 1] = e1 < T
+    assert torch.equal(out[ends], out0[ends])
+    ok[e0:e1, 0] = False        # (dB and dC are sums over the heads)
+    for k in ("xbc", "z", "dt"):
+        a, b = g[k][ok.all(-1)], g0[k][ok.all(-1)]
+        assert torch.isfinite(b).all() and torch.equal(a, b), k
+    mine = torch.ones(2, H, dtype=torch.bool, device="cuda")
+    mine[0, 1] = e0 > 0
+    assert torch.equal(g["state"][mine], g0["state"][mine])
+    for k in ("a_log", "d", "bias"):
+        assert torch.equal(g[k][[0, 2]], g0[k][[0, 2]]), k
+
+
+# 400 steps are several spans of 96 steps; the begin in another chunk of 32 steps than the step, of the same span or not
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("T,begins,where", [(400, (45,), 25), (400, (45,), 70), (400, (10, 120), 70), (400, (110,), 170), (400, (5, 390), 200),
+                                            (90, (45,), 25), (90, (45,), 70)])
+def test_a_step_in_another_chunk(T, begins, where, value, dtype):
+    apart(T, begins, where, value, dtype)
