@@ -987,9 +987,9 @@ __global__ __launch_bounds__(256) void k_scan_join(ScanArgs g) {
 //   dx_s = dt_s (sum_t E (C_t . B_s) dy_t + u_s dh^T B_s) + D dy_s,   dh_in = exp(l_31) dh + sum_t q_t C_t dy_t^T,
 // and for the decays' exponents, whose gradient at step i is the sum over the pairs (t, s) that it lies between,
 //   d(dt_i a) = sum_{s < i <= t} E (C_t . B_s) dt_s R[t, s] + sum_{t >= i} C_t . q_t h_in dy_t + sum_{s < i} dt_s B_s . u_s dh x_s + exp(l_31) <h_in, dh>,
-// the first sum as that over t >= i of what the pairs with earlier steps give less what those with later ones do: the pairs of two steps from i on
-// are in both.  (As sum_{t >= i} (C_t . dC_t - dt_t B_t . dB'_t) + <h_out, dh> the pair of a step with itself and what ends in h_out come in and
-// go out again: dt's gradient was 4.4e-7 off where it is 2.6e-7 now, and the last chunk's state had to be saved.)
+// the first sum as a product of the pairs with a triangle of ones over t, then those s of i's own episode: every term is there once and nothing
+// is taken away again.  (As a sum over t >= i of what the pairs with earlier steps give less what those with later ones do, all pairs of later steps
+// come in and go out again: what they round to, and a step of a later episode that is undefined, stayed in the earlier steps' gradients.)
 // Half the environments of the forward's example: 305 us.  Bound by instructions and their waits: 60 million of the vector unit's (98 us of its
 // time) at one wave a SIMD, whose 470 registers and 37 KB of LDS leave no room for a second; 34 % of the cycles wait.
 template <typename T, int PB, int SB>
@@ -1123,10 +1123,9 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
             mma_p<true>(fd, ox, r2);
         }
         phase();
-        // row_s, col_s: the sums over earlier steps of E scores R dt, over later ones of E scores R; self: the pair of a step with itself
-        float row_s = 0.f, col_s = 0.f, self = 0.f;
-        // m1: scores that give y [s | t]; v1: E R dt_s [s | t]; g2: E scores [t | s]; r2: E R [t | s]
-        float16_t m1;
+        float col_tot = 0.f;  // B_s . dB'_s: the sum over the step and later ones of E scores R, and end_tot below
+        // m1: scores that give y [s | t]; r1: E R dt_s [s | t]; g2: E scores [t | s]; r2: E R [t | s]; pairs: E scores R dt_s [t | s]
+        float16_t m1, pairs;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             const int r = acc_row(e, lg);
@@ -1135,13 +1134,36 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
             const bool on1 = r <= lr && r >= s.e, on2 = r >= lr && lr >= re;
             const float d1 = on1 ? decay(s.hi, s.lo, rhi, rlo) * rdt : 0.f, d2 = on2 ? decay(rhi, rlo, s.hi, s.lo) : 0.f;
             m1[e] = counted(g1[e], d1);
-            row_s += r != lr ? counted(r1[e], m1[e]) : 0.f;
             r1[e] = counted(r1[e], d1);
             g2[e] = counted(g2[e], d2);
             const float pair = counted(r2[e], g2[e]);
-            col_s += r != lr ? pair : 0.f;
-            self += r != lr ? 0.f : pair;
+            col_tot += pair;
+            pairs[e] = counted(pair, s.dt);
             r2[e] = counted(r2[e], d2);
+        }
+        float between = 0.f;  // the pairs of an earlier step with this or a later one: pairs [s | i] summed over t >= i, then over s < i
+        {
+            float16_t o;
+            zero(o);
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk) {
+                uint4 fp[3];
+                uint32_t w[4];  // ones where the contraction's step is i or later
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int t2 = acc_row(8 * kk + 2 * k, lg);
+                    w[k] = (t2 >= lr ? 0x3f80u : 0u) | (t2 + 1 >= lr ? 0x3f800000u : 0u);
+                }
+                const uint4 ones = make_uint4(w[0], w[1], w[2], w[3]);
+                acc_parts(pairs, kk, fp);
+#pragma unroll
+                for (int q = 2; q >= 0; --q) Mma32<bf16_t>::run(fp[q], ones, o);
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int r = acc_row(e, lg);
+                between += r < lr && r >= s.e ? o[e] : 0.f;
+            }
         }
         phase();
         // dz needs y again
@@ -1346,12 +1368,13 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
         }
         // gradients of the steps
         {
-            // later steps: pairs with two of them are in row_s and in col_s, with the same bits, or nearly
-            float acc = row_s - s.dt * col_s + state_tot, col_tot = self + col_s + end_tot;  // col_tot: B_s . dB'_s
+            float acc = state_tot;
+            col_tot += end_tot;
             acc += __shfl_xor(acc, 32);
+            between += __shfl_xor(between, 32);
             col_tot += __shfl_xor(col_tot, 32);
             end_tot += __shfl_xor(end_tot, 32);
-            float before = s.dt * end_tot;
+            float before = lr >= eq ? s.dt * end_tot : 0.f;  // (a select: a step of an episode that ends in the chunk may be undefined)
             if (lr >= cnt) acc = before = 0.f;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -1361,7 +1384,7 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
             }
             before = __shfl_up(before, 1, 32);
             if (lr > 0) acc += before;
-            acc += counted(through, left);
+            acc += between + counted(through, left);
             if (s.begins) acc = 0.f;
             const float ddt = col_tot + av * acc;
             const float draw = s.raw > 20.f ? ddt : ddt * sigmoid_f(s.raw);

@@ -68,3 +68,32 @@ def apart(T, begins, where, value, dtype):
                                             (90, (45,), 25), (90, (45,), 70)])
 def test_a_step_in_another_chunk(T, begins, where, value, dtype):
     apart(T, begins, where, value, dtype)
+
+
+# begin and step within the same 32 steps, on either side, with other begins about them; the begin itself; one chunk, several, several spans
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("T,begins,where", [(20, (9,), 14), (20, (9,), 4), (20, (9,), 9), (32, (3, 16, 29), 20), (90, (40, 50), 45), (90, (40,), 35),
+                                            (400, (110, 150), 98), (400, (110,), 98), (400, (105,), 111), (400, (200, 210, 220), 215)])
+def test_a_step_in_the_same_chunk(T, begins, where, value, dtype):
+    apart(T, begins, where, value, dtype)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T,begin", [(20, 9), (90, 50), (400, 110)])
+@pytest.mark.parametrize("scale", [2.0 ** 20, 2.0 ** 60, 2.0 ** 110])   # the last: sums within the later episode overflow
+def test_gradients_of_a_later_episode_leave_nothing_behind(T, begin, scale, dtype):
+    """Large gradients behind a begin change no bit of those before it."""
+    from test_gpu_memory import run_scan, run_scan_bwd, scan_problem
+    torch = _torch()
+    dims, h, d = scan_problem(T, 2, H, P, G, S, dtype, 0.0, True, seed=T)
+    d["first"] = torch.zeros(T, 2, dtype=torch.uint8, device="cuda")
+    d["first"][begin, 0] = 1
+    _, _, saved = run_scan(dims, d, saved=True)
+    want = {k: v.clone() for k, v in run_scan_bwd(dims, d, saved).items()}
+    d["dy"][begin:, 0] *= scale
+    got = run_scan_bwd(dims, d, saved)
+    for k in ("xbc", "z", "dt"):
+        assert torch.equal(got[k][:begin, 0], want[k][:begin, 0]), k
+        assert torch.equal(got[k][:, 1], want[k][:, 1]), k
+    assert torch.equal(got["state"], want["state"])
