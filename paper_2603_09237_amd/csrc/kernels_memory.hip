@@ -417,6 +417,20 @@ __device__ inline void mma_p(const uint4 (&a)[NA], const uint4 (&b)[NB], float16
             if (i < NA && s - i < NB) Mma32<bf16_t>::run(a[i], b[s - i], c);
         }
 }
+// The same with all but the leading product in a sum of their own.  A matrix instruction cuts what lies below its sum's last place, towards the
+// lower value: six on one sum left it lower by a tenth of its rounding errors' size, always, and a sum over all steps of such values, as the
+// decays' gradient is, kept it: da_log's error was 2.7 to 2.9 times the present one.
+template <bool MIRROR = false, int NA, int NB>
+__device__ inline void mma_p2(const uint4 (&a)[NA], const uint4 (&b)[NB], float16_t& c, float16_t& low) {
+#pragma unroll
+    for (int s = (NA + NB - 2 < 2 ? NA + NB - 2 : 2); s >= 1; --s)
+#pragma unroll
+        for (int k = 0; k <= s; ++k) {
+            const int i = MIRROR ? s - k : k;
+            if (i < NA && s - i < NB) Mma32<bf16_t>::run(a[i], b[s - i], low);
+        }
+    Mma32<bf16_t>::run(a[0], b[0], c);
+}
 __device__ inline void zero(float16_t& c) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) c[e] = 0.f;
@@ -1004,6 +1018,7 @@ struct ScanBwdLds {
 template <typename T, int PB, int SB>
 __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(ScanArgs g) {
     typedef ScanBwdLds<T, PB, SB> L;
+    constexpr bool FOLD = sizeof(T) == 4 && PB * SB == 4;  // no registers for both blocks' small products: 256 environments fp32 64 x 64 501 us, else 530
     constexpr int NP = L::NP, NW = L::NW, RP = 32 * SB + 4, NY = sizeof(T) == 4 ? 3 : 2;  // NY: parts of what only dz and dx see
     extern __shared__ __align__(16) unsigned char lds[];
     const int wave = wave_index(), lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5;
@@ -1104,8 +1119,8 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
         phase();
         phase();
         // scores and dy . x in both layouts: [s | t] (lane: the later step) and [t | s] (lane: the earlier one)
-        float16_t g1, g2, r1, r2;
-        zero(g1); zero(g2); zero(r1); zero(r2);
+        float16_t g1, g2, r1, r2, l1, l2;
+        zero(g1); zero(g2); zero(r1); zero(r2); zero(l1); zero(l2);
 #pragma unroll
         for (int kk = 0; kk < 2 * SB; ++kk) {
             uint4 ob[NP], oc[NP];
@@ -1119,8 +1134,8 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
             uint4 ox[NP], fd[3];
             X.rows(kk, ox);
             D.rows(kk, fd);
-            mma_p(ox, fd, r1);
-            mma_p<true>(fd, ox, r2);
+            mma_p2(ox, fd, r1, l1);
+            mma_p2<true>(fd, ox, r2, l2);
         }
         phase();
         float col_tot = 0.f;  // B_s . dB'_s: the sum over the step and later ones of E scores R, and end_tot below
@@ -1129,6 +1144,8 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             const int r = acc_row(e, lg);
+            r1[e] += l1[e];
+            r2[e] += l2[e];
             const float rhi = sl->hi[r], rlo = sl->lo[r], rdt = sl->dt[r];
             const int re = sl->e[r];
             const bool on1 = r <= lr && r >= s.e, on2 = r >= lr && lr >= re;
@@ -1276,9 +1293,12 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
         float state_tot = 0.f, end_tot = 0.f;  // C_t . q_t h_in dy_t, B_s . u_s dh x_s
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
-            float16_t o[SB];
+            float16_t o[SB], low[SB];
 #pragma unroll
-            for (int i = 0; i < SB; ++i) zero(o[i]);
+            for (int i = 0; i < SB; ++i) {
+                zero(o[i]);
+                zero(low[i]);
+            }
             // contraction over p: h_in dy_t, dh x_s; both have p in their lanes, their blocks are turned in LDS
 #pragma unroll
             for (int p = 0; p < PB; ++p) {
@@ -1299,8 +1319,13 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
                         uint4 fh[3];
                         eight(red + lr * 36, kk, v);
                         split3(v, fh);
-                        if (which) mma_p(fh, ox[kk], o[i]);
-                        else mma_p(fh, od[kk], o[i]);
+                        if (which) mma_p2(fh, ox[kk], o[i], low[i]);
+                        else mma_p2(fh, od[kk], o[i], low[i]);
+                    }
+                    if (FOLD) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) o[i][e] += low[i][e];
+                        zero(low[i]);
                     }
                     phase();
                 }
@@ -1310,7 +1335,7 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
 #pragma unroll
             for (int i = 0; i < SB; ++i)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) o[i][e] = counted(o[i][e], lane_scale);
+                for (int e = 0; e < 16; ++e) o[i][e] = counted(FOLD ? o[i][e] : o[i][e] + low[i][e], lane_scale);
             {
                 float tot = 0.f;
 #pragma unroll
