@@ -11,6 +11,7 @@
 // Every operand that is computed here (states, decays times scores) is fp32 and enters a product as bf16 parts (split3): the results are
 // fp32 ones, rounded once where they are stored as bf16.
 #include "mlp_device.h"
+#include "memory_shape.h"
 
 typedef short short4_t __attribute__((ext_vector_type(4)));
 
@@ -1592,6 +1593,7 @@ struct StepArgs {
     const float *conv_w, *conv_b;
     void* conv_out;
     int width;
+    StepLayout lay;
 };
 // A wave takes a head of an environment, or one of `parts` equal runs of its channels where there are few heads in all (each computes the
 // head's B and C for itself).  The convolution's outputs stay in fp32 in LDS; a row of the state (the state values of one channel) is shared
@@ -1601,16 +1603,16 @@ struct StepArgs {
 #define STEP_U 4
 template <typename T>
 __global__ __launch_bounds__(256) void k_memory_step(StepArgs a, int lpr, int vec, int parts) {
-    extern __shared__ float slds[];
+    extern __shared__ __align__(16) float slds[];
     const ScanArgs& g = a.s;
     const int wave = wave_index(), lane = threadIdx.x & 63;
     const int64_t unit = (int64_t)blockIdx.x * 4 + wave;
     if (unit >= (int64_t)g.N * g.H * parts) return;
     const int64_t id = unit / parts;
-    const int each = (g.P + parts - 1) / parts, q0 = (int)(unit % parts) * each, q1 = q0 + each < g.P ? q0 + each : g.P;  // its channels
+    const int each = a.lay.each, q0 = (int)(unit % parts) * each, q1 = q0 + each < g.P ? q0 + each : g.P;  // its channels
     const int n = (int)(id / g.H), h = (int)(id % g.H), rep = g.H / g.G, grp = h / rep, D = g.H * g.P;
     const int chans = D + 2 * g.G * g.S, before = a.width - 1, np = q1 > q0 ? q1 - q0 : 0;
-    float* xs = slds + wave * (g.P + 2 * g.S);
+    float *xs = slds + wave * a.lay.wave, *bs = xs + a.lay.b, *cs = xs + a.lay.c;
     const bool begins = g.first && g.first[n];
     const T* row = reinterpret_cast<const T*>(a.xbc) + (int64_t)n * g.x_n;
     const T* old = reinterpret_cast<const T*>(a.conv_in) + (int64_t)n * before * chans;
@@ -1636,7 +1638,7 @@ __global__ __launch_bounds__(256) void k_memory_step(StepArgs a, int lpr, int ve
             if (k == before || (k < before && !begins)) v += w[k] * to_f(in[k]);
             if (k > 0 && k < a.width && mine && a.conv_out) kept[(int64_t)(k - 1) * chans + c] = in[k];
         }
-        xs[i] = silu_f(v);
+        (i < np ? xs + i : i < np + g.S ? bs + (i - np) : cs + (i - np - g.S))[0] = silu_f(v);
     }
     __builtin_amdgcn_wave_barrier();
     const float raw = to_f(reinterpret_cast<const T*>(g.dt)[(int64_t)n * g.dt_n + h]) + (g.dt_bias ? g.dt_bias[h] : 0.f);
@@ -1645,7 +1647,6 @@ __global__ __launch_bounds__(256) void k_memory_step(StepArgs a, int lpr, int ve
     const bool have = g.state_in && !begins;
     const float* hi = have ? g.state_in + (id * g.P + q0) * g.S : g.state_out;  // (never read where there is none)
     float* ho = g.state_out + (id * g.P + q0) * g.S;
-    const float *bs = xs + np, *cs = bs + g.S;
     const int sub = lane % lpr, rows = 64 / lpr;
     const T* z = reinterpret_cast<const T*>(g.z) + (int64_t)n * g.z_n + (int64_t)h * g.P + q0;
     T* yo = reinterpret_cast<T*>(g.y) + (int64_t)n * g.y_n + (int64_t)h * g.P + q0;
@@ -1895,8 +1896,9 @@ void launch_memory_step(const morlax_scan_dims& d, int width, const void* xbc, c
     const int vec = g.S % 4 == 0;
     int lpr = 1;
     while (lpr < 64 && lpr * (vec ? 4 : 1) < g.S) lpr *= 2;
-    const int lds = 4 * (g.P + 2 * g.S) * 4;
     const int parts = (int64_t)g.N * g.H <= 1536 && g.P >= 4 ? 4 : 1;  // a wave for every SIMD, or nearly
+    a.lay = step_layout(g.P, g.S, parts);
+    const int lds = 4 * a.lay.wave * (int)sizeof(float);
     const int64_t blocks = cdiv((int64_t)g.N * g.H * parts, 4);
     if (d.dtype) k_memory_step<bf16_t><<<blocks, 256, lds, s>>>(a, lpr, vec, parts);
     else k_memory_step<float><<<blocks, 256, lds, s>>>(a, lpr, vec, parts);
