@@ -1612,7 +1612,7 @@ __global__ __launch_bounds__(256) void k_memory_step(StepArgs a, int lpr, int ve
     const int each = a.lay.each, q0 = (int)(unit % parts) * each, q1 = q0 + each < g.P ? q0 + each : g.P;  // its channels
     const int n = (int)(id / g.H), h = (int)(id % g.H), rep = g.H / g.G, grp = h / rep, D = g.H * g.P;
     const int chans = D + 2 * g.G * g.S, before = a.width - 1, np = q1 > q0 ? q1 - q0 : 0;
-    float *xs = slds + wave * a.lay.wave, *bs = xs + a.lay.b, *cs = xs + a.lay.c;
+    float *bs = slds + wave * a.lay.wave + a.lay.b, *cs = bs + g.S, *xs = bs - np;  // one run of values
     const bool begins = g.first && g.first[n];
     const T* row = reinterpret_cast<const T*>(a.xbc) + (int64_t)n * g.x_n;
     const T* old = reinterpret_cast<const T*>(a.conv_in) + (int64_t)n * before * chans;
@@ -1638,7 +1638,7 @@ __global__ __launch_bounds__(256) void k_memory_step(StepArgs a, int lpr, int ve
             if (k == before || (k < before && !begins)) v += w[k] * to_f(in[k]);
             if (k > 0 && k < a.width && mine && a.conv_out) kept[(int64_t)(k - 1) * chans + c] = in[k];
         }
-        (i < np ? xs + i : i < np + g.S ? bs + (i - np) : cs + (i - np - g.S))[0] = silu_f(v);
+        xs[i] = silu_f(v);
     }
     __builtin_amdgcn_wave_barrier();
     const float raw = to_f(reinterpret_cast<const T*>(g.dt)[(int64_t)n * g.dt_n + h]) + (g.dt_bias ? g.dt_bias[h] : 0.f);
