@@ -209,7 +209,8 @@ __global__ __launch_bounds__(256) void k_conv_bwd(ConvArgs g, int cols, int rows
     if (live) {
         Taps<T, V> a;
         a.init(g, c);
-        for (int n = blockIdx.y * rows + row; n < g.N; n += gridDim.y * rows) {
+        for (uint32_t at = blockIdx.y * rows + row; at < (uint32_t)g.N; at += gridDim.y * rows) {  // (N may be next to 2^31)
+            const int n = (int)at;
             const T* x = reinterpret_cast<const T*>(g.x) + (int64_t)n * g.x_n + c;
             const T* dy = reinterpret_cast<const T*>(g.dy) + (int64_t)n * g.y_n + c;
             T* dx = reinterpret_cast<T*>(g.dx) + (int64_t)n * g.x_n + c;
