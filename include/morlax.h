@@ -326,7 +326,7 @@ int morlax_conv_bwd(const morlax_conv_dims* dims, const void* x, const float* w,
  * fp32 whatever the type, y is rounded once.  An infinite or undefined input makes what depends on it infinite or undefined (not
  * always the one that step-by-step arithmetic would give).  saved: morlax_scan_saved_bytes() bytes that the backward needs, or NULL.
  * Limits: T, N, heads, groups, state, head_dim >= 1, groups | heads, heads <= 65536, N * heads < 2^25,
- * head_dim <= 64, state <= 64. */
+ * head_dim <= 64, state <= 64; of the backward, its workspace and `saved` also N * groups * ceil(heads / groups / 4) < 2^24 for bf16. */
 typedef struct {
     int32_t T, N, heads, head_dim, groups, state;
     int32_t dtype;

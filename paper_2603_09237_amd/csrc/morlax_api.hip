@@ -617,6 +617,14 @@ static int check_scan(const morlax_scan_dims* d, const char* who) {
         return fail(MORLAX_ERR_SHAPE, "%s: a stride between time steps is shorter than a row", who);
     return MORLAX_OK;
 }
+// the backward takes a workgroup per environment, group and block of the group's heads (two of them fp32, which N * heads bounds already)
+static int check_scan_back(const morlax_scan_dims* d, const char* who) {
+    const int rc = check_scan(d, who);
+    if (rc != MORLAX_OK) return rc;
+    if (d->dtype && (int64_t)d->N * d->groups * ((d->heads / d->groups + 3) / 4) >= (int64_t)1 << 24)  // 256 threads each
+        return fail(MORLAX_ERR_UNSUPPORTED, "%s: N * groups * ceil(heads / groups / 4) must stay below 2^24", who);
+    return MORLAX_OK;
+}
 static int check_gate(const morlax_scan_dims* d, const void* z, const char* who) {
     if (!z) return MORLAX_OK;
     const int64_t D = (int64_t)d->heads * d->head_dim;
@@ -624,11 +632,12 @@ static int check_gate(const morlax_scan_dims* d, const void* z, const char* who)
     return strided(z, d->dtype, "z", who);
 }
 extern "C" int64_t morlax_scan_saved_bytes(const morlax_scan_dims* d) {
-    if (check_scan(d, "morlax_scan_saved_bytes") != MORLAX_OK) return -1;
+    if (check_scan_back(d, "morlax_scan_saved_bytes") != MORLAX_OK) return -1;
     return scan_saved_bytes(*d);
 }
 extern "C" int64_t morlax_scan_workspace_bytes(const morlax_scan_dims* d, int32_t backward) {
-    if (check_scan(d, "morlax_scan_workspace_bytes") != MORLAX_OK) return -1;
+    const char* who = "morlax_scan_workspace_bytes";
+    if ((backward ? check_scan_back(d, who) : check_scan(d, who)) != MORLAX_OK) return -1;
     return scan_ws_bytes(*d, backward != 0);
 }
 extern "C" int morlax_scan_fwd(const morlax_scan_dims* dims, const void* x, const void* b, const void* c, const void* dt, const void* z,
@@ -653,7 +662,7 @@ extern "C" int morlax_scan_bwd(const morlax_scan_dims* dims, const void* x, cons
                                float* da_log, float* dd_skip, float* ddt_bias, float* dstate_in, void* ws, int64_t ws_bytes,
                                void* stream) {
     const char* who = "morlax_scan_bwd";
-    int rc = check_scan(dims, who);
+    int rc = check_scan_back(dims, who);
     if (rc != MORLAX_OK) return rc;
     STRIDED(x, dims->dtype, who); STRIDED(b, dims->dtype, who); STRIDED(c, dims->dtype, who); STRIDED(dt, dims->dtype, who);
     STRIDED(dy, dims->dtype, who); STRIDED(dx, dims->dtype, who); STRIDED(db, dims->dtype, who); STRIDED(dc, dims->dtype, who);
