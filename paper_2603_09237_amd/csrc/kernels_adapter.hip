@@ -1077,10 +1077,12 @@ __global__ __launch_bounds__(1024) void k_ad_plan(AdArgs g) {
 
 // The gradients of the factors and of the bias, one piece of sorted rows and 128 columns of dy (role 0: dA, dbias) or x (role 1:
 // dB) a workgroup: out[c][j] = sum_m src[m][c] w[m][j] with w = u or v in three bf16 parts; a column of ones beside u's gives dbias.
+// The parts of an infinite value add up to an undefined one, as do its products with the zeros beside the one of the column of ones: sums that are
+// not finite are taken again on the fp32 instructions, from memory.
 // Bound by its reads, dy and x once more, and their way through LDS: 32768 x (1160 + 512) bf16, 110 MB, 37 us (2.9 TB/s).
 // Piece c of the sorted rows: segment p and block b = c - p of AD_PIECE rows, p the last one with seg[p] / AD_PIECE + p <= c.
 template <typename T, int JB>
-__global__ __launch_bounds__(256) void k_ad_factor_grad(AdArgs g, int col_blocks_y) {
+__global__ __launch_bounds__(256, sizeof(T) == 4 ? 5 - JB : 8 - 2 * JB) void k_ad_factor_grad(AdArgs g, int col_blocks_y) {
     constexpr int NP = sizeof(T) == 4 ? 3 : 1;
     constexpr int SP = 32 * 320;                 // a plane of 32 rows x 128 columns
     constexpr int WP = (JB * 32) * 2 + 16;       // bytes of a row of w
@@ -1110,6 +1112,7 @@ __global__ __launch_bounds__(256) void k_ad_factor_grad(AdArgs g, int col_blocks
     const T* base = reinterpret_cast<const T*>(is_y ? g.dy : g.x);
     const int64_t ld = is_y ? g.ld_y : g.ld_x;
     const float* w = is_y ? g.u : g.v;
+    const bool weighed = p < g.P && (is_y ? g.dA : g.dB);  // (u is not there where dA is not asked for)
     const bool vec = ((reinterpret_cast<uintptr_t>(base) | (uintptr_t)(ld * (int64_t)sizeof(T))) & 15) == 0;
     float16_t acc[JB];
 #pragma unroll
@@ -1127,7 +1130,7 @@ __global__ __launch_bounds__(256) void k_ad_factor_grad(AdArgs g, int col_blocks
             const int j = 32 * jj + 4 * (tid % 8);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                wt[jj][i] = m < 0 ? 0.f : j + i < g.r ? (p < g.P ? w[(int64_t)(s + row) * g.rp + j + i] : 0.f) : j + i == g.r ? 1.f : 0.f;
+                wt[jj][i] = m < 0 ? 0.f : j + i < g.r ? (weighed ? w[(int64_t)(s + row) * g.rp + j + i] : 0.f) : j + i == g.r ? 1.f : 0.f;
         }
     };
     int next = place(s0);
@@ -1190,6 +1193,22 @@ __global__ __launch_bounds__(256) void k_ad_factor_grad(AdArgs g, int col_blocks
         __syncthreads();
     }
     const int col = c0 + 32 * wave + lr;
+#pragma unroll
+    for (int j = 0; j < JB; ++j)
+        if (any_undefined(acc[j])) {
+            const int jj = 32 * j + lr;
+            float16_t t = zero16();
+#pragma unroll 1
+            for (int s = s0 + lg; s < s1 + lg; s += 2) {
+                const bool on = s < s1;
+                const float wv = !on ? 0.f : jj < g.r ? (weighed ? w[(int64_t)s * g.rp + jj] : 0.f) : jj == g.r ? 1.f : 0.f;
+                const float sv = on && col < C ? to_f(base[(int64_t)g.perm[s] * ld + col]) : 0.f;
+                t = __builtin_amdgcn_mfma_f32_32x32x2f32(wv, sv, t, 0, 0, 0);
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (!(__builtin_fabsf(acc[j][e]) < __builtin_inff())) acc[j][e] = t[e];
+        }
     if (col >= C) return;
     float* out = is_y ? g.dA : g.dB;
     if (out && !whole) out = is_y ? g.pA : g.pB;
