@@ -179,8 +179,9 @@ struct AdFactor {
 // of the block per adapter among its rows, which goes to its own rows' lanes only -- so an undefined factor of one adapter stays out of
 // the others' rows, and a row's result does not depend on whose rows lie beside it.  The next adapter's factors are requested before
 // this one's product (one after the other, 64 rows with an adapter each waited 32 times for memory: 116 us a launch of 64 x 2048 x 2048).
-// bf16: u as two bf16 parts (what is left out is 2^-17 of it; rounding it to one would double the error of y); fp32 on the fp32
-// instructions.
+// bf16: u as two bf16 parts, the leading one cut, so that both have its sign, and the second never zero where u is not: an infinite factor's
+// two products are then both what its product with u is.  What is left out is 2^-16 of u (rounding u to one part would double the error of y);
+// fp32 on the fp32 instructions.
 template <typename T, bool BWD, int RP>
 struct AdExpand {
     static constexpr bool BF = sizeof(T) == 2;
@@ -219,12 +220,14 @@ struct AdExpand {
             for (int s = 0; s < K16; ++s) {
                 const float4 a = *reinterpret_cast<const float4*>(um + 16 * s + 8 * lg), b = *reinterpret_cast<const float4*>(um + 16 * s + 8 * lg + 4);
                 float t[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}, l[8];
-                hi[s] = pack_chunk<bf16_t>(t);
-                const uint32_t w[4] = {hi[s].x, hi[s].y, hi[s].z, hi[s].w};
+                uint32_t w[4];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {  // (an infinite value has no second part)
-                    const float d = t[i] - __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
-                    l[i] = __builtin_fabsf(d) < __builtin_inff() ? d : 0.f;
+                for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_perm(__float_as_uint(t[2 * i + 1]), __float_as_uint(t[2 * i]), 0x07060302);
+                hi[s] = make_uint4(w[0], w[1], w[2], w[3]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float d = t[i] - __uint_as_float(__float_as_uint(t[i]) & 0xffff0000u);
+                    l[i] = __builtin_amdgcn_classf(d, 0x267) ? t[i] * 0x1p-20f : d;  // (zero, or t infinite or undefined)
                 }
                 lo[s] = pack_chunk<bf16_t>(l);
             }

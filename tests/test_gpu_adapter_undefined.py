@@ -66,3 +66,10 @@ def where_they_go(M, I, O, r, P, mix, value, dtype, outputs):
 @pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
 def test_in_sums_over_the_rows(M, I, O, r, P, mix, value, dtype):
     where_they_go(M, I, O, r, P, mix, value, dtype, SUMS)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("M,I,O,r,P,mix", SIZES)
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+def test_in_rows(M, I, O, r, P, mix, value, dtype):
+    where_they_go(M, I, O, r, P, mix, value, dtype, ("y", "dx"))
