@@ -272,7 +272,9 @@ int morlax_pareto_hypervolume(const float* J, const float* ref, int32_t n, int32
  *   y[m] = W0 x[m] + bias + A[p] (B[p] x[m]),  p = index[m]
  *   x [rows, d_in] (row stride ld_x elements), w0 [d_out, d_in], bias [d_out] fp32 or NULL, A [n_adapters, d_out, rank],
  *   B [n_adapters, rank, d_in], index [rows] int32, y [rows, d_out] (row stride ld_y); x, w0, A, B, y of the given type.
- * B[p] x[m] is kept in fp32.  The result of a row depends on its own x and its own adapter alone.
+ * B[p] x[m] is kept in fp32.  The result of a row depends on its own x and its own adapter alone, up to rounding: the order of its sums goes by
+ * the sizes of the call and, where the rows' factors (a copy a row) are more than 64 MB, by whether more than four adapters are among the
+ * 32 rows that it lies with.
  * Limits: 1 <= rank <= 32, 1 <= d_in, d_out <= 65536, 1 <= n_adapters <= 2^20, rows <= 2^28 and fewer than 2^24 tiles of 128 rows by
  * 128 columns. */
 typedef struct {

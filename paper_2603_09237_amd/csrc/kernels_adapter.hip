@@ -177,7 +177,7 @@ struct AdFactor {
 
 // The adapters' part of a wave's 32 x 64 outputs, a lane holding row m0 + lr (accumulator: columns n0 + 8 (e / 4) + 4 lg + e % 4): one product
 // of the block per adapter among its rows, which goes to its own rows' lanes only -- so an undefined factor of one adapter stays out of
-// the others' rows, and a row's result does not depend on whose rows lie beside it.  The next adapter's factors are requested before
+// the others' rows, and these bits of a row do not depend on whose rows lie beside it.  The next adapter's factors are requested before
 // this one's product (one after the other, 64 rows with an adapter each waited 32 times for memory: 116 us a launch of 64 x 2048 x 2048).
 // bf16: u as two bf16 parts, the leading one cut, so that both have its sign, and the second never zero where u is not: an infinite factor's
 // two products are then both what its product with u is.  What is left out is 2^-16 of u (rounding u to one part would double the error of y);
@@ -886,7 +886,9 @@ __device__ inline void shrink_staged(const bf16_t* f, const bf16_t* const (&rows
 }
 
 // adapters among 32 rows beyond which these are taken one by one.  us of the forward, rows mixed: 2048 x 1160 x 1160 fp32 of 8 adapters 146
-// one by one, 292 adapter by adapter; 16384 x 512 x 1160 bf16 of 128 142 and 162; of 4 adapters 57 and 56 (above four are one by one)
+// one by one, 292 adapter by adapter; 16384 x 512 x 1160 bf16 of 128 142 and 162; of 4 adapters 57 and 56 (above four are one by one).  The two
+// add up a row's products in different orders: its u has other last bits among other rows, which the header says.  One order for both costs more
+// than it gives: fp32 one by one throughout 237 -> 263 for 16384 x 512 x 1160 grouped, and 78 -> 207 for 8192 x 512 x 512 of rank 32.
 #define AD_ONE_BY_ONE 4
 // Many rows: 32 a workgroup, its four waves a quarter of the contraction each, one pass over the rows per adapter among them.  bf16 on
 // 32x32x16, fp32 on 32x32x2 (the factor's 32 rows are at most `rank` real ones; the pass is bound by its reads).  The backward's factor,
