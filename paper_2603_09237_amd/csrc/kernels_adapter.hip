@@ -27,7 +27,7 @@ struct AdArgs {
     // scratch
     float *u, *v;        // [M][rp]
     int32_t *seg, *perm; // [P + 2], [M]
-    float *pw, *pA, *pB, *pb;  // partial sums: [split][O][I], [piece][O][r], [piece][r][I], [piece][O]
+    float *pw, *pA, *pB, *pb;  // partial sums: [split][O][I], [slot][O][r], [slot][r][I], [piece][O]
     const int32_t* order;  // perm where rows are taken sorted by adapter (u and v are then in that order), or NULL: as they lie
     int rp, split, kchunk, pieces, bf16;
     __device__ inline int row(int s) const { return order ? order[s] : s; }
@@ -1085,7 +1085,10 @@ __global__ __launch_bounds__(1024) void k_ad_plan(AdArgs g) {
 // The parts of an infinite value add up to an undefined one, as do its products with the zeros beside the one of the column of ones: sums that are
 // not finite are taken again on the fp32 instructions, from memory.
 // Bound by its reads, dy and x once more, and their way through LDS: 32768 x (1160 + 512) bf16, 110 MB, 37 us (2.9 TB/s).
-// Piece c of the sorted rows: segment p and block b = c - p of AD_PIECE rows, p the last one with seg[p] / AD_PIECE + p <= c.
+// Piece c of the sorted rows: segment p and block b = c - p of AD_PIECE rows, p the last one with seg[p] / AD_PIECE + p <= c.  A segment of one piece
+// leaves its sums in the gradient, others in slots, of which a block needs two: for a segment that began in an earlier one, and for one that began
+// in it and goes on.
+__device__ inline int ad_slot(int b, bool began_earlier) { return 2 * b + (began_earlier ? 0 : 1); }
 template <typename T, int JB>
 __global__ __launch_bounds__(256, sizeof(T) == 4 ? 5 - JB : 8 - 2 * JB) void k_ad_factor_grad(AdArgs g, int col_blocks_y) {
     constexpr int NP = sizeof(T) == 4 ? 3 : 1;
@@ -1217,7 +1220,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 5 - JB : 8 - 2 * JB) void k_a
     if (col >= C) return;
     float* out = is_y ? g.dA : g.dB;
     if (out && !whole) out = is_y ? g.pA : g.pB;
-    const int64_t pi = whole ? p : c;
+    const int64_t pi = whole ? p : ad_slot(b, g.seg[p] < b * AD_PIECE);
 #pragma unroll
     for (int j = 0; j < JB; ++j)
 #pragma unroll
@@ -1260,15 +1263,15 @@ __global__ __launch_bounds__(256) void k_ad_final(AdArgs g, int64_t n_w, int64_t
             const int p = (int)(i / per);
             int64_t k = i % per;
             const int s0 = g.seg[p], s1 = g.seg[p + 1];
-            const int c0 = s0 / AD_PIECE + p, c1 = s1 > s0 ? (s1 - 1) / AD_PIECE + p : c0 - 1;
+            const int b0 = s0 / AD_PIECE, b1 = s1 > s0 ? (s1 - 1) / AD_PIECE : b0 - 1;
             const bool in_a = k < (int64_t)g.r * g.O;
             if (!in_a) k -= (int64_t)g.r * g.O;
             const int64_t n = (int64_t)g.r * (in_a ? g.O : g.I);
             float* out = in_a ? g.dA : g.dB;
             const float* part = in_a ? g.pA : g.pB;
-            if (c1 == c0 || !out) continue;
+            if (b1 == b0 || !out) continue;
             float s = 0.f;
-            for (int c = c0; c <= c1; ++c) s += part[c * n + k];
+            for (int b = b0; b <= b1; ++b) s += part[ad_slot(b, b > b0) * n + k];
             out[p * n + k] = s;
         }
     } else {
@@ -1316,8 +1319,9 @@ static int64_t ad_carve(AdArgs& g, bool bwd, void* ws) {
         g.split = (int)cdiv(g.M > 0 ? g.M : 1, g.kchunk);
         g.pw = (float*)take(g.split > 1 ? (int64_t)g.split * g.O * g.I * 4 : 0);
         g.pieces = (int)(g.M / AD_PIECE + 1 + g.P);  // ids run to (M - 1) / AD_PIECE + P
-        g.pA = (float*)take((int64_t)g.pieces * g.O * g.r * 4);
-        g.pB = (float*)take((int64_t)g.pieces * g.I * g.r * 4);
+        const int64_t slots = g.M > AD_PIECE ? 2 * cdiv(g.M, AD_PIECE) : 0;
+        g.pA = (float*)take(slots * g.O * g.r * 4);
+        g.pB = (float*)take(slots * g.I * g.r * 4);
         g.pb = (float*)take((int64_t)g.pieces * g.O * 4);
     }
     return off > 0 ? off : 256;
