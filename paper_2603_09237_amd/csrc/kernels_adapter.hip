@@ -27,9 +27,10 @@ struct AdArgs {
     // scratch
     float *u, *v;        // [M][rp]
     int32_t *seg, *perm; // [P + 2], [M]
+    int32_t* table;      // [chunks][P + 1]: rows of each segment in a chunk, or NULL
     float *pw, *pA, *pB, *pb;  // partial sums: [split][O][I], [slot][O][r], [slot][r][I], [piece][O]
     const int32_t* order;  // perm where rows are taken sorted by adapter (u and v are then in that order), or NULL: as they lie
-    int rp, split, kchunk, pieces, bf16;
+    int rp, split, kchunk, pieces, bf16, chunk, chunks;
     __device__ inline int row(int s) const { return order ? order[s] : s; }
     // adapter of the row at position s, or -1
     __device__ inline int adapter(int s) const {
@@ -1080,6 +1081,87 @@ __global__ __launch_bounds__(1024) void k_ad_plan(AdArgs g) {
     });
 }
 
+// The same order where rows times adapters are too many for every workgroup to walk all rows: chunks of at least 4096 rows and an
+// eighth as many as there are adapters, each with a count of every segment's rows in it (at most 8 a row and adapter in all); the counts to places,
+// over the chunks and then over the segments; and every chunk's rows to their places, 64 at a time in order.
+__device__ inline int ad_segment(const AdArgs& g, int64_t m) {
+    const int p = g.index[m];
+    return p >= 0 && p < g.P ? p : g.P;
+}
+__global__ __launch_bounds__(1024) void k_ad_plan_count(AdArgs g) {
+    const int64_t lo = (int64_t)blockIdx.x * g.chunk, hi = lo + g.chunk < g.M ? lo + g.chunk : g.M;
+    int32_t* mine = g.table + (int64_t)blockIdx.x * (g.P + 1);
+    for (int p = threadIdx.x; p <= g.P; p += 1024) mine[p] = 0;
+    __threadfence();
+    __syncthreads();
+    for (int64_t m = lo + threadIdx.x; m < hi; m += 1024) atomicAdd(mine + ad_segment(g, m), 1);
+}
+// a thread a segment: rows in earlier chunks for every chunk, all rows into seg
+__global__ __launch_bounds__(256) void k_ad_plan_chunks(AdArgs g) {
+    const int p = blockIdx.x * 256 + threadIdx.x;
+    if (p > g.P) return;
+    int sum = 0;
+    for (int c0 = 0; c0 < g.chunks; c0 += 8) {
+        int v[8];
+#pragma unroll
+        for (int c = 0; c < 8; ++c) v[c] = g.table[(int64_t)(c0 + c < g.chunks ? c0 + c : 0) * (g.P + 1) + p];
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+            if (c0 + c < g.chunks) {
+                g.table[(int64_t)(c0 + c) * (g.P + 1) + p] = sum;
+                sum += v[c];
+            }
+    }
+    g.seg[p] = sum;
+}
+// seg: from counts to starts, a thread a run of segments
+__global__ __launch_bounds__(1024) void k_ad_plan_starts(AdArgs g) {
+    __shared__ int sums[1024];
+    const int tid = threadIdx.x, each = g.P / 1024 + 1, p0 = tid * each, p1 = p0 + each < g.P + 1 ? p0 + each : g.P + 1;
+    int sum = 0;
+    for (int p = p0; p < p1; ++p) sum += g.seg[p];
+    sums[tid] = sum;
+    __syncthreads();
+    for (int o = 1; o < 1024; o <<= 1) {
+        const int before = tid >= o ? sums[tid - o] : 0;
+        __syncthreads();
+        sums[tid] += before;
+        __syncthreads();
+    }
+    int at = sums[tid] - sum;
+    for (int p = p0; p < p1; ++p) {
+        const int n = g.seg[p];
+        g.seg[p] = at;
+        at += n;
+    }
+    if (tid == 0) g.seg[g.P + 1] = g.M;
+}
+__global__ __launch_bounds__(64) void k_ad_plan_place(AdArgs g) {
+    const int64_t lo = (int64_t)blockIdx.x * g.chunk, hi = lo + g.chunk < g.M ? lo + g.chunk : g.M;
+    const int lane = threadIdx.x;
+    int32_t* mine = g.table + (int64_t)blockIdx.x * (g.P + 1);
+    for (int64_t m0 = lo; m0 < hi; m0 += 64) {
+        const int64_t m = m0 + lane;
+        const int p = m < hi ? ad_segment(g, m) : -1;
+        int first = 0, rank = 0, rows = 0;  // of the lanes with this lane's segment: the first one, those before this lane, all
+        for (uint64_t todo = __ballot(p >= 0); todo;) {
+            const int l = __ffsll((unsigned long long)todo) - 1, q = __builtin_amdgcn_readlane(p, l);
+            const uint64_t same = __ballot(p == q);
+            if (p == q) {
+                first = l;
+                rank = __popcll(same & ((1ull << lane) - 1));
+                rows = __popcll(same);
+            }
+            todo &= ~same;
+        }
+        int at = 0;
+        if (p >= 0 && first == lane) at = atomicAdd(mine + p, rows) + g.seg[p];
+        at = __shfl(at, first);
+        if (p >= 0) g.perm[at + rank] = (int)m;
+        __threadfence_block();  // the next 64 rows' places follow these
+    }
+}
+
 // The gradients of the factors and of the bias, one piece of sorted rows and 128 columns of dy (role 0: dA, dbias) or x (role 1:
 // dB) a workgroup: out[c][j] = sum_m src[m][c] w[m][j] with w = u or v in three bf16 parts; a column of ones beside u's gives dbias.
 // The parts of an infinite value add up to an undefined one, as do its products with the zeros beside the one of the column of ones: sums that are
@@ -1294,6 +1376,10 @@ __global__ __launch_bounds__(256) void k_ad_final(AdArgs g, int64_t n_w, int64_t
 
 static int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// rows times segments beyond which the plan takes its four launches.  us of a call for dbias alone, one launch and four:
+// 131072 rows of 2048 adapters 201 and 277, 16384 of 16384 230 and 373, 1048576 of 512 493 and 420, of 4096 2510 and 483
+#define AD_PLAN_WORK ((int64_t)1 << 29)
+static bool ad_plan_is_large(const AdArgs& g) { return (int64_t)g.M * (g.P + 1) > AD_PLAN_WORK; }
 // sizes of the scratch regions for these dimensions; carve(nullptr) gives the total
 static int64_t ad_carve(AdArgs& g, bool bwd, void* ws) {
     char* at = reinterpret_cast<char*>(ws);
@@ -1309,6 +1395,12 @@ static int64_t ad_carve(AdArgs& g, bool bwd, void* ws) {
         g.v = (float*)take((int64_t)g.M * g.rp * 4);
         g.seg = (int32_t*)take(((int64_t)g.P + 2) * 4);
         g.perm = (int32_t*)take((int64_t)g.M * 4);
+        if (ad_plan_is_large(g)) {
+            const int64_t least = cdiv(g.M, 1024) > 4096 ? cdiv(g.M, 1024) : 4096, by_p = cdiv(g.P + 1, 8);
+            g.chunk = (int)(by_p > least ? by_p : least);
+            g.chunks = (int)cdiv(g.M, g.chunk);
+            g.table = (int32_t*)take((int64_t)g.chunks * (g.P + 1) * 4);
+        }
         // dW0's contraction in ranges: bf16, one workgroup of the large tiles a CU (32768 x 512 x 1160, us: 12 ranges 65 and 13 for their sum, 25
         // ranges 65 and 17, on small tiles 13 ranges 83 and 13); fp32, two of the small ones
         int64_t split = g.bf16 ? 256 / (cdiv(g.O, 256) * cdiv(g.I, 128)) : cdiv(512, cdiv(g.O, 128) * cdiv(g.I, 128));
@@ -1436,7 +1528,14 @@ template <typename T>
 static void bwd(AdArgs& g, hipStream_t s) {
     const bool factors = g.dA || g.dB || g.dbias;
     if (factors || g.dx) {
-        k_ad_plan<<<g.P + 1, 1024, 0, s>>>(g);
+        if (ad_plan_is_large(g)) {
+            k_ad_plan_count<<<g.chunks, 1024, 0, s>>>(g);
+            k_ad_plan_chunks<<<cdiv(g.P + 1, 256), 256, 0, s>>>(g);
+            k_ad_plan_starts<<<1, 1024, 0, s>>>(g);
+            k_ad_plan_place<<<g.chunks, 64, 0, s>>>(g);
+        } else {
+            k_ad_plan<<<g.P + 1, 1024, 0, s>>>(g);
+        }
         g.order = g.perm;
     }
     if (g.M > 0) {
