@@ -22,7 +22,8 @@ PROJECTIONS = ("in", "out")
 
 class MemoryBlock:
     """Parameters are in `p`, gradients after `backward` in `g` under the same names (the projections' matrices and factors in the
-    block's type, everything else and all gradients fp32)."""
+    block's type, everything else and all gradients fp32).  Acting has buffers of its own: it may run on one stream while segments and
+    their gradients run on another."""
 
     def __init__(self, preferences, width, heads, head_dim=64, groups=1, state=64, conv=4, rank=16, dtype=torch.bfloat16, device="cuda", seed=0):
         self.P, self.width, self.H, self.Pd, self.G, self.S, self.W, self.r = preferences, width, heads, head_dim, groups, state, conv, rank
@@ -55,21 +56,21 @@ class MemoryBlock:
             t = self.b[name] = torch.empty(*shape, dtype=dtype or self.dtype, device=self.dev)
         return t
 
-    def _scratch(self, n):
-        t = self.b.get("ws")
+    def _scratch(self, n, name="ws"):
+        t = self.b.get(name)
         if t is None or t.numel() < n:
-            t = self.b["ws"] = torch.empty(n, dtype=torch.uint8, device=self.dev)
+            t = self.b[name] = torch.empty(n, dtype=torch.uint8, device=self.dev)
         return t
 
     def _rows(self, name, rows):
         i, o = (self.width, self.L) if name == "in" else (self.D, self.width)
         return binding.AdapterDims(rows, i, o, self.r, self.P, self.kind)
 
-    def _project(self, name, rows, x, index, y):
+    def _project(self, name, rows, x, index, y, ws="ws"):
         d = self._rows(name, rows)
         q = self.p
         binding.adapter_fwd(d, x, q[name + ".w0"], q[name + ".bias"], q[name + ".A"], q[name + ".B"], index, y,
-                            self._scratch(binding.adapter_workspace_bytes(d)))
+                            self._scratch(binding.adapter_workspace_bytes(d), ws))
 
     def _dims(self, T, N):
         conv = binding.ConvDims(T, N, self.C, self.W, 1, self.kind, N * self.L, self.L, N * self.C, self.C)
@@ -143,12 +144,12 @@ class MemoryBlock:
         q = self.p
         proj, yc = self._buf("act.proj", N, self.L), self._buf("act.yc", N, self.D)
         y = torch.empty(N, self.width, dtype=self.dtype, device=self.dev)
-        self._project("in", N, x, index, proj)
+        self._project("in", N, x, index, proj, "act.ws")
         z, raw, dt = self._slices(proj)
         d = binding.ScanDims(1, N, self.H, self.Pd, self.G, self.S, self.kind, x_n=self.L, z_n=self.L, dt_n=self.L, y_n=self.D)
         binding.memory_step(d, self.W, raw, dt, z, q["conv.w"], q["conv.b"], q["a_log"], q["d_skip"], q["dt_bias"], first, state[0], state[1], yc,
                             after[0], after[1])
-        self._project("out", N, yc, index, y)
+        self._project("out", N, yc, index, y, "act.ws")
         return y
 
 

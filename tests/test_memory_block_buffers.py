@@ -1,0 +1,58 @@
+"""Which buffers the memory block's calls use, without a GPU: the entry points are replaced by ones that note what they are given."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2603_09237_amd import memory  # noqa: E402
+
+CALLS = ("adapter_fwd", "adapter_bwd", "conv_fwd", "conv_bwd", "scan_fwd", "scan_bwd", "memory_step")
+SIZES = {"adapter_workspace_bytes": 640, "conv_workspace_bytes": 320, "scan_saved_bytes": 512, "scan_workspace_bytes": 256}
+
+
+class Noted:
+    """The binding's functions as the block calls them; `calls`: (name, tensors)."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        if name in SIZES:
+            return lambda d, *a: SIZES[name]
+        if name in CALLS:
+            return lambda *a, **k: self.calls.append((name, [t for t in a if isinstance(t, torch.Tensor)]))
+        import paper_2603_09237_amd.binding as real
+        return getattr(real, name)
+
+
+@pytest.fixture
+def noted(monkeypatch):
+    n = Noted()
+    monkeypatch.setattr(memory, "binding", n)
+    return n
+
+
+def block(**over):
+    return memory.MemoryBlock(**{**dict(preferences=3, width=8, heads=2, head_dim=4, state=4, rank=2, device="cpu", dtype=torch.float32), **over})
+
+
+def inputs(b, T=4, N=5):
+    return torch.zeros(T, N, b.width, dtype=b.dtype), torch.zeros(N, dtype=torch.int32), b.new_state(N)
+
+
+def memory_of(calls):
+    """storage addresses of everything that the calls were given"""
+    return {t.untyped_storage().data_ptr() for _, ts in calls for t in ts if t.numel()}
+
+
+def test_acting_shares_no_scratch_with_segments(noted):
+    b = block()
+    x, index, state = inputs(b)
+    b.segment(x, index, None, state, train=True)
+    b.backward(torch.zeros_like(x))
+    update, noted.calls = memory_of(noted.calls), []
+    after = b.new_state(5)
+    given = [x[0].clone(), index.clone(), *b.new_state(5)]
+    b.act(given[0], given[1], None, (given[2], given[3]), after)
+    acting = memory_of(noted.calls)
+    parameters = {t.untyped_storage().data_ptr() for t in b.p.values()}
+    assert update & acting <= parameters
