@@ -23,7 +23,8 @@ PROJECTIONS = ("in", "out")
 class MemoryBlock:
     """Parameters are in `p`, gradients after `backward` in `g` under the same names (the projections' matrices and factors in the
     block's type, everything else and all gradients fp32).  Acting has buffers of its own: it may run on one stream while segments and
-    their gradients run on another."""
+    their gradients run on another.  What a call that is captured in a graph uses stays for as long as the block, also when later calls
+    of other sizes take other buffers."""
 
     def __init__(self, preferences, width, heads, head_dim=64, groups=1, state=64, conv=4, rank=16, dtype=torch.bfloat16, device="cuda", seed=0):
         self.P, self.width, self.H, self.Pd, self.G, self.S, self.W, self.r = preferences, width, heads, head_dim, groups, state, conv, rank
@@ -47,20 +48,34 @@ class MemoryBlock:
                        "a_log": torch.log(1 + 15 * torch.rand(heads, generator=gen)).to(self.dev), "d_skip": torch.ones(heads, device=self.dev),
                        "dt_bias": (step + torch.log(-torch.expm1(-step))).to(self.dev)})
         self.g = {k: torch.zeros(v.shape, device=self.dev) for k, v in self.p.items()}
-        self.b, self.saved_for = {}, None
+        self.b, self.saved_for, self.captured = {}, None, {}
+
+    def _capturing(self):
+        return self.dev.type == "cuda" and torch.cuda.is_current_stream_capturing()
+
+    def _keep(self, name, t):
+        """The buffer of this name from now on.  The one before it may be in use on this stream still, or in a graph."""
+        old = self.b.get(name)
+        if t is not old:
+            if old is not None and old.is_cuda and not self._capturing():
+                old.record_stream(torch.cuda.current_stream(self.dev))
+            self.b[name] = t
+        if self._capturing():
+            self.captured[t.data_ptr()] = t
+        return t
 
     def _buf(self, name, *shape, dtype=None):
         """A buffer of the block, kept while its size does not change."""
         t = self.b.get(name)
         if t is None or tuple(t.shape) != shape:
-            t = self.b[name] = torch.empty(*shape, dtype=dtype or self.dtype, device=self.dev)
-        return t
+            t = torch.empty(*shape, dtype=dtype or self.dtype, device=self.dev)
+        return self._keep(name, t)
 
     def _scratch(self, n, name="ws"):
         t = self.b.get(name)
         if t is None or t.numel() < n:
-            t = self.b[name] = torch.empty(n, dtype=torch.uint8, device=self.dev)
-        return t
+            t = torch.empty(n, dtype=torch.uint8, device=self.dev)
+        return self._keep(name, t)
 
     def _rows(self, name, rows):
         i, o = (self.width, self.L) if name == "in" else (self.D, self.width)
@@ -116,8 +131,8 @@ class MemoryBlock:
         cut there, as truncated back-propagation through time does)."""
         x, first, state = self.saved_for
         T, N = x.shape[:2]
-        q, g, rows = self.p, self.g, self.b["index"]
-        proj, xc, yc = self.b["proj"], self.b["xc"], self.b["yc"]
+        q, g = self.p, self.g
+        rows, proj, xc, yc, saved = (self._keep(n, self.b[n]) for n in ("index", "proj", "xc", "yc", "saved"))
         dproj, dxc, dyc, dx = (self._buf(n, T, N, w) for n, w in (("dproj", self.L), ("dxc", self.C), ("dyc", self.D), ("dx", self.width)))
 
         def back(name, xin, grad, dxin):
@@ -130,7 +145,7 @@ class MemoryBlock:
         (z, raw, dt), (dz, draw, ddt) = self._slices(proj), self._slices(dproj)
         xs, b, c = self._xbc(xc)
         dxs, db, dc = self._xbc(dxc)
-        binding.scan_bwd(scan, xs, b, c, dt, z, q["a_log"], q["d_skip"], q["dt_bias"], first, self.b["saved"], dyc, None, dxs, db, dc, ddt, dz,
+        binding.scan_bwd(scan, xs, b, c, dt, z, q["a_log"], q["d_skip"], q["dt_bias"], first, saved, dyc, None, dxs, db, dc, ddt, dz,
                          g["a_log"], g["d_skip"], g["dt_bias"], None, self._scratch(binding.scan_workspace_bytes(scan, True)))
         binding.conv_bwd(conv, raw, q["conv.w"], q["conv.b"], first, state[0], dxc, None, draw, g["conv.w"], g["conv.b"], None,
                          self._scratch(binding.conv_workspace_bytes(conv)))

@@ -56,3 +56,38 @@ def test_acting_shares_no_scratch_with_segments(noted):
     acting = memory_of(noted.calls)
     parameters = {t.untyped_storage().data_ptr() for t in b.p.values()}
     assert update & acting <= parameters
+
+
+def test_captured_buffers_stay(noted, monkeypatch):
+    """A call that is captured, then calls of other sizes, which take buffers of their own: the captured call's are still there."""
+    import gc
+    import weakref
+    b = block()
+    x, index, state = inputs(b)
+
+    def work(x, index, state):
+        b.segment(x, index, None, state, train=True)
+        b.backward(torch.zeros_like(x))
+        b.act(x[0].clone(), index, None, state, b.new_state(x.shape[1]))
+
+    work(x, index, state)       # as before a capture
+    noted.calls = []
+    monkeypatch.setattr(b, "_capturing", lambda: True, raising=False)
+    work(x, index, state)
+    buffers = {id(t): t for t in b.b.values()}
+    used = memory_of(noted.calls)
+    mine = [weakref.ref(t) for t in buffers.values() if t.untyped_storage().data_ptr() in used]
+    assert len(mine) >= 10
+    monkeypatch.setattr(b, "_capturing", lambda: False, raising=False)
+    SIZES_BEFORE = dict(SIZES)
+    try:
+        SIZES.update({k: 4 * v for k, v in SIZES.items()})
+        del buffers
+        noted.calls = []
+        work(*inputs(b, T=6, N=7))
+        work(*inputs(b, T=3, N=2))
+    finally:
+        SIZES.update(SIZES_BEFORE)
+    noted.calls = []
+    gc.collect()
+    assert all(r() is not None for r in mine)
