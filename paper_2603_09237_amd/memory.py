@@ -20,6 +20,11 @@ from . import binding
 PROJECTIONS = ("in", "out")
 
 
+def _versions(*tensors):
+    """How often each has been written to by torch (None: not known, as of inference tensors)."""
+    return tuple(None if t is None or t.is_inference() else t._version for t in tensors)
+
+
 class MemoryBlock:
     """Parameters are in `p`, gradients after `backward` in `g` under the same names (the projections' matrices and factors in the
     block's type, everything else and all gradients fp32).  Acting has buffers of its own: it may run on one stream while segments and
@@ -123,13 +128,21 @@ class MemoryBlock:
         binding.scan_fwd(scan, xs, b, c, dt, z, q["a_log"], q["d_skip"], q["dt_bias"], first, state[1], yc, after[1], saved,
                          self._scratch(binding.scan_workspace_bytes(scan)))
         self._project("out", T * N, yc, rows, y)
-        self.saved_for = (x, first, state) if train else None
+        self.saved_for = None
+        if train:  # (the state may move on before the backward; x and first are the caller's to leave alone until then)
+            kept = self._buf("state", *state[0].shape)
+            kept.copy_(state[0])
+            self.saved_for = (x, first, kept, _versions(x, first))
         return y, after
 
     def backward(self, dy):
         """Gradients of the last segment(train=True) from dy [T, N, width]: parameters into `g`, that of x returned (the state's is
-        cut there, as truncated back-propagation through time does)."""
-        x, first, state = self.saved_for
+        cut there, as truncated back-propagation through time does).  That segment's x and first have to be as they were."""
+        if self.saved_for is None:
+            raise RuntimeError("backward() needs the last segment() to have been one with train=True")
+        x, first, state, versions = self.saved_for
+        if versions != _versions(x, first):
+            raise RuntimeError("backward() needs the segment's x and first, which have been written to since")
         T, N = x.shape[:2]
         q, g = self.p, self.g
         rows, proj, xc, yc, saved = (self._keep(n, self.b[n]) for n in ("index", "proj", "xc", "yc", "saved"))
@@ -147,7 +160,7 @@ class MemoryBlock:
         dxs, db, dc = self._xbc(dxc)
         binding.scan_bwd(scan, xs, b, c, dt, z, q["a_log"], q["d_skip"], q["dt_bias"], first, saved, dyc, None, dxs, db, dc, ddt, dz,
                          g["a_log"], g["d_skip"], g["dt_bias"], None, self._scratch(binding.scan_workspace_bytes(scan, True)))
-        binding.conv_bwd(conv, raw, q["conv.w"], q["conv.b"], first, state[0], dxc, None, draw, g["conv.w"], g["conv.b"], None,
+        binding.conv_bwd(conv, raw, q["conv.w"], q["conv.b"], first, state, dxc, None, draw, g["conv.w"], g["conv.b"], None,
                          self._scratch(binding.conv_workspace_bytes(conv)))
         back("in", x, dproj, dx)
         return dx

@@ -77,3 +77,17 @@ def test_acting_beside_an_update():
         torch.cuda.synchronize()
         assert torch.equal(out, steps)
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_the_memory_may_move_on_before_the_backward():
+    """Acting writes the next memory into the tensors that the segment started from, as a rollout that swaps two does; the gradients stay."""
+    torch = _torch()
+    block, x, first, index, state, dy = ready(T=5)
+    block.segment(x, index, first, state, train=True)
+    want = [block.backward(dy).clone()] + [g.clone() for g in block.g.values()]
+    _, now = block.segment(x, index, first, state, train=True)
+    block.act(x[0], index, None, now, state)     # into the segment's first state
+    state[0].fill_(float("nan"))
+    got = [block.backward(dy)] + list(block.g.values())
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)

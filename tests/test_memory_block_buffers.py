@@ -91,3 +91,27 @@ def test_captured_buffers_stay(noted, monkeypatch):
     noted.calls = []
     gc.collect()
     assert all(r() is not None for r in mine)
+
+
+def test_backward_needs_its_segment(noted):
+    """After a segment that kept nothing, or whose inputs have changed, there is no backward."""
+    b = block()
+    x, index, state = inputs(b)
+    first = torch.zeros(4, 5, dtype=torch.uint8)
+    dy = torch.zeros_like(x)
+    with pytest.raises(RuntimeError, match="train=True"):
+        b.backward(dy)
+    b.segment(x, index, first, state, train=True)
+    b.backward(dy)
+    b.segment(x, index, first, state)
+    with pytest.raises(RuntimeError, match="train=True"):
+        b.backward(dy)
+    for t in (x, first):
+        b.segment(x, index, first, state, train=True)
+        t.zero_()
+        with pytest.raises(RuntimeError, match="written to"):
+            b.backward(dy)
+    with torch.inference_mode():
+        y = x.clone()
+        b.segment(y, index, None, b.new_state(5), train=True)
+        b.backward(dy)
