@@ -25,6 +25,13 @@ def _versions(*tensors):
     return tuple(None if t is None or t.is_inference() else t._version for t in tensors)
 
 
+def _check(name, t, shape, dtypes):
+    """The calls take addresses: a tensor of another shape, type or order would be read as what it is not."""
+    if t.dtype not in dtypes or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {' or '.join(str(d) for d in dtypes)} tensor {list(shape)}, "
+                         f"not {t.dtype} {list(t.shape)} with strides {list(t.stride())}")
+
+
 class MemoryBlock:
     """Parameters are in `p`, gradients after `backward` in `g` under the same names (the projections' matrices and factors in the
     block's type, everything else and all gradients fp32).  Acting has buffers of its own: it may run on one stream while segments and
@@ -111,9 +118,17 @@ class MemoryBlock:
         return (torch.zeros(N, self.W - 1, self.C, dtype=self.dtype, device=self.dev),
                 torch.zeros(N, self.H, self.Pd, self.S, device=self.dev))
 
+    def _check_memory(self, name, state, N):
+        _check(name + "[0]", state[0], (N, self.W - 1, self.C), (self.dtype,))
+        _check(name + "[1]", state[1], (N, self.H, self.Pd, self.S), (torch.float32,))
+
     def segment(self, x, index, first, state, train=False):
         """x [T, N, width], index [N] int32, first [T, N] u8 or None -> y [T, N, width] and the state behind the segment."""
         T, N = x.shape[:2]
+        _check("x", x, (T, N, self.width), (self.dtype,))
+        if first is not None:
+            _check("first", first, (T, N), (torch.uint8, torch.bool))
+        self._check_memory("state", state, N)
         q = self.p
         rows = self._buf("index", T * N, dtype=torch.int32)
         rows.view(T, N).copy_(index)
@@ -144,6 +159,7 @@ class MemoryBlock:
         if versions != _versions(x, first):
             raise RuntimeError("backward() needs the segment's x and first, which have been written to since")
         T, N = x.shape[:2]
+        _check("dy", dy, (T, N, self.width), (self.dtype,))
         q, g = self.p, self.g
         rows, proj, xc, yc, saved = (self._keep(n, self.b[n]) for n in ("index", "proj", "xc", "yc", "saved"))
         dproj, dxc, dyc, dx = (self._buf(n, T, N, w) for n, w in (("dproj", self.L), ("dxc", self.C), ("dyc", self.D), ("dx", self.width)))
@@ -169,6 +185,12 @@ class MemoryBlock:
         """One time step: x [N, width], index [N] int32, first [N] u8 or None -> y [N, width]; the memory goes from `state` into `after`
         (its convolution part may not be the same tensor, its scan part may)."""
         N = x.shape[0]
+        _check("x", x, (N, self.width), (self.dtype,))
+        _check("index", index, (N,), (torch.int32,))
+        if first is not None:
+            _check("first", first, (N,), (torch.uint8, torch.bool))
+        self._check_memory("state", state, N)
+        self._check_memory("after", after, N)
         q = self.p
         proj, yc = self._buf("act.proj", N, self.L), self._buf("act.yc", N, self.D)
         y = torch.empty(N, self.width, dtype=self.dtype, device=self.dev)

@@ -115,3 +115,38 @@ def test_backward_needs_its_segment(noted):
         y = x.clone()
         b.segment(y, index, None, b.new_state(5), train=True)
         b.backward(dy)
+
+
+def bad(t):
+    """the tensor in other types, shapes and orders"""
+    wide = torch.zeros(*t.shape[:-1], 2 * t.shape[-1], dtype=t.dtype)
+    yield t.to(torch.int64 if t.dtype == torch.int32 else torch.float64)
+    yield torch.cat([t, t])
+    yield wide[..., ::2]
+
+
+def test_arguments_that_are_refused(noted):
+    b = block()
+    x, index, state = inputs(b)
+    first, after, dy = torch.zeros(4, 5, dtype=torch.uint8), b.new_state(5), torch.zeros_like(x)
+    good = dict(x=x, first=first, state0=state[0], state1=state[1])
+    for k in good:
+        for t in bad(good[k]):
+            a = dict(good, **{k: t})
+            if k == "x" and t.shape[0] == 8:
+                continue        # a longer segment
+            with pytest.raises(ValueError, match=k.rstrip("01")):
+                b.segment(a["x"], index, a["first"], (a["state0"], a["state1"]))
+    good = dict(x=x[0].clone(), index=index, first=first[0].clone(), state0=state[0], state1=state[1], after0=after[0], after1=after[1])
+    for k in good:
+        for t in bad(good[k]):
+            a = dict(good, **{k: t})
+            with pytest.raises(ValueError):
+                b.act(a["x"], a["index"], a["first"], (a["state0"], a["state1"]), (a["after0"], a["after1"]))
+    b.segment(x, index, first, state, train=True)
+    for t in bad(dy):
+        with pytest.raises(ValueError, match="dy"):
+            b.backward(t)
+    assert [c for c, _ in noted.calls] == ["adapter_fwd", "conv_fwd", "scan_fwd", "adapter_fwd"]
+    b.act(good["x"], index, None, state, after)
+    b.segment(x, index.long(), first.bool(), state)     # (the index is copied for every step, from any type)
