@@ -271,7 +271,7 @@ int morlax_pareto_hypervolume(const float* J, const float* ref, int32_t n, int32
  * [0, n_adapters) is a row without one.
  *   y[m] = W0 x[m] + bias + A[p] (B[p] x[m]),  p = index[m]
  *   x [rows, d_in] (row stride ld_x elements), w0 [d_out, d_in], bias [d_out] fp32 or NULL, A [n_adapters, d_out, rank],
- *   B [n_adapters, rank, d_in], index [rows] int32, y [rows, d_out] (row stride ld_y); x, w0, A, B, y of the given type.
+ *   B [n_adapters, rank, d_in], index [rows] int32, y [rows, d_out] (row stride ld_y); x, w0, A, B, y of the given type.  y must not be x.
  * B[p] x[m] is kept in fp32.  The result of a row depends on its own x and its own adapter alone, up to rounding: the order of its sums goes by
  * the sizes of the call and, where the rows' factors (a copy a row) are more than 64 MB, by whether more than four adapters are among the
  * 32 rows that it lies with.
@@ -289,7 +289,7 @@ int morlax_adapter_fwd(const morlax_adapter_dims* dims, const void* x, const voi
                        const void* B, const int32_t* index, void* y, void* ws, int64_t ws_bytes, void* stream);
 /* Reverse mode: dy [rows, d_out] (stride ld_y) -> dx [rows, d_in] (stride ld_x, dtype), dw0 [d_out, d_in], dbias [d_out],
  * dA [n_adapters, d_out, rank], dB [n_adapters, rank, d_in] (fp32, overwritten, zero for an adapter without rows).  Any of
- * the outputs may be NULL: what only it needs is left out.  Sums in a fixed order: results repeat bit for bit. */
+ * the outputs may be NULL: what only it needs is left out.  dx must not be x or dy.  Sums in a fixed order: results repeat bit for bit. */
 int morlax_adapter_bwd(const morlax_adapter_dims* dims, const void* x, const void* w0, const void* A, const void* B,
                        const int32_t* index, const void* dy, void* dx, float* dw0, float* dbias, float* dA, float* dB, void* ws,
                        int64_t ws_bytes, void* stream);
@@ -351,7 +351,7 @@ int morlax_scan_bwd(const morlax_scan_dims* dims, const void* x, const void* b, 
 /* One time step of both (dims->T = 1; the *_t strides are not used): the convolution with SiLU over the rows xbc [N, heads *
  * head_dim + 2 groups * state] (x, then B, then C), stride x_n, and the scan on its outputs, which stay in fp32 between the two.
  * width, conv_w, conv_b, conv_in, conv_out as in morlax_conv_fwd on those channels, the others as in morlax_scan_fwd; first [N].
- * conv_out must not be conv_in; state_out may be state_in. */
+ * conv_out must not be conv_in, y not xbc (it may be z, with z's stride); state_out may be state_in. */
 int morlax_memory_step(const morlax_scan_dims* dims, int32_t width, const void* xbc, const void* dt, const void* z,
                        const float* conv_w, const float* conv_b, const float* a_log, const float* d_skip, const float* dt_bias,
                        const uint8_t* first, const void* conv_in, const float* state_in, void* y, void* conv_out, float* state_out,

@@ -533,6 +533,7 @@ extern "C" int morlax_adapter_fwd(const morlax_adapter_dims* dims, const void* x
     STRIDED(x, dims->dtype, who); STRIDED(y, dims->dtype, who);
     REQ(index, who);
     WS(ws, ws_bytes, adapter_ws_bytes(*dims, false), who);
+    if (x == y) return fail(MORLAX_ERR_SHAPE, "%s: an output is its input", who);
     launch_adapter_fwd(*dims, x, w0, bias, A, B, index, y, ws, (hipStream_t)stream);
     return finish(who);
 }
@@ -551,6 +552,7 @@ extern "C" int morlax_adapter_bwd(const morlax_adapter_dims* dims, const void* x
         REQ(index, who);
     }
     WS(ws, ws_bytes, adapter_ws_bytes(*dims, true), who);
+    if (dims->rows > 0 && dx && (dx == x || dx == dy)) return fail(MORLAX_ERR_SHAPE, "%s: an output is its input", who);
     launch_adapter_bwd(*dims, x, w0, A, B, index, dy, dx, dw0, dbias, dA, dB, ws, (hipStream_t)stream);
     return finish(who);
 }
@@ -697,6 +699,7 @@ extern "C" int morlax_memory_step(const morlax_scan_dims* dims, int32_t width, c
     REQ(conv_w, who); OPT(conv_b, who); REQ(a_log, who); OPT(d_skip, who); OPT(dt_bias, who); OPT(conv_in, who); OPT(state_in, who);
     OPT(conv_out, who); REQ(state_out, who);
     if (conv_in && conv_in == conv_out) return fail(MORLAX_ERR_SHAPE, "%s: conv_out is conv_in", who);
+    if (y == xbc || (y == z && dims->N > 1 && dims->y_n != dims->z_n)) return fail(MORLAX_ERR_SHAPE, "%s: an output is its input", who);
     launch_memory_step(*dims, width, xbc, dt, z, conv_w, conv_b, a_log, d_skip, dt_bias, first, conv_in, state_in, y, conv_out, state_out,
                        (hipStream_t)stream);
     return finish(who);

@@ -38,3 +38,20 @@ def test_scan_backward_beyond_a_launch():
 def test_scan_backward_within_a_launch(N, heads, groups, dtype):
     d = dims(N, heads, groups, dtype)
     assert binding.scan_workspace_bytes(d, True) > 0 and binding.scan_saved_bytes(d) > 0
+
+
+def refused_as_its_input(call):
+    with pytest.raises(binding.MorlaxError) as e:
+        call()
+    assert e.value.code == binding.ERR_SHAPE and "an output is its input" in str(e.value)
+
+
+def test_outputs_over_inputs():
+    """Other workgroups read what an output over its input would have overwritten."""
+    d, ws = binding.AdapterDims(8, 16, 16, 4, 3, 1), (GOOD, 1 << 40)
+    refused_as_its_input(lambda: binding.adapter_fwd(d, GOOD, GOOD, None, GOOD, GOOD, GOOD, GOOD, ws, stream=0))
+    for dx in (GOOD, GOOD + 64):
+        refused_as_its_input(lambda: binding.adapter_bwd(d, GOOD, GOOD, GOOD, GOOD, GOOD, GOOD + 64, dx, None, None, None, None, ws, stream=0))
+    d = binding.ScanDims(1, 3, 4, 16, 2, 8, 1, z_n=72)
+    for y in (GOOD, GOOD + 64):
+        refused_as_its_input(lambda: binding.memory_step(d, 4, GOOD, GOOD, GOOD + 64, GOOD, None, GOOD, None, None, None, None, None, y, None, GOOD, stream=0))
