@@ -360,8 +360,7 @@ __global__ __launch_bounds__(256, 2) void k_ad_gemm(AdArgs g) {
     __shared__ __align__(16) unsigned char lds[(2 * NP * OpA::PLANE > 4 * AD_PATCH) ? 2 * NP * OpA::PLANE : 4 * AD_PATCH];
     const int wave = threadIdx.x >> 6, lr = threadIdx.x & 31;
     const int wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
-    const int rows_a = ROLE == AD_DW ? g.O : g.M, rows_b = ROLE == AD_FWD ? g.O : g.I;
-    const int tiles_n = (rows_b + 127) / 128;
+    const int tiles_n = ((ROLE == AD_FWD ? g.O : g.I) + 127) / 128;
     const int tile = blockIdx.x;
     const int tm = (tile / tiles_n) * 128, tn = (tile % tiles_n) * 128;
     OpA a;
@@ -509,7 +508,7 @@ template <int MB, int NB> struct AdDma {
 };
 
 template <int ROLE, int MB, int NB, int RP>
-__global__ __launch_bounds__(256, NB == 4 ? 1 : MB == 2 ? 3 : 2) void k_ad_gemm_dma(AdArgs g) {
+__global__ __launch_bounds__(256, MB == 2 ? 3 : 2) void k_ad_gemm_dma(AdArgs g) {
     constexpr int KA = AdRole<ROLE>::KA, KB = AdRole<ROLE>::KB, TM = 64 * MB, TN = 64 * NB;
     typedef AdTile<KA, TM> TA;
     typedef AdTile<KB, TN> TB;

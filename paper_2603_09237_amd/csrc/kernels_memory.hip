@@ -482,13 +482,6 @@ struct Tile {
             v[2] += __uint_as_float(u.y << 16); v[3] += __uint_as_float(u.y & 0xffff0000u);
         }
     }
-    __device__ inline float get(int row, int col) const {
-        float v = 0.f;
-#pragma unroll
-        for (int q = NP - 1; q >= 0; --q)
-            v += __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(at + q * PLANE + row * PITCH + col * 2) << 16);
-        return v;
-    }
 };
 
 // The rows t0 .. t0 + cnt - 1 of a tensor on their way to a tile (others zero), 2 B pieces of eight values a lane.  All of a chunk's tensors
@@ -958,8 +951,8 @@ __global__ __launch_bounds__((ScanFwdLds<T, PB, SB>::NW * 64), 2) void k_scan_fw
         if (lane == 0) g.left[unit] = all;
         return;
     }
-    if (span + 1 < g.spans) return;
-    if (g.state_out && g.spans == 1) st.store(g.state_out + id * g.P * g.S, g.P, g.S, patch);
+    if (g.state_out && g.spans == 1)  // (of several spans k_scan_join has left it)
+        st.store(g.state_out + id * g.P * g.S, g.P, g.S, patch);
 }
 
 // The states between the spans of an environment's head, a thread four values of the register order: what span i leaves is replaced by what
@@ -1118,7 +1111,6 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
         const float qs = s.e < 0 ? __builtin_amdgcn_exp2f(s.hi + s.lo) : 0.f;              // from its start
         const float left = eq < 0 ? __builtin_amdgcn_exp2f(hiq + loq) : 0.f;                // over all of it
         if (lane < 32) sl->w[lr] = qs;
-        phase();
         phase();
         // scores and dy . x in both layouts: [s | t] (lane: the later step) and [t | s] (lane: the earlier one)
         float16_t g1, g2, r1, r2, l1, l2;

@@ -17,8 +17,6 @@ import torch
 
 from . import binding
 
-PROJECTIONS = ("in", "out")
-
 
 def _versions(*tensors):
     """How often each has been written to by torch (None: not known, as of inference tensors)."""
