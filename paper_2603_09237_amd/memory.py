@@ -23,11 +23,16 @@ def _versions(*tensors):
     return tuple(None if t is None or t.is_inference() else t._version for t in tensors)
 
 
-def _check(name, t, shape, dtypes):
+def _check(name, t, shape, dtype):
     """The calls take addresses: a tensor of another shape, type or order would be read as what it is not."""
-    if t.dtype not in dtypes or tuple(t.shape) != shape or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {' or '.join(str(d) for d in dtypes)} tensor {list(shape)}, "
-                         f"not {t.dtype} {list(t.shape)} with strides {list(t.stride())}")
+    if t.shape == shape and t.dtype is dtype and t.is_contiguous():
+        return
+    raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)}, not {t.dtype} {list(t.shape)} with strides {list(t.stride())}")
+
+
+def _check_first(first, shape):
+    if first is not None:
+        _check("first", first, shape, torch.bool if first.dtype is torch.bool else torch.uint8)
 
 
 class MemoryBlock:
@@ -58,34 +63,38 @@ class MemoryBlock:
                        "a_log": torch.log(1 + 15 * torch.rand(heads, generator=gen)).to(self.dev), "d_skip": torch.ones(heads, device=self.dev),
                        "dt_bias": (step + torch.log(-torch.expm1(-step))).to(self.dev)})
         self.g = {k: torch.zeros(v.shape, device=self.dev) for k, v in self.p.items()}
-        self.b, self.saved_for, self.captured = {}, None, {}
+        self.b, self.saved_for = {}, None
+        self.captured, self.recording = {}, False   # buffers that graphs use; whether the present call is being captured
 
     def _capturing(self):
         return self.dev.type == "cuda" and torch.cuda.is_current_stream_capturing()
 
-    def _keep(self, name, t):
-        """The buffer of this name from now on.  The one before it may be in use on this stream still, or in a graph."""
+    def _replace(self, name, t):
+        """The buffer of this name from now on.  The one before it may be in use on this stream still."""
         old = self.b.get(name)
-        if t is not old:
-            if old is not None and old.is_cuda and not self._capturing():
-                old.record_stream(torch.cuda.current_stream(self.dev))
-            self.b[name] = t
-        if self._capturing():
+        if old is not None and old.is_cuda and not self.recording:
+            old.record_stream(torch.cuda.current_stream(self.dev))
+        self.b[name] = t
+        return t
+
+    def _used(self, t):
+        """A buffer that is about to be used: one that a graph will use on replays is kept."""
+        if self.recording:
             self.captured[t.data_ptr()] = t
         return t
 
     def _buf(self, name, *shape, dtype=None):
         """A buffer of the block, kept while its size does not change."""
         t = self.b.get(name)
-        if t is None or tuple(t.shape) != shape:
-            t = torch.empty(*shape, dtype=dtype or self.dtype, device=self.dev)
-        return self._keep(name, t)
+        if t is None or t.shape != shape:
+            t = self._replace(name, torch.empty(*shape, dtype=dtype or self.dtype, device=self.dev))
+        return self._used(t)
 
     def _scratch(self, n, name="ws"):
         t = self.b.get(name)
         if t is None or t.numel() < n:
-            t = torch.empty(n, dtype=torch.uint8, device=self.dev)
-        return self._keep(name, t)
+            t = self._replace(name, torch.empty(n, dtype=torch.uint8, device=self.dev))
+        return self._used(t)
 
     def _rows(self, name, rows):
         i, o = (self.width, self.L) if name == "in" else (self.D, self.width)
@@ -117,15 +126,15 @@ class MemoryBlock:
                 torch.zeros(N, self.H, self.Pd, self.S, device=self.dev))
 
     def _check_memory(self, name, state, N):
-        _check(name + "[0]", state[0], (N, self.W - 1, self.C), (self.dtype,))
-        _check(name + "[1]", state[1], (N, self.H, self.Pd, self.S), (torch.float32,))
+        _check(name + "[0]", state[0], (N, self.W - 1, self.C), self.dtype)
+        _check(name + "[1]", state[1], (N, self.H, self.Pd, self.S), torch.float32)
 
     def segment(self, x, index, first, state, train=False):
         """x [T, N, width], index [N] int32, first [T, N] u8 or None -> y [T, N, width] and the state behind the segment."""
         T, N = x.shape[:2]
-        _check("x", x, (T, N, self.width), (self.dtype,))
-        if first is not None:
-            _check("first", first, (T, N), (torch.uint8, torch.bool))
+        self.recording = self._capturing()
+        _check("x", x, (T, N, self.width), self.dtype)
+        _check_first(first, (T, N))
         self._check_memory("state", state, N)
         q = self.p
         rows = self._buf("index", T * N, dtype=torch.int32)
@@ -157,9 +166,10 @@ class MemoryBlock:
         if versions != _versions(x, first):
             raise RuntimeError("backward() needs the segment's x and first, which have been written to since")
         T, N = x.shape[:2]
-        _check("dy", dy, (T, N, self.width), (self.dtype,))
+        self.recording = self._capturing()
+        _check("dy", dy, (T, N, self.width), self.dtype)
         q, g = self.p, self.g
-        rows, proj, xc, yc, saved = (self._keep(n, self.b[n]) for n in ("index", "proj", "xc", "yc", "saved"))
+        rows, proj, xc, yc, saved = (self._used(self.b[n]) for n in ("index", "proj", "xc", "yc", "saved"))
         dproj, dxc, dyc, dx = (self._buf(n, T, N, w) for n, w in (("dproj", self.L), ("dxc", self.C), ("dyc", self.D), ("dx", self.width)))
 
         def back(name, xin, grad, dxin):
@@ -183,10 +193,10 @@ class MemoryBlock:
         """One time step: x [N, width], index [N] int32, first [N] u8 or None -> y [N, width]; the memory goes from `state` into `after`
         (its convolution part may not be the same tensor, its scan part may)."""
         N = x.shape[0]
-        _check("x", x, (N, self.width), (self.dtype,))
-        _check("index", index, (N,), (torch.int32,))
-        if first is not None:
-            _check("first", first, (N,), (torch.uint8, torch.bool))
+        self.recording = self._capturing()
+        _check("x", x, (N, self.width), self.dtype)
+        _check("index", index, (N,), torch.int32)
+        _check_first(first, (N,))
         self._check_memory("state", state, N)
         self._check_memory("after", after, N)
         q = self.p
