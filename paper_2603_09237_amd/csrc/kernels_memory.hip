@@ -999,8 +999,8 @@ __global__ __launch_bounds__(256) void k_scan_join(ScanArgs g) {
 // the first sum as a product of the pairs with a triangle of ones over t, then those s of i's own episode: every term is there once and nothing
 // is taken away again.  (As a sum over t >= i of what the pairs with earlier steps give less what those with later ones do, all pairs of later steps
 // come in and go out again: what they round to, and a step of a later episode that is undefined, stayed in the earlier steps' gradients.)
-// Half the environments of the forward's example: 305 us.  Bound by instructions and their waits: 60 million of the vector unit's (98 us of its
-// time) at one wave a SIMD, whose 470 registers and 37 KB of LDS leave no room for a second; 34 % of the cycles wait.
+// Half the environments of the forward's example: 313 us.  Bound by instructions and their waits: 63 million of the vector unit's (102 us of its
+// time) at one wave a SIMD, whose 506 registers and 37 KB of LDS leave no room for a second; 36 % of the cycles wait.
 template <typename T, int PB, int SB>
 struct ScanBwdLds {
     static constexpr int NP = Planes<T>::N;
@@ -1013,7 +1013,7 @@ struct ScanBwdLds {
 template <typename T, int PB, int SB>
 __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(ScanArgs g) {
     typedef ScanBwdLds<T, PB, SB> L;
-    constexpr bool FOLD = sizeof(T) == 4 && PB * SB == 4;  // no registers for both blocks' small products: 256 environments fp32 64 x 64 501 us, else 530
+    constexpr bool FOLD = sizeof(T) == 4 && PB * SB == 4;  // no registers for both blocks' small products: with it and without, us: 256 environments fp32 64 x 64 485 and 531, 512 bf16 412 and 405
     constexpr int NP = L::NP, NW = L::NW, RP = 32 * SB + 4, NY = sizeof(T) == 4 ? 3 : 2;  // NY: parts of what only dz and dx see
     extern __shared__ __align__(16) unsigned char lds[];
     const int wave = wave_index(), lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5;
