@@ -787,7 +787,7 @@ struct ScanFwdLds {
     static constexpr int WAVE = X + 2 * N + (int)sizeof(StepLds);
 };
 
-// Bound by its reads and writes, half of them the states: 64 steps x 1024 environments x 8 heads of 64 x 64 bf16, 487 MB in 120 us, 4.1 TB/s.
+// Bound by its reads and writes, half of them the states: 64 steps x 1024 environments x 8 heads of 64 x 64 bf16, 487 MB in 121 us, 4.0 TB/s.
 // One wave a head keeps the state in registers over the whole segment.  Rounding: operands as bf16 parts (three in fp32 and where a state
 // follows; two, which leave out 2^-17, where only a bf16 y does), sums and states in fp32, y once.
 // LOCAL: only the state that a span of time leaves when nothing enters it, and what it leaves of a state that does.  (Where environments
