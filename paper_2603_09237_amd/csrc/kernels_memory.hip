@@ -552,7 +552,7 @@ struct Steps {
 };
 __device__ inline float last_of(float v) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 31)); }
 // small per-chunk arrays in LDS, for lanes that need them by accumulator row
-struct StepLds { float hi[32], lo[32], dt[32], w[32]; int e[32]; };
+struct StepLds { float hi[32], lo[32], dt[32], w[32]; };
 
 template <typename T>
 __device__ inline Steps steps(const ScanArgs& g, int n, int h, int t0, int cnt, double a2, float bias, StepLds* sl) {
@@ -581,7 +581,6 @@ __device__ inline Steps steps(const ScanArgs& g, int n, int h, int t0, int cnt, 
         sl->hi[lr] = s.hi;
         sl->lo[lr] = s.lo;
         sl->dt[lr] = s.dt;
-        sl->e[lr] = s.e;
     }
     return s;
 }
@@ -999,8 +998,8 @@ __global__ __launch_bounds__(256) void k_scan_join(ScanArgs g) {
 // the first sum as a product of the pairs with a triangle of ones over t, then those s of i's own episode: every term is there once and nothing
 // is taken away again.  (As a sum over t >= i of what the pairs with earlier steps give less what those with later ones do, all pairs of later steps
 // come in and go out again: what they round to, and a step of a later episode that is undefined, stayed in the earlier steps' gradients.)
-// Half the environments of the forward's example: 313 us.  Bound by instructions and their waits: 63 million of the vector unit's (102 us of its
-// time) at one wave a SIMD, whose 506 registers and 37 KB of LDS leave no room for a second; 36 % of the cycles wait.
+// Half the environments of the forward's example: 301 us.  Bound by instructions and their waits: 61 million of the vector unit's (99 us of its
+// time) at one wave a SIMD, whose 477 registers and 37 KB of LDS leave no room for a second; 34 % of the cycles wait.
 template <typename T, int PB, int SB>
 struct ScanBwdLds {
     static constexpr int NP = Planes<T>::N;
@@ -1013,7 +1012,7 @@ struct ScanBwdLds {
 template <typename T, int PB, int SB>
 __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(ScanArgs g) {
     typedef ScanBwdLds<T, PB, SB> L;
-    constexpr bool FOLD = sizeof(T) == 4 && PB * SB == 4;  // no registers for both blocks' small products: with it and without, us: 256 environments fp32 64 x 64 485 and 531, 512 bf16 412 and 405
+    constexpr bool FOLD = sizeof(T) == 4 && PB * SB == 4;  // no registers for both blocks' small products: with it and without, us: 256 environments fp32 64 x 64 469 and 498, 512 bf16 389 and 387
     constexpr int NP = L::NP, NW = L::NW, RP = 32 * SB + 4, NY = sizeof(T) == 4 ? 3 : 2;  // NY: parts of what only dz and dx see
     extern __shared__ __align__(16) unsigned char lds[];
     const int wave = wave_index(), lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5;
@@ -1113,8 +1112,8 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
         if (lane < 32) sl->w[lr] = qs;
         phase();
         // scores and dy . x in both layouts: [s | t] (lane: the later step) and [t | s] (lane: the earlier one)
-        float16_t g1, g2, r1, r2, l1, l2;
-        zero(g1); zero(g2); zero(r1); zero(r2); zero(l1); zero(l2);
+        float16_t g1, g2, r1, r2, l2;  // (r2 enters the decays' gradients, r1 dC alone)
+        zero(g1); zero(g2); zero(r1); zero(r2); zero(l2);
 #pragma unroll
         for (int kk = 0; kk < 2 * SB; ++kk) {
             uint4 ob[NP], oc[NP];
@@ -1128,22 +1127,26 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
             uint4 ox[NP], fd[3];
             X.rows(kk, ox);
             D.rows(kk, fd);
-            mma_p2(ox, fd, r1, l1);
+            mma_p(ox, fd, r1);
             mma_p2<true>(fd, ox, r2, l2);
         }
         phase();
         float col_tot = 0.f;  // B_s . dB'_s: the sum over the step and later ones of E scores R, and end_tot below
         // m1: scores that give y [s | t]; r1: E R dt_s [s | t]; g2: E scores [t | s]; r2: E R [t | s]; pairs: E scores R dt_s [t | s]
         float16_t m1, pairs;
+        // the accumulator's rows (bit 8 (e / 4) + e % 4) that are steps of this one's episode: before it, up to it, from it on
+        const uint32_t begun = (uint32_t)__ballot(s.begins), below = (1u << lr) - 1, next = begun & ~(2 * below + 1);
+        const uint32_t rows_before = (below & ~(s.e < 0 ? 0u : (1u << s.e) - 1)) >> 4 * lg, rows_t = rows_before | (1u << lr) >> 4 * lg,
+                       rows_s = (((next & -next) - 1) & ~below) >> 4 * lg;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             const int r = acc_row(e, lg);
-            r1[e] += l1[e];
             r2[e] += l2[e];
             const float rhi = sl->hi[r], rlo = sl->lo[r], rdt = sl->dt[r];
-            const int re = sl->e[r];
-            const bool on1 = r <= lr && r >= s.e, on2 = r >= lr && lr >= re;
-            const float d1 = on1 ? decay(s.hi, s.lo, rhi, rlo) * rdt : 0.f, d2 = on2 ? decay(rhi, rlo, s.hi, s.lo) : 0.f;
+            const uint32_t bit = 1u << acc_row(e, 0);
+            const bool on1 = (rows_t & bit) != 0, on2 = (rows_s & bit) != 0;
+            const float x = (s.hi - rhi) + (s.lo - rlo), d = __builtin_amdgcn_exp2f(on1 ? x : -x);  // (one of the two, or a step and itself)
+            const float d1 = on1 ? d * rdt : 0.f, d2 = on2 ? d : 0.f;
             m1[e] = counted(g1[e], d1);
             r1[e] = counted(r1[e], d1);
             g2[e] = counted(g2[e], d2);
@@ -1172,10 +1175,7 @@ __global__ __launch_bounds__((ScanBwdLds<T, PB, SB>::NW * 64)) void k_scan_bwd(S
                 for (int q = 2; q >= 0; --q) Mma32<bf16_t>::run(fp[q], ones, o);
             }
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int r = acc_row(e, lg);
-                between += r < lr && r >= s.e ? -o[e] : 0.f;
-            }
+            for (int e = 0; e < 16; ++e) between -= rows_before & (1u << acc_row(e, 0)) ? o[e] : 0.f;
         }
         phase();
         // dz needs y again
