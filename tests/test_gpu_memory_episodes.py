@@ -97,3 +97,38 @@ def test_gradients_of_a_later_episode_leave_nothing_behind(T, begin, scale, dtyp
         assert torch.equal(got[k][:begin, 0], want[k][:begin, 0]), k
         assert torch.equal(got[k][:, 1], want[k][:, 1]), k
     assert torch.equal(got["state"], want["state"])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("T,begin", [(20, 0), (20, 9), (90, 40), (400, 5), (400, 200), (400, 399)])
+def test_states_at_either_end(T, begin, value, dtype):
+    """What is undefined in the state before the segment ends with its first episode, and in the gradient of the state behind it with the last one."""
+    from test_gpu_memory import run_scan, run_scan_bwd, scan_problem
+    torch = _torch()
+    dims, h, d = scan_problem(T, 2, H, P, G, S, dtype, 0.0, True, seed=T + begin)
+    d["first"] = torch.zeros(T, 2, dtype=torch.uint8, device="cuda")
+    d["first"][begin, 0] = 1
+    heads = lambda v, n: v.reshape(*v.shape[:2], H, n)  # noqa: E731
+
+    def run():
+        y, out, saved = run_scan(dims, d, saved=True)
+        return y.clone(), out.clone(), {k: g.clone() for k, g in run_scan_bwd(dims, d, saved).items()}
+
+    y0, out0, g0 = run()
+    keep = d["state"][0, 1, 3, 5].clone()
+    d["state"][0, 1, 3, 5] = value
+    y, out, g = run()
+    ok = torch.ones(T, 2, H, dtype=torch.bool, device="cuda")
+    ok[:begin, 0, 1] = False
+    assert torch.equal(heads(y, P)[ok], heads(y0, P)[ok]) and torch.equal(out, out0)
+    assert begin == 0 or not torch.isfinite(heads(y, P)[0, 0, 1]).all()
+    for k in ("xbc", "z", "dt"):
+        assert torch.equal(g[k][begin:], g0[k][begin:]) and torch.equal(g[k][:, 1], g0[k][:, 1]), k
+    d["state"][0, 1, 3, 5] = keep
+    d["dstate"][0, 1, 3, 5] = value
+    y, out, g = run()
+    assert torch.equal(y, y0) and torch.equal(out, out0)
+    for k in ("xbc", "z", "dt"):
+        assert torch.equal(g[k][:begin], g0[k][:begin]) and torch.equal(g[k][:, 1], g0[k][:, 1]), k
+    assert torch.equal(g["state"], g0["state"])

@@ -24,3 +24,27 @@ def test_convolution_of_as_many_environments_as_there_may_be():
     binding.conv_bwd(dims, x, w, b, None, None, dy, None, out, dw, db, None, ws)
     assert bool((out[:N] == 0.5).all()) and bool((out[N:] == 7.0).all())
     assert abs(float(dw) - N) <= 256 and abs(float(db) - N) <= 256
+
+
+def test_scan_and_step_of_as_many_heads_as_there_may_be():
+    """N * heads next to 2^25, a wave each: every one gets h = e^(-ln 2) 1 + ln 2 (a step of softplus(0), a = -1), and y = h; in the step x, B and C
+    have been through SiLU."""
+    import math
+    import torch
+    N, H = 8191, 4096
+    xbc = torch.ones(1, N, H + 2, device="cuda")
+    dt, a_log = torch.zeros(1, N, H, device="cuda"), torch.zeros(H, device="cuda")
+    y, state, out = torch.empty(1, N, H, device="cuda"), torch.ones(N, H, 1, 1, device="cuda"), torch.full((N * H + 64,), 7.0, device="cuda")
+    dims = binding.ScanDims(1, N, H, 1, 1, 1, 0)
+    ws = torch.empty(binding.scan_workspace_bytes(dims), dtype=torch.uint8, device="cuda")
+    binding.scan_fwd(dims, xbc, xbc[..., H:], xbc[..., H + 1:], dt, None, a_log, None, None, None, state, y, out, None, ws)
+    want = 0.5 + math.log(2)
+    assert float((y - want).abs().max()) < 1e-6 and float((out[:N * H] - want).abs().max()) < 1e-6
+    assert bool((out[N * H:] == 7.0).all())
+    y.zero_()
+    w = torch.ones(H + 2, 1, device="cuda")
+    binding.memory_step(dims, 1, xbc, dt, None, w, None, a_log, None, None, None, None, state, y, None, out)
+    s = 1 / (1 + math.exp(-1))
+    h = 0.5 + math.log(2) * s * s
+    assert float((out[:N * H] - h).abs().max()) < 1e-6 and float((y - h * s).abs().max()) < 1e-6
+    assert bool((out[N * H:] == 7.0).all())

@@ -79,7 +79,7 @@ def test_captured_buffers_stay(noted, monkeypatch):
     mine = [weakref.ref(t) for t in buffers.values() if t.untyped_storage().data_ptr() in used]
     assert len(mine) >= 10
     monkeypatch.setattr(b, "_capturing", lambda: False, raising=False)
-    SIZES_BEFORE = dict(SIZES)
+    before = dict(SIZES)
     try:
         SIZES.update({k: 4 * v for k, v in SIZES.items()})
         del buffers
@@ -87,7 +87,7 @@ def test_captured_buffers_stay(noted, monkeypatch):
         work(*inputs(b, T=6, N=7))
         work(*inputs(b, T=3, N=2))
     finally:
-        SIZES.update(SIZES_BEFORE)
+        SIZES.update(before)
     noted.calls = []
     gc.collect()
     assert all(r() is not None for r in mine)
