@@ -357,6 +357,102 @@ int morlax_memory_step(const morlax_scan_dims* dims, int32_t width, const void* 
                        const uint8_t* first, const void* conv_in, const float* state_in, void* y, void* conv_out, float* state_out,
                        void* stream);
 
+/* ---- Memory by attention -------------------------------------------------------------------------------------------
+ * Conventions of the section above (no context, dtype 0 fp32 and 1 bf16, tensors with strides aligned to an element and everything else
+ * to 16 bytes, sums and softmax statistics fp32, outputs rounded once).
+ *
+ * Attention of a segment's steps over the past steps of their own episode.  Query heads share heads of keys: heads / kv_heads consecutive
+ * ones each.  The T queries are the last T of the S >= T steps whose keys and values are given (the S - T before them are what an earlier
+ * segment left); p_t = S - T + t:
+ *   a[t, s] = scale q_t . k_s + bias[h, bucket(p_t - s)],   y_t = sum_s exp(a[t, s] - L_t) v_s,   L_t = log sum_s exp(a[t, s]),
+ * over the s <= p_t with p_t - s < window and no episode's begin in (s, p_t] (first [S, N] u8, non-zero: an episode begins at that step;
+ * NULL: nowhere).  bucket(d) = the number of edges[j] <= d with j >= 1: edges [buckets] int32 ascending, bucket j holds the distances from
+ * edges[j] on (0 for the first, whatever edges[0] says).  buckets 0: no bias (bias, edges NULL).  What is not seen is never used: it may be
+ * infinite or undefined, in values and in gradients.  A row whose seen scores are all -infinity is undefined.
+ *   q, y [T, N, heads * head_dim] (strides q_t, q_n and y_t, y_n), k, v [S, N, kv_heads * head_dim] (strides k_t, k_n both), bias [heads,
+ *   buckets] fp32.  saved: morlax_attn_saved_bytes() bytes that the backward needs, or NULL.
+ * Limits: 1 <= T <= S <= 2^20, 1 <= head_dim <= 128, kv_heads | heads <= 1024, 0 <= buckets <= 64, window >= 1, and fewer than 2^24 workgroups:
+ * N * heads * ceil(T / 64) and N * kv_heads * ceil(S / 64) below 2^24, N * heads * buckets * ceil(T / 64) below 2^38. */
+typedef struct {
+    int32_t T, S, N, heads, kv_heads, head_dim, buckets, window;
+    int32_t dtype;
+    float scale;
+    int64_t q_t, q_n, k_t, k_n, y_t, y_n;
+} morlax_attn_dims;
+
+int64_t morlax_attn_saved_bytes(const morlax_attn_dims* dims); /* -1 for dimensions that are not served, also of the next */
+int64_t morlax_attn_workspace_bytes(const morlax_attn_dims* dims, int32_t backward);
+int morlax_attn_fwd(const morlax_attn_dims* dims, const void* q, const void* k, const void* v, const float* bias, const int32_t* edges,
+                    const uint8_t* first, void* y, void* saved, void* ws, int64_t ws_bytes, void* stream);
+/* Reverse mode, the probabilities computed again.  y and saved come from the matching morlax_attn_fwd (same dims and inputs).  dy (strides
+ * of y) -> dq (strides of q), dk, dv (strides of k; all S steps) and dbias [heads, buckets] fp32 (or NULL).  Sums in a fixed order. */
+int morlax_attn_bwd(const morlax_attn_dims* dims, const void* q, const void* k, const void* v, const float* bias, const int32_t* edges,
+                    const uint8_t* first, const void* y, const void* saved, const void* dy, void* dq, void* dk, void* dv, float* dbias,
+                    void* ws, int64_t ws_bytes, void* stream);
+
+/* A cache of keys and values in pages: step p of environment n's episode lies in row p % page of page table[n, (p / page) % slots], so that an
+ * episode of any length goes round its slots, the oldest steps' pages used again.  One step's bookkeeping: for every environment
+ *   length_in[n] < 0: nothing, slot[n] = -1 (a row that no environment uses);
+ *   else p = 0 where first[n] (NULL: nowhere), length_in[n] elsewhere; the pages of an episode that gives way to a new one go back, in the order
+ *   of the environments and their slots, all but the one in slot 0, which serves again; where the slot of p has no page, one is taken from the
+ *   queue, in the order of the environments, while there are any (pages that went back in this call serve from the next one on);
+ *   length[n] = p + 1, slot[n] = the row p lies in, page * page_rows + p % page_rows, or -1 where no page was left.
+ * A table entry outside [0, pages) is none.  queue [pages] is a ring of free pages, state = {where it begins, how many there are}.
+ * length_in, length, slot [N], table_in, table [N, slots], queue_in, queue [pages], state_in, state [2], all int32.  Each output but slot may be its
+ * own input.  Lengths must stay below 2^31 - 1.
+ * Limits: page a power of two up to 4096, pages * page < 2^31, N * slots < 2^31, N <= 2^24. */
+typedef struct {
+    int32_t N, page, slots, pages;
+} morlax_pages_dims;
+
+int64_t morlax_pages_workspace_bytes(const morlax_pages_dims* dims);
+int morlax_cache_pages(const morlax_pages_dims* dims, const uint8_t* first, const int32_t* length_in, const int32_t* table_in,
+                       const int32_t* queue_in, const int32_t* state_in, int32_t* length, int32_t* table, int32_t* queue, int32_t* state,
+                       int32_t* slot, void* ws, int64_t ws_bytes, void* stream);
+
+/* Attention of one new step of every environment over such a cache, the new step's key and value put there first: morlax_attn_fwd's formula
+ * with p = length[n] - 1 (the step itself) and the steps of the episode that the window holds.  An environment of length <= 0 gets zeros and
+ * leaves the cache alone; a step whose slot has no page is seen by itself, but not kept; steps whose slots have none are not seen.
+ *   q, y [N, heads * head_dim] (strides q_n, y_n), k, v [N, kv_heads * head_dim] (stride k_n both), table [N, slots], length [N] int32 (as
+ *   morlax_cache_pages leaves them), k_cache, v_cache [pages, page, kv_heads, head_dim] of the given type.
+ * No two environments may hold the same page.
+ * Limits: as morlax_attn_fwd's and morlax_cache_pages', window <= slots * page, N * heads < 2^22. */
+typedef struct {
+    int32_t N, heads, kv_heads, head_dim, buckets, window;
+    int32_t page, slots, pages;
+    int32_t dtype;
+    float scale;
+    int64_t q_n, k_n, y_n;
+} morlax_cache_dims;
+
+int64_t morlax_attn_step_workspace_bytes(const morlax_cache_dims* dims);
+int morlax_attn_step(const morlax_cache_dims* dims, const void* q, const void* k, const void* v, const float* bias, const int32_t* edges,
+                     const int32_t* table, const int32_t* length, void* k_cache, void* v_cache, void* y, void* ws, int64_t ws_bytes,
+                     void* stream);
+
+/* What stands between two blocks of a stack, row by row:
+ *   n = u / sqrt(mean(u^2) + eps) w_post,   y = x + scale sigmoid(gate) n,   h = y / sqrt(mean(y^2) + eps) w_pre
+ * x: the sum of the blocks so far, u: the last block's output, h: the next block's input (of y before its rounding).
+ *   x, y [rows, width] (row stride ld_x), u (ld_u), gate (ld_g), h (ld_h) of the given type; scale, w_post, w_pre [width] fp32.
+ *   NULL: gate: no gate; scale: 1; w_post: u is not normed, n = u; w_pre: no h (h NULL too); u: y = x (gate, scale and w_post NULL too; y may
+ *   be NULL then).  y may be x.
+ * Limits: rows <= 2^28, 1 <= width <= 8192. */
+typedef struct {
+    int32_t rows, width;
+    int32_t dtype;
+    float eps;
+    int64_t ld_x, ld_u, ld_g, ld_h;
+} morlax_norm_dims;
+
+int64_t morlax_norm_workspace_bytes(const morlax_norm_dims* dims); /* of the backward */
+int morlax_norm_fwd(const morlax_norm_dims* dims, const void* x, const void* u, const void* gate, const float* scale, const float* w_post,
+                    const float* w_pre, void* y, void* h, void* stream);
+/* Reverse mode from the forward's inputs (x as it was): dy (stride ld_x) and dh (ld_h), NULL: zero -> dx (ld_x), du (ld_u), dgate (ld_g),
+ * dscale, dw_post, dw_pre [width] fp32, each or NULL.  dx may be dy.  Sums in a fixed order. */
+int morlax_norm_bwd(const morlax_norm_dims* dims, const void* x, const void* u, const void* gate, const float* scale, const float* w_post,
+                    const float* w_pre, const void* dy, const void* dh, void* dx, void* du, void* dgate, float* dscale, float* dw_post,
+                    float* dw_pre, void* ws, int64_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

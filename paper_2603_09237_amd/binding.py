@@ -57,6 +57,44 @@ class ScanDims(C.Structure):
                          *[f if v is None else v for v, f in zip((x_t, x_n, z_t, z_n, dt_t, dt_n, y_t, y_n), full)])
 
 
+class AttnDims(C.Structure):
+    """morlax_attn_dims: scale head_dim^-1/2 and the strides (in elements) of contiguous tensors where they are not given."""
+    _fields_ = [(n, C.c_int32) for n in ("T", "S", "N", "heads", "kv_heads", "head_dim", "buckets", "window", "dtype")] + \
+               [("scale", C.c_float)] + [(n, C.c_int64) for n in ("q_t", "q_n", "k_t", "k_n", "y_t", "y_n")]
+
+    def __init__(self, T, S, N, heads, kv_heads, head_dim, buckets, window, dtype, scale=None, q_t=None, q_n=None, k_t=None, k_n=None, y_t=None,
+                 y_n=None):
+        full = [k for w in (heads * head_dim, kv_heads * head_dim, heads * head_dim) for k in (N * w, w)]
+        super().__init__(T, S, N, heads, kv_heads, head_dim, buckets, window, dtype, head_dim ** -0.5 if scale is None and head_dim > 0 else scale or 0.0,
+                         *[f if v is None else v for v, f in zip((q_t, q_n, k_t, k_n, y_t, y_n), full)])
+
+
+class PagesDims(C.Structure):
+    """morlax_pages_dims"""
+    _fields_ = [(n, C.c_int32) for n in ("N", "page", "slots", "pages")]
+
+
+class CacheDims(C.Structure):
+    """morlax_cache_dims: scale head_dim^-1/2 and the strides (in elements) of contiguous rows where they are not given."""
+    _fields_ = [(n, C.c_int32) for n in ("N", "heads", "kv_heads", "head_dim", "buckets", "window", "page", "slots", "pages", "dtype")] + \
+               [("scale", C.c_float)] + [(n, C.c_int64) for n in ("q_n", "k_n", "y_n")]
+
+    def __init__(self, N, heads, kv_heads, head_dim, buckets, window, page, slots, pages, dtype, scale=None, q_n=None, k_n=None, y_n=None):
+        full = [w * head_dim for w in (heads, kv_heads, heads)]
+        super().__init__(N, heads, kv_heads, head_dim, buckets, window, page, slots, pages, dtype,
+                         head_dim ** -0.5 if scale is None and head_dim > 0 else scale or 0.0,
+                         *[f if v is None else v for v, f in zip((q_n, k_n, y_n), full)])
+
+
+class NormDims(C.Structure):
+    """morlax_norm_dims: row strides in elements, those of contiguous rows where they are not given."""
+    _fields_ = [(n, C.c_int32) for n in ("rows", "width", "dtype")] + [("eps", C.c_float)] + \
+               [(n, C.c_int64) for n in ("ld_x", "ld_u", "ld_g", "ld_h")]
+
+    def __init__(self, rows, width, dtype, eps=1e-6, ld_x=None, ld_u=None, ld_g=None, ld_h=None):
+        super().__init__(rows, width, dtype, eps, *[width if v is None else v for v in (ld_x, ld_u, ld_g, ld_h)])
+
+
 class MorlaxError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__(f"morlax error {code}: {msg}")
@@ -75,7 +113,10 @@ EXPORTS = ("morlax_create", "morlax_destroy", "morlax_last_error", "morlax_hpara
            "morlax_hypervolume_workspace_bytes", "morlax_pareto_hypervolume", "morlax_profile_begin",
            "morlax_profile_end", "morlax_adapter_workspace_bytes", "morlax_adapter_fwd", "morlax_adapter_bwd",
            "morlax_conv_workspace_bytes", "morlax_conv_fwd", "morlax_conv_bwd", "morlax_scan_saved_bytes",
-           "morlax_scan_workspace_bytes", "morlax_scan_fwd", "morlax_scan_bwd", "morlax_memory_step")
+           "morlax_scan_workspace_bytes", "morlax_scan_fwd", "morlax_scan_bwd", "morlax_memory_step",
+           "morlax_attn_saved_bytes", "morlax_attn_workspace_bytes", "morlax_attn_fwd", "morlax_attn_bwd", "morlax_pages_workspace_bytes",
+           "morlax_cache_pages", "morlax_attn_step_workspace_bytes", "morlax_attn_step", "morlax_norm_workspace_bytes",
+           "morlax_norm_fwd", "morlax_norm_bwd")
 
 GEMM_KINDS = ("fwd_first", "fwd_hidden", "dx_hidden", "dw_hidden", "dw_first", "fwd_fused")
 
@@ -147,6 +188,23 @@ def load():
     for name in ("morlax_conv_fwd", "morlax_conv_bwd", "morlax_scan_fwd", "morlax_scan_bwd", "morlax_memory_step"):
         getattr(lib, name).restype = C.c_int
     for name in ("morlax_adapter_fwd", "morlax_adapter_bwd"):
+        getattr(lib, name).restype = C.c_int
+    tp, pp, kp, np_ = C.POINTER(AttnDims), C.POINTER(PagesDims), C.POINTER(CacheDims), C.POINTER(NormDims)
+    lib.morlax_attn_saved_bytes.argtypes = [tp]
+    lib.morlax_attn_workspace_bytes.argtypes = [tp, i32]
+    lib.morlax_pages_workspace_bytes.argtypes = [pp]
+    lib.morlax_attn_step_workspace_bytes.argtypes = [kp]
+    lib.morlax_norm_workspace_bytes.argtypes = [np_]
+    for name in ("morlax_attn_saved_bytes", "morlax_attn_workspace_bytes", "morlax_pages_workspace_bytes", "morlax_attn_step_workspace_bytes",
+                 "morlax_norm_workspace_bytes"):
+        getattr(lib, name).restype = i64
+    lib.morlax_attn_fwd.argtypes = [tp] + [vp] * 9 + [i64, vp]
+    lib.morlax_attn_bwd.argtypes = [tp] + [vp] * 14 + [i64, vp]
+    lib.morlax_cache_pages.argtypes = [pp] + [vp] * 11 + [i64, vp]
+    lib.morlax_attn_step.argtypes = [kp] + [vp] * 11 + [i64, vp]
+    lib.morlax_norm_fwd.argtypes = [np_] + [vp] * 9
+    lib.morlax_norm_bwd.argtypes = [np_] + [vp] * 15 + [i64, vp]
+    for name in ("morlax_attn_fwd", "morlax_attn_bwd", "morlax_cache_pages", "morlax_attn_step", "morlax_norm_fwd", "morlax_norm_bwd"):
         getattr(lib, name).restype = C.c_int
     lib.morlax_profile_begin.argtypes = [vp]
     lib.morlax_profile_begin.restype = C.c_int
@@ -435,3 +493,64 @@ def memory_step(dims, width, xbc, dt, z, conv_w, conv_b, a_log, d_skip, dt_bias,
     _call(load().morlax_memory_step, C.byref(dims), int(width), _ptr(xbc), _ptr(dt), _ptr(z), _ptr(conv_w), _ptr(conv_b), _ptr(a_log),
           _ptr(d_skip), _ptr(dt_bias), _ptr(first), _ptr(conv_in), _ptr(state_in), _ptr(y), _ptr(conv_out), _ptr(state_out),
           stream if stream is not None else _stream())
+
+
+def attn_saved_bytes(dims):
+    """Bytes of the `saved` buffer that attn_fwd fills for attn_bwd."""
+    return _size(load().morlax_attn_saved_bytes(C.byref(dims)))
+
+
+def attn_workspace_bytes(dims, backward=False):
+    """Bytes of device scratch that attn_fwd (without `saved`) or attn_bwd needs."""
+    return _size(load().morlax_attn_workspace_bytes(C.byref(dims), int(bool(backward))))
+
+
+def attn_fwd(dims, q, k, v, bias, edges, first, y, saved, ws, stream=None):
+    """morlax_attn_fwd: attention of a segment's steps over the past steps of their own episode."""
+    _call(load().morlax_attn_fwd, C.byref(dims), _ptr(q), _ptr(k), _ptr(v), _ptr(bias), _ptr(edges), _ptr(first), _ptr(y), _ptr(saved), _ptr(ws),
+          _nbytes(ws), stream if stream is not None else _stream())
+
+
+def attn_bwd(dims, q, k, v, bias, edges, first, y, saved, dy, dq, dk, dv, dbias, ws, stream=None):
+    """morlax_attn_bwd: gradients of attn_fwd, the probabilities computed again."""
+    _call(load().morlax_attn_bwd, C.byref(dims), _ptr(q), _ptr(k), _ptr(v), _ptr(bias), _ptr(edges), _ptr(first), _ptr(y), _ptr(saved), _ptr(dy),
+          _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dbias), _ptr(ws), _nbytes(ws), stream if stream is not None else _stream())
+
+
+def pages_workspace_bytes(dims):
+    """Bytes of device scratch that cache_pages needs."""
+    return _size(load().morlax_pages_workspace_bytes(C.byref(dims)))
+
+
+def cache_pages(dims, first, length_in, table_in, queue_in, state_in, length, table, queue, state, slot, ws, stream=None):
+    """morlax_cache_pages: one step's bookkeeping of a paged cache."""
+    _call(load().morlax_cache_pages, C.byref(dims), _ptr(first), _ptr(length_in), _ptr(table_in), _ptr(queue_in), _ptr(state_in), _ptr(length),
+          _ptr(table), _ptr(queue), _ptr(state), _ptr(slot), _ptr(ws), _nbytes(ws), stream if stream is not None else _stream())
+
+
+def attn_step_workspace_bytes(dims):
+    """Bytes of device scratch that attn_step needs."""
+    return _size(load().morlax_attn_step_workspace_bytes(C.byref(dims)))
+
+
+def attn_step(dims, q, k, v, bias, edges, table, length, k_cache, v_cache, y, ws, stream=None):
+    """morlax_attn_step: attention of one new step of every environment over the paged cache that it is put into."""
+    _call(load().morlax_attn_step, C.byref(dims), _ptr(q), _ptr(k), _ptr(v), _ptr(bias), _ptr(edges), _ptr(table), _ptr(length), _ptr(k_cache),
+          _ptr(v_cache), _ptr(y), _ptr(ws), _nbytes(ws), stream if stream is not None else _stream())
+
+
+def norm_workspace_bytes(dims):
+    """Bytes of device scratch that norm_bwd needs for the gradients of scale, w_post and w_pre."""
+    return _size(load().morlax_norm_workspace_bytes(C.byref(dims)))
+
+
+def norm_fwd(dims, x, u, gate, scale, w_post, w_pre, y, h, stream=None):
+    """morlax_norm_fwd: y = x + scale sigmoid(gate) norm(u) w_post, h = norm(y) w_pre."""
+    _call(load().morlax_norm_fwd, C.byref(dims), _ptr(x), _ptr(u), _ptr(gate), _ptr(scale), _ptr(w_post), _ptr(w_pre), _ptr(y), _ptr(h),
+          stream if stream is not None else _stream())
+
+
+def norm_bwd(dims, x, u, gate, scale, w_post, w_pre, dy, dh, dx, du, dgate, dscale, dw_post, dw_pre, ws, stream=None):
+    """morlax_norm_bwd: gradients of norm_fwd from its inputs; outputs that are None are left out."""
+    _call(load().morlax_norm_bwd, C.byref(dims), _ptr(x), _ptr(u), _ptr(gate), _ptr(scale), _ptr(w_post), _ptr(w_pre), _ptr(dy), _ptr(dh), _ptr(dx),
+          _ptr(du), _ptr(dgate), _ptr(dscale), _ptr(dw_post), _ptr(dw_pre), _ptr(ws), _nbytes(ws), stream if stream is not None else _stream())

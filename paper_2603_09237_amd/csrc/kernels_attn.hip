@@ -1,0 +1,933 @@
+// Attention of a rollout segment's steps over the past steps of their own episode, on time-major tensors of N environments, with a learned
+// bias by buckets of the distance in time.
+//
+//   a[t, s] = scale q_t . k_s + bias[h, bucket(p_t - s)],   p_t = S - T + t,   seen where lo_t <= s <= p_t,
+//   y_t = sum_s P[t, s] v_s,   P = exp(a - L),   L_t = log sum_s exp(a[t, s]);     lo_t: the episode's begin or p_t - window + 1, the later one
+//   dP = dy_t . v_s,   dA = P (dP - delta_t),   delta_t = dy_t . y_t,
+//   dq_t = scale sum_s dA k_s,   dk_s = scale sum_t dA q_t,   dv_s = sum_t P dy_t,   dbias[h, b] = sum of dA over the pairs in bucket b
+//
+// One pass over the keys with the running maximum and sum; scores never leave the registers.  Products run on the matrix instructions with
+// the operands turned so that a computed operand (P, dA) is already where the next product wants it: keys lie along a lane's registers,
+// queries along the lanes (the other way round in the pass over the keys), and the other operand is read transposed out of LDS.  What is seen of
+// a row is an interval, [lo_t, p_t], and every mask is a select: what an unseen key, value or row holds is never multiplied (see Wide below).
+// Query heads that share a head of keys are rows of the same tile (`pack` of them), so the keys are read once for all of them and the sums over
+// heads in dk and dv are sums over rows.
+#include "mlp_device.h"
+
+static int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+typedef short short4_t __attribute__((ext_vector_type(4)));
+#define ATTN_K 64      // rows of a tile that is walked through (keys; in the pass over the keys, queries)
+#define ATTN_THREADS 256
+#define ATTN_TAB 3     // table entries that a thread stages: pack <= 4 heads, distances of a tile
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kNever = 1 << 30;  // begin of the seen interval of a row that is not there
+
+struct AttnArgs {
+    const void *q, *k, *v, *y, *dy;
+    void *out, *dq, *dk, *dv;
+    const float* bias;
+    const int32_t* edges;
+    const uint8_t* first;
+    int32_t* lo;      // [N, S] begin of every step's episode; NULL: no episodes
+    float* table;     // [H, reach] bias by distance, in units of log2; NULL: no bias
+    int32_t* bucket;  // [reach]
+    float* lse;       // [N, H, T] L, in units of log2; NULL: not wanted
+    bf16_t* low;      // [T, N, H, D] what y's rounding took away (bf16)
+    float* delta;     // [N, H, T]
+    float* part;      // [H, B, parts] sums of dA of each workgroup
+    float* dbias;
+    float scale;
+    int T, S, N, H, KV, D, B, window, reach, lgp, tiles;
+    int64_t q_t, q_n, k_t, k_n, y_t, y_n;
+    uint32_t total;
+    int whole;  // rows hold whole pieces of 16 bytes
+};
+
+// ---- episodes and the bias by distance --------------------------------------------------------------------------------
+// Blocks below `spans`: 2^lgn environments at a time, the threads of an environment taking a run of steps each; the others: the table.
+__global__ __launch_bounds__(1024) void k_attn_prepare(AttnArgs g, int spans, int lgn) {
+    __shared__ int last[1024];
+    if ((int)blockIdx.x < spans) {
+        const int NB = 1 << lgn, lanes = 1024 >> lgn, e = threadIdx.x & (NB - 1), c = threadIdx.x >> lgn;
+        const int64_t n = (int64_t)blockIdx.x * NB + e;
+        const int run = (g.S + lanes - 1) / lanes, s0 = c * run, s1 = s0 + run < g.S ? s0 + run : g.S;
+        int mine = -1;
+        if (n < g.N) {
+#pragma unroll 8
+            for (int s = s0; s < s1; ++s)
+                if (g.first[(int64_t)s * g.N + n]) mine = s;
+        }
+        last[threadIdx.x] = mine;
+        __syncthreads();
+        for (int o = 1; o < lanes; o <<= 1) {  // the last begin up to and with each run
+            const int v = c >= o ? last[((c - o) << lgn) + e] : -1;
+            __syncthreads();
+            if (v > last[threadIdx.x]) last[threadIdx.x] = v;
+            __syncthreads();
+        }
+        if (n >= g.N) return;
+        int begin = c ? last[((c - 1) << lgn) + e] : 0;
+        begin = begin < 0 ? 0 : begin;
+        for (int s = s0; s < s1; ++s) {
+            if (mine >= 0 && g.first[(int64_t)s * g.N + n]) begin = s;
+            g.lo[n * g.S + s] = begin;
+        }
+        return;
+    }
+    const int d = ((int)blockIdx.x - spans) * 1024 + threadIdx.x;
+    if (d >= g.reach) return;
+    int b = 0;
+    for (int j = 1; j < g.B; ++j) b += g.edges[j] <= d;
+    g.bucket[d] = b;
+    for (int h = 0; h < g.H; ++h) g.table[(int64_t)h * g.reach + d] = g.bias[(int64_t)h * g.B + b] * kLog2e;
+}
+
+// ---- tiles ------------------------------------------------------------------------------------------------------------
+// A tile of ATTN_K rows of up to DP elements in LDS, rows 16 bytes apart beyond their length: reads of whole pieces along a row and transposed
+// reads (16 x 16 elements bf16, single ones fp32) both touch every bank equally often.
+template <typename T, int DP>
+struct Tile {
+    static constexpr int ES = sizeof(T), VE = 16 / ES, PITCH = DP * ES + 16, CPR = DP / VE, KS = DP * ES / 64, NB = DP / 16;
+    static constexpr int TU = ES == 2 ? 32 : 16, NU = ATTN_K / TU;  // rows of one transposed operand, operands of a tile
+    static constexpr int NP = ES == 2 ? 2 : 1;                      // parts of a computed operand
+    static constexpr int BYTES = ATTN_K * PITCH;
+    // the lane's operand of rows row .. row + 15, contraction indices of piece ks along the row
+    static __device__ inline uint4 rows(const unsigned char* lds, int row, int ks) {
+        const int lane = threadIdx.x & 63;
+        return *reinterpret_cast<const uint4*>(lds + (row + (lane & 15)) * PITCH + ks * 64 + (lane >> 4) * 16);
+    }
+    // columns 16 dt .. + 15 as the rows of an operand, contraction over the rows u TU .. : in the order in which a lane holds the products'
+    // results (bf16: 4 g + r of two blocks of 16; fp32: of one)
+    static __device__ inline uint4 turned(const unsigned char* lds, int u, int dt) {
+        const int lane = threadIdx.x & 63, a = lane & 15, gr = lane >> 4;
+        if constexpr (ES == 2) {
+            typedef __attribute__((address_space(3))) short4_t lds_s4;
+            const unsigned char* s = lds + (32 * u + 4 * gr + (a >> 2)) * PITCH + (16 * dt + 4 * (a & 3)) * 2;
+            const uint2 u0 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)s));
+            const uint2 u1 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(s + 16 * PITCH)));
+            return make_uint4(u0.x, u0.y, u1.x, u1.y);
+        } else {
+            const unsigned char* s = lds + (16 * u + 4 * gr) * PITCH + (16 * dt + a) * 4;
+            return make_uint4(*reinterpret_cast<const uint32_t*>(s), *reinterpret_cast<const uint32_t*>(s + PITCH),
+                              *reinterpret_cast<const uint32_t*>(s + 2 * PITCH), *reinterpret_cast<const uint32_t*>(s + 3 * PITCH));
+        }
+    }
+    static __device__ inline float at(const unsigned char* lds, int row, int d) {
+        return to_f(*reinterpret_cast<const T*>(lds + row * PITCH + d * ES));
+    }
+};
+
+// VE elements from p on (aligned to an element), those from `n` on zero; whole: n is a multiple of VE
+typedef uint32_t piece_t __attribute__((ext_vector_type(4), aligned(2)));
+template <typename T>
+__device__ inline uint4 piece(const T* p, int n, bool whole) {
+    constexpr int VE = 16 / sizeof(T);
+    if (whole || n >= VE) {
+        if (n <= 0) return make_uint4(0, 0, 0, 0);
+        const piece_t u = *reinterpret_cast<const piece_t*>(p);
+        return make_uint4(u[0], u[1], u[2], u[3]);
+    }
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < VE; ++i) {
+        if (i >= n) break;
+        if constexpr (sizeof(T) == 2) w[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << (16 * (i & 1));
+        else w[i] = reinterpret_cast<const uint32_t*>(p)[i];
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// z plus zero, or undefined if the piece holds an infinite or undefined element
+template <typename T>
+__device__ inline float probe(const uint4& u, float z) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 2) {
+            z = __builtin_fmaf(__uint_as_float(w[i] << 16), 0.f, z);
+            z = __builtin_fmaf(__uint_as_float(w[i] & 0xffff0000u), 0.f, z);
+        } else {
+            z = __builtin_fmaf(__uint_as_float(w[i]), 0.f, z);
+        }
+    }
+    return z;
+}
+
+// A thread's pieces of a tile on their way: requested before the tile ahead of it is worked on, put down after.
+template <typename T, int DP>
+struct Stage {
+    typedef Tile<T, DP> L;
+    static constexpr int CH = ATTN_K * L::CPR / ATTN_THREADS;
+    uint4 u[CH];
+    // row r (of rows [0, end)) lies at base + (r >> lgp) * stride + (r & (pack - 1)) * D
+    __device__ inline void load(const T* base, int64_t stride, int r0, int end, int lgp, int D, bool vec) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int i = threadIdx.x + c * ATTN_THREADS, row = r0 + i / L::CPR, col = (i % L::CPR) * L::VE;
+            const bool in = row < end;
+            const int r = in ? row : end - 1;
+            u[c] = piece(base + (int64_t)(r >> lgp) * stride + (r & ((1 << lgp) - 1)) * D + (col < D ? col : 0), in ? D - col : 0, vec);
+        }
+    }
+    __device__ inline void put(unsigned char* lds, float& z) const {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int i = threadIdx.x + c * ATTN_THREADS;
+            *reinterpret_cast<uint4*>(lds + i / L::CPR * L::PITCH + (i % L::CPR) * 16) = u[c];
+            z = probe<T>(u[c], z);
+        }
+    }
+};
+
+// A lane's computed operand of four values a block: bf16 in two parts (16 bits: what is added up then is the fp32 result up to 2^-17, and the
+// one rounding that counts is the output's.  One part: y off by 2.0e-3 of its size instead of 1.6e-3, dbias by 1e-3 instead of 1e-6).
+template <typename T, int DP>
+struct Computed {
+    typedef Tile<T, DP> L;
+    uint4 part[L::NP];
+    __device__ inline void set(const float4_t* p, int u) {  // p: blocks of 16 rows
+        if constexpr (L::ES == 2) {
+            const float4_t a = p[2 * u], b = p[2 * u + 1];
+            const uint4 h = make_uint4(pack2(a[0], a[1]), pack2(a[2], a[3]), pack2(b[0], b[1]), pack2(b[2], b[3]));
+            part[0] = h;
+            const uint32_t w[4] = {h.x, h.y, h.z, h.w};
+            const float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+            uint32_t l[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) l[i] = pack2(v[2 * i] - __uint_as_float(w[i] << 16), v[2 * i + 1] - __uint_as_float(w[i] & 0xffff0000u));
+            part[1] = make_uint4(l[0], l[1], l[2], l[3]);
+        } else {
+            const float4_t a = p[u];
+            part[0] = make_uint4(__float_as_uint(a[0]), __float_as_uint(a[1]), __float_as_uint(a[2]), __float_as_uint(a[3]));
+        }
+    }
+    __device__ inline void product(const uint4& turned, float4_t& acc) const {
+#pragma unroll
+        for (int i = 0; i < L::NP; ++i) Mma16<T>::run(turned, part[i], acc);
+    }
+};
+
+// acc[b][dt] (rows: columns 16 dt + 4 g + r of the tile; column: lane & 15) += tile^T computed[b], for NBLK blocks of 16 lanes' columns.
+// Wide: the tile holds an infinite or undefined element, and a computed zero times it would reach rows that do not see it: those pairs are left
+// out one by one.  seen(b, row): is the pair of the tile's row and the lane's column of block b one that is seen.
+template <typename T, int DP, int NBLK, typename F>
+__device__ inline void fold(const unsigned char* lds, const float4_t (&p)[NBLK][4], float4_t (&acc)[NBLK][DP / 16], bool wide, F seen) {
+    typedef Tile<T, DP> L;
+    if (!wide) {
+#pragma unroll
+        for (int u = 0; u < L::NU; ++u) {
+            Computed<T, DP> c[NBLK];
+#pragma unroll
+            for (int b = 0; b < NBLK; ++b) c[b].set(p[b], u);
+#pragma unroll
+            for (int dt = 0; dt < L::NB; ++dt) {
+                const uint4 a = L::turned(lds, u, dt);
+#pragma unroll
+                for (int b = 0; b < NBLK; ++b) c[b].product(a, acc[b][dt]);
+            }
+        }
+        return;
+    }
+    const int lane = threadIdx.x & 63, a = lane & 15, gr = lane >> 4;
+#pragma unroll
+    for (int b = 0; b < NBLK; ++b)
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll 1
+                for (int o = 0; o < 4; ++o) {
+                    const float v = __shfl(p[b][t][r], 16 * o + a);
+                    const int row = 16 * t + 4 * o + r;
+                    const bool s = seen(b, row);
+#pragma unroll
+                    for (int dt = 0; dt < L::NB; ++dt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float x = acc[b][dt][e], m = __builtin_fmaf(v, L::at(lds, row, 16 * dt + 4 * gr + e), x);
+                            acc[b][dt][e] = s ? m : x;
+                        }
+                }
+}
+
+// Four consecutive elements of a row of D from column d on
+typedef uint32_t half_piece_t __attribute__((ext_vector_type(2), aligned(2)));
+typedef float run4_t __attribute__((ext_vector_type(4), aligned(4)));
+template <typename T>
+__device__ inline void store4(T* p, int d, int D, const float4_t& v) {
+    if (d + 4 <= D) {
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<half_piece_t*>(p + d) = half_piece_t{pack2(v[0], v[1]), pack2(v[2], v[3])};
+        else *reinterpret_cast<run4_t*>(p + d) = run4_t{v[0], v[1], v[2], v[3]};
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (d + i < D) p[d + i] = cvt<T>(v[i]);
+}
+
+// Workgroups go round the eight XCDs: consecutive pieces of work to the same one, where their keys are in its L2
+__device__ inline uint32_t work_item(uint32_t total) {
+    const uint32_t x = blockIdx.x & 7, i = blockIdx.x >> 3, each = total >> 3, over = total & 7;
+    return x * each + (x < over ? x : over) + i;
+}
+
+// A workgroup's rows of queries: (step, head of the pack), heads next to each other
+struct Rows {
+    int n, kv, h0, r0, rows, past;
+    __device__ inline void init(const AttnArgs& g, int per) {
+        const uint32_t w = work_item(g.total), packs = g.H >> g.lgp, rest = w / g.tiles;
+        n = rest / packs;
+        h0 = (rest % packs) << g.lgp;
+        kv = h0 / (g.H / g.KV);
+        r0 = (g.tiles - 1 - (int)(w % g.tiles)) * per;  // the longest first
+        rows = g.T << g.lgp;
+        past = g.S - g.T;
+    }
+    __device__ inline int lo(const AttnArgs& g, int p) const {
+        const int b = g.lo ? g.lo[(int64_t)n * g.S + p] : 0, w = p - g.window + 1, v = b > w ? b : w;
+        return v < 0 ? 0 : v > p ? p : v;  // (within the row whatever `saved` holds)
+    }
+};
+
+// The bias of a tile by distance: entry [head][j] belongs to the distance `far` - j (or `far` + j), clamped to those there are
+struct Table {
+    float v[ATTN_TAB];
+    int b[ATTN_TAB];
+    template <bool BUCKET>
+    __device__ inline void load(const AttnArgs& g, int h0, int each, int far, int dir) {
+        const int count = each << g.lgp;
+#pragma unroll
+        for (int c = 0; c < ATTN_TAB; ++c) {
+            const int i = threadIdx.x + c * ATTN_THREADS;
+            if (i >= count) break;
+            const int hh = i / each;
+            int d = far + dir * (i - hh * each);
+            d = d < 0 ? 0 : d >= g.reach ? g.reach - 1 : d;
+            v[c] = g.table[(int64_t)(h0 + hh) * g.reach + d];
+            if (BUCKET) {  // (a bucket whatever `saved` holds)
+                const int i = g.bucket[d];
+                b[c] = i < 0 ? 0 : i >= g.B ? g.B - 1 : i;
+            }
+        }
+    }
+    template <bool BUCKET>
+    __device__ inline void put(const AttnArgs& g, int each, float* tab, int* idx) const {
+        const int count = each << g.lgp;
+#pragma unroll
+        for (int c = 0; c < ATTN_TAB; ++c) {
+            const int i = threadIdx.x + c * ATTN_THREADS;
+            if (i >= count) break;
+            tab[i] = v[c];
+            if (BUCKET) idx[i] = b[c];
+        }
+    }
+};
+#define ATTN_TAB_ROOM (ATTN_TAB * ATTN_THREADS)
+
+// ---- forward ------------------------------------------------------------------------------------------------------------
+template <typename T, int DP, int QB>
+struct FwdLds {
+    static constexpr int K = 0, V = Tile<T, DP>::BYTES, TAB = 2 * V, FLAG = TAB + ATTN_TAB_ROOM * 4, TOTAL = FLAG + 16;
+};
+template <typename T, int DP, int QB>
+__global__ __launch_bounds__(ATTN_THREADS) void k_attn_fwd(AttnArgs g) {
+    typedef Tile<T, DP> L;
+    typedef FwdLds<T, DP, QB> M;
+    extern __shared__ __align__(16) unsigned char lds[];
+    float* tab = reinterpret_cast<float*>(lds + M::TAB);
+    int* flag = reinterpret_cast<int*>(lds + M::FLAG);
+    constexpr int BQ = 64 * QB;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, a = lane & 15, gr = lane >> 4;
+    Rows R;
+    R.init(g, BQ);
+    int t[QB], p[QB], lo[QB];
+    uint4 qf[QB][L::KS];
+#pragma unroll
+    for (int b = 0; b < QB; ++b) {
+        const int r = R.r0 + (wave * QB + b) * 16 + a;
+        const bool in = r < R.rows;
+        t[b] = in ? r >> g.lgp : -1;
+        p[b] = in ? R.past + t[b] : -1;
+        lo[b] = in ? R.lo(g, p[b]) : kNever;
+        const T* src = reinterpret_cast<const T*>(g.q) + (int64_t)(in ? t[b] : 0) * g.q_t + (int64_t)R.n * g.q_n +
+                       (int64_t)(R.h0 + (r & ((1 << g.lgp) - 1))) * g.D;
+#pragma unroll
+        for (int ks = 0; ks < L::KS; ++ks) {
+            const int d = ks * (64 / L::ES) + gr * L::VE;
+            qf[b][ks] = piece(src + (d < g.D ? d : 0), in ? g.D - d : 0, g.whole);
+        }
+    }
+    const int first_p = R.past + (R.r0 >> g.lgp), each = (BQ >> g.lgp) + ATTN_K, far = first_p + (BQ >> g.lgp) - 1;
+    const int last_row = (R.r0 + BQ < R.rows ? R.r0 + BQ : R.rows) - 1;
+    const int k_begin = R.lo(g, first_p), k_end = R.past + (last_row >> g.lgp) + 1;
+    const int last_edge = g.table ? g.edges[g.B - 1] : 0;
+    const float beyond = g.table ? g.bias[(int64_t)(R.h0 + (lane & ((1 << g.lgp) - 1))) * g.B + g.B - 1] * kLog2e : 0.f;
+    const T* kb = reinterpret_cast<const T*>(g.k) + (int64_t)R.n * g.k_n + (int64_t)R.kv * g.D;
+    const T* vb = reinterpret_cast<const T*>(g.v) + (int64_t)R.n * g.k_n + (int64_t)R.kv * g.D;
+    const float c = g.scale * kLog2e;
+    float m[QB], l[QB];
+    float4_t o[QB][L::NB];
+#pragma unroll
+    for (int b = 0; b < QB; ++b) {
+        m[b] = -__builtin_inff();
+        l[b] = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < L::NB; ++dt) o[b][dt] = float4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    if (threadIdx.x == 0) *flag = 0;
+    Stage<T, DP> sk, sv;
+    Table st;
+    auto request = [&](int k0) {
+        sk.load(kb, g.k_t, k0, k_end, 0, g.D, g.whole);
+        sv.load(vb, g.k_t, k0, k_end, 0, g.D, g.whole);
+        if (g.table && first_p - (k0 + ATTN_K - 1) < last_edge) st.load<false>(g, R.h0, each, far - k0, -1);
+    };
+    request(k_begin);
+    __syncthreads();
+    for (int k0 = k_begin; k0 < k_end; k0 += ATTN_K) {
+        const bool near = g.table && first_p - (k0 + ATTN_K - 1) < last_edge;
+        float z = 0.f, zk = 0.f;
+        sk.put(lds + M::K, zk);
+        sv.put(lds + M::V, z);
+        if (z != 0.f) *flag = 1;
+        if (near) st.put<false>(g, each, tab, nullptr);
+        __syncthreads();
+        if (k0 + ATTN_K < k_end) request(k0 + ATTN_K);
+        bool any = false, all = true;
+#pragma unroll
+        for (int b = 0; b < QB; ++b) {
+            any |= p[b] >= k0 && lo[b] < k0 + ATTN_K;
+            all &= lo[b] <= k0 && p[b] >= k0 + ATTN_K - 1;
+        }
+        if (__any(any)) {
+            const bool whole = __all(all), wide = *flag != 0;
+            float4_t s[QB][4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+#pragma unroll
+                for (int b = 0; b < QB; ++b) s[b][x] = float4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int ks = 0; ks < L::KS; ++ks) {
+                    const uint4 f = L::rows(lds + M::K, 16 * x, ks);
+#pragma unroll
+                    for (int b = 0; b < QB; ++b) Mma16<T>::run(f, qf[b][ks], s[b][x]);
+                }
+            }
+#pragma unroll
+            for (int b = 0; b < QB; ++b) {
+                if (near) {
+                    const float* row = tab + (lane & ((1 << g.lgp) - 1)) * each + 4 * gr + (t[b] < 0 ? 0 : far - p[b]);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[b][x][r] = __builtin_fmaf(s[b][x][r], c, row[16 * x + r]);
+                } else {
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[b][x][r] = __builtin_fmaf(s[b][x][r], c, beyond);
+                }
+                if (!whole) {
+                    const int from = lo[b] - k0 - 4 * gr;
+                    const uint32_t span = p[b] - lo[b];  // (a row that is not there: begins at kNever, so no key lies in its span)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            s[b][x][r] = t[b] >= 0 && (uint32_t)(16 * x + r - from) <= span ? s[b][x][r] : -__builtin_inff();
+                }
+                float top = m[b];
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) top = fmaxf(top, s[b][x][r]);
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32));
+                const float base = top == -__builtin_inff() ? 0.f : top;  // nothing seen yet
+                const float fade = __builtin_amdgcn_exp2f(m[b] - base);
+                float sum = 0.f;
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        s[b][x][r] = __builtin_amdgcn_exp2f(s[b][x][r] - base);
+                        sum += s[b][x][r];
+                    }
+                if (__any(top != m[b])) {
+                    l[b] *= fade;
+#pragma unroll
+                    for (int dt = 0; dt < L::NB; ++dt)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) o[b][dt][r] *= fade;
+                }
+                l[b] += sum;
+                m[b] = top;
+            }
+            fold<T, DP, QB>(lds + M::V, s, o, wide,
+                            [&](int b, int row) { return t[b] >= 0 && k0 + row >= lo[b] && k0 + row <= p[b]; });
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int b = 0; b < QB; ++b) {
+        l[b] += __shfl_xor(l[b], 16);
+        l[b] += __shfl_xor(l[b], 32);
+        if (t[b] < 0) continue;
+        const int h = R.h0 + (a & ((1 << g.lgp) - 1));
+        const float inv = 1.f / l[b];
+        if (g.lse && gr == 0) g.lse[((int64_t)R.n * g.H + h) * g.T + t[b]] = m[b] + __builtin_amdgcn_logf(l[b]);
+        T* dst = reinterpret_cast<T*>(g.out) + (int64_t)t[b] * g.y_t + (int64_t)R.n * g.y_n + (int64_t)h * g.D;
+        bf16_t* low = g.low ? g.low + (((int64_t)t[b] * g.N + R.n) * g.H + h) * g.D : nullptr;
+#pragma unroll
+        for (int dt = 0; dt < L::NB; ++dt) {
+            float4_t y = o[b][dt];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) y[r] *= inv;
+            store4(dst, 16 * dt + 4 * gr, g.D, y);
+            if (L::ES == 2 && low) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) y[r] -= (float)(bf16_t)y[r];
+                store4(low, 16 * dt + 4 * gr, g.D, y);
+            }
+        }
+    }
+}
+
+// ---- backward, queries: dq, the sums of dA by bucket, and delta ---------------------------------------------------------------
+template <typename T, int DP, int QB>
+struct DqLds {
+    static constexpr int K = 0, V = Tile<T, DP>::BYTES, TAB = 2 * V, IDX = TAB + ATTN_TAB_ROOM * 4, FLAG = IDX + ATTN_TAB_ROOM * 4, BINS = FLAG + 16;
+};
+template <typename T, int DP, int QB>
+__global__ __launch_bounds__(ATTN_THREADS) void k_attn_dq(AttnArgs g) {
+    typedef Tile<T, DP> L;
+    typedef DqLds<T, DP, QB> M;
+    extern __shared__ __align__(16) unsigned char lds[];
+    float* tab = reinterpret_cast<float*>(lds + M::TAB);
+    int* idx = reinterpret_cast<int*>(lds + M::IDX);
+    int* flag = reinterpret_cast<int*>(lds + M::FLAG);
+    constexpr int BQ = 64 * QB;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, a = lane & 15, gr = lane >> 4, hh = lane & ((1 << g.lgp) - 1);
+    // every lane has bins of its own, one a bucket: no two lanes add to the same one, so the order of a bin's sum is the program's
+    float* bins = reinterpret_cast<float*>(lds + M::BINS) + (int64_t)wave * g.B * 64 + lane;
+    Rows R;
+    R.init(g, BQ);
+    int t[QB], p[QB], lo[QB];
+    float lse[QB], delta[QB];
+    uint4 qf[QB][L::KS], of[QB][L::KS];
+#pragma unroll
+    for (int b = 0; b < QB; ++b) {
+        const int r = R.r0 + (wave * QB + b) * 16 + a;
+        const bool in = r < R.rows;
+        t[b] = in ? r >> g.lgp : -1;
+        p[b] = in ? R.past + t[b] : -1;
+        lo[b] = in ? R.lo(g, p[b]) : kNever;
+        const int64_t at = in ? t[b] : 0, h = R.h0 + hh;
+        const T* src = reinterpret_cast<const T*>(g.q) + at * g.q_t + (int64_t)R.n * g.q_n + h * g.D;
+        const T* dsrc = reinterpret_cast<const T*>(g.dy) + at * g.y_t + (int64_t)R.n * g.y_n + h * g.D;
+        const T* ysrc = reinterpret_cast<const T*>(g.y) + at * g.y_t + (int64_t)R.n * g.y_n + h * g.D;
+        const bf16_t* lsrc = g.low ? g.low + ((at * g.N + R.n) * g.H + h) * g.D : nullptr;
+        float sum = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < L::KS; ++ks) {
+            const int d = ks * (64 / L::ES) + gr * L::VE, dc = d < g.D ? d : 0, left = in ? g.D - d : 0;
+            qf[b][ks] = piece(src + dc, left, g.whole);
+            of[b][ks] = piece(dsrc + dc, left, g.whole);
+            const uint4 yf = piece(ysrc + dc, left, g.whole);
+            const uint32_t wy[4] = {yf.x, yf.y, yf.z, yf.w}, wd[4] = {of[b][ks].x, of[b][ks].y, of[b][ks].z, of[b][ks].w};
+            if constexpr (L::ES == 2) {
+                const uint4 lf = piece(lsrc + dc, left, g.whole);
+                const uint32_t wl[4] = {lf.x, lf.y, lf.z, lf.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    sum = __builtin_fmaf(__uint_as_float(wd[i] << 16), __uint_as_float(wy[i] << 16) + __uint_as_float(wl[i] << 16), sum);
+                    sum = __builtin_fmaf(__uint_as_float(wd[i] & 0xffff0000u),
+                                         __uint_as_float(wy[i] & 0xffff0000u) + __uint_as_float(wl[i] & 0xffff0000u), sum);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum = __builtin_fmaf(__uint_as_float(wd[i]), __uint_as_float(wy[i]), sum);
+            }
+        }
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        delta[b] = sum;
+        lse[b] = 0.f;
+        if (in) {
+            const int64_t row = ((int64_t)R.n * g.H + h) * g.T + t[b];
+            lse[b] = g.lse[row];
+            if (gr == 0) g.delta[row] = sum;
+        }
+    }
+    const int first_p = R.past + (R.r0 >> g.lgp), each = (BQ >> g.lgp) + ATTN_K, far = first_p + (BQ >> g.lgp) - 1;
+    const int last_row = (R.r0 + BQ < R.rows ? R.r0 + BQ : R.rows) - 1;
+    const int k_begin = R.lo(g, first_p), k_end = R.past + (last_row >> g.lgp) + 1;
+    const int last_edge = g.table ? g.edges[g.B - 1] : 0;
+    const float beyond = g.table ? g.bias[(int64_t)(R.h0 + hh) * g.B + g.B - 1] * kLog2e : 0.f;
+    const T* kb = reinterpret_cast<const T*>(g.k) + (int64_t)R.n * g.k_n + (int64_t)R.kv * g.D;
+    const T* vb = reinterpret_cast<const T*>(g.v) + (int64_t)R.n * g.k_n + (int64_t)R.kv * g.D;
+    const float c = g.scale * kLog2e;
+    float outer = 0.f;  // sum of dA over tiles beyond the last edge
+    float4_t o[QB][L::NB];
+#pragma unroll
+    for (int b = 0; b < QB; ++b)
+#pragma unroll
+        for (int dt = 0; dt < L::NB; ++dt) o[b][dt] = float4_t{0.f, 0.f, 0.f, 0.f};
+    if (threadIdx.x == 0) *flag = 0;
+    if (g.part)
+        for (int b = 0; b < g.B; ++b) bins[b * 64] = 0.f;
+    Stage<T, DP> sk, sv;
+    Table st;
+    auto request = [&](int k0) {
+        sk.load(kb, g.k_t, k0, k_end, 0, g.D, g.whole);
+        sv.load(vb, g.k_t, k0, k_end, 0, g.D, g.whole);
+        if (g.table && first_p - (k0 + ATTN_K - 1) < last_edge) st.load<true>(g, R.h0, each, far - k0, -1);
+    };
+    request(k_begin);
+    __syncthreads();
+    for (int k0 = k_begin; k0 < k_end; k0 += ATTN_K) {
+        const bool near = g.table && first_p - (k0 + ATTN_K - 1) < last_edge;
+        float z = 0.f, zv = 0.f;
+        sk.put(lds + M::K, z);
+        sv.put(lds + M::V, zv);
+        if (z != 0.f) *flag = 1;
+        if (near) st.put<true>(g, each, tab, idx);
+        __syncthreads();
+        if (k0 + ATTN_K < k_end) request(k0 + ATTN_K);
+        bool any = false, all = true;
+#pragma unroll
+        for (int b = 0; b < QB; ++b) {
+            any |= p[b] >= k0 && lo[b] < k0 + ATTN_K;
+            all &= lo[b] <= k0 && p[b] >= k0 + ATTN_K - 1;
+        }
+        if (__any(any)) {
+            const bool whole = __all(all), wide = *flag != 0;
+            float4_t s[QB][4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                float4_t dp[QB];
+#pragma unroll
+                for (int b = 0; b < QB; ++b) s[b][x] = dp[b] = float4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int ks = 0; ks < L::KS; ++ks) {
+                    const uint4 f = L::rows(lds + M::K, 16 * x, ks), fv = L::rows(lds + M::V, 16 * x, ks);
+#pragma unroll
+                    for (int b = 0; b < QB; ++b) {
+                        Mma16<T>::run(f, qf[b][ks], s[b][x]);
+                        Mma16<T>::run(fv, of[b][ks], dp[b]);
+                    }
+                }
+#pragma unroll
+                for (int b = 0; b < QB; ++b) {
+                    const int place = hh * each + 4 * gr + (t[b] < 0 ? 0 : far - p[b]);
+                    const int from = lo[b] - k0 - 4 * gr;
+                    const uint32_t span = p[b] - lo[b];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float shift = near ? tab[place + 16 * x + r] : beyond;
+                        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][x][r], c, shift) - lse[b]);
+                        const bool see = whole || (t[b] >= 0 && (uint32_t)(16 * x + r - from) <= span);
+                        const float da = see ? e * (dp[b][r] - delta[b]) : 0.f;
+                        s[b][x][r] = da;
+                        if (g.part) {
+                            if (near) __builtin_amdgcn_ds_faddf((__attribute__((address_space(3))) float*)(bins + idx[place + 16 * x + r] * 64), da, 0, 0, false);
+                            else outer += da;
+                        }
+                    }
+                }
+            }
+            fold<T, DP, QB>(lds + M::K, s, o, wide,
+                            [&](int b, int row) { return t[b] >= 0 && k0 + row >= lo[b] && k0 + row <= p[b]; });
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int b = 0; b < QB; ++b) {
+        if (t[b] < 0) continue;
+        T* dst = reinterpret_cast<T*>(g.dq) + (int64_t)t[b] * g.q_t + (int64_t)R.n * g.q_n + (int64_t)(R.h0 + hh) * g.D;
+#pragma unroll
+        for (int dt = 0; dt < L::NB; ++dt) {
+            float4_t y = o[b][dt];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) y[r] *= g.scale;
+            store4(dst, 16 * dt + 4 * gr, g.D, y);
+        }
+    }
+    if (!g.part) return;
+    bins[(g.B - 1) * 64] += outer;
+    __syncthreads();
+    const float* from = reinterpret_cast<const float*>(lds + M::BINS) + lane;
+    const int64_t parts = (int64_t)g.N * g.tiles, mine = (int64_t)R.n * g.tiles + R.r0 / BQ;
+    for (int b = wave; b < g.B; b += 4) {
+        float sum = (from[b * 64] + from[(g.B + b) * 64]) + (from[(2 * g.B + b) * 64] + from[(3 * g.B + b) * 64]);
+        for (int o = 32; o >= 1 << g.lgp; o >>= 1) sum += __shfl_xor(sum, o);
+        if (lane < 1 << g.lgp) g.part[((int64_t)(R.h0 + lane) * g.B + b) * parts + mine] = sum;
+    }
+}
+
+// dbias[h, b]: the workgroups' sums, one block each
+__global__ __launch_bounds__(256) void k_attn_dbias(AttnArgs g) {
+    __shared__ float part[4];
+    const int64_t parts = (int64_t)g.N * g.tiles;
+    const float* src = g.part + (int64_t)blockIdx.x * parts;
+    float sum = 0.f;
+    for (int64_t i = threadIdx.x; i < parts; i += 256) sum += src[i];
+#pragma unroll
+    for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) g.dbias[blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
+}
+
+// ---- backward, keys: dk and dv ---------------------------------------------------------------------------------------------------
+template <typename T, int DP, int KB>
+struct DkvLds {
+    static constexpr int Q = 0, O = Tile<T, DP>::BYTES, TAB = 2 * O, INFO = TAB + ATTN_TAB_ROOM * 4, FLAG = INFO + 3 * ATTN_K * 4, TOTAL = FLAG + 16;
+};
+template <typename T, int DP, int KB>
+__global__ __launch_bounds__(ATTN_THREADS) void k_attn_dkv(AttnArgs g) {
+    typedef Tile<T, DP> L;
+    typedef DkvLds<T, DP, KB> M;
+    extern __shared__ __align__(16) unsigned char lds[];
+    float* tab = reinterpret_cast<float*>(lds + M::TAB);
+    float* row_lse = reinterpret_cast<float*>(lds + M::INFO);
+    float* row_delta = row_lse + ATTN_K;
+    int* row_lo = reinterpret_cast<int*>(row_delta + ATTN_K);
+    int* flag = reinterpret_cast<int*>(lds + M::FLAG);
+    constexpr int BK = 64 * KB;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, a = lane & 15, gr = lane >> 4;
+    const uint32_t w = work_item(g.total), rest = w / g.tiles;
+    Rows R;
+    R.n = rest / g.KV;
+    R.kv = rest % g.KV;
+    R.past = g.S - g.T;
+    const int k0 = (int)(w % g.tiles) * BK, k_last = (k0 + BK < g.S ? k0 + BK : g.S) - 1;
+    uint4 kf[KB][L::KS], vf[KB][L::KS];
+    int key[KB];
+    float4_t dk[KB][L::NB], dv[KB][L::NB];
+#pragma unroll
+    for (int b = 0; b < KB; ++b) {
+        key[b] = k0 + (wave * KB + b) * 16 + a;
+        const bool in = key[b] < g.S;
+        const int64_t at = (int64_t)(in ? key[b] : 0) * g.k_t + (int64_t)R.n * g.k_n + (int64_t)R.kv * g.D;
+#pragma unroll
+        for (int ks = 0; ks < L::KS; ++ks) {
+            const int d = ks * (64 / L::ES) + gr * L::VE, dc = d < g.D ? d : 0, left = in ? g.D - d : 0;
+            kf[b][ks] = piece(reinterpret_cast<const T*>(g.k) + at + dc, left, g.whole);
+            vf[b][ks] = piece(reinterpret_cast<const T*>(g.v) + at + dc, left, g.whole);
+        }
+#pragma unroll
+        for (int dt = 0; dt < L::NB; ++dt) dk[b][dt] = dv[b][dt] = float4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    if (threadIdx.x == 0) *flag = 0;
+    const int pack = 1 << g.lgp, share = g.H / g.KV, each = (ATTN_K >> g.lgp) + BK;
+    const int last_edge = g.table ? g.edges[g.B - 1] : 0;
+    const float c = g.scale * kLog2e;
+    const int t_begin = k0 > R.past ? k0 - R.past : 0;
+    // the last step that may see a key here; episodes end the walk earlier
+    const int64_t t_far = (int64_t)k_last + g.window - R.past;
+    const int t_end = t_far < g.T ? (int)t_far : g.T, r_begin = (t_begin << g.lgp) & ~3, r_end = t_end << g.lgp;
+    for (int h0 = R.kv * share; h0 < (R.kv + 1) * share; h0 += pack) {
+        const T* qb = reinterpret_cast<const T*>(g.q) + (int64_t)R.n * g.q_n + (int64_t)h0 * g.D;
+        const T* ob = reinterpret_cast<const T*>(g.dy) + (int64_t)R.n * g.y_n + (int64_t)h0 * g.D;
+        Stage<T, DP> sq, so;
+        Table st;
+        float i_lse = 0.f, i_delta = 0.f;
+        int i_lo = kNever;
+        float beyond[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) beyond[r] = g.table ? g.bias[(int64_t)(h0 + (r & (pack - 1))) * g.B + g.B - 1] * kLog2e : 0.f;
+        auto near_at = [&](int r0) { return g.table && R.past + (r0 >> g.lgp) - k_last < last_edge; };
+        auto request = [&](int r0) {
+            sq.load(qb, g.q_t, r0, r_end, g.lgp, g.D, g.whole);
+            so.load(ob, g.y_t, r0, r_end, g.lgp, g.D, g.whole);
+            if (near_at(r0)) st.load<false>(g, h0, each, R.past + (r0 >> g.lgp) - (k0 + BK - 1), 1);
+            if (threadIdx.x < ATTN_K) {
+                const int r = r0 + threadIdx.x;
+                i_lo = kNever;
+                if (r < r_end) {
+                    const int tt = r >> g.lgp;
+                    const int64_t row = ((int64_t)R.n * g.H + h0 + (r & (pack - 1))) * g.T + tt;
+                    i_lse = g.lse[row];
+                    i_delta = g.delta[row];
+                    i_lo = R.lo(g, R.past + tt);
+                }
+            }
+        };
+        if (r_begin < r_end) request(r_begin);
+        __syncthreads();
+        for (int r0 = r_begin; r0 < r_end; r0 += ATTN_K) {
+            const bool near = near_at(r0);
+            float z = 0.f;
+            sq.put(lds + M::Q, z);
+            so.put(lds + M::O, z);
+            if (z != 0.f) *flag = 1;
+            if (near) st.put<false>(g, each, tab, nullptr);
+            if (threadIdx.x < ATTN_K) {
+                row_lse[threadIdx.x] = i_lse;
+                row_delta[threadIdx.x] = i_delta;
+                row_lo[threadIdx.x] = i_lo;
+            }
+            __syncthreads();
+            if (row_lo[0] > k_last) break;  // (lo never falls: no later row sees a key here)
+            if (r0 + ATTN_K < r_end) request(r0 + ATTN_K);
+            const int p0 = R.past + (r0 >> g.lgp);
+            const bool whole = row_lo[ATTN_K - 1] <= k0 && p0 >= k0 + BK - 1, wide = *flag != 0;
+            float4_t s[KB][4], e[KB][4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                float4_t dp[KB];
+#pragma unroll
+                for (int b = 0; b < KB; ++b) s[b][x] = dp[b] = float4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int ks = 0; ks < L::KS; ++ks) {
+                    const uint4 f = L::rows(lds + M::Q, 16 * x, ks), fo = L::rows(lds + M::O, 16 * x, ks);
+#pragma unroll
+                    for (int b = 0; b < KB; ++b) {
+                        Mma16<T>::run(f, kf[b][ks], s[b][x]);
+                        Mma16<T>::run(fo, vf[b][ks], dp[b]);
+                    }
+                }
+                const int row = 16 * x + 4 * gr;
+                const float4_t lse = *reinterpret_cast<const float4_t*>(row_lse + row), delta = *reinterpret_cast<const float4_t*>(row_delta + row);
+                const int4 lo4 = *reinterpret_cast<const int4*>(row_lo + row);
+                const int lo[4] = {lo4.x, lo4.y, lo4.z, lo4.w};
+#pragma unroll
+                for (int b = 0; b < KB; ++b) {
+                    const float* place = tab + (row >> g.lgp) + (k0 + BK - 1 - key[b]);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int hh = r & (pack - 1), step = r >> g.lgp;
+                        const float shift = near ? place[hh * each + step] : beyond[r];
+                        const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][x][r], c, shift) - lse[r]);
+                        const bool see = whole || (lo[r] <= key[b] && key[b] <= p0 + (row >> g.lgp) + step);
+                        e[b][x][r] = see ? v : 0.f;
+                        s[b][x][r] = see ? v * (dp[b][r] - delta[r]) : 0.f;
+                    }
+                }
+            }
+            auto seen = [&](int b, int row) { return row_lo[row] <= key[b] && key[b] <= p0 + (row >> g.lgp); };
+            fold<T, DP, KB>(lds + M::O, e, dv, wide, seen);
+            fold<T, DP, KB>(lds + M::Q, s, dk, wide, seen);
+            __syncthreads();
+        }
+        __syncthreads();  // (a walk that ended early has not waited yet)
+    }
+#pragma unroll
+    for (int b = 0; b < KB; ++b) {
+        if (key[b] >= g.S) continue;
+        const int64_t at = (int64_t)key[b] * g.k_t + (int64_t)R.n * g.k_n + (int64_t)R.kv * g.D;
+#pragma unroll
+        for (int dt = 0; dt < L::NB; ++dt) {
+            float4_t y = dk[b][dt];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) y[r] *= g.scale;
+            store4(reinterpret_cast<T*>(g.dk) + at, 16 * dt + 4 * gr, g.D, y);
+            store4(reinterpret_cast<T*>(g.dv) + at, 16 * dt + 4 * gr, g.D, dv[b][dt]);
+        }
+    }
+}
+
+// ---- host -------------------------------------------------------------------------------------------------------------------
+// query heads of a tile: the power of two that divides the heads of a head of keys, up to 4
+static int pack_bits(const morlax_attn_dims& d) {
+    const int share = d.heads / d.kv_heads;
+    return share % 4 == 0 ? 2 : share % 2 == 0 ? 1 : 0;
+}
+static AttnArgs attn_args(const morlax_attn_dims& d) {
+    AttnArgs g = {};
+    g.T = d.T; g.S = d.S; g.N = d.N; g.H = d.heads; g.KV = d.kv_heads; g.D = d.head_dim; g.B = d.buckets; g.window = d.window;
+    g.reach = d.window < d.S ? d.window : d.S;
+    g.scale = d.scale;
+    g.whole = d.head_dim % (d.dtype ? 8 : 4) == 0;
+    g.lgp = pack_bits(d);
+    g.q_t = d.q_t; g.q_n = d.q_n; g.k_t = d.k_t; g.k_n = d.k_n; g.y_t = d.y_t; g.y_n = d.y_n;
+    return g;
+}
+template <typename P>
+static int64_t carve(P*& p, int64_t at, void* base, int64_t bytes) {
+    p = base ? reinterpret_cast<P*>(reinterpret_cast<char*>(base) + at) : nullptr;
+    return at + align_up(bytes, 256);
+}
+// episodes and the bias by distance: in `saved` where there is one, else in the workspace
+static int64_t attn_carve_prepared(AttnArgs& g, void* base, int64_t at) {
+    at = carve(g.lo, at, base, (int64_t)g.N * g.S * 4);
+    if (g.B) {
+        at = carve(g.table, at, base, (int64_t)g.H * g.reach * 4);
+        at = carve(g.bucket, at, base, (int64_t)g.reach * 4);
+    }
+    return at;
+}
+static int64_t attn_carve_saved(AttnArgs& g, const morlax_attn_dims& d, void* saved) {
+    int64_t at = carve(g.lse, 0, saved, (int64_t)g.N * g.H * g.T * 4);
+    if (d.dtype) at = carve(g.low, at, saved, (int64_t)g.T * g.N * g.H * g.D * 2);
+    return attn_carve_prepared(g, saved, at);
+}
+#define ATTN_ROWS 64  // rows of queries and keys of a workgroup
+static int64_t attn_carve_bwd(AttnArgs& g, void* ws) {
+    int64_t at = carve(g.delta, 0, ws, (int64_t)g.N * g.H * g.T * 4);
+    if (g.B) at = carve(g.part, at, ws, (int64_t)g.H * g.B * g.N * cdiv((int64_t)g.T << g.lgp, ATTN_ROWS) * 4);
+    return at;
+}
+int64_t attn_saved_bytes(const morlax_attn_dims& d) {
+    AttnArgs g = attn_args(d);
+    return attn_carve_saved(g, d, nullptr);
+}
+int64_t attn_ws_bytes(const morlax_attn_dims& d, bool back) {
+    AttnArgs g = attn_args(d);
+    return back ? attn_carve_bwd(g, nullptr) : attn_carve_prepared(g, nullptr, 0);
+}
+
+static int run_kernel(void (*kernel)(AttnArgs), AttnArgs& g, int64_t total, int lds, hipStream_t s) {
+    if (hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess) return 1;
+    g.total = (uint32_t)total;
+    kernel<<<dim3((uint32_t)total), ATTN_THREADS, lds, s>>>(g);
+    return 0;
+}
+template <typename T, int DP>
+static int attn_fwd_pass(AttnArgs& g, hipStream_t s) {
+    g.tiles = (int)cdiv((int64_t)g.T << g.lgp, 64);
+    return run_kernel(k_attn_fwd<T, DP, 1>, g, (int64_t)g.tiles * g.N * (g.H >> g.lgp), FwdLds<T, DP, 1>::TOTAL, s);
+}
+template <typename T, int DP>
+static int attn_bwd_pass(AttnArgs& g, hipStream_t s) {
+    g.tiles = (int)cdiv((int64_t)g.T << g.lgp, 64);
+    if (run_kernel(k_attn_dq<T, DP, 1>, g, (int64_t)g.tiles * g.N * (g.H >> g.lgp), DqLds<T, DP, 1>::BINS + (g.part ? g.B * 1024 : 0), s)) return 1;
+    if (g.part) k_attn_dbias<<<dim3((uint32_t)(g.H * g.B)), 256, 0, s>>>(g);
+    g.tiles = (int)cdiv(g.S, 64);
+    return run_kernel(k_attn_dkv<T, DP, 1>, g, (int64_t)g.tiles * g.N * g.KV, DkvLds<T, DP, 1>::TOTAL, s);
+}
+template <typename T>
+static int attn_pick(AttnArgs& g, bool back, hipStream_t s) {
+    if (g.D <= 32) return back ? attn_bwd_pass<T, 32>(g, s) : attn_fwd_pass<T, 32>(g, s);
+    if (g.D <= 64) return back ? attn_bwd_pass<T, 64>(g, s) : attn_fwd_pass<T, 64>(g, s);
+    return back ? attn_bwd_pass<T, 128>(g, s) : attn_fwd_pass<T, 128>(g, s);
+}
+
+int launch_attn_fwd(const morlax_attn_dims& d, const void* q, const void* k, const void* v, const float* bias, const int32_t* edges,
+                    const uint8_t* first, void* y, void* saved, void* ws, hipStream_t s) {
+    AttnArgs g = attn_args(d);
+    g.q = q; g.k = k; g.v = v; g.bias = bias; g.edges = edges; g.first = first; g.out = y;
+    if (saved) attn_carve_saved(g, d, saved);
+    else attn_carve_prepared(g, ws, 0);
+    if (!first) g.lo = nullptr;
+    if (first || g.B) {
+        int lgn = 0;
+        while (lgn < 4 && 1 << lgn < d.N) ++lgn;
+        const int64_t spans = first ? cdiv(d.N, 1 << lgn) : 0;
+        k_attn_prepare<<<dim3((uint32_t)(spans + (g.B ? cdiv(g.reach, 1024) : 0))), 1024, 0, s>>>(g, (int)spans, lgn);
+    }
+    return d.dtype ? attn_pick<bf16_t>(g, false, s) : attn_pick<float>(g, false, s);
+}
+int launch_attn_bwd(const morlax_attn_dims& d, const void* q, const void* k, const void* v, const float* bias, const int32_t* edges,
+                    const uint8_t* first, const void* y, const void* saved, const void* dy, void* dq, void* dk, void* dv, float* dbias, void* ws,
+                    hipStream_t s) {
+    AttnArgs g = attn_args(d);
+    g.q = q; g.k = k; g.v = v; g.bias = bias; g.edges = edges; g.first = first; g.y = y; g.dy = dy;
+    g.dq = dq; g.dk = dk; g.dv = dv; g.dbias = dbias;
+    attn_carve_saved(g, d, const_cast<void*>(saved));
+    attn_carve_bwd(g, ws);
+    if (!first) g.lo = nullptr;
+    if (!dbias) g.part = nullptr;
+    return d.dtype ? attn_pick<bf16_t>(g, true, s) : attn_pick<float>(g, true, s);
+}

@@ -1,0 +1,520 @@
+// A paged cache of keys and values, one step at a time: the pages' bookkeeping, and the attention of every environment's new step over it.
+#include "mlp_device.h"
+
+static int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+constexpr float kLog2e = 1.4426950408889634f;
+
+// ---- pages --------------------------------------------------------------------------------------------------------------
+// Integers only: a workgroup owns 256 environments, one a thread; ranks (whose turn at the queue it is, where a page that goes back lies) are
+// sums over the workgroups before, which a first launch leaves where there is more than one.  Bound by latency for a few thousand environments
+// (two dependent launches of some microseconds), by the copy of the tables where they go into other buffers.
+#define PAGES_E 256
+struct PagesArgs {
+    const uint8_t* first;
+    const int32_t *length_in, *table_in, *queue_in, *state_in;
+    int32_t *length, *table, *queue, *state, *slot;
+    int2* sums;        // of each workgroup: environments that need a page, pages that go back
+    int32_t* was;      // [2] the state before
+    int N, lgp, slots, pages, blocks;
+};
+
+// a wave's sum of the values before a lane's, and of all
+__device__ inline int2 wave_before(int v) {
+    const int lane = threadIdx.x & 63;
+    int s = v;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int u = __shfl_up(s, o);
+        if (lane >= o) s += u;
+    }
+    return make_int2(s - v, __shfl(s, 63));
+}
+// the same over a workgroup of 256
+__device__ inline int2 block_before(int v, int* lds4) {
+    const int2 w = wave_before(v);
+    const int wave = threadIdx.x >> 6;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds4[wave] = w.y;
+    __syncthreads();
+    int before = w.x, all = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (i < wave) before += lds4[i];
+        all += lds4[i];
+    }
+    return make_int2(before, all);
+}
+
+struct PageOf {  // what one environment does
+    bool live, begins, needs;
+    int at, column, entry;
+    __device__ inline void look(const PagesArgs& g, int n) {
+        live = begins = needs = false;
+        at = column = 0;
+        entry = -1;
+        if (n >= g.N) return;
+        at = g.length_in[n];
+        live = at >= 0;
+        if (!live) return;
+        begins = g.first && g.first[n];
+        if (begins) at = 0;
+        column = (int)((uint32_t)(at >> g.lgp) % (uint32_t)g.slots);
+        entry = g.table_in[(int64_t)n * g.slots + column];
+        needs = (uint32_t)entry >= (uint32_t)g.pages;
+    }
+};
+// The pages that the environments of this wave give back, an environment at a time, all lanes along its slots: each(place among the wave's, page);
+// returns how many for this lane's environment.
+template <typename F>
+__device__ inline int wave_gives(const PagesArgs& g, int n, bool begins, F each) {
+    const int lane = threadIdx.x & 63;
+    uint64_t todo = __ballot(begins);
+    int mine = 0, done = 0;
+    while (todo) {
+        const int who = __ffsll((long long)todo) - 1;
+        todo &= todo - 1;
+        const int32_t* row = g.table_in + (int64_t)__shfl(n, who) * g.slots;
+        int count = 0;
+        for (int j0 = 1; j0 < g.slots; j0 += 64) {
+            const int j = j0 + lane;
+            const int e = j < g.slots ? row[j] : -1;
+            const bool held = (uint32_t)e < (uint32_t)g.pages;
+            const uint64_t set = __ballot(held);
+            if (held) each(done + count + __popcll(set & (((uint64_t)1 << lane) - 1)), e);
+            count += __popcll(set);
+        }
+        if (lane == who) mine = count;
+        done += count;
+    }
+    return mine;
+}
+
+__global__ __launch_bounds__(PAGES_E) void k_pages_count(PagesArgs g) {
+    __shared__ int part[4];
+    const int n = blockIdx.x * PAGES_E + threadIdx.x;
+    PageOf e;
+    e.look(g, n);
+    const int gives = wave_gives(g, n, e.begins, [](int, int) {});
+    const int2 needs = block_before(e.needs, part), back = block_before(gives, part);
+    if (threadIdx.x == 0) {
+        g.sums[blockIdx.x] = make_int2(needs.y, back.y);
+        if (blockIdx.x == 0) {
+            g.was[0] = g.state_in[0];
+            g.was[1] = g.state_in[1];
+        }
+    }
+}
+
+__global__ __launch_bounds__(PAGES_E) void k_pages_apply(PagesArgs g) {
+    __shared__ int part[4], wave_back[4];
+    __shared__ int32_t column[PAGES_E], entry[PAGES_E];
+    const int n0 = blockIdx.x * PAGES_E, n = n0 + threadIdx.x, wave = threadIdx.x >> 6;
+    PageOf e;
+    e.look(g, n);
+    int gives = 0;  // (of the wave; each pushes them below, once the place is known)
+    gives = wave_gives(g, n, e.begins, [](int, int) {});
+    const int2 needs = block_before(e.needs, part), back = block_before(gives, part);
+    int needs_before = 0, back_before = 0, needs_all = needs.y, back_all = back.y;
+    int head, count;
+    if (g.blocks > 1) {
+        int a = 0, b = 0, c = 0, d = 0;
+        for (int i = threadIdx.x; i < g.blocks; i += PAGES_E) {
+            const int2 s = g.sums[i];
+            if (i < (int)blockIdx.x) { a += s.x; b += s.y; }
+            c += s.x;
+            d += s.y;
+        }
+        needs_before = block_before(a, part).y;
+        back_before = block_before(b, part).y;
+        needs_all = block_before(c, part).y;
+        back_all = block_before(d, part).y;
+        head = g.was[0];
+        count = g.was[1];
+    } else {
+        head = g.state_in[0];
+        count = g.state_in[1];
+        __syncthreads();  // (the state may be its own output)
+    }
+    head = (int)((uint32_t)head % (uint32_t)g.pages);
+    count = count < 0 ? 0 : count > g.pages ? g.pages : count;
+    auto ring = [&](int64_t i) { return (int)((uint64_t)i % (uint32_t)g.pages); };
+    const int rank = needs_before + needs.x;
+    if (e.needs && rank < count) e.entry = g.queue_in[ring((int64_t)head + rank)];
+    column[threadIdx.x] = !e.live ? -1 : e.begins ? -2 - e.column : e.column;  // (an episode that begins is at slot 0)
+    entry[threadIdx.x] = e.entry;
+    if ((threadIdx.x & 63) == 0) wave_back[wave] = back.x;
+    if (n < g.N) {
+        const bool has = (uint32_t)e.entry < (uint32_t)g.pages;
+        g.length[n] = e.live ? e.at + 1 : e.at;
+        g.slot[n] = e.live && has ? (e.entry << g.lgp) + (e.at & ((1 << g.lgp) - 1)) : -1;
+    }
+    const int64_t tail = (int64_t)head + count + back_before;
+    __syncthreads();
+    const int64_t base = tail + wave_back[wave];
+    wave_gives(g, n, e.begins, [&](int at, int page) { g.queue[ring(base + at)] = page; });
+    __syncthreads();  // (the rows of episodes that begin have been read: they may be written)
+    const int here = g.N - n0 < PAGES_E ? g.N - n0 : PAGES_E;
+    if (g.table != g.table_in) {
+        const int64_t from = (int64_t)n0 * g.slots;
+        for (int64_t i = threadIdx.x; i < (int64_t)here * g.slots; i += PAGES_E) {
+            const int r = (int)(i / g.slots), j = (int)(i - (int64_t)r * g.slots), c = column[r];
+            int v = g.table_in[from + i];
+            if (c <= -2) v = j == 0 ? entry[r] : -1;
+            else if (c == j) v = entry[r];
+            g.table[from + i] = v;
+        }
+    } else if (n < g.N && e.live) {
+        if (e.begins)
+            for (int j = 1; j < g.slots; ++j) g.table[(int64_t)n * g.slots + j] = -1;
+        g.table[(int64_t)n * g.slots + e.column] = e.entry;
+    }
+    if (g.queue != g.queue_in) {  // what no page went back to
+        const int64_t per = ((int64_t)g.pages + g.blocks - 1) / g.blocks, i0 = blockIdx.x * per, i1 = i0 + per < g.pages ? i0 + per : g.pages;
+        const int tail0 = ring((int64_t)head + count);
+        for (int64_t i = i0 + threadIdx.x; i < i1; i += PAGES_E) {
+            const int64_t d = i - tail0 < 0 ? i - tail0 + g.pages : i - tail0;
+            if (d >= back_all) g.queue[i] = g.queue_in[i];
+        }
+    }
+    if ((int)blockIdx.x == g.blocks - 1 && threadIdx.x == 0) {
+        const int taken = needs_all < count ? needs_all : count;
+        const int64_t left = (int64_t)count - taken + back_all;
+        g.state[0] = ring((int64_t)head + taken);
+        g.state[1] = left > g.pages ? g.pages : (int)left;
+    }
+}
+
+// ---- one new step over the cache ------------------------------------------------------------------------------------------------
+// Bound: HBM, every key and value of the window once (GQ query heads share what is read).  A key lies along LPK lanes, 16 bytes each, so a
+// wave takes 64 / LPK keys at a time; every group of LPK lanes carries a running maximum, sum and output of its own, which are joined once at
+// the end, across the groups, the waves and, where few environments have to fill the chip, the workgroups that share a cache's length.
+struct StepArgs {
+    const void *q, *k, *v;
+    const float* bias;
+    const int32_t *edges, *table, *length;
+    void *k_cache, *v_cache, *y;
+    float* part_o;   // [N, H, splits, D]
+    float2* part_m;  // [N, H, splits] maximum (in units of log2) and sum
+    float scale;
+    int N, H, KV, D, B, window, lgp, slots, pages, splits, chunks, whole;
+    int64_t q_n, k_n, y_n;
+};
+
+typedef uint32_t piece_t __attribute__((ext_vector_type(4), aligned(2)));
+// 16 bytes of elements from p on (aligned to an element), those from `n` on zero; whole: n is a multiple of as many
+template <typename T>
+__device__ inline uint4 piece(const T* p, int n, bool whole) {
+    constexpr int VE = 16 / sizeof(T);
+    if (whole || n >= VE) {
+        if (n <= 0) return make_uint4(0, 0, 0, 0);
+        const piece_t u = *reinterpret_cast<const piece_t*>(p);
+        return make_uint4(u[0], u[1], u[2], u[3]);
+    }
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < VE; ++i) {
+        if (i >= n) break;
+        if constexpr (sizeof(T) == 2) w[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << (16 * (i & 1));
+        else w[i] = reinterpret_cast<const uint32_t*>(p)[i];
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <typename T>
+__device__ inline float element(const uint4& u, int i) {  // i known after unrolling
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    else return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+}
+
+#define STEP_U 4  // keys that a group of lanes requests together
+
+template <typename T, int DP, int GQ>
+__global__ __launch_bounds__(256) void k_attn_step(StepArgs g) {
+    constexpr int VE = 16 / sizeof(T), LPK = DP / VE, KPW = 64 / LPK, STRIDE = 4 * KPW * STEP_U;
+    __shared__ float bias[GQ][64];
+    __shared__ int32_t edges[64];
+    __shared__ float2 wave_m[4][GQ];
+    __shared__ float wave_o[4][GQ][DP];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane % LPK, key = lane / LPK;
+    const int split = blockIdx.x % g.splits, rest = blockIdx.x / g.splits, chunk = rest % g.chunks, rest2 = rest / g.chunks;
+    const int kv = rest2 % g.KV, n = rest2 / g.KV, share = g.H / g.KV, h0 = kv * share + chunk * GQ, heads = share - chunk * GQ < GQ ? share - chunk * GQ : GQ;
+    const int length = g.length[n], pos = length - 1;
+    const int d = sub * VE, left = g.D - d, dc = left > 0 ? d : 0;
+    T* y = reinterpret_cast<T*>(g.y) + (int64_t)n * g.y_n;
+    if (length <= 0) {
+        if (g.splits == 1)
+            for (int i = threadIdx.x; i < heads * g.D; i += 256) y[(int64_t)h0 * g.D + i] = (T)0.f;
+        return;
+    }
+    const int begin = pos - g.window + 1 > 0 ? pos - g.window + 1 : 0;
+    // this workgroup's part of the window, a whole number of keys of its waves
+    const int count = pos - begin + 1, per = ((count + g.splits - 1) / g.splits + 4 * KPW - 1) / (4 * KPW) * (4 * KPW);
+    const int64_t s0 = begin + (int64_t)split * per;
+    const int s1 = s0 + per < pos + 1 ? (int)(s0 + per) : pos + 1;
+    const int32_t* table = g.table + (int64_t)n * g.slots;
+    const int64_t row = (int64_t)g.KV * g.D;
+    const T *kn = reinterpret_cast<const T*>(g.k) + (int64_t)n * g.k_n + (int64_t)kv * g.D, *vn = reinterpret_cast<const T*>(g.v) + (int64_t)n * g.k_n + (int64_t)kv * g.D;
+    T *kc = reinterpret_cast<T*>(g.k_cache) + (int64_t)kv * g.D, *vc = reinterpret_cast<T*>(g.v_cache) + (int64_t)kv * g.D;
+    const int slot0 = (begin >> g.lgp) % g.slots, page0 = begin >> g.lgp, in_page = (1 << g.lgp) - 1;
+    auto slot_of = [&](int s) {  // (the window's pages lie once round the slots at most)
+        const int j = slot0 + (s >> g.lgp) - page0;
+        return j >= g.slots ? j - g.slots : j;
+    };
+    if (split == 0 && chunk == 0) {  // the step goes into its page; no workgroup reads it there
+        const int id = table[slot_of(pos)];
+        if ((uint32_t)id < (uint32_t)g.pages) {
+            const int64_t at = (((int64_t)id << g.lgp) + (pos & in_page)) * row;
+            for (int i = threadIdx.x; i < g.D; i += 256) {
+                kc[at + i] = kn[i];
+                vc[at + i] = vn[i];
+            }
+        }
+    }
+    float qf[GQ][VE];
+#pragma unroll
+    for (int i = 0; i < GQ; ++i) {
+        const uint4 u = piece(reinterpret_cast<const T*>(g.q) + (int64_t)n * g.q_n + (int64_t)(h0 + (i < heads ? i : 0)) * g.D + dc, left, g.whole);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) qf[i][e] = element<T>(u, e);
+    }
+    int last_edge = 0;
+    if (g.B) {
+        if (threadIdx.x < g.B) edges[threadIdx.x] = g.edges[threadIdx.x];
+        for (int i = threadIdx.x; i < GQ * g.B; i += 256) bias[i / g.B][i % g.B] = i / g.B < heads ? g.bias[(int64_t)(h0 + i / g.B) * g.B + i % g.B] * kLog2e : 0.f;
+        last_edge = g.edges[g.B - 1];
+    }
+    __syncthreads();
+    const float c = g.scale * kLog2e;
+    float m[GQ], l[GQ], o[GQ][VE];
+#pragma unroll
+    for (int i = 0; i < GQ; ++i) {
+        m[i] = -__builtin_inff();
+        l[i] = 0.f;
+#pragma unroll
+        for (int e = 0; e < VE; ++e) o[i][e] = 0.f;
+    }
+    const int my = wave * KPW + key;
+    int id[STEP_U];
+    auto look = [&](int64_t at) {
+#pragma unroll
+        for (int u = 0; u < STEP_U; ++u) {
+            const int64_t s = at + my + u * 4 * KPW;
+            id[u] = s < s1 ? table[slot_of((int)s)] : -1;
+        }
+    };
+    if (s0 < s1) look(s0);
+    for (int64_t at = s0; at < s1; at += STRIDE) {
+        uint4 ku[STEP_U], vu[STEP_U];
+        bool in[STEP_U];
+#pragma unroll
+        for (int u = 0; u < STEP_U; ++u) {
+            const int64_t s = at + my + u * 4 * KPW;
+            const bool now = s == pos;
+            in[u] = s < s1 && (now || (uint32_t)id[u] < (uint32_t)g.pages);
+            const int64_t off = (((int64_t)id[u] << g.lgp) + ((int)s & in_page)) * row;
+            const T *kp = now || !in[u] ? kn : kc + off, *vp = now || !in[u] ? vn : vc + off;
+            ku[u] = piece(kp + dc, in[u] ? left : 0, g.whole);
+            vu[u] = piece(vp + dc, in[u] ? left : 0, g.whole);
+        }
+        if (at + STRIDE < s1) look(at + STRIDE);
+        float s[STEP_U][GQ];
+#pragma unroll
+        for (int u = 0; u < STEP_U; ++u) {
+#pragma unroll
+            for (int i = 0; i < GQ; ++i) s[u][i] = 0.f;
+#pragma unroll
+            for (int e = 0; e < VE; ++e) {
+                const float x = element<T>(ku[u], e);
+#pragma unroll
+                for (int i = 0; i < GQ; ++i) s[u][i] = __builtin_fmaf(x, qf[i][e], s[u][i]);
+            }
+#pragma unroll
+            for (int x = LPK / 2; x; x >>= 1)
+#pragma unroll
+                for (int i = 0; i < GQ; ++i) s[u][i] += __shfl_xor(s[u][i], x);
+            int b = g.B - 1;
+            if (g.B) {
+                const int dist = pos - (int)(at + my + u * 4 * KPW);
+                if (dist < last_edge) {
+                    b = 0;
+                    for (int j = 1; j < g.B; ++j) b += edges[j] <= dist;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < GQ; ++i) {
+                const float a = __builtin_fmaf(s[u][i], c, g.B ? bias[i][b] : 0.f);
+                s[u][i] = in[u] ? a : -__builtin_inff();
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < GQ; ++i) {
+            float top = m[i];
+#pragma unroll
+            for (int u = 0; u < STEP_U; ++u) top = fmaxf(top, s[u][i]);
+            const float base = top == -__builtin_inff() ? 0.f : top, fade = __builtin_amdgcn_exp2f(m[i] - base);
+            m[i] = top;
+            l[i] *= fade;
+#pragma unroll
+            for (int e = 0; e < VE; ++e) o[i][e] *= fade;
+#pragma unroll
+            for (int u = 0; u < STEP_U; ++u) {
+                const float p = __builtin_amdgcn_exp2f(s[u][i] - base);
+                l[i] += p;
+#pragma unroll
+                for (int e = 0; e < VE; ++e) o[i][e] = __builtin_fmaf(p, element<T>(vu[u], e), o[i][e]);
+            }
+        }
+    }
+    // joined: the groups of a wave, then the waves
+#pragma unroll
+    for (int i = 0; i < GQ; ++i) {
+        float top = m[i];
+#pragma unroll
+        for (int x = LPK; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x));
+        const float base = top == -__builtin_inff() ? 0.f : top, w = __builtin_amdgcn_exp2f(m[i] - base);
+        l[i] *= w;
+#pragma unroll
+        for (int x = LPK; x < 64; x <<= 1) l[i] += __shfl_xor(l[i], x);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) {
+            o[i][e] *= w;
+#pragma unroll
+            for (int x = LPK; x < 64; x <<= 1) o[i][e] += __shfl_xor(o[i][e], x);
+        }
+        if (lane < LPK) {
+            if (lane == 0) wave_m[wave][i] = make_float2(top, l[i]);
+#pragma unroll
+            for (int e = 0; e < VE; ++e) wave_o[wave][i][d + e] = o[i][e];
+        }
+    }
+    __syncthreads();
+    for (int x = threadIdx.x; x < heads * DP; x += 256) {
+        const int i = x / DP, dd = x % DP;
+        if (dd >= g.D) continue;
+        float top = wave_m[0][i].x;
+#pragma unroll
+        for (int w = 1; w < 4; ++w) top = fmaxf(top, wave_m[w][i].x);
+        const float base = top == -__builtin_inff() ? 0.f : top;
+        float sum = 0.f, out = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float f = __builtin_amdgcn_exp2f(wave_m[w][i].x - base);
+            sum = __builtin_fmaf(f, wave_m[w][i].y, sum);
+            out = __builtin_fmaf(f, wave_o[w][i][dd], out);
+        }
+        if (g.splits == 1) {
+            y[(int64_t)(h0 + i) * g.D + dd] = cvt<T>(out / sum);
+        } else {
+            const int64_t at = ((int64_t)n * g.H + h0 + i) * g.splits + split;
+            if (dd == 0) g.part_m[at] = make_float2(top, sum);
+            g.part_o[at * g.D + dd] = out;
+        }
+    }
+}
+
+// the parts of an environment and head, joined: one wave each
+template <typename T>
+__global__ __launch_bounds__(256) void k_attn_join(StepArgs g) {
+    const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    if (i >= (int64_t)g.N * g.H) return;
+    const int n = (int)(i / g.H), h = (int)(i % g.H);
+    T* y = reinterpret_cast<T*>(g.y) + (int64_t)n * g.y_n + (int64_t)h * g.D;
+    if (g.length[n] <= 0) {
+        for (int d = lane; d < g.D; d += 64) y[d] = (T)0.f;
+        return;
+    }
+    const float2* pm = g.part_m + i * g.splits;
+    const float* po = g.part_o + i * g.splits * g.D;
+    float top = -__builtin_inff();
+    for (int s = lane; s < g.splits; s += 64) top = fmaxf(top, pm[s].x);
+#pragma unroll
+    for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    const float base = top == -__builtin_inff() ? 0.f : top;
+    float sum = 0.f, out[2] = {0.f, 0.f};
+    const int d0 = lane < g.D ? lane : 0, d1 = lane + 64 < g.D ? lane + 64 : 0;
+#pragma unroll 4
+    for (int s = 0; s < g.splits; ++s) {
+        const float2 p = pm[s];
+        const float f = __builtin_amdgcn_exp2f(p.x - base);
+        sum = __builtin_fmaf(f, p.y, sum);
+        out[0] = __builtin_fmaf(f, po[(int64_t)s * g.D + d0], out[0]);
+        out[1] = __builtin_fmaf(f, po[(int64_t)s * g.D + d1], out[1]);
+    }
+    if (lane < g.D) y[lane] = cvt<T>(out[0] / sum);
+    if (lane + 64 < g.D) y[lane + 64] = cvt<T>(out[1] / sum);
+}
+
+// ---- host ---------------------------------------------------------------------------------------------------------------------------
+static int log2_of(int v) {
+    int l = 0;
+    while (1 << l < v) ++l;
+    return l;
+}
+static int64_t pages_carve(PagesArgs& g, const morlax_pages_dims& d, void* ws) {
+    g.N = d.N; g.lgp = log2_of(d.page); g.slots = d.slots; g.pages = d.pages; g.blocks = (int)cdiv(d.N, PAGES_E);
+    g.was = reinterpret_cast<int32_t*>(ws);
+    g.sums = reinterpret_cast<int2*>(reinterpret_cast<char*>(ws) + 256);
+    return 256 + (int64_t)g.blocks * 8;
+}
+int64_t pages_ws_bytes(const morlax_pages_dims& d) {
+    PagesArgs g = {};
+    return pages_carve(g, d, nullptr);
+}
+void launch_cache_pages(const morlax_pages_dims& d, const uint8_t* first, const int32_t* length_in, const int32_t* table_in, const int32_t* queue_in,
+                        const int32_t* state_in, int32_t* length, int32_t* table, int32_t* queue, int32_t* state, int32_t* slot, void* ws, hipStream_t s) {
+    PagesArgs g = {};
+    g.first = first; g.length_in = length_in; g.table_in = table_in; g.queue_in = queue_in; g.state_in = state_in;
+    g.length = length; g.table = table; g.queue = queue; g.state = state; g.slot = slot;
+    pages_carve(g, d, ws);
+    if (g.blocks > 1) k_pages_count<<<dim3(g.blocks), PAGES_E, 0, s>>>(g);
+    k_pages_apply<<<dim3(g.blocks), PAGES_E, 0, s>>>(g);
+}
+
+static int heads_of_workgroup(int share) { return share >= 5 ? 8 : share >= 3 ? 4 : share; }
+static int64_t step_carve(StepArgs& g, const morlax_cache_dims& d, void* ws) {
+    g.N = d.N; g.H = d.heads; g.KV = d.kv_heads; g.D = d.head_dim; g.B = d.buckets; g.window = d.window; g.lgp = log2_of(d.page);
+    g.slots = d.slots; g.pages = d.pages; g.scale = d.scale; g.whole = d.head_dim % (d.dtype ? 8 : 4) == 0;
+    g.q_n = d.q_n; g.k_n = d.k_n; g.y_n = d.y_n;
+    const int share = d.heads / d.kv_heads;
+    g.chunks = (int)cdiv(share, heads_of_workgroup(share));
+    // few environments: the window in as many parts as fill the chip, of 128 keys at least
+    const int64_t blocks = (int64_t)d.N * d.kv_heads * g.chunks;
+    int64_t splits = 1024 / blocks, most = cdiv(d.window, 128);
+    splits = splits < most ? splits : most;
+    g.splits = splits < 1 ? 1 : (int)splits;
+    if (g.splits == 1) return 16;
+    g.part_m = reinterpret_cast<float2*>(ws);
+    const int64_t m = align_up((int64_t)d.N * d.heads * g.splits * 8, 256);
+    g.part_o = reinterpret_cast<float*>(reinterpret_cast<char*>(ws) + m);
+    return m + (int64_t)d.N * d.heads * g.splits * d.head_dim * 4;
+}
+int64_t attn_step_ws_bytes(const morlax_cache_dims& d) {
+    StepArgs g = {};
+    return step_carve(g, d, nullptr);
+}
+template <typename T, int DP>
+static void step_pass(const StepArgs& g, hipStream_t s) {
+    const dim3 grid((uint32_t)((int64_t)g.splits * g.chunks * g.KV * g.N));
+    switch (heads_of_workgroup(g.H / g.KV)) {
+        case 1: k_attn_step<T, DP, 1><<<grid, 256, 0, s>>>(g); break;
+        case 2: k_attn_step<T, DP, 2><<<grid, 256, 0, s>>>(g); break;
+        case 4: k_attn_step<T, DP, 4><<<grid, 256, 0, s>>>(g); break;
+        default: k_attn_step<T, DP, 8><<<grid, 256, 0, s>>>(g);
+    }
+    if (g.splits > 1) k_attn_join<T><<<dim3((uint32_t)cdiv((int64_t)g.N * g.H, 4)), 256, 0, s>>>(g);
+}
+template <typename T>
+static void step_pick(const StepArgs& g, hipStream_t s) {
+    if (g.D <= 32) step_pass<T, 32>(g, s);
+    else if (g.D <= 64) step_pass<T, 64>(g, s);
+    else step_pass<T, 128>(g, s);
+}
+void launch_attn_step(const morlax_cache_dims& d, const void* q, const void* k, const void* v, const float* bias, const int32_t* edges,
+                      const int32_t* table, const int32_t* length, void* k_cache, void* v_cache, void* y, void* ws, hipStream_t s) {
+    StepArgs g = {};
+    step_carve(g, d, ws);
+    g.q = q; g.k = k; g.v = v; g.bias = bias; g.edges = edges; g.table = table; g.length = length; g.k_cache = k_cache; g.v_cache = v_cache; g.y = y;
+    if (d.dtype) step_pick<bf16_t>(g, s);
+    else step_pick<float>(g, s);
+}

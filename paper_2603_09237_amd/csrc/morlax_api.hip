@@ -704,3 +704,213 @@ extern "C" int morlax_memory_step(const morlax_scan_dims* dims, int32_t width, c
                        (hipStream_t)stream);
     return finish(who);
 }
+
+// ---- memory by attention --------------------------------------------------------------------------------------------
+// what attention over a segment and over a cache have in common
+static int check_heads(int N, int heads, int kv_heads, int head_dim, int buckets, int window, int dtype, float scale, const char* who) {
+    if (N < 1 || heads < 1 || kv_heads < 1 || head_dim < 1 || window < 1 || buckets < 0)
+        return fail(MORLAX_ERR_SHAPE, "%s: N, heads, kv_heads, head_dim and window must be >= 1, buckets >= 0", who);
+    if (heads % kv_heads != 0) return fail(MORLAX_ERR_SHAPE, "%s: kv_heads = %d must divide heads = %d", who, kv_heads, heads);
+    if (dtype != 0 && dtype != 1) return fail(MORLAX_ERR_UNSUPPORTED, "%s: dtype must be 0 (fp32) or 1 (bf16)", who);
+    if (head_dim > 128 || heads > 1024 || buckets > 64)
+        return fail(MORLAX_ERR_UNSUPPORTED, "%s: head_dim must be <= 128, heads <= 1024, buckets <= 64", who);
+    if (!std::isfinite(scale)) return fail(MORLAX_ERR_SHAPE, "%s: scale must be finite", who);
+    return MORLAX_OK;
+}
+static int check_attn(const morlax_attn_dims* d, const char* who) {
+    if (!d) return fail(MORLAX_ERR_NULL, "%s: dims is NULL", who);
+    const int rc = check_heads(d->N, d->heads, d->kv_heads, d->head_dim, d->buckets, d->window, d->dtype, d->scale, who);
+    if (rc != MORLAX_OK) return rc;
+    if (d->T < 1 || d->S < d->T) return fail(MORLAX_ERR_SHAPE, "%s: T must be >= 1 and S >= T", who);
+    if (d->S > 1 << 20) return fail(MORLAX_ERR_UNSUPPORTED, "%s: S must be <= 2^20", who);
+    const int64_t D = d->head_dim, q = d->heads * D, k = d->kv_heads * D;
+    if ((d->N > 1 && (d->q_n < q || d->y_n < q || d->k_n < k)) || (d->T > 1 && (d->q_t < q || d->y_t < q)) || (d->S > 1 && d->k_t < k))
+        return fail(MORLAX_ERR_SHAPE, "%s: a stride is shorter than a row", who);
+    const int64_t rows = (int64_t)d->N * d->heads * ((d->T + 63) / 64), keys = (int64_t)d->N * d->kv_heads * ((d->S + 63) / 64);
+    if (rows >= 1 << 24 || keys >= 1 << 24 || rows * d->buckets >= (int64_t)1 << 38)
+        return fail(MORLAX_ERR_UNSUPPORTED, "%s: N * heads * ceil(T / 64) and N * kv_heads * ceil(S / 64) must stay below 2^24", who);
+    return MORLAX_OK;
+}
+static int check_bias(int buckets, const float* bias, const int32_t* edges, const char* who) {
+    if (buckets == 0) return MORLAX_OK;
+    REQ(bias, who); REQ(edges, who);
+    return MORLAX_OK;
+}
+extern "C" int64_t morlax_attn_saved_bytes(const morlax_attn_dims* d) {
+    if (check_attn(d, "morlax_attn_saved_bytes") != MORLAX_OK) return -1;
+    return attn_saved_bytes(*d);
+}
+extern "C" int64_t morlax_attn_workspace_bytes(const morlax_attn_dims* d, int32_t backward) {
+    if (check_attn(d, "morlax_attn_workspace_bytes") != MORLAX_OK) return -1;
+    return attn_ws_bytes(*d, backward != 0);
+}
+extern "C" int morlax_attn_fwd(const morlax_attn_dims* dims, const void* q, const void* k, const void* v, const float* bias, const int32_t* edges,
+                               const uint8_t* first, void* y, void* saved, void* ws, int64_t ws_bytes, void* stream) {
+    const char* who = "morlax_attn_fwd";
+    int rc = check_attn(dims, who);
+    if (rc != MORLAX_OK) return rc;
+    STRIDED(q, dims->dtype, who); STRIDED(k, dims->dtype, who); STRIDED(v, dims->dtype, who); STRIDED(y, dims->dtype, who);
+    if ((rc = check_bias(dims->buckets, bias, edges, who)) != MORLAX_OK) return rc;
+    OPT(saved, who);
+    if (y == q || y == k || y == v) return fail(MORLAX_ERR_SHAPE, "%s: an output is its input", who);
+    if (!saved) WS(ws, ws_bytes, attn_ws_bytes(*dims, false), who);
+    if (launch_attn_fwd(*dims, q, k, v, bias, edges, first, y, saved, ws, (hipStream_t)stream) != 0)
+        return fail(MORLAX_ERR_HIP, "%s: the kernel's LDS is not available on this device", who);
+    return finish(who);
+}
+extern "C" int morlax_attn_bwd(const morlax_attn_dims* dims, const void* q, const void* k, const void* v, const float* bias, const int32_t* edges,
+                               const uint8_t* first, const void* y, const void* saved, const void* dy, void* dq, void* dk, void* dv,
+                               float* dbias, void* ws, int64_t ws_bytes, void* stream) {
+    const char* who = "morlax_attn_bwd";
+    int rc = check_attn(dims, who);
+    if (rc != MORLAX_OK) return rc;
+    STRIDED(q, dims->dtype, who); STRIDED(k, dims->dtype, who); STRIDED(v, dims->dtype, who); STRIDED(y, dims->dtype, who);
+    STRIDED(dy, dims->dtype, who); STRIDED(dq, dims->dtype, who); STRIDED(dk, dims->dtype, who); STRIDED(dv, dims->dtype, who);
+    if ((rc = check_bias(dims->buckets, bias, edges, who)) != MORLAX_OK) return rc;
+    REQ(saved, who); OPT(dbias, who);
+    const void* in[] = {q, k, v, y, dy};
+    for (const void* p : in)
+        if (p == dq || p == dk || p == dv) return fail(MORLAX_ERR_SHAPE, "%s: an output is its input", who);
+    if (dq == dk || dq == dv || dk == dv) return fail(MORLAX_ERR_SHAPE, "%s: two outputs are the same", who);
+    WS(ws, ws_bytes, attn_ws_bytes(*dims, true), who);
+    if (launch_attn_bwd(*dims, q, k, v, bias, edges, first, y, saved, dy, dq, dk, dv, dims->buckets ? dbias : nullptr, ws, (hipStream_t)stream) != 0)
+        return fail(MORLAX_ERR_HIP, "%s: the kernel's LDS is not available on this device", who);
+    return finish(who);
+}
+
+static int check_page(int page, int slots, int pages, int64_t N, const char* who) {
+    if (N < 1 || page < 1 || slots < 1 || pages < 1) return fail(MORLAX_ERR_SHAPE, "%s: N, page, slots and pages must be >= 1", who);
+    if ((page & (page - 1)) != 0 || page > 4096) return fail(MORLAX_ERR_UNSUPPORTED, "%s: page must be a power of two up to 4096 (got %d)", who, page);
+    if ((int64_t)pages * page >= (int64_t)1 << 31 || N * slots >= (int64_t)1 << 31 || N > 1 << 24)
+        return fail(MORLAX_ERR_UNSUPPORTED, "%s: pages * page and N * slots must stay below 2^31, N <= 2^24", who);
+    return MORLAX_OK;
+}
+static int check_pages(const morlax_pages_dims* d, const char* who) {
+    if (!d) return fail(MORLAX_ERR_NULL, "%s: dims is NULL", who);
+    return check_page(d->page, d->slots, d->pages, d->N, who);
+}
+extern "C" int64_t morlax_pages_workspace_bytes(const morlax_pages_dims* d) {
+    if (check_pages(d, "morlax_pages_workspace_bytes") != MORLAX_OK) return -1;
+    return pages_ws_bytes(*d);
+}
+extern "C" int morlax_cache_pages(const morlax_pages_dims* dims, const uint8_t* first, const int32_t* length_in, const int32_t* table_in,
+                                  const int32_t* queue_in, const int32_t* state_in, int32_t* length, int32_t* table, int32_t* queue,
+                                  int32_t* state, int32_t* slot, void* ws, int64_t ws_bytes, void* stream) {
+    const char* who = "morlax_cache_pages";
+    const int rc = check_pages(dims, who);
+    if (rc != MORLAX_OK) return rc;
+    REQ(length_in, who); REQ(table_in, who); REQ(queue_in, who); REQ(state_in, who);
+    REQ(length, who); REQ(table, who); REQ(queue, who); REQ(state, who); REQ(slot, who);
+    const void* in[] = {length_in, table_in, queue_in, state_in};
+    const void* out[] = {length, table, queue, state, slot};
+    for (int o = 0; o < 5; ++o) {
+        for (int i = 0; i < 4; ++i)
+            if (o != i && out[o] == in[i]) return fail(MORLAX_ERR_SHAPE, "%s: an output is another's input", who);
+        for (int i = 0; i < o; ++i)
+            if (out[o] == out[i]) return fail(MORLAX_ERR_SHAPE, "%s: two outputs are the same", who);
+        if (out[o] == first) return fail(MORLAX_ERR_SHAPE, "%s: an output is its input", who);
+    }
+    WS(ws, ws_bytes, pages_ws_bytes(*dims), who);
+    launch_cache_pages(*dims, first, length_in, table_in, queue_in, state_in, length, table, queue, state, slot, ws, (hipStream_t)stream);
+    return finish(who);
+}
+
+static int check_cache(const morlax_cache_dims* d, const char* who) {
+    if (!d) return fail(MORLAX_ERR_NULL, "%s: dims is NULL", who);
+    int rc = check_heads(d->N, d->heads, d->kv_heads, d->head_dim, d->buckets, d->window, d->dtype, d->scale, who);
+    if (rc == MORLAX_OK) rc = check_page(d->page, d->slots, d->pages, d->N, who);
+    if (rc != MORLAX_OK) return rc;
+    if ((int64_t)d->slots * d->page < d->window) return fail(MORLAX_ERR_SHAPE, "%s: the window must be <= slots * page", who);
+    if ((int64_t)d->N * d->heads >= 1 << 22) return fail(MORLAX_ERR_UNSUPPORTED, "%s: N * heads must stay below 2^22", who);
+    const int64_t D = d->head_dim, q = d->heads * D;
+    if (d->N > 1 && (d->q_n < q || d->y_n < q || d->k_n < d->kv_heads * D)) return fail(MORLAX_ERR_SHAPE, "%s: a stride is shorter than a row", who);
+    return MORLAX_OK;
+}
+extern "C" int64_t morlax_attn_step_workspace_bytes(const morlax_cache_dims* d) {
+    if (check_cache(d, "morlax_attn_step_workspace_bytes") != MORLAX_OK) return -1;
+    return attn_step_ws_bytes(*d);
+}
+extern "C" int morlax_attn_step(const morlax_cache_dims* dims, const void* q, const void* k, const void* v, const float* bias, const int32_t* edges,
+                                const int32_t* table, const int32_t* length, void* k_cache, void* v_cache, void* y, void* ws,
+                                int64_t ws_bytes, void* stream) {
+    const char* who = "morlax_attn_step";
+    int rc = check_cache(dims, who);
+    if (rc != MORLAX_OK) return rc;
+    STRIDED(q, dims->dtype, who); STRIDED(k, dims->dtype, who); STRIDED(v, dims->dtype, who); STRIDED(y, dims->dtype, who);
+    if ((rc = check_bias(dims->buckets, bias, edges, who)) != MORLAX_OK) return rc;
+    REQ(table, who); REQ(length, who); REQ(k_cache, who); REQ(v_cache, who);
+    if (y == q || y == k || y == v || k_cache == v_cache || k_cache == y || v_cache == y || k_cache == k || v_cache == v || k_cache == v ||
+        v_cache == k || k_cache == q || v_cache == q)
+        return fail(MORLAX_ERR_SHAPE, "%s: an output is its input", who);
+    WS(ws, ws_bytes, attn_step_ws_bytes(*dims), who);
+    launch_attn_step(*dims, q, k, v, bias, edges, table, length, k_cache, v_cache, y, ws, (hipStream_t)stream);
+    return finish(who);
+}
+
+static int check_norm(const morlax_norm_dims* d, const char* who) {
+    if (!d) return fail(MORLAX_ERR_NULL, "%s: dims is NULL", who);
+    if (d->rows < 0 || d->width < 1) return fail(MORLAX_ERR_SHAPE, "%s: rows must be >= 0, width >= 1", who);
+    if (d->dtype != 0 && d->dtype != 1) return fail(MORLAX_ERR_UNSUPPORTED, "%s: dtype must be 0 (fp32) or 1 (bf16)", who);
+    if (d->width > 8192 || d->rows > 1 << 28) return fail(MORLAX_ERR_UNSUPPORTED, "%s: width must be <= 8192, rows <= 2^28", who);
+    if (!(d->eps >= 0.f) || !std::isfinite(d->eps)) return fail(MORLAX_ERR_SHAPE, "%s: eps must be >= 0 and finite", who);
+    if (d->ld_x < d->width || d->ld_u < d->width || d->ld_g < d->width || d->ld_h < d->width)
+        return fail(MORLAX_ERR_SHAPE, "%s: a row stride is shorter than its row", who);
+    return MORLAX_OK;
+}
+static int check_norm_inputs(const morlax_norm_dims* d, const void* x, const void* u, const void* gate, const float* scale, const float* w_post,
+                             const float* w_pre, const char* who) {
+    if (d->rows > 0) {
+        STRIDED(x, d->dtype, who);
+        if (u) STRIDED(u, d->dtype, who);
+        if (gate) STRIDED(gate, d->dtype, who);
+    }
+    OPT(scale, who); OPT(w_post, who); OPT(w_pre, who);
+    if (d->rows > 0 && !u && (gate || scale || w_post)) return fail(MORLAX_ERR_NULL, "%s: gate, scale and w_post go with u", who);
+    return MORLAX_OK;
+}
+extern "C" int64_t morlax_norm_workspace_bytes(const morlax_norm_dims* d) {
+    if (check_norm(d, "morlax_norm_workspace_bytes") != MORLAX_OK) return -1;
+    return norm_ws_bytes(*d);
+}
+extern "C" int morlax_norm_fwd(const morlax_norm_dims* dims, const void* x, const void* u, const void* gate, const float* scale, const float* w_post,
+                               const float* w_pre, void* y, void* h, void* stream) {
+    const char* who = "morlax_norm_fwd";
+    int rc = check_norm(dims, who);
+    if (rc == MORLAX_OK) rc = check_norm_inputs(dims, x, u, gate, scale, w_post, w_pre, who);
+    if (rc != MORLAX_OK || dims->rows == 0) return rc;
+    if (u || y) STRIDED(y, dims->dtype, who);
+    if ((w_pre == nullptr) != (h == nullptr)) return fail(MORLAX_ERR_NULL, "%s: h goes with w_pre, both or neither", who);
+    if (h) STRIDED(h, dims->dtype, who);
+    if ((h && (h == x || h == u || h == gate || h == y)) || (y && (y == u || y == gate)))
+        return fail(MORLAX_ERR_SHAPE, "%s: an output is its input", who);
+    launch_norm_fwd(*dims, x, u, gate, scale, w_post, w_pre, y, h, (hipStream_t)stream);
+    return finish(who);
+}
+extern "C" int morlax_norm_bwd(const morlax_norm_dims* dims, const void* x, const void* u, const void* gate, const float* scale, const float* w_post,
+                               const float* w_pre, const void* dy, const void* dh, void* dx, void* du, void* dgate, float* dscale, float* dw_post,
+                               float* dw_pre, void* ws, int64_t ws_bytes, void* stream) {
+    const char* who = "morlax_norm_bwd";
+    int rc = check_norm(dims, who);
+    if (rc == MORLAX_OK) rc = check_norm_inputs(dims, x, u, gate, scale, w_post, w_pre, who);
+    if (rc != MORLAX_OK) return rc;
+    OPT(dscale, who); OPT(dw_post, who); OPT(dw_pre, who);
+    if (dims->rows > 0) {
+        const void* out[] = {dx, du, dgate};
+        const void* in[] = {x, u, gate, dh, dy};
+        for (int o = 0; o < 3; ++o) {
+            if (!out[o]) continue;
+            if ((rc = strided(out[o], dims->dtype, o == 0 ? "dx" : o == 1 ? "du" : "dgate", who)) != MORLAX_OK) return rc;
+            for (int i = 0; i < 5; ++i)
+                if (out[o] == in[i] && !(o == 0 && i == 4)) return fail(MORLAX_ERR_SHAPE, "%s: an output is its input", who);
+            for (int i = 0; i < o; ++i)
+                if (out[o] == out[i]) return fail(MORLAX_ERR_SHAPE, "%s: two outputs are the same", who);
+        }
+        if (dy) STRIDED(dy, dims->dtype, who);
+        if (dh) STRIDED(dh, dims->dtype, who);
+        if (dh && !w_pre) return fail(MORLAX_ERR_NULL, "%s: dh goes with w_pre", who);
+        if ((!u && (du || dgate)) || (!gate && dgate)) return fail(MORLAX_ERR_NULL, "%s: a gradient of what is not there", who);
+    }
+    if (dscale || dw_post || dw_pre) WS(ws, ws_bytes, norm_ws_bytes(*dims), who);
+    launch_norm_bwd(*dims, x, u, gate, scale, w_post, w_pre, dy, dh, dx, du, dgate, dscale, dw_post, dw_pre, ws, (hipStream_t)stream);
+    return finish(who);
+}

@@ -138,4 +138,27 @@ void launch_memory_step(const morlax_scan_dims& d, int width, const void* xbc, c
                         const float* a_log, const float* d_skip, const float* dt_bias, const uint8_t* first, const void* conv_in, const float* state_in,
                         void* y, void* conv_out, float* state_out, hipStream_t s);
 
+int64_t attn_saved_bytes(const morlax_attn_dims& d);
+int64_t attn_ws_bytes(const morlax_attn_dims& d, bool back);
+// 0 on success
+int launch_attn_fwd(const morlax_attn_dims& d, const void* q, const void* k, const void* v, const float* bias, const int32_t* edges,
+                    const uint8_t* first, void* y, void* saved, void* ws, hipStream_t s);
+int launch_attn_bwd(const morlax_attn_dims& d, const void* q, const void* k, const void* v, const float* bias, const int32_t* edges,
+                    const uint8_t* first, const void* y, const void* saved, const void* dy, void* dq, void* dk, void* dv, float* dbias, void* ws,
+                    hipStream_t s);
+
+int64_t pages_ws_bytes(const morlax_pages_dims& d);
+void launch_cache_pages(const morlax_pages_dims& d, const uint8_t* first, const int32_t* length_in, const int32_t* table_in, const int32_t* queue_in,
+                        const int32_t* state_in, int32_t* length, int32_t* table, int32_t* queue, int32_t* state, int32_t* slot, void* ws, hipStream_t s);
+int64_t attn_step_ws_bytes(const morlax_cache_dims& d);
+void launch_attn_step(const morlax_cache_dims& d, const void* q, const void* k, const void* v, const float* bias, const int32_t* edges,
+                      const int32_t* table, const int32_t* length, void* k_cache, void* v_cache, void* y, void* ws, hipStream_t s);
+
+int64_t norm_ws_bytes(const morlax_norm_dims& d);
+void launch_norm_fwd(const morlax_norm_dims& d, const void* x, const void* u, const void* gate, const float* scale, const float* w_post,
+                     const float* w_pre, void* y, void* h, hipStream_t s);
+void launch_norm_bwd(const morlax_norm_dims& d, const void* x, const void* u, const void* gate, const float* scale, const float* w_post,
+                     const float* w_pre, const void* dy, const void* dh, void* dx, void* du, void* dgate, float* dscale, float* dw_post, float* dw_pre,
+                     void* ws, hipStream_t s);
+
 static inline int64_t align_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
