@@ -9,7 +9,8 @@
 // One pass over the keys with the running maximum and sum; scores never leave the registers.  Products run on the matrix instructions with
 // the operands turned so that a computed operand (P, dA) is already where the next product wants it: keys lie along a lane's registers,
 // queries along the lanes (the other way round in the pass over the keys), and the other operand is read transposed out of LDS.  What is seen of
-// a row is an interval, [lo_t, p_t], and every mask is a select: what an unseen key, value or row holds is never multiplied (see Wide below).
+// a row is an interval, [lo_t, p_t], and every mask is a select: what an unseen key, value or row holds never counts (see `clean`
+// below).
 // Query heads that share a head of keys are rows of the same tile (`pack` of them), so the keys are read once for all of them and the sums over
 // heads in dk and dv are sums over rows.
 #include "mlp_device.h"
@@ -43,6 +44,16 @@ struct AttnArgs {
     uint32_t total;
     int whole;  // rows hold whole pieces of 16 bytes
 };
+
+// No instruction moves across (left to itself the scheduler starts the reads of a whole tile at once, and two hundred registers hold them).
+__device__ inline void phase() { __builtin_amdgcn_sched_barrier(0); }
+// The lane, as a value that the compiler cannot know to be the same for the next tile: or it computes the addresses of all of a tile's
+// accesses once, ahead of the loop, and keeps them in registers.
+__device__ inline int lane_now() {
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
 
 // ---- episodes and the bias by distance --------------------------------------------------------------------------------
 // Blocks below `spans`: 2^lgn environments at a time, the threads of an environment taking a run of steps each; the others: the table.
@@ -93,14 +104,13 @@ struct Tile {
     static constexpr int NP = ES == 2 ? 2 : 1;                      // parts of a computed operand
     static constexpr int BYTES = ATTN_K * PITCH;
     // the lane's operand of rows row .. row + 15, contraction indices of piece ks along the row
-    static __device__ inline uint4 rows(const unsigned char* lds, int row, int ks) {
-        const int lane = threadIdx.x & 63;
+    static __device__ inline uint4 rows(const unsigned char* lds, int row, int ks, int lane) {
         return *reinterpret_cast<const uint4*>(lds + (row + (lane & 15)) * PITCH + ks * 64 + (lane >> 4) * 16);
     }
     // columns 16 dt .. + 15 as the rows of an operand, contraction over the rows u TU .. : in the order in which a lane holds the products'
     // results (bf16: 4 g + r of two blocks of 16; fp32: of one)
-    static __device__ inline uint4 turned(const unsigned char* lds, int u, int dt) {
-        const int lane = threadIdx.x & 63, a = lane & 15, gr = lane >> 4;
+    static __device__ inline uint4 turned(const unsigned char* lds, int u, int dt, int lane) {
+        const int a = lane & 15, gr = lane >> 4;
         if constexpr (ES == 2) {
             typedef __attribute__((address_space(3))) short4_t lds_s4;
             const unsigned char* s = lds + (32 * u + 4 * gr + (a >> 2)) * PITCH + (16 * dt + 4 * (a & 3)) * 2;
@@ -118,12 +128,12 @@ struct Tile {
     }
 };
 
-// VE elements from p on (aligned to an element), those from `n` on zero; whole: n is a multiple of VE
+// VE elements from p on (aligned to an element), those from `n` on zero; WHOLE: n is a multiple of VE
 typedef uint32_t piece_t __attribute__((ext_vector_type(4), aligned(2)));
-template <typename T>
-__device__ inline uint4 piece(const T* p, int n, bool whole) {
+template <typename T, bool WHOLE>
+__device__ inline uint4 piece(const T* p, int n) {
     constexpr int VE = 16 / sizeof(T);
-    if (whole || n >= VE) {
+    if (WHOLE || n >= VE) {
         if (n <= 0) return make_uint4(0, 0, 0, 0);
         const piece_t u = *reinterpret_cast<const piece_t*>(p);
         return make_uint4(u[0], u[1], u[2], u[3]);
@@ -153,29 +163,71 @@ __device__ inline float probe(const uint4& u, float z) {
     return z;
 }
 
-// A thread's pieces of a tile on their way: requested before the tile ahead of it is worked on, put down after.
-template <typename T, int DP>
+// A computed zero times an infinite or undefined element would reach rows that do not see it.  So such elements are put down as zeros in
+// the tiles that computed operands are multiplied with, and a workgroup that met one adds them in the end, one by one, to what sees them
+// (as they are: the products of the definition are infinite or undefined too).
+__device__ inline bool finite(float v) { return __builtin_fabsf(v) < __builtin_inff(); }
+template <typename T>
+__device__ inline uint4 clean(const uint4& u) {
+    uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 2) {
+            if (!finite(__uint_as_float(w[i] << 16))) w[i] &= 0xffff0000u;
+            if (!finite(__uint_as_float(w[i] & 0xffff0000u))) w[i] &= 0xffffu;
+        } else if (!finite(__uint_as_float(w[i]))) {
+            w[i] = 0;
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// does a row hold such an element
+template <typename T>
+__device__ inline bool tainted(const T* row, int D) {
+    bool t = false;
+    for (int d = 0; d < D; ++d) t |= !finite(to_f(row[d]));
+    return t;
+}
+
+// A thread's pieces of a tile on their way: requested before the tile ahead of it is worked on, put down after.  Rows [r0, end) are there; the
+// requests for others go to the last row, without a branch (behind one each they would leave one by one), and zeros are put down for them.
+template <typename T, int DP, bool WHOLE>
 struct Stage {
     typedef Tile<T, DP> L;
     static constexpr int CH = ATTN_K * L::CPR / ATTN_THREADS;
     uint4 u[CH];
-    // row r (of rows [0, end)) lies at base + (r >> lgp) * stride + (r & (pack - 1)) * D
-    __device__ inline void load(const T* base, int64_t stride, int r0, int end, int lgp, int D, bool vec) {
+    // row r lies at base + (r >> lgp) * stride + (r & (pack - 1)) * D
+    __device__ inline void load(const T* base, int64_t stride, int r0, int end, int lgp, int D) {
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int i = threadIdx.x + c * ATTN_THREADS, row = r0 + i / L::CPR, col = (i % L::CPR) * L::VE;
-            const bool in = row < end;
-            const int r = in ? row : end - 1;
-            u[c] = piece(base + (int64_t)(r >> lgp) * stride + (r & ((1 << lgp) - 1)) * D + (col < D ? col : 0), in ? D - col : 0, vec);
+            const int i = threadIdx.x + c * ATTN_THREADS, col = (i % L::CPR) * L::VE;
+            int r = r0 + i / L::CPR;
+            r = r < end ? r : end - 1;
+            const T* p = base + (int64_t)(r >> lgp) * stride + (r & ((1 << lgp) - 1)) * D + (col < D ? col : 0);
+            if constexpr (WHOLE) {
+                const piece_t w = *reinterpret_cast<const piece_t*>(p);
+                u[c] = make_uint4(w[0], w[1], w[2], w[3]);
+            } else {
+                u[c] = piece<T, false>(p, D - col);
+            }
         }
     }
-    __device__ inline void put(unsigned char* lds, float& z) const {
+    // CLEAN: infinite and undefined elements as zeros; returns whether there were any
+    template <bool CLEAN>
+    __device__ inline bool put(unsigned char* lds, int r0, int end, int D) const {
+        bool met = false;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int i = threadIdx.x + c * ATTN_THREADS;
-            *reinterpret_cast<uint4*>(lds + i / L::CPR * L::PITCH + (i % L::CPR) * 16) = u[c];
-            z = probe<T>(u[c], z);
+            const bool in = (r0 + i / L::CPR < end) & ((i % L::CPR) * L::VE < D);
+            uint4 v = make_uint4(in ? u[c].x : 0, in ? u[c].y : 0, in ? u[c].z : 0, in ? u[c].w : 0);
+            if (CLEAN && probe<T>(v, 0.f) != 0.f) {
+                v = clean<T>(v);
+                met = true;
+            }
+            *reinterpret_cast<uint4*>(lds + i / L::CPR * L::PITCH + (i % L::CPR) * 16) = v;
         }
+        return met;
     }
 };
 
@@ -208,46 +260,24 @@ struct Computed {
 };
 
 // acc[b][dt] (rows: columns 16 dt + 4 g + r of the tile; column: lane & 15) += tile^T computed[b], for NBLK blocks of 16 lanes' columns.
-// Wide: the tile holds an infinite or undefined element, and a computed zero times it would reach rows that do not see it: those pairs are left
-// out one by one.  seen(b, row): is the pair of the tile's row and the lane's column of block b one that is seen.
-template <typename T, int DP, int NBLK, typename F>
-__device__ inline void fold(const unsigned char* lds, const float4_t (&p)[NBLK][4], float4_t (&acc)[NBLK][DP / 16], bool wide, F seen) {
+template <typename T, int DP, int NBLK>
+__device__ inline void fold(const unsigned char* lds, const float4_t (&p)[NBLK][4], float4_t (&acc)[NBLK][DP / 16]) {
     typedef Tile<T, DP> L;
-    if (!wide) {
+    const int lane = lane_now();
 #pragma unroll
-        for (int u = 0; u < L::NU; ++u) {
-            Computed<T, DP> c[NBLK];
+    for (int u = 0; u < L::NU; ++u) {
+        phase();
+        Computed<T, DP> c[NBLK];
 #pragma unroll
-            for (int b = 0; b < NBLK; ++b) c[b].set(p[b], u);
+        for (int b = 0; b < NBLK; ++b) c[b].set(p[b], u);
 #pragma unroll
-            for (int dt = 0; dt < L::NB; ++dt) {
-                const uint4 a = L::turned(lds, u, dt);
+        for (int dt = 0; dt < L::NB; ++dt) {
+            const uint4 f = L::turned(lds, u, dt, lane);
 #pragma unroll
-                for (int b = 0; b < NBLK; ++b) c[b].product(a, acc[b][dt]);
-            }
+            for (int b = 0; b < NBLK; ++b) c[b].product(f, acc[b][dt]);
         }
-        return;
     }
-    const int lane = threadIdx.x & 63, a = lane & 15, gr = lane >> 4;
-#pragma unroll
-    for (int b = 0; b < NBLK; ++b)
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll 1
-                for (int o = 0; o < 4; ++o) {
-                    const float v = __shfl(p[b][t][r], 16 * o + a);
-                    const int row = 16 * t + 4 * o + r;
-                    const bool s = seen(b, row);
-#pragma unroll
-                    for (int dt = 0; dt < L::NB; ++dt)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float x = acc[b][dt][e], m = __builtin_fmaf(v, L::at(lds, row, 16 * dt + 4 * gr + e), x);
-                            acc[b][dt][e] = s ? m : x;
-                        }
-                }
+    phase();
 }
 
 // Four consecutive elements of a row of D from column d on
@@ -298,8 +328,8 @@ struct Table {
         const int count = each << g.lgp;
 #pragma unroll
         for (int c = 0; c < ATTN_TAB; ++c) {
-            const int i = threadIdx.x + c * ATTN_THREADS;
-            if (i >= count) break;
+            int i = threadIdx.x + c * ATTN_THREADS;
+            i = i < count ? i : count - 1;
             const int hh = i / each;
             int d = far + dir * (i - hh * each);
             d = d < 0 ? 0 : d >= g.reach ? g.reach - 1 : d;
@@ -316,7 +346,7 @@ struct Table {
 #pragma unroll
         for (int c = 0; c < ATTN_TAB; ++c) {
             const int i = threadIdx.x + c * ATTN_THREADS;
-            if (i >= count) break;
+            if (i >= count) break;  // (behind the loads)
             tab[i] = v[c];
             if (BUCKET) idx[i] = b[c];
         }
@@ -329,7 +359,7 @@ template <typename T, int DP, int QB>
 struct FwdLds {
     static constexpr int K = 0, V = Tile<T, DP>::BYTES, TAB = 2 * V, FLAG = TAB + ATTN_TAB_ROOM * 4, TOTAL = FLAG + 16;
 };
-template <typename T, int DP, int QB>
+template <typename T, int DP, int QB, bool WHOLE>
 __global__ __launch_bounds__(ATTN_THREADS) void k_attn_fwd(AttnArgs g) {
     typedef Tile<T, DP> L;
     typedef FwdLds<T, DP, QB> M;
@@ -354,7 +384,7 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_fwd(AttnArgs g) {
 #pragma unroll
         for (int ks = 0; ks < L::KS; ++ks) {
             const int d = ks * (64 / L::ES) + gr * L::VE;
-            qf[b][ks] = piece(src + (d < g.D ? d : 0), in ? g.D - d : 0, g.whole);
+            qf[b][ks] = piece<T, WHOLE>(src + (d < g.D ? d : 0), in ? g.D - d : 0);
         }
     }
     const int first_p = R.past + (R.r0 >> g.lgp), each = (BQ >> g.lgp) + ATTN_K, far = first_p + (BQ >> g.lgp) - 1;
@@ -375,21 +405,19 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_fwd(AttnArgs g) {
         for (int dt = 0; dt < L::NB; ++dt) o[b][dt] = float4_t{0.f, 0.f, 0.f, 0.f};
     }
     if (threadIdx.x == 0) *flag = 0;
-    Stage<T, DP> sk, sv;
+    Stage<T, DP, WHOLE> sk, sv;
     Table st;
     auto request = [&](int k0) {
-        sk.load(kb, g.k_t, k0, k_end, 0, g.D, g.whole);
-        sv.load(vb, g.k_t, k0, k_end, 0, g.D, g.whole);
+        sk.load(kb, g.k_t, k0, k_end, 0, g.D);
+        sv.load(vb, g.k_t, k0, k_end, 0, g.D);
         if (g.table && first_p - (k0 + ATTN_K - 1) < last_edge) st.load<false>(g, R.h0, each, far - k0, -1);
     };
     request(k_begin);
     __syncthreads();
     for (int k0 = k_begin; k0 < k_end; k0 += ATTN_K) {
         const bool near = g.table && first_p - (k0 + ATTN_K - 1) < last_edge;
-        float z = 0.f, zk = 0.f;
-        sk.put(lds + M::K, zk);
-        sv.put(lds + M::V, z);
-        if (z != 0.f) *flag = 1;
+        sk.template put<false>(lds + M::K, k0, k_end, g.D);
+        if (sv.template put<true>(lds + M::V, k0, k_end, g.D)) *flag = 1;
         if (near) st.put<false>(g, each, tab, nullptr);
         __syncthreads();
         if (k0 + ATTN_K < k_end) request(k0 + ATTN_K);
@@ -400,15 +428,17 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_fwd(AttnArgs g) {
             all &= lo[b] <= k0 && p[b] >= k0 + ATTN_K - 1;
         }
         if (__any(any)) {
-            const bool whole = __all(all), wide = *flag != 0;
+            const bool whole = __all(all);
             float4_t s[QB][4];
+            const int now = lane_now();
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
+                phase();
 #pragma unroll
                 for (int b = 0; b < QB; ++b) s[b][x] = float4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int ks = 0; ks < L::KS; ++ks) {
-                    const uint4 f = L::rows(lds + M::K, 16 * x, ks);
+                    const uint4 f = L::rows(lds + M::K, 16 * x, ks, now);
 #pragma unroll
                     for (int b = 0; b < QB; ++b) Mma16<T>::run(f, qf[b][ks], s[b][x]);
                 }
@@ -434,7 +464,7 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_fwd(AttnArgs g) {
                     for (int x = 0; x < 4; ++x)
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
-                            s[b][x][r] = t[b] >= 0 && (uint32_t)(16 * x + r - from) <= span ? s[b][x][r] : -__builtin_inff();
+                            s[b][x][r] = ((t[b] >= 0) & ((uint32_t)(16 * x + r - from) <= span)) ? s[b][x][r] : -__builtin_inff();
                 }
                 float top = m[b];
 #pragma unroll
@@ -463,10 +493,25 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_fwd(AttnArgs g) {
                 l[b] += sum;
                 m[b] = top;
             }
-            fold<T, DP, QB>(lds + M::V, s, o, wide,
-                            [&](int b, int row) { return t[b] >= 0 && k0 + row >= lo[b] && k0 + row <= p[b]; });
+            fold<T, DP, QB>(lds + M::V, s, o);
         }
         __syncthreads();
+    }
+    if (*flag) {
+        for (int k = k_begin; k < k_end; ++k)
+#pragma unroll
+            for (int b = 0; b < QB; ++b) {
+                const bool see = (t[b] >= 0) & (k >= lo[b]) & (k <= p[b]);
+                if (!see) continue;
+#pragma unroll
+                for (int dt = 0; dt < L::NB; ++dt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int d = 16 * dt + 4 * gr + r;
+                        const float v = d < g.D ? to_f(vb[(int64_t)k * g.k_t + d]) : 0.f;
+                        o[b][dt][r] += finite(v) ? 0.f : v;
+                    }
+            }
     }
 #pragma unroll
     for (int b = 0; b < QB; ++b) {
@@ -498,7 +543,7 @@ template <typename T, int DP, int QB>
 struct DqLds {
     static constexpr int K = 0, V = Tile<T, DP>::BYTES, TAB = 2 * V, IDX = TAB + ATTN_TAB_ROOM * 4, FLAG = IDX + ATTN_TAB_ROOM * 4, BINS = FLAG + 16;
 };
-template <typename T, int DP, int QB>
+template <typename T, int DP, int QB, bool WHOLE>
 __global__ __launch_bounds__(ATTN_THREADS) void k_attn_dq(AttnArgs g) {
     typedef Tile<T, DP> L;
     typedef DqLds<T, DP, QB> M;
@@ -531,12 +576,12 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_dq(AttnArgs g) {
 #pragma unroll
         for (int ks = 0; ks < L::KS; ++ks) {
             const int d = ks * (64 / L::ES) + gr * L::VE, dc = d < g.D ? d : 0, left = in ? g.D - d : 0;
-            qf[b][ks] = piece(src + dc, left, g.whole);
-            of[b][ks] = piece(dsrc + dc, left, g.whole);
-            const uint4 yf = piece(ysrc + dc, left, g.whole);
+            qf[b][ks] = piece<T, WHOLE>(src + dc, left);
+            of[b][ks] = piece<T, WHOLE>(dsrc + dc, left);
+            const uint4 yf = piece<T, WHOLE>(ysrc + dc, left);
             const uint32_t wy[4] = {yf.x, yf.y, yf.z, yf.w}, wd[4] = {of[b][ks].x, of[b][ks].y, of[b][ks].z, of[b][ks].w};
             if constexpr (L::ES == 2) {
-                const uint4 lf = piece(lsrc + dc, left, g.whole);
+                const uint4 lf = piece<bf16_t, WHOLE>(lsrc + dc, left);
                 const uint32_t wl[4] = {lf.x, lf.y, lf.z, lf.w};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -576,21 +621,19 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_dq(AttnArgs g) {
     if (threadIdx.x == 0) *flag = 0;
     if (g.part)
         for (int b = 0; b < g.B; ++b) bins[b * 64] = 0.f;
-    Stage<T, DP> sk, sv;
+    Stage<T, DP, WHOLE> sk, sv;
     Table st;
     auto request = [&](int k0) {
-        sk.load(kb, g.k_t, k0, k_end, 0, g.D, g.whole);
-        sv.load(vb, g.k_t, k0, k_end, 0, g.D, g.whole);
+        sk.load(kb, g.k_t, k0, k_end, 0, g.D);
+        sv.load(vb, g.k_t, k0, k_end, 0, g.D);
         if (g.table && first_p - (k0 + ATTN_K - 1) < last_edge) st.load<true>(g, R.h0, each, far - k0, -1);
     };
     request(k_begin);
     __syncthreads();
     for (int k0 = k_begin; k0 < k_end; k0 += ATTN_K) {
         const bool near = g.table && first_p - (k0 + ATTN_K - 1) < last_edge;
-        float z = 0.f, zv = 0.f;
-        sk.put(lds + M::K, z);
-        sv.put(lds + M::V, zv);
-        if (z != 0.f) *flag = 1;
+        if (sk.template put<true>(lds + M::K, k0, k_end, g.D)) *flag = 1;
+        sv.template put<false>(lds + M::V, k0, k_end, g.D);
         if (near) st.put<true>(g, each, tab, idx);
         __syncthreads();
         if (k0 + ATTN_K < k_end) request(k0 + ATTN_K);
@@ -601,16 +644,18 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_dq(AttnArgs g) {
             all &= lo[b] <= k0 && p[b] >= k0 + ATTN_K - 1;
         }
         if (__any(any)) {
-            const bool whole = __all(all), wide = *flag != 0;
+            const bool whole = __all(all);
             float4_t s[QB][4];
+            const int now = lane_now();
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
+                phase();
                 float4_t dp[QB];
 #pragma unroll
                 for (int b = 0; b < QB; ++b) s[b][x] = dp[b] = float4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int ks = 0; ks < L::KS; ++ks) {
-                    const uint4 f = L::rows(lds + M::K, 16 * x, ks), fv = L::rows(lds + M::V, 16 * x, ks);
+                    const uint4 f = L::rows(lds + M::K, 16 * x, ks, now), fv = L::rows(lds + M::V, 16 * x, ks, now);
 #pragma unroll
                     for (int b = 0; b < QB; ++b) {
                         Mma16<T>::run(f, qf[b][ks], s[b][x]);
@@ -619,14 +664,14 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_dq(AttnArgs g) {
                 }
 #pragma unroll
                 for (int b = 0; b < QB; ++b) {
-                    const int place = hh * each + 4 * gr + (t[b] < 0 ? 0 : far - p[b]);
-                    const int from = lo[b] - k0 - 4 * gr;
+                    const int place = hh * each + 4 * (now >> 4) + (t[b] < 0 ? 0 : far - p[b]);
+                    const int from = lo[b] - k0 - 4 * (now >> 4);
                     const uint32_t span = p[b] - lo[b];
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const float shift = near ? tab[place + 16 * x + r] : beyond;
                         const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][x][r], c, shift) - lse[b]);
-                        const bool see = whole || (t[b] >= 0 && (uint32_t)(16 * x + r - from) <= span);
+                        const bool see = whole | ((t[b] >= 0) & ((uint32_t)(16 * x + r - from) <= span));
                         const float da = see ? e * (dp[b][r] - delta[b]) : 0.f;
                         s[b][x][r] = da;
                         if (g.part) {
@@ -636,10 +681,20 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_dq(AttnArgs g) {
                     }
                 }
             }
-            fold<T, DP, QB>(lds + M::K, s, o, wide,
-                            [&](int b, int row) { return t[b] >= 0 && k0 + row >= lo[b] && k0 + row <= p[b]; });
+            fold<T, DP, QB>(lds + M::K, s, o);
         }
         __syncthreads();
+    }
+    if (*flag) {  // a row that sees such a key has a score that is not finite: no part of its gradient is
+        for (int k = k_begin; k < k_end; ++k)
+#pragma unroll
+            for (int b = 0; b < QB; ++b) {
+                const bool see = (t[b] >= 0) & (k >= lo[b]) & (k <= p[b]);
+                if (!see || !tainted(kb + (int64_t)k * g.k_t, g.D)) continue;
+                outer = __builtin_nanf("");
+#pragma unroll
+                for (int dt = 0; dt < L::NB; ++dt) o[b][dt] = float4_t{outer, outer, outer, outer};
+            }
     }
 #pragma unroll
     for (int b = 0; b < QB; ++b) {
@@ -684,7 +739,7 @@ template <typename T, int DP, int KB>
 struct DkvLds {
     static constexpr int Q = 0, O = Tile<T, DP>::BYTES, TAB = 2 * O, INFO = TAB + ATTN_TAB_ROOM * 4, FLAG = INFO + 3 * ATTN_K * 4, TOTAL = FLAG + 16;
 };
-template <typename T, int DP, int KB>
+template <typename T, int DP, int KB, bool WHOLE>
 __global__ __launch_bounds__(ATTN_THREADS) void k_attn_dkv(AttnArgs g) {
     typedef Tile<T, DP> L;
     typedef DkvLds<T, DP, KB> M;
@@ -713,8 +768,8 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_dkv(AttnArgs g) {
 #pragma unroll
         for (int ks = 0; ks < L::KS; ++ks) {
             const int d = ks * (64 / L::ES) + gr * L::VE, dc = d < g.D ? d : 0, left = in ? g.D - d : 0;
-            kf[b][ks] = piece(reinterpret_cast<const T*>(g.k) + at + dc, left, g.whole);
-            vf[b][ks] = piece(reinterpret_cast<const T*>(g.v) + at + dc, left, g.whole);
+            kf[b][ks] = piece<T, WHOLE>(reinterpret_cast<const T*>(g.k) + at + dc, left);
+            vf[b][ks] = piece<T, WHOLE>(reinterpret_cast<const T*>(g.v) + at + dc, left);
         }
 #pragma unroll
         for (int dt = 0; dt < L::NB; ++dt) dk[b][dt] = dv[b][dt] = float4_t{0.f, 0.f, 0.f, 0.f};
@@ -730,7 +785,7 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_dkv(AttnArgs g) {
     for (int h0 = R.kv * share; h0 < (R.kv + 1) * share; h0 += pack) {
         const T* qb = reinterpret_cast<const T*>(g.q) + (int64_t)R.n * g.q_n + (int64_t)h0 * g.D;
         const T* ob = reinterpret_cast<const T*>(g.dy) + (int64_t)R.n * g.y_n + (int64_t)h0 * g.D;
-        Stage<T, DP> sq, so;
+        Stage<T, DP, WHOLE> sq, so;
         Table st;
         float i_lse = 0.f, i_delta = 0.f;
         int i_lo = kNever;
@@ -739,8 +794,8 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_dkv(AttnArgs g) {
         for (int r = 0; r < 4; ++r) beyond[r] = g.table ? g.bias[(int64_t)(h0 + (r & (pack - 1))) * g.B + g.B - 1] * kLog2e : 0.f;
         auto near_at = [&](int r0) { return g.table && R.past + (r0 >> g.lgp) - k_last < last_edge; };
         auto request = [&](int r0) {
-            sq.load(qb, g.q_t, r0, r_end, g.lgp, g.D, g.whole);
-            so.load(ob, g.y_t, r0, r_end, g.lgp, g.D, g.whole);
+            sq.load(qb, g.q_t, r0, r_end, g.lgp, g.D);
+            so.load(ob, g.y_t, r0, r_end, g.lgp, g.D);
             if (near_at(r0)) st.load<false>(g, h0, each, R.past + (r0 >> g.lgp) - (k0 + BK - 1), 1);
             if (threadIdx.x < ATTN_K) {
                 const int r = r0 + threadIdx.x;
@@ -758,10 +813,8 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_dkv(AttnArgs g) {
         __syncthreads();
         for (int r0 = r_begin; r0 < r_end; r0 += ATTN_K) {
             const bool near = near_at(r0);
-            float z = 0.f;
-            sq.put(lds + M::Q, z);
-            so.put(lds + M::O, z);
-            if (z != 0.f) *flag = 1;
+            const bool mq = sq.template put<true>(lds + M::Q, r0, r_end, g.D), mo = so.template put<true>(lds + M::O, r0, r_end, g.D);
+            if (mq | mo) *flag = 1;
             if (near) st.put<false>(g, each, tab, nullptr);
             if (threadIdx.x < ATTN_K) {
                 row_lse[threadIdx.x] = i_lse;
@@ -772,46 +825,78 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_dkv(AttnArgs g) {
             if (row_lo[0] > k_last) break;  // (lo never falls: no later row sees a key here)
             if (r0 + ATTN_K < r_end) request(r0 + ATTN_K);
             const int p0 = R.past + (r0 >> g.lgp);
-            const bool whole = row_lo[ATTN_K - 1] <= k0 && p0 >= k0 + BK - 1, wide = *flag != 0;
+            const bool whole = row_lo[ATTN_K - 1] <= k0 && p0 >= k0 + BK - 1;
             float4_t s[KB][4], e[KB][4];
+            const int now = lane_now();
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
+                phase();
                 float4_t dp[KB];
 #pragma unroll
                 for (int b = 0; b < KB; ++b) s[b][x] = dp[b] = float4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int ks = 0; ks < L::KS; ++ks) {
-                    const uint4 f = L::rows(lds + M::Q, 16 * x, ks), fo = L::rows(lds + M::O, 16 * x, ks);
+                    const uint4 f = L::rows(lds + M::Q, 16 * x, ks, now), fo = L::rows(lds + M::O, 16 * x, ks, now);
 #pragma unroll
                     for (int b = 0; b < KB; ++b) {
                         Mma16<T>::run(f, kf[b][ks], s[b][x]);
                         Mma16<T>::run(fo, vf[b][ks], dp[b]);
                     }
                 }
-                const int row = 16 * x + 4 * gr;
+                const int row = 16 * x + 4 * (now >> 4);
                 const float4_t lse = *reinterpret_cast<const float4_t*>(row_lse + row), delta = *reinterpret_cast<const float4_t*>(row_delta + row);
                 const int4 lo4 = *reinterpret_cast<const int4*>(row_lo + row);
                 const int lo[4] = {lo4.x, lo4.y, lo4.z, lo4.w};
 #pragma unroll
                 for (int b = 0; b < KB; ++b) {
-                    const float* place = tab + (row >> g.lgp) + (k0 + BK - 1 - key[b]);
+                    float shift[4];
+                    if (near) {
+                        const float* place = tab + (row >> g.lgp) + (k0 + BK - 1 - key[b]);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) shift[r] = place[(r & (pack - 1)) * each + (r >> g.lgp)];
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) shift[r] = beyond[r];
+                    }
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        const int hh = r & (pack - 1), step = r >> g.lgp;
-                        const float shift = near ? place[hh * each + step] : beyond[r];
-                        const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][x][r], c, shift) - lse[r]);
-                        const bool see = whole || (lo[r] <= key[b] && key[b] <= p0 + (row >> g.lgp) + step);
+                        const int step = r >> g.lgp;
+                        const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][x][r], c, shift[r]) - lse[r]);
+                        const bool see = whole | ((lo[r] <= key[b]) & (key[b] <= p0 + (row >> g.lgp) + step));
                         e[b][x][r] = see ? v : 0.f;
                         s[b][x][r] = see ? v * (dp[b][r] - delta[r]) : 0.f;
                     }
                 }
             }
-            auto seen = [&](int b, int row) { return row_lo[row] <= key[b] && key[b] <= p0 + (row >> g.lgp); };
-            fold<T, DP, KB>(lds + M::O, e, dv, wide, seen);
-            fold<T, DP, KB>(lds + M::Q, s, dk, wide, seen);
+            fold<T, DP, KB>(lds + M::O, e, dv);
+            fold<T, DP, KB>(lds + M::Q, s, dk);
             __syncthreads();
         }
         __syncthreads();  // (a walk that ended early has not waited yet)
+        if (*flag) {  // an undefined q: undefined probabilities; an undefined dy: undefined dA, and itself in dv
+            for (int r = r_begin; r < r_end; ++r) {
+                const int tt = r >> g.lgp, p = R.past + tt, lo = R.lo(g, p);
+                const T *qr = qb + (int64_t)tt * g.q_t + (r & (pack - 1)) * g.D, *orow = ob + (int64_t)tt * g.y_t + (r & (pack - 1)) * g.D;
+                const bool bad_q = tainted(qr, g.D), bad_o = tainted(orow, g.D);
+                if (!(bad_q | bad_o)) continue;
+                const float nan = __builtin_nanf("");
+#pragma unroll
+                for (int b = 0; b < KB; ++b) {
+                    const bool see = (lo <= key[b]) & (key[b] <= p);
+                    if (!see) continue;
+#pragma unroll
+                    for (int dt = 0; dt < L::NB; ++dt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int d = 16 * dt + 4 * gr + e;
+                            const float v = d < g.D ? to_f(orow[d]) : 0.f;
+                            dk[b][dt][e] = nan;
+                            dv[b][dt][e] += bad_q ? nan : finite(v) ? 0.f : v;
+                        }
+                }
+            }
+            __syncthreads();  // (the next heads' walk may set it again)
+        }
     }
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
@@ -863,7 +948,7 @@ static int64_t attn_carve_saved(AttnArgs& g, const morlax_attn_dims& d, void* sa
     if (d.dtype) at = carve(g.low, at, saved, (int64_t)g.T * g.N * g.H * g.D * 2);
     return attn_carve_prepared(g, saved, at);
 }
-#define ATTN_ROWS 64  // rows of queries and keys of a workgroup
+#define ATTN_ROWS 64  // the fewest rows of queries of a workgroup
 static int64_t attn_carve_bwd(AttnArgs& g, void* ws) {
     int64_t at = carve(g.delta, 0, ws, (int64_t)g.N * g.H * g.T * 4);
     if (g.B) at = carve(g.part, at, ws, (int64_t)g.H * g.B * g.N * cdiv((int64_t)g.T << g.lgp, ATTN_ROWS) * 4);
@@ -884,24 +969,36 @@ static int run_kernel(void (*kernel)(AttnArgs), AttnArgs& g, int64_t total, int 
     kernel<<<dim3((uint32_t)total), ATTN_THREADS, lds, s>>>(g);
     return 0;
 }
-template <typename T, int DP>
+template <typename T, int DP, int QB, bool WHOLE>
 static int attn_fwd_pass(AttnArgs& g, hipStream_t s) {
-    g.tiles = (int)cdiv((int64_t)g.T << g.lgp, 64);
-    return run_kernel(k_attn_fwd<T, DP, 1>, g, (int64_t)g.tiles * g.N * (g.H >> g.lgp), FwdLds<T, DP, 1>::TOTAL, s);
+    g.tiles = (int)cdiv((int64_t)g.T << g.lgp, 64 * QB);
+    return run_kernel(k_attn_fwd<T, DP, QB, WHOLE>, g, (int64_t)g.tiles * g.N * (g.H >> g.lgp), FwdLds<T, DP, QB>::TOTAL, s);
 }
-template <typename T, int DP>
+template <typename T, int DP, int QB, bool WHOLE>
 static int attn_bwd_pass(AttnArgs& g, hipStream_t s) {
-    g.tiles = (int)cdiv((int64_t)g.T << g.lgp, 64);
-    if (run_kernel(k_attn_dq<T, DP, 1>, g, (int64_t)g.tiles * g.N * (g.H >> g.lgp), DqLds<T, DP, 1>::BINS + (g.part ? g.B * 1024 : 0), s)) return 1;
+    g.tiles = (int)cdiv((int64_t)g.T << g.lgp, 64 * QB);
+    if (run_kernel(k_attn_dq<T, DP, QB, WHOLE>, g, (int64_t)g.tiles * g.N * (g.H >> g.lgp), DqLds<T, DP, QB>::BINS + (g.part ? g.B * 1024 : 0), s))
+        return 1;
     if (g.part) k_attn_dbias<<<dim3((uint32_t)(g.H * g.B)), 256, 0, s>>>(g);
-    g.tiles = (int)cdiv(g.S, 64);
-    return run_kernel(k_attn_dkv<T, DP, 1>, g, (int64_t)g.tiles * g.N * g.KV, DkvLds<T, DP, 1>::TOTAL, s);
+    g.tiles = (int)cdiv(g.S, 64 * QB);
+    return run_kernel(k_attn_dkv<T, DP, QB, WHOLE>, g, (int64_t)g.tiles * g.N * g.KV, DkvLds<T, DP, QB>::TOTAL, s);
+}
+template <typename T, int DP, int QB>
+static int attn_pass(AttnArgs& g, bool back, hipStream_t s) {
+    if (g.whole) return back ? attn_bwd_pass<T, DP, QB, true>(g, s) : attn_fwd_pass<T, DP, QB, true>(g, s);
+    return back ? attn_bwd_pass<T, DP, QB, false>(g, s) : attn_fwd_pass<T, DP, QB, false>(g, s);
+}
+// Two blocks of rows a wave where there are rows for them: what is read of the keys' tiles serves both
+template <typename T, int DP>
+static int attn_rows(AttnArgs& g, bool back, hipStream_t s) {
+    if (sizeof(T) == 2 && ((int64_t)g.T << g.lgp) > 64) return attn_pass<T, DP, sizeof(T) == 2 ? 2 : 1>(g, back, s);
+    return attn_pass<T, DP, 1>(g, back, s);
 }
 template <typename T>
 static int attn_pick(AttnArgs& g, bool back, hipStream_t s) {
-    if (g.D <= 32) return back ? attn_bwd_pass<T, 32>(g, s) : attn_fwd_pass<T, 32>(g, s);
-    if (g.D <= 64) return back ? attn_bwd_pass<T, 64>(g, s) : attn_fwd_pass<T, 64>(g, s);
-    return back ? attn_bwd_pass<T, 128>(g, s) : attn_fwd_pass<T, 128>(g, s);
+    if (g.D <= 32) return attn_rows<T, 32>(g, back, s);
+    if (g.D <= 64) return attn_rows<T, 64>(g, back, s);
+    return attn_rows<T, 128>(g, back, s);
 }
 
 int launch_attn_fwd(const morlax_attn_dims& d, const void* q, const void* k, const void* v, const float* bias, const int32_t* edges,

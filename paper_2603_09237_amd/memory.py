@@ -35,33 +35,23 @@ def _check_first(first, shape):
         _check("first", first, shape, torch.bool if first.dtype is torch.bool else torch.uint8)
 
 
-class MemoryBlock:
-    """Parameters are in `p`, gradients after `backward` in `g` under the same names (the projections' matrices and factors in the
-    block's type, everything else and all gradients fp32).  Acting has buffers of its own: it may run on one stream while segments and
-    their gradients run on another.  What a call that is captured in a graph uses stays for as long as the block, also when later calls
-    of other sizes take other buffers."""
+class Block:
+    """What blocks have in common: buffers by name, the two projections, parameters in `p`, gradients in `g`."""
 
-    def __init__(self, preferences, width, heads, head_dim=64, groups=1, state=64, conv=4, rank=16, dtype=torch.bfloat16, device="cuda", seed=0):
-        self.P, self.width, self.H, self.Pd, self.G, self.S, self.W, self.r = preferences, width, heads, head_dim, groups, state, conv, rank
-        self.D = heads * head_dim
-        self.C = self.D + 2 * groups * state           # channels of the convolution: x, B, C
-        self.L = self.D + self.C + heads               # a projected row: gate, x, B, C, dt
-        self.dtype, self.kind, self.dev = dtype, 1 if dtype == torch.bfloat16 else 0, torch.device(device)
-        gen = torch.Generator().manual_seed(seed)
-
+    def _projections(self, preferences, width, inner, outer, rank, dtype, gen):
+        """Parameters of the projections width -> inner and outer -> width."""
         def normal(*shape, scale, t=torch.float32):
             return (torch.randn(*shape, generator=gen) * scale).to(t).to(self.dev)
 
-        self.p = {}
-        for name, i, o in (("in", width, self.L), ("out", self.D, width)):
-            self.p[name + ".w0"] = normal(o, i, scale=i ** -0.5, t=dtype)
-            self.p[name + ".bias"] = torch.zeros(o, device=self.dev)
-            self.p[name + ".A"] = normal(preferences, o, rank, scale=0.36 * rank ** -0.5, t=dtype)
-            self.p[name + ".B"] = normal(preferences, rank, i, scale=0.36 * i ** -0.5, t=dtype)
-        step = torch.exp(torch.rand(heads, generator=gen) * math.log(100.0) + math.log(1e-3))
-        self.p.update({"conv.w": normal(self.C, conv, scale=conv ** -0.5), "conv.b": torch.zeros(self.C, device=self.dev),
-                       "a_log": torch.log(1 + 15 * torch.rand(heads, generator=gen)).to(self.dev), "d_skip": torch.ones(heads, device=self.dev),
-                       "dt_bias": (step + torch.log(-torch.expm1(-step))).to(self.dev)})
+        p = {}
+        for name, i, o in (("in", width, inner), ("out", outer, width)):
+            p[name + ".w0"] = normal(o, i, scale=i ** -0.5, t=dtype)
+            p[name + ".bias"] = torch.zeros(o, device=self.dev)
+            p[name + ".A"] = normal(preferences, o, rank, scale=0.36 * rank ** -0.5, t=dtype)
+            p[name + ".B"] = normal(preferences, rank, i, scale=0.36 * i ** -0.5, t=dtype)
+        return p, normal
+
+    def _ready(self):
         self.g = {k: torch.zeros(v.shape, device=self.dev) for k, v in self.p.items()}
         self.b, self.saved_for = {}, None
         self.captured, self.recording = {}, False   # buffers that graphs use; whether the present call is being captured
@@ -105,6 +95,28 @@ class MemoryBlock:
         q = self.p
         binding.adapter_fwd(d, x, q[name + ".w0"], q[name + ".bias"], q[name + ".A"], q[name + ".B"], index, y,
                             self._scratch(binding.adapter_workspace_bytes(d), ws))
+
+
+class MemoryBlock(Block):
+    """Parameters are in `p`, gradients after `backward` in `g` under the same names (the projections' matrices and factors in the
+    block's type, everything else and all gradients fp32).  Acting has buffers of its own: it may run on one stream while segments and
+    their gradients run on another.  What a call that is captured in a graph uses stays for as long as the block, also when later calls
+    of other sizes take other buffers."""
+
+    def __init__(self, preferences, width, heads, head_dim=64, groups=1, state=64, conv=4, rank=16, dtype=torch.bfloat16, device="cuda", seed=0):
+        self.P, self.width, self.H, self.Pd, self.G, self.S, self.W, self.r = preferences, width, heads, head_dim, groups, state, conv, rank
+        self.D = heads * head_dim
+        self.C = self.D + 2 * groups * state           # channels of the convolution: x, B, C
+        self.L = self.D + self.C + heads               # a projected row: gate, x, B, C, dt
+        self.dtype, self.kind, self.dev = dtype, 1 if dtype == torch.bfloat16 else 0, torch.device(device)
+        gen = torch.Generator().manual_seed(seed)
+
+        self.p, normal = self._projections(preferences, width, self.L, self.D, rank, dtype, gen)
+        step = torch.exp(torch.rand(heads, generator=gen) * math.log(100.0) + math.log(1e-3))
+        self.p.update({"conv.w": normal(self.C, conv, scale=conv ** -0.5), "conv.b": torch.zeros(self.C, device=self.dev),
+                       "a_log": torch.log(1 + 15 * torch.rand(heads, generator=gen)).to(self.dev), "d_skip": torch.ones(heads, device=self.dev),
+                       "dt_bias": (step + torch.log(-torch.expm1(-step))).to(self.dev)})
+        self._ready()
 
     def _dims(self, T, N):
         conv = binding.ConvDims(T, N, self.C, self.W, 1, self.kind, N * self.L, self.L, N * self.C, self.C)
