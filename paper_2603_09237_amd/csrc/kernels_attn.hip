@@ -20,7 +20,7 @@ static int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 typedef short short4_t __attribute__((ext_vector_type(4)));
 #define ATTN_K 64      // rows of a tile that is walked through (keys; in the pass over the keys, queries)
 #define ATTN_THREADS 256
-#define ATTN_TAB 3     // table entries that a thread stages: pack <= 4 heads, distances of a tile
+#define ATTN_ROOM(rows, keys) ((rows) + 4 * (keys))  // table entries of a tile: pack <= 4 heads, each its distances
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kNever = 1 << 30;  // begin of the seen interval of a row that is not there
 
@@ -101,6 +101,7 @@ template <typename T, int DP>
 struct Tile {
     static constexpr int ES = sizeof(T), VE = 16 / ES, PITCH = DP * ES + 16, CPR = DP / VE, KS = DP * ES / 64, NB = DP / 16;
     static constexpr int TU = ES == 2 ? 32 : 16, NU = ATTN_K / TU;  // rows of one transposed operand, operands of a tile
+    static constexpr int NX = TU / 16;                              // blocks of 16 of one
     static constexpr int NP = ES == 2 ? 2 : 1;                      // parts of a computed operand
     static constexpr int BYTES = ATTN_K * PITCH;
     // the lane's operand of rows row .. row + 15, contraction indices of piece ks along the row
@@ -147,22 +148,6 @@ __device__ inline uint4 piece(const T* p, int n) {
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
-// z plus zero, or undefined if the piece holds an infinite or undefined element
-template <typename T>
-__device__ inline float probe(const uint4& u, float z) {
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if constexpr (sizeof(T) == 2) {
-            z = __builtin_fmaf(__uint_as_float(w[i] << 16), 0.f, z);
-            z = __builtin_fmaf(__uint_as_float(w[i] & 0xffff0000u), 0.f, z);
-        } else {
-            z = __builtin_fmaf(__uint_as_float(w[i]), 0.f, z);
-        }
-    }
-    return z;
-}
-
 // A computed zero times an infinite or undefined element would reach rows that do not see it.  So such elements are put down as zeros in
 // the tiles that computed operands are multiplied with, and a workgroup that met one adds them in the end, one by one, to what sees them
 // (as they are: the products of the definition are infinite or undefined too).
@@ -181,6 +166,24 @@ __device__ inline uint4 clean(const uint4& u) {
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
+// Has any of the pieces looked at held such an element
+template <typename T> struct Probe {
+    float z = 0.f;
+    __device__ inline void look(const uint4& u) {
+        z = __builtin_fmaf(__uint_as_float(u.x), 0.f, __builtin_fmaf(__uint_as_float(u.y), 0.f, z));
+        z = __builtin_fmaf(__uint_as_float(u.z), 0.f, __builtin_fmaf(__uint_as_float(u.w), 0.f, z));
+    }
+    __device__ inline bool met() const { return z != 0.f; }
+};
+template <> struct Probe<bf16_t> {  // (the largest of the magnitudes as integers, two at a time)
+    typedef uint16_t pair_t __attribute__((ext_vector_type(2)));
+    pair_t m = {0, 0};
+    __device__ inline void look(uint32_t w) { m = __builtin_elementwise_max(m, __builtin_bit_cast(pair_t, w & 0x7fff7fffu)); }
+    __device__ inline void look(const uint4& u) {
+        look(u.x); look(u.y); look(u.z); look(u.w);
+    }
+    __device__ inline bool met() const { return (m[0] >= 0x7f80) | (m[1] >= 0x7f80); }
+};
 // does a row hold such an element
 template <typename T>
 __device__ inline bool tainted(const T* row, int D) {
@@ -194,39 +197,64 @@ __device__ inline bool tainted(const T* row, int D) {
 template <typename T, int DP, bool WHOLE>
 struct Stage {
     typedef Tile<T, DP> L;
-    static constexpr int CH = ATTN_K * L::CPR / ATTN_THREADS;
+    static constexpr int CH = ATTN_K * L::CPR / ATTN_THREADS, STEP = ATTN_THREADS / L::CPR;  // pieces, rows from one to the next
     uint4 u[CH];
-    // row r lies at base + (r >> lgp) * stride + (r & (pack - 1)) * D
+    int64_t mine;  // the first piece's place in a tile
+    __device__ static inline int row() { return threadIdx.x / L::CPR; }
+    __device__ static inline int col() { return threadIdx.x % L::CPR * L::VE; }
+    // row r (r0 a multiple of four) lies at base + (r >> lgp) * stride + (r & (pack - 1)) * D
+    __device__ inline void init(int64_t stride, int lgp, int D) {
+        mine = (int64_t)(row() >> lgp) * stride + (row() & ((1 << lgp) - 1)) * D + (col() < D ? col() : 0);
+    }
+    __device__ inline uint4 get(const T* p, int D) const {
+        if constexpr (WHOLE) {
+            const piece_t w = *reinterpret_cast<const piece_t*>(p);
+            return make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+            return piece<T, false>(p, D - col());
+        }
+    }
     __device__ inline void load(const T* base, int64_t stride, int r0, int end, int lgp, int D) {
+        if (r0 + ATTN_K <= end) {
+            const T* p = base + (int64_t)(r0 >> lgp) * stride;
+            int64_t at = mine;
+            asm volatile("" : "+v"(at));  // (or every piece's place is kept in registers of its own)
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const int i = threadIdx.x + c * ATTN_THREADS, col = (i % L::CPR) * L::VE;
-            int r = r0 + i / L::CPR;
-            r = r < end ? r : end - 1;
-            const T* p = base + (int64_t)(r >> lgp) * stride + (r & ((1 << lgp) - 1)) * D + (col < D ? col : 0);
-            if constexpr (WHOLE) {
-                const piece_t w = *reinterpret_cast<const piece_t*>(p);
-                u[c] = make_uint4(w[0], w[1], w[2], w[3]);
-            } else {
-                u[c] = piece<T, false>(p, D - col);
+            for (int c = 0; c < CH; ++c) u[c] = get(p + (int64_t)(c * STEP >> lgp) * stride + at, D);
+        } else {
+            int first = r0 + row();
+            asm volatile("" : "+v"(first));
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                int r = first + c * STEP;
+                r = r < end ? r : end - 1;
+                u[c] = get(base + (int64_t)(r >> lgp) * stride + (r & ((1 << lgp) - 1)) * D + (col() < D ? col() : 0), D);
             }
         }
     }
     // CLEAN: infinite and undefined elements as zeros; returns whether there were any
     template <bool CLEAN>
-    __device__ inline bool put(unsigned char* lds, int r0, int end, int D) const {
-        bool met = false;
+    __device__ inline bool put(unsigned char* lds, int r0, int end, int D) {
+        if (r0 + ATTN_K > end || D != DP) {
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const int i = threadIdx.x + c * ATTN_THREADS;
-            const bool in = (r0 + i / L::CPR < end) & ((i % L::CPR) * L::VE < D);
-            uint4 v = make_uint4(in ? u[c].x : 0, in ? u[c].y : 0, in ? u[c].z : 0, in ? u[c].w : 0);
-            if (CLEAN && probe<T>(v, 0.f) != 0.f) {
-                v = clean<T>(v);
-                met = true;
+            for (int c = 0; c < CH; ++c) {
+                const bool in = (r0 + row() + c * STEP < end) & (col() < D);
+                u[c] = make_uint4(in ? u[c].x : 0, in ? u[c].y : 0, in ? u[c].z : 0, in ? u[c].w : 0);
             }
-            *reinterpret_cast<uint4*>(lds + i / L::CPR * L::PITCH + (i % L::CPR) * 16) = v;
         }
+        bool met = false;
+        if (CLEAN) {
+            Probe<T> probe;
+#pragma unroll
+            for (int c = 0; c < CH; ++c) probe.look(u[c]);
+            met = probe.met();
+            if (__any(met)) {
+#pragma unroll
+                for (int c = 0; c < CH; ++c) u[c] = clean<T>(u[c]);
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < CH; ++c) *reinterpret_cast<uint4*>(lds + (row() + c * STEP) * L::PITCH + col() * L::ES) = u[c];
         return met;
     }
 };
@@ -237,9 +265,9 @@ template <typename T, int DP>
 struct Computed {
     typedef Tile<T, DP> L;
     uint4 part[L::NP];
-    __device__ inline void set(const float4_t* p, int u) {  // p: blocks of 16 rows
+    __device__ inline void set(const float4_t (&p)[L::NX]) {
         if constexpr (L::ES == 2) {
-            const float4_t a = p[2 * u], b = p[2 * u + 1];
+            const float4_t a = p[0], b = p[1];
             const uint4 h = make_uint4(pack2(a[0], a[1]), pack2(a[2], a[3]), pack2(b[0], b[1]), pack2(b[2], b[3]));
             part[0] = h;
             const uint32_t w[4] = {h.x, h.y, h.z, h.w};
@@ -249,7 +277,7 @@ struct Computed {
             for (int i = 0; i < 4; ++i) l[i] = pack2(v[2 * i] - __uint_as_float(w[i] << 16), v[2 * i + 1] - __uint_as_float(w[i] & 0xffff0000u));
             part[1] = make_uint4(l[0], l[1], l[2], l[3]);
         } else {
-            const float4_t a = p[u];
+            const float4_t a = p[0];
             part[0] = make_uint4(__float_as_uint(a[0]), __float_as_uint(a[1]), __float_as_uint(a[2]), __float_as_uint(a[3]));
         }
     }
@@ -259,23 +287,20 @@ struct Computed {
     }
 };
 
-// acc[b][dt] (rows: columns 16 dt + 4 g + r of the tile; column: lane & 15) += tile^T computed[b], for NBLK blocks of 16 lanes' columns.
+// acc[b][dt] (rows: columns 16 dt + 4 g + r of the tile; column: lane & 15) += rows^T p[b] over the tile's rows u TU .., for NBLK blocks of 16
+// lanes' columns
 template <typename T, int DP, int NBLK>
-__device__ inline void fold(const unsigned char* lds, const float4_t (&p)[NBLK][4], float4_t (&acc)[NBLK][DP / 16]) {
+__device__ inline void fold(const unsigned char* lds, int u, const float4_t (&p)[NBLK][Tile<T, DP>::NX], float4_t (&acc)[NBLK][DP / 16], int lane) {
     typedef Tile<T, DP> L;
-    const int lane = lane_now();
+    Computed<T, DP> c[NBLK];
 #pragma unroll
-    for (int u = 0; u < L::NU; ++u) {
-        phase();
-        Computed<T, DP> c[NBLK];
+    for (int b = 0; b < NBLK; ++b) c[b].set(p[b]);
 #pragma unroll
-        for (int b = 0; b < NBLK; ++b) c[b].set(p[b], u);
+    for (int dt = 0; dt < L::NB; ++dt) {
+        if (dt && dt % 4 == 0) phase();
+        const uint4 f = L::turned(lds, u, dt, lane);
 #pragma unroll
-        for (int dt = 0; dt < L::NB; ++dt) {
-            const uint4 f = L::turned(lds, u, dt, lane);
-#pragma unroll
-            for (int b = 0; b < NBLK; ++b) c[b].product(f, acc[b][dt]);
-        }
+        for (int b = 0; b < NBLK; ++b) c[b].product(f, acc[b][dt]);
     }
     phase();
 }
@@ -295,21 +320,35 @@ __device__ inline void store4(T* p, int d, int D, const float4_t& v) {
         if (d + i < D) p[d + i] = cvt<T>(v[i]);
 }
 
-// Workgroups go round the eight XCDs: consecutive pieces of work to the same one, where their keys are in its L2
-__device__ inline uint32_t work_item(uint32_t total) {
-    const uint32_t x = blockIdx.x & 7, i = blockIdx.x >> 3, each = total >> 3, over = total & 7;
-    return x * each + (x < over ? x : over) + i;
-}
+// Which tile of which environment and heads (`rest`) a workgroup takes.  Workgroups go round the eight XCDs, and what belongs to one `rest` goes to the
+// same one, where its keys are in the L2.  Later rows see more keys (earlier keys are seen by more rows): the longest tiles first, of all that an
+// XCD has where these are few, so that the last ones to end are short.
+struct Place {
+    uint32_t rest;
+    int tile;
+    __device__ inline Place(const AttnArgs& g) {
+        const uint32_t x = blockIdx.x & 7, i = blockIdx.x >> 3, rests = g.total / g.tiles, own = rests >> 3;
+        if (own <= 16 && own * 8 == rests) {
+            rest = x + 8 * (i % own);
+            tile = g.tiles - 1 - (int)(i / own);
+        } else {
+            const uint32_t each = g.total >> 3, over = g.total & 7, w = x * each + (x < over ? x : over) + i;
+            rest = w / g.tiles;
+            tile = g.tiles - 1 - (int)(w % g.tiles);
+        }
+    }
+};
 
 // A workgroup's rows of queries: (step, head of the pack), heads next to each other
 struct Rows {
     int n, kv, h0, r0, rows, past;
     __device__ inline void init(const AttnArgs& g, int per) {
-        const uint32_t w = work_item(g.total), packs = g.H >> g.lgp, rest = w / g.tiles;
-        n = rest / packs;
-        h0 = (rest % packs) << g.lgp;
+        const Place at(g);
+        const uint32_t packs = g.H >> g.lgp;
+        n = at.rest / packs;
+        h0 = (at.rest % packs) << g.lgp;
         kv = h0 / (g.H / g.KV);
-        r0 = (g.tiles - 1 - (int)(w % g.tiles)) * per;  // the longest first
+        r0 = at.tile * per;
         rows = g.T << g.lgp;
         past = g.S - g.T;
     }
@@ -320,14 +359,15 @@ struct Rows {
 };
 
 // The bias of a tile by distance: entry [head][j] belongs to the distance `far` - j (or `far` + j), clamped to those there are
+template <int NR>  // entries that a thread stages
 struct Table {
-    float v[ATTN_TAB];
-    int b[ATTN_TAB];
+    float v[NR];
+    int b[NR];
     template <bool BUCKET>
     __device__ inline void load(const AttnArgs& g, int h0, int each, int far, int dir) {
         const int count = each << g.lgp;
 #pragma unroll
-        for (int c = 0; c < ATTN_TAB; ++c) {
+        for (int c = 0; c < NR; ++c) {
             int i = threadIdx.x + c * ATTN_THREADS;
             i = i < count ? i : count - 1;
             const int hh = i / each;
@@ -344,23 +384,23 @@ struct Table {
     __device__ inline void put(const AttnArgs& g, int each, float* tab, int* idx) const {
         const int count = each << g.lgp;
 #pragma unroll
-        for (int c = 0; c < ATTN_TAB; ++c) {
+        for (int c = 0; c < NR; ++c) {
             const int i = threadIdx.x + c * ATTN_THREADS;
             if (i >= count) break;  // (behind the loads)
             tab[i] = v[c];
-            if (BUCKET) idx[i] = b[c];
+            if (BUCKET && i < each) idx[i] = b[c];
         }
     }
 };
-#define ATTN_TAB_ROOM (ATTN_TAB * ATTN_THREADS)
 
 // ---- forward ------------------------------------------------------------------------------------------------------------
 template <typename T, int DP, int QB>
 struct FwdLds {
-    static constexpr int K = 0, V = Tile<T, DP>::BYTES, TAB = 2 * V, FLAG = TAB + ATTN_TAB_ROOM * 4, TOTAL = FLAG + 16;
+    static constexpr int ROOM = ATTN_ROOM(64 * QB, ATTN_K), NR = (ROOM + ATTN_THREADS - 1) / ATTN_THREADS;
+    static constexpr int K = 0, V = Tile<T, DP>::BYTES, TAB = 2 * V, FLAG = TAB + ROOM * 4, TOTAL = FLAG + 16;
 };
 template <typename T, int DP, int QB, bool WHOLE>
-__global__ __launch_bounds__(ATTN_THREADS) void k_attn_fwd(AttnArgs g) {
+__global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_fwd(AttnArgs g) {
     typedef Tile<T, DP> L;
     typedef FwdLds<T, DP, QB> M;
     extern __shared__ __align__(16) unsigned char lds[];
@@ -405,12 +445,16 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_fwd(AttnArgs g) {
         for (int dt = 0; dt < L::NB; ++dt) o[b][dt] = float4_t{0.f, 0.f, 0.f, 0.f};
     }
     if (threadIdx.x == 0) *flag = 0;
+    if (!g.table)
+        for (int i = threadIdx.x; i < M::ROOM; i += ATTN_THREADS) tab[i] = 0.f;
     Stage<T, DP, WHOLE> sk, sv;
-    Table st;
+    Table<M::NR> st;
+    sk.init(g.k_t, 0, g.D);
+    sv.init(g.k_t, 0, g.D);
     auto request = [&](int k0) {
         sk.load(kb, g.k_t, k0, k_end, 0, g.D);
         sv.load(vb, g.k_t, k0, k_end, 0, g.D);
-        if (g.table && first_p - (k0 + ATTN_K - 1) < last_edge) st.load<false>(g, R.h0, each, far - k0, -1);
+        if (g.table) st.template load<false>(g, R.h0, each, far - k0, -1);
     };
     request(k_begin);
     __syncthreads();
@@ -418,17 +462,18 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_fwd(AttnArgs g) {
         const bool near = g.table && first_p - (k0 + ATTN_K - 1) < last_edge;
         sk.template put<false>(lds + M::K, k0, k_end, g.D);
         if (sv.template put<true>(lds + M::V, k0, k_end, g.D)) *flag = 1;
-        if (near) st.put<false>(g, each, tab, nullptr);
+        if (g.table) st.template put<false>(g, each, tab, nullptr);
         __syncthreads();
         if (k0 + ATTN_K < k_end) request(k0 + ATTN_K);
         bool any = false, all = true;
 #pragma unroll
         for (int b = 0; b < QB; ++b) {
-            any |= p[b] >= k0 && lo[b] < k0 + ATTN_K;
-            all &= lo[b] <= k0 && p[b] >= k0 + ATTN_K - 1;
+            any |= (p[b] >= k0) & (lo[b] < k0 + ATTN_K);
+            all &= (lo[b] <= k0) & (p[b] >= k0 + ATTN_K - 1);
         }
-        if (__any(any)) {
-            const bool whole = __all(all);
+        // FAST: all of the tile is seen, at distances beyond the last edge
+        auto tile = [&](auto fast) {
+            constexpr bool FAST = decltype(fast)::value;
             float4_t s[QB][4];
             const int now = lane_now();
 #pragma unroll
@@ -443,38 +488,25 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_fwd(AttnArgs g) {
                     for (int b = 0; b < QB; ++b) Mma16<T>::run(f, qf[b][ks], s[b][x]);
                 }
             }
+            phase();
 #pragma unroll
             for (int b = 0; b < QB; ++b) {
-                if (near) {
-                    const float* row = tab + (lane & ((1 << g.lgp) - 1)) * each + 4 * gr + (t[b] < 0 ? 0 : far - p[b]);
-#pragma unroll
-                    for (int x = 0; x < 4; ++x)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) s[b][x][r] = __builtin_fmaf(s[b][x][r], c, row[16 * x + r]);
-                } else {
-#pragma unroll
-                    for (int x = 0; x < 4; ++x)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) s[b][x][r] = __builtin_fmaf(s[b][x][r], c, beyond);
-                }
-                if (!whole) {
-                    const int from = lo[b] - k0 - 4 * gr;
-                    const uint32_t span = p[b] - lo[b];  // (a row that is not there: begins at kNever, so no key lies in its span)
-#pragma unroll
-                    for (int x = 0; x < 4; ++x)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            s[b][x][r] = ((t[b] >= 0) & ((uint32_t)(16 * x + r - from) <= span)) ? s[b][x][r] : -__builtin_inff();
-                }
+                const float* row = tab + (now & ((1 << g.lgp) - 1)) * each + 4 * (now >> 4) + (t[b] < 0 ? 0 : far - p[b]);
+                const int from = lo[b] - k0 - 4 * (now >> 4);
+                const uint32_t span = p[b] - lo[b];
                 float top = m[b];
 #pragma unroll
                 for (int x = 0; x < 4; ++x)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) top = fmaxf(top, s[b][x][r]);
+                    for (int r = 0; r < 4; ++r) {
+                        float v = __builtin_fmaf(s[b][x][r], c, FAST ? beyond : row[16 * x + r]);
+                        if (!FAST) v = ((t[b] >= 0) & ((uint32_t)(16 * x + r - from) <= span)) ? v : -__builtin_inff();
+                        s[b][x][r] = v;
+                        top = fmaxf(top, v);
+                    }
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
                 const float base = top == -__builtin_inff() ? 0.f : top;  // nothing seen yet
-                const float fade = __builtin_amdgcn_exp2f(m[b] - base);
                 float sum = 0.f;
 #pragma unroll
                 for (int x = 0; x < 4; ++x)
@@ -484,6 +516,7 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_fwd(AttnArgs g) {
                         sum += s[b][x][r];
                     }
                 if (__any(top != m[b])) {
+                    const float fade = __builtin_amdgcn_exp2f(m[b] - base);
                     l[b] *= fade;
 #pragma unroll
                     for (int dt = 0; dt < L::NB; ++dt)
@@ -493,7 +526,19 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_fwd(AttnArgs g) {
                 l[b] += sum;
                 m[b] = top;
             }
-            fold<T, DP, QB>(lds + M::V, s, o);
+#pragma unroll
+            for (int u = 0; u < L::NU; ++u) {
+                float4_t part[QB][L::NX];
+#pragma unroll
+                for (int b = 0; b < QB; ++b)
+#pragma unroll
+                    for (int i = 0; i < L::NX; ++i) part[b][i] = s[b][u * L::NX + i];
+                fold<T, DP, QB>(lds + M::V, u, part, o, now);
+            }
+        };
+        if (__any(any)) {
+            if (!near && __all(all)) tile(std::true_type{});
+            else tile(std::false_type{});
         }
         __syncthreads();
     }
@@ -538,13 +583,49 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_fwd(AttnArgs g) {
     }
 }
 
+// Sums of a block of 16 keys and 16 rows along its slants (pairs of one distance): lane (a, g) holds the keys 4 g + r, r = 0 .. 3, of row a, that is
+// of step a / PACK, and key 4 g + r of step t + r is as far as key 4 g of step t.  x: the lane's, distance a / PACK - 4 g; y: those that lie
+// 16 / PACK steps further on, distance a / PACK - 16 / PACK - 4 g.
+template <int CTRL>
+__device__ inline float shifted(float v) {  // another lane's of the same 16, zero from beyond them
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+template <int PACK>
+struct Slant {
+    static __device__ inline float2 sum(const float4_t& v) {
+        constexpr int SHL = 0x100, SHR = 0x110;
+        return make_float2((v[0] + shifted<SHL + PACK>(v[1])) + (shifted<SHL + 2 * PACK>(v[2]) + shifted<SHL + 3 * PACK>(v[3])),
+                           (shifted<SHR + 16 - PACK>(v[1]) + shifted<SHR + 16 - 2 * PACK>(v[2])) + shifted<SHR + 16 - 3 * PACK>(v[3]));
+    }
+};
+// Four values of distances 16 apart into a lane's bins: those of one bucket together first, so that the reads of the bins need not wait for each other
+// (the last write of a bin is the one with the sum)
+// at: the first one's entry in the table; entries from `end` on are distances that no pair of the tile has
+__device__ inline void add_to_bins(float* bins, const int* idx, int at, int end, float4_t v) {
+    int b[4];
+    float old[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) b[x] = idx[at + 16 * x < end ? at + 16 * x : end - 1] * 64;
+#pragma unroll
+    for (int x = 3; x > 0; --x) {
+        const bool same = b[x] == b[x - 1];
+        v[x - 1] += same ? v[x] : 0.f;
+        v[x] = same ? 0.f : v[x];
+    }
+#pragma unroll
+    for (int x = 0; x < 4; ++x) old[x] = bins[b[x]];
+#pragma unroll
+    for (int x = 3; x >= 0; --x) bins[b[x]] = old[x] + v[x];
+}
+
 // ---- backward, queries: dq, the sums of dA by bucket, and delta ---------------------------------------------------------------
 template <typename T, int DP, int QB>
 struct DqLds {
-    static constexpr int K = 0, V = Tile<T, DP>::BYTES, TAB = 2 * V, IDX = TAB + ATTN_TAB_ROOM * 4, FLAG = IDX + ATTN_TAB_ROOM * 4, BINS = FLAG + 16;
+    static constexpr int ROOM = ATTN_ROOM(64 * QB, ATTN_K), NR = (ROOM + ATTN_THREADS - 1) / ATTN_THREADS;
+    static constexpr int K = 0, V = Tile<T, DP>::BYTES, TAB = 2 * V, IDX = TAB + ROOM * 4, FLAG = IDX + (64 * QB + ATTN_K) * 4, BINS = FLAG + 16;
 };
 template <typename T, int DP, int QB, bool WHOLE>
-__global__ __launch_bounds__(ATTN_THREADS) void k_attn_dq(AttnArgs g) {
+__global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_dq(AttnArgs g) {
     typedef Tile<T, DP> L;
     typedef DqLds<T, DP, QB> M;
     extern __shared__ __align__(16) unsigned char lds[];
@@ -553,7 +634,9 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_dq(AttnArgs g) {
     int* flag = reinterpret_cast<int*>(lds + M::FLAG);
     constexpr int BQ = 64 * QB;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, a = lane & 15, gr = lane >> 4, hh = lane & ((1 << g.lgp) - 1);
-    // every lane has bins of its own, one a bucket: no two lanes add to the same one, so the order of a bin's sum is the program's
+    // Sums of dA by bucket.  A lane adds up what it and its neighbours hold of one distance (see Slant) and adds that to a bin of its own: no two
+    // lanes have a bin in common, so the order of every sum is the program's.  (Added pair by pair by LDS atomics: 174 cycles for 64 of them, half
+    // of this kernel's time on 2048 x 8 x 8 heads of 128; laid out by distance in LDS and added up there: still a third.)
     float* bins = reinterpret_cast<float*>(lds + M::BINS) + (int64_t)wave * g.B * 64 + lane;
     Rows R;
     R.init(g, BQ);
@@ -619,14 +702,21 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_dq(AttnArgs g) {
 #pragma unroll
         for (int dt = 0; dt < L::NB; ++dt) o[b][dt] = float4_t{0.f, 0.f, 0.f, 0.f};
     if (threadIdx.x == 0) *flag = 0;
+    if (!g.table)
+        for (int i = threadIdx.x; i < M::ROOM; i += ATTN_THREADS) tab[i] = 0.f;
     if (g.part)
         for (int b = 0; b < g.B; ++b) bins[b * 64] = 0.f;
+    float carry[QB];  // of the tile before, of distances that go on here (one head a tile)
+#pragma unroll
+    for (int b = 0; b < QB; ++b) carry[b] = 0.f;
     Stage<T, DP, WHOLE> sk, sv;
-    Table st;
+    Table<M::NR> st;
+    sk.init(g.k_t, 0, g.D);
+    sv.init(g.k_t, 0, g.D);
     auto request = [&](int k0) {
         sk.load(kb, g.k_t, k0, k_end, 0, g.D);
         sv.load(vb, g.k_t, k0, k_end, 0, g.D);
-        if (g.table && first_p - (k0 + ATTN_K - 1) < last_edge) st.load<true>(g, R.h0, each, far - k0, -1);
+        if (g.table) st.template load<true>(g, R.h0, each, far - k0, -1);
     };
     request(k_begin);
     __syncthreads();
@@ -634,54 +724,83 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_dq(AttnArgs g) {
         const bool near = g.table && first_p - (k0 + ATTN_K - 1) < last_edge;
         if (sk.template put<true>(lds + M::K, k0, k_end, g.D)) *flag = 1;
         sv.template put<false>(lds + M::V, k0, k_end, g.D);
-        if (near) st.put<true>(g, each, tab, idx);
+        if (g.table) st.template put<true>(g, each, tab, idx);
         __syncthreads();
         if (k0 + ATTN_K < k_end) request(k0 + ATTN_K);
         bool any = false, all = true;
 #pragma unroll
         for (int b = 0; b < QB; ++b) {
-            any |= p[b] >= k0 && lo[b] < k0 + ATTN_K;
-            all &= lo[b] <= k0 && p[b] >= k0 + ATTN_K - 1;
+            any |= (p[b] >= k0) & (lo[b] < k0 + ATTN_K);
+            all &= (lo[b] <= k0) & (p[b] >= k0 + ATTN_K - 1);
         }
-        if (__any(any)) {
-            const bool whole = __all(all);
-            float4_t s[QB][4];
-            const int now = lane_now();
+        auto tile = [&](auto fast) {
+            constexpr bool FAST = decltype(fast)::value;
+            const int now = lane_now(), an = now & 15, gn = now >> 4;
+            float4_t main[QB], over[QB];  // by block of 16 keys: sums along a slant
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
+            for (int u = 0; u < L::NU; ++u) {
+                float4_t s[QB][L::NX], dp[QB][L::NX];
                 phase();
-                float4_t dp[QB];
 #pragma unroll
-                for (int b = 0; b < QB; ++b) s[b][x] = dp[b] = float4_t{0.f, 0.f, 0.f, 0.f};
+                for (int i = 0; i < L::NX; ++i) {
+                    const int x = u * L::NX + i;
+                    if (i && DP > 64) phase();
 #pragma unroll
-                for (int ks = 0; ks < L::KS; ++ks) {
-                    const uint4 f = L::rows(lds + M::K, 16 * x, ks, now), fv = L::rows(lds + M::V, 16 * x, ks, now);
+                    for (int b = 0; b < QB; ++b) s[b][i] = dp[b][i] = float4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int b = 0; b < QB; ++b) {
-                        Mma16<T>::run(f, qf[b][ks], s[b][x]);
-                        Mma16<T>::run(fv, of[b][ks], dp[b]);
-                    }
-                }
+                    for (int ks = 0; ks < L::KS; ++ks) {
+                        const uint4 f = L::rows(lds + M::K, 16 * x, ks, now), fv = L::rows(lds + M::V, 16 * x, ks, now);
 #pragma unroll
-                for (int b = 0; b < QB; ++b) {
-                    const int place = hh * each + 4 * (now >> 4) + (t[b] < 0 ? 0 : far - p[b]);
-                    const int from = lo[b] - k0 - 4 * (now >> 4);
-                    const uint32_t span = p[b] - lo[b];
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float shift = near ? tab[place + 16 * x + r] : beyond;
-                        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][x][r], c, shift) - lse[b]);
-                        const bool see = whole | ((t[b] >= 0) & ((uint32_t)(16 * x + r - from) <= span));
-                        const float da = see ? e * (dp[b][r] - delta[b]) : 0.f;
-                        s[b][x][r] = da;
-                        if (g.part) {
-                            if (near) __builtin_amdgcn_ds_faddf((__attribute__((address_space(3))) float*)(bins + idx[place + 16 * x + r] * 64), da, 0, 0, false);
-                            else outer += da;
+                        for (int b = 0; b < QB; ++b) {
+                            Mma16<T>::run(f, qf[b][ks], s[b][i]);
+                            Mma16<T>::run(fv, of[b][ks], dp[b][i]);
                         }
                     }
                 }
+                phase();
+#pragma unroll
+                for (int i = 0; i < L::NX; ++i)
+#pragma unroll
+                    for (int b = 0; b < QB; ++b) {
+                        const int x = u * L::NX + i, place = hh * each + 4 * gn + (t[b] < 0 ? 0 : far - p[b]);
+                        const int from = lo[b] - k0 - 4 * gn;
+                        const uint32_t span = p[b] - lo[b];
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i][r], c, FAST ? beyond : tab[place + 16 * x + r]) - lse[b]);
+                            float da = e * (dp[b][i][r] - delta[b]);
+                            if (!FAST) da = ((t[b] >= 0) & ((uint32_t)(16 * x + r - from) <= span)) ? da : 0.f;
+                            s[b][i][r] = da;
+                            if (FAST) outer += da;
+                        }
+                        if (!FAST && g.part) {
+                            const float2 v = g.lgp == 0 ? Slant<1>::sum(s[b][i]) : g.lgp == 1 ? Slant<2>::sum(s[b][i]) : Slant<4>::sum(s[b][i]);
+                            main[b][x] = v.x;
+                            over[b][x] = v.y;
+                        }
+                    }
+                phase();
+                fold<T, DP, QB>(lds + M::K, u, s, o, now);
             }
-            fold<T, DP, QB>(lds + M::K, s, o);
+            if (!FAST && g.part) {
+#pragma unroll
+                for (int b = 0; b < QB; ++b) {
+                    // entry of the table: (the tile's last step) - (the lane's step) + (its first key)
+                    const int at = far - R.past - (((R.r0 + (wave * QB + b) * 16 + an) >> g.lgp)) + 4 * gn;
+                    if (g.lgp == 0) {  // what lies beyond a block's first query goes with the next block of keys, of the same lane
+                        const float4_t v = {main[b][0] + carry[b], main[b][1] + over[b][0], main[b][2] + over[b][1], main[b][3] + over[b][2]};
+                        carry[b] = over[b][3];
+                        add_to_bins(bins, idx, at, each, v);
+                    } else {
+                        add_to_bins(bins, idx, at, each, main[b]);
+                        add_to_bins(bins, idx, at + (16 >> g.lgp), each, over[b]);
+                    }
+                }
+            }
+        };
+        if (__any(any)) {
+            if (!near && __all(all)) tile(std::true_type{});
+            else tile(std::false_type{});
         }
         __syncthreads();
     }
@@ -691,9 +810,11 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_dq(AttnArgs g) {
             for (int b = 0; b < QB; ++b) {
                 const bool see = (t[b] >= 0) & (k >= lo[b]) & (k <= p[b]);
                 if (!see || !tainted(kb + (int64_t)k * g.k_t, g.D)) continue;
-                outer = __builtin_nanf("");
+                const float nan = __builtin_nanf("");
+                if (g.part)
+                    for (int i = 0; i < g.B; ++i) bins[i * 64] = nan;
 #pragma unroll
-                for (int dt = 0; dt < L::NB; ++dt) o[b][dt] = float4_t{outer, outer, outer, outer};
+                for (int dt = 0; dt < L::NB; ++dt) o[b][dt] = float4_t{nan, nan, nan, nan};
             }
     }
 #pragma unroll
@@ -711,12 +832,22 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_dq(AttnArgs g) {
     if (!g.part) return;
     bins[(g.B - 1) * 64] += outer;
     __syncthreads();
-    const float* from = reinterpret_cast<const float*>(lds + M::BINS) + lane;
+    // eight threads a bucket: each adds up an eighth of its lanes (of one head, in an order that touches no bank twice) of all four waves
     const int64_t parts = (int64_t)g.N * g.tiles, mine = (int64_t)R.n * g.tiles + R.r0 / BQ;
-    for (int b = wave; b < g.B; b += 4) {
-        float sum = (from[b * 64] + from[(g.B + b) * 64]) + (from[(2 * g.B + b) * 64] + from[(3 * g.B + b) * 64]);
-        for (int o = 32; o >= 1 << g.lgp; o >>= 1) sum += __shfl_xor(sum, o);
-        if (lane < 1 << g.lgp) g.part[((int64_t)(R.h0 + lane) * g.B + b) * parts + mine] = sum;
+    const int part = threadIdx.x & 7, head = part & ((1 << g.lgp) - 1), eighth = part >> g.lgp;
+    for (int b0 = 0; b0 < g.B; b0 += 32) {
+        const int b = b0 + (threadIdx.x >> 3);
+        float sum = 0.f;
+        if (b < g.B) {
+            const float* from = reinterpret_cast<const float*>(lds + M::BINS) + b * 64 + head;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int at = (eighth * 8 + ((i + b) & 7)) << g.lgp;
+                sum += (from[at] + from[at + g.B * 64]) + (from[at + 2 * g.B * 64] + from[at + 3 * g.B * 64]);
+            }
+        }
+        for (int o = 1 << g.lgp; o < 8; o <<= 1) sum += __shfl_xor(sum, o);
+        if (b < g.B && part < 1 << g.lgp) g.part[((int64_t)(R.h0 + head) * g.B + b) * parts + mine] = sum;
     }
 }
 
@@ -737,10 +868,11 @@ __global__ __launch_bounds__(256) void k_attn_dbias(AttnArgs g) {
 // ---- backward, keys: dk and dv ---------------------------------------------------------------------------------------------------
 template <typename T, int DP, int KB>
 struct DkvLds {
-    static constexpr int Q = 0, O = Tile<T, DP>::BYTES, TAB = 2 * O, INFO = TAB + ATTN_TAB_ROOM * 4, FLAG = INFO + 3 * ATTN_K * 4, TOTAL = FLAG + 16;
+    static constexpr int ROOM = ATTN_ROOM(ATTN_K, 64 * KB), NR = (ROOM + ATTN_THREADS - 1) / ATTN_THREADS;
+    static constexpr int Q = 0, O = Tile<T, DP>::BYTES, TAB = 2 * O, INFO = TAB + ROOM * 4, FLAG = INFO + 3 * ATTN_K * 4, TOTAL = FLAG + 16;
 };
 template <typename T, int DP, int KB, bool WHOLE>
-__global__ __launch_bounds__(ATTN_THREADS) void k_attn_dkv(AttnArgs g) {
+__global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn_dkv(AttnArgs g) {
     typedef Tile<T, DP> L;
     typedef DkvLds<T, DP, KB> M;
     extern __shared__ __align__(16) unsigned char lds[];
@@ -751,12 +883,12 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_dkv(AttnArgs g) {
     int* flag = reinterpret_cast<int*>(lds + M::FLAG);
     constexpr int BK = 64 * KB;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, a = lane & 15, gr = lane >> 4;
-    const uint32_t w = work_item(g.total), rest = w / g.tiles;
+    const Place at(g);
     Rows R;
-    R.n = rest / g.KV;
-    R.kv = rest % g.KV;
+    R.n = at.rest / g.KV;
+    R.kv = at.rest % g.KV;
     R.past = g.S - g.T;
-    const int k0 = (int)(w % g.tiles) * BK, k_last = (k0 + BK < g.S ? k0 + BK : g.S) - 1;
+    const int k0 = (g.tiles - 1 - at.tile) * BK, k_last = (k0 + BK < g.S ? k0 + BK : g.S) - 1;
     uint4 kf[KB][L::KS], vf[KB][L::KS];
     int key[KB];
     float4_t dk[KB][L::NB], dv[KB][L::NB];
@@ -775,6 +907,8 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_dkv(AttnArgs g) {
         for (int dt = 0; dt < L::NB; ++dt) dk[b][dt] = dv[b][dt] = float4_t{0.f, 0.f, 0.f, 0.f};
     }
     if (threadIdx.x == 0) *flag = 0;
+    if (!g.table)
+        for (int i = threadIdx.x; i < M::ROOM; i += ATTN_THREADS) tab[i] = 0.f;
     const int pack = 1 << g.lgp, share = g.H / g.KV, each = (ATTN_K >> g.lgp) + BK;
     const int last_edge = g.table ? g.edges[g.B - 1] : 0;
     const float c = g.scale * kLog2e;
@@ -786,7 +920,9 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_dkv(AttnArgs g) {
         const T* qb = reinterpret_cast<const T*>(g.q) + (int64_t)R.n * g.q_n + (int64_t)h0 * g.D;
         const T* ob = reinterpret_cast<const T*>(g.dy) + (int64_t)R.n * g.y_n + (int64_t)h0 * g.D;
         Stage<T, DP, WHOLE> sq, so;
-        Table st;
+        Table<M::NR> st;
+        sq.init(g.q_t, g.lgp, g.D);
+        so.init(g.y_t, g.lgp, g.D);
         float i_lse = 0.f, i_delta = 0.f;
         int i_lo = kNever;
         float beyond[4];
@@ -796,7 +932,7 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_dkv(AttnArgs g) {
         auto request = [&](int r0) {
             sq.load(qb, g.q_t, r0, r_end, g.lgp, g.D);
             so.load(ob, g.y_t, r0, r_end, g.lgp, g.D);
-            if (near_at(r0)) st.load<false>(g, h0, each, R.past + (r0 >> g.lgp) - (k0 + BK - 1), 1);
+            if (g.table) st.template load<false>(g, h0, each, R.past + (r0 >> g.lgp) - (k0 + BK - 1), 1);
             if (threadIdx.x < ATTN_K) {
                 const int r = r0 + threadIdx.x;
                 i_lo = kNever;
@@ -815,7 +951,7 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_dkv(AttnArgs g) {
             const bool near = near_at(r0);
             const bool mq = sq.template put<true>(lds + M::Q, r0, r_end, g.D), mo = so.template put<true>(lds + M::O, r0, r_end, g.D);
             if (mq | mo) *flag = 1;
-            if (near) st.put<false>(g, each, tab, nullptr);
+            if (g.table) st.template put<false>(g, each, tab, nullptr);
             if (threadIdx.x < ATTN_K) {
                 row_lse[threadIdx.x] = i_lse;
                 row_delta[threadIdx.x] = i_delta;
@@ -825,51 +961,61 @@ __global__ __launch_bounds__(ATTN_THREADS) void k_attn_dkv(AttnArgs g) {
             if (row_lo[0] > k_last) break;  // (lo never falls: no later row sees a key here)
             if (r0 + ATTN_K < r_end) request(r0 + ATTN_K);
             const int p0 = R.past + (r0 >> g.lgp);
-            const bool whole = row_lo[ATTN_K - 1] <= k0 && p0 >= k0 + BK - 1;
-            float4_t s[KB][4], e[KB][4];
-            const int now = lane_now();
+            auto tile = [&](auto fast) {
+                constexpr bool FAST = decltype(fast)::value;
+                const int now = lane_now();
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                phase();
-                float4_t dp[KB];
+                for (int u = 0; u < L::NU; ++u) {
+                    float4_t s[KB][L::NX], e[KB][L::NX];
+                    phase();
 #pragma unroll
-                for (int b = 0; b < KB; ++b) s[b][x] = dp[b] = float4_t{0.f, 0.f, 0.f, 0.f};
+                    for (int i = 0; i < L::NX; ++i) {
+                        const int x = u * L::NX + i;
+                        if (i && DP > 64) phase();
 #pragma unroll
-                for (int ks = 0; ks < L::KS; ++ks) {
-                    const uint4 f = L::rows(lds + M::Q, 16 * x, ks, now), fo = L::rows(lds + M::O, 16 * x, ks, now);
+                        for (int b = 0; b < KB; ++b) s[b][i] = e[b][i] = float4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int b = 0; b < KB; ++b) {
-                        Mma16<T>::run(f, kf[b][ks], s[b][x]);
-                        Mma16<T>::run(fo, vf[b][ks], dp[b]);
+                        for (int ks = 0; ks < L::KS; ++ks) {
+                            const uint4 f = L::rows(lds + M::Q, 16 * x, ks, now), fo = L::rows(lds + M::O, 16 * x, ks, now);
+#pragma unroll
+                            for (int b = 0; b < KB; ++b) {
+                                Mma16<T>::run(f, kf[b][ks], s[b][i]);
+                                Mma16<T>::run(fo, vf[b][ks], e[b][i]);
+                            }
+                        }
                     }
+                    phase();
+#pragma unroll
+                    for (int i = 0; i < L::NX; ++i) {
+                        const int row = 16 * (u * L::NX + i) + 4 * (now >> 4);
+                        const float4_t lse = *reinterpret_cast<const float4_t*>(row_lse + row), delta = *reinterpret_cast<const float4_t*>(row_delta + row);
+                        const int4 lo4 = *reinterpret_cast<const int4*>(row_lo + row);
+                        const int lo[4] = {lo4.x, lo4.y, lo4.z, lo4.w};
+#pragma unroll
+                        for (int b = 0; b < KB; ++b) {
+                            const float* place = tab + (row >> g.lgp) + (k0 + BK - 1 - key[b]);
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                const int step = r >> g.lgp;
+                                const float shift = FAST ? beyond[r] : place[(r & (pack - 1)) * each + step];
+                                float v = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i][r], c, shift) - lse[r]), da = v * (e[b][i][r] - delta[r]);
+                                if (!FAST) {
+                                    const bool see = (lo[r] <= key[b]) & (key[b] <= p0 + (row >> g.lgp) + step);
+                                    v = see ? v : 0.f;
+                                    da = see ? da : 0.f;
+                                }
+                                e[b][i][r] = v;
+                                s[b][i][r] = da;
+                            }
+                        }
+                    }
+                    phase();
+                    fold<T, DP, KB>(lds + M::O, u, e, dv, now);
+                    fold<T, DP, KB>(lds + M::Q, u, s, dk, now);
                 }
-                const int row = 16 * x + 4 * (now >> 4);
-                const float4_t lse = *reinterpret_cast<const float4_t*>(row_lse + row), delta = *reinterpret_cast<const float4_t*>(row_delta + row);
-                const int4 lo4 = *reinterpret_cast<const int4*>(row_lo + row);
-                const int lo[4] = {lo4.x, lo4.y, lo4.z, lo4.w};
-#pragma unroll
-                for (int b = 0; b < KB; ++b) {
-                    float shift[4];
-                    if (near) {
-                        const float* place = tab + (row >> g.lgp) + (k0 + BK - 1 - key[b]);
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) shift[r] = place[(r & (pack - 1)) * each + (r >> g.lgp)];
-                    } else {
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) shift[r] = beyond[r];
-                    }
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int step = r >> g.lgp;
-                        const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][x][r], c, shift[r]) - lse[r]);
-                        const bool see = whole | ((lo[r] <= key[b]) & (key[b] <= p0 + (row >> g.lgp) + step));
-                        e[b][x][r] = see ? v : 0.f;
-                        s[b][x][r] = see ? v * (dp[b][r] - delta[r]) : 0.f;
-                    }
-                }
-            }
-            fold<T, DP, KB>(lds + M::O, e, dv);
-            fold<T, DP, KB>(lds + M::Q, s, dk);
+            };
+            if (!near && row_lo[ATTN_K - 1] <= k0 && p0 >= k0 + BK - 1) tile(std::true_type{});
+            else tile(std::false_type{});
             __syncthreads();
         }
         __syncthreads();  // (a walk that ended early has not waited yet)
@@ -975,24 +1121,30 @@ static int attn_fwd_pass(AttnArgs& g, hipStream_t s) {
     return run_kernel(k_attn_fwd<T, DP, QB, WHOLE>, g, (int64_t)g.tiles * g.N * (g.H >> g.lgp), FwdLds<T, DP, QB>::TOTAL, s);
 }
 template <typename T, int DP, int QB, bool WHOLE>
-static int attn_bwd_pass(AttnArgs& g, hipStream_t s) {
+static int attn_dq_pass(AttnArgs& g, hipStream_t s) {
     g.tiles = (int)cdiv((int64_t)g.T << g.lgp, 64 * QB);
-    if (run_kernel(k_attn_dq<T, DP, QB, WHOLE>, g, (int64_t)g.tiles * g.N * (g.H >> g.lgp), DqLds<T, DP, QB>::BINS + (g.part ? g.B * 1024 : 0), s))
+    if (run_kernel(k_attn_dq<T, DP, QB, WHOLE>, g, (int64_t)g.tiles * g.N * (g.H >> g.lgp),
+                   DqLds<T, DP, QB>::BINS + (g.part ? g.B * 1024 : 0), s))
         return 1;
     if (g.part) k_attn_dbias<<<dim3((uint32_t)(g.H * g.B)), 256, 0, s>>>(g);
-    g.tiles = (int)cdiv(g.S, 64 * QB);
-    return run_kernel(k_attn_dkv<T, DP, QB, WHOLE>, g, (int64_t)g.tiles * g.N * g.KV, DkvLds<T, DP, QB>::TOTAL, s);
+    return 0;
 }
-template <typename T, int DP, int QB>
-static int attn_pass(AttnArgs& g, bool back, hipStream_t s) {
-    if (g.whole) return back ? attn_bwd_pass<T, DP, QB, true>(g, s) : attn_fwd_pass<T, DP, QB, true>(g, s);
-    return back ? attn_bwd_pass<T, DP, QB, false>(g, s) : attn_fwd_pass<T, DP, QB, false>(g, s);
+template <typename T, int DP, int KB, bool WHOLE>
+static int attn_dkv_pass(AttnArgs& g, hipStream_t s) {
+    g.tiles = (int)cdiv(g.S, 64 * KB);
+    return run_kernel(k_attn_dkv<T, DP, KB, WHOLE>, g, (int64_t)g.tiles * g.N * g.KV, DkvLds<T, DP, KB>::TOTAL, s);
 }
-// Two blocks of rows a wave where there are rows for them: what is read of the keys' tiles serves both
+// A wave takes one block of 16 rows; in the forward pass of long bf16 heads two where there are rows for them, as what is read of a tile then serves
+// both (2048 x 8 x 8 heads of 128: 167 us, one block 186; heads of 64, 64 steps: 90, one block 75; the backward kernels run out of registers).
+template <typename T, int DP, bool WHOLE>
+static int attn_whole(AttnArgs& g, bool back, hipStream_t s) {
+    constexpr int MORE = sizeof(T) == 2 && DP == 128 ? 2 : 1;
+    if (!back) return ((int64_t)g.T << g.lgp) > 64 ? attn_fwd_pass<T, DP, MORE, WHOLE>(g, s) : attn_fwd_pass<T, DP, 1, WHOLE>(g, s);
+    return attn_dq_pass<T, DP, 1, WHOLE>(g, s) || attn_dkv_pass<T, DP, 1, WHOLE>(g, s);
+}
 template <typename T, int DP>
 static int attn_rows(AttnArgs& g, bool back, hipStream_t s) {
-    if (sizeof(T) == 2 && ((int64_t)g.T << g.lgp) > 64) return attn_pass<T, DP, sizeof(T) == 2 ? 2 : 1>(g, back, s);
-    return attn_pass<T, DP, 1>(g, back, s);
+    return g.whole ? attn_whole<T, DP, true>(g, back, s) : attn_whole<T, DP, false>(g, back, s);
 }
 template <typename T>
 static int attn_pick(AttnArgs& g, bool back, hipStream_t s) {
