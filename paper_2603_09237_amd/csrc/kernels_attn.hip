@@ -65,7 +65,7 @@ __global__ __launch_bounds__(1024) void k_attn_prepare(AttnArgs g, int spans, in
         const int run = (g.S + lanes - 1) / lanes, s0 = c * run, s1 = s0 + run < g.S ? s0 + run : g.S;
         int mine = -1;
         if (n < g.N) {
-#pragma unroll 8
+#pragma unroll 16
             for (int s = s0; s < s1; ++s)
                 if (g.first[(int64_t)s * g.N + n]) mine = s;
         }
@@ -86,12 +86,14 @@ __global__ __launch_bounds__(1024) void k_attn_prepare(AttnArgs g, int spans, in
         }
         return;
     }
-    const int d = ((int)blockIdx.x - spans) * 1024 + threadIdx.x;
-    if (d >= g.reach) return;
+    const int i = ((int)blockIdx.x - spans) * 1024 + threadIdx.x, h = i / g.reach, d = i - h * g.reach;
+    if (threadIdx.x < g.B) last[threadIdx.x] = g.edges[threadIdx.x];
+    __syncthreads();
+    if (h >= g.H) return;
     int b = 0;
-    for (int j = 1; j < g.B; ++j) b += g.edges[j] <= d;
-    g.bucket[d] = b;
-    for (int h = 0; h < g.H; ++h) g.table[(int64_t)h * g.reach + d] = g.bias[(int64_t)h * g.B + b] * kLog2e;
+    for (int j = 1; j < g.B; ++j) b += last[j] <= d;
+    if (h == 0) g.bucket[d] = b;
+    g.table[i] = g.bias[h * g.B + b] * kLog2e;
 }
 
 // ---- tiles ------------------------------------------------------------------------------------------------------------
@@ -1164,7 +1166,7 @@ int launch_attn_fwd(const morlax_attn_dims& d, const void* q, const void* k, con
         int lgn = 0;
         while (lgn < 4 && 1 << lgn < d.N) ++lgn;
         const int64_t spans = first ? cdiv(d.N, 1 << lgn) : 0;
-        k_attn_prepare<<<dim3((uint32_t)(spans + (g.B ? cdiv(g.reach, 1024) : 0))), 1024, 0, s>>>(g, (int)spans, lgn);
+        k_attn_prepare<<<dim3((uint32_t)(spans + (g.B ? cdiv((int64_t)g.H * g.reach, 1024) : 0))), 1024, 0, s>>>(g, (int)spans, lgn);
     }
     return d.dtype ? attn_pick<bf16_t>(g, false, s) : attn_pick<float>(g, false, s);
 }

@@ -5,17 +5,18 @@ static int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 constexpr float kLog2e = 1.4426950408889634f;
 
 // ---- pages --------------------------------------------------------------------------------------------------------------
-// Integers only: a workgroup owns 256 environments, one a thread; ranks (whose turn at the queue it is, where a page that goes back lies) are
+// Integers only: a workgroup owns 64 environments (256 of many), one a thread of its first waves; ranks (whose turn at the queue it is, where a page that goes back lies) are
 // sums over the workgroups before, which a first launch leaves where there is more than one.  Bound by latency for a few thousand environments
 // (two dependent launches of some microseconds), by the copy of the tables where they go into other buffers.
-#define PAGES_E 256
+#define PAGES_THREADS 256
 struct PagesArgs {
     const uint8_t* first;
     const int32_t *length_in, *table_in, *queue_in, *state_in;
     int32_t *length, *table, *queue, *state, *slot;
     int2* sums;        // of each workgroup: environments that need a page, pages that go back
     int32_t* was;      // [2] the state before
-    int N, lgp, slots, pages, blocks;
+    int N, lgp, lge, slots, pages, blocks;  // lge: 2^lge environments to a workgroup
+    RowDiv by_slots;
 };
 
 // a wave's sum of the values before a lane's, and of all
@@ -89,9 +90,9 @@ __device__ inline int wave_gives(const PagesArgs& g, int n, bool begins, F each)
     return mine;
 }
 
-__global__ __launch_bounds__(PAGES_E) void k_pages_count(PagesArgs g) {
+__global__ __launch_bounds__(PAGES_THREADS) void k_pages_count(PagesArgs g) {
     __shared__ int part[4];
-    const int n = blockIdx.x * PAGES_E + threadIdx.x;
+    const int n = (int)threadIdx.x < 1 << g.lge ? ((int)blockIdx.x << g.lge) + (int)threadIdx.x : g.N;
     PageOf e;
     e.look(g, n);
     const int gives = wave_gives(g, n, e.begins, [](int, int) {});
@@ -105,10 +106,11 @@ __global__ __launch_bounds__(PAGES_E) void k_pages_count(PagesArgs g) {
     }
 }
 
-__global__ __launch_bounds__(PAGES_E) void k_pages_apply(PagesArgs g) {
+__global__ __launch_bounds__(PAGES_THREADS) void k_pages_apply(PagesArgs g) {
     __shared__ int part[4], wave_back[4];
-    __shared__ int32_t column[PAGES_E], entry[PAGES_E];
-    const int n0 = blockIdx.x * PAGES_E, n = n0 + threadIdx.x, wave = threadIdx.x >> 6;
+    __shared__ int32_t column[PAGES_THREADS], entry[PAGES_THREADS];
+    const int n0 = (int)blockIdx.x << g.lge, wave = threadIdx.x >> 6;
+    const int n = (int)threadIdx.x < 1 << g.lge ? n0 + (int)threadIdx.x : g.N;
     PageOf e;
     e.look(g, n);
     int gives = 0;  // (of the wave; each pushes them below, once the place is known)
@@ -118,7 +120,7 @@ __global__ __launch_bounds__(PAGES_E) void k_pages_apply(PagesArgs g) {
     int head, count;
     if (g.blocks > 1) {
         int a = 0, b = 0, c = 0, d = 0;
-        for (int i = threadIdx.x; i < g.blocks; i += PAGES_E) {
+        for (int i = threadIdx.x; i < g.blocks; i += PAGES_THREADS) {
             const int2 s = g.sums[i];
             if (i < (int)blockIdx.x) { a += s.x; b += s.y; }
             c += s.x;
@@ -153,15 +155,15 @@ __global__ __launch_bounds__(PAGES_E) void k_pages_apply(PagesArgs g) {
     const int64_t base = tail + wave_back[wave];
     wave_gives(g, n, e.begins, [&](int at, int page) { g.queue[ring(base + at)] = page; });
     __syncthreads();  // (the rows of episodes that begin have been read: they may be written)
-    const int here = g.N - n0 < PAGES_E ? g.N - n0 : PAGES_E;
+    const int here = g.N - n0 < 1 << g.lge ? g.N - n0 : 1 << g.lge;
     if (g.table != g.table_in) {
-        const int64_t from = (int64_t)n0 * g.slots;
-        for (int64_t i = threadIdx.x; i < (int64_t)here * g.slots; i += PAGES_E) {
-            const int r = (int)(i / g.slots), j = (int)(i - (int64_t)r * g.slots), c = column[r];
-            int v = g.table_in[from + i];
-            if (c <= -2) v = j == 0 ? entry[r] : -1;
-            else if (c == j) v = entry[r];
-            g.table[from + i] = v;
+        const int32_t* from = g.table_in + (int64_t)n0 * g.slots;
+        int32_t* to = g.table + (int64_t)n0 * g.slots;
+#pragma unroll 4
+        for (int i = threadIdx.x; i < here * g.slots; i += PAGES_THREADS) {
+            const int r = (int)g.by_slots.quotient((uint32_t)i), j = i - r * g.slots, c = column[r];
+            const int old = from[i], now = entry[r];
+            to[i] = c <= -2 ? (j == 0 ? now : -1) : c == j ? now : old;
         }
     } else if (n < g.N && e.live) {
         if (e.begins)
@@ -171,7 +173,7 @@ __global__ __launch_bounds__(PAGES_E) void k_pages_apply(PagesArgs g) {
     if (g.queue != g.queue_in) {  // what no page went back to
         const int64_t per = ((int64_t)g.pages + g.blocks - 1) / g.blocks, i0 = blockIdx.x * per, i1 = i0 + per < g.pages ? i0 + per : g.pages;
         const int tail0 = ring((int64_t)head + count);
-        for (int64_t i = i0 + threadIdx.x; i < i1; i += PAGES_E) {
+        for (int64_t i = i0 + threadIdx.x; i < i1; i += PAGES_THREADS) {
             const int64_t d = i - tail0 < 0 ? i - tail0 + g.pages : i - tail0;
             if (d >= back_all) g.queue[i] = g.queue_in[i];
         }
@@ -228,11 +230,24 @@ __device__ inline float element(const uint4& u, int i) {  // i known after unrol
 
 #define STEP_U 4  // keys that a group of lanes requests together
 
+template <int CTRL>
+__device__ inline float moved(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true)); }
+// the sum over a group of L lanes, in all of them: within four, then the other four (mirrored), the other eight, the other sixteen
+template <int L>
+__device__ inline float group_sum(float v) {
+    v += moved<0xb1>(v);
+    v += moved<0x4e>(v);
+    if (L > 4) v += moved<0x141>(v);
+    if (L > 8) v += moved<0x140>(v);
+    if (L > 16) v += __shfl_xor(v, 16);
+    return v;
+}
+
 template <typename T, int DP, int GQ>
 __global__ __launch_bounds__(256) void k_attn_step(StepArgs g) {
     constexpr int VE = 16 / sizeof(T), LPK = DP / VE, KPW = 64 / LPK, STRIDE = 4 * KPW * STEP_U;
     __shared__ float bias[GQ][64];
-    __shared__ int32_t edges[64];
+    __shared__ int32_t edges[64];  // those that are not there: no distance reaches them
     __shared__ float2 wave_m[4][GQ];
     __shared__ float wave_o[4][GQ][DP];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane % LPK, key = lane / LPK;
@@ -279,7 +294,7 @@ __global__ __launch_bounds__(256) void k_attn_step(StepArgs g) {
     }
     int last_edge = 0;
     if (g.B) {
-        if (threadIdx.x < g.B) edges[threadIdx.x] = g.edges[threadIdx.x];
+        if (threadIdx.x < 64) edges[threadIdx.x] = (int)threadIdx.x < g.B ? g.edges[threadIdx.x] : 0x7fffffff;
         for (int i = threadIdx.x; i < GQ * g.B; i += 256) bias[i / g.B][i % g.B] = i / g.B < heads ? g.bias[(int64_t)(h0 + i / g.B) * g.B + i % g.B] * kLog2e : 0.f;
         last_edge = g.edges[g.B - 1];
     }
@@ -329,16 +344,13 @@ __global__ __launch_bounds__(256) void k_attn_step(StepArgs g) {
                 for (int i = 0; i < GQ; ++i) s[u][i] = __builtin_fmaf(x, qf[i][e], s[u][i]);
             }
 #pragma unroll
-            for (int x = LPK / 2; x; x >>= 1)
-#pragma unroll
-                for (int i = 0; i < GQ; ++i) s[u][i] += __shfl_xor(s[u][i], x);
+            for (int i = 0; i < GQ; ++i) s[u][i] = group_sum<LPK>(s[u][i]);
             int b = g.B - 1;
-            if (g.B) {
-                const int dist = pos - (int)(at + my + u * 4 * KPW);
-                if (dist < last_edge) {
-                    b = 0;
-                    for (int j = 1; j < g.B; ++j) b += edges[j] <= dist;
-                }
+            const int dist = pos - (int)(at + my + u * 4 * KPW);
+            if (dist < last_edge) {  // the last edge that is not beyond the distance (one by one: 5 us of a workgroup's time)
+                b = 0;
+#pragma unroll
+                for (int x = 32; x; x >>= 1) b += edges[b + x] <= dist ? x : 0;
             }
 #pragma unroll
             for (int i = 0; i < GQ; ++i) {
@@ -412,37 +424,42 @@ __global__ __launch_bounds__(256) void k_attn_step(StepArgs g) {
     }
 }
 
-// the parts of an environment and head, joined: one wave each
+// the parts of an environment and head, joined: a workgroup each, every wave a quarter of them
 template <typename T>
 __global__ __launch_bounds__(256) void k_attn_join(StepArgs g) {
-    const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63;
-    if (i >= (int64_t)g.N * g.H) return;
+    __shared__ float sums[4], outs[4][128];
+    const int64_t i = blockIdx.x;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int n = (int)(i / g.H), h = (int)(i % g.H);
     T* y = reinterpret_cast<T*>(g.y) + (int64_t)n * g.y_n + (int64_t)h * g.D;
     if (g.length[n] <= 0) {
-        for (int d = lane; d < g.D; d += 64) y[d] = (T)0.f;
+        if ((int)threadIdx.x < g.D) y[threadIdx.x] = (T)0.f;
         return;
     }
     const float2* pm = g.part_m + i * g.splits;
     const float* po = g.part_o + i * g.splits * g.D;
+    const int d0 = lane < g.D ? lane : 0, d1 = lane + 64 < g.D ? lane + 64 : 0;
     float top = -__builtin_inff();
     for (int s = lane; s < g.splits; s += 64) top = fmaxf(top, pm[s].x);
 #pragma unroll
     for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
     const float base = top == -__builtin_inff() ? 0.f : top;
     float sum = 0.f, out[2] = {0.f, 0.f};
-    const int d0 = lane < g.D ? lane : 0, d1 = lane + 64 < g.D ? lane + 64 : 0;
-#pragma unroll 4
-    for (int s = 0; s < g.splits; ++s) {
+#pragma unroll 8
+    for (int s = wave; s < g.splits; s += 4) {
         const float2 p = pm[s];
+        const float a = po[(int64_t)s * g.D + d0], b = po[(int64_t)s * g.D + d1];
         const float f = __builtin_amdgcn_exp2f(p.x - base);
         sum = __builtin_fmaf(f, p.y, sum);
-        out[0] = __builtin_fmaf(f, po[(int64_t)s * g.D + d0], out[0]);
-        out[1] = __builtin_fmaf(f, po[(int64_t)s * g.D + d1], out[1]);
+        out[0] = __builtin_fmaf(f, a, out[0]);
+        out[1] = __builtin_fmaf(f, b, out[1]);
     }
-    if (lane < g.D) y[lane] = cvt<T>(out[0] / sum);
-    if (lane + 64 < g.D) y[lane + 64] = cvt<T>(out[1] / sum);
+    if (lane == 0) sums[wave] = sum;
+    outs[wave][lane] = out[0];
+    outs[wave][lane + 64] = out[1];
+    __syncthreads();
+    const int d = threadIdx.x;
+    if (d < g.D) y[d] = cvt<T>(((outs[0][d] + outs[1][d]) + (outs[2][d] + outs[3][d])) / ((sums[0] + sums[1]) + (sums[2] + sums[3])));
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------------------------------
@@ -452,7 +469,10 @@ static int log2_of(int v) {
     return l;
 }
 static int64_t pages_carve(PagesArgs& g, const morlax_pages_dims& d, void* ws) {
-    g.N = d.N; g.lgp = log2_of(d.page); g.slots = d.slots; g.pages = d.pages; g.blocks = (int)cdiv(d.N, PAGES_E);
+    g.N = d.N; g.lgp = log2_of(d.page); g.slots = d.slots; g.pages = d.pages;
+    g.lge = d.N <= 65536 ? 6 : 8;
+    g.blocks = (int)cdiv(d.N, 1 << g.lge);
+    g.by_slots = row_div((uint32_t)d.slots);
     g.was = reinterpret_cast<int32_t*>(ws);
     g.sums = reinterpret_cast<int2*>(reinterpret_cast<char*>(ws) + 256);
     return 256 + (int64_t)g.blocks * 8;
@@ -467,8 +487,8 @@ void launch_cache_pages(const morlax_pages_dims& d, const uint8_t* first, const 
     g.first = first; g.length_in = length_in; g.table_in = table_in; g.queue_in = queue_in; g.state_in = state_in;
     g.length = length; g.table = table; g.queue = queue; g.state = state; g.slot = slot;
     pages_carve(g, d, ws);
-    if (g.blocks > 1) k_pages_count<<<dim3(g.blocks), PAGES_E, 0, s>>>(g);
-    k_pages_apply<<<dim3(g.blocks), PAGES_E, 0, s>>>(g);
+    if (g.blocks > 1) k_pages_count<<<dim3(g.blocks), PAGES_THREADS, 0, s>>>(g);
+    k_pages_apply<<<dim3(g.blocks), PAGES_THREADS, 0, s>>>(g);
 }
 
 static int heads_of_workgroup(int share) { return share >= 5 ? 8 : share >= 3 ? 4 : share; }
@@ -502,7 +522,7 @@ static void step_pass(const StepArgs& g, hipStream_t s) {
         case 4: k_attn_step<T, DP, 4><<<grid, 256, 0, s>>>(g); break;
         default: k_attn_step<T, DP, 8><<<grid, 256, 0, s>>>(g);
     }
-    if (g.splits > 1) k_attn_join<T><<<dim3((uint32_t)cdiv((int64_t)g.N * g.H, 4)), 256, 0, s>>>(g);
+    if (g.splits > 1) k_attn_join<T><<<dim3((uint32_t)((int64_t)g.N * g.H)), 256, 0, s>>>(g);
 }
 template <typename T>
 static void step_pick(const StepArgs& g, hipStream_t s) {

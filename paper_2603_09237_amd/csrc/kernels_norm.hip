@@ -3,7 +3,7 @@
 // and its gradients, with dY = dy + r_y (w_pre dh) - y r_y^3 mean(w_pre dh y):
 //   dx = dY,  dscale = sum dY sigmoid(gate) n,  dgate = dY scale n s (1 - s),  dn = dY scale s,
 //   dw_post = sum dn u r_u,  du = r_u (w_post dn) - u r_u^3 mean(w_post dn u),  dw_pre = sum dh y r_y.
-// Bound: HBM.  Every tensor goes through registers once: a row lies along the lanes of a wave (or of four, beyond 128 pieces of 16 bytes), the
+// Bound: HBM.  Every tensor goes through registers once: a row lies along the lanes of a wave, 16 bytes each (or of up to sixteen waves), the
 // backward computes n, y and both means again, and a workgroup keeps the three columns' sums of its rows in registers until its last row.
 #include "mlp_device.h"
 
@@ -24,18 +24,6 @@ template <typename T> struct Run16 {  // 16 bytes of elements, aligned to one
     typedef T vec_t __attribute__((ext_vector_type(V), aligned(sizeof(T))));
 };
 template <typename T>
-__device__ inline void load_run(const T* p, int n, float (&v)[16 / sizeof(T)]) {
-    constexpr int V = Run16<T>::V;
-    if (n >= V) {
-        const typename Run16<T>::vec_t u = *reinterpret_cast<const typename Run16<T>::vec_t*>(p);
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = (float)u[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = i < n ? to_f(p[i]) : 0.f;
-    }
-}
-template <typename T>
 __device__ inline void save_run(T* p, int n, const float (&v)[16 / sizeof(T)]) {
     constexpr int V = Run16<T>::V;
     if (n >= V) {
@@ -49,16 +37,26 @@ __device__ inline void save_run(T* p, int n, const float (&v)[16 / sizeof(T)]) {
             if (i < n) p[i] = cvt<T>(v[i]);
     }
 }
-// sum over the W waves of a row
+// sum over the W waves of a row, the same in all lanes
+template <int CTRL, int ROWS>
+__device__ inline float moved(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, ROWS, 0xf, true)); }
 template <int W>
 __device__ inline float row_sum(float v, float* lds) {
-#pragma unroll
-    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+    v += moved<0x111, 0xf>(v);  // along 16 lanes, into the last of them
+    v += moved<0x112, 0xf>(v);
+    v += moved<0x114, 0xf>(v);
+    v += moved<0x118, 0xf>(v);
+    v += moved<0x142, 0xa>(v);  // from the row before, from the two before
+    v += moved<0x143, 0xc>(v);
+    v = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
     if constexpr (W == 1) return v;
     __syncthreads();
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
-    return (lds[0] + lds[1]) + (lds[2] + lds[3]);
+    float all = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) all += lds[w];
+    return all;
 }
 // sigmoid, and what it lacks to one (from the exponential of -|v|, so that neither loses its digits or overflows)
 __device__ inline float2 sigmoid_of(float v) {
@@ -66,20 +64,58 @@ __device__ inline float2 sigmoid_of(float v) {
     return v >= 0.f ? make_float2(r, e * r) : make_float2(e * r, v == v ? r : v);
 }
 
-// A row of up to W * 64 * V * CH elements, W waves of 64 lanes
+// 16 bytes of a row as they are in memory; elements from n on are zero
+template <typename T>
+struct Piece {
+    typename Run16<T>::vec_t u;
+    __device__ inline void load(const T* p, int n) {
+        constexpr int V = Run16<T>::V;
+        if (n >= V) {
+            u = *reinterpret_cast<const typename Run16<T>::vec_t*>(p);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) u[i] = i < n ? p[i] : (T)0.f;
+        }
+    }
+    __device__ inline void get(float (&v)[16 / sizeof(T)]) const {
+#pragma unroll
+        for (int i = 0; i < Run16<T>::V; ++i) v[i] = (float)u[i];
+    }
+};
+// A row of up to W * 64 * V * CH elements, W waves of 64 lanes: what is requested of it ...
+template <typename T, int W, int CH, bool BACK>
+struct NormInput {
+    Piece<T> x[CH], u[CH], s[CH], dy[BACK ? CH : 1], dh[BACK ? CH : 1];
+    __device__ static inline int col(int c) { return (c * W * 64 + (W == 1 ? threadIdx.x & 63 : threadIdx.x)) * Run16<T>::V; }
+    __device__ inline void load(const NormArgs& g, int64_t row) {
+        row = row < g.rows ? row : g.rows - 1;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int at = col(c), left = g.width - at;
+            x[c].load(reinterpret_cast<const T*>(g.x) + row * g.ld_x + at, left);
+            u[c].load(reinterpret_cast<const T*>(g.u) + row * g.ld_u + at, g.u ? left : 0);
+            s[c].load(reinterpret_cast<const T*>(g.gate) + row * g.ld_g + at, g.gate ? left : 0);
+            if (BACK) {
+                dy[c].load(reinterpret_cast<const T*>(g.dy) + row * g.ld_x + at, g.dy ? left : 0);
+                dh[c].load(reinterpret_cast<const T*>(g.dh) + row * g.ld_h + at, g.dh ? left : 0);
+            }
+        }
+    }
+};
+// ... and what becomes of it
 template <typename T, int W, int CH>
 struct NormRow {
     static constexpr int V = 16 / sizeof(T);
     float x[CH][V], u[CH][V], s[CH][V], n[CH][V];  // s: the gate; after value(): x is y, n the normed u
     float r_u, r_y;
-    __device__ static inline int col(int c) { return (c * W * 64 + (W == 1 ? threadIdx.x & 63 : threadIdx.x)) * V; }
-    __device__ inline void load(const NormArgs& g, int64_t row) {
+    __device__ static inline int col(int c) { return NormInput<T, W, CH, false>::col(c); }
+    template <bool BACK>
+    __device__ inline void take(const NormInput<T, W, CH, BACK>& in) {
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int at = col(c), left = g.width - at;
-            load_run(reinterpret_cast<const T*>(g.x) + row * g.ld_x + at, left, x[c]);
-            if (g.u) load_run(reinterpret_cast<const T*>(g.u) + row * g.ld_u + at, left, u[c]);
-            if (g.gate) load_run(reinterpret_cast<const T*>(g.gate) + row * g.ld_g + at, left, s[c]);
+            in.x[c].get(x[c]);
+            in.u[c].get(u[c]);
+            in.s[c].get(s[c]);
         }
     }
     __device__ inline void value(const NormArgs& g, const float (&sc)[CH][V], const float (&wo)[CH][V], float* lds) {
@@ -124,17 +160,20 @@ __device__ inline void columns(const NormArgs& g, const float* p, float (&v)[CH]
 }
 
 template <typename T, int W, int CH>
-__global__ __launch_bounds__(256) void k_norm_fwd(NormArgs g) {
+__global__ __launch_bounds__(W == 1 ? 256 : W * 64) void k_norm_fwd(NormArgs g) {
     constexpr int V = 16 / sizeof(T);
-    __shared__ float lds[4];
+    __shared__ float lds[W];
     float sc[CH][V], wo[CH][V], wi[CH][V];
     columns<T, W, CH>(g, g.scale, sc);
     columns<T, W, CH>(g, g.w_post, wo);
     columns<T, W, CH>(g, g.w_pre, wi);
-    const int64_t per = W == 1 ? 4 : 1;
-    for (int64_t row = blockIdx.x * per + (W == 1 ? threadIdx.x >> 6 : 0); row < g.rows; row += gridDim.x * per) {
+    const int64_t per = W == 1 ? 4 : 1, first = blockIdx.x * per + (W == 1 ? threadIdx.x >> 6 : 0);
+    NormInput<T, W, CH, false> in;
+    if (first < g.rows) in.load(g, first);
+    for (int64_t row = first; row < g.rows; row += gridDim.x * per) {
         NormRow<T, W, CH> r;
-        r.load(g, row);
+        r.take(in);
+        in.load(g, row + gridDim.x * per);  // the next one's
         r.value(g, sc, wo, lds);
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
@@ -151,9 +190,9 @@ __global__ __launch_bounds__(256) void k_norm_fwd(NormArgs g) {
 }
 
 template <typename T, int W, int CH>
-__global__ __launch_bounds__(256) void k_norm_bwd(NormArgs g) {
+__global__ __launch_bounds__(W == 1 ? 256 : W * 64) void k_norm_bwd(NormArgs g) {
     constexpr int V = 16 / sizeof(T), CAP = 64 * V * CH;  // columns of a wave
-    __shared__ float lds[4];
+    __shared__ float lds[W];
     __shared__ float sums[W == 1 ? 3 * CAP : 1];
     float sc[CH][V], wo[CH][V], wi[CH][V], ds[CH][V], dwo[CH][V], dwi[CH][V];
     columns<T, W, CH>(g, g.scale, sc);
@@ -163,17 +202,19 @@ __global__ __launch_bounds__(256) void k_norm_bwd(NormArgs g) {
     for (int c = 0; c < CH; ++c)
 #pragma unroll
         for (int i = 0; i < V; ++i) ds[c][i] = dwo[c][i] = dwi[c][i] = 0.f;
-    const int64_t per = W == 1 ? 4 : 1;
-    for (int64_t row = blockIdx.x * per + (W == 1 ? threadIdx.x >> 6 : 0); row < g.rows; row += gridDim.x * per) {
+    const int64_t per = W == 1 ? 4 : 1, first = blockIdx.x * per + (W == 1 ? threadIdx.x >> 6 : 0);
+    NormInput<T, W, CH, true> in;
+    if (first < g.rows) in.load(g, first);
+    for (int64_t row = first; row < g.rows; row += gridDim.x * per) {
         NormRow<T, W, CH> r;
         float dy[CH][V], dh[CH][V];
-        r.load(g, row);
+        r.take(in);
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int at = r.col(c), left = g.width - at;
-            load_run(reinterpret_cast<const T*>(g.dy) + row * g.ld_x + at, g.dy ? left : 0, dy[c]);
-            load_run(reinterpret_cast<const T*>(g.dh) + row * g.ld_h + at, g.dh ? left : 0, dh[c]);
+            in.dy[c].get(dy[c]);
+            in.dh[c].get(dh[c]);
         }
+        in.load(g, row + gridDim.x * per);  // the next one's
         r.value(g, sc, wo, lds);
         if (g.dh) {
             float q = 0.f;
@@ -259,22 +300,25 @@ __global__ __launch_bounds__(256) void k_norm_bwd(NormArgs g) {
             }
     }
 }
-// the workgroups' sums: 64 columns of the three to a block, four threads a column
-__global__ __launch_bounds__(256) void k_norm_columns(NormArgs g) {
-    __shared__ float part[4][64];
-    const int c = blockIdx.x * 64 + (threadIdx.x & 63), w = threadIdx.x >> 6, all = 3 * g.width;
+// the workgroups' sums: 16 columns of the three to a block, 64 threads a column
+__global__ __launch_bounds__(1024) void k_norm_columns(NormArgs g) {
+    __shared__ float part[64][17];
+    const int lane = threadIdx.x & 15, w = threadIdx.x >> 4, c = blockIdx.x * 16 + lane, all = 3 * g.width;
     float sum = 0.f;
     if (c < all) {
 #pragma unroll 8
-        for (int b = w; b < g.blocks; b += 4) sum += g.part[(int64_t)b * all + c];
+        for (int b = w; b < g.blocks; b += 64) sum += g.part[(int64_t)b * all + c];
     }
-    part[w][threadIdx.x & 63] = sum;
+    part[w][lane] = sum;
     __syncthreads();
+    for (int o = 32; o; o >>= 1) {
+        if (w < o) part[w][lane] += part[w + o][lane];
+        __syncthreads();
+    }
     if (w || c >= all) return;
-    sum = (part[0][threadIdx.x] + part[1][threadIdx.x]) + (part[2][threadIdx.x] + part[3][threadIdx.x]);
     const int k = c / g.width, at = c - k * g.width;
     float* out = k == 0 ? g.dscale : k == 1 ? g.dw_post : g.dw_pre;
-    if (out) out[at] = sum;
+    if (out) out[at] = part[0][lane];
 }
 
 static NormArgs norm_args(const morlax_norm_dims& d) {
@@ -283,38 +327,49 @@ static NormArgs norm_args(const morlax_norm_dims& d) {
     g.ld_x = d.ld_x; g.ld_u = d.ld_u; g.ld_g = d.ld_g; g.ld_h = d.ld_h;
     return g;
 }
-// pieces of 16 bytes of a row; a wave holds two a lane
-static int norm_pieces(const morlax_norm_dims& d) { return (int)cdiv(d.width, d.dtype ? 8 : 4); }
+// Waves along a row: a lane holds one piece of 16 bytes (two in rows of more than 16 KB), as the backward keeps a piece's five tensors, their columns'
+// weights and sums and the next row's pieces in registers (two pieces a lane: 304 of them).  Workgroups of four rows where one wave is enough.
+static int norm_waves(const morlax_norm_dims& d) {
+    const int pieces = (int)cdiv(d.width, d.dtype ? 8 : 4);
+    int w = 1;
+    while (w < 16 && 64 * w < pieces) w *= 2;
+    return w;
+}
 static int norm_blocks(const morlax_norm_dims& d) {
-    const int64_t all = cdiv(d.rows, norm_pieces(d) <= 128 ? 4 : 1);
-    return (int)(all < 1 ? 1 : all < 1024 ? all : 1024);
+    const int w = norm_waves(d);
+    const int64_t all = cdiv(d.rows, w == 1 ? 4 : 1), most = w == 1 ? 1024 : 4096 / w;  // (what the last launch adds up stays a few per cent of the rows)
+    return (int)(all < 1 ? 1 : all < most ? all : most);
 }
 int64_t norm_ws_bytes(const morlax_norm_dims& d) { return (int64_t)norm_blocks(d) * 3 * d.width * 4; }
 
 template <typename T, int W, int CH>
 static void norm_pass(const NormArgs& g, bool back, hipStream_t s) {
+    constexpr int THREADS = W == 1 ? 256 : W * 64;
     if (back) {
-        k_norm_bwd<T, W, CH><<<dim3(g.blocks), 256, 0, s>>>(g);
+        k_norm_bwd<T, W, CH><<<dim3(g.blocks), THREADS, 0, s>>>(g);
     } else {
-        const int64_t all = cdiv(g.rows, W == 1 ? 4 : 1);
-        k_norm_fwd<T, W, CH><<<dim3((uint32_t)(all < 4096 ? all : 4096)), 256, 0, s>>>(g);
+        const int64_t all = cdiv(g.rows, W == 1 ? 4 : 1), most = W == 1 ? 4096 : 16384 / W;
+        k_norm_fwd<T, W, CH><<<dim3((uint32_t)(all < most ? all : most)), THREADS, 0, s>>>(g);
     }
 }
 template <typename T>
-static void norm_pick(const NormArgs& g, int pieces, bool back, hipStream_t s) {
-    if (pieces <= 64) norm_pass<T, 1, 1>(g, back, s);
-    else if (pieces <= 128) norm_pass<T, 1, 2>(g, back, s);
-    else if (pieces <= 256) norm_pass<T, 4, 1>(g, back, s);
-    else if (pieces <= 512) norm_pass<T, 4, 2>(g, back, s);
-    else if (sizeof(T) == 2 || pieces <= 1024) norm_pass<T, 4, 4>(g, back, s);
-    else norm_pass<T, 4, sizeof(T) == 2 ? 4 : 8>(g, back, s);
+static void norm_pick(const NormArgs& g, int waves, bool back, hipStream_t s) {
+    switch (waves) {
+        case 1: norm_pass<T, 1, 1>(g, back, s); break;
+        case 2: norm_pass<T, 2, 1>(g, back, s); break;
+        case 4: norm_pass<T, 4, 1>(g, back, s); break;
+        case 8: norm_pass<T, 8, 1>(g, back, s); break;
+        default:
+            if (sizeof(T) == 2 || g.width <= 4096) norm_pass<T, 16, 1>(g, back, s);
+            else norm_pass<T, 16, sizeof(T) == 2 ? 1 : 2>(g, back, s);
+    }
 }
 void launch_norm_fwd(const morlax_norm_dims& d, const void* x, const void* u, const void* gate, const float* scale, const float* w_post,
                      const float* w_pre, void* y, void* h, hipStream_t s) {
     NormArgs g = norm_args(d);
     g.x = x; g.u = u; g.gate = gate; g.scale = scale; g.w_post = w_post; g.w_pre = w_pre; g.y = y; g.h = h;
-    if (d.dtype) norm_pick<bf16_t>(g, norm_pieces(d), false, s);
-    else norm_pick<float>(g, norm_pieces(d), false, s);
+    if (d.dtype) norm_pick<bf16_t>(g, norm_waves(d), false, s);
+    else norm_pick<float>(g, norm_waves(d), false, s);
 }
 void launch_norm_bwd(const morlax_norm_dims& d, const void* x, const void* u, const void* gate, const float* scale, const float* w_post,
                      const float* w_pre, const void* dy, const void* dh, void* dx, void* du, void* dgate, float* dscale, float* dw_post, float* dw_pre,
@@ -324,7 +379,7 @@ void launch_norm_bwd(const morlax_norm_dims& d, const void* x, const void* u, co
     g.dx = dx; g.du = du; g.dgate = dgate; g.dscale = dscale; g.dw_post = dw_post; g.dw_pre = dw_pre;
     g.blocks = norm_blocks(d);
     if (dscale || dw_post || dw_pre) g.part = reinterpret_cast<float*>(ws);
-    if (d.dtype) norm_pick<bf16_t>(g, norm_pieces(d), true, s);
-    else norm_pick<float>(g, norm_pieces(d), true, s);
-    if (g.part) k_norm_columns<<<dim3((uint32_t)cdiv(3 * (int64_t)d.width, 64)), 256, 0, s>>>(g);
+    if (d.dtype) norm_pick<bf16_t>(g, norm_waves(d), true, s);
+    else norm_pick<float>(g, norm_waves(d), true, s);
+    if (g.part) k_norm_columns<<<dim3((uint32_t)cdiv(3 * (int64_t)d.width, 16)), 1024, 0, s>>>(g);
 }
