@@ -14,6 +14,7 @@
 // Query heads that share a head of keys are rows of the same tile (`pack` of them), so the keys are read once for all of them and the sums over
 // heads in dk and dv are sums over rows.
 #include "mlp_device.h"
+#include "pieces.h"
 
 static int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -131,25 +132,6 @@ struct Tile {
     }
 };
 
-// VE elements from p on (aligned to an element), those from `n` on zero; WHOLE: n is a multiple of VE
-typedef uint32_t piece_t __attribute__((ext_vector_type(4), aligned(2)));
-template <typename T, bool WHOLE>
-__device__ inline uint4 piece(const T* p, int n) {
-    constexpr int VE = 16 / sizeof(T);
-    if (WHOLE || n >= VE) {
-        if (n <= 0) return make_uint4(0, 0, 0, 0);
-        const piece_t u = *reinterpret_cast<const piece_t*>(p);
-        return make_uint4(u[0], u[1], u[2], u[3]);
-    }
-    uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-    for (int i = 0; i < VE; ++i) {
-        if (i >= n) break;
-        if constexpr (sizeof(T) == 2) w[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << (16 * (i & 1));
-        else w[i] = reinterpret_cast<const uint32_t*>(p)[i];
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
-}
 // A computed zero times an infinite or undefined element would reach rows that do not see it.  So such elements are put down as zeros in
 // the tiles that computed operands are multiplied with, and a workgroup that met one adds them in the end, one by one, to what sees them
 // (as they are: the products of the definition are infinite or undefined too).
@@ -200,21 +182,13 @@ template <typename T, int DP, bool WHOLE>
 struct Stage {
     typedef Tile<T, DP> L;
     static constexpr int CH = ATTN_K * L::CPR / ATTN_THREADS, STEP = ATTN_THREADS / L::CPR;  // pieces, rows from one to the next
-    uint4 u[CH];
-    int64_t mine;  // the first piece's place in a tile
+    RowPiece<T, WHOLE> in[CH];
+    int64_t mine;  // the first piece's row in a tile
     __device__ static inline int row() { return threadIdx.x / L::CPR; }
     __device__ static inline int col() { return threadIdx.x % L::CPR * L::VE; }
     // row r (r0 a multiple of four) lies at base + (r >> lgp) * stride + (r & (pack - 1)) * D
     __device__ inline void init(int64_t stride, int lgp, int D) {
-        mine = (int64_t)(row() >> lgp) * stride + (row() & ((1 << lgp) - 1)) * D + (col() < D ? col() : 0);
-    }
-    __device__ inline uint4 get(const T* p, int D) const {
-        if constexpr (WHOLE) {
-            const piece_t w = *reinterpret_cast<const piece_t*>(p);
-            return make_uint4(w[0], w[1], w[2], w[3]);
-        } else {
-            return piece<T, false>(p, D - col());
-        }
+        mine = (int64_t)(row() >> lgp) * stride + (row() & ((1 << lgp) - 1)) * D;
     }
     __device__ inline void load(const T* base, int64_t stride, int r0, int end, int lgp, int D) {
         if (r0 + ATTN_K <= end) {
@@ -222,7 +196,7 @@ struct Stage {
             int64_t at = mine;
             asm volatile("" : "+v"(at));  // (or every piece's place is kept in registers of its own)
 #pragma unroll
-            for (int c = 0; c < CH; ++c) u[c] = get(p + (int64_t)(c * STEP >> lgp) * stride + at, D);
+            for (int c = 0; c < CH; ++c) in[c].load(p + (int64_t)(c * STEP >> lgp) * stride + at, col(), D);
         } else {
             int first = r0 + row();
             asm volatile("" : "+v"(first));
@@ -230,19 +204,20 @@ struct Stage {
             for (int c = 0; c < CH; ++c) {
                 int r = first + c * STEP;
                 r = r < end ? r : end - 1;
-                u[c] = get(base + (int64_t)(r >> lgp) * stride + (r & ((1 << lgp) - 1)) * D + (col() < D ? col() : 0), D);
+                in[c].load(base + (int64_t)(r >> lgp) * stride + (r & ((1 << lgp) - 1)) * D, col(), D);
             }
         }
     }
     // CLEAN: infinite and undefined elements as zeros; returns whether there were any
     template <bool CLEAN>
     __device__ inline bool put(unsigned char* lds, int r0, int end, int D) {
-        if (r0 + ATTN_K > end || D != DP) {
+        uint4 u[CH];
+        if (WHOLE && r0 + ATTN_K <= end && D == DP) {
 #pragma unroll
-            for (int c = 0; c < CH; ++c) {
-                const bool in = (r0 + row() + c * STEP < end) & (col() < D);
-                u[c] = make_uint4(in ? u[c].x : 0, in ? u[c].y : 0, in ? u[c].z : 0, in ? u[c].w : 0);
-            }
+            for (int c = 0; c < CH; ++c) u[c] = in[c].u;
+        } else {
+#pragma unroll
+            for (int c = 0; c < CH; ++c) u[c] = in[c].get(col(), D, r0 + row() + c * STEP < end);
         }
         bool met = false;
         if (CLEAN) {
@@ -426,7 +401,9 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_fwd(At
 #pragma unroll
         for (int ks = 0; ks < L::KS; ++ks) {
             const int d = ks * (64 / L::ES) + gr * L::VE;
-            qf[b][ks] = piece<T, WHOLE>(src + (d < g.D ? d : 0), in ? g.D - d : 0);
+            RowPiece<T, WHOLE> u;
+            u.load(src, d, g.D);
+            qf[b][ks] = u.get(d, g.D, in);
         }
     }
     const int first_p = R.past + (R.r0 >> g.lgp), each = (BQ >> g.lgp) + ATTN_K, far = first_p + (BQ >> g.lgp) - 1;
@@ -660,13 +637,19 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_dq(Att
         float sum = 0.f;
 #pragma unroll
         for (int ks = 0; ks < L::KS; ++ks) {
-            const int d = ks * (64 / L::ES) + gr * L::VE, dc = d < g.D ? d : 0, left = in ? g.D - d : 0;
-            qf[b][ks] = piece<T, WHOLE>(src + dc, left);
-            of[b][ks] = piece<T, WHOLE>(dsrc + dc, left);
-            const uint4 yf = piece<T, WHOLE>(ysrc + dc, left);
+            const int d = ks * (64 / L::ES) + gr * L::VE;
+            RowPiece<T, WHOLE> uq, uo, uy;
+            uq.load(src, d, g.D);
+            uo.load(dsrc, d, g.D);
+            uy.load(ysrc, d, g.D);
+            RowPiece<bf16_t, WHOLE> ul;
+            if constexpr (L::ES == 2) ul.load(lsrc, d, g.D);
+            qf[b][ks] = uq.get(d, g.D, in);
+            of[b][ks] = uo.get(d, g.D, in);
+            const uint4 yf = uy.get(d, g.D, in);
             const uint32_t wy[4] = {yf.x, yf.y, yf.z, yf.w}, wd[4] = {of[b][ks].x, of[b][ks].y, of[b][ks].z, of[b][ks].w};
             if constexpr (L::ES == 2) {
-                const uint4 lf = piece<bf16_t, WHOLE>(lsrc + dc, left);
+                const uint4 lf = ul.get(d, g.D, in);
                 const uint32_t wl[4] = {lf.x, lf.y, lf.z, lf.w};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -708,9 +691,14 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_dq(Att
         for (int i = threadIdx.x; i < M::ROOM; i += ATTN_THREADS) tab[i] = 0.f;
     if (g.part)
         for (int b = 0; b < g.B; ++b) bins[b * 64] = 0.f;
-    float carry[QB];  // of the tile before, of distances that go on here (one head a tile)
+    float carry[QB];  // of the tile before, of distances that go on with the key `carry_k` (one head a tile)
+    int carry_k = 0;
+    bool lone[QB];    // sees itself only: its probability is one whatever the score, and dA nothing, not what two sums' roundings leave
 #pragma unroll
-    for (int b = 0; b < QB; ++b) carry[b] = 0.f;
+    for (int b = 0; b < QB; ++b) {
+        carry[b] = 0.f;
+        lone[b] = lo[b] == p[b];
+    }
     Stage<T, DP, WHOLE> sk, sv;
     Table<M::NR> st;
     sk.init(g.k_t, 0, g.D);
@@ -771,7 +759,7 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_dq(Att
                         for (int r = 0; r < 4; ++r) {
                             const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i][r], c, FAST ? beyond : tab[place + 16 * x + r]) - lse[b]);
                             float da = e * (dp[b][i][r] - delta[b]);
-                            if (!FAST) da = ((t[b] >= 0) & ((uint32_t)(16 * x + r - from) <= span)) ? da : 0.f;
+                            if (!FAST) da = ((t[b] >= 0) & !lone[b] & ((uint32_t)(16 * x + r - from) <= span)) ? da : 0.f;
                             s[b][i][r] = da;
                             if (FAST) outer += da;
                         }
@@ -784,6 +772,13 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_dq(Att
                 phase();
                 fold<T, DP, QB>(lds + M::K, u, s, o, now);
             }
+            if (FAST) {
+#pragma unroll
+                for (int b = 0; b < QB; ++b) {
+                    outer += carry[b];
+                    carry[b] = 0.f;
+                }
+            }
             if (!FAST && g.part) {
 #pragma unroll
                 for (int b = 0; b < QB; ++b) {
@@ -792,6 +787,7 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_dq(Att
                     if (g.lgp == 0) {  // what lies beyond a block's first query goes with the next block of keys, of the same lane
                         const float4_t v = {main[b][0] + carry[b], main[b][1] + over[b][0], main[b][2] + over[b][1], main[b][3] + over[b][2]};
                         carry[b] = over[b][3];
+                        carry_k = k0 + ATTN_K;
                         add_to_bins(bins, idx, at, each, v);
                     } else {
                         add_to_bins(bins, idx, at, each, main[b]);
@@ -833,6 +829,15 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_dq(Att
     }
     if (!g.part) return;
     bins[(g.B - 1) * 64] += outer;
+    if (g.lgp == 0) {
+#pragma unroll
+        for (int b = 0; b < QB; ++b) {  // (rows that are not there may lie between the last tile's keys and the block's last row)
+            int d = R.past + R.r0 + (wave * QB + b) * 16 + a - carry_k - 4 * gr;
+            d = d < 0 ? 0 : d >= g.reach ? g.reach - 1 : d;
+            const int i = g.bucket[d];
+            bins[(i < 0 ? 0 : i >= g.B ? g.B - 1 : i) * 64] += carry[b];
+        }
+    }
     __syncthreads();
     // eight threads a bucket: each adds up an eighth of its lanes (of one head, in an order that touches no bank twice) of all four waves
     const int64_t parts = (int64_t)g.N * g.tiles, mine = (int64_t)R.n * g.tiles + R.r0 / BQ;
@@ -901,9 +906,12 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn_dkv(AttnArgs g) {
         const int64_t at = (int64_t)(in ? key[b] : 0) * g.k_t + (int64_t)R.n * g.k_n + (int64_t)R.kv * g.D;
 #pragma unroll
         for (int ks = 0; ks < L::KS; ++ks) {
-            const int d = ks * (64 / L::ES) + gr * L::VE, dc = d < g.D ? d : 0, left = in ? g.D - d : 0;
-            kf[b][ks] = piece<T, WHOLE>(reinterpret_cast<const T*>(g.k) + at + dc, left);
-            vf[b][ks] = piece<T, WHOLE>(reinterpret_cast<const T*>(g.v) + at + dc, left);
+            const int d = ks * (64 / L::ES) + gr * L::VE;
+            RowPiece<T, WHOLE> uk, uv;
+            uk.load(reinterpret_cast<const T*>(g.k) + at, d, g.D);
+            uv.load(reinterpret_cast<const T*>(g.v) + at, d, g.D);
+            kf[b][ks] = uk.get(d, g.D, in);
+            vf[b][ks] = uv.get(d, g.D, in);
         }
 #pragma unroll
         for (int dt = 0; dt < L::NB; ++dt) dk[b][dt] = dv[b][dt] = float4_t{0.f, 0.f, 0.f, 0.f};
@@ -1002,9 +1010,10 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn_dkv(AttnArgs g) {
                                 const float shift = FAST ? beyond[r] : place[(r & (pack - 1)) * each + step];
                                 float v = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i][r], c, shift) - lse[r]), da = v * (e[b][i][r] - delta[r]);
                                 if (!FAST) {
-                                    const bool see = (lo[r] <= key[b]) & (key[b] <= p0 + (row >> g.lgp) + step);
+                                    const int p = p0 + (row >> g.lgp) + step;
+                                    const bool see = (lo[r] <= key[b]) & (key[b] <= p);
                                     v = see ? v : 0.f;
-                                    da = see ? da : 0.f;
+                                    da = see & (lo[r] != p) ? da : 0.f;  // (a row that sees itself only: nothing, see above)
                                 }
                                 e[b][i][r] = v;
                                 s[b][i][r] = da;

@@ -1,5 +1,6 @@
 // A paged cache of keys and values, one step at a time: the pages' bookkeeping, and the attention of every environment's new step over it.
 #include "mlp_device.h"
+#include "pieces.h"
 
 static int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 constexpr float kLog2e = 1.4426950408889634f;
@@ -202,25 +203,6 @@ struct StepArgs {
     int64_t q_n, k_n, y_n;
 };
 
-typedef uint32_t piece_t __attribute__((ext_vector_type(4), aligned(2)));
-// 16 bytes of elements from p on (aligned to an element), those from `n` on zero; whole: n is a multiple of as many
-template <typename T>
-__device__ inline uint4 piece(const T* p, int n, bool whole) {
-    constexpr int VE = 16 / sizeof(T);
-    if (whole || n >= VE) {
-        if (n <= 0) return make_uint4(0, 0, 0, 0);
-        const piece_t u = *reinterpret_cast<const piece_t*>(p);
-        return make_uint4(u[0], u[1], u[2], u[3]);
-    }
-    uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-    for (int i = 0; i < VE; ++i) {
-        if (i >= n) break;
-        if constexpr (sizeof(T) == 2) w[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << (16 * (i & 1));
-        else w[i] = reinterpret_cast<const uint32_t*>(p)[i];
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
-}
 template <typename T>
 __device__ inline float element(const uint4& u, int i) {  // i known after unrolling
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
@@ -243,7 +225,7 @@ __device__ inline float group_sum(float v) {
     return v;
 }
 
-template <typename T, int DP, int GQ>
+template <typename T, int DP, int GQ, bool WHOLE>
 __global__ __launch_bounds__(256) void k_attn_step(StepArgs g) {
     constexpr int VE = 16 / sizeof(T), LPK = DP / VE, KPW = 64 / LPK, STRIDE = 4 * KPW * STEP_U;
     __shared__ float bias[GQ][64];
@@ -254,7 +236,7 @@ __global__ __launch_bounds__(256) void k_attn_step(StepArgs g) {
     const int split = blockIdx.x % g.splits, rest = blockIdx.x / g.splits, chunk = rest % g.chunks, rest2 = rest / g.chunks;
     const int kv = rest2 % g.KV, n = rest2 / g.KV, share = g.H / g.KV, h0 = kv * share + chunk * GQ, heads = share - chunk * GQ < GQ ? share - chunk * GQ : GQ;
     const int length = g.length[n], pos = length - 1;
-    const int d = sub * VE, left = g.D - d, dc = left > 0 ? d : 0;
+    const int d = sub * VE;
     T* y = reinterpret_cast<T*>(g.y) + (int64_t)n * g.y_n;
     if (length <= 0) {
         if (g.splits == 1)
@@ -288,7 +270,9 @@ __global__ __launch_bounds__(256) void k_attn_step(StepArgs g) {
     float qf[GQ][VE];
 #pragma unroll
     for (int i = 0; i < GQ; ++i) {
-        const uint4 u = piece(reinterpret_cast<const T*>(g.q) + (int64_t)n * g.q_n + (int64_t)(h0 + (i < heads ? i : 0)) * g.D + dc, left, g.whole);
+        RowPiece<T, WHOLE> in;
+        in.load(reinterpret_cast<const T*>(g.q) + (int64_t)n * g.q_n + (int64_t)(h0 + (i < heads ? i : 0)) * g.D, d, g.D);
+        const uint4 u = in.get(d, g.D);
 #pragma unroll
         for (int e = 0; e < VE; ++e) qf[i][e] = element<T>(u, e);
     }
@@ -314,22 +298,22 @@ __global__ __launch_bounds__(256) void k_attn_step(StepArgs g) {
 #pragma unroll
         for (int u = 0; u < STEP_U; ++u) {
             const int64_t s = at + my + u * 4 * KPW;
-            id[u] = s < s1 ? table[slot_of((int)s)] : -1;
+            id[u] = table[slot_of((int)(s < s1 ? s : s1 - 1))];
         }
     };
     if (s0 < s1) look(s0);
     for (int64_t at = s0; at < s1; at += STRIDE) {
-        uint4 ku[STEP_U], vu[STEP_U];
+        RowPiece<T, WHOLE> kp[STEP_U], vp[STEP_U];
         bool in[STEP_U];
 #pragma unroll
         for (int u = 0; u < STEP_U; ++u) {
             const int64_t s = at + my + u * 4 * KPW;
             const bool now = s == pos;
-            in[u] = s < s1 && (now || (uint32_t)id[u] < (uint32_t)g.pages);
+            in[u] = (s < s1) & (now | ((uint32_t)id[u] < (uint32_t)g.pages));
             const int64_t off = (((int64_t)id[u] << g.lgp) + ((int)s & in_page)) * row;
-            const T *kp = now || !in[u] ? kn : kc + off, *vp = now || !in[u] ? vn : vc + off;
-            ku[u] = piece(kp + dc, in[u] ? left : 0, g.whole);
-            vu[u] = piece(vp + dc, in[u] ? left : 0, g.whole);
+            const bool held = in[u] & !now;
+            kp[u].load(held ? kc + off : kn, d, g.D);
+            vp[u].load(held ? vc + off : vn, d, g.D);
         }
         if (at + STRIDE < s1) look(at + STRIDE);
         float s[STEP_U][GQ];
@@ -337,9 +321,10 @@ __global__ __launch_bounds__(256) void k_attn_step(StepArgs g) {
         for (int u = 0; u < STEP_U; ++u) {
 #pragma unroll
             for (int i = 0; i < GQ; ++i) s[u][i] = 0.f;
+            const uint4 ku = kp[u].get(d, g.D, in[u]);
 #pragma unroll
             for (int e = 0; e < VE; ++e) {
-                const float x = element<T>(ku[u], e);
+                const float x = element<T>(ku, e);
 #pragma unroll
                 for (int i = 0; i < GQ; ++i) s[u][i] = __builtin_fmaf(x, qf[i][e], s[u][i]);
             }
@@ -370,10 +355,18 @@ __global__ __launch_bounds__(256) void k_attn_step(StepArgs g) {
             for (int e = 0; e < VE; ++e) o[i][e] *= fade;
 #pragma unroll
             for (int u = 0; u < STEP_U; ++u) {
-                const float p = __builtin_amdgcn_exp2f(s[u][i] - base);
-                l[i] += p;
+                s[u][i] = __builtin_amdgcn_exp2f(s[u][i] - base);
+                l[i] += s[u][i];
+            }
+        }
 #pragma unroll
-                for (int e = 0; e < VE; ++e) o[i][e] = __builtin_fmaf(p, element<T>(vu[u], e), o[i][e]);
+        for (int u = 0; u < STEP_U; ++u) {
+            const uint4 vu = vp[u].get(d, g.D, in[u]);
+#pragma unroll
+            for (int e = 0; e < VE; ++e) {
+                const float x = element<T>(vu, e);
+#pragma unroll
+                for (int i = 0; i < GQ; ++i) o[i][e] = __builtin_fmaf(s[u][i], x, o[i][e]);
             }
         }
     }
@@ -513,22 +506,22 @@ int64_t attn_step_ws_bytes(const morlax_cache_dims& d) {
     StepArgs g = {};
     return step_carve(g, d, nullptr);
 }
-template <typename T, int DP>
+template <typename T, int DP, bool WHOLE>
 static void step_pass(const StepArgs& g, hipStream_t s) {
     const dim3 grid((uint32_t)((int64_t)g.splits * g.chunks * g.KV * g.N));
     switch (heads_of_workgroup(g.H / g.KV)) {
-        case 1: k_attn_step<T, DP, 1><<<grid, 256, 0, s>>>(g); break;
-        case 2: k_attn_step<T, DP, 2><<<grid, 256, 0, s>>>(g); break;
-        case 4: k_attn_step<T, DP, 4><<<grid, 256, 0, s>>>(g); break;
-        default: k_attn_step<T, DP, 8><<<grid, 256, 0, s>>>(g);
+        case 1: k_attn_step<T, DP, 1, WHOLE><<<grid, 256, 0, s>>>(g); break;
+        case 2: k_attn_step<T, DP, 2, WHOLE><<<grid, 256, 0, s>>>(g); break;
+        case 4: k_attn_step<T, DP, 4, WHOLE><<<grid, 256, 0, s>>>(g); break;
+        default: k_attn_step<T, DP, 8, WHOLE><<<grid, 256, 0, s>>>(g);
     }
     if (g.splits > 1) k_attn_join<T><<<dim3((uint32_t)((int64_t)g.N * g.H)), 256, 0, s>>>(g);
 }
 template <typename T>
 static void step_pick(const StepArgs& g, hipStream_t s) {
-    if (g.D <= 32) step_pass<T, 32>(g, s);
-    else if (g.D <= 64) step_pass<T, 64>(g, s);
-    else step_pass<T, 128>(g, s);
+    if (g.D <= 32) g.whole ? step_pass<T, 32, true>(g, s) : step_pass<T, 32, false>(g, s);
+    else if (g.D <= 64) g.whole ? step_pass<T, 64, true>(g, s) : step_pass<T, 64, false>(g, s);
+    else g.whole ? step_pass<T, 128, true>(g, s) : step_pass<T, 128, false>(g, s);
 }
 void launch_attn_step(const morlax_cache_dims& d, const void* q, const void* k, const void* v, const float* bias, const int32_t* edges,
                       const int32_t* table, const int32_t* length, void* k_cache, void* v_cache, void* y, void* ws, hipStream_t s) {

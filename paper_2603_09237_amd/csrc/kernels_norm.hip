@@ -6,6 +6,7 @@
 // Bound: HBM.  Every tensor goes through registers once: a row lies along the lanes of a wave, 16 bytes each (or of up to sixteen waves), the
 // backward computes n, y and both means again, and a workgroup keeps the three columns' sums of its rows in registers until its last row.
 #include "mlp_device.h"
+#include "pieces.h"
 
 static int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -64,40 +65,37 @@ __device__ inline float2 sigmoid_of(float v) {
     return v >= 0.f ? make_float2(r, e * r) : make_float2(e * r, v == v ? r : v);
 }
 
-// 16 bytes of a row as they are in memory; elements from n on are zero
 template <typename T>
-struct Piece {
-    typename Run16<T>::vec_t u;
-    __device__ inline void load(const T* p, int n) {
-        constexpr int V = Run16<T>::V;
-        if (n >= V) {
-            u = *reinterpret_cast<const typename Run16<T>::vec_t*>(p);
-        } else {
+__device__ inline void values(const uint4& u, float (&v)[16 / sizeof(T)]) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-            for (int i = 0; i < V; ++i) u[i] = i < n ? p[i] : (T)0.f;
-        }
+    for (int i = 0; i < 16 / (int)sizeof(T); ++i) {
+        if constexpr (sizeof(T) == 4) v[i] = __uint_as_float(w[i]);
+        else v[i] = __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
     }
-    __device__ inline void get(float (&v)[16 / sizeof(T)]) const {
-#pragma unroll
-        for (int i = 0; i < Run16<T>::V; ++i) v[i] = (float)u[i];
-    }
-};
+}
 // A row of up to W * 64 * V * CH elements, W waves of 64 lanes: what is requested of it ...
-template <typename T, int W, int CH, bool BACK>
+template <typename T, int W, int CH, bool WHOLE, bool BACK>
 struct NormInput {
-    Piece<T> x[CH], u[CH], s[CH], dy[BACK ? CH : 1], dh[BACK ? CH : 1];
-    __device__ static inline int col(int c) { return (c * W * 64 + (W == 1 ? threadIdx.x & 63 : threadIdx.x)) * Run16<T>::V; }
+    typedef RowPiece<T, WHOLE> piece;
+    piece x[CH], u[CH], s[CH], dy[BACK ? CH : 1], dh[BACK ? CH : 1];
+    __device__ static inline int col(int c) { return (c * W * 64 + (W == 1 ? threadIdx.x & 63 : threadIdx.x)) * piece::VE; }
+    // tensors that are not there stand for x (what comes of them is not used, or taken for zero)
     __device__ inline void load(const NormArgs& g, int64_t row) {
         row = row < g.rows ? row : g.rows - 1;
+        const T* px = reinterpret_cast<const T*>(g.x) + row * g.ld_x;
+        const T* pu = g.u ? reinterpret_cast<const T*>(g.u) + row * g.ld_u : px;
+        const T* ps = g.gate ? reinterpret_cast<const T*>(g.gate) + row * g.ld_g : px;
+        const T* py = g.dy ? reinterpret_cast<const T*>(g.dy) + row * g.ld_x : px;
+        const T* ph = g.dh ? reinterpret_cast<const T*>(g.dh) + row * g.ld_h : px;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int at = col(c), left = g.width - at;
-            x[c].load(reinterpret_cast<const T*>(g.x) + row * g.ld_x + at, left);
-            u[c].load(reinterpret_cast<const T*>(g.u) + row * g.ld_u + at, g.u ? left : 0);
-            s[c].load(reinterpret_cast<const T*>(g.gate) + row * g.ld_g + at, g.gate ? left : 0);
+            x[c].load(px, col(c), g.width);
+            u[c].load(pu, col(c), g.width);
+            s[c].load(ps, col(c), g.width);
             if (BACK) {
-                dy[c].load(reinterpret_cast<const T*>(g.dy) + row * g.ld_x + at, g.dy ? left : 0);
-                dh[c].load(reinterpret_cast<const T*>(g.dh) + row * g.ld_h + at, g.dh ? left : 0);
+                dy[c].load(py, col(c), g.width);
+                dh[c].load(ph, col(c), g.width);
             }
         }
     }
@@ -108,14 +106,14 @@ struct NormRow {
     static constexpr int V = 16 / sizeof(T);
     float x[CH][V], u[CH][V], s[CH][V], n[CH][V];  // s: the gate; after value(): x is y, n the normed u
     float r_u, r_y;
-    __device__ static inline int col(int c) { return NormInput<T, W, CH, false>::col(c); }
-    template <bool BACK>
-    __device__ inline void take(const NormInput<T, W, CH, BACK>& in) {
+    __device__ static inline int col(int c) { return NormInput<T, W, CH, true, false>::col(c); }
+    template <bool WHOLE, bool BACK>
+    __device__ inline void take(const NormInput<T, W, CH, WHOLE, BACK>& in, int width) {
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            in.x[c].get(x[c]);
-            in.u[c].get(u[c]);
-            in.s[c].get(s[c]);
+            values<T>(in.x[c].get(col(c), width), x[c]);
+            values<T>(in.u[c].get(col(c), width), u[c]);
+            values<T>(in.s[c].get(col(c), width), s[c]);
         }
     }
     __device__ inline void value(const NormArgs& g, const float (&sc)[CH][V], const float (&wo)[CH][V], float* lds) {
@@ -159,7 +157,7 @@ __device__ inline void columns(const NormArgs& g, const float* p, float (&v)[CH]
         }
 }
 
-template <typename T, int W, int CH>
+template <typename T, int W, int CH, bool WHOLE>
 __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void k_norm_fwd(NormArgs g) {
     constexpr int V = 16 / sizeof(T);
     __shared__ float lds[W];
@@ -168,11 +166,11 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void k_norm_fwd(NormArgs g) 
     columns<T, W, CH>(g, g.w_post, wo);
     columns<T, W, CH>(g, g.w_pre, wi);
     const int64_t per = W == 1 ? 4 : 1, first = blockIdx.x * per + (W == 1 ? threadIdx.x >> 6 : 0);
-    NormInput<T, W, CH, false> in;
+    NormInput<T, W, CH, WHOLE, false> in;
     if (first < g.rows) in.load(g, first);
     for (int64_t row = first; row < g.rows; row += gridDim.x * per) {
         NormRow<T, W, CH> r;
-        r.take(in);
+        r.take(in, g.width);
         in.load(g, row + gridDim.x * per);  // the next one's
         r.value(g, sc, wo, lds);
 #pragma unroll
@@ -189,7 +187,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void k_norm_fwd(NormArgs g) 
     }
 }
 
-template <typename T, int W, int CH>
+template <typename T, int W, int CH, bool WHOLE>
 __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void k_norm_bwd(NormArgs g) {
     constexpr int V = 16 / sizeof(T), CAP = 64 * V * CH;  // columns of a wave
     __shared__ float lds[W];
@@ -203,16 +201,16 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void k_norm_bwd(NormArgs g) 
 #pragma unroll
         for (int i = 0; i < V; ++i) ds[c][i] = dwo[c][i] = dwi[c][i] = 0.f;
     const int64_t per = W == 1 ? 4 : 1, first = blockIdx.x * per + (W == 1 ? threadIdx.x >> 6 : 0);
-    NormInput<T, W, CH, true> in;
+    NormInput<T, W, CH, WHOLE, true> in;
     if (first < g.rows) in.load(g, first);
     for (int64_t row = first; row < g.rows; row += gridDim.x * per) {
         NormRow<T, W, CH> r;
         float dy[CH][V], dh[CH][V];
-        r.take(in);
+        r.take(in, g.width);
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            in.dy[c].get(dy[c]);
-            in.dh[c].get(dh[c]);
+            values<T>(in.dy[c].get(r.col(c), g.width, g.dy != nullptr), dy[c]);
+            values<T>(in.dh[c].get(r.col(c), g.width, g.dh != nullptr), dh[c]);
         }
         in.load(g, row + gridDim.x * per);  // the next one's
         r.value(g, sc, wo, lds);
@@ -342,15 +340,19 @@ static int norm_blocks(const morlax_norm_dims& d) {
 }
 int64_t norm_ws_bytes(const morlax_norm_dims& d) { return (int64_t)norm_blocks(d) * 3 * d.width * 4; }
 
-template <typename T, int W, int CH>
-static void norm_pass(const NormArgs& g, bool back, hipStream_t s) {
+template <typename T, int W, int CH, bool WHOLE>
+static void norm_run(const NormArgs& g, bool back, hipStream_t s) {
     constexpr int THREADS = W == 1 ? 256 : W * 64;
     if (back) {
-        k_norm_bwd<T, W, CH><<<dim3(g.blocks), THREADS, 0, s>>>(g);
+        k_norm_bwd<T, W, CH, WHOLE><<<dim3(g.blocks), THREADS, 0, s>>>(g);
     } else {
         const int64_t all = cdiv(g.rows, W == 1 ? 4 : 1), most = W == 1 ? 4096 : 16384 / W;
-        k_norm_fwd<T, W, CH><<<dim3((uint32_t)(all < most ? all : most)), THREADS, 0, s>>>(g);
+        k_norm_fwd<T, W, CH, WHOLE><<<dim3((uint32_t)(all < most ? all : most)), THREADS, 0, s>>>(g);
     }
+}
+template <typename T, int W, int CH>
+static void norm_pass(const NormArgs& g, bool back, hipStream_t s) {
+    g.width % (16 / (int)sizeof(T)) == 0 ? norm_run<T, W, CH, true>(g, back, s) : norm_run<T, W, CH, false>(g, back, s);
 }
 template <typename T>
 static void norm_pick(const NormArgs& g, int waves, bool back, hipStream_t s) {

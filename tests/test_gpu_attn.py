@@ -163,6 +163,10 @@ SHAPES = [  # T, S, N, H, KV, D, B, window, p_first
     (200, 200, 1, 4, 4, 72, 32, 130, 0.0),  # tiles that all rows see, beyond the last edge
     (300, 300, 1, 4, 1, 64, 6, 300, 0.0),   # four heads to a head of keys, beyond the last edge
     (40, 41, 70, 2, 1, 24, 9, 41, 0.1),
+    (2, 128, 3, 2, 2, 128, 32, 128, 0.0),   # few rows that end with a tile of keys
+    (70, 192, 2, 3, 3, 16, 16, 192, 0.0),   # a last block of few rows, the same
+    (256, 400, 1, 2, 2, 64, 4, 300, 0.0),   # tiles at the window's begin, then ones beyond the last edge
+    (9, 9, 2, 2, 1, 8, 3, 1, 0.0),          # rows that see themselves only
 ]
 
 
@@ -186,6 +190,15 @@ def test_strides(kind, pad, order):
         a, b = run(c), run(c, pad, order)
         for k in a:
             assert torch.equal(a[k], b[k]), k
+
+
+def test_rows_that_see_themselves_only():
+    """Their probability is one whatever the scores are: their scores' gradients are zeros, not what two sums' roundings leave."""
+    torch = _torch()
+    for kind in (torch.float32, torch.bfloat16):
+        got = run(make(kind, 70, 75, 3, 4, 2, 40, 6, 1, 0.0))
+        for k in ("q", "k", "bias"):
+            assert not bool(got[k].any()), k
 
 
 def test_definition_against_differences():
