@@ -35,7 +35,7 @@ struct AttnArgs {
     float* table;     // [H, reach] bias by distance, in units of log2; NULL: no bias
     int32_t* bucket;  // [reach]
     float* lse;       // [N, H, T] L, in units of log2; NULL: not wanted
-    bf16_t* low;      // [T, N, H, D] what y's rounding took away (bf16)
+    uint16_t* low;    // [T, N, H, D] what y's rounding to bf16 took away: the fp32 value's bits less the rounded one's
     float* delta;     // [N, H, T]
     float* part;      // [H, B, parts] sums of dA of each workgroup
     float* dbias;
@@ -105,7 +105,7 @@ struct Tile {
     static constexpr int ES = sizeof(T), VE = 16 / ES, PITCH = DP * ES + 16, CPR = DP / VE, KS = DP * ES / 64, NB = DP / 16;
     static constexpr int TU = ES == 2 ? 32 : 16, NU = ATTN_K / TU;  // rows of one transposed operand, operands of a tile
     static constexpr int NX = TU / 16;                              // blocks of 16 of one
-    static constexpr int NP = ES == 2 ? 2 : 1;                      // parts of a computed operand
+    static constexpr int NP = ES == 2 ? 3 : 1;                      // parts of a computed operand (see Computed)
     static constexpr int BYTES = ATTN_K * PITCH;
     // the lane's operand of rows row .. row + 15, contraction indices of piece ks along the row
     static __device__ inline uint4 rows(const unsigned char* lds, int row, int ks, int lane) {
@@ -236,37 +236,42 @@ struct Stage {
     }
 };
 
-// A lane's computed operand of four values a block: bf16 in two parts (16 bits: what is added up then is the fp32 result up to 2^-17, and the
-// one rounding that counts is the output's.  One part: y off by 2.0e-3 of its size instead of 1.6e-3, dbias by 1e-3 instead of 1e-6).
+// A lane's computed operand of four values a block: bf16 in two parts (off by 2^-18 of the value at most), so that the one rounding that counts is the
+// output's (one part: y off by 2.0e-3 of its size instead of 1.6e-3; the second costs nothing that can be measured).  The forward of a training
+// pass takes a third: delta comes of y, and what it is off by adds up in the bias's gradient, which is an fp32 sum.
 template <typename T, int DP>
 struct Computed {
     typedef Tile<T, DP> L;
     uint4 part[L::NP];
     __device__ inline void set(const float4_t (&p)[L::NX]) {
         if constexpr (L::ES == 2) {
-            const float4_t a = p[0], b = p[1];
-            const uint4 h = make_uint4(pack2(a[0], a[1]), pack2(a[2], a[3]), pack2(b[0], b[1]), pack2(b[2], b[3]));
-            part[0] = h;
-            const uint32_t w[4] = {h.x, h.y, h.z, h.w};
-            const float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-            uint32_t l[4];
+            float v[8] = {p[0][0], p[0][1], p[0][2], p[0][3], p[1][0], p[1][1], p[1][2], p[1][3]};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) l[i] = pack2(v[2 * i] - __uint_as_float(w[i] << 16), v[2 * i + 1] - __uint_as_float(w[i] & 0xffff0000u));
-            part[1] = make_uint4(l[0], l[1], l[2], l[3]);
+            for (int q = 0; q < L::NP; ++q) {
+                uint32_t w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    w[i] = pack2(v[2 * i], v[2 * i + 1]);
+                    v[2 * i] -= __uint_as_float(w[i] << 16);
+                    v[2 * i + 1] -= __uint_as_float(w[i] & 0xffff0000u);
+                }
+                part[q] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
         } else {
             const float4_t a = p[0];
             part[0] = make_uint4(__float_as_uint(a[0]), __float_as_uint(a[1]), __float_as_uint(a[2]), __float_as_uint(a[3]));
         }
     }
+    template <bool FINE>
     __device__ inline void product(const uint4& turned, float4_t& acc) const {
 #pragma unroll
-        for (int i = 0; i < L::NP; ++i) Mma16<T>::run(turned, part[i], acc);
+        for (int i = 0; i < (FINE || L::NP < 3 ? L::NP : 2); ++i) Mma16<T>::run(turned, part[i], acc);
     }
 };
 
 // acc[b][dt] (rows: columns 16 dt + 4 g + r of the tile; column: lane & 15) += rows^T p[b] over the tile's rows u TU .., for NBLK blocks of 16
 // lanes' columns
-template <typename T, int DP, int NBLK>
+template <typename T, int DP, int NBLK, bool FINE = false>
 __device__ inline void fold(const unsigned char* lds, int u, const float4_t (&p)[NBLK][Tile<T, DP>::NX], float4_t (&acc)[NBLK][DP / 16], int lane) {
     typedef Tile<T, DP> L;
     Computed<T, DP> c[NBLK];
@@ -277,7 +282,7 @@ __device__ inline void fold(const unsigned char* lds, int u, const float4_t (&p)
         if (dt && dt % 4 == 0) phase();
         const uint4 f = L::turned(lds, u, dt, lane);
 #pragma unroll
-        for (int b = 0; b < NBLK; ++b) c[b].product(f, acc[b][dt]);
+        for (int b = 0; b < NBLK; ++b) c[b].template product<FINE>(f, acc[b][dt]);
     }
     phase();
 }
@@ -376,7 +381,7 @@ struct FwdLds {
     static constexpr int ROOM = ATTN_ROOM(64 * QB, ATTN_K), NR = (ROOM + ATTN_THREADS - 1) / ATTN_THREADS;
     static constexpr int K = 0, V = Tile<T, DP>::BYTES, TAB = 2 * V, FLAG = TAB + ROOM * 4, TOTAL = FLAG + 16;
 };
-template <typename T, int DP, int QB, bool WHOLE>
+template <typename T, int DP, int QB, bool WHOLE, bool FINE>
 __global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_fwd(AttnArgs g) {
     typedef Tile<T, DP> L;
     typedef FwdLds<T, DP, QB> M;
@@ -512,7 +517,7 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_fwd(At
                 for (int b = 0; b < QB; ++b)
 #pragma unroll
                     for (int i = 0; i < L::NX; ++i) part[b][i] = s[b][u * L::NX + i];
-                fold<T, DP, QB>(lds + M::V, u, part, o, now);
+                fold<T, DP, QB, FINE>(lds + M::V, u, part, o, now);
             }
         };
         if (__any(any)) {
@@ -546,17 +551,28 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_fwd(At
         const float inv = 1.f / l[b];
         if (g.lse && gr == 0) g.lse[((int64_t)R.n * g.H + h) * g.T + t[b]] = m[b] + __builtin_amdgcn_logf(l[b]);
         T* dst = reinterpret_cast<T*>(g.out) + (int64_t)t[b] * g.y_t + (int64_t)R.n * g.y_n + (int64_t)h * g.D;
-        bf16_t* low = g.low ? g.low + (((int64_t)t[b] * g.N + R.n) * g.H + h) * g.D : nullptr;
+        uint16_t* low = g.low ? g.low + (((int64_t)t[b] * g.N + R.n) * g.H + h) * g.D : nullptr;
 #pragma unroll
         for (int dt = 0; dt < L::NB; ++dt) {
             float4_t y = o[b][dt];
+            uint32_t rest[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) y[r] *= inv;
             store4(dst, 16 * dt + 4 * gr, g.D, y);
             if (L::ES == 2 && low) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) y[r] -= (float)(bf16_t)y[r];
-                store4(low, 16 * dt + 4 * gr, g.D, y);
+                for (int r = 0; r < 4; ++r) {
+                    const int d = __float_as_int(y[r]) - __float_as_int((float)(bf16_t)y[r]);
+                    rest[r] = (uint32_t)(d < 0x7fff ? d : 0x7fff) & 0xffff;  // (a tie that went down is one more)
+                }
+                const int d = 16 * dt + 4 * gr;
+                if (d + 4 <= g.D) {
+                    *reinterpret_cast<half_piece_t*>(low + d) = half_piece_t{rest[0] | rest[1] << 16, rest[2] | rest[3] << 16};
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (d + r < g.D) low[d + r] = (uint16_t)rest[r];
+                }
             }
         }
     }
@@ -633,7 +649,7 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_dq(Att
         const T* src = reinterpret_cast<const T*>(g.q) + at * g.q_t + (int64_t)R.n * g.q_n + h * g.D;
         const T* dsrc = reinterpret_cast<const T*>(g.dy) + at * g.y_t + (int64_t)R.n * g.y_n + h * g.D;
         const T* ysrc = reinterpret_cast<const T*>(g.y) + at * g.y_t + (int64_t)R.n * g.y_n + h * g.D;
-        const bf16_t* lsrc = g.low ? g.low + ((at * g.N + R.n) * g.H + h) * g.D : nullptr;
+        const uint16_t* lsrc = g.low ? g.low + ((at * g.N + R.n) * g.H + h) * g.D : nullptr;
         float sum = 0.f;
 #pragma unroll
         for (int ks = 0; ks < L::KS; ++ks) {
@@ -642,7 +658,7 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_dq(Att
             uq.load(src, d, g.D);
             uo.load(dsrc, d, g.D);
             uy.load(ysrc, d, g.D);
-            RowPiece<bf16_t, WHOLE> ul;
+            RowPiece<uint16_t, WHOLE> ul;
             if constexpr (L::ES == 2) ul.load(lsrc, d, g.D);
             qf[b][ks] = uq.get(d, g.D, in);
             of[b][ks] = uo.get(d, g.D, in);
@@ -653,9 +669,8 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_dq(Att
                 const uint32_t wl[4] = {lf.x, lf.y, lf.z, lf.w};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    sum = __builtin_fmaf(__uint_as_float(wd[i] << 16), __uint_as_float(wy[i] << 16) + __uint_as_float(wl[i] << 16), sum);
-                    sum = __builtin_fmaf(__uint_as_float(wd[i] & 0xffff0000u),
-                                         __uint_as_float(wy[i] & 0xffff0000u) + __uint_as_float(wl[i] & 0xffff0000u), sum);
+                    sum = __builtin_fmaf(__uint_as_float(wd[i] << 16), __int_as_float((int)(wy[i] << 16) + ((int)(wl[i] << 16) >> 16)), sum);
+                    sum = __builtin_fmaf(__uint_as_float(wd[i] & 0xffff0000u), __int_as_float((int)(wy[i] & 0xffff0000u) + ((int)wl[i] >> 16)), sum);
                 }
             } else {
 #pragma unroll
@@ -1126,10 +1141,13 @@ static int run_kernel(void (*kernel)(AttnArgs), AttnArgs& g, int64_t total, int 
     kernel<<<dim3((uint32_t)total), ATTN_THREADS, lds, s>>>(g);
     return 0;
 }
-template <typename T, int DP, int QB, bool WHOLE>
+template <typename T, int DP, int QB, bool WHOLE, bool FINE = false>
 static int attn_fwd_pass(AttnArgs& g, hipStream_t s) {
+    if constexpr (!FINE && sizeof(T) == 2) {
+        if (g.low) return attn_fwd_pass<T, DP, QB, WHOLE, true>(g, s);
+    }
     g.tiles = (int)cdiv((int64_t)g.T << g.lgp, 64 * QB);
-    return run_kernel(k_attn_fwd<T, DP, QB, WHOLE>, g, (int64_t)g.tiles * g.N * (g.H >> g.lgp), FwdLds<T, DP, QB>::TOTAL, s);
+    return run_kernel(k_attn_fwd<T, DP, QB, WHOLE, FINE>, g, (int64_t)g.tiles * g.N * (g.H >> g.lgp), FwdLds<T, DP, QB>::TOTAL, s);
 }
 template <typename T, int DP, int QB, bool WHOLE>
 static int attn_dq_pass(AttnArgs& g, hipStream_t s) {

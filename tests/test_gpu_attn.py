@@ -294,7 +294,10 @@ def test_same_again_without_saving_and_on_another_stream(kind):
         other = run(c)
     for k in a:
         assert torch.equal(a[k], b[k]) and torch.equal(a[k], other[k]), k
-    assert torch.equal(a["y"], alone["y"])
+    # (a pass that saves holds its probabilities in more bits: the same up to where a value lies between two bf16 ones)
+    if kind == "float32":
+        assert torch.equal(a["y"], alone["y"])
+    assert bool(((a["y"].float() - alone["y"].float()).abs() <= 2.0 ** -7 * a["y"].float().abs()).all())
 
 
 def test_without_the_bias_gradient():
