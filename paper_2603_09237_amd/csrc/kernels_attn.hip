@@ -13,16 +13,12 @@
 // below).
 // Query heads that share a head of keys are rows of the same tile (`pack` of them), so the keys are read once for all of them and the sums over
 // heads in dk and dv are sums over rows.
-#include "mlp_device.h"
-#include "pieces.h"
+#include "attn_tile.h"
 
 static int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-typedef short short4_t __attribute__((ext_vector_type(4)));
-#define ATTN_K 64      // rows of a tile that is walked through (keys; in the pass over the keys, queries)
 #define ATTN_THREADS 256
 #define ATTN_ROOM(rows, keys) ((rows) + 4 * (keys))  // table entries of a tile: pack <= 4 heads, each its distances
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kNever = 1 << 30;  // begin of the seen interval of a row that is not there
 
 struct AttnArgs {
@@ -45,16 +41,6 @@ struct AttnArgs {
     uint32_t total;
     int whole;  // rows hold whole pieces of 16 bytes
 };
-
-// No instruction moves across (left to itself the scheduler starts the reads of a whole tile at once, and two hundred registers hold them).
-__device__ inline void phase() { __builtin_amdgcn_sched_barrier(0); }
-// The lane, as a value that the compiler cannot know to be the same for the next tile: or it computes the addresses of all of a tile's
-// accesses once, ahead of the loop, and keeps them in registers.
-__device__ inline int lane_now() {
-    int lane = threadIdx.x & 63;
-    asm volatile("" : "+v"(lane));
-    return lane;
-}
 
 // ---- episodes and the bias by distance --------------------------------------------------------------------------------
 // Blocks below `spans`: 2^lgn environments at a time, the threads of an environment taking a run of steps each; the others: the table.
@@ -98,40 +84,6 @@ __global__ __launch_bounds__(1024) void k_attn_prepare(AttnArgs g, int spans, in
 }
 
 // ---- tiles ------------------------------------------------------------------------------------------------------------
-// A tile of ATTN_K rows of up to DP elements in LDS, rows 16 bytes apart beyond their length: reads of whole pieces along a row and transposed
-// reads (16 x 16 elements bf16, single ones fp32) both touch every bank equally often.
-template <typename T, int DP>
-struct Tile {
-    static constexpr int ES = sizeof(T), VE = 16 / ES, PITCH = DP * ES + 16, CPR = DP / VE, KS = DP * ES / 64, NB = DP / 16;
-    static constexpr int TU = ES == 2 ? 32 : 16, NU = ATTN_K / TU;  // rows of one transposed operand, operands of a tile
-    static constexpr int NX = TU / 16;                              // blocks of 16 of one
-    static constexpr int NP = ES == 2 ? 3 : 1;                      // parts of a computed operand (see Computed)
-    static constexpr int BYTES = ATTN_K * PITCH;
-    // the lane's operand of rows row .. row + 15, contraction indices of piece ks along the row
-    static __device__ inline uint4 rows(const unsigned char* lds, int row, int ks, int lane) {
-        return *reinterpret_cast<const uint4*>(lds + (row + (lane & 15)) * PITCH + ks * 64 + (lane >> 4) * 16);
-    }
-    // columns 16 dt .. + 15 as the rows of an operand, contraction over the rows u TU .. : in the order in which a lane holds the products'
-    // results (bf16: 4 g + r of two blocks of 16; fp32: of one)
-    static __device__ inline uint4 turned(const unsigned char* lds, int u, int dt, int lane) {
-        const int a = lane & 15, gr = lane >> 4;
-        if constexpr (ES == 2) {
-            typedef __attribute__((address_space(3))) short4_t lds_s4;
-            const unsigned char* s = lds + (32 * u + 4 * gr + (a >> 2)) * PITCH + (16 * dt + 4 * (a & 3)) * 2;
-            const uint2 u0 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)s));
-            const uint2 u1 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(s + 16 * PITCH)));
-            return make_uint4(u0.x, u0.y, u1.x, u1.y);
-        } else {
-            const unsigned char* s = lds + (16 * u + 4 * gr) * PITCH + (16 * dt + a) * 4;
-            return make_uint4(*reinterpret_cast<const uint32_t*>(s), *reinterpret_cast<const uint32_t*>(s + PITCH),
-                              *reinterpret_cast<const uint32_t*>(s + 2 * PITCH), *reinterpret_cast<const uint32_t*>(s + 3 * PITCH));
-        }
-    }
-    static __device__ inline float at(const unsigned char* lds, int row, int d) {
-        return to_f(*reinterpret_cast<const T*>(lds + row * PITCH + d * ES));
-    }
-};
-
 // A computed zero times an infinite or undefined element would reach rows that do not see it.  So such elements are put down as zeros in
 // the tiles that computed operands are multiplied with, and a workgroup that met one adds them in the end, one by one, to what sees them
 // (as they are: the products of the definition are infinite or undefined too).
@@ -236,39 +188,6 @@ struct Stage {
     }
 };
 
-// A lane's computed operand of four values a block: bf16 in two parts (off by 2^-18 of the value at most), so that the one rounding that counts is the
-// output's (one part: y off by 2.0e-3 of its size instead of 1.6e-3; the second costs nothing that can be measured).  The forward of a training
-// pass takes a third: delta comes of y, and what it is off by adds up in the bias's gradient, which is an fp32 sum.
-template <typename T, int DP>
-struct Computed {
-    typedef Tile<T, DP> L;
-    uint4 part[L::NP];
-    __device__ inline void set(const float4_t (&p)[L::NX]) {
-        if constexpr (L::ES == 2) {
-            float v[8] = {p[0][0], p[0][1], p[0][2], p[0][3], p[1][0], p[1][1], p[1][2], p[1][3]};
-#pragma unroll
-            for (int q = 0; q < L::NP; ++q) {
-                uint32_t w[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    w[i] = pack2(v[2 * i], v[2 * i + 1]);
-                    v[2 * i] -= __uint_as_float(w[i] << 16);
-                    v[2 * i + 1] -= __uint_as_float(w[i] & 0xffff0000u);
-                }
-                part[q] = make_uint4(w[0], w[1], w[2], w[3]);
-            }
-        } else {
-            const float4_t a = p[0];
-            part[0] = make_uint4(__float_as_uint(a[0]), __float_as_uint(a[1]), __float_as_uint(a[2]), __float_as_uint(a[3]));
-        }
-    }
-    template <bool FINE>
-    __device__ inline void product(const uint4& turned, float4_t& acc) const {
-#pragma unroll
-        for (int i = 0; i < (FINE || L::NP < 3 ? L::NP : 2); ++i) Mma16<T>::run(turned, part[i], acc);
-    }
-};
-
 // acc[b][dt] (rows: columns 16 dt + 4 g + r of the tile; column: lane & 15) += rows^T p[b] over the tile's rows u TU .., for NBLK blocks of 16
 // lanes' columns
 template <typename T, int DP, int NBLK, bool FINE = false>
@@ -287,19 +206,45 @@ __device__ inline void fold(const unsigned char* lds, int u, const float4_t (&p)
     phase();
 }
 
-// Four consecutive elements of a row of D from column d on
-typedef uint32_t half_piece_t __attribute__((ext_vector_type(2), aligned(2)));
-typedef float run4_t __attribute__((ext_vector_type(4), aligned(4)));
-template <typename T>
-__device__ inline void store4(T* p, int d, int D, const float4_t& v) {
-    if (d + 4 <= D) {
-        if constexpr (sizeof(T) == 2) *reinterpret_cast<half_piece_t*>(p + d) = half_piece_t{pack2(v[0], v[1]), pack2(v[2], v[3])};
-        else *reinterpret_cast<run4_t*>(p + d) = run4_t{v[0], v[1], v[2], v[3]};
-        return;
-    }
+template <typename T, int DP, bool WHOLE, typename F>
+__device__ inline void send_rows(const unsigned char* lds, int D, F to) {
+    typedef Tile<T, DP> L;
+    const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (d + i < D) p[d + i] = cvt<T>(v[i]);
+    for (int i = 0; i < 16 * L::CPR / 64; ++i) {
+        const int p = i * 64 + lane, row = p / L::CPR, col = p % L::CPR * L::VE;
+        T* dst = reinterpret_cast<T*>(to(row));
+        const uint4 u = *reinterpret_cast<const uint4*>(lds + row * L::PITCH + col * L::ES);
+        if (!dst) continue;
+        if (WHOLE ? col < D : col + L::VE <= D) {
+            *reinterpret_cast<piece_t*>(dst + col) = piece_t{u.x, u.y, u.z, u.w};
+        } else if (!WHOLE) {
+            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int e = 0; e < L::VE; ++e) {
+                if (col + e >= D) continue;
+                if constexpr (L::ES == 2) reinterpret_cast<uint16_t*>(dst)[col + e] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
+                else reinterpret_cast<uint32_t*>(dst)[col + e] = w[e];
+            }
+        }
+    }
+}
+// A wave's block of 16 rows goes out by whole rows: laid down in LDS as its lanes hold it (row: the lane's; columns 16 dt + 4 g + r), read back in
+// pieces along the rows (8 bytes a lane straight from the registers touch 32 bytes of each line four times over).
+// lds: 16 rows of the wave's own; to(row): where a row of D elements begins, or NULL
+template <typename T, int DP, bool WHOLE, typename F>
+__device__ inline void put_rows(unsigned char* lds, const float4_t (&v)[DP / 16], float scale, int D, F to) {
+    typedef Tile<T, DP> L;
+    const int lane = threadIdx.x & 63, a = lane & 15, gr = lane >> 4;
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int dt = 0; dt < L::NB; ++dt) {
+        unsigned char* at = lds + a * L::PITCH + (16 * dt + 4 * gr) * L::ES;
+        if constexpr (L::ES == 2) *reinterpret_cast<uint2*>(at) = make_uint2(pack2(v[dt][0] * scale, v[dt][1] * scale), pack2(v[dt][2] * scale, v[dt][3] * scale));
+        else *reinterpret_cast<float4_t*>(at) = float4_t{v[dt][0] * scale, v[dt][1] * scale, v[dt][2] * scale, v[dt][3] * scale};
+    }
+    __builtin_amdgcn_wave_barrier();
+    send_rows<T, DP, WHOLE>(lds, D, to);
 }
 
 // Which tile of which environment and heads (`rest`) a workgroup takes.  Workgroups go round the eight XCDs, and what belongs to one `rest` goes to the
@@ -546,34 +491,35 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_fwd(At
     for (int b = 0; b < QB; ++b) {
         l[b] += __shfl_xor(l[b], 16);
         l[b] += __shfl_xor(l[b], 32);
-        if (t[b] < 0) continue;
-        const int h = R.h0 + (a & ((1 << g.lgp) - 1));
         const float inv = 1.f / l[b];
-        if (g.lse && gr == 0) g.lse[((int64_t)R.n * g.H + h) * g.T + t[b]] = m[b] + __builtin_amdgcn_logf(l[b]);
-        T* dst = reinterpret_cast<T*>(g.out) + (int64_t)t[b] * g.y_t + (int64_t)R.n * g.y_n + (int64_t)h * g.D;
-        uint16_t* low = g.low ? g.low + (((int64_t)t[b] * g.N + R.n) * g.H + h) * g.D : nullptr;
+        if (g.lse && gr == 0 && t[b] >= 0)
+            g.lse[((int64_t)R.n * g.H + R.h0 + (a & ((1 << g.lgp) - 1))) * g.T + t[b]] = m[b] + __builtin_amdgcn_logf(l[b]);
+        unsigned char* mine = lds + wave * 16 * L::PITCH;
+        const int first = R.r0 + (wave * QB + b) * 16;
+        put_rows<T, DP, WHOLE>(mine, o[b], inv, g.D, [&](int row) -> T* {
+            const int r = first + row;
+            if (r >= R.rows) return nullptr;
+            return reinterpret_cast<T*>(g.out) + (int64_t)(r >> g.lgp) * g.y_t + (int64_t)R.n * g.y_n + (int64_t)(R.h0 + (r & ((1 << g.lgp) - 1))) * g.D;
+        });
+        if constexpr (FINE) {  // what the rounding took: the fp32 value's bits less the rounded one's (a tie that went down is one more)
+            __builtin_amdgcn_wave_barrier();
 #pragma unroll
-        for (int dt = 0; dt < L::NB; ++dt) {
-            float4_t y = o[b][dt];
-            uint32_t rest[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) y[r] *= inv;
-            store4(dst, 16 * dt + 4 * gr, g.D, y);
-            if (L::ES == 2 && low) {
+            for (int dt = 0; dt < L::NB; ++dt) {
+                uint32_t rest[4];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int d = __float_as_int(y[r]) - __float_as_int((float)(bf16_t)y[r]);
-                    rest[r] = (uint32_t)(d < 0x7fff ? d : 0x7fff) & 0xffff;  // (a tie that went down is one more)
+                    const float y = o[b][dt][r] * inv;
+                    const int d = __float_as_int(y) - __float_as_int((float)(bf16_t)y);
+                    rest[r] = (uint32_t)(d < 0x7fff ? d : 0x7fff) & 0xffff;
                 }
-                const int d = 16 * dt + 4 * gr;
-                if (d + 4 <= g.D) {
-                    *reinterpret_cast<half_piece_t*>(low + d) = half_piece_t{rest[0] | rest[1] << 16, rest[2] | rest[3] << 16};
-                } else {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (d + r < g.D) low[d + r] = (uint16_t)rest[r];
-                }
+                *reinterpret_cast<uint2*>(mine + a * L::PITCH + (16 * dt + 4 * gr) * 2) = make_uint2(rest[0] | rest[1] << 16, rest[2] | rest[3] << 16);
             }
+            __builtin_amdgcn_wave_barrier();
+            send_rows<T, DP, WHOLE>(mine, g.D, [&](int row) -> T* {
+                const int r = first + row;
+                if (r >= R.rows) return nullptr;
+                return reinterpret_cast<T*>(g.low) + (((int64_t)(r >> g.lgp) * g.N + R.n) * g.H + R.h0 + (r & ((1 << g.lgp) - 1))) * g.D;
+            });
         }
     }
 }
@@ -832,15 +778,12 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_dq(Att
     }
 #pragma unroll
     for (int b = 0; b < QB; ++b) {
-        if (t[b] < 0) continue;
-        T* dst = reinterpret_cast<T*>(g.dq) + (int64_t)t[b] * g.q_t + (int64_t)R.n * g.q_n + (int64_t)(R.h0 + hh) * g.D;
-#pragma unroll
-        for (int dt = 0; dt < L::NB; ++dt) {
-            float4_t y = o[b][dt];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) y[r] *= g.scale;
-            store4(dst, 16 * dt + 4 * gr, g.D, y);
-        }
+        const int first = R.r0 + (wave * QB + b) * 16;
+        put_rows<T, DP, WHOLE>(lds + wave * 16 * L::PITCH, o[b], g.scale, g.D, [&](int row) -> T* {
+            const int r = first + row;
+            if (r >= R.rows) return nullptr;
+            return reinterpret_cast<T*>(g.dq) + (int64_t)(r >> g.lgp) * g.q_t + (int64_t)R.n * g.q_n + (int64_t)(R.h0 + (r & ((1 << g.lgp) - 1))) * g.D;
+        });
     }
     if (!g.part) return;
     bins[(g.B - 1) * 64] += outer;
@@ -893,8 +836,11 @@ struct DkvLds {
     static constexpr int ROOM = ATTN_ROOM(ATTN_K, 64 * KB), NR = (ROOM + ATTN_THREADS - 1) / ATTN_THREADS;
     static constexpr int Q = 0, O = Tile<T, DP>::BYTES, TAB = 2 * O, INFO = TAB + ROOM * 4, FLAG = INFO + 3 * ATTN_K * 4, TOTAL = FLAG + 16;
 };
+#ifndef DKVW
+#define DKVW 2
+#endif
 template <typename T, int DP, int KB, bool WHOLE>
-__global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn_dkv(AttnArgs g) {
+__global__ __launch_bounds__(ATTN_THREADS, DP == 64 ? DKVW : 2) void k_attn_dkv(AttnArgs g) {
     typedef Tile<T, DP> L;
     typedef DkvLds<T, DP, KB> M;
     extern __shared__ __align__(16) unsigned char lds[];
@@ -1028,7 +974,7 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn_dkv(AttnArgs g) {
                                     const int p = p0 + (row >> g.lgp) + step;
                                     const bool see = (lo[r] <= key[b]) & (key[b] <= p);
                                     v = see ? v : 0.f;
-                                    da = see & (lo[r] != p) ? da : 0.f;  // (a row that sees itself only: nothing, see above)
+                                    da = (see & (lo[r] != p)) ? da : 0.f;  // (a row that sees itself only: nothing, see above)
                                 }
                                 e[b][i][r] = v;
                                 s[b][i][r] = da;
@@ -1072,16 +1018,12 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn_dkv(AttnArgs g) {
     }
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
-        if (key[b] >= g.S) continue;
-        const int64_t at = (int64_t)key[b] * g.k_t + (int64_t)R.n * g.k_n + (int64_t)R.kv * g.D;
-#pragma unroll
-        for (int dt = 0; dt < L::NB; ++dt) {
-            float4_t y = dk[b][dt];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) y[r] *= g.scale;
-            store4(reinterpret_cast<T*>(g.dk) + at, 16 * dt + 4 * gr, g.D, y);
-            store4(reinterpret_cast<T*>(g.dv) + at, 16 * dt + 4 * gr, g.D, dv[b][dt]);
-        }
+        const int first = k0 + (wave * KB + b) * 16;
+        const auto place = [&](void* base, int row) -> T* {
+            return first + row < g.S ? reinterpret_cast<T*>(base) + (int64_t)(first + row) * g.k_t + (int64_t)R.n * g.k_n + (int64_t)R.kv * g.D : nullptr;
+        };
+        put_rows<T, DP, WHOLE>(lds + wave * 16 * L::PITCH, dk[b], g.scale, g.D, [&](int row) { return place(g.dk, row); });
+        put_rows<T, DP, WHOLE>(lds + wave * 16 * L::PITCH, dv[b], 1.f, g.D, [&](int row) { return place(g.dv, row); });
     }
 }
 

@@ -1,9 +1,7 @@
 // A paged cache of keys and values, one step at a time: the pages' bookkeeping, and the attention of every environment's new step over it.
-#include "mlp_device.h"
-#include "pieces.h"
+#include "attn_tile.h"
 
 static int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
-constexpr float kLog2e = 1.4426950408889634f;
 
 // ---- pages --------------------------------------------------------------------------------------------------------------
 // Integers only: a workgroup owns 64 environments (256 of many), one a thread of its first waves; ranks (whose turn at the queue it is, where a page that goes back lies) are
@@ -417,6 +415,213 @@ __global__ __launch_bounds__(256) void k_attn_step(StepArgs g) {
     }
 }
 
+// ---- one new step over the cache, bf16: on the matrix instructions ------------------------------------------------------------------
+// Up to sixteen query heads that share a head of keys are the columns of a product's result, 32 keys its rows: the arithmetic of a key is then a
+// few instructions of a wave whatever the number of heads (one lane's products and sums for every head: a step of 1024 environments, four heads to a
+// head of keys, 82 us, bound by them).  A lane's two rows of keys and values come straight from the cache; values go through LDS, which turns them.
+template <int DP>
+struct StepLds {
+    typedef Tile<bf16_t, DP> L;
+    static constexpr int V = 32 * L::PITCH, OUT = 16 * (DP + 1) * 4, WAVE = V > OUT ? V : OUT;  // (a wave's output lies where its values lay)
+};
+template <int DP, bool WHOLE>
+__global__ __launch_bounds__(256, DP == 128 ? 2 : 3) void k_attn_step_bf16(StepArgs g) {
+    typedef bf16_t T;
+    typedef Tile<T, DP> L;
+    __shared__ __align__(16) unsigned char lds[4 * StepLds<DP>::WAVE];
+    __shared__ float bias[16][65];
+    __shared__ int32_t edges[64];  // those that are not there: no distance reaches them
+    __shared__ __align__(16) int32_t buckets[4][32];
+    __shared__ float2 wave_m[4][16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, a = lane & 15, gr = lane >> 4;
+    const int split = blockIdx.x % g.splits, rest = blockIdx.x / g.splits, chunk = rest % g.chunks, rest2 = rest / g.chunks;
+    const int kv = rest2 % g.KV, n = rest2 / g.KV, share = g.H / g.KV, h0 = kv * share + chunk * 16, heads = share - chunk * 16 < 16 ? share - chunk * 16 : 16;
+    const int length = g.length[n], pos = length - 1;
+    T* y = reinterpret_cast<T*>(g.y) + (int64_t)n * g.y_n;
+    if (length <= 0) {
+        if (g.splits == 1)
+            for (int i = threadIdx.x; i < heads * g.D; i += 256) y[(int64_t)h0 * g.D + i] = (T)0.f;
+        return;
+    }
+    const int begin = pos - g.window + 1 > 0 ? pos - g.window + 1 : 0;
+    const int count = pos - begin + 1, per = ((count + g.splits - 1) / g.splits + 127) / 128 * 128;  // a whole number of keys of the four waves
+    const int64_t s0 = begin + (int64_t)split * per;
+    const int s1 = s0 + per < pos + 1 ? (int)(s0 + per) : pos + 1;
+    const int32_t* table = g.table + (int64_t)n * g.slots;
+    const int64_t row = (int64_t)g.KV * g.D;
+    const T *kn = reinterpret_cast<const T*>(g.k) + (int64_t)n * g.k_n + (int64_t)kv * g.D, *vn = reinterpret_cast<const T*>(g.v) + (int64_t)n * g.k_n + (int64_t)kv * g.D;
+    T *kc = reinterpret_cast<T*>(g.k_cache) + (int64_t)kv * g.D, *vc = reinterpret_cast<T*>(g.v_cache) + (int64_t)kv * g.D;
+    const int slot0 = (begin >> g.lgp) % g.slots, page0 = begin >> g.lgp, in_page = (1 << g.lgp) - 1;
+    auto slot_of = [&](int s) {  // (the window's pages lie once round the slots at most)
+        const int j = slot0 + (s >> g.lgp) - page0;
+        return j >= g.slots ? j - g.slots : j;
+    };
+    if (split == 0 && chunk == 0) {  // the step goes into its page; no workgroup reads it there
+        const int id = table[slot_of(pos)];
+        if ((uint32_t)id < (uint32_t)g.pages) {
+            const int64_t at = (((int64_t)id << g.lgp) + (pos & in_page)) * row;
+            for (int i = threadIdx.x; i < g.D; i += 256) {
+                kc[at + i] = kn[i];
+                vc[at + i] = vn[i];
+            }
+        }
+    }
+    uint4 qf[L::KS];
+#pragma unroll
+    for (int ks = 0; ks < L::KS; ++ks) {
+        const int d = 32 * ks + 8 * gr;
+        RowPiece<T, WHOLE> u;
+        u.load(reinterpret_cast<const T*>(g.q) + (int64_t)n * g.q_n + (int64_t)(h0 + (a < heads ? a : 0)) * g.D, d, g.D);
+        qf[ks] = u.get(d, g.D, a < heads);
+    }
+    int last_edge = 0;
+    float beyond = 0.f;
+    if (g.B) {
+        if (threadIdx.x < 64) edges[threadIdx.x] = (int)threadIdx.x < g.B ? g.edges[threadIdx.x] : 0x7fffffff;
+        for (int i = threadIdx.x; i < 16 * g.B; i += 256) {
+            const int h = i / g.B, b = i - h * g.B;
+            bias[h][b] = h < heads ? g.bias[(int64_t)(h0 + h) * g.B + b] * kLog2e : 0.f;
+        }
+        last_edge = g.edges[g.B - 1];
+    }
+    __syncthreads();
+    if (g.B) beyond = bias[a][g.B - 1];
+    const float c = g.scale * kLog2e;
+    unsigned char* mine = lds + wave * StepLds<DP>::WAVE;
+    float m = -__builtin_inff(), l = 0.f;
+    float4_t o[1][L::NB];
+#pragma unroll
+    for (int dt = 0; dt < L::NB; ++dt) o[0][dt] = float4_t{0.f, 0.f, 0.f, 0.f};
+    int id[2];
+    RowPiece<T, WHOLE> kp[2][L::KS], vp[2][L::KS];
+    bool in[2];
+    auto look = [&](int64_t at) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int64_t s = at + 16 * x + a;
+            id[x] = table[slot_of((int)(s < s1 ? s : s1 - 1))];
+        }
+    };
+    auto request = [&](int64_t at) {  // (its pages' numbers are there) and the next one's numbers
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int64_t s = at + 16 * x + a;
+            const bool now = s == pos;
+            in[x] = (s < s1) & (now | ((uint32_t)id[x] < (uint32_t)g.pages));
+            const bool held = in[x] & !now;
+            const int64_t off = (((int64_t)id[x] << g.lgp) + ((int)s & in_page)) * row;
+            const T *pk = held ? kc + off : kn, *pv = held ? vc + off : vn;
+#pragma unroll
+            for (int ks = 0; ks < L::KS; ++ks) {
+                kp[x][ks].load(pk, 32 * ks + 8 * gr, g.D);
+                vp[x][ks].load(pv, 32 * ks + 8 * gr, g.D);
+            }
+        }
+        look(at + 128);
+    };
+    int64_t at = s0 + 32 * wave;
+    if (at < s1) {
+        look(at);
+        request(at);
+    }
+    for (; at < s1; at += 128) {
+        float4_t s[1][2];
+        // which of the 32 keys are there, a bit each (a lane's keys: 4 gr + r of both halves)
+        const uint32_t there0 = (uint32_t)__ballot(in[0]) & 0xffff, there1 = (uint32_t)__ballot(in[1]) & 0xffff;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            s[0][x] = float4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ks = 0; ks < L::KS; ++ks) {
+                const int d = 32 * ks + 8 * gr;
+                Mma16<T>::run(kp[x][ks].get(d, g.D, in[x]), qf[ks], s[0][x]);
+                *reinterpret_cast<uint4*>(mine + (16 * x + a) * L::PITCH + d * 2) = vp[x][ks].get(d, g.D, in[x]);
+            }
+        }
+        if (at + 128 < s1) request(at + 128);
+        const bool near = g.B && pos - (int)(at + 31) < last_edge;
+        if (near && lane < 32) {  // the bucket of a key: the last edge that is not beyond its distance
+            const int dist = pos - (int)(at + lane);
+            int b = 0;
+#pragma unroll
+            for (int x = 32; x; x >>= 1) b += edges[b + x] <= dist ? x : 0;
+            buckets[wave][lane] = b;
+        }
+        __builtin_amdgcn_wave_barrier();
+        float top = m;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const uint32_t bits = (x ? there1 : there0) >> (4 * gr);
+            int4 b4 = make_int4(0, 0, 0, 0);
+            if (near) b4 = *reinterpret_cast<const int4*>(&buckets[wave][16 * x + 4 * gr]);
+            const int b[4] = {b4.x, b4.y, b4.z, b4.w};
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float v = __builtin_fmaf(s[0][x][r], c, near ? bias[a][b[r]] : beyond);
+                s[0][x][r] = (bits >> r) & 1 ? v : -__builtin_inff();
+                top = fmaxf(top, s[0][x][r]);
+            }
+        }
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float base = top == -__builtin_inff() ? 0.f : top;
+        if (__any(top != m)) {
+            const float fade = __builtin_amdgcn_exp2f(m - base);
+            l *= fade;
+#pragma unroll
+            for (int dt = 0; dt < L::NB; ++dt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[0][dt][r] *= fade;
+        }
+        m = top;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                s[0][x][r] = __builtin_amdgcn_exp2f(s[0][x][r] - base);
+                l += s[0][x][r];
+            }
+        Computed<T, DP> p;
+        p.set(s[0]);
+#pragma unroll
+        for (int dt = 0; dt < L::NB; ++dt) p.template product<false>(L::turned(mine, 0, dt, lane), o[0][dt]);
+        __builtin_amdgcn_wave_barrier();
+    }
+    // joined: the waves
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (gr == 0) wave_m[wave][a] = make_float2(m, l);
+    float* out = reinterpret_cast<float*>(mine);
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int dt = 0; dt < L::NB; ++dt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) out[a * (DP + 1) + 16 * dt + 4 * gr + r] = o[0][dt][r];
+    __syncthreads();
+    for (int x = threadIdx.x; x < heads * DP; x += 256) {
+        const int i = x / DP, dd = x % DP;
+        if (dd >= g.D) continue;
+        float top = wave_m[0][i].x;
+#pragma unroll
+        for (int w = 1; w < 4; ++w) top = fmaxf(top, wave_m[w][i].x);
+        const float base = top == -__builtin_inff() ? 0.f : top;
+        float sum = 0.f, acc = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float f = __builtin_amdgcn_exp2f(wave_m[w][i].x - base);
+            sum = __builtin_fmaf(f, wave_m[w][i].y, sum);
+            acc = __builtin_fmaf(f, *reinterpret_cast<const float*>(lds + w * StepLds<DP>::WAVE + (i * (DP + 1) + dd) * 4), acc);
+        }
+        if (g.splits == 1) {
+            y[(int64_t)(h0 + i) * g.D + dd] = cvt<T>(acc / sum);
+        } else {
+            const int64_t p = ((int64_t)n * g.H + h0 + i) * g.splits + split;
+            if (dd == 0) g.part_m[p] = make_float2(top, sum);
+            g.part_o[p * g.D + dd] = acc;
+        }
+    }
+}
+
 // the parts of an environment and head, joined: a workgroup each, every wave a quarter of them
 template <typename T>
 __global__ __launch_bounds__(256) void k_attn_join(StepArgs g) {
@@ -490,7 +695,7 @@ static int64_t step_carve(StepArgs& g, const morlax_cache_dims& d, void* ws) {
     g.slots = d.slots; g.pages = d.pages; g.scale = d.scale; g.whole = d.head_dim % (d.dtype ? 8 : 4) == 0;
     g.q_n = d.q_n; g.k_n = d.k_n; g.y_n = d.y_n;
     const int share = d.heads / d.kv_heads;
-    g.chunks = (int)cdiv(share, heads_of_workgroup(share));
+    g.chunks = (int)cdiv(share, d.dtype ? 16 : heads_of_workgroup(share));
     // few environments: the window in as many parts as fill the chip, of 128 keys at least
     const int64_t blocks = (int64_t)d.N * d.kv_heads * g.chunks;
     int64_t splits = 1024 / blocks, most = cdiv(d.window, 128);
@@ -509,7 +714,8 @@ int64_t attn_step_ws_bytes(const morlax_cache_dims& d) {
 template <typename T, int DP, bool WHOLE>
 static void step_pass(const StepArgs& g, hipStream_t s) {
     const dim3 grid((uint32_t)((int64_t)g.splits * g.chunks * g.KV * g.N));
-    switch (heads_of_workgroup(g.H / g.KV)) {
+    if constexpr (sizeof(T) == 2) k_attn_step_bf16<DP, WHOLE><<<grid, 256, 0, s>>>(g);
+    else switch (heads_of_workgroup(g.H / g.KV)) {
         case 1: k_attn_step<T, DP, 1, WHOLE><<<grid, 256, 0, s>>>(g); break;
         case 2: k_attn_step<T, DP, 2, WHOLE><<<grid, 256, 0, s>>>(g); break;
         case 4: k_attn_step<T, DP, 4, WHOLE><<<grid, 256, 0, s>>>(g); break;

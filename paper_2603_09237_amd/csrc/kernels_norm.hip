@@ -59,12 +59,12 @@ __device__ inline float row_sum(float v, float* lds) {
     for (int w = 0; w < W; ++w) all += lds[w];
     return all;
 }
-// sigmoid, and what it lacks to one (from the exponential of -|v|, so that neither loses its digits or overflows)
-__device__ inline float2 sigmoid_of(float v) {
-    const float e = __expf(-__builtin_fabsf(v)), r = __builtin_amdgcn_rcpf(1.f + e);
-    return v >= 0.f ? make_float2(r, e * r) : make_float2(e * r, v == v ? r : v);
+__device__ inline float sigmoid_of(float v) { return __builtin_amdgcn_rcpf(1.f + __expf(-v)); }
+// and what it lacks to one, all digits of it: neither the infinite exponential of a low gate nor the sigmoid of a high one leaves any
+__device__ inline float2 sigmoid_both(float v) {
+    const float e = __expf(-v), s = __builtin_amdgcn_rcpf(1.f + e);
+    return make_float2(s, v < 0.f ? 1.f - s : e * s);
 }
-
 template <typename T>
 __device__ inline void values(const uint4& u, float (&v)[16 / sizeof(T)]) {
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
@@ -125,14 +125,14 @@ struct NormRow {
                 for (int c = 0; c < CH; ++c)
 #pragma unroll
                     for (int i = 0; i < V; ++i) q = __builtin_fmaf(u[c][i], u[c][i], q);
-                r_u = 1.f / sqrtf(row_sum<W>(q, lds) * g.over + g.eps);
+                r_u = __builtin_amdgcn_rsqf(row_sum<W>(q, lds) * g.over + g.eps);
             }
 #pragma unroll
             for (int c = 0; c < CH; ++c)
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     n[c][i] = u[c][i] * r_u * wo[c][i];
-                    x[c][i] = __builtin_fmaf(g.gate ? sc[c][i] * sigmoid_of(s[c][i]).x : sc[c][i], n[c][i], x[c][i]);
+                    x[c][i] = __builtin_fmaf(g.gate ? sc[c][i] * sigmoid_of(s[c][i]) : sc[c][i], n[c][i], x[c][i]);
                 }
         }
         r_y = 1.f;
@@ -142,7 +142,7 @@ struct NormRow {
             for (int c = 0; c < CH; ++c)
 #pragma unroll
                 for (int i = 0; i < V; ++i) q = __builtin_fmaf(x[c][i], x[c][i], q);
-            r_y = 1.f / sqrtf(row_sum<W>(q, lds) * g.over + g.eps);
+            r_y = __builtin_amdgcn_rsqf(row_sum<W>(q, lds) * g.over + g.eps);
         }
     }
 };
@@ -241,7 +241,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void k_norm_bwd(NormArgs g) 
             float dg[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const float2 sig = g.gate ? sigmoid_of(r.s[c][i]) : make_float2(1.f, 0.f);
+                const float2 sig = g.gate ? sigmoid_both(r.s[c][i]) : make_float2(1.f, 0.f);
                 const float t = dy[c][i] * sig.x, dn = t * sc[c][i];
                 ds[c][i] = __builtin_fmaf(t, r.n[c][i], ds[c][i]);
                 dg[i] = dn * r.n[c][i] * sig.y;
@@ -335,7 +335,7 @@ static int norm_waves(const morlax_norm_dims& d) {
 }
 static int norm_blocks(const morlax_norm_dims& d) {
     const int w = norm_waves(d);
-    const int64_t all = cdiv(d.rows, w == 1 ? 4 : 1), most = w == 1 ? 1024 : 4096 / w;  // (what the last launch adds up stays a few per cent of the rows)
+    const int64_t all = cdiv(d.rows, w == 1 ? 4 : 1), most = w == 1 ? 768 : 4096 / w;  // (what the last launch adds up stays a few per cent of the rows)
     return (int)(all < 1 ? 1 : all < most ? all : most);
 }
 int64_t norm_ws_bytes(const morlax_norm_dims& d) { return (int64_t)norm_blocks(d) * 3 * d.width * 4; }
