@@ -8,6 +8,7 @@ static int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // sums over the workgroups before, which a first launch leaves where there is more than one.  Bound by latency for a few thousand environments
 // (two dependent launches of some microseconds), by the copy of the tables where they go into other buffers.
 #define PAGES_THREADS 256
+#define PAGES_AHEAD 8
 struct PagesArgs {
     const uint8_t* first;
     const int32_t *length_in, *table_in, *queue_in, *state_in;
@@ -18,31 +19,32 @@ struct PagesArgs {
     RowDiv by_slots;
 };
 
-// a wave's sum of the values before a lane's, and of all
-__device__ inline int2 wave_before(int v) {
-    const int lane = threadIdx.x & 63;
-    int s = v;
+// of two values at once, over a workgroup of 256: the sums before a thread's, and of all (x, y; z, w)
+__device__ inline int4 block_before(int u, int v, int2* lds4) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int a = u, b = v;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-        const int u = __shfl_up(s, o);
-        if (lane >= o) s += u;
+        const int c = __shfl_up(a, o), d = __shfl_up(b, o);
+        if (lane >= o) {
+            a += c;
+            b += d;
+        }
     }
-    return make_int2(s - v, __shfl(s, 63));
-}
-// the same over a workgroup of 256
-__device__ inline int2 block_before(int v, int* lds4) {
-    const int2 w = wave_before(v);
-    const int wave = threadIdx.x >> 6;
+    if (lane == 63) lds4[wave] = make_int2(a, b);
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) lds4[wave] = w.y;
-    __syncthreads();
-    int before = w.x, all = 0;
+    int4 r = make_int4(a - u, b - v, 0, 0);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if (i < wave) before += lds4[i];
-        all += lds4[i];
+        const int2 w = lds4[i];
+        if (i < wave) {
+            r.x += w.x;
+            r.y += w.y;
+        }
+        r.z += w.x;
+        r.w += w.y;
     }
-    return make_int2(before, all);
+    return r;
 }
 
 struct PageOf {  // what one environment does
@@ -90,14 +92,14 @@ __device__ inline int wave_gives(const PagesArgs& g, int n, bool begins, F each)
 }
 
 __global__ __launch_bounds__(PAGES_THREADS) void k_pages_count(PagesArgs g) {
-    __shared__ int part[4];
+    __shared__ int2 part[4];
     const int n = (int)threadIdx.x < 1 << g.lge ? ((int)blockIdx.x << g.lge) + (int)threadIdx.x : g.N;
     PageOf e;
     e.look(g, n);
     const int gives = wave_gives(g, n, e.begins, [](int, int) {});
-    const int2 needs = block_before(e.needs, part), back = block_before(gives, part);
+    const int4 own = block_before(e.needs, gives, part);
     if (threadIdx.x == 0) {
-        g.sums[blockIdx.x] = make_int2(needs.y, back.y);
+        g.sums[blockIdx.x] = make_int2(own.z, own.w);
         if (blockIdx.x == 0) {
             g.was[0] = g.state_in[0];
             g.was[1] = g.state_in[1];
@@ -106,44 +108,55 @@ __global__ __launch_bounds__(PAGES_THREADS) void k_pages_count(PagesArgs g) {
 }
 
 __global__ __launch_bounds__(PAGES_THREADS) void k_pages_apply(PagesArgs g) {
-    __shared__ int part[4], wave_back[4];
+    __shared__ int2 part[4], sums[4], totals[4];
+    __shared__ int wave_back[4];
     __shared__ int32_t column[PAGES_THREADS], entry[PAGES_THREADS];
     const int n0 = (int)blockIdx.x << g.lge, wave = threadIdx.x >> 6;
     const int n = (int)threadIdx.x < 1 << g.lge ? n0 + (int)threadIdx.x : g.N;
-    PageOf e;
-    e.look(g, n);
-    int gives = 0;  // (of the wave; each pushes them below, once the place is known)
-    gives = wave_gives(g, n, e.begins, [](int, int) {});
-    const int2 needs = block_before(e.needs, part), back = block_before(gives, part);
-    int needs_before = 0, back_before = 0, needs_all = needs.y, back_all = back.y;
-    int head, count;
+    const int here = g.N - n0 < 1 << g.lge ? g.N - n0 : 1 << g.lge, cells = here * g.slots;
+    // the tables' first entries and the workgroups' sums, requested ahead of what they wait for
+    int32_t ahead[PAGES_AHEAD];
+    if (g.table != g.table_in)
+#pragma unroll
+        for (int i = 0; i < PAGES_AHEAD; ++i) {
+            const int at = threadIdx.x + i * PAGES_THREADS;
+            ahead[i] = g.table_in[(int64_t)n0 * g.slots + (at < cells ? at : 0)];
+        }
+    int a = 0, b = 0, c = 0, d = 0, head, count;
     if (g.blocks > 1) {
-        int a = 0, b = 0, c = 0, d = 0;
         for (int i = threadIdx.x; i < g.blocks; i += PAGES_THREADS) {
             const int2 s = g.sums[i];
-            if (i < (int)blockIdx.x) { a += s.x; b += s.y; }
+            a += i < (int)blockIdx.x ? s.x : 0;
+            b += i < (int)blockIdx.x ? s.y : 0;
             c += s.x;
             d += s.y;
         }
-        needs_before = block_before(a, part).y;
-        back_before = block_before(b, part).y;
-        needs_all = block_before(c, part).y;
-        back_all = block_before(d, part).y;
         head = g.was[0];
         count = g.was[1];
     } else {
         head = g.state_in[0];
         count = g.state_in[1];
-        __syncthreads();  // (the state may be its own output)
+    }
+    PageOf e;
+    e.look(g, n);
+    const int gives = wave_gives(g, n, e.begins, [](int, int) {});  // (each pushes them below, once the place is known)
+    const int4 own = block_before(e.needs, gives, part);  // (its barrier stands between the state's reads and its write: it may be its own output)
+    int needs_before = 0, back_before = 0, needs_all = own.z, back_all = own.w;
+    if (g.blocks > 1) {
+        const int4 u = block_before(a, b, sums), v = block_before(c, d, totals);
+        needs_before = u.z;
+        back_before = u.w;
+        needs_all = v.z;
+        back_all = v.w;
     }
     head = (int)((uint32_t)head % (uint32_t)g.pages);
     count = count < 0 ? 0 : count > g.pages ? g.pages : count;
     auto ring = [&](int64_t i) { return (int)((uint64_t)i % (uint32_t)g.pages); };
-    const int rank = needs_before + needs.x;
+    const int rank = needs_before + own.x;
     if (e.needs && rank < count) e.entry = g.queue_in[ring((int64_t)head + rank)];
     column[threadIdx.x] = !e.live ? -1 : e.begins ? -2 - e.column : e.column;  // (an episode that begins is at slot 0)
     entry[threadIdx.x] = e.entry;
-    if ((threadIdx.x & 63) == 0) wave_back[wave] = back.x;
+    if ((threadIdx.x & 63) == 0) wave_back[wave] = own.y;
     if (n < g.N) {
         const bool has = (uint32_t)e.entry < (uint32_t)g.pages;
         g.length[n] = e.live ? e.at + 1 : e.at;
@@ -154,16 +167,20 @@ __global__ __launch_bounds__(PAGES_THREADS) void k_pages_apply(PagesArgs g) {
     const int64_t base = tail + wave_back[wave];
     wave_gives(g, n, e.begins, [&](int at, int page) { g.queue[ring(base + at)] = page; });
     __syncthreads();  // (the rows of episodes that begin have been read: they may be written)
-    const int here = g.N - n0 < 1 << g.lge ? g.N - n0 : 1 << g.lge;
     if (g.table != g.table_in) {
         const int32_t* from = g.table_in + (int64_t)n0 * g.slots;
         int32_t* to = g.table + (int64_t)n0 * g.slots;
-#pragma unroll 4
-        for (int i = threadIdx.x; i < here * g.slots; i += PAGES_THREADS) {
-            const int r = (int)g.by_slots.quotient((uint32_t)i), j = i - r * g.slots, c = column[r];
-            const int old = from[i], now = entry[r];
+        auto put = [&](int i, int old) {
+            const int r = (int)g.by_slots.quotient((uint32_t)i), j = i - r * g.slots, c = column[r], now = entry[r];
             to[i] = c <= -2 ? (j == 0 ? now : -1) : c == j ? now : old;
+        };
+#pragma unroll
+        for (int i = 0; i < PAGES_AHEAD; ++i) {
+            const int at = threadIdx.x + i * PAGES_THREADS;
+            if (at < cells) put(at, ahead[i]);
         }
+#pragma unroll 4
+        for (int i = threadIdx.x + PAGES_AHEAD * PAGES_THREADS; i < cells; i += PAGES_THREADS) put(i, from[i]);
     } else if (n < g.N && e.live) {
         if (e.begins)
             for (int j = 1; j < g.slots; ++j) g.table[(int64_t)n * g.slots + j] = -1;
