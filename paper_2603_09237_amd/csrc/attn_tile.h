@@ -18,70 +18,115 @@ __device__ inline int lane_now() {
     return lane;
 }
 
-// A tile of ATTN_K rows of up to DP elements in LDS, rows 16 bytes apart beyond their length: reads of whole pieces along a row and transposed
-// reads (16 x 16 elements bf16, single ones fp32) both touch every bank equally often.
+// Operands hold bf16 values; an fp32 one is the sum of three (split3), a product of two the six larger ones of nine products, the smallest first: fp32
+// results, at 96 cycles for 16 x 16 x 32 where the fp32 instructions take 256 (a history of 4099 steps, 2 x 4 heads of 32: 175 us on those).
+template <typename T>
+struct Operand {
+    static constexpr int N = sizeof(T) == 4 ? 3 : 1;
+    uint4 p[N];
+};
+template <int N, int M>
+__device__ inline void multiply(const uint4 (&a)[N], const uint4 (&b)[M], float4_t& acc) {
+    if constexpr (N == 1) {  // the second operand in parts, or none
+#pragma unroll
+        for (int i = 0; i < M; ++i) Mma16<bf16_t>::run(a[0], b[i], acc);
+    } else {
+        Mma16<bf16_t>::run(a[0], b[2], acc);
+        Mma16<bf16_t>::run(a[2], b[0], acc);
+        Mma16<bf16_t>::run(a[1], b[1], acc);
+        Mma16<bf16_t>::run(a[0], b[1], acc);
+        Mma16<bf16_t>::run(a[1], b[0], acc);
+        Mma16<bf16_t>::run(a[0], b[0], acc);
+    }
+}
+// Eight elements of a row from element d on, as they are in memory
+template <typename T, bool WHOLE>
+struct RowOperand {
+    RowPiece<T, WHOLE> u[sizeof(T) / 2];
+    __device__ inline void load(const T* row, int d, int D) {
+        u[0].load(row, d, D);
+        if constexpr (sizeof(T) == 4) u[1].load(row, d + 4, D);
+    }
+    __device__ inline void values(int d, int D, bool in, float (&v)[8]) const {
+        static_assert(sizeof(T) == 4, "");
+        const uint4 a = u[0].get(d, D, in), b = u[sizeof(T) / 2 - 1].get(d + 4, D, in);
+        v[0] = __uint_as_float(a.x); v[1] = __uint_as_float(a.y); v[2] = __uint_as_float(a.z); v[3] = __uint_as_float(a.w);
+        v[4] = __uint_as_float(b.x); v[5] = __uint_as_float(b.y); v[6] = __uint_as_float(b.z); v[7] = __uint_as_float(b.w);
+    }
+    __device__ inline Operand<T> get(int d, int D, bool in = true) const {
+        Operand<T> r;
+        if constexpr (sizeof(T) == 2) {
+            r.p[0] = u[0].get(d, D, in);
+        } else {
+            float v[8];
+            values(d, D, in, v);
+            split3<true>(v, r.p);
+        }
+        return r;
+    }
+};
+
+// A tile of ATTN_K rows of up to DP values in LDS, a plane for each part, rows 16 bytes apart beyond their length: reads of whole pieces along a row and
+// transposed reads of 16 x 16 values both touch every bank equally often.
 template <typename T, int DP>
 struct Tile {
-    static constexpr int ES = sizeof(T), VE = 16 / ES, PITCH = DP * ES + 16, CPR = DP / VE, KS = DP * ES / 64, NB = DP / 16;
-    static constexpr int TU = ES == 2 ? 32 : 16, NU = ATTN_K / TU;  // rows of one transposed operand, operands of a tile
-    static constexpr int NX = TU / 16;                              // blocks of 16 of one
-    static constexpr int NP = ES == 2 ? 3 : 1;                      // parts of a computed operand (see Computed)
-    static constexpr int BYTES = ATTN_K * PITCH;
-    // the lane's operand of rows row .. row + 15, contraction indices of piece ks along the row
-    static __device__ inline uint4 rows(const unsigned char* lds, int row, int ks, int lane) {
-        return *reinterpret_cast<const uint4*>(lds + (row + (lane & 15)) * PITCH + ks * 64 + (lane >> 4) * 16);
+    static constexpr int ES = sizeof(T), VE = 16 / ES, CPR = DP / VE;  // in memory: pieces of a row
+    static constexpr int N = Operand<T>::N, PITCH = DP * 2 + 16, PLANE = ATTN_K * PITCH, BYTES = N * PLANE;
+    static constexpr int KS = DP / 32, NB = DP / 16, TU = 32, NU = ATTN_K / TU, NX = TU / 16;  // rows of a transposed operand, operands of a tile, blocks of one
+    static constexpr int OPITCH = DP * ES + 16;                                                // rows of results on their way out
+    // the lane's operand of rows row .. row + 15, contraction over the values 32 ks .. of the rows
+    static __device__ inline Operand<T> rows(const unsigned char* lds, int row, int ks, int lane) {
+        Operand<T> r;
+#pragma unroll
+        for (int q = 0; q < N; ++q) r.p[q] = *reinterpret_cast<const uint4*>(lds + q * PLANE + (row + (lane & 15)) * PITCH + ks * 64 + (lane >> 4) * 16);
+        return r;
     }
-    // columns 16 dt .. + 15 as the rows of an operand, contraction over the rows u TU .. : in the order in which a lane holds the products'
-    // results (bf16: 4 g + r of two blocks of 16; fp32: of one)
-    static __device__ inline uint4 turned(const unsigned char* lds, int u, int dt, int lane) {
+    // columns 16 dt .. + 15 as the rows of an operand, contraction over the rows 32 u .., in the order in which a lane holds the products' results
+    // (4 g + r of two blocks of 16)
+    static __device__ inline Operand<T> turned(const unsigned char* lds, int u, int dt, int lane) {
+        typedef __attribute__((address_space(3))) short4_t lds_s4;
         const int a = lane & 15, gr = lane >> 4;
-        if constexpr (ES == 2) {
-            typedef __attribute__((address_space(3))) short4_t lds_s4;
-            const unsigned char* s = lds + (32 * u + 4 * gr + (a >> 2)) * PITCH + (16 * dt + 4 * (a & 3)) * 2;
+        Operand<T> r;
+#pragma unroll
+        for (int q = 0; q < N; ++q) {
+            const unsigned char* s = lds + q * PLANE + (32 * u + 4 * gr + (a >> 2)) * PITCH + (16 * dt + 4 * (a & 3)) * 2;
             const uint2 u0 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)s));
             const uint2 u1 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(s + 16 * PITCH)));
-            return make_uint4(u0.x, u0.y, u1.x, u1.y);
-        } else {
-            const unsigned char* s = lds + (16 * u + 4 * gr) * PITCH + (16 * dt + a) * 4;
-            return make_uint4(*reinterpret_cast<const uint32_t*>(s), *reinterpret_cast<const uint32_t*>(s + PITCH),
-                              *reinterpret_cast<const uint32_t*>(s + 2 * PITCH), *reinterpret_cast<const uint32_t*>(s + 3 * PITCH));
+            r.p[q] = make_uint4(u0.x, u0.y, u1.x, u1.y);
         }
+        return r;
     }
-    static __device__ inline float at(const unsigned char* lds, int row, int d) {
-        return to_f(*reinterpret_cast<const T*>(lds + row * PITCH + d * ES));
+    // a piece from memory, columns col .. of a row
+    static __device__ inline void put(unsigned char* lds, int row, int col, const uint4& u) {
+        if constexpr (ES == 2) {
+            *reinterpret_cast<uint4*>(lds + row * PITCH + col * 2) = u;
+        } else {
+            uint2 part[3];
+            split3<true>(u, part);
+#pragma unroll
+            for (int q = 0; q < 3; ++q) *reinterpret_cast<uint2*>(lds + q * PLANE + row * PITCH + col * 2) = part[q];
+        }
     }
 };
 
-// A lane's computed operand of four values a block: bf16 in two parts (off by 2^-18 of the value at most), so that the one rounding that counts is the
-// output's (one part: y off by 2.0e-3 of its size instead of 1.6e-3; the second costs nothing that can be measured).  The forward of a training
-// pass takes a third: delta comes of y, and what it is off by adds up in the bias's gradient, which is an fp32 sum.
-template <typename T, int DP>
+// A lane's computed operand of four values a block.  For bf16 tensors in PARTS = 2 (off by 2^-18 of the value at most), so that the one rounding that
+// counts is the output's (one part: y off by 2.0e-3 of its size instead of 1.6e-3; the second costs nothing that can be measured).  The forward of
+// a training pass takes a third: delta comes of y, and what it is off by adds up in the bias's gradient, which is an fp32 sum.  fp32: three.
+template <int PARTS>
 struct Computed {
-    typedef Tile<T, DP> L;
-    uint4 part[L::NP];
-    __device__ inline void set(const float4_t (&p)[L::NX]) {
-        if constexpr (L::ES == 2) {
-            float v[8] = {p[0][0], p[0][1], p[0][2], p[0][3], p[1][0], p[1][1], p[1][2], p[1][3]};
+    uint4 p[PARTS];
+    __device__ inline void set(const float4_t (&f)[2]) {
+        float v[8] = {f[0][0], f[0][1], f[0][2], f[0][3], f[1][0], f[1][1], f[1][2], f[1][3]};
 #pragma unroll
-            for (int q = 0; q < L::NP; ++q) {
-                uint32_t w[4];
+        for (int q = 0; q < PARTS; ++q) {
+            uint32_t w[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    w[i] = pack2(v[2 * i], v[2 * i + 1]);
-                    v[2 * i] -= __uint_as_float(w[i] << 16);
-                    v[2 * i + 1] -= __uint_as_float(w[i] & 0xffff0000u);
-                }
-                part[q] = make_uint4(w[0], w[1], w[2], w[3]);
+            for (int i = 0; i < 4; ++i) {
+                w[i] = pack2(v[2 * i], v[2 * i + 1]);
+                v[2 * i] -= __uint_as_float(w[i] << 16);
+                v[2 * i + 1] -= __uint_as_float(w[i] & 0xffff0000u);
             }
-        } else {
-            const float4_t a = p[0];
-            part[0] = make_uint4(__float_as_uint(a[0]), __float_as_uint(a[1]), __float_as_uint(a[2]), __float_as_uint(a[3]));
+            p[q] = make_uint4(w[0], w[1], w[2], w[3]);
         }
     }
-    template <bool FINE>
-    __device__ inline void product(const uint4& turned, float4_t& acc) const {
-#pragma unroll
-        for (int i = 0; i < (FINE || L::NP < 3 ? L::NP : 2); ++i) Mma16<T>::run(turned, part[i], acc);
-    }
 };
-

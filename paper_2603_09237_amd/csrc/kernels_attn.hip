@@ -19,6 +19,8 @@ static int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 #define ATTN_THREADS 256
 #define ATTN_ROOM(rows, keys) ((rows) + 4 * (keys))  // table entries of a tile: pack <= 4 heads, each its distances
+// Waves of a SIMD that the registers are to leave room for (forward, backward of queries, of keys)
+constexpr int attn_waves(int pass, int es, int dp) { return es == 4 && dp == 128 ? 1 : dp == 128 || pass == 2 || (es == 4 && dp == 64) ? 2 : 3; }
 constexpr int kNever = 1 << 30;  // begin of the seen interval of a row that is not there
 
 struct AttnArgs {
@@ -183,7 +185,7 @@ struct Stage {
             }
         }
 #pragma unroll
-        for (int c = 0; c < CH; ++c) *reinterpret_cast<uint4*>(lds + (row() + c * STEP) * L::PITCH + col() * L::ES) = u[c];
+        for (int c = 0; c < CH; ++c) L::put(lds, row() + c * STEP, col(), u[c]);
         return met;
     }
 };
@@ -193,15 +195,15 @@ struct Stage {
 template <typename T, int DP, int NBLK, bool FINE = false>
 __device__ inline void fold(const unsigned char* lds, int u, const float4_t (&p)[NBLK][Tile<T, DP>::NX], float4_t (&acc)[NBLK][DP / 16], int lane) {
     typedef Tile<T, DP> L;
-    Computed<T, DP> c[NBLK];
+    Computed<sizeof(T) == 4 || FINE ? 3 : 2> c[NBLK];
 #pragma unroll
     for (int b = 0; b < NBLK; ++b) c[b].set(p[b]);
 #pragma unroll
     for (int dt = 0; dt < L::NB; ++dt) {
         if (dt && dt % 4 == 0) phase();
-        const uint4 f = L::turned(lds, u, dt, lane);
+        const Operand<T> f = L::turned(lds, u, dt, lane);
 #pragma unroll
-        for (int b = 0; b < NBLK; ++b) c[b].template product<FINE>(f, acc[b][dt]);
+        for (int b = 0; b < NBLK; ++b) multiply(f.p, c[b].p, acc[b][dt]);
     }
     phase();
 }
@@ -214,7 +216,7 @@ __device__ inline void send_rows(const unsigned char* lds, int D, F to) {
     for (int i = 0; i < 16 * L::CPR / 64; ++i) {
         const int p = i * 64 + lane, row = p / L::CPR, col = p % L::CPR * L::VE;
         T* dst = reinterpret_cast<T*>(to(row));
-        const uint4 u = *reinterpret_cast<const uint4*>(lds + row * L::PITCH + col * L::ES);
+        const uint4 u = *reinterpret_cast<const uint4*>(lds + row * L::OPITCH + col * L::ES);
         if (!dst) continue;
         if (WHOLE ? col < D : col + L::VE <= D) {
             *reinterpret_cast<piece_t*>(dst + col) = piece_t{u.x, u.y, u.z, u.w};
@@ -239,7 +241,7 @@ __device__ inline void put_rows(unsigned char* lds, const float4_t (&v)[DP / 16]
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int dt = 0; dt < L::NB; ++dt) {
-        unsigned char* at = lds + a * L::PITCH + (16 * dt + 4 * gr) * L::ES;
+        unsigned char* at = lds + a * L::OPITCH + (16 * dt + 4 * gr) * L::ES;
         if constexpr (L::ES == 2) *reinterpret_cast<uint2*>(at) = make_uint2(pack2(v[dt][0] * scale, v[dt][1] * scale), pack2(v[dt][2] * scale, v[dt][3] * scale));
         else *reinterpret_cast<float4_t*>(at) = float4_t{v[dt][0] * scale, v[dt][1] * scale, v[dt][2] * scale, v[dt][3] * scale};
     }
@@ -327,7 +329,7 @@ struct FwdLds {
     static constexpr int K = 0, V = Tile<T, DP>::BYTES, TAB = 2 * V, FLAG = TAB + ROOM * 4, TOTAL = FLAG + 16;
 };
 template <typename T, int DP, int QB, bool WHOLE, bool FINE>
-__global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_fwd(AttnArgs g) {
+__global__ __launch_bounds__(ATTN_THREADS, attn_waves(0, sizeof(T), DP)) void k_attn_fwd(AttnArgs g) {
     typedef Tile<T, DP> L;
     typedef FwdLds<T, DP, QB> M;
     extern __shared__ __align__(16) unsigned char lds[];
@@ -338,7 +340,7 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_fwd(At
     Rows R;
     R.init(g, BQ);
     int t[QB], p[QB], lo[QB];
-    uint4 qf[QB][L::KS];
+    Operand<T> qf[QB][L::KS];
 #pragma unroll
     for (int b = 0; b < QB; ++b) {
         const int r = R.r0 + (wave * QB + b) * 16 + a;
@@ -350,8 +352,8 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_fwd(At
                        (int64_t)(R.h0 + (r & ((1 << g.lgp) - 1))) * g.D;
 #pragma unroll
         for (int ks = 0; ks < L::KS; ++ks) {
-            const int d = ks * (64 / L::ES) + gr * L::VE;
-            RowPiece<T, WHOLE> u;
+            const int d = ks * 32 + gr * 8;
+            RowOperand<T, WHOLE> u;
             u.load(src, d, g.D);
             qf[b][ks] = u.get(d, g.D, in);
         }
@@ -412,9 +414,9 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_fwd(At
                 for (int b = 0; b < QB; ++b) s[b][x] = float4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int ks = 0; ks < L::KS; ++ks) {
-                    const uint4 f = L::rows(lds + M::K, 16 * x, ks, now);
+                    const Operand<T> f = L::rows(lds + M::K, 16 * x, ks, now);
 #pragma unroll
-                    for (int b = 0; b < QB; ++b) Mma16<T>::run(f, qf[b][ks], s[b][x]);
+                    for (int b = 0; b < QB; ++b) multiply(f.p, qf[b][ks].p, s[b][x]);
                 }
             }
             phase();
@@ -494,7 +496,7 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_fwd(At
         const float inv = 1.f / l[b];
         if (g.lse && gr == 0 && t[b] >= 0)
             g.lse[((int64_t)R.n * g.H + R.h0 + (a & ((1 << g.lgp) - 1))) * g.T + t[b]] = m[b] + __builtin_amdgcn_logf(l[b]);
-        unsigned char* mine = lds + wave * 16 * L::PITCH;
+        unsigned char* mine = lds + wave * 16 * L::OPITCH;
         const int first = R.r0 + (wave * QB + b) * 16;
         put_rows<T, DP, WHOLE>(mine, o[b], inv, g.D, [&](int row) -> T* {
             const int r = first + row;
@@ -512,7 +514,7 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_fwd(At
                     const int d = __float_as_int(y) - __float_as_int((float)(bf16_t)y);
                     rest[r] = (uint32_t)(d < 0x7fff ? d : 0x7fff) & 0xffff;
                 }
-                *reinterpret_cast<uint2*>(mine + a * L::PITCH + (16 * dt + 4 * gr) * 2) = make_uint2(rest[0] | rest[1] << 16, rest[2] | rest[3] << 16);
+                *reinterpret_cast<uint2*>(mine + a * L::OPITCH + (16 * dt + 4 * gr) * 2) = make_uint2(rest[0] | rest[1] << 16, rest[2] | rest[3] << 16);
             }
             __builtin_amdgcn_wave_barrier();
             send_rows<T, DP, WHOLE>(mine, g.D, [&](int row) -> T* {
@@ -541,22 +543,38 @@ struct Slant {
 };
 // Four values of distances 16 apart into a lane's bins: those of one bucket together first, so that the reads of the bins need not wait for each other
 // (the last write of a bin is the one with the sum)
-// at: the first one's entry in the table; entries from `end` on are distances that no pair of the tile has
+// at: the first one's entry in the table; entries from `end` on are distances that no pair of the tile has.  LANES 32: two lanes have a bin in common,
+// and add to it one after the other.
+template <int LANES, typename F>
+__device__ inline void by_halves(F add) {
+    if constexpr (LANES == 64) {
+        add();
+    } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if ((int)(threadIdx.x >> 5 & 1) == h) add();
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+}
+template <int LANES>
 __device__ inline void add_to_bins(float* bins, const int* idx, int at, int end, float4_t v) {
     int b[4];
-    float old[4];
 #pragma unroll
-    for (int x = 0; x < 4; ++x) b[x] = idx[at + 16 * x < end ? at + 16 * x : end - 1] * 64;
+    for (int x = 0; x < 4; ++x) b[x] = idx[at + 16 * x < end ? at + 16 * x : end - 1] * LANES;
 #pragma unroll
     for (int x = 3; x > 0; --x) {
         const bool same = b[x] == b[x - 1];
         v[x - 1] += same ? v[x] : 0.f;
         v[x] = same ? 0.f : v[x];
     }
+    by_halves<LANES>([&] {
+        float old[4];
 #pragma unroll
-    for (int x = 0; x < 4; ++x) old[x] = bins[b[x]];
+        for (int x = 0; x < 4; ++x) old[x] = bins[b[x]];
 #pragma unroll
-    for (int x = 3; x >= 0; --x) bins[b[x]] = old[x] + v[x];
+        for (int x = 3; x >= 0; --x) bins[b[x]] = old[x] + v[x];
+    });
 }
 
 // ---- backward, queries: dq, the sums of dA by bucket, and delta ---------------------------------------------------------------
@@ -564,26 +582,27 @@ template <typename T, int DP, int QB>
 struct DqLds {
     static constexpr int ROOM = ATTN_ROOM(64 * QB, ATTN_K), NR = (ROOM + ATTN_THREADS - 1) / ATTN_THREADS;
     static constexpr int K = 0, V = Tile<T, DP>::BYTES, TAB = 2 * V, IDX = TAB + ROOM * 4, FLAG = IDX + (64 * QB + ATTN_K) * 4, BINS = FLAG + 16;
+    static constexpr int LANES = BINS > 48 * 1024 ? 32 : 64;  // bins of a bucket and wave: beside the largest tiles fewer have to do
 };
 template <typename T, int DP, int QB, bool WHOLE>
-__global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_dq(AttnArgs g) {
+__global__ __launch_bounds__(ATTN_THREADS, attn_waves(1, sizeof(T), DP)) void k_attn_dq(AttnArgs g) {
     typedef Tile<T, DP> L;
     typedef DqLds<T, DP, QB> M;
     extern __shared__ __align__(16) unsigned char lds[];
     float* tab = reinterpret_cast<float*>(lds + M::TAB);
     int* idx = reinterpret_cast<int*>(lds + M::IDX);
     int* flag = reinterpret_cast<int*>(lds + M::FLAG);
-    constexpr int BQ = 64 * QB;
+    constexpr int BQ = 64 * QB, LANES = M::LANES;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, a = lane & 15, gr = lane >> 4, hh = lane & ((1 << g.lgp) - 1);
     // Sums of dA by bucket.  A lane adds up what it and its neighbours hold of one distance (see Slant) and adds that to a bin of its own: no two
     // lanes have a bin in common, so the order of every sum is the program's.  (Added pair by pair by LDS atomics: 174 cycles for 64 of them, half
     // of this kernel's time on 2048 x 8 x 8 heads of 128; laid out by distance in LDS and added up there: still a third.)
-    float* bins = reinterpret_cast<float*>(lds + M::BINS) + (int64_t)wave * g.B * 64 + lane;
+    float* bins = reinterpret_cast<float*>(lds + M::BINS) + (int64_t)wave * g.B * LANES + (lane & (LANES - 1));
     Rows R;
     R.init(g, BQ);
     int t[QB], p[QB], lo[QB];
     float lse[QB], delta[QB];
-    uint4 qf[QB][L::KS], of[QB][L::KS];
+    Operand<T> qf[QB][L::KS], of[QB][L::KS];
 #pragma unroll
     for (int b = 0; b < QB; ++b) {
         const int r = R.r0 + (wave * QB + b) * 16 + a;
@@ -599,8 +618,8 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_dq(Att
         float sum = 0.f;
 #pragma unroll
         for (int ks = 0; ks < L::KS; ++ks) {
-            const int d = ks * (64 / L::ES) + gr * L::VE;
-            RowPiece<T, WHOLE> uq, uo, uy;
+            const int d = ks * 32 + gr * 8;
+            RowOperand<T, WHOLE> uq, uo, uy;
             uq.load(src, d, g.D);
             uo.load(dsrc, d, g.D);
             uy.load(ysrc, d, g.D);
@@ -608,19 +627,20 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_dq(Att
             if constexpr (L::ES == 2) ul.load(lsrc, d, g.D);
             qf[b][ks] = uq.get(d, g.D, in);
             of[b][ks] = uo.get(d, g.D, in);
-            const uint4 yf = uy.get(d, g.D, in);
-            const uint32_t wy[4] = {yf.x, yf.y, yf.z, yf.w}, wd[4] = {of[b][ks].x, of[b][ks].y, of[b][ks].z, of[b][ks].w};
             if constexpr (L::ES == 2) {
-                const uint4 lf = ul.get(d, g.D, in);
-                const uint32_t wl[4] = {lf.x, lf.y, lf.z, lf.w};
+                const uint4 yf = uy.u[0].get(d, g.D, in), lf = ul.get(d, g.D, in), df = of[b][ks].p[0];
+                const uint32_t wy[4] = {yf.x, yf.y, yf.z, yf.w}, wd[4] = {df.x, df.y, df.z, df.w}, wl[4] = {lf.x, lf.y, lf.z, lf.w};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     sum = __builtin_fmaf(__uint_as_float(wd[i] << 16), __int_as_float((int)(wy[i] << 16) + ((int)(wl[i] << 16) >> 16)), sum);
                     sum = __builtin_fmaf(__uint_as_float(wd[i] & 0xffff0000u), __int_as_float((int)(wy[i] & 0xffff0000u) + ((int)wl[i] >> 16)), sum);
                 }
             } else {
+                float vy[8], vd[8];
+                uy.values(d, g.D, in, vy);
+                uo.values(d, g.D, in, vd);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sum = __builtin_fmaf(__uint_as_float(wd[i]), __uint_as_float(wy[i]), sum);
+                for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(vd[i], vy[i], sum);
             }
         }
         sum += __shfl_xor(sum, 16);
@@ -651,7 +671,7 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_dq(Att
     if (!g.table)
         for (int i = threadIdx.x; i < M::ROOM; i += ATTN_THREADS) tab[i] = 0.f;
     if (g.part)
-        for (int b = 0; b < g.B; ++b) bins[b * 64] = 0.f;
+        for (int b = 0; b < g.B; ++b) bins[b * LANES] = 0.f;
     float carry[QB];  // of the tile before, of distances that go on with the key `carry_k` (one head a tile)
     int carry_k = 0;
     bool lone[QB];    // sees itself only: its probability is one whatever the score, and dA nothing, not what two sums' roundings leave
@@ -700,11 +720,11 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_dq(Att
                     for (int b = 0; b < QB; ++b) s[b][i] = dp[b][i] = float4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int ks = 0; ks < L::KS; ++ks) {
-                        const uint4 f = L::rows(lds + M::K, 16 * x, ks, now), fv = L::rows(lds + M::V, 16 * x, ks, now);
+                        const Operand<T> f = L::rows(lds + M::K, 16 * x, ks, now), fv = L::rows(lds + M::V, 16 * x, ks, now);
 #pragma unroll
                         for (int b = 0; b < QB; ++b) {
-                            Mma16<T>::run(f, qf[b][ks], s[b][i]);
-                            Mma16<T>::run(fv, of[b][ks], dp[b][i]);
+                            multiply(f.p, qf[b][ks].p, s[b][i]);
+                            multiply(fv.p, of[b][ks].p, dp[b][i]);
                         }
                     }
                 }
@@ -749,10 +769,10 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_dq(Att
                         const float4_t v = {main[b][0] + carry[b], main[b][1] + over[b][0], main[b][2] + over[b][1], main[b][3] + over[b][2]};
                         carry[b] = over[b][3];
                         carry_k = k0 + ATTN_K;
-                        add_to_bins(bins, idx, at, each, v);
+                        add_to_bins<LANES>(bins, idx, at, each, v);
                     } else {
-                        add_to_bins(bins, idx, at, each, main[b]);
-                        add_to_bins(bins, idx, at + (16 >> g.lgp), each, over[b]);
+                        add_to_bins<LANES>(bins, idx, at, each, main[b]);
+                        add_to_bins<LANES>(bins, idx, at + (16 >> g.lgp), each, over[b]);
                     }
                 }
             }
@@ -771,7 +791,7 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_dq(Att
                 if (!see || !tainted(kb + (int64_t)k * g.k_t, g.D)) continue;
                 const float nan = __builtin_nanf("");
                 if (g.part)
-                    for (int i = 0; i < g.B; ++i) bins[i * 64] = nan;
+                    for (int i = 0; i < g.B; ++i) bins[i * LANES] = nan;
 #pragma unroll
                 for (int dt = 0; dt < L::NB; ++dt) o[b][dt] = float4_t{nan, nan, nan, nan};
             }
@@ -779,21 +799,21 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_dq(Att
 #pragma unroll
     for (int b = 0; b < QB; ++b) {
         const int first = R.r0 + (wave * QB + b) * 16;
-        put_rows<T, DP, WHOLE>(lds + wave * 16 * L::PITCH, o[b], g.scale, g.D, [&](int row) -> T* {
+        put_rows<T, DP, WHOLE>(lds + wave * 16 * L::OPITCH, o[b], g.scale, g.D, [&](int row) -> T* {
             const int r = first + row;
             if (r >= R.rows) return nullptr;
             return reinterpret_cast<T*>(g.dq) + (int64_t)(r >> g.lgp) * g.q_t + (int64_t)R.n * g.q_n + (int64_t)(R.h0 + (r & ((1 << g.lgp) - 1))) * g.D;
         });
     }
     if (!g.part) return;
-    bins[(g.B - 1) * 64] += outer;
+    by_halves<LANES>([&] { bins[(g.B - 1) * LANES] += outer; });
     if (g.lgp == 0) {
 #pragma unroll
         for (int b = 0; b < QB; ++b) {  // (rows that are not there may lie between the last tile's keys and the block's last row)
             int d = R.past + R.r0 + (wave * QB + b) * 16 + a - carry_k - 4 * gr;
             d = d < 0 ? 0 : d >= g.reach ? g.reach - 1 : d;
             const int i = g.bucket[d];
-            bins[(i < 0 ? 0 : i >= g.B ? g.B - 1 : i) * 64] += carry[b];
+            by_halves<LANES>([&] { bins[(i < 0 ? 0 : i >= g.B ? g.B - 1 : i) * LANES] += carry[b]; });
         }
     }
     __syncthreads();
@@ -804,11 +824,12 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 128 ? 2 : 3) void k_attn_dq(Att
         const int b = b0 + (threadIdx.x >> 3);
         float sum = 0.f;
         if (b < g.B) {
-            const float* from = reinterpret_cast<const float*>(lds + M::BINS) + b * 64 + head;
+            constexpr int EACH = LANES / 8;
+            const float* from = reinterpret_cast<const float*>(lds + M::BINS) + b * LANES + head;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int at = (eighth * 8 + ((i + b) & 7)) << g.lgp;
-                sum += (from[at] + from[at + g.B * 64]) + (from[at + 2 * g.B * 64] + from[at + 3 * g.B * 64]);
+            for (int i = 0; i < EACH; ++i) {
+                const int at = (eighth * EACH + ((i + b) & (EACH - 1))) << g.lgp, wave_ = g.B * LANES;
+                sum += (from[at] + from[at + wave_]) + (from[at + 2 * wave_] + from[at + 3 * wave_]);
             }
         }
         for (int o = 1 << g.lgp; o < 8; o <<= 1) sum += __shfl_xor(sum, o);
@@ -836,11 +857,8 @@ struct DkvLds {
     static constexpr int ROOM = ATTN_ROOM(ATTN_K, 64 * KB), NR = (ROOM + ATTN_THREADS - 1) / ATTN_THREADS;
     static constexpr int Q = 0, O = Tile<T, DP>::BYTES, TAB = 2 * O, INFO = TAB + ROOM * 4, FLAG = INFO + 3 * ATTN_K * 4, TOTAL = FLAG + 16;
 };
-#ifndef DKVW
-#define DKVW 2
-#endif
 template <typename T, int DP, int KB, bool WHOLE>
-__global__ __launch_bounds__(ATTN_THREADS, DP == 64 ? DKVW : 2) void k_attn_dkv(AttnArgs g) {
+__global__ __launch_bounds__(ATTN_THREADS, attn_waves(2, sizeof(T), DP)) void k_attn_dkv(AttnArgs g) {
     typedef Tile<T, DP> L;
     typedef DkvLds<T, DP, KB> M;
     extern __shared__ __align__(16) unsigned char lds[];
@@ -857,7 +875,7 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 64 ? DKVW : 2) void k_attn_dkv(
     R.kv = at.rest % g.KV;
     R.past = g.S - g.T;
     const int k0 = (g.tiles - 1 - at.tile) * BK, k_last = (k0 + BK < g.S ? k0 + BK : g.S) - 1;
-    uint4 kf[KB][L::KS], vf[KB][L::KS];
+    Operand<T> kf[KB][L::KS], vf[KB][L::KS];
     int key[KB];
     float4_t dk[KB][L::NB], dv[KB][L::NB];
 #pragma unroll
@@ -867,8 +885,8 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 64 ? DKVW : 2) void k_attn_dkv(
         const int64_t at = (int64_t)(in ? key[b] : 0) * g.k_t + (int64_t)R.n * g.k_n + (int64_t)R.kv * g.D;
 #pragma unroll
         for (int ks = 0; ks < L::KS; ++ks) {
-            const int d = ks * (64 / L::ES) + gr * L::VE;
-            RowPiece<T, WHOLE> uk, uv;
+            const int d = ks * 32 + gr * 8;
+            RowOperand<T, WHOLE> uk, uv;
             uk.load(reinterpret_cast<const T*>(g.k) + at, d, g.D);
             uv.load(reinterpret_cast<const T*>(g.v) + at, d, g.D);
             kf[b][ks] = uk.get(d, g.D, in);
@@ -947,11 +965,11 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 64 ? DKVW : 2) void k_attn_dkv(
                         for (int b = 0; b < KB; ++b) s[b][i] = e[b][i] = float4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                         for (int ks = 0; ks < L::KS; ++ks) {
-                            const uint4 f = L::rows(lds + M::Q, 16 * x, ks, now), fo = L::rows(lds + M::O, 16 * x, ks, now);
+                            const Operand<T> f = L::rows(lds + M::Q, 16 * x, ks, now), fo = L::rows(lds + M::O, 16 * x, ks, now);
 #pragma unroll
                             for (int b = 0; b < KB; ++b) {
-                                Mma16<T>::run(f, kf[b][ks], s[b][i]);
-                                Mma16<T>::run(fo, vf[b][ks], e[b][i]);
+                                multiply(f.p, kf[b][ks].p, s[b][i]);
+                                multiply(fo.p, vf[b][ks].p, e[b][i]);
                             }
                         }
                     }
@@ -1022,8 +1040,8 @@ __global__ __launch_bounds__(ATTN_THREADS, DP == 64 ? DKVW : 2) void k_attn_dkv(
         const auto place = [&](void* base, int row) -> T* {
             return first + row < g.S ? reinterpret_cast<T*>(base) + (int64_t)(first + row) * g.k_t + (int64_t)R.n * g.k_n + (int64_t)R.kv * g.D : nullptr;
         };
-        put_rows<T, DP, WHOLE>(lds + wave * 16 * L::PITCH, dk[b], g.scale, g.D, [&](int row) { return place(g.dk, row); });
-        put_rows<T, DP, WHOLE>(lds + wave * 16 * L::PITCH, dv[b], 1.f, g.D, [&](int row) { return place(g.dv, row); });
+        put_rows<T, DP, WHOLE>(lds + wave * 16 * L::OPITCH, dk[b], g.scale, g.D, [&](int row) { return place(g.dk, row); });
+        put_rows<T, DP, WHOLE>(lds + wave * 16 * L::OPITCH, dv[b], 1.f, g.D, [&](int row) { return place(g.dv, row); });
     }
 }
 
@@ -1095,7 +1113,7 @@ template <typename T, int DP, int QB, bool WHOLE>
 static int attn_dq_pass(AttnArgs& g, hipStream_t s) {
     g.tiles = (int)cdiv((int64_t)g.T << g.lgp, 64 * QB);
     if (run_kernel(k_attn_dq<T, DP, QB, WHOLE>, g, (int64_t)g.tiles * g.N * (g.H >> g.lgp),
-                   DqLds<T, DP, QB>::BINS + (g.part ? g.B * 1024 : 0), s))
+                   DqLds<T, DP, QB>::BINS + (g.part ? g.B * DqLds<T, DP, QB>::LANES * 16 : 0), s))
         return 1;
     if (g.part) k_attn_dbias<<<dim3((uint32_t)(g.H * g.B)), 256, 0, s>>>(g);
     return 0;

@@ -483,13 +483,13 @@ __global__ __launch_bounds__(256, DP == 128 ? 2 : 3) void k_attn_step_bf16(StepA
             }
         }
     }
-    uint4 qf[L::KS];
+    Operand<T> qf[L::KS];
 #pragma unroll
     for (int ks = 0; ks < L::KS; ++ks) {
         const int d = 32 * ks + 8 * gr;
         RowPiece<T, WHOLE> u;
         u.load(reinterpret_cast<const T*>(g.q) + (int64_t)n * g.q_n + (int64_t)(h0 + (a < heads ? a : 0)) * g.D, d, g.D);
-        qf[ks] = u.get(d, g.D, a < heads);
+        qf[ks].p[0] = u.get(d, g.D, a < heads);
     }
     int last_edge = 0;
     float beyond = 0.f;
@@ -551,7 +551,7 @@ __global__ __launch_bounds__(256, DP == 128 ? 2 : 3) void k_attn_step_bf16(StepA
 #pragma unroll
             for (int ks = 0; ks < L::KS; ++ks) {
                 const int d = 32 * ks + 8 * gr;
-                Mma16<T>::run(kp[x][ks].get(d, g.D, in[x]), qf[ks], s[0][x]);
+                Mma16<T>::run(kp[x][ks].get(d, g.D, in[x]), qf[ks].p[0], s[0][x]);
                 *reinterpret_cast<uint4*>(mine + (16 * x + a) * L::PITCH + d * 2) = vp[x][ks].get(d, g.D, in[x]);
             }
         }
@@ -598,10 +598,10 @@ __global__ __launch_bounds__(256, DP == 128 ? 2 : 3) void k_attn_step_bf16(StepA
                 s[0][x][r] = __builtin_amdgcn_exp2f(s[0][x][r] - base);
                 l += s[0][x][r];
             }
-        Computed<T, DP> p;
+        Computed<2> p;
         p.set(s[0]);
 #pragma unroll
-        for (int dt = 0; dt < L::NB; ++dt) p.template product<false>(L::turned(mine, 0, dt, lane), o[0][dt]);
+        for (int dt = 0; dt < L::NB; ++dt) multiply(L::turned(mine, 0, dt, lane).p, p.p, o[0][dt]);
         __builtin_amdgcn_wave_barrier();
     }
     // joined: the waves
