@@ -368,9 +368,11 @@ int morlax_memory_step(const morlax_scan_dims* dims, int32_t width, const void* 
  * over the s <= p_t with p_t - s < window and no episode's begin in (s, p_t] (first [S, N] u8, non-zero: an episode begins at that step;
  * NULL: nowhere).  bucket(d) = the number of edges[j] <= d with j >= 1: edges [buckets] int32 ascending, bucket j holds the distances from
  * edges[j] on (0 for the first, whatever edges[0] says).  buckets 0: no bias (bias, edges NULL).  What is not seen is never used: it may be
- * infinite or undefined, in values and in gradients.  A row whose seen scores are all -infinity is undefined.
+ * infinite or undefined, in values and in gradients.  A row whose seen scores are all -infinity is undefined; infinite or undefined inputs that
+ * are seen make what depends on them infinite or undefined (not always which of the two the formula, step by step, gives).
  *   q, y [T, N, heads * head_dim] (strides q_t, q_n and y_t, y_n), k, v [S, N, kv_heads * head_dim] (strides k_t, k_n both), bias [heads,
- *   buckets] fp32.  saved: morlax_attn_saved_bytes() bytes that the backward needs, or NULL.
+ *   buckets] fp32.  saved: morlax_attn_saved_bytes() bytes that the backward needs, or NULL.  fp32 operands are multiplied as three bf16 parts:
+ *   those below 1e-30 lose digits.
  * Limits: 1 <= T <= S <= 2^20, 1 <= head_dim <= 128, kv_heads | heads <= 1024, 0 <= buckets <= 64, window >= 1, and fewer than 2^24 workgroups:
  * N * heads * ceil(T / 64) and N * kv_heads * ceil(S / 64) below 2^24, N * heads * buckets * ceil(T / 64) below 2^38. */
 typedef struct {

@@ -501,7 +501,7 @@ def attn_saved_bytes(dims):
 
 
 def attn_workspace_bytes(dims, backward=False):
-    """Bytes of device scratch that attn_fwd (without `saved`) or attn_bwd needs."""
+    """Bytes of device scratch that attn_fwd (attn_bwd) needs."""
     return _size(load().morlax_attn_workspace_bytes(C.byref(dims), int(bool(backward))))
 
 

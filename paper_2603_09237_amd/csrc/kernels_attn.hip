@@ -20,7 +20,9 @@ static int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 #define ATTN_THREADS 256
 #define ATTN_ROOM(rows, keys) ((rows) + 4 * (keys))  // table entries of a tile: pack <= 4 heads, each its distances
 // Waves of a SIMD that the registers are to leave room for (forward, backward of queries, of keys)
-constexpr int attn_waves(int pass, int es, int dp) { return es == 4 && dp == 128 ? 1 : dp == 128 || pass == 2 || (es == 4 && dp == 64) ? 2 : 3; }
+constexpr int attn_waves(int pass, int es, int dp) {
+    return es == 4 && dp == 128 ? 1 : dp == 128 || pass == 2 || (es == 4 && dp == 64) ? 2 : pass == 0 && dp == 32 ? 4 : 3;
+}
 constexpr int kNever = 1 << 30;  // begin of the seen interval of a row that is not there
 
 struct AttnArgs {
@@ -41,6 +43,11 @@ struct AttnArgs {
     int T, S, N, H, KV, D, B, window, reach, lgp, tiles;
     int64_t q_t, q_n, k_t, k_n, y_t, y_n;
     uint32_t total;
+    // few long walks are cut into `chunks` of `span` tiles each, whose parts are joined by a launch of their own
+    int chunks, span;
+    float* part_o;    // forward: [chunks, N H T, DP] outputs ahead of their division; backward of keys: [2, chunks, S N KV, DP] dk and dv
+    float2* part_m;   // [chunks, N H T] maximum (in units of log2) and sum
+    int32_t* part_n;  // [chunks, N KV tiles] is there a part
     int whole;  // rows hold whole pieces of 16 bytes
 };
 
@@ -254,9 +261,10 @@ __device__ inline void put_rows(unsigned char* lds, const float4_t (&v)[DP / 16]
 // XCD has where these are few, so that the last ones to end are short.
 struct Place {
     uint32_t rest;
-    int tile;
+    int tile, chunk;
     __device__ inline Place(const AttnArgs& g) {
-        const uint32_t x = blockIdx.x & 7, i = blockIdx.x >> 3, rests = g.total / g.tiles, own = rests >> 3;
+        chunk = blockIdx.x / g.total;
+        const uint32_t at = blockIdx.x - chunk * g.total, x = at & 7, i = at >> 3, rests = g.total / g.tiles, own = rests >> 3;
         if (own <= 16 && own * 8 == rests) {
             rest = x + 8 * (i % own);
             tile = g.tiles - 1 - (int)(i / own);
@@ -270,7 +278,7 @@ struct Place {
 
 // A workgroup's rows of queries: (step, head of the pack), heads next to each other
 struct Rows {
-    int n, kv, h0, r0, rows, past;
+    int n, kv, h0, r0, rows, past, chunk;
     __device__ inline void init(const AttnArgs& g, int per) {
         const Place at(g);
         const uint32_t packs = g.H >> g.lgp;
@@ -278,6 +286,7 @@ struct Rows {
         h0 = (at.rest % packs) << g.lgp;
         kv = h0 / (g.H / g.KV);
         r0 = at.tile * per;
+        chunk = at.chunk;
         rows = g.T << g.lgp;
         past = g.S - g.T;
     }
@@ -360,7 +369,12 @@ __global__ __launch_bounds__(ATTN_THREADS, attn_waves(0, sizeof(T), DP)) void k_
     }
     const int first_p = R.past + (R.r0 >> g.lgp), each = (BQ >> g.lgp) + ATTN_K, far = first_p + (BQ >> g.lgp) - 1;
     const int last_row = (R.r0 + BQ < R.rows ? R.r0 + BQ : R.rows) - 1;
-    const int k_begin = R.lo(g, first_p), k_end = R.past + (last_row >> g.lgp) + 1;
+    int k_begin = R.lo(g, first_p), k_end = R.past + (last_row >> g.lgp) + 1;
+    if (g.chunks > 1) {
+        k_begin += R.chunk * g.span * ATTN_K;
+        const int end = k_begin + g.span * ATTN_K;
+        k_end = end < k_end ? end : k_end;
+    }
     const int last_edge = g.table ? g.edges[g.B - 1] : 0;
     const float beyond = g.table ? g.bias[(int64_t)(R.h0 + (lane & ((1 << g.lgp) - 1))) * g.B + g.B - 1] * kLog2e : 0.f;
     const T* kb = reinterpret_cast<const T*>(g.k) + (int64_t)R.n * g.k_n + (int64_t)R.kv * g.D;
@@ -387,7 +401,7 @@ __global__ __launch_bounds__(ATTN_THREADS, attn_waves(0, sizeof(T), DP)) void k_
         sv.load(vb, g.k_t, k0, k_end, 0, g.D);
         if (g.table) st.template load<false>(g, R.h0, each, far - k0, -1);
     };
-    request(k_begin);
+    if (k_begin < k_end) request(k_begin);  // (a chunk may be empty)
     __syncthreads();
     for (int k0 = k_begin; k0 < k_end; k0 += ATTN_K) {
         const bool near = g.table && first_p - (k0 + ATTN_K - 1) < last_edge;
@@ -493,6 +507,16 @@ __global__ __launch_bounds__(ATTN_THREADS, attn_waves(0, sizeof(T), DP)) void k_
     for (int b = 0; b < QB; ++b) {
         l[b] += __shfl_xor(l[b], 16);
         l[b] += __shfl_xor(l[b], 32);
+        if (g.chunks > 1) {
+            if (t[b] < 0) continue;
+            const int64_t row = ((int64_t)R.n * g.H + R.h0 + (a & ((1 << g.lgp) - 1))) * g.T + t[b], all = (int64_t)g.N * g.H * g.T;
+            if (gr == 0) g.part_m[R.chunk * all + row] = make_float2(m[b], k_begin < k_end ? l[b] : -1.f);
+            float* dst = g.part_o + (R.chunk * all + row) * DP + 4 * gr;
+            if (k_begin < k_end)
+#pragma unroll
+                for (int dt = 0; dt < L::NB; ++dt) *reinterpret_cast<float4_t*>(dst + 16 * dt) = o[b][dt];
+            continue;
+        }
         const float inv = 1.f / l[b];
         if (g.lse && gr == 0 && t[b] >= 0)
             g.lse[((int64_t)R.n * g.H + R.h0 + (a & ((1 << g.lgp) - 1))) * g.T + t[b]] = m[b] + __builtin_amdgcn_logf(l[b]);
@@ -522,6 +546,43 @@ __global__ __launch_bounds__(ATTN_THREADS, attn_waves(0, sizeof(T), DP)) void k_
                 if (r >= R.rows) return nullptr;
                 return reinterpret_cast<T*>(g.low) + (((int64_t)(r >> g.lgp) * g.N + R.n) * g.H + R.h0 + (r & ((1 << g.lgp) - 1))) * g.D;
             });
+        }
+    }
+}
+
+// The parts of a row, joined: DP / 4 lanes a row, four columns each
+template <typename T, int DP>
+__global__ __launch_bounds__(256) void k_attn_fwd_join(AttnArgs g) {
+    constexpr int LANES = DP / 4;
+    const int64_t all = (int64_t)g.N * g.H * g.T, row = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+    if (row >= all) return;
+    const int d = threadIdx.x % LANES * 4, t = (int)(row % g.T), h = (int)(row / g.T % g.H), n = (int)(row / g.T / g.H);
+    float top = -__builtin_inff();
+    for (int c = 0; c < g.chunks; ++c) top = fmaxf(top, g.part_m[c * all + row].x);
+    const float base = top == -__builtin_inff() ? 0.f : top;
+    float sum = 0.f;
+    float4_t y = {0.f, 0.f, 0.f, 0.f};
+    for (int c = 0; c < g.chunks; ++c) {
+        const float2 p = g.part_m[c * all + row];
+        if (p.y < 0.f) continue;  // (an empty chunk, which wrote no part)
+        const float f = __builtin_amdgcn_exp2f(p.x - base);
+        const float4_t o = *reinterpret_cast<const float4_t*>(g.part_o + (c * all + row) * DP + d);
+        sum = __builtin_fmaf(f, p.y, sum);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = __builtin_fmaf(f, o[i], y[i]);
+    }
+    if (g.lse && d == 0) g.lse[row] = top + __builtin_amdgcn_logf(sum);
+    T* dst = reinterpret_cast<T*>(g.out) + (int64_t)t * g.y_t + (int64_t)n * g.y_n + (int64_t)h * g.D;
+    uint16_t* low = g.low ? g.low + (((int64_t)t * g.N + n) * g.H + h) * g.D : nullptr;
+    const float inv = 1.f / sum;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (d + i >= g.D) continue;
+        const float v = y[i] * inv;
+        dst[d + i] = cvt<T>(v);
+        if (sizeof(T) == 2 && low) {
+            const int rest = __float_as_int(v) - __float_as_int((float)(bf16_t)v);
+            low[d + i] = (uint16_t)(rest < 0x7fff ? rest : 0x7fff);
         }
     }
 }
@@ -904,7 +965,14 @@ __global__ __launch_bounds__(ATTN_THREADS, attn_waves(2, sizeof(T), DP)) void k_
     const int t_begin = k0 > R.past ? k0 - R.past : 0;
     // the last step that may see a key here; episodes end the walk earlier
     const int64_t t_far = (int64_t)k_last + g.window - R.past;
-    const int t_end = t_far < g.T ? (int)t_far : g.T, r_begin = (t_begin << g.lgp) & ~3, r_end = t_end << g.lgp;
+    const int t_end = t_far < g.T ? (int)t_far : g.T, r_first = (t_begin << g.lgp) & ~3, r_last = t_end << g.lgp;
+    int r_begin = r_first, r_end = r_last;
+    if (g.chunks > 1) {
+        r_begin += at.chunk * g.span * ATTN_K;
+        const int64_t end = (int64_t)r_begin + g.span * ATTN_K;
+        r_end = end < r_last ? (int)end : r_last;
+    }
+    bool some = false;  // (of a chunk: has a row been looked at)
     for (int h0 = R.kv * share; h0 < (R.kv + 1) * share; h0 += pack) {
         const T* qb = reinterpret_cast<const T*>(g.q) + (int64_t)R.n * g.q_n + (int64_t)h0 * g.D;
         const T* ob = reinterpret_cast<const T*>(g.dy) + (int64_t)R.n * g.y_n + (int64_t)h0 * g.D;
@@ -948,6 +1016,7 @@ __global__ __launch_bounds__(ATTN_THREADS, attn_waves(2, sizeof(T), DP)) void k_
             }
             __syncthreads();
             if (row_lo[0] > k_last) break;  // (lo never falls: no later row sees a key here)
+            some = true;
             if (r0 + ATTN_K < r_end) request(r0 + ATTN_K);
             const int p0 = R.past + (r0 >> g.lgp);
             auto tile = [&](auto fast) {
@@ -1034,6 +1103,22 @@ __global__ __launch_bounds__(ATTN_THREADS, attn_waves(2, sizeof(T), DP)) void k_
             __syncthreads();  // (the next heads' walk may set it again)
         }
     }
+    if (g.chunks > 1) {
+        if (threadIdx.x == 0) g.part_n[(int64_t)at.chunk * g.total + (int64_t)at.rest * g.tiles + at.tile] = some;
+        if (!some) return;
+        const int64_t all = (int64_t)g.S * g.N * g.KV;
+#pragma unroll
+        for (int b = 0; b < KB; ++b) {
+            if (key[b] >= g.S) continue;
+            float* to = g.part_o + (at.chunk * all + ((int64_t)key[b] * g.N + R.n) * g.KV + R.kv) * DP + 4 * gr;
+#pragma unroll
+            for (int dt = 0; dt < L::NB; ++dt) {
+                *reinterpret_cast<float4_t*>(to + 16 * dt) = dk[b][dt];
+                *reinterpret_cast<float4_t*>(to + g.chunks * all * DP + 16 * dt) = dv[b][dt];
+            }
+        }
+        return;
+    }
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
         const int first = k0 + (wave * KB + b) * 16;
@@ -1045,11 +1130,65 @@ __global__ __launch_bounds__(ATTN_THREADS, attn_waves(2, sizeof(T), DP)) void k_
     }
 }
 
+// The parts of dk and dv, added up in the chunks' order: DP / 4 lanes a key, four columns each
+template <typename T, int DP>
+__global__ __launch_bounds__(256) void k_attn_dkv_join(AttnArgs g, int keys) {
+    constexpr int LANES = DP / 4;
+    const int64_t all = (int64_t)g.S * g.N * g.KV, row = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+    if (row >= all) return;
+    const int d = threadIdx.x % LANES * 4, kv = (int)(row % g.KV), n = (int)(row / g.KV % g.N), s = (int)(row / g.KV / g.N);
+    const int64_t flag = ((int64_t)n * g.KV + kv) * g.tiles + (g.tiles - 1 - s / keys);
+    float4_t dk = {0.f, 0.f, 0.f, 0.f}, dv = dk;
+    for (int c = 0; c < g.chunks; ++c) {
+        if (!g.part_n[(int64_t)c * g.total + flag]) continue;
+        const float* from = g.part_o + (c * all + row) * DP + d;
+        const float4_t a = *reinterpret_cast<const float4_t*>(from), b = *reinterpret_cast<const float4_t*>(from + g.chunks * all * DP);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            dk[i] += a[i];
+            dv[i] += b[i];
+        }
+    }
+    const int64_t at = (int64_t)s * g.k_t + (int64_t)n * g.k_n + (int64_t)kv * g.D;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (d + i >= g.D) continue;
+        reinterpret_cast<T*>(g.dk)[at + d + i] = cvt<T>(dk[i] * g.scale);
+        reinterpret_cast<T*>(g.dv)[at + d + i] = cvt<T>(dv[i]);
+    }
+}
+
 // ---- host -------------------------------------------------------------------------------------------------------------------
 // query heads of a tile: the power of two that divides the heads of a head of keys, up to 4
 static int pack_bits(const morlax_attn_dims& d) {
     const int share = d.heads / d.kv_heads;
     return share % 4 == 0 ? 2 : share % 2 == 0 ? 1 : 0;
+}
+static int padded(int D) { return D <= 32 ? 32 : D <= 64 ? 64 : 128; }
+// rows of queries that a workgroup of the forward takes: two blocks of 16 a wave in long bf16 heads where there are rows for them
+static int fwd_rows(const morlax_attn_dims& d) { return d.dtype && d.head_dim > 64 && ((int64_t)d.T << pack_bits(d)) > 64 ? 128 : 64; }
+// Where the workgroups are no more than the chip holds at once, the time is that of the longest walk (earlier keys are seen by more rows, later rows see
+// more keys), and most of the chip is idle at its end: such walks are cut until there is work for the chip twice over, into no chunk of under eight
+// tiles, as each part is written and read again.  4099 steps of 2 x 4 fp32 heads of 32, forward (260 workgroups, 1024 places): 149 us in one piece,
+// 116 in four, 96 in seven; dk and dv of 2048 x 8 x 8 heads of 128 to 2 of keys (512 workgroups, 512 places): 519 in one piece, 382 in two, 433
+// in four.  The forward of the latter (1024 workgroups of twice the rows): 200 in one piece, 308 in four.
+static void cut(AttnArgs& g, int waves, int64_t workgroups, int64_t tiles) {
+    int64_t c = 2 * 256 * waves / workgroups;
+    c = c < tiles / 8 ? c : tiles / 8;
+    c = c < 8 ? c : 8;
+    g.chunks = c > 1 ? (int)c : 1;
+    g.span = (int)cdiv(tiles, g.chunks);
+}
+static void cut_fwd(AttnArgs& g, const morlax_attn_dims& d) {
+    const int rows = fwd_rows(d);
+    const int64_t seen = (int64_t)d.window + (rows >> g.lgp);
+    cut(g, attn_waves(0, d.dtype ? 2 : 4, padded(d.head_dim)), cdiv((int64_t)d.T << g.lgp, rows) * d.N * (d.heads >> g.lgp),
+        cdiv(seen < d.S ? seen : d.S, ATTN_K));
+}
+static void cut_dkv(AttnArgs& g, const morlax_attn_dims& d) {
+    const int64_t seeing = (int64_t)d.window + 64;
+    cut(g, attn_waves(2, d.dtype ? 2 : 4, padded(d.head_dim)), cdiv(d.S, 64) * d.N * d.kv_heads,
+        cdiv(((seeing < d.T ? seeing : d.T) << g.lgp) + 3, ATTN_K));
 }
 static AttnArgs attn_args(const morlax_attn_dims& d) {
     AttnArgs g = {};
@@ -1081,8 +1220,20 @@ static int64_t attn_carve_saved(AttnArgs& g, const morlax_attn_dims& d, void* sa
     return attn_carve_prepared(g, saved, at);
 }
 #define ATTN_ROWS 64  // the fewest rows of queries of a workgroup
-static int64_t attn_carve_bwd(AttnArgs& g, void* ws) {
+static int64_t attn_carve_fwd(AttnArgs& g, const morlax_attn_dims& d, void* ws, int64_t at) {
+    cut_fwd(g, d);
+    if (g.chunks == 1) return at;
+    const int64_t rows = (int64_t)g.chunks * g.N * g.H * g.T;
+    at = carve(g.part_m, at, ws, rows * 8);
+    return carve(g.part_o, at, ws, rows * padded(g.D) * 4);
+}
+static int64_t attn_carve_bwd(AttnArgs& g, const morlax_attn_dims& d, void* ws) {
     int64_t at = carve(g.delta, 0, ws, (int64_t)g.N * g.H * g.T * 4);
+    cut_dkv(g, d);
+    if (g.chunks > 1) {
+        at = carve(g.part_n, at, ws, (int64_t)g.chunks * g.N * g.KV * cdiv(g.S, 64) * 4);
+        at = carve(g.part_o, at, ws, 2 * (int64_t)g.chunks * g.S * g.N * g.KV * padded(g.D) * 4);
+    }
     if (g.B) at = carve(g.part, at, ws, (int64_t)g.H * g.B * g.N * cdiv((int64_t)g.T << g.lgp, ATTN_ROWS) * 4);
     return at;
 }
@@ -1092,13 +1243,13 @@ int64_t attn_saved_bytes(const morlax_attn_dims& d) {
 }
 int64_t attn_ws_bytes(const morlax_attn_dims& d, bool back) {
     AttnArgs g = attn_args(d);
-    return back ? attn_carve_bwd(g, nullptr) : attn_carve_prepared(g, nullptr, 0);
+    return back ? attn_carve_bwd(g, d, nullptr) : attn_carve_fwd(g, d, nullptr, attn_carve_prepared(g, nullptr, 0));
 }
 
-static int run_kernel(void (*kernel)(AttnArgs), AttnArgs& g, int64_t total, int lds, hipStream_t s) {
+static int run_kernel(void (*kernel)(AttnArgs), AttnArgs& g, int64_t total, int chunks, int lds, hipStream_t s) {
     if (hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess) return 1;
     g.total = (uint32_t)total;
-    kernel<<<dim3((uint32_t)total), ATTN_THREADS, lds, s>>>(g);
+    kernel<<<dim3((uint32_t)(total * chunks)), ATTN_THREADS, lds, s>>>(g);
     return 0;
 }
 template <typename T, int DP, int QB, bool WHOLE, bool FINE = false>
@@ -1107,12 +1258,14 @@ static int attn_fwd_pass(AttnArgs& g, hipStream_t s) {
         if (g.low) return attn_fwd_pass<T, DP, QB, WHOLE, true>(g, s);
     }
     g.tiles = (int)cdiv((int64_t)g.T << g.lgp, 64 * QB);
-    return run_kernel(k_attn_fwd<T, DP, QB, WHOLE, FINE>, g, (int64_t)g.tiles * g.N * (g.H >> g.lgp), FwdLds<T, DP, QB>::TOTAL, s);
+    if (run_kernel(k_attn_fwd<T, DP, QB, WHOLE, FINE>, g, (int64_t)g.tiles * g.N * (g.H >> g.lgp), g.chunks, FwdLds<T, DP, QB>::TOTAL, s)) return 1;
+    if (g.chunks > 1) k_attn_fwd_join<T, DP><<<dim3((uint32_t)cdiv((int64_t)g.N * g.H * g.T * (DP / 4), 256)), 256, 0, s>>>(g);
+    return 0;
 }
 template <typename T, int DP, int QB, bool WHOLE>
 static int attn_dq_pass(AttnArgs& g, hipStream_t s) {
     g.tiles = (int)cdiv((int64_t)g.T << g.lgp, 64 * QB);
-    if (run_kernel(k_attn_dq<T, DP, QB, WHOLE>, g, (int64_t)g.tiles * g.N * (g.H >> g.lgp),
+    if (run_kernel(k_attn_dq<T, DP, QB, WHOLE>, g, (int64_t)g.tiles * g.N * (g.H >> g.lgp), 1,
                    DqLds<T, DP, QB>::BINS + (g.part ? g.B * DqLds<T, DP, QB>::LANES * 16 : 0), s))
         return 1;
     if (g.part) k_attn_dbias<<<dim3((uint32_t)(g.H * g.B)), 256, 0, s>>>(g);
@@ -1121,13 +1274,15 @@ static int attn_dq_pass(AttnArgs& g, hipStream_t s) {
 template <typename T, int DP, int KB, bool WHOLE>
 static int attn_dkv_pass(AttnArgs& g, hipStream_t s) {
     g.tiles = (int)cdiv(g.S, 64 * KB);
-    return run_kernel(k_attn_dkv<T, DP, KB, WHOLE>, g, (int64_t)g.tiles * g.N * g.KV, DkvLds<T, DP, KB>::TOTAL, s);
+    if (run_kernel(k_attn_dkv<T, DP, KB, WHOLE>, g, (int64_t)g.tiles * g.N * g.KV, g.chunks, DkvLds<T, DP, KB>::TOTAL, s)) return 1;
+    if (g.chunks > 1) k_attn_dkv_join<T, DP><<<dim3((uint32_t)cdiv((int64_t)g.S * g.N * g.KV * (DP / 4), 256)), 256, 0, s>>>(g, 64 * KB);
+    return 0;
 }
 // A wave takes one block of 16 rows; in the forward pass of long bf16 heads two where there are rows for them, as what is read of a tile then serves
 // both (2048 x 8 x 8 heads of 128: 167 us, one block 186; heads of 64, 64 steps: 90, one block 75; the backward kernels run out of registers).
 template <typename T, int DP, bool WHOLE>
 static int attn_whole(AttnArgs& g, bool back, hipStream_t s) {
-    constexpr int MORE = sizeof(T) == 2 && DP == 128 ? 2 : 1;
+    constexpr int MORE = sizeof(T) == 2 && DP == 128 ? 2 : 1;  // (fwd_rows says the same)
     if (!back) return ((int64_t)g.T << g.lgp) > 64 ? attn_fwd_pass<T, DP, MORE, WHOLE>(g, s) : attn_fwd_pass<T, DP, 1, WHOLE>(g, s);
     return attn_dq_pass<T, DP, 1, WHOLE>(g, s) || attn_dkv_pass<T, DP, 1, WHOLE>(g, s);
 }
@@ -1146,8 +1301,9 @@ int launch_attn_fwd(const morlax_attn_dims& d, const void* q, const void* k, con
                     const uint8_t* first, void* y, void* saved, void* ws, hipStream_t s) {
     AttnArgs g = attn_args(d);
     g.q = q; g.k = k; g.v = v; g.bias = bias; g.edges = edges; g.first = first; g.out = y;
+    const int64_t at = attn_carve_prepared(g, ws, 0);
+    attn_carve_fwd(g, d, ws, at);
     if (saved) attn_carve_saved(g, d, saved);
-    else attn_carve_prepared(g, ws, 0);
     if (!first) g.lo = nullptr;
     if (first || g.B) {
         int lgn = 0;
@@ -1164,7 +1320,7 @@ int launch_attn_bwd(const morlax_attn_dims& d, const void* q, const void* k, con
     g.q = q; g.k = k; g.v = v; g.bias = bias; g.edges = edges; g.first = first; g.y = y; g.dy = dy;
     g.dq = dq; g.dk = dk; g.dv = dv; g.dbias = dbias;
     attn_carve_saved(g, d, const_cast<void*>(saved));
-    attn_carve_bwd(g, ws);
+    attn_carve_bwd(g, d, ws);
     if (!first) g.lo = nullptr;
     if (!dbias) g.part = nullptr;
     return d.dtype ? attn_pick<bf16_t>(g, true, s) : attn_pick<float>(g, true, s);

@@ -753,7 +753,7 @@ extern "C" int morlax_attn_fwd(const morlax_attn_dims* dims, const void* q, cons
     if ((rc = check_bias(dims->buckets, bias, edges, who)) != MORLAX_OK) return rc;
     OPT(saved, who);
     if (y == q || y == k || y == v) return fail(MORLAX_ERR_SHAPE, "%s: an output is its input", who);
-    if (!saved) WS(ws, ws_bytes, attn_ws_bytes(*dims, false), who);
+    WS(ws, ws_bytes, attn_ws_bytes(*dims, false), who);
     if (launch_attn_fwd(*dims, q, k, v, bias, edges, first, y, saved, ws, (hipStream_t)stream) != 0)
         return fail(MORLAX_ERR_HIP, "%s: the kernel's LDS is not available on this device", who);
     return finish(who);

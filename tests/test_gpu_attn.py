@@ -180,6 +180,45 @@ def test_values_and_gradients(kind, shape):
         near(got[k], want[k], bound[k], k)
 
 
+# walks of so many tiles, by so few workgroups, that they are cut into chunks whose parts are joined
+LONG = [
+    (1100, 1100, 1, 2, 1, 40, 17, 1100, 0.002),   # forward in two chunks, keys in four; chunks behind an episode's end
+    (1, 1200, 2, 4, 1, 64, 8, 1200, 0.0),
+    (600, 600, 1, 4, 1, 128, 8, 600, 0.01),       # keys only
+    (130, 1300, 2, 2, 2, 33, 0, 1025, 0.0),       # forward only, no bias, rows that are no whole pieces
+    (1030, 1031, 1, 1, 1, 8, 3, 1000, 0.3),       # most chunks see nothing
+]
+
+
+@pytest.mark.parametrize("shape", LONG, ids=lambda s: "x".join(str(v) for v in s))
+@pytest.mark.parametrize("kind", ["float32", "bfloat16"])
+def test_long_walks_of_few_workgroups(kind, shape):
+    torch = _torch()
+    c = make(getattr(torch, kind), *shape)
+    want, bound = define(c)
+    got, again, strided = run(c), run(c), run(c, 5, "environments")
+    for k in got:
+        near(got[k], want[k], bound[k], k)
+        assert torch.equal(got[k], again[k]) and torch.equal(got[k], strided[k]), k
+
+
+@pytest.mark.parametrize("kind", ["float32", "bfloat16"])
+def test_undefined_in_a_chunk(kind):
+    """An undefined value, key, query or gradient in a cut walk reaches what sees it and nothing else."""
+    torch = _torch()
+    c = make(getattr(torch, kind), 1100, 1100, 1, 1, 1, 16, 0, 600, 0.0)
+    clean, t = run(c), torch.arange(1100)
+    sees, seen = (t >= 30) & (t < 630), (t <= 900) & (t > 300)
+    for name, at, affected in (("v", 30, {"y": sees}), ("k", 30, {"y": sees, "q": sees}), ("q", 900, {"y": t == 900, "k": seen, "v": seen}),
+                               ("dy", 900, {"q": t == 900, "k": seen})):
+        d = dict(c, **{name: c[name].clone()})
+        d[name][at, 0, 0] = float("nan")
+        got = run(d)
+        for k, rows in affected.items():
+            assert not bool(torch.isfinite(got[k][rows].float()).any()), (name, k)
+            assert torch.equal(got[k][~rows], clean[k][~rows]), (name, k)
+
+
 @pytest.mark.parametrize("pad,order", [(3, "time"), (8, "environments"), (5, "environments")])
 @pytest.mark.parametrize("kind", ["float32", "bfloat16"])
 def test_strides(kind, pad, order):
