@@ -25,6 +25,14 @@ constexpr int attn_waves(int pass, int es, int dp) {
 }
 constexpr int kNever = 1 << 30;  // begin of the seen interval of a row that is not there
 
+// Few long walks are cut into `chunks` of `span` tiles each, whose parts are joined by a launch of their own (see `cut` below)
+struct Cut {
+    int chunks, span;
+    float* o;         // forward: [chunks, N H T, DP] outputs ahead of their division; queries: the same of dq; keys: [2, chunks, S N KV, DP] dk and dv
+    float2* m;        // forward: [chunks, N H T] maximum (in units of log2) and sum, -1: no part
+    int32_t* there;   // backward: [chunks, workgroups of a chunk] is there a part
+};
+
 struct AttnArgs {
     const void *q, *k, *v, *y, *dy;
     void *out, *dq, *dk, *dv;
@@ -43,11 +51,7 @@ struct AttnArgs {
     int T, S, N, H, KV, D, B, window, reach, lgp, tiles;
     int64_t q_t, q_n, k_t, k_n, y_t, y_n;
     uint32_t total;
-    // few long walks are cut into `chunks` of `span` tiles each, whose parts are joined by a launch of their own
-    int chunks, span;
-    float* part_o;    // forward: [chunks, N H T, DP] outputs ahead of their division; backward of keys: [2, chunks, S N KV, DP] dk and dv
-    float2* part_m;   // [chunks, N H T] maximum (in units of log2) and sum
-    int32_t* part_n;  // [chunks, N KV tiles] is there a part
+    Cut cut, cut_q;  // of the forward or of the backward's pass over the keys; of its pass over the queries
     int whole;  // rows hold whole pieces of 16 bytes
 };
 
@@ -370,9 +374,9 @@ __global__ __launch_bounds__(ATTN_THREADS, attn_waves(0, sizeof(T), DP)) void k_
     const int first_p = R.past + (R.r0 >> g.lgp), each = (BQ >> g.lgp) + ATTN_K, far = first_p + (BQ >> g.lgp) - 1;
     const int last_row = (R.r0 + BQ < R.rows ? R.r0 + BQ : R.rows) - 1;
     int k_begin = R.lo(g, first_p), k_end = R.past + (last_row >> g.lgp) + 1;
-    if (g.chunks > 1) {
-        k_begin += R.chunk * g.span * ATTN_K;
-        const int end = k_begin + g.span * ATTN_K;
+    if (g.cut.chunks > 1) {
+        k_begin += R.chunk * g.cut.span * ATTN_K;
+        const int end = k_begin + g.cut.span * ATTN_K;
         k_end = end < k_end ? end : k_end;
     }
     const int last_edge = g.table ? g.edges[g.B - 1] : 0;
@@ -507,11 +511,11 @@ __global__ __launch_bounds__(ATTN_THREADS, attn_waves(0, sizeof(T), DP)) void k_
     for (int b = 0; b < QB; ++b) {
         l[b] += __shfl_xor(l[b], 16);
         l[b] += __shfl_xor(l[b], 32);
-        if (g.chunks > 1) {
+        if (g.cut.chunks > 1) {
             if (t[b] < 0) continue;
             const int64_t row = ((int64_t)R.n * g.H + R.h0 + (a & ((1 << g.lgp) - 1))) * g.T + t[b], all = (int64_t)g.N * g.H * g.T;
-            if (gr == 0) g.part_m[R.chunk * all + row] = make_float2(m[b], k_begin < k_end ? l[b] : -1.f);
-            float* dst = g.part_o + (R.chunk * all + row) * DP + 4 * gr;
+            if (gr == 0) g.cut.m[R.chunk * all + row] = make_float2(m[b], k_begin < k_end ? l[b] : -1.f);
+            float* dst = g.cut.o + (R.chunk * all + row) * DP + 4 * gr;
             if (k_begin < k_end)
 #pragma unroll
                 for (int dt = 0; dt < L::NB; ++dt) *reinterpret_cast<float4_t*>(dst + 16 * dt) = o[b][dt];
@@ -558,15 +562,15 @@ __global__ __launch_bounds__(256) void k_attn_fwd_join(AttnArgs g) {
     if (row >= all) return;
     const int d = threadIdx.x % LANES * 4, t = (int)(row % g.T), h = (int)(row / g.T % g.H), n = (int)(row / g.T / g.H);
     float top = -__builtin_inff();
-    for (int c = 0; c < g.chunks; ++c) top = fmaxf(top, g.part_m[c * all + row].x);
+    for (int c = 0; c < g.cut.chunks; ++c) top = fmaxf(top, g.cut.m[c * all + row].x);
     const float base = top == -__builtin_inff() ? 0.f : top;
     float sum = 0.f;
     float4_t y = {0.f, 0.f, 0.f, 0.f};
-    for (int c = 0; c < g.chunks; ++c) {
-        const float2 p = g.part_m[c * all + row];
+    for (int c = 0; c < g.cut.chunks; ++c) {
+        const float2 p = g.cut.m[c * all + row];
         if (p.y < 0.f) continue;  // (an empty chunk, which wrote no part)
         const float f = __builtin_amdgcn_exp2f(p.x - base);
-        const float4_t o = *reinterpret_cast<const float4_t*>(g.part_o + (c * all + row) * DP + d);
+        const float4_t o = *reinterpret_cast<const float4_t*>(g.cut.o + (c * all + row) * DP + d);
         sum = __builtin_fmaf(f, p.y, sum);
 #pragma unroll
         for (int i = 0; i < 4; ++i) y[i] = __builtin_fmaf(f, o[i], y[i]);
@@ -711,12 +715,17 @@ __global__ __launch_bounds__(ATTN_THREADS, attn_waves(1, sizeof(T), DP)) void k_
         if (in) {
             const int64_t row = ((int64_t)R.n * g.H + h) * g.T + t[b];
             lse[b] = g.lse[row];
-            if (gr == 0) g.delta[row] = sum;
+            if (gr == 0 && R.chunk == 0) g.delta[row] = sum;
         }
     }
     const int first_p = R.past + (R.r0 >> g.lgp), each = (BQ >> g.lgp) + ATTN_K, far = first_p + (BQ >> g.lgp) - 1;
     const int last_row = (R.r0 + BQ < R.rows ? R.r0 + BQ : R.rows) - 1;
-    const int k_begin = R.lo(g, first_p), k_end = R.past + (last_row >> g.lgp) + 1;
+    int k_begin = R.lo(g, first_p), k_end = R.past + (last_row >> g.lgp) + 1;
+    if (g.cut_q.chunks > 1) {
+        k_begin += R.chunk * g.cut_q.span * ATTN_K;
+        const int end = k_begin + g.cut_q.span * ATTN_K;
+        k_end = end < k_end ? end : k_end;
+    }
     const int last_edge = g.table ? g.edges[g.B - 1] : 0;
     const float beyond = g.table ? g.bias[(int64_t)(R.h0 + hh) * g.B + g.B - 1] * kLog2e : 0.f;
     const T* kb = reinterpret_cast<const T*>(g.k) + (int64_t)R.n * g.k_n + (int64_t)R.kv * g.D;
@@ -750,7 +759,7 @@ __global__ __launch_bounds__(ATTN_THREADS, attn_waves(1, sizeof(T), DP)) void k_
         sv.load(vb, g.k_t, k0, k_end, 0, g.D);
         if (g.table) st.template load<true>(g, R.h0, each, far - k0, -1);
     };
-    request(k_begin);
+    if (k_begin < k_end) request(k_begin);
     __syncthreads();
     for (int k0 = k_begin; k0 < k_end; k0 += ATTN_K) {
         const bool near = g.table && first_p - (k0 + ATTN_K - 1) < last_edge;
@@ -857,14 +866,26 @@ __global__ __launch_bounds__(ATTN_THREADS, attn_waves(1, sizeof(T), DP)) void k_
                 for (int dt = 0; dt < L::NB; ++dt) o[b][dt] = float4_t{nan, nan, nan, nan};
             }
     }
+    if (g.cut_q.chunks > 1) {
+        if (threadIdx.x == 0) g.cut_q.there[R.chunk * g.total + (R.n * (g.H >> g.lgp) + (R.h0 >> g.lgp)) * g.tiles + R.r0 / BQ] = k_begin < k_end;
+        const int64_t all = (int64_t)g.N * g.H * g.T;
 #pragma unroll
-    for (int b = 0; b < QB; ++b) {
-        const int first = R.r0 + (wave * QB + b) * 16;
-        put_rows<T, DP, WHOLE>(lds + wave * 16 * L::OPITCH, o[b], g.scale, g.D, [&](int row) -> T* {
-            const int r = first + row;
-            if (r >= R.rows) return nullptr;
-            return reinterpret_cast<T*>(g.dq) + (int64_t)(r >> g.lgp) * g.q_t + (int64_t)R.n * g.q_n + (int64_t)(R.h0 + (r & ((1 << g.lgp) - 1))) * g.D;
-        });
+        for (int b = 0; b < QB; ++b) {
+            if (t[b] < 0 || k_begin >= k_end) continue;
+            float* to = g.cut_q.o + (R.chunk * all + ((int64_t)R.n * g.H + R.h0 + hh) * g.T + t[b]) * DP + 4 * gr;
+#pragma unroll
+            for (int dt = 0; dt < L::NB; ++dt) *reinterpret_cast<float4_t*>(to + 16 * dt) = o[b][dt];
+        }
+    } else {
+#pragma unroll
+        for (int b = 0; b < QB; ++b) {
+            const int first = R.r0 + (wave * QB + b) * 16;
+            put_rows<T, DP, WHOLE>(lds + wave * 16 * L::OPITCH, o[b], g.scale, g.D, [&](int row) -> T* {
+                const int r = first + row;
+                if (r >= R.rows) return nullptr;
+                return reinterpret_cast<T*>(g.dq) + (int64_t)(r >> g.lgp) * g.q_t + (int64_t)R.n * g.q_n + (int64_t)(R.h0 + (r & ((1 << g.lgp) - 1))) * g.D;
+            });
+        }
     }
     if (!g.part) return;
     by_halves<LANES>([&] { bins[(g.B - 1) * LANES] += outer; });
@@ -879,7 +900,7 @@ __global__ __launch_bounds__(ATTN_THREADS, attn_waves(1, sizeof(T), DP)) void k_
     }
     __syncthreads();
     // eight threads a bucket: each adds up an eighth of its lanes (of one head, in an order that touches no bank twice) of all four waves
-    const int64_t parts = (int64_t)g.N * g.tiles, mine = (int64_t)R.n * g.tiles + R.r0 / BQ;
+    const int64_t parts = (int64_t)g.N * g.tiles * g.cut_q.chunks, mine = ((int64_t)R.n * g.tiles + R.r0 / BQ) * g.cut_q.chunks + R.chunk;
     const int part = threadIdx.x & 7, head = part & ((1 << g.lgp) - 1), eighth = part >> g.lgp;
     for (int b0 = 0; b0 < g.B; b0 += 32) {
         const int b = b0 + (threadIdx.x >> 3);
@@ -901,7 +922,7 @@ __global__ __launch_bounds__(ATTN_THREADS, attn_waves(1, sizeof(T), DP)) void k_
 // dbias[h, b]: the workgroups' sums, one block each
 __global__ __launch_bounds__(256) void k_attn_dbias(AttnArgs g) {
     __shared__ float part[4];
-    const int64_t parts = (int64_t)g.N * g.tiles;
+    const int64_t parts = (int64_t)g.N * g.tiles * g.cut_q.chunks;
     const float* src = g.part + (int64_t)blockIdx.x * parts;
     float sum = 0.f;
     for (int64_t i = threadIdx.x; i < parts; i += 256) sum += src[i];
@@ -967,9 +988,9 @@ __global__ __launch_bounds__(ATTN_THREADS, attn_waves(2, sizeof(T), DP)) void k_
     const int64_t t_far = (int64_t)k_last + g.window - R.past;
     const int t_end = t_far < g.T ? (int)t_far : g.T, r_first = (t_begin << g.lgp) & ~3, r_last = t_end << g.lgp;
     int r_begin = r_first, r_end = r_last;
-    if (g.chunks > 1) {
-        r_begin += at.chunk * g.span * ATTN_K;
-        const int64_t end = (int64_t)r_begin + g.span * ATTN_K;
+    if (g.cut.chunks > 1) {
+        r_begin += at.chunk * g.cut.span * ATTN_K;
+        const int64_t end = (int64_t)r_begin + g.cut.span * ATTN_K;
         r_end = end < r_last ? (int)end : r_last;
     }
     bool some = false;  // (of a chunk: has a row been looked at)
@@ -1103,18 +1124,18 @@ __global__ __launch_bounds__(ATTN_THREADS, attn_waves(2, sizeof(T), DP)) void k_
             __syncthreads();  // (the next heads' walk may set it again)
         }
     }
-    if (g.chunks > 1) {
-        if (threadIdx.x == 0) g.part_n[(int64_t)at.chunk * g.total + (int64_t)at.rest * g.tiles + at.tile] = some;
+    if (g.cut.chunks > 1) {
+        if (threadIdx.x == 0) g.cut.there[at.chunk * g.total + at.rest * g.tiles + k0 / BK] = some;
         if (!some) return;
         const int64_t all = (int64_t)g.S * g.N * g.KV;
 #pragma unroll
         for (int b = 0; b < KB; ++b) {
             if (key[b] >= g.S) continue;
-            float* to = g.part_o + (at.chunk * all + ((int64_t)key[b] * g.N + R.n) * g.KV + R.kv) * DP + 4 * gr;
+            float* to = g.cut.o + (at.chunk * all + ((int64_t)key[b] * g.N + R.n) * g.KV + R.kv) * DP + 4 * gr;
 #pragma unroll
             for (int dt = 0; dt < L::NB; ++dt) {
                 *reinterpret_cast<float4_t*>(to + 16 * dt) = dk[b][dt];
-                *reinterpret_cast<float4_t*>(to + g.chunks * all * DP + 16 * dt) = dv[b][dt];
+                *reinterpret_cast<float4_t*>(to + g.cut.chunks * all * DP + 16 * dt) = dv[b][dt];
             }
         }
         return;
@@ -1130,25 +1151,40 @@ __global__ __launch_bounds__(ATTN_THREADS, attn_waves(2, sizeof(T), DP)) void k_
     }
 }
 
-// The parts of dk and dv, added up in the chunks' order: DP / 4 lanes a key, four columns each
+// The parts of a row's gradient, added up in the chunks' order: DP / 4 lanes a row, four columns each
+template <int DP>
+__device__ inline float4_t add_parts(const Cut& c, const float* from, int64_t rows, uint32_t total, uint32_t workgroup) {
+    float4_t sum = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < c.chunks; ++i) {
+        if (!c.there[i * total + workgroup]) continue;
+        const float4_t v = *reinterpret_cast<const float4_t*>(from + i * rows * DP);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += v[e];
+    }
+    return sum;
+}
+template <typename T, int DP>
+__global__ __launch_bounds__(256) void k_attn_dq_join(AttnArgs g, int queries) {
+    constexpr int LANES = DP / 4;
+    const int64_t all = (int64_t)g.N * g.H * g.T, row = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+    if (row >= all) return;
+    const int d = threadIdx.x % LANES * 4, t = (int)(row % g.T), h = (int)(row / g.T % g.H), n = (int)(row / g.T / g.H);
+    const uint32_t workgroup = (n * (g.H >> g.lgp) + (h >> g.lgp)) * g.tiles + ((t << g.lgp) + (h & ((1 << g.lgp) - 1))) / queries;
+    const float4_t v = add_parts<DP>(g.cut_q, g.cut_q.o + row * DP + d, all, g.total, workgroup);
+    T* to = reinterpret_cast<T*>(g.dq) + (int64_t)t * g.q_t + (int64_t)n * g.q_n + (int64_t)h * g.D;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (d + i < g.D) to[d + i] = cvt<T>(v[i] * g.scale);
+}
 template <typename T, int DP>
 __global__ __launch_bounds__(256) void k_attn_dkv_join(AttnArgs g, int keys) {
     constexpr int LANES = DP / 4;
     const int64_t all = (int64_t)g.S * g.N * g.KV, row = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
     if (row >= all) return;
     const int d = threadIdx.x % LANES * 4, kv = (int)(row % g.KV), n = (int)(row / g.KV % g.N), s = (int)(row / g.KV / g.N);
-    const int64_t flag = ((int64_t)n * g.KV + kv) * g.tiles + (g.tiles - 1 - s / keys);
-    float4_t dk = {0.f, 0.f, 0.f, 0.f}, dv = dk;
-    for (int c = 0; c < g.chunks; ++c) {
-        if (!g.part_n[(int64_t)c * g.total + flag]) continue;
-        const float* from = g.part_o + (c * all + row) * DP + d;
-        const float4_t a = *reinterpret_cast<const float4_t*>(from), b = *reinterpret_cast<const float4_t*>(from + g.chunks * all * DP);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            dk[i] += a[i];
-            dv[i] += b[i];
-        }
-    }
+    const uint32_t workgroup = (n * g.KV + kv) * g.tiles + s / keys;
+    const float* from = g.cut.o + row * DP + d;
+    const float4_t dk = add_parts<DP>(g.cut, from, all, g.total, workgroup), dv = add_parts<DP>(g.cut, from + g.cut.chunks * all * DP, all, g.total, workgroup);
     const int64_t at = (int64_t)s * g.k_t + (int64_t)n * g.k_n + (int64_t)kv * g.D;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -1172,23 +1208,23 @@ static int fwd_rows(const morlax_attn_dims& d) { return d.dtype && d.head_dim > 
 // tiles, as each part is written and read again.  4099 steps of 2 x 4 fp32 heads of 32, forward (260 workgroups, 1024 places): 149 us in one piece,
 // 116 in four, 96 in seven; dk and dv of 2048 x 8 x 8 heads of 128 to 2 of keys (512 workgroups, 512 places): 519 in one piece, 382 in two, 433
 // in four.  The forward of the latter (1024 workgroups of twice the rows): 200 in one piece, 308 in four.
-static void cut(AttnArgs& g, int waves, int64_t workgroups, int64_t tiles) {
+// One environment's 4096 steps, 4 bf16 heads of 64 (256 workgroups): forward 105, dq 102, dk and dv 150 us in one piece; 66, 75 and 105 cut, with their
+// joins.
+static Cut cut(int waves, int64_t workgroups, int64_t tiles) {
     int64_t c = 2 * 256 * waves / workgroups;
     c = c < tiles / 8 ? c : tiles / 8;
     c = c < 8 ? c : 8;
-    g.chunks = c > 1 ? (int)c : 1;
-    g.span = (int)cdiv(tiles, g.chunks);
+    Cut r = {};
+    r.chunks = c > 1 ? (int)c : 1;
+    r.span = (int)cdiv(tiles, r.chunks);
+    return r;
 }
-static void cut_fwd(AttnArgs& g, const morlax_attn_dims& d) {
-    const int rows = fwd_rows(d);
-    const int64_t seen = (int64_t)d.window + (rows >> g.lgp);
-    cut(g, attn_waves(0, d.dtype ? 2 : 4, padded(d.head_dim)), cdiv((int64_t)d.T << g.lgp, rows) * d.N * (d.heads >> g.lgp),
-        cdiv(seen < d.S ? seen : d.S, ATTN_K));
-}
-static void cut_dkv(AttnArgs& g, const morlax_attn_dims& d) {
-    const int64_t seeing = (int64_t)d.window + 64;
-    cut(g, attn_waves(2, d.dtype ? 2 : 4, padded(d.head_dim)), cdiv(d.S, 64) * d.N * d.kv_heads,
-        cdiv(((seeing < d.T ? seeing : d.T) << g.lgp) + 3, ATTN_K));
+// pass 0, 1: `rows` rows of queries to a workgroup, along the keys; 2: 64 keys, along the queries
+static Cut cut_of(const morlax_attn_dims& d, int pass, int rows) {
+    const int lgp = pack_bits(d), waves = attn_waves(pass, d.dtype ? 2 : 4, padded(d.head_dim));
+    const int64_t reach = (int64_t)d.window + (pass == 2 ? rows : rows >> lgp), most = pass == 2 ? d.T : d.S, seen = reach < most ? reach : most;
+    return pass == 2 ? cut(waves, cdiv(d.S, rows) * d.N * d.kv_heads, cdiv((seen << lgp) + 3, ATTN_K))
+                     : cut(waves, cdiv((int64_t)d.T << lgp, rows) * d.N * (d.heads >> lgp), cdiv(seen, ATTN_K));
 }
 static AttnArgs attn_args(const morlax_attn_dims& d) {
     AttnArgs g = {};
@@ -1221,20 +1257,25 @@ static int64_t attn_carve_saved(AttnArgs& g, const morlax_attn_dims& d, void* sa
 }
 #define ATTN_ROWS 64  // the fewest rows of queries of a workgroup
 static int64_t attn_carve_fwd(AttnArgs& g, const morlax_attn_dims& d, void* ws, int64_t at) {
-    cut_fwd(g, d);
-    if (g.chunks == 1) return at;
-    const int64_t rows = (int64_t)g.chunks * g.N * g.H * g.T;
-    at = carve(g.part_m, at, ws, rows * 8);
-    return carve(g.part_o, at, ws, rows * padded(g.D) * 4);
+    g.cut = cut_of(d, 0, fwd_rows(d));
+    if (g.cut.chunks == 1) return at;
+    const int64_t rows = (int64_t)g.cut.chunks * g.N * g.H * g.T;
+    at = carve(g.cut.m, at, ws, rows * 8);
+    return carve(g.cut.o, at, ws, rows * padded(g.D) * 4);
 }
 static int64_t attn_carve_bwd(AttnArgs& g, const morlax_attn_dims& d, void* ws) {
     int64_t at = carve(g.delta, 0, ws, (int64_t)g.N * g.H * g.T * 4);
-    cut_dkv(g, d);
-    if (g.chunks > 1) {
-        at = carve(g.part_n, at, ws, (int64_t)g.chunks * g.N * g.KV * cdiv(g.S, 64) * 4);
-        at = carve(g.part_o, at, ws, 2 * (int64_t)g.chunks * g.S * g.N * g.KV * padded(g.D) * 4);
+    g.cut_q = cut_of(d, 1, ATTN_ROWS);
+    if (g.cut_q.chunks > 1) {
+        at = carve(g.cut_q.there, at, ws, (int64_t)g.cut_q.chunks * g.N * (g.H >> g.lgp) * cdiv((int64_t)g.T << g.lgp, ATTN_ROWS) * 4);
+        at = carve(g.cut_q.o, at, ws, (int64_t)g.cut_q.chunks * g.N * g.H * g.T * padded(g.D) * 4);
     }
-    if (g.B) at = carve(g.part, at, ws, (int64_t)g.H * g.B * g.N * cdiv((int64_t)g.T << g.lgp, ATTN_ROWS) * 4);
+    g.cut = cut_of(d, 2, 64);
+    if (g.cut.chunks > 1) {
+        at = carve(g.cut.there, at, ws, (int64_t)g.cut.chunks * g.N * g.KV * cdiv(g.S, 64) * 4);
+        at = carve(g.cut.o, at, ws, 2 * (int64_t)g.cut.chunks * g.S * g.N * g.KV * padded(g.D) * 4);
+    }
+    if (g.B) at = carve(g.part, at, ws, (int64_t)g.H * g.B * g.N * cdiv((int64_t)g.T << g.lgp, ATTN_ROWS) * g.cut_q.chunks * 4);
     return at;
 }
 int64_t attn_saved_bytes(const morlax_attn_dims& d) {
@@ -1258,24 +1299,25 @@ static int attn_fwd_pass(AttnArgs& g, hipStream_t s) {
         if (g.low) return attn_fwd_pass<T, DP, QB, WHOLE, true>(g, s);
     }
     g.tiles = (int)cdiv((int64_t)g.T << g.lgp, 64 * QB);
-    if (run_kernel(k_attn_fwd<T, DP, QB, WHOLE, FINE>, g, (int64_t)g.tiles * g.N * (g.H >> g.lgp), g.chunks, FwdLds<T, DP, QB>::TOTAL, s)) return 1;
-    if (g.chunks > 1) k_attn_fwd_join<T, DP><<<dim3((uint32_t)cdiv((int64_t)g.N * g.H * g.T * (DP / 4), 256)), 256, 0, s>>>(g);
+    if (run_kernel(k_attn_fwd<T, DP, QB, WHOLE, FINE>, g, (int64_t)g.tiles * g.N * (g.H >> g.lgp), g.cut.chunks, FwdLds<T, DP, QB>::TOTAL, s)) return 1;
+    if (g.cut.chunks > 1) k_attn_fwd_join<T, DP><<<dim3((uint32_t)cdiv((int64_t)g.N * g.H * g.T * (DP / 4), 256)), 256, 0, s>>>(g);
     return 0;
 }
 template <typename T, int DP, int QB, bool WHOLE>
 static int attn_dq_pass(AttnArgs& g, hipStream_t s) {
     g.tiles = (int)cdiv((int64_t)g.T << g.lgp, 64 * QB);
-    if (run_kernel(k_attn_dq<T, DP, QB, WHOLE>, g, (int64_t)g.tiles * g.N * (g.H >> g.lgp), 1,
+    if (run_kernel(k_attn_dq<T, DP, QB, WHOLE>, g, (int64_t)g.tiles * g.N * (g.H >> g.lgp), g.cut_q.chunks,
                    DqLds<T, DP, QB>::BINS + (g.part ? g.B * DqLds<T, DP, QB>::LANES * 16 : 0), s))
         return 1;
+    if (g.cut_q.chunks > 1) k_attn_dq_join<T, DP><<<dim3((uint32_t)cdiv((int64_t)g.N * g.H * g.T * (DP / 4), 256)), 256, 0, s>>>(g, 64 * QB);
     if (g.part) k_attn_dbias<<<dim3((uint32_t)(g.H * g.B)), 256, 0, s>>>(g);
     return 0;
 }
 template <typename T, int DP, int KB, bool WHOLE>
 static int attn_dkv_pass(AttnArgs& g, hipStream_t s) {
     g.tiles = (int)cdiv(g.S, 64 * KB);
-    if (run_kernel(k_attn_dkv<T, DP, KB, WHOLE>, g, (int64_t)g.tiles * g.N * g.KV, g.chunks, DkvLds<T, DP, KB>::TOTAL, s)) return 1;
-    if (g.chunks > 1) k_attn_dkv_join<T, DP><<<dim3((uint32_t)cdiv((int64_t)g.S * g.N * g.KV * (DP / 4), 256)), 256, 0, s>>>(g, 64 * KB);
+    if (run_kernel(k_attn_dkv<T, DP, KB, WHOLE>, g, (int64_t)g.tiles * g.N * g.KV, g.cut.chunks, DkvLds<T, DP, KB>::TOTAL, s)) return 1;
+    if (g.cut.chunks > 1) k_attn_dkv_join<T, DP><<<dim3((uint32_t)cdiv((int64_t)g.S * g.N * g.KV * (DP / 4), 256)), 256, 0, s>>>(g, 64 * KB);
     return 0;
 }
 // A wave takes one block of 16 rows; in the forward pass of long bf16 heads two where there are rows for them, as what is read of a tile then serves

@@ -182,11 +182,12 @@ def test_values_and_gradients(kind, shape):
 
 # walks of so many tiles, by so few workgroups, that they are cut into chunks whose parts are joined
 LONG = [
-    (1100, 1100, 1, 2, 1, 40, 17, 1100, 0.002),   # forward in two chunks, keys in four; chunks behind an episode's end
+    (1100, 1100, 1, 2, 1, 40, 17, 1100, 0.002),   # forward and queries in two chunks, keys in four; chunks behind an episode's end
     (1, 1200, 2, 4, 1, 64, 8, 1200, 0.0),
     (600, 600, 1, 4, 1, 128, 8, 600, 0.01),       # keys only
     (130, 1300, 2, 2, 2, 33, 0, 1025, 0.0),       # forward only, no bias, rows that are no whole pieces
     (1030, 1031, 1, 1, 1, 8, 3, 1000, 0.3),       # most chunks see nothing
+    (1100, 1150, 1, 1, 1, 64, 40, 1150, 0.0),     # a chunk's end among the distances that have buckets of their own
 ]
 
 
