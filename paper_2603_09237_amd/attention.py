@@ -48,7 +48,7 @@ class Cache:
 class AttentionBlock(Block):
     """Parameters are in `p`, gradients after `backward` in `g` under the same names (the projections' matrices and factors in the block's type,
     everything else and all gradients fp32).  Acting has buffers of its own: it may run on one stream while segments and their gradients run
-    on another.  What a call that is captured in a graph uses stays for as long as the block, also when later calls of other sizes take others."""
+    on another (two calls of a kind, or two graphs that hold them, may not run at once).  What a call that is captured in a graph uses stays for as long as the block, also when later calls of other sizes take others."""
 
     def __init__(self, preferences, width, heads, kv_heads=None, head_dim=64, buckets=32, window=256, rank=16, dtype=torch.bfloat16, device="cuda",
                  seed=0, eps=1e-6):
@@ -170,9 +170,11 @@ class AttentionBlock(Block):
         _check("h", h, (N, self.width), self.dtype)
         _check("index", index, (N,), torch.int32)
         _check_first(first, (N,))
-        if cache.N != N:
-            raise ValueError(f"the cache is one of {cache.N} environments, not {N}")
         q, c = self.p, cache
+        _check("the cache's length", c.length, (N,), torch.int32)
+        _check("the cache's table", c.table, (N, c.slots), torch.int32)
+        for t in (c.k, c.v):
+            _check("the cache's keys and values", t, (c.pages, c.page, self.KV, self.hd), self.dtype)
         proj, yc, u = self._buf("act.proj", N, self.L), self._buf("act.yc", N, self.D), self._buf("act.u", N, self.width)
         y, nxt = (torch.empty(N, self.width, dtype=self.dtype, device=self.dev) for _ in range(2))
         binding.cache_pages(c.dims, first, c.length, c.table, c.queue, c.state, c.length, c.table, c.queue, c.state, c.slot,
