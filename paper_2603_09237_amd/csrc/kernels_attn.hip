@@ -1206,7 +1206,7 @@ static int fwd_rows(const morlax_attn_dims& d) { return d.dtype && d.head_dim > 
 // Where the workgroups are no more than the chip holds at once, the time is that of the longest walk (earlier keys are seen by more rows, later rows see
 // more keys), and most of the chip is idle at its end: such walks are cut until there is work for the chip twice over, into no chunk of under eight
 // tiles, as each part is written and read again.  4099 steps of 2 x 4 fp32 heads of 32, forward (260 workgroups, 1024 places): 149 us in one piece,
-// 116 in four, 96 in seven; dk and dv of 2048 x 8 x 8 heads of 128 to 2 of keys (512 workgroups, 512 places): 519 in one piece, 382 in two, 433
+// 99 in seven (with today's sums of products 110); dk and dv of 2048 x 8 x 8 heads of 128 to 2 of keys (512 workgroups, 512 places): 519 in one piece, 382 in two, 433
 // in four.  The forward of the latter (1024 workgroups of twice the rows): 200 in one piece, 308 in four.
 // One environment's 4096 steps, 4 bf16 heads of 64 (256 workgroups): forward 105, dq 102, dk and dv 150 us in one piece; 66, 75 and 105 cut, with their
 // joins.
