@@ -50,7 +50,10 @@ struct AttnArgs {
     float scale;
     int T, S, N, H, KV, D, B, window, reach, lgp, tiles;
     int64_t q_t, q_n, k_t, k_n, y_t, y_n;
-    uint32_t total;
+    uint32_t total;   // workgroups of a chunk
+    uint32_t own;     // heads of an XCD where these are few, or 0
+    RowDiv by_total, by_tiles, by_own, by_heads;
+    int share;        // query heads to a head of keys
     Cut cut, cut_q;  // of the forward or of the backward's pass over the keys; of its pass over the queries
     int whole;  // rows hold whole pieces of 16 bytes
 };
@@ -267,15 +270,16 @@ struct Place {
     uint32_t rest;
     int tile, chunk;
     __device__ inline Place(const AttnArgs& g) {
-        chunk = blockIdx.x / g.total;
-        const uint32_t at = blockIdx.x - chunk * g.total, x = at & 7, i = at >> 3, rests = g.total / g.tiles, own = rests >> 3;
-        if (own <= 16 && own * 8 == rests) {
-            rest = x + 8 * (i % own);
-            tile = g.tiles - 1 - (int)(i / own);
+        chunk = (int)g.by_total.quotient(blockIdx.x);
+        const uint32_t at = blockIdx.x - chunk * g.total, x = at & 7, i = at >> 3;
+        if (g.own) {
+            const uint32_t row = g.by_own.quotient(i);
+            rest = x + 8 * (i - row * g.own);
+            tile = g.tiles - 1 - (int)row;
         } else {
             const uint32_t each = g.total >> 3, over = g.total & 7, w = x * each + (x < over ? x : over) + i;
-            rest = w / g.tiles;
-            tile = g.tiles - 1 - (int)(w % g.tiles);
+            rest = g.by_tiles.quotient(w);
+            tile = g.tiles - 1 - (int)(w - rest * g.tiles);
         }
     }
 };
@@ -285,10 +289,9 @@ struct Rows {
     int n, kv, h0, r0, rows, past, chunk;
     __device__ inline void init(const AttnArgs& g, int per) {
         const Place at(g);
-        const uint32_t packs = g.H >> g.lgp;
-        n = at.rest / packs;
-        h0 = (at.rest % packs) << g.lgp;
-        kv = h0 / (g.H / g.KV);
+        n = (int)g.by_heads.quotient(at.rest);
+        h0 = (int)(at.rest - n * (g.H >> g.lgp)) << g.lgp;
+        kv = h0 / g.share;
         r0 = at.tile * per;
         chunk = at.chunk;
         rows = g.T << g.lgp;
@@ -312,7 +315,7 @@ struct Table {
         for (int c = 0; c < NR; ++c) {
             int i = threadIdx.x + c * ATTN_THREADS;
             i = i < count ? i : count - 1;
-            const int hh = i / each;
+            const int hh = (i >= each) + (i >= 2 * each) + (i >= 3 * each);
             int d = far + dir * (i - hh * each);
             d = d < 0 ? 0 : d >= g.reach ? g.reach - 1 : d;
             v[c] = g.table[(int64_t)(h0 + hh) * g.reach + d];
@@ -341,8 +344,10 @@ struct FwdLds {
     static constexpr int ROOM = ATTN_ROOM(64 * QB, ATTN_K), NR = (ROOM + ATTN_THREADS - 1) / ATTN_THREADS;
     static constexpr int K = 0, V = Tile<T, DP>::BYTES, TAB = 2 * V, FLAG = TAB + ROOM * 4, TOTAL = FLAG + 16;
 };
-template <typename T, int DP, int QB, bool WHOLE, bool FINE>
-__global__ __launch_bounds__(ATTN_THREADS, attn_waves(0, sizeof(T), DP)) void k_attn_fwd(AttnArgs g) {
+template <typename T, int DP, int QB, bool WHOLE, bool FINE, int LGP>
+__global__ __launch_bounds__(ATTN_THREADS, attn_waves(0, sizeof(T), DP)) void k_attn_fwd(AttnArgs given) {
+    AttnArgs g = given;
+    g.lgp = LGP;
     typedef Tile<T, DP> L;
     typedef FwdLds<T, DP, QB> M;
     extern __shared__ __align__(16) unsigned char lds[];
@@ -649,8 +654,10 @@ struct DqLds {
     static constexpr int K = 0, V = Tile<T, DP>::BYTES, TAB = 2 * V, IDX = TAB + ROOM * 4, FLAG = IDX + (64 * QB + ATTN_K) * 4, BINS = FLAG + 16;
     static constexpr int LANES = BINS > 48 * 1024 ? 32 : 64;  // bins of a bucket and wave: beside the largest tiles fewer have to do
 };
-template <typename T, int DP, int QB, bool WHOLE>
-__global__ __launch_bounds__(ATTN_THREADS, attn_waves(1, sizeof(T), DP)) void k_attn_dq(AttnArgs g) {
+template <typename T, int DP, int QB, bool WHOLE, int LGP>
+__global__ __launch_bounds__(ATTN_THREADS, attn_waves(1, sizeof(T), DP)) void k_attn_dq(AttnArgs given) {
+    AttnArgs g = given;
+    g.lgp = LGP;
     typedef Tile<T, DP> L;
     typedef DqLds<T, DP, QB> M;
     extern __shared__ __align__(16) unsigned char lds[];
@@ -939,8 +946,10 @@ struct DkvLds {
     static constexpr int ROOM = ATTN_ROOM(ATTN_K, 64 * KB), NR = (ROOM + ATTN_THREADS - 1) / ATTN_THREADS;
     static constexpr int Q = 0, O = Tile<T, DP>::BYTES, TAB = 2 * O, INFO = TAB + ROOM * 4, FLAG = INFO + 3 * ATTN_K * 4, TOTAL = FLAG + 16;
 };
-template <typename T, int DP, int KB, bool WHOLE>
-__global__ __launch_bounds__(ATTN_THREADS, attn_waves(2, sizeof(T), DP)) void k_attn_dkv(AttnArgs g) {
+template <typename T, int DP, int KB, bool WHOLE, int LGP>
+__global__ __launch_bounds__(ATTN_THREADS, attn_waves(2, sizeof(T), DP)) void k_attn_dkv(AttnArgs given) {
+    AttnArgs g = given;
+    g.lgp = LGP;
     typedef Tile<T, DP> L;
     typedef DkvLds<T, DP, KB> M;
     extern __shared__ __align__(16) unsigned char lds[];
@@ -953,8 +962,8 @@ __global__ __launch_bounds__(ATTN_THREADS, attn_waves(2, sizeof(T), DP)) void k_
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, a = lane & 15, gr = lane >> 4;
     const Place at(g);
     Rows R;
-    R.n = at.rest / g.KV;
-    R.kv = at.rest % g.KV;
+    R.n = (int)g.by_heads.quotient(at.rest);
+    R.kv = (int)(at.rest - R.n * g.KV);
     R.past = g.S - g.T;
     const int k0 = (g.tiles - 1 - at.tile) * BK, k_last = (k0 + BK < g.S ? k0 + BK : g.S) - 1;
     Operand<T> kf[KB][L::KS], vf[KB][L::KS];
@@ -980,7 +989,7 @@ __global__ __launch_bounds__(ATTN_THREADS, attn_waves(2, sizeof(T), DP)) void k_
     if (threadIdx.x == 0) *flag = 0;
     if (!g.table)
         for (int i = threadIdx.x; i < M::ROOM; i += ATTN_THREADS) tab[i] = 0.f;
-    const int pack = 1 << g.lgp, share = g.H / g.KV, each = (ATTN_K >> g.lgp) + BK;
+    const int pack = 1 << g.lgp, share = g.share, each = (ATTN_K >> g.lgp) + BK;
     const int last_edge = g.table ? g.edges[g.B - 1] : 0;
     const float c = g.scale * kLog2e;
     const int t_begin = k0 > R.past ? k0 - R.past : 0;
@@ -1233,6 +1242,7 @@ static AttnArgs attn_args(const morlax_attn_dims& d) {
     g.scale = d.scale;
     g.whole = d.head_dim % (d.dtype ? 8 : 4) == 0;
     g.lgp = pack_bits(d);
+    g.share = d.heads / d.kv_heads;
     g.q_t = d.q_t; g.q_n = d.q_n; g.k_t = d.k_t; g.k_n = d.k_n; g.y_t = d.y_t; g.y_n = d.y_n;
     return g;
 }
@@ -1290,43 +1300,53 @@ int64_t attn_ws_bytes(const morlax_attn_dims& d, bool back) {
 static int run_kernel(void (*kernel)(AttnArgs), AttnArgs& g, int64_t total, int chunks, int lds, hipStream_t s) {
     if (hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess) return 1;
     g.total = (uint32_t)total;
+    const uint32_t rests = g.total / g.tiles;
+    g.own = rests % 8 == 0 && rests <= 128 ? rests / 8 : 0;
+    g.by_total = row_div((int)g.total);
+    g.by_tiles = row_div(g.tiles);
+    g.by_own = row_div(g.own ? (int)g.own : 1);
+    g.by_heads = row_div((int)(rests / g.N));
     kernel<<<dim3((uint32_t)(total * chunks)), ATTN_THREADS, lds, s>>>(g);
     return 0;
 }
-template <typename T, int DP, int QB, bool WHOLE, bool FINE = false>
+template <typename T, int DP, int QB, bool WHOLE, int LGP, bool FINE = false>
 static int attn_fwd_pass(AttnArgs& g, hipStream_t s) {
     if constexpr (!FINE && sizeof(T) == 2) {
-        if (g.low) return attn_fwd_pass<T, DP, QB, WHOLE, true>(g, s);
+        if (g.low) return attn_fwd_pass<T, DP, QB, WHOLE, LGP, true>(g, s);
     }
     g.tiles = (int)cdiv((int64_t)g.T << g.lgp, 64 * QB);
-    if (run_kernel(k_attn_fwd<T, DP, QB, WHOLE, FINE>, g, (int64_t)g.tiles * g.N * (g.H >> g.lgp), g.cut.chunks, FwdLds<T, DP, QB>::TOTAL, s)) return 1;
+    if (run_kernel(k_attn_fwd<T, DP, QB, WHOLE, FINE, LGP>, g, (int64_t)g.tiles * g.N * (g.H >> g.lgp), g.cut.chunks, FwdLds<T, DP, QB>::TOTAL, s)) return 1;
     if (g.cut.chunks > 1) k_attn_fwd_join<T, DP><<<dim3((uint32_t)cdiv((int64_t)g.N * g.H * g.T * (DP / 4), 256)), 256, 0, s>>>(g);
     return 0;
 }
-template <typename T, int DP, int QB, bool WHOLE>
+template <typename T, int DP, int QB, bool WHOLE, int LGP>
 static int attn_dq_pass(AttnArgs& g, hipStream_t s) {
     g.tiles = (int)cdiv((int64_t)g.T << g.lgp, 64 * QB);
-    if (run_kernel(k_attn_dq<T, DP, QB, WHOLE>, g, (int64_t)g.tiles * g.N * (g.H >> g.lgp), g.cut_q.chunks,
+    if (run_kernel(k_attn_dq<T, DP, QB, WHOLE, LGP>, g, (int64_t)g.tiles * g.N * (g.H >> g.lgp), g.cut_q.chunks,
                    DqLds<T, DP, QB>::BINS + (g.part ? g.B * DqLds<T, DP, QB>::LANES * 16 : 0), s))
         return 1;
     if (g.cut_q.chunks > 1) k_attn_dq_join<T, DP><<<dim3((uint32_t)cdiv((int64_t)g.N * g.H * g.T * (DP / 4), 256)), 256, 0, s>>>(g, 64 * QB);
     if (g.part) k_attn_dbias<<<dim3((uint32_t)(g.H * g.B)), 256, 0, s>>>(g);
     return 0;
 }
-template <typename T, int DP, int KB, bool WHOLE>
+template <typename T, int DP, int KB, bool WHOLE, int LGP>
 static int attn_dkv_pass(AttnArgs& g, hipStream_t s) {
     g.tiles = (int)cdiv(g.S, 64 * KB);
-    if (run_kernel(k_attn_dkv<T, DP, KB, WHOLE>, g, (int64_t)g.tiles * g.N * g.KV, g.cut.chunks, DkvLds<T, DP, KB>::TOTAL, s)) return 1;
+    if (run_kernel(k_attn_dkv<T, DP, KB, WHOLE, LGP>, g, (int64_t)g.tiles * g.N * g.KV, g.cut.chunks, DkvLds<T, DP, KB>::TOTAL, s)) return 1;
     if (g.cut.chunks > 1) k_attn_dkv_join<T, DP><<<dim3((uint32_t)cdiv((int64_t)g.S * g.N * g.KV * (DP / 4), 256)), 256, 0, s>>>(g, 64 * KB);
     return 0;
 }
 // A wave takes one block of 16 rows; in the forward pass of long bf16 heads two where there are rows for them, as what is read of a tile then serves
 // both (2048 x 8 x 8 heads of 128: 167 us, one block 186; heads of 64, 64 steps: 90, one block 75; the backward kernels run out of registers).
+template <typename T, int DP, bool WHOLE, int LGP>
+static int attn_packed(AttnArgs& g, bool back, hipStream_t s) {
+    constexpr int MORE = sizeof(T) == 2 && DP == 128 ? 2 : 1;  // (fwd_rows says the same)
+    if (!back) return ((int64_t)g.T << LGP) > 64 ? attn_fwd_pass<T, DP, MORE, WHOLE, LGP>(g, s) : attn_fwd_pass<T, DP, 1, WHOLE, LGP>(g, s);
+    return attn_dq_pass<T, DP, 1, WHOLE, LGP>(g, s) || attn_dkv_pass<T, DP, 1, WHOLE, LGP>(g, s);
+}
 template <typename T, int DP, bool WHOLE>
 static int attn_whole(AttnArgs& g, bool back, hipStream_t s) {
-    constexpr int MORE = sizeof(T) == 2 && DP == 128 ? 2 : 1;  // (fwd_rows says the same)
-    if (!back) return ((int64_t)g.T << g.lgp) > 64 ? attn_fwd_pass<T, DP, MORE, WHOLE>(g, s) : attn_fwd_pass<T, DP, 1, WHOLE>(g, s);
-    return attn_dq_pass<T, DP, 1, WHOLE>(g, s) || attn_dkv_pass<T, DP, 1, WHOLE>(g, s);
+    return g.lgp == 0 ? attn_packed<T, DP, WHOLE, 0>(g, back, s) : g.lgp == 1 ? attn_packed<T, DP, WHOLE, 1>(g, back, s) : attn_packed<T, DP, WHOLE, 2>(g, back, s);
 }
 template <typename T, int DP>
 static int attn_rows(AttnArgs& g, bool back, hipStream_t s) {
