@@ -222,6 +222,8 @@ __device__ inline void fold(const unsigned char* lds, int u, const float4_t (&p)
     phase();
 }
 
+// Rows of results go out as what no workgroup here reads again, and leave the L2 to the tiles that others share (512 environments, 64 of 128 steps, 8
+// heads of 64: dk and dv 131 -> 117 us, the passes over the queries 5% less; requests of what is read once marked so too: 10% more).
 template <typename T, int DP, bool WHOLE, typename F>
 __device__ inline void send_rows(const unsigned char* lds, int D, F to) {
     typedef Tile<T, DP> L;
@@ -233,7 +235,7 @@ __device__ inline void send_rows(const unsigned char* lds, int D, F to) {
         const uint4 u = *reinterpret_cast<const uint4*>(lds + row * L::OPITCH + col * L::ES);
         if (!dst) continue;
         if (WHOLE ? col < D : col + L::VE <= D) {
-            *reinterpret_cast<piece_t*>(dst + col) = piece_t{u.x, u.y, u.z, u.w};
+            __builtin_nontemporal_store(piece_t{u.x, u.y, u.z, u.w}, reinterpret_cast<piece_t*>(dst + col));
         } else if (!WHOLE) {
             const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
