@@ -995,15 +995,33 @@ __global__ __launch_bounds__(ATTN_THREADS, attn_waves(2, sizeof(T), DP)) void k_
     const int last_edge = g.table ? g.edges[g.B - 1] : 0;
     const float c = g.scale * kLog2e;
     const int t_begin = k0 > R.past ? k0 - R.past : 0;
-    // the last step that may see a key here; episodes end the walk earlier
+    // The steps that may see a key here end where the window or an episode does (lo never falls).  The walk is one from its end: workgroups of one
+    // environment then meet at the same rows at the same time, which the L2 holds (2048 x 8 x 8 heads of 128 to 2 of keys: 1.6 million requests miss it,
+    // from each one's own first row on 5.9 million; 3% of the time).
     const int64_t t_far = (int64_t)k_last + g.window - R.past;
-    const int t_end = t_far < g.T ? (int)t_far : g.T, r_first = (t_begin << g.lgp) & ~3, r_last = t_end << g.lgp;
-    int r_begin = r_first, r_end = r_last;
-    if (g.cut.chunks > 1) {
-        r_begin += at.chunk * g.cut.span * ATTN_K;
-        const int64_t end = (int64_t)r_begin + g.cut.span * ATTN_K;
-        r_end = end < r_last ? (int)end : r_last;
+    int t_end = t_far < g.T ? (int)t_far : g.T;
+    if (g.lo && (t_end - t_begin) << g.lgp > 4 * ATTN_K) {
+        int from = t_begin;
+        while (from < t_end) {
+            const int stride = (t_end - from + 63) / 64, t = from + lane * stride;
+            const uint64_t over = __ballot(t >= t_end || R.lo(g, R.past + (t < t_end ? t : t_end - 1)) > k_last);
+            const int one = over ? __ffsll((long long)over) - 1 : 64;
+            if (one == 0) {
+                t_end = from;
+            } else {
+                const int upto = from + one * stride;
+                t_end = upto < t_end ? upto : t_end;
+                from += (one - 1) * stride + 1;
+            }
+        }
     }
+    int r_begin = (t_begin << g.lgp) & ~3, r_end = t_end << g.lgp;
+    if (g.cut.chunks > 1) {
+        const int tiles = r_end > r_begin ? (r_end - r_begin + ATTN_K - 1) / ATTN_K : 0, upto = tiles - at.chunk * g.cut.span, from = upto - g.cut.span;
+        r_end = at.chunk == 0 ? r_end : r_begin + (upto > 0 ? upto : 0) * ATTN_K;
+        r_begin += (from > 0 ? from : 0) * ATTN_K;
+    }
+    const int r_last = r_begin < r_end ? r_begin + (r_end - 1 - r_begin) / ATTN_K * ATTN_K : r_begin - ATTN_K;  // where the last tile of rows begins
     bool some = false;  // (of a chunk: has a row been looked at)
     for (int h0 = R.kv * share; h0 < (R.kv + 1) * share; h0 += pack) {
         const T* qb = reinterpret_cast<const T*>(g.q) + (int64_t)R.n * g.q_n + (int64_t)h0 * g.D;
@@ -1034,9 +1052,9 @@ __global__ __launch_bounds__(ATTN_THREADS, attn_waves(2, sizeof(T), DP)) void k_
                 }
             }
         };
-        if (r_begin < r_end) request(r_begin);
+        if (r_begin < r_end) request(r_last);
         __syncthreads();
-        for (int r0 = r_begin; r0 < r_end; r0 += ATTN_K) {
+        for (int r0 = r_last; r0 >= r_begin; r0 -= ATTN_K) {
             const bool near = near_at(r0);
             const bool mq = sq.template put<true>(lds + M::Q, r0, r_end, g.D), mo = so.template put<true>(lds + M::O, r0, r_end, g.D);
             if (mq | mo) *flag = 1;
@@ -1047,9 +1065,9 @@ __global__ __launch_bounds__(ATTN_THREADS, attn_waves(2, sizeof(T), DP)) void k_
                 row_lo[threadIdx.x] = i_lo;
             }
             __syncthreads();
-            if (row_lo[0] > k_last) break;  // (lo never falls: no later row sees a key here)
-            some = true;
-            if (r0 + ATTN_K < r_end) request(r0 + ATTN_K);
+            if (r0 > r_begin) request(r0 - ATTN_K);
+            const bool seen = row_lo[0] <= k_last;  // (of a short walk: an episode may end it earlier)
+            some |= seen;
             const int p0 = R.past + (r0 >> g.lgp);
             auto tile = [&](auto fast) {
                 constexpr bool FAST = decltype(fast)::value;
@@ -1105,11 +1123,12 @@ __global__ __launch_bounds__(ATTN_THREADS, attn_waves(2, sizeof(T), DP)) void k_
                     fold<T, DP, KB>(lds + M::Q, u, s, dk, now);
                 }
             };
-            if (!near && row_lo[ATTN_K - 1] <= k0 && p0 >= k0 + BK - 1) tile(std::true_type{});
-            else tile(std::false_type{});
+            if (seen) {
+                if (!near && row_lo[ATTN_K - 1] <= k0 && p0 >= k0 + BK - 1) tile(std::true_type{});
+                else tile(std::false_type{});
+            }
             __syncthreads();
         }
-        __syncthreads();  // (a walk that ended early has not waited yet)
         if (*flag) {  // an undefined q: undefined probabilities; an undefined dy: undefined dA, and itself in dv
             for (int r = r_begin; r < r_end; ++r) {
                 const int tt = r >> g.lgp, p = R.past + tt, lo = R.lo(g, p);
