@@ -59,6 +59,8 @@ struct AttnArgs {
 };
 
 // ---- episodes and the bias by distance --------------------------------------------------------------------------------
+// A launch ahead of the others, which are bound by what they read once per tile of theirs, not once per pair.  Bound by latency: 5 us, 14 for 8 environments of
+// 2048 steps (each a few threads' walk over its flags).
 // Blocks below `spans`: 2^lgn environments at a time, the threads of an environment taking a run of steps each; the others: the table.
 __global__ __launch_bounds__(1024) void k_attn_prepare(AttnArgs g, int spans, int lgn) {
     __shared__ int last[1024];
@@ -341,6 +343,9 @@ struct Table {
 };
 
 // ---- forward ------------------------------------------------------------------------------------------------------------
+// Four waves, 16 rows each (32: see below), and a tile of 64 keys at a time, the next one's requests on their way.  Bound by instructions, and by what is
+// read and written where there are few keys to a row: 1024 environments, 64 of 128 steps, 8 heads of 64 to 2 of keys 72 us (201 MB; 2.8 TB/s);
+// for training 512 of them, 8 heads of keys 48 us (235 MB, 4.9 TB/s); 2048 x 8 x 8 heads of 128 190 us (137 GF of parts, 0.7 PFLOP/s).
 template <typename T, int DP, int QB>
 struct FwdLds {
     static constexpr int ROOM = ATTN_ROOM(64 * QB, ATTN_K), NR = (ROOM + ATTN_THREADS - 1) / ATTN_THREADS;
@@ -650,6 +655,8 @@ __device__ inline void add_to_bins(float* bins, const int* idx, int at, int end,
 }
 
 // ---- backward, queries: dq, the sums of dA by bucket, and delta ---------------------------------------------------------------
+// As the forward, with dP beside the scores.  512 environments, 64 of 128 steps, 8 heads of 64: 73 us (302 MB, 4.1 TB/s); 2048 x 8 x 8 heads of 128
+// to 2 of keys: 230 us (0.6 PFLOP/s of parts): instructions, the matrix ones a third of the time.
 template <typename T, int DP, int QB>
 struct DqLds {
     static constexpr int ROOM = ATTN_ROOM(64 * QB, ATTN_K), NR = (ROOM + ATTN_THREADS - 1) / ATTN_THREADS;
@@ -943,6 +950,9 @@ __global__ __launch_bounds__(256) void k_attn_dbias(AttnArgs g) {
 }
 
 // ---- backward, keys: dk and dv ---------------------------------------------------------------------------------------------------
+// Four waves, 16 keys each in registers, and a tile of 64 rows of queries at a time.  512 environments, 64 of 128 steps, 8 heads of 64: 110 us (330 MB,
+// 3.0 TB/s: one tile to a workgroup, most of its time is the wait for it; workgroups that go on to a next tile and ask for it ahead 133, three waves
+// a SIMD 140); 2048 x 8 x 8 heads of 128 to 2 of keys: 345 us (206 GF of parts, 0.6 PFLOP/s): two waves a SIMD, half of the time in waits.
 template <typename T, int DP, int KB>
 struct DkvLds {
     static constexpr int ROOM = ATTN_ROOM(ATTN_K, 64 * KB), NR = (ROOM + ATTN_THREADS - 1) / ATTN_THREADS;
@@ -1358,7 +1368,7 @@ static int attn_dkv_pass(AttnArgs& g, hipStream_t s) {
     return 0;
 }
 // A wave takes one block of 16 rows; in the forward pass of long bf16 heads two where there are rows for them, as what is read of a tile then serves
-// both (2048 x 8 x 8 heads of 128: 167 us, one block 186; heads of 64, 64 steps: 90, one block 75; the backward kernels run out of registers).
+// both (2048 x 8 x 8 heads of 128: 167 us, one block 186; heads of 64, 64 steps: 77, one block 72; the backward kernels run out of registers).
 template <typename T, int DP, bool WHOLE, int LGP>
 static int attn_packed(AttnArgs& g, bool back, hipStream_t s) {
     constexpr int MORE = sizeof(T) == 2 && DP == 128 ? 2 : 1;  // (fwd_rows says the same)

@@ -203,9 +203,10 @@ __global__ __launch_bounds__(PAGES_THREADS) void k_pages_apply(PagesArgs g) {
 }
 
 // ---- one new step over the cache ------------------------------------------------------------------------------------------------
-// Bound: HBM, every key and value of the window once (GQ query heads share what is read).  A key lies along LPK lanes, 16 bytes each, so a
-// wave takes 64 / LPK keys at a time; every group of LPK lanes carries a running maximum, sum and output of its own, which are joined once at
-// the end, across the groups, the waves and, where few environments have to fill the chip, the workgroups that share a cache's length.
+// Bound: HBM, every key and value of the window once (the query heads that share a head of keys share what is read), split over the length and joined
+// where few environments have to fill the chip.  fp32: a key lies along LPK lanes, 16 bytes each, so a wave takes 64 / LPK keys at a time; every group
+// of LPK lanes carries a running maximum, sum and output of its own, which are joined once at the end, across the groups, the waves and the
+// workgroups of a length (33 environments, 384 steps, 6 heads of 40: 9 us and 3.5 for the join, latency of dependent loads: length, table, key).
 struct StepArgs {
     const void *q, *k, *v;
     const float* bias;
@@ -218,12 +219,7 @@ struct StepArgs {
     int64_t q_n, k_n, y_n;
 };
 
-template <typename T>
-__device__ inline float element(const uint4& u, int i) {  // i known after unrolling
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
-    else return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
-}
+__device__ inline float element(const uint4& u, int i) { return __uint_as_float(i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w); }  // i known after unrolling
 
 #define STEP_U 4  // keys that a group of lanes requests together
 
@@ -240,9 +236,10 @@ __device__ inline float group_sum(float v) {
     return v;
 }
 
-template <typename T, int DP, int GQ, bool WHOLE>
+template <int DP, int GQ, bool WHOLE>
 __global__ __launch_bounds__(256) void k_attn_step(StepArgs g) {
-    constexpr int VE = 16 / sizeof(T), LPK = DP / VE, KPW = 64 / LPK, STRIDE = 4 * KPW * STEP_U;
+    typedef float T;
+    constexpr int VE = 4, LPK = DP / VE, KPW = 64 / LPK, STRIDE = 4 * KPW * STEP_U;
     __shared__ float bias[GQ][64];
     __shared__ int32_t edges[64];  // those that are not there: no distance reaches them
     __shared__ float2 wave_m[4][GQ];
@@ -289,7 +286,7 @@ __global__ __launch_bounds__(256) void k_attn_step(StepArgs g) {
         in.load(reinterpret_cast<const T*>(g.q) + (int64_t)n * g.q_n + (int64_t)(h0 + (i < heads ? i : 0)) * g.D, d, g.D);
         const uint4 u = in.get(d, g.D);
 #pragma unroll
-        for (int e = 0; e < VE; ++e) qf[i][e] = element<T>(u, e);
+        for (int e = 0; e < VE; ++e) qf[i][e] = element(u, e);
     }
     int last_edge = 0;
     if (g.B) {
@@ -339,7 +336,7 @@ __global__ __launch_bounds__(256) void k_attn_step(StepArgs g) {
             const uint4 ku = kp[u].get(d, g.D, in[u]);
 #pragma unroll
             for (int e = 0; e < VE; ++e) {
-                const float x = element<T>(ku, e);
+                const float x = element(ku, e);
 #pragma unroll
                 for (int i = 0; i < GQ; ++i) s[u][i] = __builtin_fmaf(x, qf[i][e], s[u][i]);
             }
@@ -379,7 +376,7 @@ __global__ __launch_bounds__(256) void k_attn_step(StepArgs g) {
             const uint4 vu = vp[u].get(d, g.D, in[u]);
 #pragma unroll
             for (int e = 0; e < VE; ++e) {
-                const float x = element<T>(vu, e);
+                const float x = element(vu, e);
 #pragma unroll
                 for (int i = 0; i < GQ; ++i) o[i][e] = __builtin_fmaf(s[u][i], x, o[i][e]);
             }
@@ -435,7 +432,7 @@ __global__ __launch_bounds__(256) void k_attn_step(StepArgs g) {
 // ---- one new step over the cache, bf16: on the matrix instructions ------------------------------------------------------------------
 // Up to sixteen query heads that share a head of keys are the columns of a product's result, 32 keys its rows: the arithmetic of a key is then a
 // few instructions of a wave whatever the number of heads (one lane's products and sums for every head: a step of 1024 environments, four heads to a
-// head of keys, 82 us, bound by them).  A lane's two rows of keys and values come straight from the cache; values go through LDS, which turns them.
+// head of keys, 82 us, bound by them; so 58, 4.7 TB/s; one environment of 8192 steps 6.4 and 4.4 for the join, latency).  A lane's two rows of keys and values come straight from the cache; values go through LDS, which turns them.
 template <int DP>
 struct StepLds {
     typedef Tile<bf16_t, DP> L;
@@ -733,10 +730,10 @@ static void step_pass(const StepArgs& g, hipStream_t s) {
     const dim3 grid((uint32_t)((int64_t)g.splits * g.chunks * g.KV * g.N));
     if constexpr (sizeof(T) == 2) k_attn_step_bf16<DP, WHOLE><<<grid, 256, 0, s>>>(g);
     else switch (heads_of_workgroup(g.H / g.KV)) {
-        case 1: k_attn_step<T, DP, 1, WHOLE><<<grid, 256, 0, s>>>(g); break;
-        case 2: k_attn_step<T, DP, 2, WHOLE><<<grid, 256, 0, s>>>(g); break;
-        case 4: k_attn_step<T, DP, 4, WHOLE><<<grid, 256, 0, s>>>(g); break;
-        default: k_attn_step<T, DP, 8, WHOLE><<<grid, 256, 0, s>>>(g);
+        case 1: k_attn_step<DP, 1, WHOLE><<<grid, 256, 0, s>>>(g); break;
+        case 2: k_attn_step<DP, 2, WHOLE><<<grid, 256, 0, s>>>(g); break;
+        case 4: k_attn_step<DP, 4, WHOLE><<<grid, 256, 0, s>>>(g); break;
+        default: k_attn_step<DP, 8, WHOLE><<<grid, 256, 0, s>>>(g);
     }
     if (g.splits > 1) k_attn_join<T><<<dim3((uint32_t)((int64_t)g.N * g.H)), 256, 0, s>>>(g);
 }
