@@ -402,7 +402,7 @@ int morlax_attn_bwd(const morlax_attn_dims* dims, const void* q, const void* k, 
  * A table entry outside [0, pages) is none.  queue [pages] is a ring of free pages, state = {where it begins, how many there are}.
  * length_in, length, slot [N], table_in, table [N, slots], queue_in, queue [pages], state_in, state [2], all int32.  Each output but slot may be its
  * own input.  Lengths must stay below 2^31 - 1.
- * Limits: page a power of two up to 4096, pages * page < 2^31, N * slots < 2^31, N <= 2^24. */
+ * Limits: page a power of two up to 4096, pages * page < 2^31, N * slots <= 2^30, N <= 2^24. */
 typedef struct {
     int32_t N, page, slots, pages;
 } morlax_pages_dims;

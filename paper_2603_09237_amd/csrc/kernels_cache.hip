@@ -257,7 +257,7 @@ __global__ __launch_bounds__(256) void k_attn_step(StepArgs g) {
     }
     const int begin = pos - g.window + 1 > 0 ? pos - g.window + 1 : 0;
     // this workgroup's part of the window, a whole number of keys of its waves
-    const int count = pos - begin + 1, per = ((count + g.splits - 1) / g.splits + 4 * KPW - 1) / (4 * KPW) * (4 * KPW);
+    const uint32_t count = pos - begin + 1, per = ((count + g.splits - 1) / g.splits + 4 * KPW - 1) / (4 * KPW) * (4 * KPW);  // (sums pass 2^31)
     const int64_t s0 = begin + (int64_t)split * per;
     const int s1 = s0 + per < pos + 1 ? (int)(s0 + per) : pos + 1;
     const int32_t* table = g.table + (int64_t)n * g.slots;
@@ -458,7 +458,7 @@ __global__ __launch_bounds__(256, DP == 128 ? 2 : 3) void k_attn_step_bf16(StepA
         return;
     }
     const int begin = pos - g.window + 1 > 0 ? pos - g.window + 1 : 0;
-    const int count = pos - begin + 1, per = ((count + g.splits - 1) / g.splits + 127) / 128 * 128;  // a whole number of keys of the four waves
+    const uint32_t count = pos - begin + 1, per = ((count + g.splits - 1) / g.splits + 127) / 128 * 128;  // a whole number of keys of the four waves
     const int64_t s0 = begin + (int64_t)split * per;
     const int s1 = s0 + per < pos + 1 ? (int)(s0 + per) : pos + 1;
     const int32_t* table = g.table + (int64_t)n * g.slots;

@@ -781,8 +781,8 @@ extern "C" int morlax_attn_bwd(const morlax_attn_dims* dims, const void* q, cons
 static int check_page(int page, int slots, int pages, int64_t N, const char* who) {
     if (N < 1 || page < 1 || slots < 1 || pages < 1) return fail(MORLAX_ERR_SHAPE, "%s: N, page, slots and pages must be >= 1", who);
     if ((page & (page - 1)) != 0 || page > 4096) return fail(MORLAX_ERR_UNSUPPORTED, "%s: page must be a power of two up to 4096 (got %d)", who, page);
-    if ((int64_t)pages * page >= (int64_t)1 << 31 || N * slots >= (int64_t)1 << 31 || N > 1 << 24)
-        return fail(MORLAX_ERR_UNSUPPORTED, "%s: pages * page and N * slots must stay below 2^31, N <= 2^24", who);
+    if ((int64_t)pages * page >= (int64_t)1 << 31 || N * slots > (int64_t)1 << 30 || N > 1 << 24)
+        return fail(MORLAX_ERR_UNSUPPORTED, "%s: pages * page must stay below 2^31, N * slots <= 2^30, N <= 2^24", who);
     return MORLAX_OK;
 }
 static int check_pages(const morlax_pages_dims* d, const char* who) {

@@ -102,6 +102,7 @@ def pages(**over):
 
 @pytest.mark.parametrize("over,code", [(dict(N=0), SHAPE), (dict(page=0), SHAPE), (dict(slots=0), SHAPE), (dict(pages=0), SHAPE), (dict(page=3), UNSUPPORTED),
                                        (dict(page=8192), UNSUPPORTED), (dict(pages=1 << 29), UNSUPPORTED), (dict(N=1 << 20, slots=1 << 11), UNSUPPORTED),
+                                       (dict(N=1, slots=(1 << 30) + 1), UNSUPPORTED),
                                        (dict(N=(1 << 24) + 1), UNSUPPORTED)])
 def test_pages_dimensions(over, code):
     d, f = pages(**over), places("first", "length_in", "table_in", "queue_in", "state_in", "length", "table", "queue", "state", "slot")

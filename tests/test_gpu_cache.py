@@ -163,6 +163,34 @@ def check(c):
 
 
 @pytest.mark.parametrize("kind", ["float32", "bfloat16"])
+def test_step_of_the_longest_episode_and_window(kind):
+    """Counts whose rounding up passes 2^31: two pages of an episode of 2^31 - 2 steps are there, the newest and one from near its begin."""
+    from paper_2603_09237_amd import binding
+    torch = _torch()
+    dtype, H, D, B, page, slots, window, length = getattr(torch, kind), 2, 8, 3, 4096, 1 << 19, 2 ** 31 - 1, 2 ** 31 - 2
+    g = torch.Generator().manual_seed(11)
+    r = lambda *s: torch.randn(*s, generator=g).to(dtype)  # noqa: E731
+    table = torch.full((1, slots), -1, dtype=torch.int32)
+    pos = length - 1
+    table[0, pos // page % slots], table[0, 5] = 1, 0
+    c = dict(N=1, H=H, KV=1, D=D, pad=0, dtype=dtype, q=r(1, H, D), k=r(1, 1, D), v=r(1, 1, D), kc=r(2, page, 1, D), vc=r(2, page, 1, D),
+             bias=torch.randn(H, B, generator=g), edges=torch.tensor([0, 10, 5000], dtype=torch.int32), table=table,
+             length=torch.tensor([length], dtype=torch.int32), dims=binding.CacheDims(1, H, 1, D, B, window, page, slots, 2, int(kind == "bfloat16")))
+    here = pos % page
+    gaps = torch.cat([pos - (5 * page + torch.arange(page)), here - torch.arange(here + 1)])
+    ks, vs = (torch.cat([t[0], t[1, :here], n]).double()[:, 0] for t, n in ((c["kc"], c["k"]), (c["vc"], c["v"])))
+    a = c["q"][0].double() @ ks.T * D ** -0.5 + c["bias"].double()[:, (gaps[:, None] >= c["edges"][1:]).sum(-1)]
+    p = torch.softmax(a, -1)
+    y, size = p @ vs, p @ vs.abs()
+    bound = (2 * ((D + 4) * U * D ** -0.5 * float((c["q"][0].double().abs() @ ks.abs().T).max()) + 4 * U * float(a.abs().max())) + (2 * len(gaps) + 16) * U) * size
+    dev = launch(c)
+    half = 2.0 ** -8 if kind == "bfloat16" else U
+    err = (dev["y"].cpu().double().reshape(H, D) - y).abs()
+    assert bool((err <= bound + half * (y.abs() + bound) + 1e-30).all())
+    assert torch.equal(dev["kc"].cpu()[1, here], c["k"][0]) and torch.equal(dev["vc"].cpu()[1, here], c["v"][0])
+
+
+@pytest.mark.parametrize("kind", ["float32", "bfloat16"])
 @pytest.mark.parametrize("N,H,KV,D,B,window,page,lengths,pad", [
     (1, 1, 1, 1, 0, 1, 1, [1], 0), (1, 1, 1, 16, 3, 8, 4, [1], 0), (5, 2, 2, 8, 4, 9, 2, [0, 1, 9, 10, 400], 0),
     (4, 4, 1, 33, 6, 40, 8, [40, 41, 39, -5], 3), (3, 6, 2, 64, 32, 300, 16, [300, 1000, 17], 0), (2, 8, 1, 128, 0, 700, 64, [700, 699], 8),
