@@ -53,6 +53,8 @@ struct AttnArgs {
     uint32_t total;   // workgroups of a chunk
     uint32_t own;     // heads of an XCD where these are few, or 0
     RowDiv by_total, by_tiles, by_own, by_heads;
+    uint32_t before;  // workgroups of the launch that do something else
+    int64_t parts;    // of a sum of dbias
     int share;        // query heads to a head of keys
     Cut cut, cut_q;  // of the forward or of the backward's pass over the keys; of its pass over the queries
     int whole;  // rows hold whole pieces of 16 bytes
@@ -274,8 +276,9 @@ struct Place {
     uint32_t rest;
     int tile, chunk;
     __device__ inline Place(const AttnArgs& g) {
-        chunk = (int)g.by_total.quotient(blockIdx.x);
-        const uint32_t at = blockIdx.x - chunk * g.total, x = at & 7, i = at >> 3;
+        const uint32_t index = blockIdx.x - g.before;
+        chunk = (int)g.by_total.quotient(index);
+        const uint32_t at = index - chunk * g.total, x = at & 7, i = at >> 3;
         if (g.own) {
             const uint32_t row = g.by_own.quotient(i);
             rest = x + 8 * (i - row * g.own);
@@ -916,7 +919,7 @@ __global__ __launch_bounds__(ATTN_THREADS, attn_waves(1, sizeof(T), DP)) void k_
     }
     __syncthreads();
     // eight threads a bucket: each adds up an eighth of its lanes (of one head, in an order that touches no bank twice) of all four waves
-    const int64_t parts = (int64_t)g.N * g.tiles * g.cut_q.chunks, mine = ((int64_t)R.n * g.tiles + R.r0 / BQ) * g.cut_q.chunks + R.chunk;
+    const int64_t parts = g.parts, mine = ((int64_t)R.n * g.tiles + R.r0 / BQ) * g.cut_q.chunks + R.chunk;
     const int part = threadIdx.x & 7, head = part & ((1 << g.lgp) - 1), eighth = part >> g.lgp;
     for (int b0 = 0; b0 < g.B; b0 += 32) {
         const int b = b0 + (threadIdx.x >> 3);
@@ -935,13 +938,11 @@ __global__ __launch_bounds__(ATTN_THREADS, attn_waves(1, sizeof(T), DP)) void k_
     }
 }
 
-// dbias[h, b]: the workgroups' sums, one block each
-__global__ __launch_bounds__(256) void k_attn_dbias(AttnArgs g) {
-    __shared__ float part[4];
-    const int64_t parts = (int64_t)g.N * g.tiles * g.cut_q.chunks;
-    const float* src = g.part + (int64_t)blockIdx.x * parts;
+// dbias[h, b]: the workgroups' sums, a workgroup of the next launch each (of a launch of their own: 5 us)
+__device__ inline void add_bias(const AttnArgs& g, float* part) {
+    const float* src = g.part + (int64_t)blockIdx.x * g.parts;
     float sum = 0.f;
-    for (int64_t i = threadIdx.x; i < parts; i += 256) sum += src[i];
+    for (int64_t i = threadIdx.x; i < g.parts; i += ATTN_THREADS) sum += src[i];
 #pragma unroll
     for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
@@ -970,6 +971,7 @@ __global__ __launch_bounds__(ATTN_THREADS, attn_waves(2, sizeof(T), DP)) void k_
     float* row_delta = row_lse + ATTN_K;
     int* row_lo = reinterpret_cast<int*>(row_delta + ATTN_K);
     int* flag = reinterpret_cast<int*>(lds + M::FLAG);
+    if (blockIdx.x < g.before) return add_bias(g, reinterpret_cast<float*>(lds));
     constexpr int BK = 64 * KB;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, a = lane & 15, gr = lane >> 4;
     const Place at(g);
@@ -1337,7 +1339,7 @@ static int run_kernel(void (*kernel)(AttnArgs), AttnArgs& g, int64_t total, int 
     g.by_tiles = row_div(g.tiles);
     g.by_own = row_div(g.own ? (int)g.own : 1);
     g.by_heads = row_div((int)(rests / g.N));
-    kernel<<<dim3((uint32_t)(total * chunks)), ATTN_THREADS, lds, s>>>(g);
+    kernel<<<dim3((uint32_t)(g.before + total * chunks)), ATTN_THREADS, lds, s>>>(g);
     return 0;
 }
 template <typename T, int DP, int QB, bool WHOLE, int LGP, bool FINE = false>
@@ -1353,11 +1355,12 @@ static int attn_fwd_pass(AttnArgs& g, hipStream_t s) {
 template <typename T, int DP, int QB, bool WHOLE, int LGP>
 static int attn_dq_pass(AttnArgs& g, hipStream_t s) {
     g.tiles = (int)cdiv((int64_t)g.T << g.lgp, 64 * QB);
+    g.parts = (int64_t)g.N * g.tiles * g.cut_q.chunks;
     if (run_kernel(k_attn_dq<T, DP, QB, WHOLE, LGP>, g, (int64_t)g.tiles * g.N * (g.H >> g.lgp), g.cut_q.chunks,
                    DqLds<T, DP, QB>::BINS + (g.part ? g.B * DqLds<T, DP, QB>::LANES * 16 : 0), s))
         return 1;
     if (g.cut_q.chunks > 1) k_attn_dq_join<T, DP><<<dim3((uint32_t)cdiv((int64_t)g.N * g.H * g.T * (DP / 4), 256)), 256, 0, s>>>(g, 64 * QB);
-    if (g.part) k_attn_dbias<<<dim3((uint32_t)(g.H * g.B)), 256, 0, s>>>(g);
+    if (g.part) g.before = (uint32_t)(g.H * g.B);  // (of the next launch)
     return 0;
 }
 template <typename T, int DP, int KB, bool WHOLE, int LGP>
