@@ -61,8 +61,8 @@ struct AttnArgs {
 };
 
 // ---- episodes and the bias by distance --------------------------------------------------------------------------------
-// A launch ahead of the others, which are bound by what they read once per tile of theirs, not once per pair.  Bound by latency: 5 us, 14 for 8 environments of
-// 2048 steps (each a few threads' walk over its flags).
+// A launch ahead of the others, which are bound by what they read once per tile of theirs, not once per pair.  Bound by latency: 5 us
+// (8 environments of 2048 steps in one workgroup, in runs of 16 steps: 14).
 // Blocks below `spans`: 2^lgn environments at a time, the threads of an environment taking a run of steps each; the others: the table.
 __global__ __launch_bounds__(1024) void k_attn_prepare(AttnArgs g, int spans, int lgn) {
     __shared__ int last[1024];
@@ -1402,8 +1402,9 @@ int launch_attn_fwd(const morlax_attn_dims& d, const void* q, const void* k, con
     if (saved) attn_carve_saved(g, d, saved);
     if (!first) g.lo = nullptr;
     if (first || g.B) {
+        // up to 16 environments to a workgroup, whose flags lie next to each other; of few with long histories fewer, for runs of two steps
         int lgn = 0;
-        while (lgn < 4 && 1 << lgn < d.N) ++lgn;
+        while (lgn < 4 && 1 << lgn < d.N && (1024 >> lgn >= d.S || d.N >> lgn > 64)) ++lgn;
         const int64_t spans = first ? cdiv(d.N, 1 << lgn) : 0;
         k_attn_prepare<<<dim3((uint32_t)(spans + (g.B ? cdiv((int64_t)g.H * g.reach, 1024) : 0))), 1024, 0, s>>>(g, (int)spans, lgn);
     }

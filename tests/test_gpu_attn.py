@@ -187,6 +187,8 @@ LONG = [
     (600, 600, 1, 4, 1, 128, 8, 600, 0.01),       # keys only
     (130, 1300, 2, 2, 2, 33, 0, 1025, 0.0),       # forward only, no bias, rows that are no whole pieces
     (1030, 1031, 1, 1, 1, 8, 3, 1000, 0.3),       # most chunks see nothing
+    (3, 1100, 20, 1, 1, 8, 2, 1100, 0.004),       # long histories of some environments, of more
+    (2, 1100, 70, 1, 1, 8, 2, 1100, 0.004),
     (1100, 1150, 1, 1, 1, 64, 40, 1150, 0.0),     # a chunk's end among the distances that have buckets of their own
 ]
 
