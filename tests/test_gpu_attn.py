@@ -358,3 +358,54 @@ def test_without_the_bias_gradient():
     binding.attn_bwd(d, x["q"], x["k"], x["v"], x["bias"], x["edges"], x["first"], y, saved, x["dy"], *g, None, ws)
     for t, k in zip(g, ("q", "k", "v")):
         assert torch.equal(t.cpu().reshape(want[k].shape), want[k]), k
+
+
+@pytest.mark.parametrize("kind", ["float32", "bfloat16"])
+def test_chunks_whose_scores_are_minus_infinity(kind):
+    """Distances from five on are not looked at: most chunks of a cut walk are there and hold nothing of a row."""
+    torch = _torch()
+    c = make(getattr(torch, kind), 1100, 1100, 1, 2, 1, 16, 4, 1100, 0.0)
+    c["bias"][:, 3] = -float("inf")
+    want, bound = define(c)
+    got = run(c)
+    for k in ("y", "v"):
+        near(got[k], want[k], torch.nan_to_num(bound[k], 1e-4, 1e-4).clamp(max=1e-4 if kind == "float32" else 1e-3), k)
+    assert all(bool(torch.isfinite(got[k].float()).all()) for k in got) and bool((got["bias"][:, 3] == 0).all())
+
+
+@pytest.mark.parametrize("shape", [(1100, 1100, 1, 2, 1, 40, 17, 1100, 0.002), (70, 192, 3, 3, 3, 16, 16, 192, 0.02)], ids=["cut", "whole"])
+def test_replays(shape):
+    """Forward and backward recorded once, replayed with changed inputs and other calls between, against the calls themselves."""
+    from paper_2603_09237_amd import binding
+    torch = _torch()
+    c = make(torch.bfloat16, *shape)
+    T, S, N, H, KV, D, B = (c[k] for k in ("T", "S", "N", "H", "KV", "D", "B"))
+    d = binding.AttnDims(T, S, N, H, KV, D, B, c["window"], 1)
+    x = {k: c[k].cuda() for k in ("q", "k", "v", "dy", "bias", "edges", "first")}
+    out = {k: torch.empty_like(v) for k, v in x.items() if k in ("q", "k", "v", "bias")}
+    out["y"], saved = torch.empty_like(x["q"]), torch.empty(binding.attn_saved_bytes(d), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(max(binding.attn_workspace_bytes(d), binding.attn_workspace_bytes(d, True)), dtype=torch.uint8, device="cuda")
+
+    def work():
+        binding.attn_fwd(d, x["q"], x["k"], x["v"], x["bias"], x["edges"], x["first"], out["y"], saved, ws)
+        binding.attn_bwd(d, x["q"], x["k"], x["v"], x["bias"], x["edges"], x["first"], out["y"], saved, x["dy"], out["q"], out["k"], out["v"], out["bias"], ws)
+
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        work()
+    stream.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        work()
+    for i in range(4):
+        x["k"].normal_()
+        x["first"].copy_(torch.rand(S, N, device="cuda") < 0.01)
+        work()
+        want = {k: v.clone() for k, v in out.items()}
+        for t in (*out.values(), saved, ws):
+            t.fill_(3)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for k in out:
+            assert torch.equal(out[k], want[k]), (i, k)
