@@ -399,9 +399,13 @@ int morlax_attn_bwd(const morlax_attn_dims* dims, const void* q, const void* k, 
  *   of the environments and their slots, all but the one in slot 0, which serves again; where the slot of p has no page, one is taken from the
  *   queue, in the order of the environments, while there are any (pages that went back in this call serve from the next one on);
  *   length[n] = p + 1, slot[n] = the row p lies in, page * page_rows + p % page_rows, or -1 where no page was left.
+ * Where the queue has run dry a page may come late: in the middle of its rows, or after a round of the slots in which its slot had none.  The rows that
+ * were to hold the steps before then hold what others left.  morlax_cache_pages_since keeps since [N, slots] as well, the step of the episode from which
+ * on a slot's page holds its steps: for the slot of p that is p where the episode begins, where the slot had no page, and where since_in says a
+ * step beyond p; everything else stays.  Where a table holds no page, since_in may be anything.
  * A table entry outside [0, pages) is none.  queue [pages] is a ring of free pages, state = {where it begins, how many there are}.
- * length_in, length, slot [N], table_in, table [N, slots], queue_in, queue [pages], state_in, state [2], all int32.  Each output but slot may be its
- * own input.  Lengths must stay below 2^31 - 1.
+ * length_in, length, slot [N], table_in, table, since_in, since [N, slots], queue_in, queue [pages], state_in, state [2], all int32.  Each output but
+ * slot may be its own input.  Lengths must stay below 2^31 - 1.
  * Limits: page a power of two up to 4096, pages * page < 2^31, N * slots <= 2^30, N <= 2^24. */
 typedef struct {
     int32_t N, page, slots, pages;
@@ -411,10 +415,16 @@ int64_t morlax_pages_workspace_bytes(const morlax_pages_dims* dims);
 int morlax_cache_pages(const morlax_pages_dims* dims, const uint8_t* first, const int32_t* length_in, const int32_t* table_in,
                        const int32_t* queue_in, const int32_t* state_in, int32_t* length, int32_t* table, int32_t* queue, int32_t* state,
                        int32_t* slot, void* ws, int64_t ws_bytes, void* stream);
+int morlax_cache_pages_since(const morlax_pages_dims* dims, const uint8_t* first, const int32_t* length_in, const int32_t* table_in,
+                             const int32_t* queue_in, const int32_t* state_in, const int32_t* since_in, int32_t* length, int32_t* table,
+                             int32_t* queue, int32_t* state, int32_t* since, int32_t* slot, void* ws, int64_t ws_bytes, void* stream);
 
 /* Attention of one new step of every environment over such a cache, the new step's key and value put there first: morlax_attn_fwd's formula
  * with p = length[n] - 1 (the step itself) and the steps of the episode that the window holds.  An environment of length <= 0 gets zeros and
  * leaves the cache alone; a step whose slot has no page is seen by itself, but not kept; steps whose slots have none are not seen.
+ * morlax_attn_step takes every row of a page for the step whose place it is: it goes with books whose queue never runs dry (pages >= N * slots is
+ * always enough).  morlax_attn_step_since does not see, nor read, steps before the one that since [N, slots] names for their slot (as
+ * morlax_cache_pages_since leaves it): with a page that came late, the steps before it, which were not kept.
  *   q, y [N, heads * head_dim] (strides q_n, y_n), k, v [N, kv_heads * head_dim] (stride k_n both), table [N, slots], length [N] int32 (as
  *   morlax_cache_pages leaves them), k_cache, v_cache [pages, page, kv_heads, head_dim] of the given type.
  * No two environments may hold the same page.
@@ -431,6 +441,9 @@ int64_t morlax_attn_step_workspace_bytes(const morlax_cache_dims* dims);
 int morlax_attn_step(const morlax_cache_dims* dims, const void* q, const void* k, const void* v, const float* bias, const int32_t* edges,
                      const int32_t* table, const int32_t* length, void* k_cache, void* v_cache, void* y, void* ws, int64_t ws_bytes,
                      void* stream);
+int morlax_attn_step_since(const morlax_cache_dims* dims, const void* q, const void* k, const void* v, const float* bias, const int32_t* edges,
+                           const int32_t* table, const int32_t* length, const int32_t* since, void* k_cache, void* v_cache, void* y, void* ws,
+                           int64_t ws_bytes, void* stream);
 
 /* What stands between two blocks of a stack, row by row:
  *   n = u / sqrt(mean(u^2) + eps) w_post,   y = x + scale sigmoid(gate) n,   h = y / sqrt(mean(y^2) + eps) w_pre

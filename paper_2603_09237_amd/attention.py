@@ -39,6 +39,7 @@ class Cache:
         ints = dict(dtype=torch.int32, device=device)
         self.length = torch.zeros(N, **ints)                 # steps of the present episode; below zero: no environment in this row
         self.table = torch.full((N, slots), -1, **ints)
+        self.since = torch.zeros(N, slots, **ints)           # the step from which on a slot's page is the episode's (a page may come late)
         self.queue = torch.arange(pages, **ints)             # free pages, a ring
         self.state = torch.tensor([0, pages], **ints)        # where it begins, how many there are
         self.slot = torch.empty(N, **ints)                   # the row of the last step, -1 where no page was left
@@ -83,7 +84,8 @@ class AttentionBlock(Block):
         return (torch.zeros(0, N, 2 * self.E, dtype=self.dtype, device=self.dev), torch.zeros(0, N, dtype=torch.uint8, device=self.dev))
 
     def new_cache(self, N, page=32, pages=None):
-        """An empty cache of N environments.  pages: enough for every environment to hold a whole window, where it is not given."""
+        """An empty cache of N environments.  pages: enough for every environment to hold a whole window, where it is not given; with fewer, steps
+        for which none was left are not kept."""
         slots = -(-self.window // page)
         return Cache(N, self.KV, self.hd, page, slots, N * slots if pages is None else pages, self.dtype, self.dev)
 
@@ -178,12 +180,13 @@ class AttentionBlock(Block):
         proj, yc, u = self._buf("act.proj", N, self.L), self._buf("act.yc", N, self.D), self._buf("act.u", N, self.width)
         y, nxt = (torch.empty(N, self.width, dtype=self.dtype, device=self.dev) for _ in range(2))
         binding.cache_pages(c.dims, first, c.length, c.table, c.queue, c.state, c.length, c.table, c.queue, c.state, c.slot,
-                            self._scratch(binding.pages_workspace_bytes(c.dims), "act.pages"))
+                            self._scratch(binding.pages_workspace_bytes(c.dims), "act.pages"), since_in=c.since, since=c.since)
         self._project("in", N, h, index, proj, "act.ws")
         qs, k, v, gate = self._slices(proj)
         d = binding.CacheDims(N, self.H, self.KV, self.hd, self.buckets, self.window, c.page, c.slots, c.pages, self.kind, q_n=self.L, k_n=self.L,
                               y_n=self.D)
-        binding.attn_step(d, qs, k, v, q.get("bias"), self.edges, c.table, c.length, c.k, c.v, yc, self._scratch(binding.attn_step_workspace_bytes(d), "act.ws"))
+        binding.attn_step(d, qs, k, v, q.get("bias"), self.edges, c.table, c.length, c.k, c.v, yc, self._scratch(binding.attn_step_workspace_bytes(d), "act.ws"),
+                          since=c.since)
         self._project("out", N, yc, index, u, "act.ws")
         binding.norm_fwd(self._norm(N), x, u, gate, q["scale"], q["w_post"], q["w_pre"], y, nxt)
         return y, nxt

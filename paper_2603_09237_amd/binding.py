@@ -115,7 +115,7 @@ EXPORTS = ("morlax_create", "morlax_destroy", "morlax_last_error", "morlax_hpara
            "morlax_conv_workspace_bytes", "morlax_conv_fwd", "morlax_conv_bwd", "morlax_scan_saved_bytes",
            "morlax_scan_workspace_bytes", "morlax_scan_fwd", "morlax_scan_bwd", "morlax_memory_step",
            "morlax_attn_saved_bytes", "morlax_attn_workspace_bytes", "morlax_attn_fwd", "morlax_attn_bwd", "morlax_pages_workspace_bytes",
-           "morlax_cache_pages", "morlax_attn_step_workspace_bytes", "morlax_attn_step", "morlax_norm_workspace_bytes",
+           "morlax_cache_pages", "morlax_cache_pages_since", "morlax_attn_step_workspace_bytes", "morlax_attn_step", "morlax_attn_step_since", "morlax_norm_workspace_bytes",
            "morlax_norm_fwd", "morlax_norm_bwd")
 
 GEMM_KINDS = ("fwd_first", "fwd_hidden", "dx_hidden", "dw_hidden", "dw_first", "fwd_fused")
@@ -201,10 +201,13 @@ def load():
     lib.morlax_attn_fwd.argtypes = [tp] + [vp] * 9 + [i64, vp]
     lib.morlax_attn_bwd.argtypes = [tp] + [vp] * 14 + [i64, vp]
     lib.morlax_cache_pages.argtypes = [pp] + [vp] * 11 + [i64, vp]
+    lib.morlax_cache_pages_since.argtypes = [pp] + [vp] * 13 + [i64, vp]
     lib.morlax_attn_step.argtypes = [kp] + [vp] * 11 + [i64, vp]
+    lib.morlax_attn_step_since.argtypes = [kp] + [vp] * 12 + [i64, vp]
     lib.morlax_norm_fwd.argtypes = [np_] + [vp] * 9
     lib.morlax_norm_bwd.argtypes = [np_] + [vp] * 15 + [i64, vp]
-    for name in ("morlax_attn_fwd", "morlax_attn_bwd", "morlax_cache_pages", "morlax_attn_step", "morlax_norm_fwd", "morlax_norm_bwd"):
+    for name in ("morlax_attn_fwd", "morlax_attn_bwd", "morlax_cache_pages", "morlax_cache_pages_since", "morlax_attn_step", "morlax_attn_step_since",
+                 "morlax_norm_fwd", "morlax_norm_bwd"):
         getattr(lib, name).restype = C.c_int
     lib.morlax_profile_begin.argtypes = [vp]
     lib.morlax_profile_begin.restype = C.c_int
@@ -522,10 +525,16 @@ def pages_workspace_bytes(dims):
     return _size(load().morlax_pages_workspace_bytes(C.byref(dims)))
 
 
-def cache_pages(dims, first, length_in, table_in, queue_in, state_in, length, table, queue, state, slot, ws, stream=None):
-    """morlax_cache_pages: one step's bookkeeping of a paged cache."""
-    _call(load().morlax_cache_pages, C.byref(dims), _ptr(first), _ptr(length_in), _ptr(table_in), _ptr(queue_in), _ptr(state_in), _ptr(length),
-          _ptr(table), _ptr(queue), _ptr(state), _ptr(slot), _ptr(ws), _nbytes(ws), stream if stream is not None else _stream())
+def cache_pages(dims, first, length_in, table_in, queue_in, state_in, length, table, queue, state, slot, ws, stream=None, since_in=None, since=None):
+    """morlax_cache_pages: one step's bookkeeping of a paged cache; with since_in and since morlax_cache_pages_since, which a cache whose pages may
+    run out needs."""
+    stream = stream if stream is not None else _stream()
+    if since_in is None and since is None:
+        _call(load().morlax_cache_pages, C.byref(dims), _ptr(first), _ptr(length_in), _ptr(table_in), _ptr(queue_in), _ptr(state_in), _ptr(length),
+              _ptr(table), _ptr(queue), _ptr(state), _ptr(slot), _ptr(ws), _nbytes(ws), stream)
+    else:
+        _call(load().morlax_cache_pages_since, C.byref(dims), _ptr(first), _ptr(length_in), _ptr(table_in), _ptr(queue_in), _ptr(state_in),
+              _ptr(since_in), _ptr(length), _ptr(table), _ptr(queue), _ptr(state), _ptr(since), _ptr(slot), _ptr(ws), _nbytes(ws), stream)
 
 
 def attn_step_workspace_bytes(dims):
@@ -533,10 +542,16 @@ def attn_step_workspace_bytes(dims):
     return _size(load().morlax_attn_step_workspace_bytes(C.byref(dims)))
 
 
-def attn_step(dims, q, k, v, bias, edges, table, length, k_cache, v_cache, y, ws, stream=None):
-    """morlax_attn_step: attention of one new step of every environment over the paged cache that it is put into."""
-    _call(load().morlax_attn_step, C.byref(dims), _ptr(q), _ptr(k), _ptr(v), _ptr(bias), _ptr(edges), _ptr(table), _ptr(length), _ptr(k_cache),
-          _ptr(v_cache), _ptr(y), _ptr(ws), _nbytes(ws), stream if stream is not None else _stream())
+def attn_step(dims, q, k, v, bias, edges, table, length, k_cache, v_cache, y, ws, stream=None, since=None):
+    """morlax_attn_step: attention of one new step of every environment over the paged cache that it is put into; with since (of cache_pages)
+    morlax_attn_step_since, which a cache whose pages may run out needs."""
+    stream = stream if stream is not None else _stream()
+    if since is None:
+        _call(load().morlax_attn_step, C.byref(dims), _ptr(q), _ptr(k), _ptr(v), _ptr(bias), _ptr(edges), _ptr(table), _ptr(length), _ptr(k_cache),
+              _ptr(v_cache), _ptr(y), _ptr(ws), _nbytes(ws), stream)
+    else:
+        _call(load().morlax_attn_step_since, C.byref(dims), _ptr(q), _ptr(k), _ptr(v), _ptr(bias), _ptr(edges), _ptr(table), _ptr(length),
+              _ptr(since), _ptr(k_cache), _ptr(v_cache), _ptr(y), _ptr(ws), _nbytes(ws), stream)
 
 
 def norm_workspace_bytes(dims):

@@ -7,12 +7,16 @@ static int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // Integers only: a workgroup owns 64 environments (256 of many), one a thread of its first waves; ranks (whose turn at the queue it is, where a page that goes back lies) are
 // sums over the workgroups before, which a first launch leaves where there is more than one.  Bound by latency for a few thousand environments
 // (two dependent launches of some microseconds), by the copy of the tables where they go into other buffers.
+// A page may come late, in the middle of its rows or a round of the slots later: the rows that its steps have not reached hold what others left.  `since`
+// says from which step on a slot's page is the episode's: the step that took it.
 #define PAGES_THREADS 256
 #define PAGES_AHEAD 8
 struct PagesArgs {
     const uint8_t* first;
     const int32_t *length_in, *table_in, *queue_in, *state_in;
     int32_t *length, *table, *queue, *state, *slot;
+    const int32_t* since_in;
+    int32_t* since;    // [N, slots], or NULL
     int2* sums;        // of each workgroup: environments that need a page, pages that go back
     int32_t* was;      // [2] the state before
     int N, lgp, lge, slots, pages, blocks;  // lge: 2^lge environments to a workgroup
@@ -110,7 +114,7 @@ __global__ __launch_bounds__(PAGES_THREADS) void k_pages_count(PagesArgs g) {
 __global__ __launch_bounds__(PAGES_THREADS) void k_pages_apply(PagesArgs g) {
     __shared__ int2 part[4], sums[4], totals[4];
     __shared__ int wave_back[4];
-    __shared__ int32_t column[PAGES_THREADS], entry[PAGES_THREADS];
+    __shared__ int32_t column[PAGES_THREADS], entry[PAGES_THREADS], from[PAGES_THREADS];
     const int n0 = (int)blockIdx.x << g.lge, wave = threadIdx.x >> 6;
     const int n = (int)threadIdx.x < 1 << g.lge ? n0 + (int)threadIdx.x : g.N;
     const int here = g.N - n0 < 1 << g.lge ? g.N - n0 : 1 << g.lge, cells = here * g.slots;
@@ -157,6 +161,11 @@ __global__ __launch_bounds__(PAGES_THREADS) void k_pages_apply(PagesArgs g) {
     column[threadIdx.x] = !e.live ? -1 : e.begins ? -2 - e.column : e.column;  // (an episode that begins is at slot 0)
     entry[threadIdx.x] = e.entry;
     if ((threadIdx.x & 63) == 0) wave_back[wave] = own.y;
+    if (g.since && e.live) {  // (a step that is still to come kept nothing)
+        const int old = g.since_in[(int64_t)n * g.slots + e.column], now = e.begins | e.needs | (old > e.at) ? e.at : old;
+        from[threadIdx.x] = now;
+        if (g.since == g.since_in) g.since[(int64_t)n * g.slots + e.column] = now;
+    }
     if (n < g.N) {
         const bool has = (uint32_t)e.entry < (uint32_t)g.pages;
         g.length[n] = e.live ? e.at + 1 : e.at;
@@ -168,11 +177,11 @@ __global__ __launch_bounds__(PAGES_THREADS) void k_pages_apply(PagesArgs g) {
     wave_gives(g, n, e.begins, [&](int at, int page) { g.queue[ring(base + at)] = page; });
     __syncthreads();  // (the rows of episodes that begin have been read: they may be written)
     if (g.table != g.table_in) {
-        const int32_t* from = g.table_in + (int64_t)n0 * g.slots;
+        const int32_t* old = g.table_in + (int64_t)n0 * g.slots;
         int32_t* to = g.table + (int64_t)n0 * g.slots;
-        auto put = [&](int i, int old) {
+        auto put = [&](int i, int was) {
             const int r = (int)g.by_slots.quotient((uint32_t)i), j = i - r * g.slots, c = column[r], now = entry[r];
-            to[i] = c <= -2 ? (j == 0 ? now : -1) : c == j ? now : old;
+            to[i] = c <= -2 ? (j == 0 ? now : -1) : c == j ? now : was;
         };
 #pragma unroll
         for (int i = 0; i < PAGES_AHEAD; ++i) {
@@ -180,12 +189,18 @@ __global__ __launch_bounds__(PAGES_THREADS) void k_pages_apply(PagesArgs g) {
             if (at < cells) put(at, ahead[i]);
         }
 #pragma unroll 4
-        for (int i = threadIdx.x + PAGES_AHEAD * PAGES_THREADS; i < cells; i += PAGES_THREADS) put(i, from[i]);
+        for (int i = threadIdx.x + PAGES_AHEAD * PAGES_THREADS; i < cells; i += PAGES_THREADS) put(i, old[i]);
     } else if (n < g.N && e.live) {
         if (e.begins)
             for (int j = 1; j < g.slots; ++j) g.table[(int64_t)n * g.slots + j] = -1;
         g.table[(int64_t)n * g.slots + e.column] = e.entry;
     }
+    if (g.since != g.since_in)
+        for (int i = threadIdx.x; i < cells; i += PAGES_THREADS) {
+            const int r = (int)g.by_slots.quotient((uint32_t)i), j = i - r * g.slots, c = column[r];
+            const int64_t at = (int64_t)n0 * g.slots + i;
+            g.since[at] = j == (c <= -2 ? 0 : c) ? from[r] : g.since_in[at];
+        }
     if (g.queue != g.queue_in) {  // what no page went back to
         const int64_t per = ((int64_t)g.pages + g.blocks - 1) / g.blocks, i0 = blockIdx.x * per, i1 = i0 + per < g.pages ? i0 + per : g.pages;
         const int tail0 = ring((int64_t)head + count);
@@ -210,7 +225,7 @@ __global__ __launch_bounds__(PAGES_THREADS) void k_pages_apply(PagesArgs g) {
 struct StepArgs {
     const void *q, *k, *v;
     const float* bias;
-    const int32_t *edges, *table, *length;
+    const int32_t *edges, *table, *length, *since;
     void *k_cache, *v_cache, *y;
     float* part_o;   // [N, H, splits, D]
     float2* part_m;  // [N, H, splits] maximum (in units of log2) and sum
@@ -236,7 +251,9 @@ __device__ inline float group_sum(float v) {
     return v;
 }
 
-template <int DP, int GQ, bool WHOLE>
+// SINCE: pages may have come late, and steps from before are not seen (an instance of its own, as the word of each key costs 1024 environments 1 us of
+// 54 in bf16, 4 of 122 in fp32).
+template <int DP, int GQ, bool WHOLE, bool SINCE>
 __global__ __launch_bounds__(256) void k_attn_step(StepArgs g) {
     typedef float T;
     constexpr int VE = 4, LPK = DP / VE, KPW = 64 / LPK, STRIDE = 4 * KPW * STEP_U;
@@ -260,7 +277,7 @@ __global__ __launch_bounds__(256) void k_attn_step(StepArgs g) {
     const uint32_t count = pos - begin + 1, per = ((count + g.splits - 1) / g.splits + 4 * KPW - 1) / (4 * KPW) * (4 * KPW);  // (sums pass 2^31)
     const int64_t s0 = begin + (int64_t)split * per;
     const int s1 = s0 + per < pos + 1 ? (int)(s0 + per) : pos + 1;
-    const int32_t* table = g.table + (int64_t)n * g.slots;
+    const int32_t *table = g.table + (int64_t)n * g.slots, *since = SINCE ? g.since + (int64_t)n * g.slots : nullptr;
     const int64_t row = (int64_t)g.KV * g.D;
     const T *kn = reinterpret_cast<const T*>(g.k) + (int64_t)n * g.k_n + (int64_t)kv * g.D, *vn = reinterpret_cast<const T*>(g.v) + (int64_t)n * g.k_n + (int64_t)kv * g.D;
     T *kc = reinterpret_cast<T*>(g.k_cache) + (int64_t)kv * g.D, *vc = reinterpret_cast<T*>(g.v_cache) + (int64_t)kv * g.D;
@@ -305,12 +322,14 @@ __global__ __launch_bounds__(256) void k_attn_step(StepArgs g) {
         for (int e = 0; e < VE; ++e) o[i][e] = 0.f;
     }
     const int my = wave * KPW + key;
-    int id[STEP_U];
+    int id[STEP_U], from[SINCE ? STEP_U : 1];
     auto look = [&](int64_t at) {
 #pragma unroll
         for (int u = 0; u < STEP_U; ++u) {
             const int64_t s = at + my + u * 4 * KPW;
-            id[u] = table[slot_of((int)(s < s1 ? s : s1 - 1))];
+            const int j = slot_of((int)(s < s1 ? s : s1 - 1));
+            id[u] = table[j];
+            if (SINCE) from[u] = since[j];
         }
     };
     if (s0 < s1) look(s0);
@@ -321,7 +340,7 @@ __global__ __launch_bounds__(256) void k_attn_step(StepArgs g) {
         for (int u = 0; u < STEP_U; ++u) {
             const int64_t s = at + my + u * 4 * KPW;
             const bool now = s == pos;
-            in[u] = (s < s1) & (now | ((uint32_t)id[u] < (uint32_t)g.pages));
+            in[u] = (s < s1) & (now | (((uint32_t)id[u] < (uint32_t)g.pages) & (!SINCE || s >= from[SINCE ? u : 0])));
             const int64_t off = (((int64_t)id[u] << g.lgp) + ((int)s & in_page)) * row;
             const bool held = in[u] & !now;
             kp[u].load(held ? kc + off : kn, d, g.D);
@@ -438,7 +457,7 @@ struct StepLds {
     typedef Tile<bf16_t, DP> L;
     static constexpr int V = 32 * L::PITCH, OUT = 16 * (DP + 1) * 4, WAVE = V > OUT ? V : OUT;  // (a wave's output lies where its values lay)
 };
-template <int DP, bool WHOLE>
+template <int DP, bool WHOLE, bool SINCE>
 __global__ __launch_bounds__(256, DP == 128 ? 2 : 3) void k_attn_step_bf16(StepArgs g) {
     typedef bf16_t T;
     typedef Tile<T, DP> L;
@@ -461,7 +480,7 @@ __global__ __launch_bounds__(256, DP == 128 ? 2 : 3) void k_attn_step_bf16(StepA
     const uint32_t count = pos - begin + 1, per = ((count + g.splits - 1) / g.splits + 127) / 128 * 128;  // a whole number of keys of the four waves
     const int64_t s0 = begin + (int64_t)split * per;
     const int s1 = s0 + per < pos + 1 ? (int)(s0 + per) : pos + 1;
-    const int32_t* table = g.table + (int64_t)n * g.slots;
+    const int32_t *table = g.table + (int64_t)n * g.slots, *since = SINCE ? g.since + (int64_t)n * g.slots : nullptr;
     const int64_t row = (int64_t)g.KV * g.D;
     const T *kn = reinterpret_cast<const T*>(g.k) + (int64_t)n * g.k_n + (int64_t)kv * g.D, *vn = reinterpret_cast<const T*>(g.v) + (int64_t)n * g.k_n + (int64_t)kv * g.D;
     T *kc = reinterpret_cast<T*>(g.k_cache) + (int64_t)kv * g.D, *vc = reinterpret_cast<T*>(g.v_cache) + (int64_t)kv * g.D;
@@ -506,14 +525,16 @@ __global__ __launch_bounds__(256, DP == 128 ? 2 : 3) void k_attn_step_bf16(StepA
     float4_t o[1][L::NB];
 #pragma unroll
     for (int dt = 0; dt < L::NB; ++dt) o[0][dt] = float4_t{0.f, 0.f, 0.f, 0.f};
-    int id[2];
+    int id[2], from[SINCE ? 2 : 1];
     RowPiece<T, WHOLE> kp[2][L::KS], vp[2][L::KS];
     bool in[2];
     auto look = [&](int64_t at) {
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             const int64_t s = at + 16 * x + a;
-            id[x] = table[slot_of((int)(s < s1 ? s : s1 - 1))];
+            const int j = slot_of((int)(s < s1 ? s : s1 - 1));
+            id[x] = table[j];
+            if (SINCE) from[x] = since[j];
         }
     };
     auto request = [&](int64_t at) {  // (its pages' numbers are there) and the next one's numbers
@@ -521,7 +542,7 @@ __global__ __launch_bounds__(256, DP == 128 ? 2 : 3) void k_attn_step_bf16(StepA
         for (int x = 0; x < 2; ++x) {
             const int64_t s = at + 16 * x + a;
             const bool now = s == pos;
-            in[x] = (s < s1) & (now | ((uint32_t)id[x] < (uint32_t)g.pages));
+            in[x] = (s < s1) & (now | (((uint32_t)id[x] < (uint32_t)g.pages) & (!SINCE || s >= from[SINCE ? x : 0])));
             const bool held = in[x] & !now;
             const int64_t off = (((int64_t)id[x] << g.lgp) + ((int)s & in_page)) * row;
             const T *pk = held ? kc + off : kn, *pv = held ? vc + off : vn;
@@ -694,10 +715,12 @@ int64_t pages_ws_bytes(const morlax_pages_dims& d) {
     return pages_carve(g, d, nullptr);
 }
 void launch_cache_pages(const morlax_pages_dims& d, const uint8_t* first, const int32_t* length_in, const int32_t* table_in, const int32_t* queue_in,
-                        const int32_t* state_in, int32_t* length, int32_t* table, int32_t* queue, int32_t* state, int32_t* slot, void* ws, hipStream_t s) {
+                        const int32_t* state_in, const int32_t* since_in, int32_t* length, int32_t* table, int32_t* queue, int32_t* state, int32_t* since,
+                        int32_t* slot, void* ws, hipStream_t s) {
     PagesArgs g = {};
     g.first = first; g.length_in = length_in; g.table_in = table_in; g.queue_in = queue_in; g.state_in = state_in;
     g.length = length; g.table = table; g.queue = queue; g.state = state; g.slot = slot;
+    g.since_in = since_in; g.since = since;
     pages_carve(g, d, ws);
     if (g.blocks > 1) k_pages_count<<<dim3(g.blocks), PAGES_THREADS, 0, s>>>(g);
     k_pages_apply<<<dim3(g.blocks), PAGES_THREADS, 0, s>>>(g);
@@ -725,17 +748,21 @@ int64_t attn_step_ws_bytes(const morlax_cache_dims& d) {
     StepArgs g = {};
     return step_carve(g, d, nullptr);
 }
-template <typename T, int DP, bool WHOLE>
-static void step_pass(const StepArgs& g, hipStream_t s) {
+template <typename T, int DP, bool WHOLE, bool SINCE>
+static void step_run(const StepArgs& g, hipStream_t s) {
     const dim3 grid((uint32_t)((int64_t)g.splits * g.chunks * g.KV * g.N));
-    if constexpr (sizeof(T) == 2) k_attn_step_bf16<DP, WHOLE><<<grid, 256, 0, s>>>(g);
+    if constexpr (sizeof(T) == 2) k_attn_step_bf16<DP, WHOLE, SINCE><<<grid, 256, 0, s>>>(g);
     else switch (heads_of_workgroup(g.H / g.KV)) {
-        case 1: k_attn_step<DP, 1, WHOLE><<<grid, 256, 0, s>>>(g); break;
-        case 2: k_attn_step<DP, 2, WHOLE><<<grid, 256, 0, s>>>(g); break;
-        case 4: k_attn_step<DP, 4, WHOLE><<<grid, 256, 0, s>>>(g); break;
-        default: k_attn_step<DP, 8, WHOLE><<<grid, 256, 0, s>>>(g);
+        case 1: k_attn_step<DP, 1, WHOLE, SINCE><<<grid, 256, 0, s>>>(g); break;
+        case 2: k_attn_step<DP, 2, WHOLE, SINCE><<<grid, 256, 0, s>>>(g); break;
+        case 4: k_attn_step<DP, 4, WHOLE, SINCE><<<grid, 256, 0, s>>>(g); break;
+        default: k_attn_step<DP, 8, WHOLE, SINCE><<<grid, 256, 0, s>>>(g);
     }
     if (g.splits > 1) k_attn_join<T><<<dim3((uint32_t)((int64_t)g.N * g.H)), 256, 0, s>>>(g);
+}
+template <typename T, int DP, bool WHOLE>
+static void step_pass(const StepArgs& g, hipStream_t s) {
+    g.since ? step_run<T, DP, WHOLE, true>(g, s) : step_run<T, DP, WHOLE, false>(g, s);
 }
 template <typename T>
 static void step_pick(const StepArgs& g, hipStream_t s) {
@@ -744,10 +771,10 @@ static void step_pick(const StepArgs& g, hipStream_t s) {
     else g.whole ? step_pass<T, 128, true>(g, s) : step_pass<T, 128, false>(g, s);
 }
 void launch_attn_step(const morlax_cache_dims& d, const void* q, const void* k, const void* v, const float* bias, const int32_t* edges,
-                      const int32_t* table, const int32_t* length, void* k_cache, void* v_cache, void* y, void* ws, hipStream_t s) {
+                      const int32_t* table, const int32_t* length, const int32_t* since, void* k_cache, void* v_cache, void* y, void* ws, hipStream_t s) {
     StepArgs g = {};
     step_carve(g, d, ws);
-    g.q = q; g.k = k; g.v = v; g.bias = bias; g.edges = edges; g.table = table; g.length = length; g.k_cache = k_cache; g.v_cache = v_cache; g.y = y;
+    g.q = q; g.k = k; g.v = v; g.bias = bias; g.edges = edges; g.table = table; g.length = length; g.since = since; g.k_cache = k_cache; g.v_cache = v_cache; g.y = y;
     if (d.dtype) step_pick<bf16_t>(g, s);
     else step_pick<float>(g, s);
 }

@@ -793,26 +793,39 @@ extern "C" int64_t morlax_pages_workspace_bytes(const morlax_pages_dims* d) {
     if (check_pages(d, "morlax_pages_workspace_bytes") != MORLAX_OK) return -1;
     return pages_ws_bytes(*d);
 }
-extern "C" int morlax_cache_pages(const morlax_pages_dims* dims, const uint8_t* first, const int32_t* length_in, const int32_t* table_in,
-                                  const int32_t* queue_in, const int32_t* state_in, int32_t* length, int32_t* table, int32_t* queue,
-                                  int32_t* state, int32_t* slot, void* ws, int64_t ws_bytes, void* stream) {
-    const char* who = "morlax_cache_pages";
+static int cache_pages(const morlax_pages_dims* dims, const uint8_t* first, const int32_t* length_in, const int32_t* table_in, const int32_t* queue_in,
+                       const int32_t* state_in, const int32_t* since_in, int32_t* length, int32_t* table, int32_t* queue, int32_t* state, int32_t* since,
+                       int32_t* slot, bool late, void* ws, int64_t ws_bytes, void* stream, const char* who) {
     const int rc = check_pages(dims, who);
     if (rc != MORLAX_OK) return rc;
     REQ(length_in, who); REQ(table_in, who); REQ(queue_in, who); REQ(state_in, who);
     REQ(length, who); REQ(table, who); REQ(queue, who); REQ(state, who); REQ(slot, who);
-    const void* in[] = {length_in, table_in, queue_in, state_in};
-    const void* out[] = {length, table, queue, state, slot};
-    for (int o = 0; o < 5; ++o) {
-        for (int i = 0; i < 4; ++i)
+    if (late) { REQ(since_in, who); REQ(since, who); }
+    const void* in[] = {length_in, table_in, queue_in, state_in, since_in};
+    const void* out[] = {length, table, queue, state, since, slot};
+    for (int o = 0; o < 6; ++o) {
+        if (!out[o]) continue;
+        for (int i = 0; i < 5; ++i)
             if (o != i && out[o] == in[i]) return fail(MORLAX_ERR_SHAPE, "%s: an output is another's input", who);
         for (int i = 0; i < o; ++i)
             if (out[o] == out[i]) return fail(MORLAX_ERR_SHAPE, "%s: two outputs are the same", who);
         if (out[o] == first) return fail(MORLAX_ERR_SHAPE, "%s: an output is its input", who);
     }
     WS(ws, ws_bytes, pages_ws_bytes(*dims), who);
-    launch_cache_pages(*dims, first, length_in, table_in, queue_in, state_in, length, table, queue, state, slot, ws, (hipStream_t)stream);
+    launch_cache_pages(*dims, first, length_in, table_in, queue_in, state_in, since_in, length, table, queue, state, since, slot, ws, (hipStream_t)stream);
     return finish(who);
+}
+extern "C" int morlax_cache_pages(const morlax_pages_dims* dims, const uint8_t* first, const int32_t* length_in, const int32_t* table_in,
+                                  const int32_t* queue_in, const int32_t* state_in, int32_t* length, int32_t* table, int32_t* queue,
+                                  int32_t* state, int32_t* slot, void* ws, int64_t ws_bytes, void* stream) {
+    return cache_pages(dims, first, length_in, table_in, queue_in, state_in, nullptr, length, table, queue, state, nullptr, slot, false, ws, ws_bytes, stream,
+                       "morlax_cache_pages");
+}
+extern "C" int morlax_cache_pages_since(const morlax_pages_dims* dims, const uint8_t* first, const int32_t* length_in, const int32_t* table_in,
+                                        const int32_t* queue_in, const int32_t* state_in, const int32_t* since_in, int32_t* length, int32_t* table,
+                                        int32_t* queue, int32_t* state, int32_t* since, int32_t* slot, void* ws, int64_t ws_bytes, void* stream) {
+    return cache_pages(dims, first, length_in, table_in, queue_in, state_in, since_in, length, table, queue, state, since, slot, true, ws, ws_bytes, stream,
+                       "morlax_cache_pages_since");
 }
 
 static int check_cache(const morlax_cache_dims* d, const char* who) {
@@ -830,21 +843,31 @@ extern "C" int64_t morlax_attn_step_workspace_bytes(const morlax_cache_dims* d) 
     if (check_cache(d, "morlax_attn_step_workspace_bytes") != MORLAX_OK) return -1;
     return attn_step_ws_bytes(*d);
 }
-extern "C" int morlax_attn_step(const morlax_cache_dims* dims, const void* q, const void* k, const void* v, const float* bias, const int32_t* edges,
-                                const int32_t* table, const int32_t* length, void* k_cache, void* v_cache, void* y, void* ws,
-                                int64_t ws_bytes, void* stream) {
-    const char* who = "morlax_attn_step";
+static int attn_step(const morlax_cache_dims* dims, const void* q, const void* k, const void* v, const float* bias, const int32_t* edges,
+                     const int32_t* table, const int32_t* length, const int32_t* since, bool late, void* k_cache, void* v_cache, void* y, void* ws,
+                     int64_t ws_bytes, void* stream, const char* who) {
     int rc = check_cache(dims, who);
     if (rc != MORLAX_OK) return rc;
     STRIDED(q, dims->dtype, who); STRIDED(k, dims->dtype, who); STRIDED(v, dims->dtype, who); STRIDED(y, dims->dtype, who);
     if ((rc = check_bias(dims->buckets, bias, edges, who)) != MORLAX_OK) return rc;
     REQ(table, who); REQ(length, who); REQ(k_cache, who); REQ(v_cache, who);
+    if (late) REQ(since, who);
     if (y == q || y == k || y == v || k_cache == v_cache || k_cache == y || v_cache == y || k_cache == k || v_cache == v || k_cache == v ||
         v_cache == k || k_cache == q || v_cache == q)
         return fail(MORLAX_ERR_SHAPE, "%s: an output is its input", who);
     WS(ws, ws_bytes, attn_step_ws_bytes(*dims), who);
-    launch_attn_step(*dims, q, k, v, bias, edges, table, length, k_cache, v_cache, y, ws, (hipStream_t)stream);
+    launch_attn_step(*dims, q, k, v, bias, edges, table, length, since, k_cache, v_cache, y, ws, (hipStream_t)stream);
     return finish(who);
+}
+extern "C" int morlax_attn_step(const morlax_cache_dims* dims, const void* q, const void* k, const void* v, const float* bias, const int32_t* edges,
+                                const int32_t* table, const int32_t* length, void* k_cache, void* v_cache, void* y, void* ws,
+                                int64_t ws_bytes, void* stream) {
+    return attn_step(dims, q, k, v, bias, edges, table, length, nullptr, false, k_cache, v_cache, y, ws, ws_bytes, stream, "morlax_attn_step");
+}
+extern "C" int morlax_attn_step_since(const morlax_cache_dims* dims, const void* q, const void* k, const void* v, const float* bias,
+                                      const int32_t* edges, const int32_t* table, const int32_t* length, const int32_t* since, void* k_cache,
+                                      void* v_cache, void* y, void* ws, int64_t ws_bytes, void* stream) {
+    return attn_step(dims, q, k, v, bias, edges, table, length, since, true, k_cache, v_cache, y, ws, ws_bytes, stream, "morlax_attn_step_since");
 }
 
 static int check_norm(const morlax_norm_dims* d, const char* who) {

@@ -149,10 +149,11 @@ int launch_attn_bwd(const morlax_attn_dims& d, const void* q, const void* k, con
 
 int64_t pages_ws_bytes(const morlax_pages_dims& d);
 void launch_cache_pages(const morlax_pages_dims& d, const uint8_t* first, const int32_t* length_in, const int32_t* table_in, const int32_t* queue_in,
-                        const int32_t* state_in, int32_t* length, int32_t* table, int32_t* queue, int32_t* state, int32_t* slot, void* ws, hipStream_t s);
+                        const int32_t* state_in, const int32_t* since_in, int32_t* length, int32_t* table, int32_t* queue, int32_t* state, int32_t* since,
+                        int32_t* slot, void* ws, hipStream_t s);
 int64_t attn_step_ws_bytes(const morlax_cache_dims& d);
 void launch_attn_step(const morlax_cache_dims& d, const void* q, const void* k, const void* v, const float* bias, const int32_t* edges,
-                      const int32_t* table, const int32_t* length, void* k_cache, void* v_cache, void* y, void* ws, hipStream_t s);
+                      const int32_t* table, const int32_t* length, const int32_t* since, void* k_cache, void* v_cache, void* y, void* ws, hipStream_t s);
 
 int64_t norm_ws_bytes(const morlax_norm_dims& d);
 void launch_norm_fwd(const morlax_norm_dims& d, const void* x, const void* u, const void* gate, const float* scale, const float* w_post,
