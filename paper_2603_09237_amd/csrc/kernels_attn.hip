@@ -880,7 +880,10 @@ __global__ __launch_bounds__(ATTN_THREADS, attn_waves(1, sizeof(T), DP)) void k_
                 if (!see || !tainted(kb + (int64_t)k * g.k_t, g.D)) continue;
                 const float nan = __builtin_nanf("");
                 if (g.part)
-                    for (int i = 0; i < g.B; ++i) bins[i * LANES] = nan;
+                    for (int i = 0; i < g.B; ++i) {  // the buckets of the distances that the row sees, 0 .. p - lo
+                        const int from = i && g.edges[i] > 0 ? g.edges[i] : 0;
+                        if (from <= p[b] - lo[b] && (i + 1 == g.B || from < g.edges[i + 1])) bins[i * LANES] = nan;
+                    }
 #pragma unroll
                 for (int dt = 0; dt < L::NB; ++dt) o[b][dt] = float4_t{nan, nan, nan, nan};
             }
