@@ -1342,6 +1342,10 @@ static int run_kernel(void (*kernel)(AttnArgs), AttnArgs& g, int64_t total, int 
     g.by_tiles = row_div(g.tiles);
     g.by_own = row_div(g.own ? (int)g.own : 1);
     g.by_heads = row_div((int)(rests / g.N));
+    if (g.before + total * chunks >= 1 << 24) {  // (a launch holds fewer than 2^32 threads: what else there is to do in one of its own)
+        kernel<<<dim3(g.before), ATTN_THREADS, lds, s>>>(g);
+        g.before = 0;
+    }
     kernel<<<dim3((uint32_t)(g.before + total * chunks)), ATTN_THREADS, lds, s>>>(g);
     return 0;
 }
