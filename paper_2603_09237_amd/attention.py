@@ -101,6 +101,7 @@ class AttentionBlock(Block):
         _check("state[0]", state[0], (past, N, 2 * self.E), self.dtype)
         _check("state[1]", state[1], (past, N), torch.uint8)
         S, q = past + T, self.p
+        self.saved_for = None  # (from here on buffers change)
         rows = self._buf("index", T * N, dtype=torch.int32)
         rows.view(T, N).copy_(index)
         proj, yc, u = self._buf("proj", S, N, self.L), self._buf("yc", T, N, self.D), self._buf("u", T, N, self.width)
@@ -122,7 +123,8 @@ class AttentionBlock(Block):
         keep = min(self.window - 1, S)
         marks = torch.zeros(keep, N, dtype=torch.uint8, device=self.dev) if begins is None else begins[S - keep:].to(torch.uint8, copy=True)
         after = (proj[S - keep:, :, self.D:self.D + 2 * self.E].contiguous() if keep else self.new_state(N)[0], marks)
-        self.saved_for = (x, h, begins, past, _versions(x, h, begins)) if train else None
+        if train:
+            self.saved_for = (x, h, begins, past, _versions(x, h, begins))
         return y, nxt, after
 
     def backward(self, dy, dh):

@@ -149,6 +149,7 @@ class MemoryBlock(Block):
         _check_first(first, (T, N))
         self._check_memory("state", state, N)
         q = self.p
+        self.saved_for = None  # (from here on buffers change)
         rows = self._buf("index", T * N, dtype=torch.int32)
         rows.view(T, N).copy_(index)
         proj, xc, yc = self._buf("proj", T, N, self.L), self._buf("xc", T, N, self.C), self._buf("yc", T, N, self.D)
@@ -162,7 +163,6 @@ class MemoryBlock(Block):
         binding.scan_fwd(scan, xs, b, c, dt, z, q["a_log"], q["d_skip"], q["dt_bias"], first, state[1], yc, after[1], saved,
                          self._scratch(binding.scan_workspace_bytes(scan)))
         self._project("out", T * N, yc, rows, y)
-        self.saved_for = None
         if train:  # (the state may move on before the backward; x and first are the caller's to leave alone until then)
             kept = self._buf("state", *state[0].shape)
             kept.copy_(state[0])
