@@ -175,20 +175,23 @@ class AttentionBlock(Block):
         _check("index", index, (N,), torch.int32)
         _check_first(first, (N,))
         q, c = self.p, cache
-        _check("the cache's length", c.length, (N,), torch.int32)
-        _check("the cache's table", c.table, (N, c.slots), torch.int32)
+        for name, shape in (("length", (N,)), ("table", (N, c.slots)), ("since", (N, c.slots)), ("queue", (c.pages,)), ("state", (2,)), ("slot", (N,))):
+            _check("the cache's " + name, getattr(c, name), shape, torch.int32)
         for t in (c.k, c.v):
             _check("the cache's keys and values", t, (c.pages, c.page, self.KV, self.hd), self.dtype)
+        if c.slots * c.page < self.window:
+            raise ValueError(f"the cache holds {c.slots * c.page} steps of an environment, fewer than the window of {self.window}")
         proj, yc, u = self._buf("act.proj", N, self.L), self._buf("act.yc", N, self.D), self._buf("act.u", N, self.width)
         y, nxt = (torch.empty(N, self.width, dtype=self.dtype, device=self.dev) for _ in range(2))
-        binding.cache_pages(c.dims, first, c.length, c.table, c.queue, c.state, c.length, c.table, c.queue, c.state, c.slot,
-                            self._scratch(binding.pages_workspace_bytes(c.dims), "act.pages"), since_in=c.since, since=c.since)
-        self._project("in", N, h, index, proj, "act.ws")
-        qs, k, v, gate = self._slices(proj)
         d = binding.CacheDims(N, self.H, self.KV, self.hd, self.buckets, self.window, c.page, c.slots, c.pages, self.kind, q_n=self.L, k_n=self.L,
                               y_n=self.D)
-        binding.attn_step(d, qs, k, v, q.get("bias"), self.edges, c.table, c.length, c.k, c.v, yc, self._scratch(binding.attn_step_workspace_bytes(d), "act.ws"),
-                          since=c.since)
+        need, books = binding.attn_step_workspace_bytes(d), self._scratch(binding.pages_workspace_bytes(c.dims), "act.pages")
+        self._project("in", N, h, index, proj, "act.ws")
+        qs, k, v, gate = self._slices(proj)
+        # (what can be refused has been: a cache whose books have moved on without the step would lack it)
+        binding.cache_pages(c.dims, first, c.length, c.table, c.queue, c.state, c.length, c.table, c.queue, c.state, c.slot, books, since_in=c.since,
+                            since=c.since)
+        binding.attn_step(d, qs, k, v, q.get("bias"), self.edges, c.table, c.length, c.k, c.v, yc, self._scratch(need, "act.ws"), since=c.since)
         self._project("out", N, yc, index, u, "act.ws")
         binding.norm_fwd(self._norm(N), x, u, gate, q["scale"], q["w_post"], q["w_pre"], y, nxt)
         return y, nxt
