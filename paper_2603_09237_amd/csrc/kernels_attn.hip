@@ -873,20 +873,27 @@ __global__ __launch_bounds__(ATTN_THREADS, attn_waves(1, sizeof(T), DP)) void k_
         __syncthreads();
     }
     if (*flag) {  // a row that sees such a key has a score that is not finite: no part of its gradient is
-        for (int k = k_begin; k < k_end; ++k)
 #pragma unroll
-            for (int b = 0; b < QB; ++b) {
-                const bool see = (t[b] >= 0) & (k >= lo[b]) & (k <= p[b]);
-                if (!see || !tainted(kb + (int64_t)k * g.k_t, g.D)) continue;
-                const float nan = __builtin_nanf("");
-                if (g.part)
-                    for (int i = 0; i < g.B; ++i) {  // the buckets of the distances that the row sees, 0 .. p - lo
-                        const int from = i && g.edges[i] > 0 ? g.edges[i] : 0;
-                        if (from <= p[b] - lo[b] && (i + 1 == g.B || from < g.edges[i + 1])) bins[i * LANES] = nan;
-                    }
+        for (int b = 0; b < QB; ++b) {
+            bool hit = false;
+            for (int k = k_begin; k < k_end; ++k) hit |= (t[b] >= 0) & (k >= lo[b]) & (k <= p[b]) && tainted(kb + (int64_t)k * g.k_t, g.D);
+            if (!hit) continue;
+            const float nan = __builtin_nanf("");
 #pragma unroll
-                for (int dt = 0; dt < L::NB; ++dt) o[b][dt] = float4_t{nan, nan, nan, nan};
+            for (int dt = 0; dt < L::NB; ++dt) o[b][dt] = float4_t{nan, nan, nan, nan};
+            if (!g.part) continue;
+            for (int d = 0, end = p[b] - lo[b] + 1; d < end;) {  // the buckets of the distances that it sees, each by its first one
+                const int i = g.bucket[d];
+                bins[(i < 0 ? 0 : i >= g.B ? g.B - 1 : i) * LANES] = nan;
+                int next = end;
+                while (next - d > 1) {
+                    const int mid = d + (next - d) / 2;
+                    if (g.bucket[mid] > i) next = mid;
+                    else d = mid;
+                }
+                d = next;
             }
+        }
     }
     if (g.cut_q.chunks > 1) {
         if (threadIdx.x == 0) g.cut_q.there[R.chunk * g.total + (R.n * (g.H >> g.lgp) + (R.h0 >> g.lgp)) * g.tiles + R.r0 / BQ] = k_begin < k_end;
