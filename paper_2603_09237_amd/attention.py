@@ -66,6 +66,7 @@ class AttentionBlock(Block):
         self.p.update({"scale": torch.full((width,), 0.5, device=self.dev), "w_post": torch.ones(width, device=self.dev),
                        "w_pre": torch.ones(width, device=self.dev)})
         self._ready()
+        self.acting = (None,)  # sizes of the last step's cache, what the entry points make of them
 
     def _dims(self, T, S, N):
         return binding.AttnDims(T, S, N, self.H, self.KV, self.hd, self.buckets, self.window, self.kind, q_t=N * self.L, q_n=self.L, k_t=N * self.L,
@@ -183,9 +184,13 @@ class AttentionBlock(Block):
             raise ValueError(f"the cache holds {c.slots * c.page} steps of an environment, fewer than the window of {self.window}")
         proj, yc, u = self._buf("act.proj", N, self.L), self._buf("act.yc", N, self.D), self._buf("act.u", N, self.width)
         y, nxt = (torch.empty(N, self.width, dtype=self.dtype, device=self.dev) for _ in range(2))
-        d = binding.CacheDims(N, self.H, self.KV, self.hd, self.buckets, self.window, c.page, c.slots, c.pages, self.kind, q_n=self.L, k_n=self.L,
-                              y_n=self.D)
-        need, books = binding.attn_step_workspace_bytes(d), self._scratch(binding.pages_workspace_bytes(c.dims), "act.pages")
+        sizes = (N, c.page, c.slots, c.pages)
+        if self.acting[0] != sizes:  # (asking again for every step: 2 of 52 us of 16 environments)
+            d = binding.CacheDims(N, self.H, self.KV, self.hd, self.buckets, self.window, c.page, c.slots, c.pages, self.kind, q_n=self.L, k_n=self.L,
+                                  y_n=self.D)
+            self.acting = (sizes, d, binding.attn_step_workspace_bytes(d), binding.pages_workspace_bytes(c.dims))
+        _, d, need, books = self.acting
+        books = self._scratch(books, "act.pages")
         self._project("in", N, h, index, proj, "act.ws")
         qs, k, v, gate = self._slices(proj)
         # (what can be refused has been: a cache whose books have moved on without the step would lack it)
