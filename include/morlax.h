@@ -447,7 +447,8 @@ int morlax_attn_step_since(const morlax_cache_dims* dims, const void* q, const v
 
 /* What stands between two blocks of a stack, row by row:
  *   n = u / sqrt(mean(u^2) + eps) w_post,   y = x + scale sigmoid(gate) n,   h = y / sqrt(mean(y^2) + eps) w_pre
- * x: the sum of the blocks so far, u: the last block's output, h: the next block's input (of y before its rounding).
+ * x: the sum of the blocks so far, u: the last block's output, h: the next block's input (of y before its rounding).  Squares are summed in fp32: of a row
+ * whose mean square lies beyond 3.4e38, n (or h) is zeros.
  *   x, y [rows, width] (row stride ld_x), u (ld_u), gate (ld_g), h (ld_h) of the given type; scale, w_post, w_pre [width] fp32.
  *   NULL: gate: no gate; scale: 1; w_post: u is not normed, n = u; w_pre: no h (h NULL too); u: y = x (gate, scale and w_post NULL too; y may
  *   be NULL then).  y may be x.

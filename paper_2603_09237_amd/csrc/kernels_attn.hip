@@ -348,7 +348,8 @@ struct Table {
 // ---- forward ------------------------------------------------------------------------------------------------------------
 // Four waves, 16 rows each (32: see below), and a tile of 64 keys at a time, the next one's requests on their way.  Bound by instructions, and by what is
 // read and written where there are few keys to a row: 1024 environments, 64 of 128 steps, 8 heads of 64 to 2 of keys 72 us (201 MB; 2.8 TB/s);
-// for training 512 of them, 8 heads of keys 48 us (235 MB, 4.9 TB/s); 2048 x 8 x 8 heads of 128 190 us (137 GF of parts, 0.7 PFLOP/s).
+// for training 512 of them, 8 heads of keys 48 us (235 MB, 4.9 TB/s); 2048 x 8 x 8 heads of 128 190 us (137 GF of parts, 0.7 PFLOP/s; 30 to 43 of this
+// variant's 256 registers lie in memory).
 template <typename T, int DP, int QB>
 struct FwdLds {
     static constexpr int ROOM = ATTN_ROOM(64 * QB, ATTN_K), NR = (ROOM + ATTN_THREADS - 1) / ATTN_THREADS;
@@ -963,7 +964,8 @@ __device__ inline void add_bias(const AttnArgs& g, float* part) {
 // ---- backward, keys: dk and dv ---------------------------------------------------------------------------------------------------
 // Four waves, 16 keys each in registers, and a tile of 64 rows of queries at a time.  512 environments, 64 of 128 steps, 8 heads of 64: 110 us (330 MB,
 // 3.0 TB/s: one tile to a workgroup, most of its time is the wait for it; workgroups that go on to a next tile and ask for it ahead 133, three waves
-// a SIMD 140); 2048 x 8 x 8 heads of 128 to 2 of keys: 345 us (206 GF of parts, 0.6 PFLOP/s): two waves a SIMD, half of the time in waits.
+// a SIMD 140); 2048 x 8 x 8 heads of 128 to 2 of keys: 345 us (206 GF of parts, 0.6 PFLOP/s): two waves a SIMD, 14 to 46 registers in memory, half of the
+// time in waits.
 template <typename T, int DP, int KB>
 struct DkvLds {
     static constexpr int ROOM = ATTN_ROOM(ATTN_K, 64 * KB), NR = (ROOM + ATTN_THREADS - 1) / ATTN_THREADS;

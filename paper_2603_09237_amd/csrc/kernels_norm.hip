@@ -4,7 +4,9 @@
 //   dx = dY,  dscale = sum dY sigmoid(gate) n,  dgate = dY scale n s (1 - s),  dn = dY scale s,
 //   dw_post = sum dn u r_u,  du = r_u (w_post dn) - u r_u^3 mean(w_post dn u),  dw_pre = sum dh y r_y.
 // Bound: HBM.  Every tensor goes through registers once: a row lies along the lanes of a wave, 16 bytes each (or of up to sixteen waves), the
-// backward computes n, y and both means again, and a workgroup keeps the three columns' sums of its rows in registers until its last row.
+// backward computes n, y and both means again, and a workgroup keeps the three columns' sums of its rows in registers until its last row.  65536 rows of
+// 512 with gradients: bf16 182 us (4.3 and 5.1 TB/s), fp32 128 and 224 (5.2, 4.8).  Rows that take sixteen waves have 128 registers for all of that and
+// 58 to 72 of their backward's in memory: 4096 rows of 8192 bf16 281 us, 1.9 TB/s, of the same elements in rows of 4096 132.
 #include "mlp_device.h"
 #include "pieces.h"
 
